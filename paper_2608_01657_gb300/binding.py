@@ -34,7 +34,9 @@ EXPORTED = ("ps_workspace_bytes", "ps_create", "ps_step", "ps_step_host", "ps_st
             "ps_step_host_wait", "ps_stats", "ps_clear_status",
             "ps_reset", "ps_destroy", "ps_status_string", "ps_export_state", "ps_export_history",
             "ps_export_ghost", "ps_set_stage_timing", "ps_get_stage_times", "ps_cached_prefix",
-            "ps_cached_prefix_noalloc", "ps_uses_graph", "ps_set_graph")
+            "ps_cached_prefix_noalloc", "ps_uses_graph", "ps_set_graph", "ps_step_blocks",
+            "ps_kv_workspace_bytes", "ps_kv_create", "ps_kv_destroy", "ps_kv_append", "ps_kv_plan",
+            "ps_kv_attention", "ps_kv_copy", "ps_kv_fork", "ps_kv_release", "ps_kv_compact")
 PS_NUM_STAGES = 11
 STAGE_NAMES = ("validate", "hash_lookup", "claims", "grant_instep", "meter", "touch_gate", "select",
                "take_lists", "evict", "insert", "commit")
@@ -85,6 +87,40 @@ class PsStateView(C.Structure):
         "resident", "key", "group", "contract", "prefix", "klass", "stamp", "acc", "freq", "s3q", "s3seq",
         "balances")] + [("t_prev", C.c_int64), ("step", C.c_uint64), ("s3_ctr", C.c_uint64),
                         ("ghost_ctr", C.c_uint64)]
+
+
+# -- the operators on KV pages (include/prefixshield_kv.h) --------------------
+PS_KV_BF16, PS_KV_F16 = 0, 1
+PS_KV_MAX_HEAD_DIM, PS_KV_MAX_HEADS = 128, 1024
+
+
+class PsKvConfig(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int64) for n in (
+        "num_pages", "first_page", "layer_stride", "page_stride", "token_stride", "head_stride")] + [
+        (n, C.c_int32) for n in ("num_layers", "page_size", "num_kv_heads", "num_q_heads", "head_dim", "dtype",
+                                 "max_requests", "max_tokens", "max_row_pages", "pad0")]
+
+
+class PsKvAppend(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out")] + [
+        (n, C.c_int64 * 2) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")] + [
+        (n, C.c_void_p) for n in ("slots", "positions", "rope", "q_weight", "k_weight")] + [("eps", C.c_float)] + [
+        (n, C.c_int32) for n in ("num_tokens", "rope_rows", "rope_dim", "rope_interleaved", "pad0")]
+
+
+class PsKvBatch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_offsets", "kv_lens", "tables", "group_offsets")] + [
+        ("table_stride", C.c_int64)] + [(n, C.c_int32) for n in ("num_requests", "num_groups", "num_tokens", "causal")]
+
+
+class PsKvAttention(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + [
+        (n, C.c_int64 * 2) for n in ("q_stride", "out_stride")] + [("scale", C.c_float), ("pad0", C.c_int32)]
+
+
+class PsKvRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("tables", "lens", "held")] + [
+        ("table_stride", C.c_int64), ("num_rows", C.c_int32), ("pad0", C.c_int32)]
 
 
 _lib = None
@@ -139,6 +175,28 @@ def load():
     L.ps_uses_graph.argtypes = [C.c_void_p]
     L.ps_set_graph.restype = i32
     L.ps_set_graph.argtypes = [C.c_void_p, i32]
+    L.ps_step_blocks.restype = i32
+    L.ps_step_blocks.argtypes = [vp, vp, i32, vp, vp, i64, vp, vp]
+    L.ps_kv_workspace_bytes.restype = sz
+    L.ps_kv_workspace_bytes.argtypes = [C.POINTER(PsKvConfig)]
+    L.ps_kv_create.restype = i32
+    L.ps_kv_create.argtypes = [C.POINTER(vp), C.POINTER(PsKvConfig), vp, sz, vp]
+    L.ps_kv_destroy.restype = None
+    L.ps_kv_destroy.argtypes = [vp]
+    L.ps_kv_append.restype = i32
+    L.ps_kv_append.argtypes = [vp, vp, i32, C.POINTER(PsKvAppend), vp]
+    L.ps_kv_plan.restype = i32
+    L.ps_kv_plan.argtypes = [vp, vp, C.POINTER(PsKvBatch), vp]
+    L.ps_kv_attention.restype = i32
+    L.ps_kv_attention.argtypes = [vp, vp, i32, C.POINTER(PsKvAttention)]
+    L.ps_kv_copy.restype = i32
+    L.ps_kv_copy.argtypes = [vp, vp, i32, vp, vp, vp]
+    L.ps_kv_fork.restype = i32
+    L.ps_kv_fork.argtypes = [vp, vp, i32, vp, vp, vp, C.POINTER(PsKvRows), vp, vp, vp]
+    L.ps_kv_release.restype = i32
+    L.ps_kv_release.argtypes = [vp, vp, i32, vp, C.POINTER(PsKvRows), vp, vp]
+    L.ps_kv_compact.restype = i32
+    L.ps_kv_compact.argtypes = [vp, vp, C.POINTER(PsKvRows), vp, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -275,6 +333,25 @@ class Cache:
         R = int(groups.shape[0])
         return load().ps_cached_prefix_noalloc(self._h, _stream_ptr(stream), R, _ptr(groups), _ptr(offsets),
                                                _ptr(tokens), _ptr(out), _ptr(status))
+
+    def step_blocks(self, groups, tables, counts=None, status=None, stream=None):
+        """The block ids of every request of the last step (device tensors):
+        row i of ``tables`` [R, width] receives request i's leading resident
+        blocks, ``counts`` [R] their number.  ``groups``: the step's.  Call it
+        right after the step.  Returns counts."""
+        import torch
+        R = int(groups.shape[0])
+        if counts is None:
+            counts = torch.empty(max(1, R), dtype=torch.int32, device=groups.device)
+        if tables.dim() != 2 or tables.shape[0] < R or tables.dtype != torch.int32 or tables.stride(1) != 1:
+            raise ValueError("tables must be int32 [requests, blocks] with contiguous rows")
+        if tables.stride(0) != tables.shape[1]:
+            raise ValueError("tables must have rows of exactly their width")
+        rc = load().ps_step_blocks(self._h, _stream_ptr(stream), R, _ptr(groups), _ptr(tables), tables.shape[1],
+                                   _ptr(counts), _ptr(status))
+        if rc != PS_OK:
+            raise RuntimeError(f"ps_step_blocks failed ({rc})")
+        return counts
 
     def step_host(self, now: int, groups, offsets, tokens, contracts=None, prefixes=None, stream=None,
                   out: Optional[dict] = None) -> dict:

@@ -1,0 +1,226 @@
+// Internal declarations of the operators on KV pages (prefixshield_kv.h).
+//
+// Every kernel receives its arguments by value: the pool's description, the
+// carved scratch pointers and the call's own pointers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "prefixshield_kv.h"
+
+namespace pskv {
+
+// ---- the pool ----------------------------------------------------------------
+struct Pool {
+  char* k;
+  char* v;
+  int64_t num_pages, first_page;
+  int64_t layer_stride, page_stride, token_stride, head_stride;  // elements
+  int32_t num_layers, page_size, page_log2, kv_heads, q_heads, ratio, head_dim, dtype;
+};
+
+// ---- a batch's plan ------------------------------------------------------------
+// The work of a batch is a list of tiles: some query rows against a range of
+// keys.  The rows of a tile are (token, query head of one kv head) pairs, token
+// major, so a tile is run once for each kv head.  A tile's keys are cut into
+// units; unit u of the whole list (tile major, then kv head, then unit) belongs
+// to CTA c with floor(U c / C) <= u < floor(U (c + 1) / C): every CTA gets the
+// same number of units whatever the lengths are.  A (tile, head) that several
+// CTAs work on, or whose rows also have a shared prefix, leaves partial results
+// (a running maximum, a sum, an unnormalized output) that k_attend_join puts
+// together in a fixed order.
+struct __align__(32) Tile {
+  int32_t tok0;   // token of row 0 of the tile's item (a request or a group)
+  int32_t row0;   // the tile's first row within the item
+  int32_t nrows;  // rows of the tile
+  int32_t kv0;    // keys [kv0, kv1) of table row req
+  int32_t kv1;
+  int32_t req;
+  int32_t ctx;    // row r of the item sees the keys < ctx + 1 + r / ratio
+  int32_t sidx;   // index of (tile, head 0) among the shared (tile, head)s, -1: not shared
+};
+
+struct ReqRec {
+  int32_t tile0;   // first tile of the request's own keys
+  int32_t list;    // and the list it is in
+  int32_t ptile0;  // first tile of its group's shared prefix, -1: none
+  int32_t plist;
+  int32_t prow0;   // the request's first row among the group's
+};
+
+constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen05)
+__host__ __device__ constexpr int tile_rows(int list) { return list ? 128 : 16; }
+__host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 64; }
+constexpr int kNoMask = 1 << 30;
+
+struct PlanHdr {
+  int32_t status;       // PS_OK, or why the plan is empty
+  int32_t join;         // some rows have partial results
+  int32_t ntiles[kLists];
+  int32_t nshared[kLists];  // shared (tile, head)s
+  int32_t ctas[kLists];     // C, 0 without tiles
+  int64_t units[kLists];    // U
+};
+
+// Requests of more rows than this fill tiles of their own; a prefix shared by
+// smaller ones is read once for all of them.
+constexpr int kShareRows = 64;
+constexpr int kMaxSms = 160;
+
+// Tiles of one list, and (tile, kv head)s per kv head whose rows have a shared
+// prefix, for at most R requests of at most 'rows' rows in all.  An item (a
+// request's own keys, or a group's prefix; at most R of each) of x rows has at
+// most 1 + x / H tiles.
+struct PlanBounds {
+  int64_t tiles, shared;
+};
+inline PlanBounds plan_bounds(int list, int64_t R, int64_t rows) {
+  const int H = tile_rows(list);
+  const int64_t srows = rows < R * kShareRows ? rows : R * kShareRows;
+  return {2 * (R + rows / H) + 2, 2 * (R + srows / H) + 2};
+}
+
+// The CTA of unit u: the largest c with floor(U c / C) <= u.
+__host__ __device__ __forceinline__ int cta_of(int64_t u, int64_t U, int64_t C) {
+  return (int)(((u + 1) * C - 1) / U);
+}
+
+struct Plan {
+  PlanHdr* hdr;
+  ReqRec* req;        // [max_requests]
+  int32_t* tok_req;   // [max_tokens] request of a token
+  int32_t* group;     // [max_requests] group of a request
+  int32_t* grp_tile;  // [max_requests] first tile of a group's shared prefix, -1: none
+  int32_t* grp_list;  // [max_requests] and the list it is in
+  int32_t* common;    // [max_requests] leading pages in common with the group's first request
+  int32_t* bad;       // [max_requests]
+  Tile* tiles[kLists];
+  int64_t* ucum[kLists];      // [tiles + 1] units before a tile, all heads
+  int32_t* cta_tile[kLists];  // [C] tile of a CTA's first unit
+  float* part_o[kLists];      // [slots][tile rows][head_dim]
+  float2* part_ml[kLists];    // [slots][tile rows] (maximum, sum), base 2
+  int32_t max_tiles[kLists], max_slots[kLists], max_ctas[kLists];
+};
+
+// The partial-result slot of a (tile, head)'s part that CTA c computed.  A CTA
+// leaves at most two partial results of (tile, head)s that are not shared: of
+// the one it continues and of the one it leaves unfinished.  Along the list of
+// shared (tile, head)s neither the index i nor c ever decreases and one of them
+// grows from each part to the next, so i + c is a slot of its own.
+__host__ __device__ __forceinline__ int part_slot(int sidx, int head, int c, bool continued, int C) {
+  return sidx >= 0 ? 2 * C + sidx + head + c : 2 * c + (continued ? 0 : 1);
+}
+
+struct Batch {
+  const int32_t *q_offsets, *kv_lens, *tables, *group_offsets;
+  int64_t table_stride;
+  int32_t num_requests, num_groups, num_tokens, causal, row_pages;
+};
+
+// ---- page calls -----------------------------------------------------------------
+struct PageHdr {
+  int32_t done;    // CTAs of the scan that have finished (back to 0 after each call)
+  int32_t status;  // verdict of the call
+  int32_t live;    // pages in use (compact)
+  int32_t free_pages;
+};
+constexpr int kScanThreads = 256;
+constexpr int kMaxChunks = 1024;  // chunks of the reference array: one CTA each
+
+struct PageScratch {
+  PageHdr* hdr;
+  int32_t* chunk_cnt;   // [chunks] free (fork) or used (compact) pages of a chunk
+  int32_t* chunk_base;  // [chunks] those of the chunks before it
+  int32_t* list;        // [private pages] fork: each chunk's free pages; compact: holes
+  int32_t* movers;      // [private pages]
+  int32_t* inv;         // [private pages] rank of a mover
+  int32_t* mover_refs;  // [private pages]
+  int32_t* need;        // [max_requests]
+  int32_t* start;       // [max_requests]
+  int32_t* bad;         // [max_requests]
+  int32_t chunks, chunk_size;
+};
+
+// ---- device helpers ----------------------------------------------------------------
+__device__ __forceinline__ void set_error(int32_t* status, int32_t code) {
+  if (status) atomicMin(status, code);
+}
+// Wait for the kernels before this one, then let the next one be scheduled (its
+// CTAs wait here in turn).  Every kernel of these operators starts with it.
+__device__ __forceinline__ void chain() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <typename T>
+struct Num;
+template <>
+struct Num<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 unpack(uint32_t x) {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+};
+template <>
+struct Num<__half> {
+  static __device__ __forceinline__ float2 unpack(uint32_t x) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&x));
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+};
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// ---- host ------------------------------------------------------------------------
+// Launch that may be scheduled while its predecessor finishes (see chain()).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+inline int32_t status_of(cudaError_t e) { return e == cudaSuccess ? PS_OK : PS_ERR_CUDA; }
+
+int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& a, int32_t* status, int nsm, cudaStream_t st);
+int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* status, cudaStream_t st);
+int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& a,
+                         cudaStream_t st);
+int32_t launch_copy(const Pool& p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* status, int nsm,
+                    cudaStream_t st);
+int32_t launch_fork(const Pool& p, const PageScratch& w, int32_t n, const int32_t* parents, const int32_t* children,
+                    const int32_t* room, const ps_kv_rows_t& rows, int32_t row_pages, const int32_t* refs_in,
+                    int32_t* refs_out, int32_t* status, int nsm, cudaStream_t st);
+int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_kv_rows_t& rows, int32_t row_pages,
+                       int32_t* refs, int32_t* status, cudaStream_t st);
+int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, int32_t row_pages,
+                       const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
+                       int32_t* status, int nsm, cudaStream_t st);
+// Kernel attributes (shared-memory opt-ins) and the CTAs of each attention list
+// that the current device holds at once.
+int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]);
+
+}  // namespace pskv

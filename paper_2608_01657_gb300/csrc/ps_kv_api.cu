@@ -1,0 +1,252 @@
+// C ABI of the operators on KV pages (declared in include/prefixshield_kv.h).
+//
+// Host side only: argument checks, the workspace layout and the handle.
+#include <new>
+
+#include "ps_kv.cuh"
+
+using namespace pskv;
+
+struct ps_kv {
+  Pool pool;
+  Plan plan;
+  PageScratch pages;
+  Batch batch;
+  bool planned;
+  int32_t nsm, max_requests, max_tokens, max_row_pages;
+};
+
+namespace {
+
+inline cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool good_strides(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && s[0] % 8 == 0 && s[1] % 8 == 0; }
+
+bool check_config(const ps_kv_config_t* c) {
+  if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return false;
+  if (c->num_pages < 1 || c->num_pages > (1ll << 30) || c->first_page < 0 || c->first_page > c->num_pages) return false;
+  const int32_t ps = c->page_size;
+  if (ps != 2 && ps != 4 && ps != 8 && ps != 16 && ps != 32 && ps != 64) return false;
+  for (int64_t s : {c->layer_stride, c->page_stride, c->token_stride, c->head_stride})
+    if (s < 0 || s % 8 != 0) return false;
+  if (c->num_layers < 1 || c->num_kv_heads < 1 || c->num_q_heads < c->num_kv_heads ||
+      c->num_q_heads > PS_KV_MAX_HEADS || c->num_q_heads % c->num_kv_heads != 0)
+    return false;
+  if (c->head_dim < 8 || c->head_dim > PS_KV_MAX_HEAD_DIM || c->head_dim % 8 != 0) return false;
+  if (c->dtype != PS_KV_BF16 && c->dtype != PS_KV_F16) return false;
+  if (c->max_requests < 1 || c->max_requests > PS_MAX_REQUESTS_PER_STEP) return false;
+  if (c->max_tokens < 1 || c->max_tokens > (1 << 22) || (int64_t)c->max_tokens * c->num_q_heads >= (1ll << 31))
+    return false;
+  if (c->max_row_pages < 1 || (int64_t)c->max_row_pages * ps >= (1ll << 30)) return false;
+  return true;
+}
+
+Pool make_pool(const ps_kv_config_t& c) {
+  Pool p{};
+  p.k = static_cast<char*>(c.k);
+  p.v = static_cast<char*>(c.v);
+  p.num_pages = c.num_pages; p.first_page = c.first_page;
+  p.layer_stride = c.layer_stride; p.page_stride = c.page_stride;
+  p.token_stride = c.token_stride; p.head_stride = c.head_stride;
+  p.num_layers = c.num_layers; p.page_size = c.page_size;
+  while ((1 << p.page_log2) < c.page_size) ++p.page_log2;
+  p.kv_heads = c.num_kv_heads; p.q_heads = c.num_q_heads; p.ratio = c.num_q_heads / c.num_kv_heads;
+  p.head_dim = c.head_dim; p.dtype = c.dtype;
+  return p;
+}
+
+struct Carver {
+  char* base;
+  size_t off = 0;
+  template <typename T>
+  T* take(size_t count) {
+    off = (off + 255) / 256 * 256;
+    T* p = base ? reinterpret_cast<T*>(base + off) : nullptr;
+    off += sizeof(T) * (count ? count : 1);
+    return p;
+  }
+};
+
+// The workspace: sizes with base == nullptr, pointers otherwise.  Every region
+// starts on a 256-byte boundary.  The page header comes first (cleared once).
+size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Plan* plan, PageScratch* pages) {
+  Carver cv{base};
+  const int64_t R = c.max_requests, T = c.max_tokens, ratio = c.num_q_heads / c.num_kv_heads;
+  PageScratch w{};
+  w.hdr = cv.take<PageHdr>(1);
+  const int64_t np = c.num_pages - c.first_page;
+  // chunks of at least 2048 references, at most kMaxChunks of them
+  int64_t chunk = (np + kMaxChunks - 1) / kMaxChunks;
+  chunk = chunk < 2048 ? 2048 : (chunk + kScanThreads - 1) / kScanThreads * kScanThreads;
+  w.chunk_size = (int32_t)chunk;
+  w.chunks = (int32_t)((np + chunk - 1) / chunk);
+  if (w.chunks < 1) w.chunks = 1;
+  w.chunk_cnt = cv.take<int32_t>(w.chunks);
+  w.chunk_base = cv.take<int32_t>(w.chunks);
+  w.list = cv.take<int32_t>((size_t)w.chunks * chunk);
+  w.movers = cv.take<int32_t>((size_t)np);
+  w.inv = cv.take<int32_t>((size_t)np);
+  w.mover_refs = cv.take<int32_t>((size_t)np);
+  w.need = cv.take<int32_t>((size_t)R);
+  w.start = cv.take<int32_t>((size_t)R);
+  w.bad = cv.take<int32_t>((size_t)R);
+  Plan p{};
+  p.hdr = cv.take<PlanHdr>(1);
+  p.req = cv.take<ReqRec>((size_t)R);
+  p.tok_req = cv.take<int32_t>((size_t)T);
+  p.group = cv.take<int32_t>((size_t)R);
+  p.grp_tile = cv.take<int32_t>((size_t)R);
+  p.grp_list = cv.take<int32_t>((size_t)R);
+  p.common = cv.take<int32_t>((size_t)R);
+  p.bad = cv.take<int32_t>((size_t)R);
+  for (int l = 0; l < kLists; ++l) {
+    const PlanBounds b = plan_bounds(l, R, T * ratio);
+    const int64_t shared = b.shared * c.num_kv_heads;
+    p.max_ctas[l] = ctas[l];
+    p.max_tiles[l] = (int32_t)b.tiles;
+    p.max_slots[l] = (int32_t)(3 * (int64_t)ctas[l] + shared);
+    p.tiles[l] = cv.take<Tile>((size_t)b.tiles);
+    p.ucum[l] = cv.take<int64_t>((size_t)b.tiles + 1);
+    p.cta_tile[l] = cv.take<int32_t>((size_t)ctas[l]);
+    p.part_o[l] = cv.take<float>((size_t)p.max_slots[l] * tile_rows(l) * c.head_dim);
+    p.part_ml[l] = cv.take<float2>((size_t)p.max_slots[l] * tile_rows(l));
+  }
+  if (plan) *plan = p;
+  if (pages) *pages = w;
+  return (cv.off + 255) / 256 * 256;
+}
+
+// The workspace has the same size wherever it is asked for: the CTA counts are
+// bounded by the device's at ps_kv_create().
+constexpr int32_t kSizedCtas[kLists] = {kMaxSms * 4, kMaxSms};
+
+bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
+  return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
+}
+int32_t row_pages(const ps_kv* kv, int64_t stride) {
+  return stride < kv->max_row_pages ? (int32_t)stride : kv->max_row_pages;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ps_kv_workspace_bytes(const ps_kv_config_t* cfg) {
+  return check_config(cfg) ? carve(*cfg, kSizedCtas, nullptr, nullptr, nullptr) : 0;
+}
+
+int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace, size_t workspace_bytes,
+                     void* stream) {
+  if (!out || !check_config(cfg) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0 ||
+      workspace_bytes < carve(*cfg, kSizedCtas, nullptr, nullptr, nullptr))
+    return PS_ERR_INVALID_ARG;
+  int dev = 0, nsm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return PS_ERR_CUDA;
+  ps_kv* kv = new (std::nothrow) ps_kv{};
+  if (!kv) return PS_ERR_CUDA;
+  kv->pool = make_pool(*cfg);
+  kv->nsm = nsm < kMaxSms ? nsm : kMaxSms;
+  kv->max_requests = cfg->max_requests;
+  kv->max_tokens = cfg->max_tokens;
+  kv->max_row_pages = cfg->max_row_pages;
+  int32_t ctas[kLists];
+  int32_t rc = configure_attention(kv->pool, kv->nsm, ctas);
+  for (int l = 0; l < kLists; ++l)
+    if (ctas[l] > kSizedCtas[l]) ctas[l] = kSizedCtas[l];
+  if (rc == PS_OK) {
+    carve(*cfg, kSizedCtas, static_cast<char*>(d_workspace), &kv->plan, &kv->pages);
+    for (int l = 0; l < kLists; ++l) kv->plan.max_ctas[l] = ctas[l];
+    if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess) rc = PS_ERR_CUDA;
+  }
+  if (rc != PS_OK) {
+    delete kv;
+    return rc;
+  }
+  *out = kv;
+  return PS_OK;
+}
+
+void ps_kv_destroy(ps_kv_t* kv) { delete kv; }
+
+int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_append_t* a, int32_t* d_status) {
+  if (!kv || !a || layer < 0 || layer >= kv->pool.num_layers || a->num_tokens < 0) return PS_ERR_INVALID_ARG;
+  if (a->num_tokens == 0) return PS_OK;
+  if (!a->q || !a->k || !a->v || !a->q_out || !a->slots) return PS_ERR_INVALID_ARG;
+  for (const void* p : {a->q, a->k, a->v, (const void*)a->q_out, a->q_weight, a->k_weight, (const void*)a->rope})
+    if (!aligned16(p)) return PS_ERR_INVALID_ARG;
+  if (!good_strides(a->q_stride) || !good_strides(a->k_stride) || !good_strides(a->v_stride) ||
+      !good_strides(a->q_out_stride))
+    return PS_ERR_INVALID_ARG;
+  if ((a->q_weight || a->k_weight) && !(a->eps > 0)) return PS_ERR_INVALID_ARG;
+  if (a->rope && (!a->positions || a->rope_rows < 1 || a->rope_dim < 16 || a->rope_dim % 16 != 0 ||
+                  a->rope_dim > kv->pool.head_dim))
+    return PS_ERR_INVALID_ARG;
+  return launch_append(kv->pool, layer, *a, d_status, kv->nsm, as_stream(stream));
+}
+
+int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* b, int32_t* d_status) {
+  if (!kv || !b) return PS_ERR_INVALID_ARG;
+  if (b->num_requests < 0 || b->num_requests > kv->max_requests || b->num_tokens < 0 ||
+      b->num_tokens > kv->max_tokens || b->table_stride < 0)
+    return PS_ERR_INVALID_ARG;
+  if (b->num_requests > 0 && (!b->q_offsets || !b->kv_lens || (!b->tables && b->table_stride > 0)))
+    return PS_ERR_INVALID_ARG;
+  if (b->group_offsets && (b->num_groups < 1 || b->num_groups > b->num_requests)) return PS_ERR_INVALID_ARG;
+  Batch x{};
+  x.q_offsets = b->q_offsets; x.kv_lens = b->kv_lens; x.tables = b->tables; x.group_offsets = b->group_offsets;
+  x.table_stride = b->table_stride;
+  x.num_requests = b->num_requests; x.num_groups = b->num_groups; x.num_tokens = b->num_tokens;
+  x.causal = b->causal != 0;
+  x.row_pages = row_pages(kv, b->table_stride);
+  const int32_t rc = launch_plan(kv->pool, kv->plan, x, d_status, as_stream(stream));
+  kv->batch = x;
+  kv->planned = rc == PS_OK;
+  return rc;
+}
+
+int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a) {
+  if (!kv || !a || !kv->planned || layer < 0 || layer >= kv->pool.num_layers) return PS_ERR_INVALID_ARG;
+  if (kv->batch.num_tokens == 0 || kv->batch.num_requests == 0) return PS_OK;
+  if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) || !good_strides(a->q_stride) ||
+      !good_strides(a->out_stride) || !(a->scale - a->scale == 0))
+    return PS_ERR_INVALID_ARG;
+  return launch_attention(kv->pool, kv->plan, kv->batch, layer, *a, as_stream(stream));
+}
+
+int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,
+                   int32_t* d_status) {
+  if (!kv || n < 0 || (n > 0 && (!d_src || !d_dst))) return PS_ERR_INVALID_ARG;
+  if (n == 0) return PS_OK;
+  return launch_copy(kv->pool, n, d_src, d_dst, d_status, kv->nsm, as_stream(stream));
+}
+
+int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parents, const int32_t* d_children,
+                   const int32_t* d_room, const ps_kv_rows_t* rows, const int32_t* d_refs_in, int32_t* d_refs_out,
+                   int32_t* d_status) {
+  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !d_refs_in || !d_refs_out) return PS_ERR_INVALID_ARG;
+  if (n > 0 && (!d_parents || !d_children || !d_room)) return PS_ERR_INVALID_ARG;
+  return launch_fork(kv->pool, kv->pages, n, d_parents, d_children, d_room, *rows, row_pages(kv, rows->table_stride),
+                     d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
+}
+
+int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_rows, const ps_kv_rows_t* rows,
+                      int32_t* d_refs, int32_t* d_status) {
+  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !d_refs || (n > 0 && !d_rows))
+    return PS_ERR_INVALID_ARG;
+  if (n == 0) return PS_OK;
+  return launch_release(kv->pool, n, d_rows, *rows, row_pages(kv, rows->table_stride), d_refs, d_status,
+                        as_stream(stream));
+}
+
+int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
+                      int32_t* d_tables_out, int32_t* d_refs_out, int32_t* d_counts, int32_t* d_status) {
+  if (!kv || !rows || !rows->tables || !rows->held || rows->num_rows < 1 || rows->table_stride < 1 || !d_refs_in ||
+      !d_tables_out || !d_refs_out || !d_counts)
+    return PS_ERR_INVALID_ARG;
+  return launch_compact(kv->pool, kv->pages, *rows, row_pages(kv, rows->table_stride), d_refs_in, d_tables_out,
+                        d_refs_out, d_counts, d_status, kv->nsm, as_stream(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,469 @@
+// ps_kv_attention: the narrow tiles (up to 16 query rows, mma) and the join of
+// partial results.  The wide tiles are in ps_kv_attend_wide.cu.
+//
+// The mathematics, for one query row and the keys j that it sees:
+//   t_j = scale log2(e) q k_j,  m = max t_j,  l = sum 2^(t_j - m),
+//   o = sum 2^(t_j - m) v_j / l,
+// kept as (m, l, sum) over a growing set of keys: a new key set's maximum m'
+// scales what was there by 2^(m - max(m, m')), and two sets' (m, l, sum) join
+// the same way.  m, l and the sums are in 32 bits; the weights 2^(t - m) are
+// rounded to the pool's type for the product with V, as the matrix
+// instructions want them.
+#include "ps_kv_attend.cuh"
+
+namespace pskv {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kWarps = 4;
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes into shared memory, or zeros where !ok (src is not read then).
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Shared memory of a warp: STAGES x (16 keys, 16 values) of ROW bytes each, a
+// 16-byte word c of row r at word c ^ (r & 7), so that the eight rows of an
+// ldmatrix lie in eight different banks groups.
+template <int DP>
+struct Shape {
+  static constexpr int kRow = DP <= 64 ? 128 : 256;  // bytes
+  static constexpr int kStages = DP <= 64 ? 6 : 3;
+  static constexpr int kStage = 2 * 16 * kRow;
+  static constexpr int kWarpBytes = kStages * kStage;
+  static constexpr int kMergeRow = DP + 2;  // floats: padded against bank conflicts
+  static constexpr int kMergeBytes = 2 * 16 * (kMergeRow + 2) * 4;
+  static constexpr int kSmem = kWarps * kWarpBytes + kMergeBytes;
+};
+
+// Narrow tiles: decode.  Bound by HBM (a key is used by at most 16 rows).  A
+// unit is 64 keys, 16 for each warp; a warp streams its own keys and values
+// through its own ring of stages with no barrier, runs its own (m, l, sum) over
+// them, and the four are joined where a (tile, head) ends.  The stream of units
+// runs on across tiles, so that short requests do not drain it.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
+  using S = Shape<DP>;
+  constexpr int CH = DP / 8;   // 16-byte words of a row
+  constexpr int KS = DP / 16;  // k steps of q k^T
+  constexpr int H = tile_rows(0), UNIT = unit_keys(0);
+  extern __shared__ __align__(128) char smem[];
+  chain();
+  const PlanHdr* hdr = a.plan.hdr;
+  const int C = hdr->ctas[0], c = blockIdx.x;
+  if (c >= C) return;
+  const int64_t U = hdr->units[0];
+  const int64_t u0 = U * c / C;
+  const int n = (int)(U * (c + 1) / C - u0);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t ring = smem_addr(smem) + warp * S::kWarpBytes;
+  const Tile* tiles = a.plan.tiles[0];
+  const int64_t* ucum = a.plan.ucum[0];
+
+  // where the first unit lies
+  int tile = a.plan.cta_tile[0][c], head, unit, nunits;
+  {
+    const int64_t b = ucum[tile];
+    nunits = (int)((ucum[tile + 1] - b) / a.pool.kv_heads);
+    head = (int)((u0 - b) / nunits);
+    unit = (int)((u0 - b) % nunits);
+  }
+
+  // ---- the loader: runs STAGES - 1 units ahead ----
+  Tile lt = tiles[tile];
+  int ltile = tile, lhead = head, lunit = unit, lnunits = nunits, lleft = n;
+  const char* kbase = a.k;
+  const char* vbase = a.v;
+  // page id of this lane's key in the loader's unit, -1 past the end
+  auto key_page = [&]() -> int {
+    const int t = lt.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
+    return t < lt.kv1 ? __ldg(a.tables + lt.req * a.table_stride + (t >> a.pool.page_log2)) : -1;
+  };
+  int page = lleft > 0 ? key_page() : -1;
+  int lstage = 0;
+  auto load_unit = [&]() {
+    if (lleft > 0) {
+      const int t = lt.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
+      int64_t off = -1;
+      if (page >= 0)
+        off = page * a.pool.page_stride + (int64_t)(t & (a.pool.page_size - 1)) * a.pool.token_stride +
+              lhead * a.pool.head_stride;
+      const uint32_t dst = ring + lstage * S::kStage;
+#pragma unroll
+      for (int j = 0; j < 16 * CH / 32; ++j) {
+        const int idx = j * 32 + lane, row = idx / CH, w = idx % CH;
+        const int64_t o = __shfl_sync(0xFFFFFFFFu, off, row);
+        const bool ok = o >= 0 && w * 8 < a.pool.head_dim;
+        const int64_t at = ok ? 2 * o + w * 16 : 0;
+        const uint32_t d = dst + row * S::kRow + ((w ^ (row & 7)) << 4);
+        cp16(d, kbase + at, ok);
+        cp16(d + 16 * S::kRow, vbase + at, ok);
+      }
+      --lleft;
+      if (lleft > 0) {
+        if (++lunit == lnunits) {
+          lunit = 0;
+          if (++lhead == a.pool.kv_heads) {
+            lhead = 0;
+            ++ltile;
+            lt = tiles[ltile];
+            lnunits = (int)((ucum[ltile + 1] - ucum[ltile]) / a.pool.kv_heads);
+          }
+        }
+        page = key_page();
+      }
+    }
+    cp_commit();
+    lstage = lstage + 1 == S::kStages ? 0 : lstage + 1;
+  };
+#pragma unroll
+  for (int s = 0; s < S::kStages - 1; ++s) load_unit();
+
+  // ---- the consumer ----
+  int stage = 0, left = n;
+  const int g = lane >> 2, q4 = lane & 3;
+  while (left > 0) {
+    const Tile t = tiles[tile];
+    // queries of the 16 rows, as the A operand
+    uint32_t qf[KS][4];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int r = g + 8 * hf;
+      const bool in = r < t.nrows;
+      const int rr = t.row0 + (in ? r : 0);
+      const char* qp = a.q + 2 * ((int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
+                                  (int64_t)(head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1]);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int e = ks * 16 + q4 * 2;
+        qf[ks][hf] = in && e < a.pool.head_dim ? *reinterpret_cast<const uint32_t*>(qp + 2 * e) : 0u;
+        qf[ks][hf + 2] = in && e + 8 < a.pool.head_dim ? *reinterpret_cast<const uint32_t*>(qp + 2 * e + 16) : 0u;
+      }
+    }
+    // the keys before lim[.] are seen by rows g and g + 8; those before lim0 by all
+    const int lim0 = min(t.kv1, t.ctx + 1 + t.row0 / a.pool.ratio);
+    const int lim[2] = {min(t.kv1, t.ctx + 1 + (t.row0 + g) / a.pool.ratio),
+                        min(t.kv1, t.ctx + 1 + (t.row0 + g + 8) / a.pool.ratio)};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0, 0};
+    float o[DP / 8][4];
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0;
+
+    const int first = unit, count = min(left, nunits - unit);
+    for (int it = 0; it < count; ++it) {
+      cp_wait<S::kStages - 2>();
+      __syncwarp();  // the unit has landed, and the stage of the one before it is read
+      load_unit();
+      const int base = t.kv0 + (first + it) * UNIT + warp * 16;
+      if (base < t.kv1) {
+        const uint32_t ks_at = ring + stage * S::kStage, vs_at = ks_at + 16 * S::kRow;
+        float s[2][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          uint32_t b[4];
+          const int row = (lane & 7) + ((lane >> 4) << 3), w = 2 * ks + ((lane >> 3) & 1);
+          ldsm4(b, ks_at + row * S::kRow + ((w ^ (row & 7)) << 4));
+          mma<T>(s[0], qf[ks], b[0], b[1]);
+          mma<T>(s[1], qf[ks], b[2], b[3]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] *= a.scale2;
+        if (base + 16 > lim0) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (base + i * 8 + q4 * 2 + (j & 1) >= lim[j >> 1]) s[i][j] = -INFINITY;
+        }
+        bool grew = false;
+        float mn[2], ms[2];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          float x = fmaxf(fmaxf(s[0][2 * hf], s[0][2 * hf + 1]), fmaxf(s[1][2 * hf], s[1][2 * hf + 1]));
+          x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1));
+          x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
+          mn[hf] = fmaxf(m[hf], x);
+          grew = grew || mn[hf] > m[hf];
+          ms[hf] = mn[hf] == -INFINITY ? 0.0f : mn[hf];
+        }
+        if (__any_sync(0xFFFFFFFFu, grew)) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float f = ex2(m[hf] - ms[hf]);
+            l[hf] *= f;
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) {
+              o[i][2 * hf] *= f;
+              o[i][2 * hf + 1] *= f;
+            }
+            m[hf] = mn[hf];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i][j] = ex2(s[i][j] - ms[j >> 1]);
+            l[j >> 1] += s[i][j];
+          }
+        const uint32_t pf[4] = {Num<T>::pack(s[0][0], s[0][1]), Num<T>::pack(s[0][2], s[0][3]),
+                                Num<T>::pack(s[1][0], s[1][1]), Num<T>::pack(s[1][2], s[1][3])};
+#pragma unroll
+        for (int np = 0; np < DP / 16; ++np) {
+          uint32_t b[4];
+          const int row = (lane & 7) + (((lane >> 3) & 1) << 3), w = 2 * np + (lane >> 4);
+          ldsm4t(b, vs_at + row * S::kRow + ((w ^ (row & 7)) << 4));
+          mma<T>(o[2 * np], pf, b[0], b[1]);
+          mma<T>(o[2 * np + 1], pf, b[2], b[3]);
+        }
+      }
+      stage = stage + 1 == S::kStages ? 0 : stage + 1;
+    }
+
+    // ---- join the four warps' results: 2 into 0, 3 into 1, then 1 into 0 ----
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      l[hf] += __shfl_xor_sync(0xFFFFFFFFu, l[hf], 1);
+      l[hf] += __shfl_xor_sync(0xFFFFFFFFu, l[hf], 2);
+    }
+    float* mbuf = reinterpret_cast<float*>(smem + kWarps * S::kWarpBytes);
+    constexpr int BUF = 16 * (S::kMergeRow + 2);
+#pragma unroll
+    for (int round = 0; round < 2; ++round) {
+      const int from = round == 0 ? 2 : 1;  // warps [from, 2 from) give to [0, from)
+      __syncthreads();
+      if (warp >= from && warp < 2 * from) {
+        float* b = mbuf + (warp - from) * BUF;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          float* row = b + (g + 8 * hf) * S::kMergeRow;
+#pragma unroll
+          for (int i = 0; i < DP / 8; ++i)
+            *reinterpret_cast<float2*>(row + i * 8 + q4 * 2) = make_float2(o[i][2 * hf], o[i][2 * hf + 1]);
+          if (q4 == 0) *reinterpret_cast<float2*>(b + 16 * S::kMergeRow + 2 * (g + 8 * hf)) = make_float2(m[hf], l[hf]);
+        }
+      }
+      __syncthreads();
+      if (warp < from) {
+        const float* b = mbuf + warp * BUF;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const float2 ml = *reinterpret_cast<const float2*>(b + 16 * S::kMergeRow + 2 * (g + 8 * hf));
+          const float mn = fmaxf(m[hf], ml.x), ms = mn == -INFINITY ? 0.0f : mn;
+          const float f0 = ex2(m[hf] - ms), f1 = ex2(ml.x - ms);
+          const float* row = b + (g + 8 * hf) * S::kMergeRow;
+#pragma unroll
+          for (int i = 0; i < DP / 8; ++i) {
+            const float2 x = *reinterpret_cast<const float2*>(row + i * 8 + q4 * 2);
+            o[i][2 * hf] = o[i][2 * hf] * f0 + x.x * f1;
+            o[i][2 * hf + 1] = o[i][2 * hf + 1] * f0 + x.y * f1;
+          }
+          l[hf] = l[hf] * f0 + ml.y * f1;
+          m[hf] = mn;
+        }
+      }
+    }
+    if (warp == 0) {
+      const bool whole = first == 0 && count == nunits;
+      if (whole && t.sidx < 0) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int r = g + 8 * hf;
+          if (r < t.nrows) {
+            const int rr = t.row0 + r;
+            const int64_t tok = t.tok0 + rr / a.pool.ratio;
+            const int hq = head * a.pool.ratio + rr % a.pool.ratio;
+            const float inv = l[hf] > 0 ? 1.0f / l[hf] : (l[hf] == 0 ? 0.0f : l[hf]);
+            char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i)
+              if (i * 8 < a.pool.head_dim)
+                *reinterpret_cast<uint32_t*>(op + 2 * (i * 8 + q4 * 2)) =
+                    Num<T>::pack(o[i][2 * hf] * inv, o[i][2 * hf + 1] * inv);
+            if (a.lse && q4 == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m[hf], l[hf]);
+          }
+        }
+      } else {
+        const int64_t slot = part_slot(t.sidx, head, c, first > 0, C);
+        float* po = a.plan.part_o[0] + slot * H * a.pool.head_dim;
+        float2* pml = a.plan.part_ml[0] + slot * H;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int r = g + 8 * hf;
+          if (r < t.nrows) {
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i)
+              if (i * 8 < a.pool.head_dim)
+                *reinterpret_cast<float2*>(po + r * a.pool.head_dim + i * 8 + q4 * 2) =
+                    make_float2(o[i][2 * hf], o[i][2 * hf + 1]);
+            if (q4 == 0) pml[r] = make_float2(m[hf], l[hf]);
+          }
+        }
+      }
+    }
+    left -= count;
+    unit = 0;
+    if (++head == a.pool.kv_heads) {
+      head = 0;
+      ++tile;
+      if (left > 0) nunits = (int)((ucum[tile + 1] - ucum[tile]) / a.pool.kv_heads);
+    }
+  }
+  cp_wait<0>();
+}
+
+// ---- the join --------------------------------------------------------------------
+// A warp for each (token, query head) whose row has partial results: those of
+// its own keys' tile, then those of its group's shared prefix, in CTA order.
+// Bound by the latency of a few dependent reads; the partial results were
+// written just before and lie in L2.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
+  chain();
+  const PlanHdr* hdr = a.plan.hdr;
+  if (hdr->status != PS_OK || !hdr->join) return;
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
+  if (w >= (int64_t)a.num_tokens * a.pool.q_heads) return;
+  const int tok = (int)(w / a.pool.q_heads), hq = (int)(w % a.pool.q_heads);
+  const int head = hq / a.pool.ratio;
+  const int req = a.plan.tok_req[tok];
+  const ReqRec rec = a.plan.req[req];
+  const int row = (tok - a.q_offsets[req]) * a.pool.ratio + hq % a.pool.ratio;
+  const int dim = a.pool.head_dim;
+  float m = -INFINITY, l = 0;
+  float4 o = make_float4(0, 0, 0, 0);
+  bool parts = false;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const int tile0 = side ? rec.ptile0 : rec.tile0, list = side ? rec.plist : rec.list;
+    if (side && tile0 < 0) break;
+    const int rr = side ? rec.prow0 + row : row;
+    const int H = tile_rows(list);
+    const int tile = tile0 + rr / H, r = rr % H;
+    const int sidx = a.plan.tiles[list][tile].sidx;
+    const int64_t U = hdr->units[list], b = a.plan.ucum[list][tile];
+    const int C = hdr->ctas[list];
+    const int64_t nu = (a.plan.ucum[list][tile + 1] - b) / a.pool.kv_heads;
+    const int64_t ua = b + head * nu;
+    const int ca = cta_of(ua, U, C), cb = cta_of(ua + nu - 1, U, C);
+    if (sidx < 0 && ca == cb) return;  // written by the one CTA that worked on it
+    parts = true;
+    // a CTA's range may begin exactly with this (tile, head)
+    for (int c = ca; c <= cb; ++c) {
+      const int64_t slot = part_slot(sidx, head, c, U * c / C > ua, C);
+      const float2 ml = a.plan.part_ml[list][slot * H + r];
+      float4 x = make_float4(0, 0, 0, 0);
+      if (lane * 4 < dim)
+        x = *reinterpret_cast<const float4*>(a.plan.part_o[list] + (slot * H + r) * dim + lane * 4);
+      const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
+      const float f0 = ex2(m - ms), f1 = ex2(ml.x - ms);
+      o.x = o.x * f0 + x.x * f1;
+      o.y = o.y * f0 + x.y * f1;
+      o.z = o.z * f0 + x.z * f1;
+      o.w = o.w * f0 + x.w * f1;
+      l = l * f0 + ml.y * f1;
+      m = mn;
+    }
+  }
+  if (!parts) return;
+  const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+  if (lane * 4 < dim)
+    *reinterpret_cast<uint2*>(a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + lane * 4)) =
+        make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
+  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.pool.q_heads + hq] = log_sum(m, l);
+}
+
+template <typename T, int DP>
+cudaError_t narrow(const AttendArgs& a, cudaStream_t st) {
+  return launch(k_attend_narrow<T, DP>, dim3((unsigned)a.plan.max_ctas[0]), kThreads, Shape<DP>::kSmem, st, a);
+}
+template <typename T>
+cudaError_t narrow_t(const AttendArgs& a, cudaStream_t st) {
+  const int d = a.pool.head_dim;
+  return d <= 64 ? narrow<T, 64>(a, st) : d <= 80 ? narrow<T, 80>(a, st) : d <= 96 ? narrow<T, 96>(a, st) : narrow<T, 128>(a, st);
+}
+template <typename T, int DP>
+cudaError_t configure_narrow(int nsm, int32_t* ctas) {
+  cudaError_t e = cudaFuncSetAttribute(k_attend_narrow<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem);
+  int occ = 0;
+  if (e == cudaSuccess)
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_attend_narrow<T, DP>, kThreads, Shape<DP>::kSmem);
+  *ctas = nsm * (occ > 0 ? occ : 1);
+  return e;
+}
+template <typename T>
+cudaError_t configure_t(int d, int nsm, int32_t* ctas) {
+  return d <= 64 ? configure_narrow<T, 64>(nsm, ctas) : d <= 80 ? configure_narrow<T, 80>(nsm, ctas)
+       : d <= 96 ? configure_narrow<T, 96>(nsm, ctas) : configure_narrow<T, 128>(nsm, ctas);
+}
+
+}  // namespace
+
+int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]) {
+  ctas[1] = nsm;
+  return status_of(p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim, nsm, ctas)
+                                         : configure_t<__half>(p.head_dim, nsm, ctas));
+}
+
+int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& in,
+                         cudaStream_t st) {
+  AttendArgs a{};
+  a.pool = p;
+  a.plan = plan;
+  a.k = p.k + 2 * layer * p.layer_stride;
+  a.v = p.v + 2 * layer * p.layer_stride;
+  a.q = (const char*)in.q;
+  a.out = (char*)in.out;
+  a.lse = in.lse;
+  for (int i = 0; i < 2; ++i) {
+    a.q_stride[i] = in.q_stride[i];
+    a.out_stride[i] = in.out_stride[i];
+  }
+  a.tables = b.tables;
+  a.table_stride = b.table_stride;
+  a.q_offsets = b.q_offsets;
+  a.num_tokens = b.num_tokens;
+  a.scale2 = in.scale * 1.4426950408889634f;
+  cudaError_t e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
+  if (e != cudaSuccess) return status_of(e);
+  const int64_t warps = (int64_t)b.num_tokens * p.q_heads;
+  const dim3 grid((unsigned)((warps + 7) / 8));
+  e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 256, 0, st, a)
+                            : launch(k_attend_join<__half>, grid, 256, 0, st, a);
+  return status_of(e);
+}
+
+}  // namespace pskv

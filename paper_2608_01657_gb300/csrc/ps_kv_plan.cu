@@ -1,0 +1,302 @@
+// ps_kv_plan: shared prefixes, tiles and the division of a batch's attention
+// into equal parts (see ps_kv.cuh for the plan's shape).
+#include "ps_kv.cuh"
+
+namespace pskv {
+namespace {
+
+constexpr int kReqThreads = 128;
+constexpr int kPlanThreads = 1024;
+constexpr int kAnyPages = 0x7FFFFFFF;
+
+// Shared tokens below which the second part of a row costs more than it saves.
+constexpr int kShareTokens = 128;
+
+// Pages of a request that every one of its queries sees whole.
+__device__ __forceinline__ int whole_pages(const Pool& p, const Batch& b, int r) {
+  const int n = b.q_offsets[r + 1] - b.q_offsets[r], len = b.kv_lens[r];
+  const int seen = b.causal ? len - n : len;
+  return seen > 0 ? seen >> p.page_log2 : 0;
+}
+
+// One CTA a request: its offsets, length and page ids are in range; the leading
+// pages that it has in common with its group's first request; its tokens' map.
+__global__ void __launch_bounds__(kReqThreads) k_plan_requests(Pool p, Plan plan, Batch b) {
+  chain();
+  const int r = blockIdx.x;
+  const int q0 = b.q_offsets[r], q1 = b.q_offsets[r + 1], len = b.kv_lens[r];
+  bool ok = q0 >= 0 && q1 >= q0 && q1 <= b.num_tokens && len >= 0 && len <= (int64_t)b.row_pages << p.page_log2;
+  if (r == 0) ok = ok && q0 == 0;
+  if (r == b.num_requests - 1) ok = ok && q1 == b.num_tokens;
+  const bool sane = ok;
+  const int32_t* row = b.tables + r * b.table_stride;
+  int common = kAnyPages;
+  if (sane) {
+    const int pages = (int)(((int64_t)len + p.page_size - 1) >> p.page_log2);
+    for (int k = threadIdx.x; k < pages; k += kReqThreads) {
+      const int id = row[k];
+      if (id < 0 || id >= p.num_pages) ok = false;
+    }
+    for (int t = q0 + threadIdx.x; t < q1; t += kReqThreads) plan.tok_req[t] = r;
+    // the group that holds r: the last one that starts at or before it
+    int lo = 0, hi = b.group_offsets ? b.num_groups - 1 : 0;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (b.group_offsets[mid] <= r) lo = mid;
+      else hi = mid - 1;
+    }
+    if (threadIdx.x == 0) plan.group[r] = lo;
+    if (b.group_offsets && q1 > q0) {
+      const int first = b.group_offsets[lo];
+      common = 0;
+      if (first >= 0 && first <= r) {
+        const int f0 = b.kv_lens[first], w = whole_pages(p, b, r);
+        if (f0 >= 0 && f0 <= (int64_t)b.row_pages << p.page_log2) {
+          const int wf = whole_pages(p, b, first);
+          common = w < wf ? w : wf;
+          const int32_t* lead = b.tables + first * b.table_stride;
+          // wf may be out of range where the first request's offsets are: bounded by its length's pages
+          const int most = (int)((int64_t)f0 >> p.page_log2);
+          common = common < most ? common : most;
+          if (first != r)
+            for (int k = threadIdx.x; k < common; k += kReqThreads)
+              if (row[k] != lead[k]) {
+                common = k;
+                break;
+              }
+        }
+      }
+    }
+  }
+  __shared__ int s_common;
+  if (threadIdx.x == 0) s_common = kAnyPages;
+  __syncthreads();
+  atomicMin(&s_common, common);
+  ok = __syncthreads_and(ok);
+  if (threadIdx.x == 0) {
+    plan.common[r] = s_common;
+    plan.bad[r] = !ok;
+  }
+}
+
+// Exclusive scan of one 64-bit value a thread over the CTA.
+__device__ int64_t scan64(int64_t v, int64_t* total) {
+  __shared__ int64_t wsum[kPlanThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) wsum[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    int64_t w = wsum[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xFFFFFFFFu, w, o);
+      if (lane >= o) w += x;
+    }
+    wsum[lane] = w;
+  }
+  __syncthreads();
+  const int64_t base = warp ? wsum[warp - 1] : 0;
+  *total = wsum[kPlanThreads / 32 - 1];
+  __syncthreads();
+  return base + incl - v;
+}
+
+// The rows of one item (a group's shared prefix, or a request's own keys).
+struct Item {
+  int tok0, rows, kv0, kv1, req, ctx, list;
+  bool shared;
+};
+__device__ __forceinline__ int tile_end(const Item& it, const Pool& p, int last_row) {
+  // keys past the last row's bound are never seen
+  const int64_t bound = (int64_t)it.ctx + 1 + last_row / p.ratio;
+  return bound < it.kv1 ? (int)(bound > it.kv0 ? bound : it.kv0) : it.kv1;
+}
+__device__ __forceinline__ int unit_count(int keys, int unit) { return keys > 0 ? (keys + unit - 1) / unit : 1; }
+
+__device__ __forceinline__ int list_of(int rows) {
+  (void)rows;
+  return 0;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, Batch b, int32_t* status) {
+  chain();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  __shared__ int s_bad, s_join;
+  if (tid == 0) s_bad = s_join = 0;
+  __syncthreads();
+  int bad = 0;
+  for (int r = tid; r < b.num_requests; r += kPlanThreads) bad |= plan.bad[r];
+  if (b.num_requests == 0) bad |= b.num_tokens != 0;
+  if (b.group_offsets) {
+    for (int g = tid; g < b.num_groups; g += kPlanThreads) bad |= b.group_offsets[g] > b.group_offsets[g + 1];
+    if (tid == 0) bad |= b.group_offsets[0] != 0 || b.group_offsets[b.num_groups] != b.num_requests;
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) {
+      PlanHdr h{};
+      h.status = PS_ERR_INVALID_ARG;
+      *plan.hdr = h;
+      set_error(status, PS_ERR_INVALID_ARG);
+    }
+    return;
+  }
+  // the groups' shared tokens, kept in common[] for each member (0: none)
+  if (b.group_offsets) {
+    for (int g = warp; g < b.num_groups; g += kPlanThreads / 32) {
+      const int r0 = b.group_offsets[g], r1 = b.group_offsets[g + 1];
+      int common = kAnyPages, members = 0, most = 0;
+      for (int r = r0 + lane; r < r1; r += 32) {
+        const int n = b.q_offsets[r + 1] - b.q_offsets[r];
+        if (n == 0) continue;
+        common = min(common, plan.common[r]);
+        members += 1;
+        most = max(most, n);
+      }
+      common = __reduce_min_sync(0xFFFFFFFFu, common);
+      members = __reduce_add_sync(0xFFFFFFFFu, members);
+      most = __reduce_max_sync(0xFFFFFFFFu, most);
+      const bool share = members > 1 && (int64_t)most * p.ratio <= kShareRows &&
+                         ((int64_t)common << p.page_log2) >= kShareTokens;
+      for (int r = r0 + lane; r < r1; r += 32) plan.common[r] = share ? common << p.page_log2 : 0;
+    }
+  } else {
+    for (int r = tid; r < b.num_requests; r += kPlanThreads) plan.common[r] = 0;
+  }
+  __syncthreads();
+  // items: the groups' prefixes, then the requests
+  const int ngroups = b.group_offsets ? b.num_groups : 0;
+  const int nitems = ngroups + b.num_requests;
+  int64_t tiles[kLists] = {}, units[kLists] = {}, shared[kLists] = {};
+  for (int i0 = 0; i0 < nitems; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    Item it{};
+    if (i < ngroups) {
+      const int r0 = b.group_offsets[i], r1 = b.group_offsets[i + 1];
+      if (r1 > r0 && plan.common[r0] > 0) {
+        it.tok0 = b.q_offsets[r0];
+        it.rows = (b.q_offsets[r1] - it.tok0) * p.ratio;
+        it.kv1 = plan.common[r0];
+        it.req = r0;
+        it.ctx = kNoMask;
+        it.shared = true;
+      }
+    } else if (i < nitems) {
+      const int r = i - ngroups, n = b.q_offsets[r + 1] - b.q_offsets[r];
+      it.tok0 = b.q_offsets[r];
+      it.rows = n * p.ratio;
+      it.kv0 = plan.common[r];
+      it.kv1 = b.kv_lens[r];
+      it.req = r;
+      it.ctx = b.causal ? b.kv_lens[r] - n : kNoMask;
+      it.shared = plan.common[r] > 0;
+    }
+    it.list = list_of(it.rows);
+    const int H = tile_rows(it.list), unit = unit_keys(it.list);
+    const int nt = (it.rows + H - 1) / H;
+    int64_t nu = 0;
+    for (int t = 0; t < nt; ++t) {
+      const int last = min(it.rows, (t + 1) * H) - 1;
+      nu += unit_count(tile_end(it, p, last) - it.kv0, unit);
+    }
+    int64_t tile_at = 0, unit_at = 0, shared_at = 0;
+    for (int l = 0; l < kLists; ++l) {
+      int64_t tot;
+      const bool mine = it.list == l;
+      int64_t e = scan64(mine ? nt : 0, &tot);
+      if (mine) tile_at = tiles[l] + e;
+      tiles[l] += tot;
+      e = scan64(mine ? nu * p.kv_heads : 0, &tot);
+      if (mine) unit_at = units[l] + e;
+      units[l] += tot;
+      e = scan64(mine && it.shared ? (int64_t)nt * p.kv_heads : 0, &tot);
+      if (mine) shared_at = shared[l] + e;
+      shared[l] += tot;
+    }
+    for (int t = 0; t < nt; ++t) {
+      const int last = min(it.rows, (t + 1) * H) - 1;
+      Tile x;
+      x.tok0 = it.tok0;
+      x.row0 = t * H;
+      x.nrows = last + 1 - t * H;
+      x.kv0 = it.kv0;
+      x.kv1 = tile_end(it, p, last);
+      x.req = it.req;
+      x.ctx = it.ctx;
+      x.sidx = it.shared ? (int)shared_at + t * p.kv_heads : -1;
+      plan.tiles[it.list][tile_at + t] = x;
+      plan.ucum[it.list][tile_at + t] = unit_at;
+      unit_at += (int64_t)unit_count(x.kv1 - x.kv0, unit) * p.kv_heads;
+    }
+    if (i < ngroups) {
+      plan.grp_tile[i] = it.rows > 0 ? (int)tile_at : -1;
+      plan.grp_list[i] = it.list;
+    } else if (i < nitems) {
+      ReqRec q{};
+      q.tile0 = (int)tile_at;
+      q.list = it.list;
+      q.ptile0 = -1;
+      plan.req[i - ngroups] = q;
+    }
+  }
+  __syncthreads();
+  if (b.group_offsets) {  // the requests' places in their groups' prefix tiles
+    for (int r = tid; r < b.num_requests; r += kPlanThreads) {
+      const int g = plan.group[r];
+      plan.req[r].ptile0 = plan.grp_tile[g];
+      plan.req[r].plist = plan.grp_list[g];
+      plan.req[r].prow0 = (b.q_offsets[r] - b.q_offsets[b.group_offsets[g]]) * p.ratio;
+    }
+  }
+  int ctas[kLists];
+  for (int l = 0; l < kLists; ++l) {
+    ctas[l] = (int)(units[l] < plan.max_ctas[l] ? units[l] : plan.max_ctas[l]);
+    if (tid == 0) plan.ucum[l][tiles[l]] = units[l];
+    if (shared[l] > 0) s_join = 1;
+  }
+  __syncthreads();
+  for (int l = 0; l < kLists; ++l) {
+    for (int c = tid; c < ctas[l]; c += kPlanThreads) {
+      const int64_t u = units[l] * c / ctas[l];
+      int lo = 0, hi = (int)tiles[l] - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (plan.ucum[l][mid] <= u) lo = mid;
+        else hi = mid - 1;
+      }
+      plan.cta_tile[l][c] = lo;
+      const int64_t per_head = (plan.ucum[l][lo + 1] - plan.ucum[l][lo]) / p.kv_heads;
+      if ((u - plan.ucum[l][lo]) % per_head) s_join = 1;  // a (tile, head) is cut here
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    PlanHdr h{};
+    h.status = PS_OK;
+    h.join = s_join;
+    for (int l = 0; l < kLists; ++l) {
+      h.ntiles[l] = (int)tiles[l];
+      h.nshared[l] = (int)shared[l];
+      h.ctas[l] = ctas[l];
+      h.units[l] = units[l];
+    }
+    *plan.hdr = h;
+  }
+}
+
+}  // namespace
+
+int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* status, cudaStream_t st) {
+  if (b.num_requests > 0) {
+    const cudaError_t e = launch(k_plan_requests, dim3((unsigned)b.num_requests), kReqThreads, 0, st, p, plan, b);
+    if (e != cudaSuccess) return status_of(e);
+  }
+  return status_of(launch(k_plan_tiles, dim3(1), kPlanThreads, 0, st, p, plan, b, status));
+}
+
+}  // namespace pskv

@@ -1,0 +1,282 @@
+"""Attention over KV pages against a plain 64-bit statement of it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from _kv_ref import attention, attention_bound, make_pool
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+def batch(new, kv, prefix, groups, page_size, seed=0, extra_pages=3):
+    """Tables of a batch; the requests of a group share its prefix's full pages.
+
+    ``groups``: first requests of the groups; ``prefix``: each group's shared tokens."""
+    R = len(new)
+    r = np.random.RandomState(seed)
+    width = max(1, max(-(-n // page_size) for n in kv)) + 2
+    need = R * width + sum(prefix) // page_size + extra_pages
+    ids = iter(r.permutation(need))
+    tables = np.full((R, width), -7, np.int64)   # never a page
+    bounds = list(groups) + [R]
+    for g in range(len(groups)):
+        shared = [next(ids) for _ in range(prefix[g] // page_size)]
+        for i in range(bounds[g], bounds[g + 1]):
+            n = -(-kv[i] // page_size)
+            row = (shared + [next(ids) for _ in range(n)])[:n]
+            tables[i, :n] = row
+    return tables, need, bounds
+
+
+def run(new, kv, heads, ratio, dim, page_size, dtype, prefix=None, groups=None, layout="token", causal=True, seed=0,
+        scale=None, shared=True, poison=True, stream=None):
+    from paper_2608_01657_gb300 import kv as KV
+    groups = [0] if groups is None else groups
+    prefix = [0] * len(groups) if prefix is None else prefix
+    tables, pages, bounds = batch(new, kv, prefix, groups, page_size, seed)
+    k, v = make_pool(1, pages, page_size, heads, dim, dtype, layout, seed + 1)
+    qo = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(qo[-1])
+    if poison:  # what no request holds: NaN, and the unwritten end of each last page
+        held = torch.zeros(pages, page_size, dtype=torch.bool, device="cuda")
+        for i, n in enumerate(kv):
+            for t in range(n):
+                held[tables[i, t // page_size], t % page_size] = True
+        k[0][~held] = float("nan")
+        v[0][~held] = float("nan")
+    g = torch.Generator("cuda").manual_seed(seed + 2)
+    q = torch.randn(T, heads * ratio, dim, generator=g, device="cuda").mul_(1.5).to(dtype)
+    scale = dim ** -0.5 if scale is None else scale
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    t_dev = dev(tables)
+    pool = KV.KVPool(k, v, num_q_heads=heads * ratio, max_requests=len(new), max_tokens=max(1, T),
+                     max_row_pages=tables.shape[1])
+    out = torch.full((T, heads * ratio, dim), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((T, heads * ratio), 7.0, device="cuda")
+    pool.plan(dev(qo), dev(kv), t_dev, T, group_offsets=dev(bounds) if shared else None, causal=causal, stream=stream)
+    pool.attention(0, q, scale, out=out, lse=lse, stream=stream)
+    pool.check()
+    want, want_lse, spread, size = attention(q, k[0], v[0], qo.tolist(), list(kv), t_dev, scale, causal)
+    assert torch.isfinite(out.double()).all()
+    if T:
+        vmax = max([1.0] + [float(v[0][t_dev[i, :-(-n // page_size)].long()].reshape(-1, heads, dim)[:n].abs().max())
+                            for i, n in enumerate(kv) if n])
+        bound = attention_bound(want, spread, size, dtype, dim, max(max(kv), 1), vmax)
+        err = (out.double() - want).abs()
+        assert (err <= bound).all(), float((err / bound).max())
+        empty = torch.isinf(want_lse)
+        assert torch.equal(torch.isinf(lse) & (lse < 0), empty)
+        # scores' error, and the sum's: up to the longest row's additions in 32 bits
+        lb = dim * 2.0 ** -22 * size + max(max(kv), 1) * 2.0 ** -23 + 2.0 ** -20 * want_lse.abs().nan_to_num(0, 0, 0) + 2.0 ** -19
+        assert ((lse.double() - want_lse).abs() <= lb)[~empty].all()
+    return pool, q, out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [8, 40, 64, 72, 80, 96, 104, 128])
+def test_head_sizes(dim, dtype):
+    run([1, 3, 1, 40], [70, 3, 1, 129], 2, 2, dim, 16, dtype, seed=dim)
+
+
+@pytest.mark.parametrize("page_size", [2, 4, 8, 16, 32, 64])
+@pytest.mark.parametrize("layout", ["token", "head", "both"])
+def test_page_sizes_and_layouts(page_size, layout):
+    ps = page_size
+    run([1, 1, 2, 33], [ps, ps + 1, 5 * ps - 1, 130], 3, 2, 64, ps, BF, layout=layout, seed=ps)
+
+
+@pytest.mark.parametrize("heads,ratio", [(1, 1), (7, 1), (2, 3), (1, 16), (1, 17), (3, 5), (2, 64)])
+def test_head_groups(heads, ratio):
+    run([1, 2, 1, 9], [50, 200, 16, 33], heads, ratio, 64, 16, BF, seed=heads * ratio)
+
+
+@pytest.mark.parametrize("new,kv", [
+    ([1], [1]), ([1], [63]), ([1], [64]), ([1], [65]), ([1], [1000]), ([128], [128]), ([129], [129]), ([257], [300]),
+    ([1, 0, 1], [5, 9, 0]), ([0], [0]), ([0, 0, 2], [0, 40, 2]), ([4, 4], [0, 0]), ([5, 3], [2, 1]), ([300], [17]),
+    ([31, 32, 33, 127], [31, 512, 100, 127]),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_lengths_and_empty_rows(new, kv, causal):
+    """Rows that see nothing (no keys, or more new tokens than keys) give 0."""
+    run(new, kv, 2, 4, 64, 16, BF, causal=causal, seed=len(new))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("ratio,new", [(1, 1), (4, 1), (8, 1), (4, 5), (4, 16), (4, 17)])
+def test_shared_prefix(ratio, new, dtype):
+    r = np.random.RandomState(ratio * 100 + new)
+    groups, R = [0, 1, 6, 7, 20], 24
+    prefix = [256, 640, 1024, 128, 336]
+    bounds = groups + [R]
+    n = r.randint(1, new + 1, R)
+    kv = [prefix[g] + int(r.randint(0, 150)) + int(n[i]) for g in range(5) for i in range(bounds[g], bounds[g + 1])]
+    run(n, kv, 2, ratio, 128, 16, dtype, prefix=prefix, groups=groups, seed=new)
+
+
+def test_shared_prefix_equals_unshared():
+    """The grouping changes what is read, not what is computed (within the outputs' own bounds)."""
+    args = ([1] * 20, [700 + 13 * i for i in range(20)], 2, 4, 64, 16, BF)
+    kw = dict(prefix=[640], groups=[0], seed=4)
+    _, _, a, la = run(*args, **kw)
+    _, _, b, lb = run(*args, shared=False, **kw)
+    assert (a.double() - b.double()).abs().max() <= 2 * 2.0 ** -8 * b.double().abs().max()
+    assert (la - lb).abs().max() < 1e-4
+
+
+def test_groups_that_share_less_than_their_lengths():
+    """Tables part ways inside the shorter rows, a member has no queries, another's prefix is all it has."""
+    run([1, 0, 1, 1, 2], [400, 320, 321, 1000, 323], 2, 4, 64, 16, BF, prefix=[320], groups=[0], seed=9)
+    run([1, 1, 1], [300, 301, 302], 2, 4, 64, 16, BF, prefix=[0], groups=[0], seed=10)
+    run([1, 1, 60], [600, 601, 662], 1, 4, 64, 16, BF, prefix=[592], groups=[0], seed=11)
+    run([1, 1, 1], [512, 512, 512], 1, 4, 64, 16, BF, prefix=[512], groups=[0], seed=12, causal=False)
+
+
+@pytest.mark.parametrize("kv", [4097, 20000])
+def test_long_rows_are_split(kv):
+    run([1, 1], [kv, 3], 1, 8, 128, 16, BF, seed=kv)
+    run([200], [kv], 1, 2, 128, 16, BF, seed=kv + 1)
+
+
+def test_prompts_after_a_cached_prefix():
+    run([500, 130, 1, 64], [900, 130, 301, 464], 2, 4, 128, 16, BF, seed=21)
+    run([513, 200], [1025, 640], 1, 3, 96, 32, HF, seed=22, layout="head")
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
+def test_scales(scale):
+    """A scale of 0 averages the values; large scores underflow all weights but a few."""
+    run([1, 70], [300, 100], 2, 2, 64, 16, BF, scale=scale, seed=31)
+
+
+def test_strided_queries_and_outputs():
+    from paper_2608_01657_gb300 import kv as KV
+    pool, q, out, _ = run([3, 1], [40, 17], 2, 2, 64, 16, BF, seed=41)
+    wide = torch.randn(4, 6, 80, device="cuda").to(BF)
+    wide[:, 1:5, 8:72] = q
+    got = torch.zeros(4, 4, 3, 64, device="cuda", dtype=BF)
+    pool.attention(0, wide[:, 1:5, 8:72], 64 ** -0.5, out=got[:, :, 1])
+    assert torch.equal(got[:, :, 1], out)
+    assert not got[:, :, 0].any() and not got[:, :, 2].any()
+    assert KV is not None
+
+
+def test_same_bits_again_and_on_another_stream():
+    args, kw = ([1] * 9 + [70], [2000 + 31 * i for i in range(9)] + [900], 2, 4, 64, 16, BF), dict(prefix=[800], groups=[0], seed=51)
+    _, _, a, la = run(*args[:1], args[1], *args[2:], **kw)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _, _, b, lb = run(*args[:1], args[1], *args[2:], stream=s, **kw)
+    s.synchronize()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_non_finite_values_stay_with_their_rows():
+    """A NaN key or value reaches the rows that see it and no others."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 40, 16, 1, 64, BF, seed=61)
+    tables = torch.arange(40, device="cuda", dtype=torch.int32).view(4, 10)
+    kv = torch.tensor([100, 100, 100, 100], dtype=torch.int32, device="cuda")
+    qo = torch.arange(5, dtype=torch.int32, device="cuda")
+    q = torch.randn(4, 4, 64, device="cuda").to(BF)
+    pool = KV.KVPool(k, v, num_q_heads=4, max_requests=4, max_tokens=4, max_row_pages=10)
+    k[0, 3, 2] = float("nan")        # a key of request 0
+    v[0, 14, 1, 0, 5] = float("inf")  # a value of request 1
+    pool.plan(qo, kv, tables, 4)
+    out = pool.attention(0, q, 0.125)
+    pool.check()
+    assert torch.isnan(out[0]).all()
+    assert not torch.isfinite(out[1, :, 5]).any() and torch.isfinite(out[1, :, :5]).all()
+    assert torch.isfinite(out[2:]).all()
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond 2^31 elements of the pool."""
+    from paper_2608_01657_gb300 import kv as KV
+    pages = (1 << 31) // (16 * 2 * 64) + 300
+    k = torch.empty(1, pages, 16, 2, 64, dtype=BF, device="cuda")
+    v = torch.empty_like(k)
+    ids = torch.arange(pages - 7, pages, device="cuda")
+    g = torch.Generator("cuda").manual_seed(5)
+    k[0, ids] = torch.randn(7, 16, 2, 64, generator=g, device="cuda").to(BF)
+    v[0, ids] = torch.randn(7, 16, 2, 64, generator=g, device="cuda").to(BF)
+    q = torch.randn(33, 4, 64, generator=g, device="cuda").to(BF)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    for new in (1, 33):
+        tables = ids.int().view(1, 7).contiguous()
+        pool = KV.KVPool(k, v, num_q_heads=4, max_requests=1, max_tokens=33, max_row_pages=7)
+        pool.plan(dev([0, new]), dev([110]), tables, new)
+        out = pool.attention(0, q[:new], 0.125)
+        pool.check()
+        want, _, spread, size = attention(q[:new], k[0], v[0], [0, new], [110], tables, 0.125, True)
+        assert ((out.double() - want).abs() <= attention_bound(want, spread, size, BF, 64, 110, 1.0)).all()
+
+
+@pytest.mark.parametrize("what", ["offset", "last", "length", "page", "negative", "group"])
+def test_bad_batches_are_reported_and_write_nothing(what):
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 20, 16, 1, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=2, max_requests=3, max_tokens=8, max_row_pages=4)
+    qo, kv, go = [0, 1, 3, 4], [20, 30, 64], [0, 2, 3]
+    tables = np.arange(12).reshape(3, 4)
+    if what == "offset":
+        qo = [0, 3, 1, 4]
+    elif what == "last":
+        qo = [0, 1, 3, 5]
+    elif what == "length":
+        kv = [20, 65, 64]
+    elif what == "page":
+        tables[2, 3] = 20
+    elif what == "negative":
+        tables[0, 0] = -1
+    else:
+        go = [0, 3, 2]
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    out = torch.full((4, 2, 64), 3.0, dtype=BF, device="cuda")
+    q = torch.randn(4, 2, 64, device="cuda").to(BF)
+    pool.plan(dev(qo), dev(kv), dev(tables), 4, group_offsets=dev(go))
+    pool.attention(0, q, 0.125, out=out)
+    with pytest.raises(RuntimeError, match="invalid argument"):
+        pool.check()
+    assert (out == 3.0).all()
+    # the handle goes on
+    pool.plan(dev([0, 1, 3, 4]), dev([20, 30, 64]), dev(np.arange(12).reshape(3, 4)), 4)
+    pool.attention(0, q, 0.125, out=out)
+    pool.check()
+    assert not (out == 3.0).any()
+
+
+def test_refusals():
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 8, 16, 2, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=4, max_requests=2, max_tokens=4, max_row_pages=4)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    q = torch.zeros(4, 4, 64, dtype=BF, device="cuda")
+    with pytest.raises(ValueError):
+        pool.attention(0, q, 1.0)                                       # no plan
+    with pytest.raises(RuntimeError):
+        pool.plan(dev([0, 1, 2, 3]), dev([1, 1, 1]), torch.zeros(3, 4, dtype=torch.int32, device="cuda"), 3)  # requests
+    with pytest.raises(RuntimeError):
+        pool.plan(dev([0, 5]), dev([5]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 5)             # tokens
+    pool.plan(dev([0, 4]), dev([4]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 4)
+    for bad in (q.half(), q[:3], torch.zeros(4, 2, 64, dtype=BF, device="cuda"), q.cpu(),
+                torch.zeros(4, 4, 68, dtype=BF, device="cuda")[..., 4:]):
+        with pytest.raises(ValueError):
+            pool.attention(0, bad, 1.0)
+    for bad in (math.inf, math.nan):
+        with pytest.raises(RuntimeError):
+            pool.attention(0, q, bad)
+    with pytest.raises(RuntimeError):
+        pool.attention(1, q, 1.0)                                       # layer
+    for kw in (dict(num_q_heads=3), dict(num_q_heads=4, first_page=9), dict(num_q_heads=4, max_tokens=0)):
+        with pytest.raises(ValueError):
+            KV.KVPool(k, v, **kw)
+    with pytest.raises(ValueError):
+        KV.KVPool(k.float(), v.float(), num_q_heads=4)
+    with pytest.raises(ValueError):
+        KV.KVPool(*make_pool(1, 8, 16, 2, 136, BF), num_q_heads=4)       # head size
+    with pytest.raises(ValueError):
+        KV.KVPool(*make_pool(1, 8, 12, 2, 64, BF), num_q_heads=4)        # page size
