@@ -53,7 +53,7 @@ typedef struct {
   void* k;
   void* v;
   int64_t num_pages;      /* page ids are [0, num_pages), at most 2^30 */
-  int64_t first_page;     /* first private page, 0..num_pages */
+  int64_t first_page;     /* first private page; from num_pages on: there are none */
   int64_t layer_stride, page_stride, token_stride, head_stride; /* in elements */
   int32_t num_layers;
   int32_t page_size;      /* tokens: 2, 4, 8, 16, 32 or 64, as ps_create()'s block_size */
@@ -62,7 +62,7 @@ typedef struct {
   int32_t head_dim;       /* a multiple of 8, 8..PS_KV_MAX_HEAD_DIM */
   int32_t dtype;          /* ps_kv_dtype_t */
   int32_t max_requests;   /* rows of a batch, and items of one page call: 1..2^18 - 1 */
-  int32_t max_tokens;     /* query tokens of a batch, 1..2^22 */
+  int32_t max_tokens;     /* query tokens of a batch, 1..2^22, and max_tokens * num_q_heads < 2^30 */
   int32_t max_row_pages;  /* pages of one request: max_row_pages * page_size < 2^30 */
   int32_t pad0;
 } ps_kv_config_t;
@@ -115,7 +115,7 @@ typedef struct {
   float eps;                 /* > 0 */
   int32_t num_tokens;        /* T, any number >= 0 */
   int32_t rope_rows;
-  int32_t rope_dim;          /* rotated leading elements of a head: a multiple of 16, at most head_dim */
+  int32_t rope_dim;          /* rotated leading elements of a head: a multiple of 8, at most head_dim */
   int32_t rope_interleaved;  /* pairs (2i, 2i + 1) instead of (i, i + rope_dim / 2) */
   int32_t pad0;
 } ps_kv_append_t;
@@ -160,7 +160,8 @@ int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* batch, int32_
  * e, on 16-byte boundaries with strides that are multiples of 8 elements.
  * lse (NULL: none): float [num_tokens][num_q_heads], log of the sum of the
  * exponentials of a query's scaled scores.  Results do not depend on timing:
- * the same call gives the same bits. */
+ * the same call gives the same bits.  *d_status: PS_ERR_TIMEOUT if a wait inside
+ * the kernel ran out (never expected). */
 typedef struct {
   const void* q;
   void* out;
@@ -169,7 +170,7 @@ typedef struct {
   float scale;
   int32_t pad0;
 } ps_kv_attention_t;
-int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a);
+int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a, int32_t* d_status);
 
 /* Copy whole pages, all layers: page d_dst[i] becomes a copy of page d_src[i].
  * The destinations are distinct and none is a source.  An id out of range

@@ -188,7 +188,7 @@ def load():
     L.ps_kv_plan.restype = i32
     L.ps_kv_plan.argtypes = [vp, vp, C.POINTER(PsKvBatch), vp]
     L.ps_kv_attention.restype = i32
-    L.ps_kv_attention.argtypes = [vp, vp, i32, C.POINTER(PsKvAttention)]
+    L.ps_kv_attention.argtypes = [vp, vp, i32, C.POINTER(PsKvAttention), vp]
     L.ps_kv_copy.restype = i32
     L.ps_kv_copy.argtypes = [vp, vp, i32, vp, vp, vp]
     L.ps_kv_fork.restype = i32

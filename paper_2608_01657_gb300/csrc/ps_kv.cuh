@@ -42,7 +42,7 @@ struct __align__(32) Tile {
   int32_t kv1;
   int32_t req;
   int32_t ctx;    // row r of the item sees the keys < ctx + 1 + r / ratio
-  int32_t sidx;   // index of (tile, head 0) among the shared (tile, head)s, -1: not shared
+  int32_t sidx;   // rows of the shared (tile, head)s before (tile, head 0), -1: not shared
 };
 
 struct ReqRec {
@@ -54,7 +54,7 @@ struct ReqRec {
 };
 
 constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen05)
-__host__ __device__ constexpr int tile_rows(int list) { return list ? 128 : 16; }
+__host__ __device__ constexpr int tile_rows(int list) { return list ? 256 : 16; }
 __host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 64; }
 constexpr int kNoMask = 1 << 30;
 
@@ -62,7 +62,6 @@ struct PlanHdr {
   int32_t status;       // PS_OK, or why the plan is empty
   int32_t join;         // some rows have partial results
   int32_t ntiles[kLists];
-  int32_t nshared[kLists];  // shared (tile, head)s
   int32_t ctas[kLists];     // C, 0 without tiles
   int64_t units[kLists];    // U
 };
@@ -72,17 +71,15 @@ struct PlanHdr {
 constexpr int kShareRows = 64;
 constexpr int kMaxSms = 160;
 
-// Tiles of one list, and (tile, kv head)s per kv head whose rows have a shared
-// prefix, for at most R requests of at most 'rows' rows in all.  An item (a
-// request's own keys, or a group's prefix; at most R of each) of x rows has at
-// most 1 + x / H tiles.
+// Tiles of one list, and rows of one kv head that have a shared prefix (in its
+// tiles, and in their own), for at most R requests of at most 'rows' rows in
+// all.  An item (a request's own keys, or a group's prefix; at most R of each)
+// of x rows has at most 1 + x / H tiles.
 struct PlanBounds {
   int64_t tiles, shared;
 };
 inline PlanBounds plan_bounds(int list, int64_t R, int64_t rows) {
-  const int H = tile_rows(list);
-  const int64_t srows = rows < R * kShareRows ? rows : R * kShareRows;
-  return {2 * (R + rows / H) + 2, 2 * (R + srows / H) + 2};
+  return {2 * (R + rows / tile_rows(list)) + 2, 2 * (rows < R * kShareRows ? rows : R * kShareRows)};
 }
 
 // The CTA of unit u: the largest c with floor(U c / C) <= u.
@@ -102,18 +99,20 @@ struct Plan {
   Tile* tiles[kLists];
   int64_t* ucum[kLists];      // [tiles + 1] units before a tile, all heads
   int32_t* cta_tile[kLists];  // [C] tile of a CTA's first unit
-  float* part_o[kLists];      // [slots][tile rows][head_dim]
-  float2* part_ml[kLists];    // [slots][tile rows] (maximum, sum), base 2
-  int32_t max_tiles[kLists], max_slots[kLists], max_ctas[kLists];
+  float* part_o[kLists];      // [rows][head_dim] unnormalized outputs, see part_row
+  float2* part_ml[kLists];    // [rows] (maximum, sum), base 2
+  int32_t max_ctas[kLists];
 };
 
-// The partial-result slot of a (tile, head)'s part that CTA c computed.  A CTA
-// leaves at most two partial results of (tile, head)s that are not shared: of
-// the one it continues and of the one it leaves unfinished.  Along the list of
-// shared (tile, head)s neither the index i nor c ever decreases and one of them
-// grows from each part to the next, so i + c is a slot of its own.
-__host__ __device__ __forceinline__ int part_slot(int sidx, int head, int c, bool continued, int C) {
-  return sidx >= 0 ? 2 * C + sidx + head + c : 2 * c + (continued ? 0 : 1);
+// The first row of the partial results of a (tile, head)'s part that CTA c
+// computed.  A CTA leaves at most two partial results of (tile, head)s that are
+// not shared, of the one it continues and of the one it leaves unfinished: two
+// places of H rows each.  Along the list of shared (tile, head)s neither the
+// rows before one nor c ever decreases, and one of them grows by as much as a
+// part takes from each part to the next.
+template <int H>
+__host__ __device__ __forceinline__ int64_t part_row(int sidx, int nrows, int head, int c, bool continued, int C) {
+  return sidx >= 0 ? (int64_t)(2 * C + c) * H + sidx + (int64_t)head * nrows : (int64_t)(2 * c + (continued ? 0 : 1)) * H;
 }
 
 struct Batch {
@@ -161,6 +160,7 @@ template <typename T>
 struct Num;
 template <>
 struct Num<__nv_bfloat16> {
+  static constexpr bool kBf16 = true;
   static __device__ __forceinline__ float2 unpack(uint32_t x) {
     return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
   }
@@ -172,6 +172,7 @@ struct Num<__nv_bfloat16> {
 };
 template <>
 struct Num<__half> {
+  static constexpr bool kBf16 = false;
   static __device__ __forceinline__ float2 unpack(uint32_t x) {
     return __half22float2(*reinterpret_cast<const __half2*>(&x));
   }
@@ -208,7 +209,7 @@ inline int32_t status_of(cudaError_t e) { return e == cudaSuccess ? PS_OK : PS_E
 int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& a, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* status, cudaStream_t st);
 int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& a,
-                         cudaStream_t st);
+                         int32_t* status, cudaStream_t st);
 int32_t launch_copy(const Pool& p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* status, int nsm,
                     cudaStream_t st);
 int32_t launch_fork(const Pool& p, const PageScratch& w, int32_t n, const int32_t* parents, const int32_t* children,

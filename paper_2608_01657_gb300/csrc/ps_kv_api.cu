@@ -24,7 +24,7 @@ inline bool good_strides(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && 
 
 bool check_config(const ps_kv_config_t* c) {
   if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return false;
-  if (c->num_pages < 1 || c->num_pages > (1ll << 30) || c->first_page < 0 || c->first_page > c->num_pages) return false;
+  if (c->num_pages < 1 || c->num_pages > (1ll << 30) || c->first_page < 0) return false;
   const int32_t ps = c->page_size;
   if (ps != 2 && ps != 4 && ps != 8 && ps != 16 && ps != 32 && ps != 64) return false;
   for (int64_t s : {c->layer_stride, c->page_stride, c->token_stride, c->head_stride})
@@ -35,7 +35,7 @@ bool check_config(const ps_kv_config_t* c) {
   if (c->head_dim < 8 || c->head_dim > PS_KV_MAX_HEAD_DIM || c->head_dim % 8 != 0) return false;
   if (c->dtype != PS_KV_BF16 && c->dtype != PS_KV_F16) return false;
   if (c->max_requests < 1 || c->max_requests > PS_MAX_REQUESTS_PER_STEP) return false;
-  if (c->max_tokens < 1 || c->max_tokens > (1 << 22) || (int64_t)c->max_tokens * c->num_q_heads >= (1ll << 31))
+  if (c->max_tokens < 1 || c->max_tokens > (1 << 22) || (int64_t)c->max_tokens * c->num_q_heads >= (1ll << 30))
     return false;
   if (c->max_row_pages < 1 || (int64_t)c->max_row_pages * ps >= (1ll << 30)) return false;
   return true;
@@ -45,7 +45,8 @@ Pool make_pool(const ps_kv_config_t& c) {
   Pool p{};
   p.k = static_cast<char*>(c.k);
   p.v = static_cast<char*>(c.v);
-  p.num_pages = c.num_pages; p.first_page = c.first_page;
+  p.num_pages = c.num_pages;
+  p.first_page = c.first_page < c.num_pages ? c.first_page : c.num_pages;  // no private pages past the end
   p.layer_stride = c.layer_stride; p.page_stride = c.page_stride;
   p.token_stride = c.token_stride; p.head_stride = c.head_stride;
   p.num_layers = c.num_layers; p.page_size = c.page_size;
@@ -74,7 +75,7 @@ size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Pl
   const int64_t R = c.max_requests, T = c.max_tokens, ratio = c.num_q_heads / c.num_kv_heads;
   PageScratch w{};
   w.hdr = cv.take<PageHdr>(1);
-  const int64_t np = c.num_pages - c.first_page;
+  const int64_t np = c.first_page < c.num_pages ? c.num_pages - c.first_page : 0;
   // chunks of at least 2048 references, at most kMaxChunks of them
   int64_t chunk = (np + kMaxChunks - 1) / kMaxChunks;
   chunk = chunk < 2048 ? 2048 : (chunk + kScanThreads - 1) / kScanThreads * kScanThreads;
@@ -103,13 +104,12 @@ size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Pl
     const PlanBounds b = plan_bounds(l, R, T * ratio);
     const int64_t shared = b.shared * c.num_kv_heads;
     p.max_ctas[l] = ctas[l];
-    p.max_tiles[l] = (int32_t)b.tiles;
-    p.max_slots[l] = (int32_t)(3 * (int64_t)ctas[l] + shared);
+    const size_t part_rows = (size_t)(3 * (int64_t)ctas[l] * tile_rows(l) + shared);
     p.tiles[l] = cv.take<Tile>((size_t)b.tiles);
     p.ucum[l] = cv.take<int64_t>((size_t)b.tiles + 1);
     p.cta_tile[l] = cv.take<int32_t>((size_t)ctas[l]);
-    p.part_o[l] = cv.take<float>((size_t)p.max_slots[l] * tile_rows(l) * c.head_dim);
-    p.part_ml[l] = cv.take<float2>((size_t)p.max_slots[l] * tile_rows(l));
+    p.part_o[l] = cv.take<float>(part_rows * c.head_dim);
+    p.part_ml[l] = cv.take<float2>(part_rows);
   }
   if (plan) *plan = p;
   if (pages) *pages = w;
@@ -180,7 +180,7 @@ int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_appen
       !good_strides(a->q_out_stride))
     return PS_ERR_INVALID_ARG;
   if ((a->q_weight || a->k_weight) && !(a->eps > 0)) return PS_ERR_INVALID_ARG;
-  if (a->rope && (!a->positions || a->rope_rows < 1 || a->rope_dim < 16 || a->rope_dim % 16 != 0 ||
+  if (a->rope && (!a->positions || a->rope_rows < 1 || a->rope_dim < 8 || a->rope_dim % 8 != 0 ||
                   a->rope_dim > kv->pool.head_dim))
     return PS_ERR_INVALID_ARG;
   return launch_append(kv->pool, layer, *a, d_status, kv->nsm, as_stream(stream));
@@ -206,13 +206,14 @@ int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* b, int32_t* d
   return rc;
 }
 
-int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a) {
+int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a,
+                        int32_t* d_status) {
   if (!kv || !a || !kv->planned || layer < 0 || layer >= kv->pool.num_layers) return PS_ERR_INVALID_ARG;
   if (kv->batch.num_tokens == 0 || kv->batch.num_requests == 0) return PS_OK;
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) || !good_strides(a->q_stride) ||
       !good_strides(a->out_stride) || !(a->scale - a->scale == 0))
     return PS_ERR_INVALID_ARG;
-  return launch_attention(kv->pool, kv->plan, kv->batch, layer, *a, as_stream(stream));
+  return launch_attention(kv->pool, kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
 }
 
 int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,

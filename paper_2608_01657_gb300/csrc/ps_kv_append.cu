@@ -24,7 +24,7 @@ struct AppendArgs {
 // Bound by HBM: every element is read once and written once.  A head's
 // elements are held by G = 8 or 16 lanes, 8 elements (16 bytes) each, so the
 // sum of squares is a shuffle over G lanes, and a pair's partner is either in
-// the lane itself (interleaved) or rope_dim / 16 lanes away.  A group of lanes
+// the lane itself (interleaved) or rope_dim / 2 elements away.  A group of lanes
 // takes several heads of one token, so that the token's cosines and sines are
 // read once into registers; a CTA's blockIdx.y takes a slice of the heads
 // (queries, then keys, then values).
@@ -42,20 +42,30 @@ __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
     return;
   }
   const bool on = lane * 8 < a.dim;
-  const int half = a.rope_dim / 16;  // lanes of half the rotated elements
-  const bool rotated = lane < 2 * half;
+  // Rotated elements in quarter words of four: quarter g is one of the lane's
+  // two, g = 2 lane + s; without interleaving its partner is 'half' quarters
+  // up or down (in the lane's other place where half is odd).
+  const int half = a.rope_dim / 8;
+  const bool odd = half & 1;
   // this lane's cosines and sines: of its own 8 elements, or of its 4 pairs
   constexpr int NC = INTERLEAVED ? 4 : 8;
   float cs[NC], sn[NC];
-  if (a.rope && rotated) {
-    const float* row = a.rope + (int64_t)pos * a.rope_dim;
-    const int c0 = INTERLEAVED ? lane * 4 : (lane % half) * 8;
 #pragma unroll
-    for (int i = 0; i < NC; i += 4) {
-      const float4 c = __ldg(reinterpret_cast<const float4*>(row + c0 + i));
-      const float4 s = __ldg(reinterpret_cast<const float4*>(row + a.rope_dim / 2 + c0 + i));
-      cs[i] = c.x; cs[i + 1] = c.y; cs[i + 2] = c.z; cs[i + 3] = c.w;
-      sn[i] = s.x; sn[i + 1] = s.y; sn[i + 2] = s.z; sn[i + 3] = s.w;
+  for (int s = 0; s < NC / 4; ++s) {
+    const int g = INTERLEAVED ? lane : 2 * lane + s;
+    const int at = INTERLEAVED || g < half ? g : g - half;
+    if (a.rope && at < half) {
+      const float* row = a.rope + (int64_t)pos * a.rope_dim + 4 * at;
+      const float4 c = __ldg(reinterpret_cast<const float4*>(row));
+      const float4 x = __ldg(reinterpret_cast<const float4*>(row + a.rope_dim / 2));
+      cs[4 * s] = c.x; cs[4 * s + 1] = c.y; cs[4 * s + 2] = c.z; cs[4 * s + 3] = c.w;
+      sn[4 * s] = x.x; sn[4 * s + 1] = x.y; sn[4 * s + 2] = x.z; sn[4 * s + 3] = x.w;
+    } else {  // not rotated
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        cs[4 * s + i] = 1.0f;
+        sn[4 * s + i] = 0.0f;
+      }
     }
   }
   const int64_t at = slot < 0 ? 0 : (slot >> a.page_log2) * a.page_stride +
@@ -96,7 +106,7 @@ __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
     }
     if (a.rope) {
       if (INTERLEAVED) {
-        if (kind < 2 && rotated) {
+        if (kind < 2 && lane < half) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float u = x[2 * i], w = x[2 * i + 1];
@@ -105,13 +115,22 @@ __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
           }
         }
       } else {
-        // the partner's elements: half lanes up for the first half, down for the second
-        const int peer = lane < half ? lane + half : (rotated ? lane - half : lane);
-        const float sign = lane < half ? -1.0f : 1.0f;
+        float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float o = __shfl_sync(0xFFFFFFFFu, x[i], peer, G);
-          if (kind < 2 && rotated) x[i] = x[i] * cs[i % NC] + sign * o * sn[i % NC];
+        for (int s = 0; s < 2; ++s) {
+          const int g = 2 * lane + s;
+          const int peer = g < half ? g + half : (g < 2 * half ? g - half : g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            o[4 * s + i] = __shfl_sync(0xFFFFFFFFu, odd ? x[4 * (1 - s) + i] : x[4 * s + i], peer >> 1, G);
+        }
+        if (kind < 2) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int g = 2 * lane + i / 4;
+            if (g < half) x[i] = x[i] * cs[i % NC] - o[i] * sn[i % NC];
+            else if (g < 2 * half) x[i] = x[i] * cs[i % NC] + o[i] * sn[i % NC];
+          }
         }
       }
     }

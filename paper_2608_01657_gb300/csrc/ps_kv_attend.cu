@@ -316,9 +316,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
           }
         }
       } else {
-        const int64_t slot = part_slot(t.sidx, head, c, first > 0, C);
-        float* po = a.plan.part_o[0] + slot * H * a.pool.head_dim;
-        float2* pml = a.plan.part_ml[0] + slot * H;
+        const int64_t prow = part_row<H>(t.sidx, t.nrows, head, c, first > 0, C);
+        float* po = a.plan.part_o[0] + prow * a.pool.head_dim;
+        float2* pml = a.plan.part_ml[0] + prow;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           const int r = g + 8 * hf;
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
     const int rr = side ? rec.prow0 + row : row;
     const int H = tile_rows(list);
     const int tile = tile0 + rr / H, r = rr % H;
-    const int sidx = a.plan.tiles[list][tile].sidx;
+    const int sidx = a.plan.tiles[list][tile].sidx, nrows = a.plan.tiles[list][tile].nrows;
     const int64_t U = hdr->units[list], b = a.plan.ucum[list][tile];
     const int C = hdr->ctas[list];
     const int64_t nu = (a.plan.ucum[list][tile + 1] - b) / a.pool.kv_heads;
@@ -383,11 +383,13 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
     parts = true;
     // a CTA's range may begin exactly with this (tile, head)
     for (int c = ca; c <= cb; ++c) {
-      const int64_t slot = part_slot(sidx, head, c, U * c / C > ua, C);
-      const float2 ml = a.plan.part_ml[list][slot * H + r];
+      const bool continued = U * c / C > ua;
+      const int64_t prow = r + (list ? part_row<tile_rows(1)>(sidx, nrows, head, c, continued, C)
+                                     : part_row<tile_rows(0)>(sidx, nrows, head, c, continued, C));
+      const float2 ml = a.plan.part_ml[list][prow];
       float4 x = make_float4(0, 0, 0, 0);
       if (lane * 4 < dim)
-        x = *reinterpret_cast<const float4*>(a.plan.part_o[list] + (slot * H + r) * dim + lane * 4);
+        x = *reinterpret_cast<const float4*>(a.plan.part_o[list] + prow * dim + lane * 4);
       const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
       const float f0 = ex2(m - ms), f1 = ex2(ml.x - ms);
       o.x = o.x * f0 + x.x * f1;
@@ -434,12 +436,14 @@ cudaError_t configure_t(int d, int nsm, int32_t* ctas) {
 
 int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]) {
   ctas[1] = nsm;
+  const cudaError_t e = configure_wide(p);
+  if (e != cudaSuccess) return status_of(e);
   return status_of(p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim, nsm, ctas)
                                          : configure_t<__half>(p.head_dim, nsm, ctas));
 }
 
 int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& in,
-                         cudaStream_t st) {
+                         int32_t* status, cudaStream_t st) {
   AttendArgs a{};
   a.pool = p;
   a.plan = plan;
@@ -455,9 +459,11 @@ int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_
   a.tables = b.tables;
   a.table_stride = b.table_stride;
   a.q_offsets = b.q_offsets;
+  a.status = status;
   a.num_tokens = b.num_tokens;
   a.scale2 = in.scale * 1.4426950408889634f;
-  cudaError_t e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
+  cudaError_t e = launch_wide(a, st);
+  if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
   if (e != cudaSuccess) return status_of(e);
   const int64_t warps = (int64_t)b.num_tokens * p.q_heads;
   const dim3 grid((unsigned)((warps + 7) / 8));

@@ -16,6 +16,7 @@ struct AttendArgs {
   const int32_t* tables;
   int64_t table_stride;
   const int32_t* q_offsets;
+  int32_t* status;
   int32_t num_tokens;
   float scale2;  // scale log2(e)
 };
@@ -24,5 +25,9 @@ struct AttendArgs {
 __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0 ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
+
+// The wide tiles' kernel (ps_kv_attend_wide.cu).
+cudaError_t launch_wide(const AttendArgs& a, cudaStream_t st);
+cudaError_t configure_wide(const Pool& p);
 
 }  // namespace pskv

@@ -119,16 +119,14 @@ __device__ __forceinline__ int tile_end(const Item& it, const Pool& p, int last_
 }
 __device__ __forceinline__ int unit_count(int keys, int unit) { return keys > 0 ? (keys + unit - 1) / unit : 1; }
 
-__device__ __forceinline__ int list_of(int rows) {
-  (void)rows;
-  return 0;
-}
+// More rows than a narrow tile's 16 go to the wide tiles.
+__device__ __forceinline__ int list_of(int rows) { return rows > tile_rows(0) ? 1 : 0; }
 
 __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, Batch b, int32_t* status) {
   chain();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ int s_bad, s_join;
-  if (tid == 0) s_bad = s_join = 0;
+  __shared__ int s_join;
+  if (tid == 0) s_join = 0;
   __syncthreads();
   int bad = 0;
   for (int r = tid; r < b.num_requests; r += kPlanThreads) bad |= plan.bad[r];
@@ -214,7 +212,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
       e = scan64(mine ? nu * p.kv_heads : 0, &tot);
       if (mine) unit_at = units[l] + e;
       units[l] += tot;
-      e = scan64(mine && it.shared ? (int64_t)nt * p.kv_heads : 0, &tot);
+      e = scan64(mine && it.shared ? (int64_t)it.rows * p.kv_heads : 0, &tot);
       if (mine) shared_at = shared[l] + e;
       shared[l] += tot;
     }
@@ -228,7 +226,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
       x.kv1 = tile_end(it, p, last);
       x.req = it.req;
       x.ctx = it.ctx;
-      x.sidx = it.shared ? (int)shared_at + t * p.kv_heads : -1;
+      x.sidx = it.shared ? (int)shared_at + t * H * p.kv_heads : -1;
       plan.tiles[it.list][tile_at + t] = x;
       plan.ucum[it.list][tile_at + t] = unit_at;
       unit_at += (int64_t)unit_count(x.kv1 - x.kv0, unit) * p.kv_heads;
@@ -281,7 +279,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
     h.join = s_join;
     for (int l = 0; l < kLists; ++l) {
       h.ntiles[l] = (int)tiles[l];
-      h.nshared[l] = (int)shared[l];
       h.ctas[l] = ctas[l];
       h.units[l] = units[l];
     }

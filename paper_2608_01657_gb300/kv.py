@@ -172,7 +172,8 @@ class KVPool:
             _need(lse.dtype == torch.float32 and tuple(lse.shape) == (T, self.q_heads) and lse.is_contiguous()
                   and lse.device == self.device, "lse must be contiguous float32 [tokens, q_heads]")
             a.lse = lse.data_ptr()
-        self._raise("ps_kv_attention", B.load().ps_kv_attention(self._h, B._stream_ptr(stream), int(layer), C.byref(a)))
+        self._raise("ps_kv_attention", B.load().ps_kv_attention(self._h, B._stream_ptr(stream), int(layer), C.byref(a),
+                                                                self.status.data_ptr()))
         return out
 
     # -- pages -------------------------------------------------------------------
@@ -193,7 +194,7 @@ class KVPool:
 
     def _refs(self, refs, name="refs"):
         import torch
-        return self._array(refs, torch.int32, name, self.pages - self.first_page)
+        return self._array(refs, torch.int32, name, max(0, self.pages - self.first_page))
 
     def fork(self, parents, children, room, tables, lens, held, refs, refs_out=None, stream=None):
         """Rows ``children`` become continuations of rows ``parents`` with

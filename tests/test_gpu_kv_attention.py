@@ -271,7 +271,7 @@ def test_refusals():
             pool.attention(0, q, bad)
     with pytest.raises(RuntimeError):
         pool.attention(1, q, 1.0)                                       # layer
-    for kw in (dict(num_q_heads=3), dict(num_q_heads=4, first_page=9), dict(num_q_heads=4, max_tokens=0)):
+    for kw in (dict(num_q_heads=3), dict(num_q_heads=4, first_page=-1), dict(num_q_heads=4, max_tokens=0)):
         with pytest.raises(ValueError):
             KV.KVPool(k, v, **kw)
     with pytest.raises(ValueError):

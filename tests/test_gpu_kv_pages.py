@@ -91,6 +91,13 @@ def test_append_parts(qn, kn, rope_dim):
     check_append(9, 1, 1, 96, 2, HF, rope_dim=rope_dim, interleaved=True, qn=qn, kn=kn, inplace=True, seed=4)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rope_dim", [(80, 40), (64, 8), (64, 24), (128, 120), (8, 8), (72, 72)])
+def test_append_odd_rotations(dim, rope_dim, interleaved):
+    """Rotated parts whose halves end inside a 16-byte word."""
+    check_append(6, 2, 2, dim, 16, BF, rope_dim=rope_dim, interleaved=interleaved, seed=rope_dim)
+
+
 def test_append_many_heads():
     check_append(3, 40, 2, 128, 16, BF, rope_dim=128, seed=6)
     check_append(600, 1, 1, 64, 64, BF, rope_dim=64, skip=(5, 599), seed=7)
@@ -138,7 +145,7 @@ def test_append_refusals():
         args = dict(q=x, k=x, v=x, slots=s) | b
         with pytest.raises(ValueError):
             pool.append(0, **args)
-    for b in (dict(rope=rope_table(4, 24)), dict(rope=rope_table(4, 80)), dict(q_weight=torch.ones(64, device="cuda", dtype=BF), eps=0.0)):
+    for b in (dict(rope=rope_table(4, 20)), dict(rope=rope_table(4, 80)), dict(q_weight=torch.ones(64, device="cuda", dtype=BF), eps=0.0)):
         with pytest.raises(RuntimeError):
             pool.append(0, x, x, x, s, positions=pos, **b)
     with pytest.raises(RuntimeError):

@@ -71,7 +71,7 @@ def test_workspace_grows_with_the_bounds(B):
 
 @pytest.mark.parametrize("bad", [
     dict(k=None), dict(v=None), dict(k=(1 << 20) + 8), dict(num_pages=0), dict(num_pages=(1 << 30) + 1), dict(first_page=-1),
-    dict(first_page=65), dict(page_size=0), dict(page_size=12), dict(page_size=128), dict(page_stride=-8),
+    dict(page_size=0), dict(page_size=12), dict(page_size=128), dict(page_stride=-8),
     dict(token_stride=12), dict(head_stride=63), dict(layer_stride=4), dict(num_layers=0), dict(num_kv_heads=0),
     dict(num_q_heads=3), dict(num_q_heads=1), dict(num_q_heads=1026), dict(head_dim=0), dict(head_dim=12), dict(head_dim=136),
     dict(dtype=2), dict(max_requests=0), dict(max_requests=1 << 18), dict(max_tokens=0), dict(max_tokens=(1 << 22) + 1),
@@ -91,7 +91,7 @@ def test_null_and_misaligned_arguments_are_refused(B):
     assert L.ps_kv_create(C.byref(h), C.byref(c), 1 << 20, n - 1, None) == bad
     assert L.ps_kv_append(None, None, 0, C.byref(B.PsKvAppend()), None) == bad
     assert L.ps_kv_plan(None, None, C.byref(B.PsKvBatch()), None) == bad
-    assert L.ps_kv_attention(None, None, 0, C.byref(B.PsKvAttention())) == bad
+    assert L.ps_kv_attention(None, None, 0, C.byref(B.PsKvAttention()), None) == bad
     assert L.ps_kv_copy(None, None, 0, None, None, None) == bad
     assert L.ps_kv_fork(None, None, 0, None, None, None, C.byref(B.PsKvRows()), None, None, None) == bad
     assert L.ps_kv_release(None, None, 0, None, C.byref(B.PsKvRows()), None, None) == bad
