@@ -4,6 +4,7 @@
 // carved scratch pointers and the call's own pointers.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -115,6 +116,15 @@ __host__ __device__ __forceinline__ int64_t part_row(int sidx, int nrows, int he
   return sidx >= 0 ? (int64_t)(2 * C + c) * H + sidx + (int64_t)head * nrows : (int64_t)(2 * c + (continued ? 0 : 1)) * H;
 }
 
+// Tensor maps of the pool's keys and values: (element, head, token, page, layer),
+// a box of 64 elements of min(page_size, 32) tokens.
+struct PoolMaps {
+  CUtensorMap k, v;
+  int32_t ok;  // 0: pages of fewer than 8 tokens, or no maps
+  int32_t box;
+};
+bool make_maps(const Pool& p, PoolMaps* m);
+
 struct Batch {
   const int32_t *q_offsets, *kv_lens, *tables, *group_offsets;
   int64_t table_stride;
@@ -208,7 +218,7 @@ inline int32_t status_of(cudaError_t e) { return e == cudaSuccess ? PS_OK : PS_E
 
 int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& a, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* status, cudaStream_t st);
-int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& a,
+int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& a,
                          int32_t* status, cudaStream_t st);
 int32_t launch_copy(const Pool& p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* status, int nsm,
                     cudaStream_t st);

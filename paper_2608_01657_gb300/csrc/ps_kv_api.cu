@@ -9,6 +9,7 @@ using namespace pskv;
 
 struct ps_kv {
   Pool pool;
+  PoolMaps maps;
   Plan plan;
   PageScratch pages;
   Batch batch;
@@ -147,6 +148,7 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   ps_kv* kv = new (std::nothrow) ps_kv{};
   if (!kv) return PS_ERR_CUDA;
   kv->pool = make_pool(*cfg);
+  make_maps(kv->pool, &kv->maps);
   kv->nsm = nsm < kMaxSms ? nsm : kMaxSms;
   kv->max_requests = cfg->max_requests;
   kv->max_tokens = cfg->max_tokens;
@@ -213,7 +215,7 @@ int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_at
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) || !good_strides(a->q_stride) ||
       !good_strides(a->out_stride) || !(a->scale - a->scale == 0))
     return PS_ERR_INVALID_ARG;
-  return launch_attention(kv->pool, kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
+  return launch_attention(kv->pool, kv->maps, kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
 }
 
 int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,

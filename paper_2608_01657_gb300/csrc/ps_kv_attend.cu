@@ -442,8 +442,8 @@ int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]) {
                                          : configure_t<__half>(p.head_dim, nsm, ctas));
 }
 
-int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& in,
-                         int32_t* status, cudaStream_t st) {
+int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer,
+                         const ps_kv_attention_t& in, int32_t* status, cudaStream_t st) {
   AttendArgs a{};
   a.pool = p;
   a.plan = plan;
@@ -461,8 +461,9 @@ int32_t launch_attention(const Pool& p, const Plan& plan, const Batch& b, int32_
   a.q_offsets = b.q_offsets;
   a.status = status;
   a.num_tokens = b.num_tokens;
+  a.layer = layer;
   a.scale2 = in.scale * 1.4426950408889634f;
-  cudaError_t e = launch_wide(a, st);
+  cudaError_t e = launch_wide(a, maps, st);
   if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
   if (e != cudaSuccess) return status_of(e);
   const int64_t warps = (int64_t)b.num_tokens * p.q_heads;

@@ -1,6 +1,8 @@
 // Arguments and helpers of the attention kernels (narrow and wide tiles).
 #pragma once
 
+#include <cuda.h>
+
 #include "ps_kv.cuh"
 
 namespace pskv {
@@ -17,7 +19,7 @@ struct AttendArgs {
   int64_t table_stride;
   const int32_t* q_offsets;
   int32_t* status;
-  int32_t num_tokens;
+  int32_t num_tokens, layer;
   float scale2;  // scale log2(e)
 };
 
@@ -27,7 +29,7 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 }
 
 // The wide tiles' kernel (ps_kv_attend_wide.cu).
-cudaError_t launch_wide(const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& maps, cudaStream_t st);
 cudaError_t configure_wide(const Pool& p);
 
 }  // namespace pskv

@@ -4,10 +4,14 @@
 // The mathematics is the narrow tiles' (ps_kv_attend.cu).  One CTA an SM takes
 // its part of the list of units; a unit is 128 keys.  Its warps:
 //   8 softmax warps, two groups t of four, a thread a query row;
-//   4 loader warps, gathering queries, keys and values from their pages with
-//     16-byte asynchronous copies (pages end anywhere inside a unit, and what
-//     lies past a request's end must read as zero, which the copies fill in);
-//   1 warp whose first lane issues the matrix instructions (3 more idle).
+//   4 loader warps, each with a quarter of every unit's keys and values: whole
+//     units by TMA, a box for a page (or half a page of 64) and 64 elements.  A
+//     request's last unit, whose values past its end must read as zero, queries,
+//     and pages of 2 or 4 tokens, whose boxes would not fill the 1024 bytes after
+//     which the swizzle repeats, go by 16-byte asynchronous copies instead, eight
+//     times the instructions and waited for by the copying threads: with them for
+//     all units the loader warps took 7400 cycles a unit, the products 2350;
+//   1 warp that issues the matrix instructions (3 more idle).
 // A tile of more than 128 rows is two row blocks, one for each group, that use
 // every unit's keys and values (pair mode).  A tile of up to 128 rows is one
 // row block; the groups take its units in turn, each with a softmax of its own
@@ -83,6 +87,7 @@ __device__ __forceinline__ bool warp_wait(Shared* sh, uint64_t* b, uint32_t pari
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// The commits and products below are one thread's.
 __device__ __forceinline__ void tc_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
 }
@@ -114,6 +119,32 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* x) {
 }
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Two 32-bit numbers in one 64-bit register, worked on by one instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
@@ -174,112 +205,171 @@ struct Parts {
 };
 
 // ---- loader warps ------------------------------------------------------------------
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int page,
+                                         int layer) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
+}
+
 template <int DP>
-__device__ __forceinline__ bool load_role(const AttendArgs& a, Shared* sh, uint32_t qs, uint32_t ring, Parts ps) {
+struct Loader {
   using S = Shape<DP>;
-  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kSoftmaxWarps;
-  constexpr int CH = DP / 8;              // 16-byte words of a row that hold elements
-  constexpr int RPI = 32 / (CH <= 8 ? 8 : 16);  // rows an instruction covers
-  const int w = lane % (32 / RPI), sub = lane / (32 / RPI);
-  const bool on = w * 8 < a.pool.head_dim, pad = w < CH;
-  // word w of row r: half w / 8, swizzled within its 128 bytes
-  auto place = [&](int r) -> uint32_t { return (uint32_t)((w >> 3) * (128 * 128) + r * 128 + (((w & 7) ^ (r & 7)) << 4)); };
+  static constexpr int CH = DP / 8;                      // 16-byte words of a row that hold elements
+  static constexpr int RPI = 32 / (CH <= 8 ? 8 : 16);    // rows that one copy instruction covers
+  const AttendArgs& a;
+  Shared* sh;
+  const int lane, warp;
+  const int w, sub;  // the lane's word of a row, and row of an instruction's
   uint32_t issued = 0, told = 0;  // blocks issued, blocks whose arrival was signalled
-  auto tell = [&](uint32_t upto) {
+
+  __device__ __forceinline__ Loader(const AttendArgs& args, Shared* s)
+      : a(args), sh(s), lane(threadIdx.x & 31), warp((threadIdx.x >> 5) - kSoftmaxWarps), w(lane % (32 / RPI)), sub(lane / (32 / RPI)) {}
+
+  // 32 rows of the warp's, row r at element off (of lane r; -1: zeros).
+  __device__ __forceinline__ void copy_rows(uint32_t dst, const char* base, int64_t off) const {
+    const bool on = w * 8 < a.pool.head_dim;
+    int64_t o[32 / RPI];
+#pragma unroll
+    for (int j = 0; j < 32 / RPI; ++j) o[j] = __shfl_sync(0xFFFFFFFFu, off, j * RPI + sub);
+#pragma unroll
+    for (int j = 0; j < 32 / RPI; ++j) {
+      const int r = warp * 32 + j * RPI + sub;
+      const bool ok = o[j] >= 0 && on;
+      // word w of row r: half w / 8, swizzled within its 128 bytes
+      if (w < CH)
+        cp16(dst + (w >> 3) * (128 * 128) + r * 128 + (((w & 7) ^ (r & 7)) << 4), base + (ok ? 2 * o[j] + w * 16 : 0), ok);
+    }
+    cp_commit();
+  }
+  __device__ __forceinline__ void tell(uint32_t upto) {
     to_async_proxy();
     __syncwarp();
     for (; told < upto; ++told)
       if (lane == 0) bar_arrive(&sh->full[told % S::kBuffers]);
-  };
-  uint32_t seg = 0;
-  bool more = true;
-  for (; more; ++seg, more = ps.next()) {
-    const Tile& t = ps.t;
-    // queries: rows [64 warp, 64 warp + 64) of the tile's two blocks
-    if (issued > told) {  // what is in flight is not held back by the wait below
+  }
+  __device__ __forceinline__ void tell_all() {
+    if (issued > told) {
       cp_wait<0>();
       tell(issued);
     }
-    if (!warp_wait(sh, &sh->q_empty, (seg & 1) ^ 1)) return false;
-    const int blocks = ps.pair() ? 2 : 1;
-    for (int blk = 0; blk < blocks; ++blk) {
-      const int r0 = blk * 128 + warp * 32;
-      const int rr = t.row0 + r0 + lane;
-      int64_t off = -1;
-      if (r0 + lane < t.nrows)
-        off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
-              (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
-#pragma unroll
-      for (int j = 0; j < 32; j += RPI) {
-        const int64_t o = __shfl_sync(0xFFFFFFFFu, off, j + sub);
-        const bool ok = o >= 0 && on;
-        if (pad) cp16(qs + blk * S::kBlock + place(warp * 32 + j + sub), a.q + (ok ? 2 * o + w * 16 : 0), ok);
-      }
-    }
-    cp_commit();
-    cp_wait<0>();
-    to_async_proxy();
-    __syncwarp();
-    if (lane == 0) bar_arrive(&sh->q_full);
-    // keys and values of the units; this lane's key is number 32 warp + lane of each
+  }
+  // The next block of the ring is free.  What was copied is not held back by the wait.
+  __device__ __forceinline__ bool room() {
+    uint64_t* e = &sh->empty[issued % S::kBuffers];
+    const uint32_t parity = ((issued / S::kBuffers) & 1) ^ 1;
+    if (__all_sync(0xFFFFFFFFu, bar_test(e, parity))) return true;
+    tell_all();
+    return warp_wait(sh, e, parity);
+  }
+};
+
+template <int DP>
+__device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& maps, Shared* sh, uint32_t qs, uint32_t ring, Parts ps) {
+  using S = Shape<DP>;
+  Loader<DP> ld(a, sh);
+  const int lane = ld.lane, warp = ld.warp;
+  const bool tma = maps.ok;
+  // TMA: lane i issues box i % boxes of the warp's keys, half i / boxes
+  const int boxes = 32 / maps.box, mybox = lane % boxes, myhalf = lane / boxes;
+  const bool issues = tma && lane < boxes * S::kHalves;
+  uint32_t seg = 0;
+  bool more = true;
+  for (; more; ++seg, more = ps.next()) {
+    const Tile t = ps.t;
     const int32_t* row = a.tables + t.req * a.table_stride;
     const int64_t head_off = (int64_t)ps.head * a.pool.head_stride;
-    int key = t.kv0 + ps.unit * UNIT + warp * 32 + lane;
-    int page = key < t.kv1 ? __ldg(row + (key >> a.pool.page_log2)) : -1;
+    ld.tell_all();
+    // ids are looked up one unit ahead
+    auto id_of = [&](int u) -> int {
+      const int base = t.kv0 + (ps.unit + u) * UNIT;
+      const bool whole = tma && base + UNIT <= t.kv1;
+      const int key = base + warp * 32 + (whole ? mybox * maps.box : lane);
+      return u < ps.count && key < t.kv1 ? __ldg(row + (key >> a.pool.page_log2)) : -1;
+    };
+    int page = id_of(0);
     for (int u = 0; u < ps.count; ++u) {
-      int64_t off = -1;
-      if (page >= 0)
-        off = page * a.pool.page_stride + (int64_t)(key & (a.pool.page_size - 1)) * a.pool.token_stride + head_off;
-      key += UNIT;
-      if (u + 1 < ps.count) page = key < t.kv1 ? __ldg(row + (key >> a.pool.page_log2)) : -1;
+      const int base = t.kv0 + (ps.unit + u) * UNIT;
+      const int id = page;
+      page = id_of(u + 1);
+      if (tma && base + UNIT <= t.kv1) {
+        const int token = (base + warp * 32 + mybox * maps.box) & (a.pool.page_size - 1);
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const uint32_t b = issued % S::kBuffers, parity = ((issued / S::kBuffers) & 1) ^ 1;
-        if (!__all_sync(0xFFFFFFFFu, bar_test(&sh->empty[b], parity))) {
-          if (issued > told) {
-            cp_wait<0>();
-            tell(issued);
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!ld.room()) return false;
+          uint64_t* bar = &sh->full[ld.issued % S::kBuffers];
+          if (lane == 0) bar_expect(bar, 32 * 128 * S::kHalves);
+          __syncwarp();
+          if (issues)
+            tma_load(ring + ld.issued % S::kBuffers * S::kBlock + myhalf * (128 * 128) + (warp * 32 + mybox * maps.box) * 128,
+                     kv ? &maps.v : &maps.k, bar, myhalf * 64, ps.head, token, id, a.layer);
+          ++ld.issued;
+          ++ld.told;
+        }
+      } else {
+        const int key = base + warp * 32 + lane;
+        int64_t off = -1;
+        if (id >= 0) off = id * a.pool.page_stride + (int64_t)(key & (a.pool.page_size - 1)) * a.pool.token_stride + head_off;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!ld.room()) return false;
+          ld.copy_rows(ring + ld.issued % S::kBuffers * S::kBlock, kv ? a.v : a.k, off);
+          ++ld.issued;
+          if (ld.issued - ld.told > S::kLag) {
+            cp_wait<S::kLag>();
+            ld.tell(ld.issued - S::kLag);
           }
-          if (!warp_wait(sh, &sh->empty[b], parity)) return false;
         }
-        const char* base = kv ? a.v : a.k;
-        const uint32_t dst = ring + b * S::kBlock;
-#pragma unroll
-        for (int j = 0; j < 32; j += RPI) {
-          const int64_t o = __shfl_sync(0xFFFFFFFFu, off, j + sub);
-          const bool ok = o >= 0 && on;
-          if (pad) cp16(dst + place(warp * 32 + j + sub), base + (ok ? 2 * o + w * 16 : 0), ok);
+      }
+      if (u == 0) {  // queries, once the last tile's are read; its first keys are under way
+        ld.tell_all();
+        if (!warp_wait(sh, &sh->q_empty, (seg & 1) ^ 1)) return false;
+        for (int blk = 0; blk < (ps.pair() ? 2 : 1); ++blk) {
+          const int r = blk * 128 + warp * 32 + lane, rr = t.row0 + r;
+          int64_t off = -1;
+          if (r < t.nrows)
+            off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
+                  (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
+          ld.copy_rows(qs + blk * S::kBlock, a.q, off);
         }
-        cp_commit();
-        ++issued;
-        if (issued - told > S::kLag) {
-          cp_wait<S::kLag>();
-          tell(issued - S::kLag);
-        }
+        cp_wait<0>();
+        to_async_proxy();
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sh->q_full);
       }
     }
   }
-  cp_wait<0>();
-  tell(issued);
+  ld.tell_all();
   return true;
 }
 
-// ---- the matrix instructions' issuing thread ----------------------------------------
+// ---- the warp that issues the matrix instructions ------------------------------------
+// One thread (the warp's first): products issued under a predicate by a whole
+// warp took nearly twice as long (113 cycles against 64, 128 x 128 x 16).
 template <typename T, int DP>
 __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, uint32_t tmem, uint32_t qs, uint32_t ring, Parts ps) {
   using S = Shape<DP>;
   const uint32_t id_qk = instr_desc<T>(UNIT, false), id_pv = instr_desc<T>(DP, true);
-  const int steps = (a.pool.head_dim + 15) / 16;
-  uint32_t base = 0;  // blocks of the tiles before this one
-  uint32_t p_phase[2] = {0, 0};
-  auto wait_block = [&](uint32_t i) { return bar_wait(sh, &sh->full[i % S::kBuffers], (i / S::kBuffers) & 1); };
-  auto scores = [&](int t, int qblk, uint32_t i) {
-    const uint32_t q = qs + qblk * S::kBlock, k = ring + (i % S::kBuffers) * S::kBlock;
+  // descriptors differ in their address field alone
+  const uint64_t q_desc = smem_desc(qs, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, 128 * 128);
+  uint32_t p_phase = 0;  // bit t: of group t
+  uint32_t k_slot = 0, k_par = 0;  // ring place of the tile's unit 0, and how often the ring has gone round (mod 2)
+  // place and parity of a block 'ahead' of the tile's first
+  auto slot_of = [&](uint32_t ahead, uint32_t* par) {
+    const uint32_t i = k_slot + ahead;
+    *par = (k_par + i / S::kBuffers) & 1;
+    return i % S::kBuffers;
+  };
+  auto scores = [&](int t, int qblk, uint32_t slot) {
+    const uint64_t q = q_desc + (uint64_t)(qblk * (S::kBlock >> 4)), k = k_desc + (uint64_t)(slot * (S::kBlock >> 4));
 #pragma unroll
     for (int s = 0; s < S::kSteps; ++s) {
-      if (s >= steps) break;
-      const uint32_t at = (s >> 2) * (128 * 128) + (s & 3) * 32;
-      mma_ss(tmem + col_s(t), smem_desc(q + at, 16), smem_desc(k + at, 16), id_qk, s > 0);
+      constexpr int kHalf = 128 * 128 >> 4;
+      const int at = (s >> 2) * kHalf + (s & 3) * 2;
+      mma_ss(tmem + col_s(t), q + at, k + at, id_qk, s > 0);
     }
     tc_commit(&sh->s_full[t]);
   };
@@ -288,46 +378,48 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, uint32
   for (; more; ++seg, more = ps.next()) {
     const bool pair = ps.pair();
     const int n = ps.count;
-    const int steps_of[2] = {pair ? n : (n + 1) / 2, pair ? n : n / 2};
-    auto unit_of = [&](int t, int i) { return pair ? i : 2 * i + t; };
+    const int steps0 = pair ? n : (n + 1) / 2, steps1 = pair ? n : n / 2;
     if (!bar_wait(sh, &sh->q_full, seg & 1)) return false;
-#pragma unroll
+#pragma unroll 1
     for (int t = 0; t < 2; ++t) {
-      if (steps_of[t] == 0) continue;
-      const uint32_t kb = base + 2 * unit_of(t, 0);
-      if (!wait_block(kb)) return false;
+      if (t == 1 && steps1 == 0) continue;
+      uint32_t par;
+      const uint32_t kb = slot_of(pair ? 0 : 2 * t, &par);
+      if (!bar_wait(sh, &sh->full[kb], par)) return false;
       tc_after();
       scores(t, pair ? t : 0, kb);
-      if (!pair || t == 1) tc_commit(&sh->empty[kb % S::kBuffers]);
+      if (!pair || t == 1) tc_commit(&sh->empty[kb]);
     }
-    if (steps_of[0] == 1) tc_commit(&sh->q_empty);
-    for (int i = 0; i < steps_of[0]; ++i) {
-#pragma unroll
+    if (steps0 == 1) tc_commit(&sh->q_empty);
+    for (int i = 0; i < steps0; ++i) {
+#pragma unroll 1
       for (int t = 0; t < 2; ++t) {
-        if (i >= steps_of[t]) continue;
-        const uint32_t vb = base + 2 * unit_of(t, i) + 1;
-        if (!bar_wait(sh, &sh->p_full[t], p_phase[t])) return false;
-        p_phase[t] ^= 1;
-        if (!wait_block(vb)) return false;
+        const int mine = t ? steps1 : steps0;
+        if (i >= mine) continue;
+        const uint32_t unit = pair ? i : 2 * i + t, step = pair ? 1 : 2;
+        uint32_t vpar, kpar;
+        const uint32_t vb = slot_of(2 * unit + 1, &vpar), kb = slot_of(2 * (unit + step), &kpar);
+        if (!bar_wait(sh, &sh->full[vb], vpar)) return false;
+        if (!bar_wait(sh, &sh->p_full[t], p_phase >> t & 1)) return false;
+        p_phase ^= 1u << t;
         tc_after();
-        const uint32_t v = ring + (vb % S::kBuffers) * S::kBlock;
+        const uint64_t v = v_desc + (uint64_t)(vb * (S::kBlock >> 4));
 #pragma unroll
         for (int s = 0; s < UNIT / 16; ++s)
-          mma_ts(tmem + col_o(t), tmem + col_s(t) + s * 8, smem_desc(v + s * 2048, 128 * 128), id_pv, i > 0 || s > 0);
-        if (!pair || t == 1) tc_commit(&sh->empty[vb % S::kBuffers]);
-        if (i + 1 < steps_of[t]) {
-          const uint32_t kb = base + 2 * unit_of(t, i + 1);
-          if (!wait_block(kb)) return false;
+          mma_ts(tmem + col_o(t), tmem + col_s(t) + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
+        if (!pair || t == 1) tc_commit(&sh->empty[vb]);
+        if (i + 1 < mine) {
+          if (!bar_wait(sh, &sh->full[kb], kpar)) return false;
           tc_after();
           scores(t, pair ? t : 0, kb);
-          if (!pair || t == 1) tc_commit(&sh->empty[kb % S::kBuffers]);
+          if (!pair || t == 1) tc_commit(&sh->empty[kb]);
         } else {
           tc_commit(&sh->o_full[t]);
         }
       }
-      if (i + 2 == steps_of[0]) tc_commit(&sh->q_empty);  // the last scores are on their way
+      if (i + 2 == steps0) tc_commit(&sh->q_empty);  // the last scores are on their way
     }
-    base += 2 * n;
+    k_slot = slot_of(2 * n, &k_par);
   }
   return true;
 }
@@ -383,7 +475,11 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       }
       float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int j = 4; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], s[j]);
+      for (int j = 4; j + 8 <= 128; j += 8)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[j + 2 * x], s[j + 2 * x + 1]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], s[124 + x]);
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc;
       const bool move = top > m + kRescale || m == -INFINITY;
       if (__any_sync(0xFFFFFFFFu, move)) {
@@ -404,20 +500,22 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         }
       }
       const float ref = m == -INFINITY ? 0.0f : m;
-      float sum[4] = {0, 0, 0, 0};
+      const uint64_t sc2 = pack2(sc, sc), ref2 = pack2(-ref, -ref);
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int j = 0; j < 128; j += 32) {
         uint32_t p[16];
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
-          const float e0 = ex2(fmaf(s[j + 2 * x], sc, -ref)), e1 = ex2(fmaf(s[j + 2 * x + 1], sc, -ref));
-          sum[x & 1] += e0;
-          sum[2 + (x & 1)] += e1;
+          const float2 e = unpack2(fma2(pack2(s[j + 2 * x], s[j + 2 * x + 1]), sc2, ref2));
+          const float e0 = ex2(e.x), e1 = ex2(e.y);
+          sum[x & 1] = add2(sum[x & 1], pack2(e0, e1));
           p[x] = Num<T>::pack(e0, e1);
         }
         tm_store16(s_at + j / 2, p);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const float2 total = unpack2(add2(sum[0], sum[1]));
+      l += total.x + total.y;
       tm_wait_st();
       if (i == 0 && !let_go()) return false;
       tc_before();
@@ -505,7 +603,8 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_constant__ AttendArgs a,
+                                                             const __grid_constant__ PoolMaps maps) {
   using S = Shape<DP>;
   extern __shared__ char dyn[];
   __shared__ Shared sh;
@@ -552,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(AttendArgs a) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   }
   if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoaderWarps) {
-    ok = load_role<DP>(a, &sh, qs, ring, ps);
+    ok = load_role<DP>(a, maps, &sh, qs, ring, ps);
     cp_wait<0>();
   } else if (warp == kSoftmaxWarps + kLoaderWarps && lane == 0) {
     ok = mma_role<T, DP>(a, &sh, tmem, qs, ring, ps);
@@ -567,13 +666,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(AttendArgs a) {
 }
 
 template <typename T, int DP>
-cudaError_t wide(const AttendArgs& a, cudaStream_t st) {
-  return launch(k_attend_wide<T, DP>, dim3((unsigned)a.plan.max_ctas[1]), kThreads, Shape<DP>::kSmem, st, a);
+cudaError_t wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
+  return launch(k_attend_wide<T, DP>, dim3((unsigned)a.plan.max_ctas[1]), kThreads, Shape<DP>::kSmem, st, a, m);
 }
 template <typename T>
-cudaError_t wide_t(const AttendArgs& a, cudaStream_t st) {
+cudaError_t wide_t(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
   const int d = a.pool.head_dim;
-  return d <= 64 ? wide<T, 64>(a, st) : d <= 80 ? wide<T, 80>(a, st) : d <= 96 ? wide<T, 96>(a, st) : wide<T, 128>(a, st);
+  return d <= 64 ? wide<T, 64>(a, m, st) : d <= 80 ? wide<T, 80>(a, m, st) : d <= 96 ? wide<T, 96>(a, m, st) : wide<T, 128>(a, m, st);
 }
 template <typename T, int DP>
 cudaError_t configure_dp() {
@@ -586,8 +685,36 @@ cudaError_t configure_t(int d) {
 
 }  // namespace
 
-cudaError_t launch_wide(const AttendArgs& a, cudaStream_t st) {
-  return a.pool.dtype == PS_KV_BF16 ? wide_t<__nv_bfloat16>(a, st) : wide_t<__half>(a, st);
+cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
+  return a.pool.dtype == PS_KV_BF16 ? wide_t<__nv_bfloat16>(a, m, st) : wide_t<__half>(a, m, st);
+}
+
+bool make_maps(const Pool& p, PoolMaps* m) {
+  m->ok = 0;
+  m->box = p.page_size < 32 ? p.page_size : 32;
+  if (p.page_size < 8) return false;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess || !fn)
+    return false;
+  const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
+  const cuuint64_t dims[5] = {(cuuint64_t)p.head_dim, (cuuint64_t)p.kv_heads, (cuuint64_t)p.page_size, (cuuint64_t)p.num_pages,
+                              (cuuint64_t)p.num_layers};
+  const int64_t stride[4] = {p.head_stride, p.token_stride, p.page_stride, p.layer_stride};
+  cuuint64_t bytes[4];
+  for (int i = 0; i < 4; ++i) {  // an axis of one place is never stepped over: any stride will do
+    bytes[i] = dims[i + 1] > 1 ? 2 * (cuuint64_t)stride[i] : 16;
+    if (bytes[i] == 0 || bytes[i] >= (1ull << 40)) return false;
+  }
+  const cuuint32_t box[5] = {64, 1, (cuuint32_t)m->box, 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const CUtensorMapDataType type = p.dtype == PS_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  for (int i = 0; i < 2; ++i)
+    if (encode(i ? &m->v : &m->k, type, 5, i ? p.v : p.k, dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  m->ok = 1;
+  return true;
 }
 cudaError_t configure_wide(const Pool& p) {
   return p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim) : configure_t<__half>(p.head_dim);
