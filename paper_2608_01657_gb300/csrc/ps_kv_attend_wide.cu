@@ -11,7 +11,7 @@
 //     which the swizzle repeats, go by 16-byte asynchronous copies instead, eight
 //     times the instructions and waited for by the copying threads: with them for
 //     all units the loader warps took 7400 cycles a unit, the products 2350;
-//   1 warp that issues the matrix instructions (3 more idle).
+//   2 warps that issue the matrix instructions, one for each group (2 more idle).
 // A tile of more than 128 rows is two row blocks, one for each group, that use
 // every unit's keys and values (pair mode).  A tile of up to 128 rows is one
 // row block; the groups take its units in turn, each with a softmax of its own
@@ -45,7 +45,6 @@ struct Shape {
   static constexpr int kHalves = DP > 64 ? 2 : 1;          // 64-element halves of a row
   static constexpr int kBlock = 128 * 128 * kHalves;       // bytes of 128 rows
   static constexpr int kBuffers = DP > 64 ? 5 : 10;        // ring of key and value blocks, in turn
-  static constexpr int kLag = kBuffers - 2;                // blocks in flight before the oldest is waited for
   static constexpr int kSmem = 1024 + (2 + kBuffers) * kBlock;
   static constexpr int kSteps = DP / 16;                   // k steps of Q K^T
 };
@@ -54,7 +53,6 @@ struct Shared {
   uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full, q_empty, ml_full, ml_free;
   uint32_t tmem;
   float2 ml[128];  // split mode: group 1's (maximum, sum)
-  int failed;
 };
 
 // ---- barriers, tensor memory ---------------------------------------------------
@@ -72,33 +70,35 @@ __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
       : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return ok != 0;
 }
-// False if the wait ran out, here or in another warp.
-__device__ __forceinline__ bool bar_wait(Shared* sh, uint64_t* b, uint32_t parity) {
-  for (int i = 0; i < kWaitLimit; ++i) {
+// False if the wait ran out.  (The other roles' waits then run out too.)
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity) {
+#pragma unroll 1
+  for (int i = 0; i < kWaitLimit; ++i)
     if (bar_test(b, parity)) return true;
-    if ((i & 255) == 255 && *(volatile int*)&sh->failed) return false;
-  }
-  *(volatile int*)&sh->failed = 1;
   return false;
 }
 // The same by a whole warp, with one answer.
-__device__ __forceinline__ bool warp_wait(Shared* sh, uint64_t* b, uint32_t parity) {
-  return __all_sync(0xFFFFFFFFu, bar_wait(sh, b, parity));
-}
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, bar_wait(b, parity)); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // The commits and products below are one thread's.
 __device__ __forceinline__ void tc_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-// d (+)= a b: both operands in shared memory, or a in tensor memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-               "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// d (+)= a b: both operands in shared memory, or a in tensor memory.  Of a shared
+// memory operand's descriptor the low word differs, see desc_low.
+constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;  // 8 rows are 1024 bytes; 128-byte swizzle
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 a, b; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5}; setp.ne.u32 p, %4, 0;"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add),
+      "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
-               "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.u32 p, %4, 0;"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add),
+      "r"(kDescHigh) : "memory");
 }
 #define R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -155,13 +155,11 @@ __device__ __forceinline__ void cp_wait() {
 }
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Descriptor of a block of 128-byte rows with the 128-byte swizzle.  Eight rows
-// are 1024 bytes; 'lead' is the distance of the second 64-element half where the
-// rows are the contraction's (values), unused where they are the result's.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lead >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Low word of the descriptor of a block of 128-byte rows with the 128-byte
+// swizzle: its address, and the distance 'lead' of the second 64-element half
+// where the rows are the contraction's (values), unused where they are the
+// result's.
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return addr >> 4 | lead >> 4 << 16; }
 // Instruction descriptor: 32-bit sums of 16-bit products, 128 rows, n columns.
 template <typename T>
 __device__ __forceinline__ uint32_t instr_desc(int n, bool b_rows_contract) {
@@ -215,74 +213,73 @@ __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
 }
 
-template <int DP>
-struct Loader {
-  using S = Shape<DP>;
-  static constexpr int CH = DP / 8;                      // 16-byte words of a row that hold elements
-  static constexpr int RPI = 32 / (CH <= 8 ? 8 : 16);    // rows that one copy instruction covers
-  const AttendArgs& a;
-  Shared* sh;
-  const int lane, warp;
-  const int w, sub;  // the lane's word of a row, and row of an instruction's
-  uint32_t issued = 0, told = 0;  // blocks issued, blocks whose arrival was signalled
-
-  __device__ __forceinline__ Loader(const AttendArgs& args, Shared* s)
-      : a(args), sh(s), lane(threadIdx.x & 31), warp((threadIdx.x >> 5) - kSoftmaxWarps), w(lane % (32 / RPI)), sub(lane / (32 / RPI)) {}
-
-  // 32 rows of the warp's, row r at element off (of lane r; -1: zeros).
-  __device__ __forceinline__ void copy_rows(uint32_t dst, const char* base, int64_t off) const {
-    const bool on = w * 8 < a.pool.head_dim;
-    int64_t o[32 / RPI];
-#pragma unroll
-    for (int j = 0; j < 32 / RPI; ++j) o[j] = __shfl_sync(0xFFFFFFFFu, off, j * RPI + sub);
-#pragma unroll
-    for (int j = 0; j < 32 / RPI; ++j) {
-      const int r = warp * 32 + j * RPI + sub;
-      const bool ok = o[j] >= 0 && on;
-      // word w of row r: half w / 8, swizzled within its 128 bytes
-      if (w < CH)
-        cp16(dst + (w >> 3) * (128 * 128) + r * 128 + (((w & 7) ^ (r & 7)) << 4), base + (ok ? 2 * o[j] + w * 16 : 0), ok);
+// A place in the ring of blocks, and the parity of its use.
+template <int N>
+struct Place {
+  uint32_t slot = 0, par = 0;
+  __device__ __forceinline__ Place ahead(uint32_t n) const {  // n < N
+    Place p;
+    p.slot = slot + n;
+    p.par = par;
+    if (p.slot >= N) {
+      p.slot -= N;
+      p.par ^= 1;
     }
-    cp_commit();
+    return p;
   }
-  __device__ __forceinline__ void tell(uint32_t upto) {
-    to_async_proxy();
-    __syncwarp();
-    for (; told < upto; ++told)
-      if (lane == 0) bar_arrive(&sh->full[told % S::kBuffers]);
-  }
-  __device__ __forceinline__ void tell_all() {
-    if (issued > told) {
-      cp_wait<0>();
-      tell(issued);
-    }
-  }
-  // The next block of the ring is free.  What was copied is not held back by the wait.
-  __device__ __forceinline__ bool room() {
-    uint64_t* e = &sh->empty[issued % S::kBuffers];
-    const uint32_t parity = ((issued / S::kBuffers) & 1) ^ 1;
-    if (__all_sync(0xFFFFFFFFu, bar_test(e, parity))) return true;
-    tell_all();
-    return warp_wait(sh, e, parity);
+  __device__ __forceinline__ Place skip(uint32_t n) const {
+    Place p;
+    p.slot = (slot + n) % N;
+    p.par = (par + (slot + n) / N) & 1;
+    return p;
   }
 };
+
+// 32 rows of the warp's, row r at element off (of lane r; -1: zeros), as one
+// group of asynchronous copies.
+template <int DP>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const char* base, int64_t off, int head_dim) {
+  constexpr int CH = DP / 8;                    // 16-byte words of a row that hold elements
+  constexpr int RPI = 32 / (CH <= 8 ? 8 : 16);  // rows that one copy instruction covers
+  const int lane = threadIdx.x & 31, row0 = (threadIdx.x >> 5 & 3) * 32;
+  const int w = lane % (32 / RPI), sub = lane / (32 / RPI);
+  const bool on = w * 8 < head_dim;
+#pragma unroll 4
+  for (int j = 0; j < 32; j += RPI) {
+    const int64_t o = __shfl_sync(0xFFFFFFFFu, off, j + sub);
+    const int r = row0 + j + sub;
+    const bool ok = o >= 0 && on;
+    // word w of row r: half w / 8, swizzled within its 128 bytes
+    if (w < CH) cp16(dst + (w >> 3) * (128 * 128) + r * 128 + (((w & 7) ^ (r & 7)) << 4), base + (ok ? 2 * o + w * 16 : 0), ok);
+  }
+  cp_commit();
+}
 
 template <int DP>
 __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& maps, Shared* sh, uint32_t qs, uint32_t ring, Parts ps) {
   using S = Shape<DP>;
-  Loader<DP> ld(a, sh);
-  const int lane = ld.lane, warp = ld.warp;
+  static_assert(kSoftmaxWarps % 4 == 0, "copy_rows takes the warp's place in its group");
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kSoftmaxWarps;
   const bool tma = maps.ok;
   // TMA: lane i issues box i % boxes of the warp's keys, half i / boxes
   const int boxes = 32 / maps.box, mybox = lane % boxes, myhalf = lane / boxes;
   const bool issues = tma && lane < boxes * S::kHalves;
+  const uint32_t box_at = myhalf * (128 * 128) + (warp * 32 + mybox * maps.box) * 128;
+  Place<S::kBuffers> at;       // the next block
+  uint64_t* copied = nullptr;  // a block whose copies are under way
+  auto told = [&]() {          // wait for them and say so
+    if (!copied) return;
+    cp_wait<0>();
+    to_async_proxy();
+    __syncwarp();
+    if (lane == 0) bar_arrive(copied);
+    copied = nullptr;
+  };
   uint32_t seg = 0;
   bool more = true;
   for (; more; ++seg, more = ps.next()) {
     const Tile t = ps.t;
     const int32_t* row = a.tables + t.req * a.table_stride;
-    const int64_t head_off = (int64_t)ps.head * a.pool.head_stride;
-    ld.tell_all();
     // ids are looked up one unit ahead
     auto id_of = [&](int u) -> int {
       const int base = t.kv0 + (ps.unit + u) * UNIT;
@@ -291,135 +288,126 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
       return u < ps.count && key < t.kv1 ? __ldg(row + (key >> a.pool.page_log2)) : -1;
     };
     int page = id_of(0);
+#pragma unroll 1
     for (int u = 0; u < ps.count; ++u) {
       const int base = t.kv0 + (ps.unit + u) * UNIT;
+      const bool whole = tma && base + UNIT <= t.kv1;
       const int id = page;
       page = id_of(u + 1);
-      if (tma && base + UNIT <= t.kv1) {
-        const int token = (base + warp * 32 + mybox * maps.box) & (a.pool.page_size - 1);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          if (!ld.room()) return false;
-          uint64_t* bar = &sh->full[ld.issued % S::kBuffers];
-          if (lane == 0) bar_expect(bar, 32 * 128 * S::kHalves);
-          __syncwarp();
-          if (issues)
-            tma_load(ring + ld.issued % S::kBuffers * S::kBlock + myhalf * (128 * 128) + (warp * 32 + mybox * maps.box) * 128,
-                     kv ? &maps.v : &maps.k, bar, myhalf * 64, ps.head, token, id, a.layer);
-          ++ld.issued;
-          ++ld.told;
+      const int key = base + warp * 32 + (whole ? mybox * maps.box : lane), token = key & (a.pool.page_size - 1);
+      // keys, values; with a tile's first unit under way its queries, once the last
+      // tile's are read (one loop, so that the copies' code is there once)
+      const int jobs = u > 0 ? 2 : (ps.pair() ? 4 : 3);
+#pragma unroll 1
+      for (int job = 0; job < jobs; ++job) {
+        uint64_t* bar = job < 2 ? &sh->full[at.slot] : &sh->q_full;
+        uint64_t* free = job < 2 ? &sh->empty[at.slot] : &sh->q_empty;
+        const uint32_t parity = job < 2 ? at.par ^ 1 : (seg & 1) ^ 1;
+        if (job < 3 && !__all_sync(0xFFFFFFFFu, bar_test(free, parity))) {
+          told();  // what was copied is not held back by the wait
+          if (!warp_wait(free, parity)) return false;
         }
-      } else {
-        const int key = base + warp * 32 + lane;
-        int64_t off = -1;
-        if (id >= 0) off = id * a.pool.page_stride + (int64_t)(key & (a.pool.page_size - 1)) * a.pool.token_stride + head_off;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          if (!ld.room()) return false;
-          ld.copy_rows(ring + ld.issued % S::kBuffers * S::kBlock, kv ? a.v : a.k, off);
-          ++ld.issued;
-          if (ld.issued - ld.told > S::kLag) {
-            cp_wait<S::kLag>();
-            ld.tell(ld.issued - S::kLag);
+        const char* src = job == 0 ? a.k : (job == 1 ? a.v : a.q);
+        uint32_t dst;
+        int64_t off;
+        if (job < 2) {
+          dst = ring + at.slot * S::kBlock;
+          at = at.ahead(1);
+          if (whole) {
+            if (lane == 0) bar_expect(bar, 32 * 128 * S::kHalves);
+            __syncwarp();
+            if (issues) tma_load(dst + box_at, job ? &maps.v : &maps.k, bar, myhalf * 64, ps.head, token, id, a.layer);
+            continue;
           }
+          off = id * a.pool.page_stride + (int64_t)token * a.pool.token_stride + (int64_t)ps.head * a.pool.head_stride;
+          if (id < 0) off = -1;
+        } else {
+          const int r = (job - 2) * 128 + warp * 32 + lane, rr = t.row0 + r;
+          dst = qs + (job - 2) * S::kBlock;
+          off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
+                (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
+          if (r >= t.nrows) off = -1;
         }
+        if (job != 3) told();
+        copy_rows<DP>(dst, src, off, a.pool.head_dim);
+        copied = bar;
       }
-      if (u == 0) {  // queries, once the last tile's are read; its first keys are under way
-        ld.tell_all();
-        if (!warp_wait(sh, &sh->q_empty, (seg & 1) ^ 1)) return false;
-        for (int blk = 0; blk < (ps.pair() ? 2 : 1); ++blk) {
-          const int r = blk * 128 + warp * 32 + lane, rr = t.row0 + r;
-          int64_t off = -1;
-          if (r < t.nrows)
-            off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
-                  (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
-          ld.copy_rows(qs + blk * S::kBlock, a.q, off);
-        }
-        cp_wait<0>();
-        to_async_proxy();
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sh->q_full);
-      }
+      if (u == 0) told();
     }
   }
-  ld.tell_all();
+  told();
   return true;
 }
 
-// ---- the warp that issues the matrix instructions ------------------------------------
-// One thread (the warp's first): products issued under a predicate by a whole
-// warp took nearly twice as long (113 cycles against 64, 128 x 128 x 16).
+// ---- the warps that issue the matrix instructions -------------------------------------
+// One warp for each group t, of which one thread issues: a product issued under
+// a predicate by a whole warp took nearly twice as long (113 cycles against 64,
+// 128 x 128 x 16), and every wait between products drains the issuing thread's
+// queue (some 200 cycles), which the other group's products fill.
 template <typename T, int DP>
-__device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, uint32_t tmem, uint32_t qs, uint32_t ring, Parts ps) {
+__device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t, uint32_t tmem, uint32_t qs, uint32_t ring, Parts ps) {
   using S = Shape<DP>;
-  const uint32_t id_qk = instr_desc<T>(UNIT, false), id_pv = instr_desc<T>(DP, true);
+  // scores are negated where the scale is negative
+  const uint32_t id_qk = instr_desc<T>(UNIT, false) | (a.scale2 < 0 ? 1u << 13 : 0), id_pv = instr_desc<T>(DP, true);
   // descriptors differ in their address field alone
-  const uint64_t q_desc = smem_desc(qs, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, 128 * 128);
-  uint32_t p_phase = 0;  // bit t: of group t
-  uint32_t k_slot = 0, k_par = 0;  // ring place of the tile's unit 0, and how often the ring has gone round (mod 2)
-  // place and parity of a block 'ahead' of the tile's first
-  auto slot_of = [&](uint32_t ahead, uint32_t* par) {
-    const uint32_t i = k_slot + ahead;
-    *par = (k_par + i / S::kBuffers) & 1;
-    return i % S::kBuffers;
-  };
-  auto scores = [&](int t, int qblk, uint32_t slot) {
-    const uint64_t q = q_desc + (uint64_t)(qblk * (S::kBlock >> 4)), k = k_desc + (uint64_t)(slot * (S::kBlock >> 4));
-#pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) {
-      constexpr int kHalf = 128 * 128 >> 4;
-      const int at = (s >> 2) * kHalf + (s & 3) * 2;
-      mma_ss(tmem + col_s(t), q + at, k + at, id_qk, s > 0);
-    }
-    tc_commit(&sh->s_full[t]);
-  };
+  const uint32_t q_desc = desc_low(qs, 16), k_desc = desc_low(ring, 16), v_desc = desc_low(ring, 128 * 128);
+  constexpr uint32_t kBlk = S::kBlock >> 4;
+  const uint32_t s_at = tmem + col_s(t), o_at = tmem + col_o(t);
+  uint32_t p_phase = 0;
+  Place<S::kBuffers> at;  // the key block of the tile's unit in turn; its value block is the next
   uint32_t seg = 0;
   bool more = true;
   for (; more; ++seg, more = ps.next()) {
     const bool pair = ps.pair();
     const int n = ps.count;
-    const int steps0 = pair ? n : (n + 1) / 2, steps1 = pair ? n : n / 2;
-    if (!bar_wait(sh, &sh->q_full, seg & 1)) return false;
+    if (!bar_wait(&sh->q_full, seg & 1)) return false;
+    const uint32_t q = q_desc + (pair ? t : 0) * kBlk;
+    // a block's two arrivals: one of each group, or both of the one that uses it
+    auto release = [&](const Place<S::kBuffers>& b) {
+      tc_commit(&sh->empty[b.slot]);
+      if (!pair) tc_commit(&sh->empty[b.slot]);
+    };
+    Place<S::kBuffers> kb = at;
+    if (!pair && t == 1) kb = kb.ahead(2);
+    const int step = pair ? 1 : 2;
+    // unit u's values, then the scores of this group's next unit; the first
+    // turn is the first scores alone.  The blocks' waits come before the wait for
+    // the weights, where there is time.
 #pragma unroll 1
-    for (int t = 0; t < 2; ++t) {
-      if (t == 1 && steps1 == 0) continue;
-      uint32_t par;
-      const uint32_t kb = slot_of(pair ? 0 : 2 * t, &par);
-      if (!bar_wait(sh, &sh->full[kb], par)) return false;
-      tc_after();
-      scores(t, pair ? t : 0, kb);
-      if (!pair || t == 1) tc_commit(&sh->empty[kb]);
-    }
-    if (steps0 == 1) tc_commit(&sh->q_empty);
-    for (int i = 0; i < steps0; ++i) {
-#pragma unroll 1
-      for (int t = 0; t < 2; ++t) {
-        const int mine = t ? steps1 : steps0;
-        if (i >= mine) continue;
-        const uint32_t unit = pair ? i : 2 * i + t, step = pair ? 1 : 2;
-        uint32_t vpar, kpar;
-        const uint32_t vb = slot_of(2 * unit + 1, &vpar), kb = slot_of(2 * (unit + step), &kpar);
-        if (!bar_wait(sh, &sh->full[vb], vpar)) return false;
-        if (!bar_wait(sh, &sh->p_full[t], p_phase >> t & 1)) return false;
-        p_phase ^= 1u << t;
-        tc_after();
-        const uint64_t v = v_desc + (uint64_t)(vb * (S::kBlock >> 4));
-#pragma unroll
-        for (int s = 0; s < UNIT / 16; ++s)
-          mma_ts(tmem + col_o(t), tmem + col_s(t) + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
-        if (!pair || t == 1) tc_commit(&sh->empty[vb]);
-        if (i + 1 < mine) {
-          if (!bar_wait(sh, &sh->full[kb], kpar)) return false;
-          tc_after();
-          scores(t, pair ? t : 0, kb);
-          if (!pair || t == 1) tc_commit(&sh->empty[kb]);
-        } else {
-          tc_commit(&sh->o_full[t]);
-        }
+    for (int u = (pair ? 0 : t) - step; u < n; u += step) {
+      const Place<S::kBuffers> vb = kb.ahead(1);
+      const bool product = u >= 0, more_keys = u + step < n;
+      if (product) {
+        if (!bar_wait(&sh->full[vb.slot], vb.par)) return false;
+        kb = kb.ahead(2 * step);
       }
-      if (i + 2 == steps0) tc_commit(&sh->q_empty);  // the last scores are on their way
+      if (more_keys && !bar_wait(&sh->full[kb.slot], kb.par)) return false;
+      if (product) {
+        if (!bar_wait(&sh->p_full[t], p_phase)) return false;
+        p_phase ^= 1;
+        tc_after();
+        const uint32_t v = v_desc + vb.slot * kBlk;
+#pragma unroll
+        for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, u >= step || s > 0);
+      }
+      if (more_keys) {
+        tc_after();
+        const uint32_t k = k_desc + kb.slot * kBlk;
+#pragma unroll
+        for (int s = 0; s < S::kSteps; ++s) {
+          const int x = (s >> 2) * (128 * 128 >> 4) + (s & 3) * 2;
+          mma_ss(s_at, q + x, k + x, id_qk, s > 0);
+        }
+        tc_commit(&sh->s_full[t]);
+      } else if (product) {
+        tc_commit(&sh->o_full[t]);
+      }
+      if (product) release(vb);
+      if (more_keys) release(kb);
+      if (more_keys && u + 2 * step >= n) tc_commit(&sh->q_empty);  // the last scores are on their way
     }
-    k_slot = slot_of(2 * n, &k_par);
+    if (!pair && t == 1 && n == 1) tc_commit(&sh->q_empty);  // no scores at all
+    at = at.skip(2 * n);
   }
   return true;
 }
@@ -431,15 +419,15 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
   const int row = (warp & 3) * 32 + lane;  // of the row block, and the tensor memory lane
   const uint32_t at = tmem + ((uint32_t)(warp & 3) << 21);
   const uint32_t s_at = at + col_s(t), o_at = at + col_o(t);
-  // 2^(s sc - m): a scale of 0 or below goes into the scores
-  const float sign = a.scale2 > 0 ? 1.0f : (a.scale2 < 0 ? -1.0f : 0.0f);
-  const float sc = a.scale2 != 0 ? fabsf(a.scale2) : 1.0f;
+  // a negative scale's sign is in the scores already; at a scale of 0 the least
+  // one stands for it, so that hidden scores of -infinity stay what they are
+  const float sc = fmaxf(fabsf(a.scale2), 1e-30f);
   uint32_t s_phase = 0, o_mine = 0, o_other = 0, ml_phase = 0;  // o_other: group 1's, as group 0 counts it
   bool held = false;  // group 1: the last tile's O_1 and ml may still be read by group 0
   auto let_go = [&]() {
     if (!held) return true;
     held = false;
-    const bool ok = warp_wait(sh, &sh->ml_free, ml_phase);
+    const bool ok = warp_wait(&sh->ml_free, ml_phase);
     ml_phase ^= 1;
     return ok;
   };
@@ -455,7 +443,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
     float m = -INFINITY, l = 0;  // m: the scaled reference
     for (int i = 0; i < mine; ++i) {
       const int base = tl.kv0 + (ps.unit + (pair ? i : 2 * i + t)) * UNIT;
-      if (!warp_wait(sh, &sh->s_full[t], s_phase)) return false;
+      if (!warp_wait(&sh->s_full[t], s_phase)) return false;
       s_phase ^= 1;
       tc_after();
       uint32_t raw[128];
@@ -463,10 +451,6 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       for (int j = 0; j < 128; j += 32) tm_load32(raw + j, s_at + j);
       tm_wait_ld();
       float* s = reinterpret_cast<float*>(raw);
-      if (sign != 1.0f) {
-#pragma unroll
-        for (int j = 0; j < 128; ++j) s[j] *= sign;
-      }
       const int seen = lim - base;
       if (__any_sync(0xFFFFFFFFu, seen < UNIT)) {
 #pragma unroll
@@ -488,7 +472,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         m = mn;
         l *= f;
         if (i > 0) {
-#pragma unroll
+#pragma unroll 1
           for (int j = 0; j < DP; j += 16) {
             uint32_t o[16];
             tm_load16(o, o_at + j);
@@ -514,13 +498,13 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         }
         tm_store16(s_at + j / 2, p);
       }
-      const float2 total = unpack2(add2(sum[0], sum[1]));
-      l += total.x + total.y;
       tm_wait_st();
       if (i == 0 && !let_go()) return false;
       tc_before();
       __syncwarp();
       if (lane == 0) bar_arrive(&sh->p_full[t]);
+      const float2 total = unpack2(add2(sum[0], sum[1]));
+      l += total.x + total.y;
     }
     // the tile's end
     const bool whole = ps.unit == 0 && n == ps.nunits;
@@ -535,7 +519,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         if (mine > 0) o_mine ^= 1;
         continue;
       }
-      if (!warp_wait(sh, &sh->ml_full, ml_phase)) return false;
+      if (!warp_wait(&sh->ml_full, ml_phase)) return false;
       ml_phase ^= 1;
       const float2 x = sh->ml[row];
       const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.0f : mn;
@@ -544,10 +528,10 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       l = l * f[0] + x.y * f[1];
       m = mn;
     }
-    if (!warp_wait(sh, &sh->o_full[t], o_mine)) return false;
+    if (!warp_wait(&sh->o_full[t], o_mine)) return false;
     o_mine ^= 1;
     const bool both = !pair && n > 1;
-    if (both && !warp_wait(sh, &sh->o_full[1], o_other)) return false;
+    if (both && !warp_wait(&sh->o_full[1], o_other)) return false;
     if (pair || n > 1) o_other ^= 1;
     tc_after();
     const bool direct = whole && tl.sidx < 0;
@@ -558,7 +542,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
     char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
     const int64_t prow = part_row<H>(tl.sidx, tl.nrows, ps.head, c, ps.unit > 0, C) + trow;
     float* po = a.plan.part_o[1] + prow * a.pool.head_dim;
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < DP; j += 16) {
       uint32_t o[16];
       tm_load16(o, o_at + j);
@@ -623,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   if (threadIdx.x == 0) {
     for (int b = 0; b < S::kBuffers; ++b) {
       bar_init(&sh.full[b], kLoaderWarps);
-      bar_init(&sh.empty[b], 1);
+      bar_init(&sh.empty[b], 2);
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(&sh.s_full[t], 1);
@@ -631,10 +615,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
       bar_init(&sh.o_full[t], 1);
     }
     bar_init(&sh.q_full, kLoaderWarps);
-    bar_init(&sh.q_empty, 1);
+    bar_init(&sh.q_empty, 2);
     bar_init(&sh.ml_full, 4);
     bar_init(&sh.ml_free, 4);
-    sh.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc_before();
@@ -653,8 +636,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoaderWarps) {
     ok = load_role<DP>(a, maps, &sh, qs, ring, ps);
     cp_wait<0>();
-  } else if (warp == kSoftmaxWarps + kLoaderWarps && lane == 0) {
-    ok = mma_role<T, DP>(a, &sh, tmem, qs, ring, ps);
+  } else if (warp >= kSoftmaxWarps + kLoaderWarps && warp < kSoftmaxWarps + kLoaderWarps + 2 && lane == 0) {
+    ok = mma_role<T, DP>(a, &sh, warp & 1, tmem, qs, ring, ps);
   }
   if (!ok && lane == 0) set_error(a.status, PS_ERR_TIMEOUT);
   __syncwarp();
