@@ -57,11 +57,29 @@ struct ReqRec {
 constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen05)
 __host__ __device__ constexpr int tile_rows(int list) { return list ? 256 : 16; }
 __host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 64; }
+// The list of an item of so many rows.
+__host__ __device__ constexpr int list_of(int rows) { return rows > tile_rows(0) ? 1 : 0; }
 constexpr int kNoMask = 1 << 30;
 
-struct PlanHdr {
-  int32_t status;       // PS_OK, or why the plan is empty
-  int32_t join;         // some rows have partial results
+// A (tile, head)'s partial results: 'count' of them, the first at row 'first' of
+// the list's partial rows, the others 'stride' rows apart from 'second' on.
+struct Parts4 {
+  int32_t first, second, count, stride;
+};
+// A (tile, head) of a request's own keys whose rows have partial results: its
+// own, and those of its group's shared prefix.  The tile's rows may lie in two
+// of the prefix's tiles: row r is row r + pofs of the first below psplit, and
+// row r - psplit of the second from there on.
+struct __align__(16) JoinRec {
+  Parts4 own, pa, pb;
+  int32_t tok0, row0, nrows, head;
+  int32_t plist, pofs, psplit, pad0;  // plist -1: no prefix
+};
+
+struct __align__(16) PlanHdr {
+  int32_t status;           // PS_OK, or why the plan is empty
+  int32_t joins[kLists];    // entries of joins[]
+  int32_t pad0;
   int32_t ntiles[kLists];
   int32_t ctas[kLists];     // C, 0 without tiles
   int64_t units[kLists];    // U
@@ -77,10 +95,11 @@ constexpr int kMaxSms = 160;
 // all.  An item (a request's own keys, or a group's prefix; at most R of each)
 // of x rows has at most 1 + x / H tiles.
 struct PlanBounds {
-  int64_t tiles, shared;
+  int64_t tiles, own_tiles, shared;  // own_tiles: without the prefixes'
 };
 inline PlanBounds plan_bounds(int list, int64_t R, int64_t rows) {
-  return {2 * (R + rows / tile_rows(list)) + 2, 2 * (rows < R * kShareRows ? rows : R * kShareRows)};
+  const int64_t own = R + rows / tile_rows(list) + 1;
+  return {2 * own, own, 2 * (rows < R * kShareRows ? rows : R * kShareRows)};
 }
 
 // The CTA of unit u: the largest c with floor(U c / C) <= u.
@@ -100,6 +119,7 @@ struct Plan {
   Tile* tiles[kLists];
   int64_t* ucum[kLists];      // [tiles + 1] units before a tile, all heads
   int32_t* cta_tile[kLists];  // [C] tile of a CTA's first unit
+  JoinRec* joins[kLists];     // [tiles of requests x kv heads]
   float* part_o[kLists];      // [rows][head_dim] unnormalized outputs, see part_row
   float2* part_ml[kLists];    // [rows] (maximum, sum), base 2
   int32_t max_ctas[kLists];

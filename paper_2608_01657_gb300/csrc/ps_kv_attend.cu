@@ -50,6 +50,8 @@ __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ void after_wide() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Shared memory of a warp: STAGES x (16 keys, 16 values) of ROW bytes each, a
 // 16-byte word c of row r at word c ^ (r & 7), so that the eight rows of an
 // ldmatrix lie in eight different banks groups.
@@ -76,10 +78,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
   constexpr int KS = DP / 16;  // k steps of q k^T
   constexpr int H = tile_rows(0), UNIT = unit_keys(0);
   extern __shared__ __align__(128) char smem[];
-  chain();
+  // If the wide tiles' kernel goes before this one, it is independent of it, so
+  // this one's CTAs run as soon as there is room: every CTA of that kernel has
+  // waited for the work before both by then.  Its end is waited for at this
+  // one's end instead, so that the join after this kernel follows both.
+  if (!a.after_wide) chain();
+  else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PlanHdr* hdr = a.plan.hdr;
   const int C = hdr->ctas[0], c = blockIdx.x;
-  if (c >= C) return;
+  if (c >= C) {
+    after_wide();
+    return;
+  }
   const int64_t U = hdr->units[0];
   const int64_t u0 = U * c / C;
   const int n = (int)(U * (c + 1) / C - u0);
@@ -342,70 +352,90 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
     }
   }
   cp_wait<0>();
+  after_wide();
 }
 
 // ---- the join --------------------------------------------------------------------
-// A warp for each (token, query head) whose row has partial results: those of
-// its own keys' tile, then those of its group's shared prefix, in CTA order.
-// Bound by the latency of a few dependent reads; the partial results were
-// written just before and lie in L2.
-template <typename T>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
-  chain();
-  const PlanHdr* hdr = a.plan.hdr;
-  if (hdr->status != PS_OK || !hdr->join) return;
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
-  if (w >= (int64_t)a.num_tokens * a.pool.q_heads) return;
-  const int tok = (int)(w / a.pool.q_heads), hq = (int)(w % a.pool.q_heads);
-  const int head = hq / a.pool.ratio;
-  const int req = a.plan.tok_req[tok];
-  const ReqRec rec = a.plan.req[req];
-  const int row = (tok - a.q_offsets[req]) * a.pool.ratio + hq % a.pool.ratio;
+// W warps for each (tile, head) that has partial results, a row at a time: its
+// own tile's parts, then its group's prefix's, in CTA order, a lane for each.
+// Bound by the latency of its four dependent reads (the entry, the parts' maxima
+// and sums, their outputs, written just before and so in L2), which is why a
+// row's parts are all in flight at once.
+template <typename T, int W>
+__device__ __forceinline__ void join_rows(const AttendArgs& a, int list, int entries, int64_t item0, int64_t step, int lane) {
   const int dim = a.pool.head_dim;
-  float m = -INFINITY, l = 0;
-  float4 o = make_float4(0, 0, 0, 0);
-  bool parts = false;
+  const bool on = lane * 4 < dim;
+  for (int64_t it = item0; it < (int64_t)entries * W; it += step) {
+    static_assert(sizeof(JoinRec) == 80, "one word a lane");
+    const int word = lane < 20 ? __ldg(reinterpret_cast<const int*>(a.plan.joins[list] + it / W) + lane) : 0;
+    auto field = [&](int i) { return __shfl_sync(0xFFFFFFFFu, word, i); };
+    const Parts4 own = {field(0), field(1), field(2), field(3)};
+    const Parts4 pa = {field(4), field(5), field(6), field(7)}, pb = {field(8), field(9), field(10), field(11)};
+    const int tok0 = field(12), row0 = field(13), nrows = field(14), head = field(15);
+    const int plist = field(16), pofs = field(17), psplit = field(18);
+    for (int r = (int)(it % W); r < nrows; r += W) {
+      const bool second = r >= psplit;
+      const Parts4 pp = second ? pb : pa;
+      const int prow = second ? r - psplit : r + pofs, n = own.count + (plist >= 0 ? pp.count : 0);
+      float m = -INFINITY, l = 0;
+      float4 o = make_float4(0, 0, 0, 0);
+      for (int k0 = 0; k0 < n; k0 += 32) {
+        const int k = k0 + lane, kp = k - own.count;
+        const bool mine = kp < 0;
+        const int from = mine ? list : plist;
+        int64_t at = 0;
+        if (mine) at = (k ? own.second + (int64_t)(k - 1) * own.stride : own.first) + r;
+        else if (k < n) at = (kp ? pp.second + (int64_t)(kp - 1) * pp.stride : pp.first) + prow;
+        float2 ml = make_float2(-INFINITY, 0);
+        if (k < n) ml = from ? a.plan.part_ml[1][at] : a.plan.part_ml[0][at];
+        const uint64_t src = reinterpret_cast<uint64_t>((k < n && from ? a.plan.part_o[1] : a.plan.part_o[0]) + at * dim);
+        float top = ml.x;
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const int tile0 = side ? rec.ptile0 : rec.tile0, list = side ? rec.plist : rec.list;
-    if (side && tile0 < 0) break;
-    const int rr = side ? rec.prow0 + row : row;
-    const int H = tile_rows(list);
-    const int tile = tile0 + rr / H, r = rr % H;
-    const int sidx = a.plan.tiles[list][tile].sidx, nrows = a.plan.tiles[list][tile].nrows;
-    const int64_t U = hdr->units[list], b = a.plan.ucum[list][tile];
-    const int C = hdr->ctas[list];
-    const int64_t nu = (a.plan.ucum[list][tile + 1] - b) / a.pool.kv_heads;
-    const int64_t ua = b + head * nu;
-    const int ca = cta_of(ua, U, C), cb = cta_of(ua + nu - 1, U, C);
-    if (sidx < 0 && ca == cb) return;  // written by the one CTA that worked on it
-    parts = true;
-    // a CTA's range may begin exactly with this (tile, head)
-    for (int c = ca; c <= cb; ++c) {
-      const bool continued = U * c / C > ua;
-      const int64_t prow = r + (list ? part_row<tile_rows(1)>(sidx, nrows, head, c, continued, C)
-                                     : part_row<tile_rows(0)>(sidx, nrows, head, c, continued, C));
-      const float2 ml = a.plan.part_ml[list][prow];
-      float4 x = make_float4(0, 0, 0, 0);
-      if (lane * 4 < dim)
-        x = *reinterpret_cast<const float4*>(a.plan.part_o[list] + prow * dim + lane * 4);
-      const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
-      const float f0 = ex2(m - ms), f1 = ex2(ml.x - ms);
-      o.x = o.x * f0 + x.x * f1;
-      o.y = o.y * f0 + x.y * f1;
-      o.z = o.z * f0 + x.z * f1;
-      o.w = o.w * f0 + x.w * f1;
-      l = l * f0 + ml.y * f1;
-      m = mn;
+        for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
+        const float f0 = ex2(m - ref), f = ex2(ml.x - ref);
+        float sum = ml.y * f;
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+        l = l * f0 + sum;
+        m = mn;
+        o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+        const int count = min(32, n - k0);
+        for (int i0 = 0; i0 < count; i0 += 4) {
+          float4 x[4];
+          float w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4* q = reinterpret_cast<const float4*>(__shfl_sync(0xFFFFFFFFu, src, i0 + i)) + lane;
+            w[i] = __shfl_sync(0xFFFFFFFFu, f, i0 + i);
+            x[i] = on && i0 + i < count ? __ldcg(q) : make_float4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (i0 + i >= count) break;
+            o.x += x[i].x * w[i]; o.y += x[i].y * w[i]; o.z += x[i].z * w[i]; o.w += x[i].w * w[i];
+          }
+        }
+      }
+      const int rr = row0 + r;
+      const int64_t tok = tok0 + rr / a.pool.ratio;
+      const int hq = head * a.pool.ratio + rr % a.pool.ratio;
+      const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+      if (on)
+        *reinterpret_cast<uint2*>(a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + lane * 4)) =
+            make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
+      if (a.lse && lane == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
     }
   }
-  if (!parts) return;
-  const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-  if (lane * 4 < dim)
-    *reinterpret_cast<uint2*>(a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + lane * 4)) =
-        make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
-  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.pool.q_heads + hq] = log_sum(m, l);
+}
+template <typename T>
+__global__ void __launch_bounds__(128, 8) k_attend_join(AttendArgs a) {
+  chain();
+  const int4 h = __ldg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries
+  if (h.x != PS_OK) return;
+  const int64_t warp = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5, warps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  join_rows<T, 4>(a, 0, h.y, warp, warps, threadIdx.x & 31);
+  join_rows<T, 128>(a, 1, h.z, warp, warps, threadIdx.x & 31);
 }
 
 template <typename T, int DP>
@@ -460,16 +490,19 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   a.table_stride = b.table_stride;
   a.q_offsets = b.q_offsets;
   a.status = status;
-  a.num_tokens = b.num_tokens;
   a.layer = layer;
   a.scale2 = in.scale * 1.4426950408889634f;
-  cudaError_t e = launch_wide(a, maps, st);
+  // no tile has more rows than the whole batch
+  const bool wide = list_of(b.num_tokens * p.ratio) == 1;
+  a.after_wide = wide;
+  cudaError_t e = wide ? launch_wide(a, maps, st) : cudaSuccess;
   if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
   if (e != cudaSuccess) return status_of(e);
-  const int64_t warps = (int64_t)b.num_tokens * p.q_heads;
-  const dim3 grid((unsigned)((warps + 7) / 8));
-  e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 256, 0, st, a)
-                            : launch(k_attend_join<__half>, grid, 256, 0, st, a);
+  // warps for every narrow tile's rows at once, up to one full wave
+  const int64_t want = (int64_t)b.num_tokens * p.kv_heads, most = (int64_t)plan.max_ctas[1] * 16;
+  const dim3 grid((unsigned)(want < most ? want : most));
+  e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 128, 0, st, a)
+                            : launch(k_attend_join<__half>, grid, 128, 0, st, a);
   return status_of(e);
 }
 

@@ -19,7 +19,7 @@ struct AttendArgs {
   int64_t table_stride;
   const int32_t* q_offsets;
   int32_t* status;
-  int32_t num_tokens, layer;
+  int32_t layer, after_wide;  // after_wide: the wide tiles' kernel was launched
   float scale2;  // scale log2(e)
 };
 

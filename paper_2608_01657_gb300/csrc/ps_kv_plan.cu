@@ -119,15 +119,10 @@ __device__ __forceinline__ int tile_end(const Item& it, const Pool& p, int last_
 }
 __device__ __forceinline__ int unit_count(int keys, int unit) { return keys > 0 ? (keys + unit - 1) / unit : 1; }
 
-// More rows than a narrow tile's 16 go to the wide tiles.
-__device__ __forceinline__ int list_of(int rows) { return rows > tile_rows(0) ? 1 : 0; }
 
 __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, Batch b, int32_t* status) {
   chain();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ int s_join;
-  if (tid == 0) s_join = 0;
-  __syncthreads();
   int bad = 0;
   for (int r = tid; r < b.num_requests; r += kPlanThreads) bad |= plan.bad[r];
   if (b.num_requests == 0) bad |= b.num_tokens != 0;
@@ -255,7 +250,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   for (int l = 0; l < kLists; ++l) {
     ctas[l] = (int)(units[l] < plan.max_ctas[l] ? units[l] : plan.max_ctas[l]);
     if (tid == 0) plan.ucum[l][tiles[l]] = units[l];
-    if (shared[l] > 0) s_join = 1;
   }
   __syncthreads();
   for (int l = 0; l < kLists; ++l) {
@@ -268,21 +262,69 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
         else hi = mid - 1;
       }
       plan.cta_tile[l][c] = lo;
-      const int64_t per_head = (plan.ucum[l][lo + 1] - plan.ucum[l][lo]) / p.kv_heads;
-      if ((u - plan.ucum[l][lo]) % per_head) s_join = 1;  // a (tile, head) is cut here
     }
   }
-  __syncthreads();
   if (tid == 0) {
     PlanHdr h{};
     h.status = PS_OK;
-    h.join = s_join;
     for (int l = 0; l < kLists; ++l) {
       h.ntiles[l] = (int)tiles[l];
       h.ctas[l] = ctas[l];
       h.units[l] = units[l];
     }
     *plan.hdr = h;
+  }
+}
+
+// The partial results of a (tile, head).
+template <int H>
+__device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, const PlanHdr& h, int list, int tile, int head) {
+  const int64_t U = h.units[list], b = plan.ucum[list][tile];
+  const int C = h.ctas[list];
+  const int64_t nu = (plan.ucum[list][tile + 1] - b) / p.kv_heads, ua = b + head * nu;
+  const int ca = cta_of(ua, U, C), cb = cta_of(ua + nu - 1, U, C);
+  const Tile& t = plan.tiles[list][tile];
+  Parts4 r;
+  r.count = t.sidx < 0 && ca == cb ? 0 : cb - ca + 1;  // a whole one is written where it is computed
+  r.first = (int)part_row<H>(t.sidx, t.nrows, head, ca, U * ca / C > ua, C);
+  r.second = (int)part_row<H>(t.sidx, t.nrows, head, ca + 1, true, C);
+  r.stride = t.sidx < 0 ? 2 * H : H;
+  return r;
+}
+__device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, const PlanHdr& h, int list, int tile, int head) {
+  return list ? parts_of<tile_rows(1)>(plan, p, h, 1, tile, head) : parts_of<tile_rows(0)>(plan, p, h, 0, tile, head);
+}
+
+// One CTA a request: the (tile, head)s whose rows have partial results.  Their
+// order is left to the counter: each is joined by itself.
+__global__ void __launch_bounds__(kReqThreads) k_plan_joins(Pool p, Plan plan, Batch b) {
+  chain();
+  const PlanHdr h = *plan.hdr;
+  if (h.status != PS_OK) return;
+  const ReqRec rec = plan.req[blockIdx.x];
+  const int H = tile_rows(rec.list);
+  const int rows = (b.q_offsets[blockIdx.x + 1] - b.q_offsets[blockIdx.x]) * p.ratio;
+  const int n = (rows + H - 1) / H * p.kv_heads;
+  for (int i = threadIdx.x; i < n; i += kReqThreads) {
+    const int tile = rec.tile0 + i / p.kv_heads, head = i % p.kv_heads;
+    JoinRec j{};
+    j.own = parts_of(plan, p, h, rec.list, tile, head);
+    if (j.own.count == 0) continue;
+    const Tile& t = plan.tiles[rec.list][tile];
+    j.tok0 = t.tok0;
+    j.row0 = t.row0;
+    j.nrows = t.nrows;
+    j.head = head;
+    j.plist = -1;
+    if (rec.ptile0 >= 0) {
+      const int PH = tile_rows(rec.plist), prow = rec.prow0 + t.row0, pt = rec.ptile0 + prow / PH;
+      j.plist = rec.plist;
+      j.pofs = prow % PH;
+      j.psplit = PH - j.pofs;
+      j.pa = parts_of(plan, p, h, rec.plist, pt, head);
+      if (j.psplit < t.nrows) j.pb = parts_of(plan, p, h, rec.plist, pt + 1, head);
+    }
+    plan.joins[rec.list][atomicAdd(&plan.hdr->joins[rec.list], 1)] = j;
   }
 }
 
@@ -293,7 +335,10 @@ int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* st
     const cudaError_t e = launch(k_plan_requests, dim3((unsigned)b.num_requests), kReqThreads, 0, st, p, plan, b);
     if (e != cudaSuccess) return status_of(e);
   }
-  return status_of(launch(k_plan_tiles, dim3(1), kPlanThreads, 0, st, p, plan, b, status));
+  cudaError_t e = launch(k_plan_tiles, dim3(1), kPlanThreads, 0, st, p, plan, b, status);
+  if (e == cudaSuccess && b.num_requests > 0)
+    e = launch(k_plan_joins, dim3((unsigned)b.num_requests), kReqThreads, 0, st, p, plan, b);
+  return status_of(e);
 }
 
 }  // namespace pskv

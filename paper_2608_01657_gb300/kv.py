@@ -15,7 +15,12 @@ from __future__ import annotations
 import ctypes as C
 from typing import Optional
 
+import torch
+
 from . import binding as B
+
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _need(ok: bool, what: str):
@@ -33,7 +38,6 @@ class KVPool:
 
     def __init__(self, k, v, num_q_heads: int, first_page: int = 0, max_requests: int = 1, max_tokens: int = 1,
                  max_row_pages: int = 1, stream=None):
-        import torch
         L = B.load()
         _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype,
               "k and v must be alike: [layers, pages, page_size, kv_heads, head_dim]")
@@ -60,6 +64,17 @@ class KVPool:
                                                    B._stream_ptr(stream)))
         self._h = h
         self._batch = None
+        # argument structures and entry points of the calls that a decode step
+        # makes for every layer; their fields are filled in anew each time
+        self._lib = L
+        self._status = self.status.data_ptr()
+        self._append_args, self._attention_args = B.PsKvAppend(), B.PsKvAttention()
+        self._append_ref, self._attention_ref = C.byref(self._append_args), C.byref(self._attention_args)
+        self._rows_args = B.PsKvRows()
+        self._rows_ref = C.byref(self._rows_args)
+        self._private = max(0, self.pages - self.first_page)
+        self._append_strides = [getattr(self._append_args, n) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+        self._attention_strides = [getattr(self._attention_args, n) for n in ("q_stride", "out_stride")]
 
     def close(self):
         if getattr(self, "_h", None):
@@ -84,27 +99,40 @@ class KVPool:
             self.status.zero_()
             self._raise("a call on the pool", rc)
 
+    def _made(self, tokens: int, stream):
+        """A new [tokens, q_heads, head_dim] tensor that a call on ``stream`` writes."""
+        t = torch.empty(tokens, self.q_heads, self.head_dim, dtype=self.dtype, device=self.device)
+        if stream is not None:
+            t.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+        return t
+
     # -- argument checks ---------------------------------------------------
-    def _heads(self, t, heads: int, name: str, tokens: Optional[int] = None):
-        _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.head_dim and t.dtype == self.dtype
-              and t.device == self.device, f"{name} must be {self.dtype} [tokens, {heads}, {self.head_dim}]")
-        _need(tokens is None or t.shape[0] == tokens, f"{name} must have {tokens} tokens")
+    def _stream(self, stream):
+        return _raw_stream(self.device.index) if stream is None else B._stream_ptr(stream)
+
+    def _heads(self, t, tokens: int, heads: int, name: str, strides):
+        """Checks [tokens, heads, head_dim]; its strides go to ``strides``."""
+        if t.shape != (tokens, heads, self.head_dim) or t.dtype is not self.dtype or t.device != self.device:
+            raise ValueError(f"{name} must be {self.dtype} [{tokens}, {heads}, {self.head_dim}] on {self.device}")
+        s0, s1, s2 = t.stride()
         # an axis of one element is never stepped over: its stride may be any number
-        s = [t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)]
-        _need((t.stride(2) == 1 or self.head_dim == 1) and s[0] % 8 == 0 and s[1] % 8 == 0 and t.data_ptr() % 16 == 0,
-              f"{name}: heads must be contiguous, on 16-byte boundaries")
-        return (C.c_int64 * 2)(*s)
+        strides[0] = s0 = s0 if tokens > 1 else 0
+        strides[1] = s1 = s1 if heads > 1 else 0
+        p = t.data_ptr()
+        if s2 != 1 or (s0 | s1) & 7 or p & 15:
+            raise ValueError(f"{name}: heads must be contiguous, on 16-byte boundaries")
+        return p
 
     def _array(self, t, dtype, name: str, n: Optional[int] = None):
-        _need(t.dim() == 1 and t.dtype == dtype and t.device == self.device and t.is_contiguous()
-              and (n is None or t.shape[0] == n), f"{name} must be a contiguous {dtype} array" +
-              ("" if n is None else f" of {n}"))
+        sh = t.shape
+        if len(sh) != 1 or t.dtype is not dtype or t.device != self.device or not t.is_contiguous() or (
+                n is not None and sh[0] != n):
+            raise ValueError(f"{name} must be a contiguous {dtype} array" + ("" if n is None else f" of {n}"))
         return t.data_ptr()
 
     def _table(self, t, name: str):
-        import torch
-        _need(t.dim() == 2 and t.dtype == torch.int32 and t.device == self.device and t.is_contiguous(),
-              f"{name} must be a contiguous int32 [rows, pages] tensor")
+        if len(t.shape) != 2 or t.dtype is not torch.int32 or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 [rows, pages] tensor")
 
     # -- one layer's new tokens ----------------------------------------------
     def append(self, layer: int, q, k, v, slots, positions=None, rope=None, interleaved: bool = False, q_weight=None,
@@ -113,29 +141,33 @@ class KVPool:
         [rows, rope_dim] float32: cosines, then sines) of the new tokens'
         queries and keys; keys and values go to ``slots`` (page * page_size +
         offset, int64; negative: not written).  Returns the queries."""
-        import torch
-        T = int(q.shape[0])
-        a = B.PsKvAppend(q_stride=self._heads(q, self.q_heads, "q"), k_stride=self._heads(k, self.kv_heads, "k", T),
-                         v_stride=self._heads(v, self.kv_heads, "v", T))
+        a, st = self._append_args, self._append_strides
+        T = q.shape[0]
         if q_out is None:
-            q_out = torch.empty(T, self.q_heads, self.head_dim, dtype=self.dtype, device=self.device)
-        a.q_out_stride = self._heads(q_out, self.q_heads, "q_out", T)
-        a.q, a.k, a.v, a.q_out = q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr()
+            q_out = self._made(T, stream)
+        a.q = self._heads(q, T, self.q_heads, "q", st[0])
+        a.k = self._heads(k, T, self.kv_heads, "k", st[1])
+        a.v = self._heads(v, T, self.kv_heads, "v", st[2])
+        a.q_out = self._heads(q_out, T, self.q_heads, "q_out", st[3])
         a.slots = self._array(slots, torch.int64, "slots", T)
         if rope is not None:
-            _need(positions is not None, "a rotation needs positions")
-            _need(rope.dim() == 2 and rope.dtype == torch.float32 and rope.is_contiguous() and rope.device == self.device,
-                  "rope must be a contiguous float32 [rows, rope_dim] table")
+            if positions is None:
+                raise ValueError("a rotation needs positions")
+            if len(rope.shape) != 2 or rope.dtype is not torch.float32 or not rope.is_contiguous() or rope.device != self.device:
+                raise ValueError("rope must be a contiguous float32 [rows, rope_dim] table")
             a.positions = self._array(positions, torch.int32, "positions", T)
-            a.rope, a.rope_rows, a.rope_dim = rope.data_ptr(), int(rope.shape[0]), int(rope.shape[1])
-            a.rope_interleaved = int(interleaved)
-        if q_weight is not None:
-            a.q_weight = self._array(q_weight, self.dtype, "q_weight", self.head_dim)
-        if k_weight is not None:
-            a.k_weight = self._array(k_weight, self.dtype, "k_weight", self.head_dim)
+            a.rope = rope.data_ptr()
+            a.rope_rows, a.rope_dim = rope.shape
+            a.rope_interleaved = 1 if interleaved else 0
+        else:
+            a.positions = a.rope = None
+            a.rope_dim = 0
+        a.q_weight = None if q_weight is None else self._array(q_weight, self.dtype, "q_weight", self.head_dim)
+        a.k_weight = None if k_weight is None else self._array(k_weight, self.dtype, "k_weight", self.head_dim)
         a.eps, a.num_tokens = eps, T
-        self._raise("ps_kv_append", B.load().ps_kv_append(self._h, B._stream_ptr(stream), int(layer), C.byref(a),
-                                                          self.status.data_ptr()))
+        rc = self._lib.ps_kv_append(self._h, self._stream(stream), layer, self._append_ref, self._status)
+        if rc:
+            self._raise("ps_kv_append", rc)
         return q_out
 
     # -- attention -------------------------------------------------------------
@@ -145,89 +177,99 @@ class KVPool:
         last of its kv_lens[i]; ``group_offsets`` divides the requests into
         runs of neighbours that may share a prefix.  The tensors must stay
         unchanged while the plan is used."""
-        import torch
         R = int(kv_lens.shape[0])
         self._table(tables, "tables")
-        _need(tables.shape[0] >= R, "tables must have a row for each request")
+        _need(int(tables.shape[0]) >= R, "tables must have a row for each request")
         b = B.PsKvBatch(q_offsets=self._array(q_offsets, torch.int32, "q_offsets", R + 1),
                         kv_lens=self._array(kv_lens, torch.int32, "kv_lens"), tables=tables.data_ptr(),
                         table_stride=int(tables.shape[1]), num_requests=R, num_tokens=int(num_tokens), causal=int(causal))
         if group_offsets is not None:
             b.group_offsets, b.num_groups = self._array(group_offsets, torch.int32, "group_offsets"), int(group_offsets.shape[0]) - 1
         self._batch = None
-        self._raise("ps_kv_plan", B.load().ps_kv_plan(self._h, B._stream_ptr(stream), C.byref(b), self.status.data_ptr()))
+        self._raise("ps_kv_plan", self._lib.ps_kv_plan(self._h, self._stream(stream), C.byref(b), self._status))
         self._batch = (q_offsets, kv_lens, tables, group_offsets, int(num_tokens))  # alive while the plan is
 
     def attention(self, layer: int, q, scale: float, out=None, lse=None, stream=None):
         """softmax(scale q k^T) v of one layer for the planned batch.  ``lse``
         (optional, float32 [tokens, q_heads]) receives the scores' log-sum-exp."""
-        import torch
-        _need(self._batch is not None, "attention needs a plan")
+        if self._batch is None:
+            raise ValueError("attention needs a plan")
         T = self._batch[4]
         if out is None:
-            out = torch.empty(T, self.q_heads, self.head_dim, dtype=self.dtype, device=self.device)
-        a = B.PsKvAttention(q=q.data_ptr(), out=out.data_ptr(), q_stride=self._heads(q, self.q_heads, "q", T),
-                            out_stride=self._heads(out, self.q_heads, "out", T), scale=scale)
+            out = self._made(T, stream)
+        a, st = self._attention_args, self._attention_strides
+        a.q = self._heads(q, T, self.q_heads, "q", st[0])
+        a.out = self._heads(out, T, self.q_heads, "out", st[1])
+        a.scale = scale
         if lse is not None:
-            _need(lse.dtype == torch.float32 and tuple(lse.shape) == (T, self.q_heads) and lse.is_contiguous()
-                  and lse.device == self.device, "lse must be contiguous float32 [tokens, q_heads]")
+            if lse.shape != (T, self.q_heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.device != self.device:
+                raise ValueError("lse must be contiguous float32 [tokens, q_heads]")
             a.lse = lse.data_ptr()
-        self._raise("ps_kv_attention", B.load().ps_kv_attention(self._h, B._stream_ptr(stream), int(layer), C.byref(a),
-                                                                self.status.data_ptr()))
+        else:
+            a.lse = None
+        rc = self._lib.ps_kv_attention(self._h, self._stream(stream), layer, self._attention_ref, self._status)
+        if rc:
+            self._raise("ps_kv_attention", rc)
         return out
 
     # -- pages -------------------------------------------------------------------
     def copy(self, src, dst, stream=None):
         """Copy whole pages src[i] -> dst[i], all layers."""
-        import torch
-        n = int(src.shape[0])
-        self._raise("ps_kv_copy", B.load().ps_kv_copy(
-            self._h, B._stream_ptr(stream), n, self._array(src, torch.int32, "src"),
-            self._array(dst, torch.int32, "dst", n), self.status.data_ptr()))
+        n = src.shape[0]
+        rc = self._lib.ps_kv_copy(self._h, self._stream(stream), n, self._array(src, torch.int32, "src"),
+                                  self._array(dst, torch.int32, "dst", n), self._status)
+        if rc:
+            self._raise("ps_kv_copy", rc)
 
     def _rows(self, tables, lens, held):
-        import torch
+        """Fills in the structure of the rows; returns the reference to pass."""
         self._table(tables, "tables")
-        n = int(tables.shape[0])
-        return B.PsKvRows(tables=tables.data_ptr(), lens=None if lens is None else self._array(lens, torch.int32, "lens", n),
-                          held=self._array(held, torch.int32, "held", n), table_stride=int(tables.shape[1]), num_rows=n)
+        r = self._rows_args
+        r.num_rows, r.table_stride = n, _ = tables.shape
+        r.tables = tables.data_ptr()
+        r.lens = None if lens is None else self._array(lens, torch.int32, "lens", n)
+        r.held = self._array(held, torch.int32, "held", n)
+        return self._rows_ref
 
     def _refs(self, refs, name="refs"):
-        import torch
-        return self._array(refs, torch.int32, name, max(0, self.pages - self.first_page))
+        return self._array(refs, torch.int32, name, self._private)
 
     def fork(self, parents, children, room, tables, lens, held, refs, refs_out=None, stream=None):
         """Rows ``children`` become continuations of rows ``parents`` with
         pages for ``room`` tokens: in place (parent == child), new (parent -1)
         or a fork that shares the full pages and copies the partial one."""
-        import torch
-        n = int(parents.shape[0])
-        rows = self._rows(tables, lens, held)
-        self._raise("ps_kv_fork", B.load().ps_kv_fork(
-            self._h, B._stream_ptr(stream), n, self._array(parents, torch.int32, "parents"),
-            self._array(children, torch.int32, "children", n), self._array(room, torch.int32, "room", n), C.byref(rows),
-            self._refs(refs), self._refs(refs if refs_out is None else refs_out, "refs_out"), self.status.data_ptr()))
+        n = parents.shape[0]
+        rows, before = self._rows(tables, lens, held), self._refs(refs)
+        rc = self._lib.ps_kv_fork(
+            self._h, self._stream(stream), n, self._array(parents, torch.int32, "parents"),
+            self._array(children, torch.int32, "children", n), self._array(room, torch.int32, "room", n), rows,
+            before, before if refs_out is None else self._refs(refs_out, "refs_out"), self._status)
+        if rc:
+            self._raise("ps_kv_fork", rc)
 
     def release(self, rows, tables, lens, held, refs, stream=None):
         """Free the pages that ``rows`` hold."""
-        import torch
         r = self._rows(tables, lens, held)
-        self._raise("ps_kv_release", B.load().ps_kv_release(
-            self._h, B._stream_ptr(stream), int(rows.shape[0]), self._array(rows, torch.int32, "rows"), C.byref(r),
-            self._refs(refs), self.status.data_ptr()))
+        rc = self._lib.ps_kv_release(self._h, self._stream(stream), rows.shape[0], self._array(rows, torch.int32, "rows"), r,
+                                     self._refs(refs), self._status)
+        if rc:
+            self._raise("ps_kv_release", rc)
 
     def compact(self, tables, held, refs, tables_out=None, refs_out=None, counts=None, stream=None):
         """Move the private pages in use to the lowest ids.  Returns the int32
         tensor (pages in use, pages moved)."""
-        import torch
-        r = self._rows(tables, None, held)
+        r, before = self._rows(tables, None, held), self._refs(refs)
         if counts is None:
             counts = torch.empty(2, dtype=torch.int32, device=self.device)
+            if stream is not None:
+                counts.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
         tables_out = tables if tables_out is None else tables_out
         self._table(tables_out, "tables_out")
         _need(tables_out.shape == tables.shape, "tables_out must be shaped as tables")
-        self._raise("ps_kv_compact", B.load().ps_kv_compact(
-            self._h, B._stream_ptr(stream), C.byref(r), self._refs(refs), tables_out.data_ptr(),
-            self._refs(refs if refs_out is None else refs_out, "refs_out"), self._array(counts, torch.int32, "counts", 2),
-            self.status.data_ptr()))
+        rc = self._lib.ps_kv_compact(
+            self._h, self._stream(stream), r, before, tables_out.data_ptr(),
+            before if refs_out is None else self._refs(refs_out, "refs_out"), self._array(counts, torch.int32, "counts", 2),
+            self._status)
+        if rc:
+            self._raise("ps_kv_compact", rc)
         return counts
