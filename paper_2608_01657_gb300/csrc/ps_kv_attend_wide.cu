@@ -50,7 +50,7 @@ struct Shape {
 };
 
 struct Shared {
-  uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full, q_empty, ml_full, ml_free;
+  uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full, q_empty, ml_full, ml_free, turn[2];
   uint32_t tmem;
   float2 ml[128];  // split mode: group 1's (maximum, sum)
 };
@@ -343,7 +343,9 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
 // One warp for each group t, of which one thread issues: a product issued under
 // a predicate by a whole warp took nearly twice as long (113 cycles against 64,
 // 128 x 128 x 16), and every wait between products drains the issuing thread's
-// queue (some 200 cycles), which the other group's products fill.
+// queue (some 200 cycles), which the other group's products fill.  The groups
+// take turns: left to themselves they fell into step, both waiting for weights
+// or both for products (4500 cycles for a unit's 2048 of products).
 template <typename T, int DP>
 __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t, uint32_t tmem, uint32_t qs, uint32_t ring, Parts ps) {
   using S = Shape<DP>;
@@ -353,7 +355,7 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
   const uint32_t q_desc = desc_low(qs, 16), k_desc = desc_low(ring, 16), v_desc = desc_low(ring, 128 * 128);
   constexpr uint32_t kBlk = S::kBlock >> 4;
   const uint32_t s_at = tmem + col_s(t), o_at = tmem + col_o(t);
-  uint32_t p_phase = 0;
+  uint32_t p_phase = 0, turn = t ^ 1;  // group 0 has the first turn
   Place<S::kBuffers> at;  // the key block of the tile's unit in turn; its value block is the next
   uint32_t seg = 0;
   bool more = true;
@@ -369,14 +371,15 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
     };
     Place<S::kBuffers> kb = at;
     if (!pair && t == 1) kb = kb.ahead(2);
-    const int step = pair ? 1 : 2;
-    // unit u's values, then the scores of this group's next unit; the first
-    // turn is the first scores alone.  The blocks' waits come before the wait for
-    // the weights, where there is time.
+    const int step = pair ? 1 : 2, first = pair ? 0 : t, turns = pair ? n : (n + 1) / 2;
+    // Turn i: unit u's values, then the scores of this group's next unit (turn -1
+    // is the first scores alone).  The blocks' waits come before the wait for the
+    // weights, where there is time; the groups' turns alternate.
 #pragma unroll 1
-    for (int u = (pair ? 0 : t) - step; u < n; u += step) {
+    for (int i = -1; i < turns; ++i) {
+      const int u = first + i * step;
       const Place<S::kBuffers> vb = kb.ahead(1);
-      const bool product = u >= 0, more_keys = u + step < n;
+      const bool product = i >= 0 && u < n, more_keys = u + step < n;
       if (product) {
         if (!bar_wait(&sh->full[vb.slot], vb.par)) return false;
         kb = kb.ahead(2 * step);
@@ -385,13 +388,16 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
       if (product) {
         if (!bar_wait(&sh->p_full[t], p_phase)) return false;
         p_phase ^= 1;
-        tc_after();
+      }
+      if (!bar_wait(&sh->turn[t], turn)) return false;
+      turn ^= 1;
+      tc_after();
+      if (product) {
         const uint32_t v = v_desc + vb.slot * kBlk;
 #pragma unroll
-        for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, u >= step || s > 0);
+        for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
       }
       if (more_keys) {
-        tc_after();
         const uint32_t k = k_desc + kb.slot * kBlk;
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) {
@@ -402,11 +408,12 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
       } else if (product) {
         tc_commit(&sh->o_full[t]);
       }
+      bar_arrive(&sh->turn[t ^ 1]);
       if (product) release(vb);
       if (more_keys) release(kb);
       if (more_keys && u + 2 * step >= n) tc_commit(&sh->q_empty);  // the last scores are on their way
     }
-    if (!pair && t == 1 && n == 1) tc_commit(&sh->q_empty);  // no scores at all
+    if (first >= n) tc_commit(&sh->q_empty);  // no scores at all
     at = at.skip(2 * n);
   }
   return true;
@@ -613,6 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
       bar_init(&sh.s_full[t], 1);
       bar_init(&sh.p_full[t], 4);
       bar_init(&sh.o_full[t], 1);
+      bar_init(&sh.turn[t], 1);
     }
     bar_init(&sh.q_full, kLoaderWarps);
     bar_init(&sh.q_empty, 2);
