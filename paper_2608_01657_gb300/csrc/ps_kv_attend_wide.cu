@@ -85,20 +85,22 @@ __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_
 __device__ __forceinline__ void tc_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-// d (+)= a b: both operands in shared memory, or a in tensor memory.  Of a shared
-// memory operand's descriptor the low word differs, see desc_low.
-constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;  // 8 rows are 1024 bytes; 128-byte swizzle
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
-  asm volatile(
-      "{ .reg .pred p; .reg .b64 a, b; mov.b64 a, {%1, %5}; mov.b64 b, {%2, %5}; setp.ne.u32 p, %4, 0;"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add),
-      "r"(kDescHigh) : "memory");
+// d (+)= a b: both operands in shared memory, or a in tensor memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+               "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
-  asm volatile(
-      "{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.u32 p, %4, 0;"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add),
-      "r"(kDescHigh) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+               "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// True in one lane of a converged warp.  The matrix instructions' operands are
+// uniform registers: issued by the elected lane they take 5 instructions each,
+// under a test of the lane's number up to 44.
+__device__ __forceinline__ bool elect() {
+  uint32_t e;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(e));
+  return e != 0;
 }
 #define R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -155,11 +157,12 @@ __device__ __forceinline__ void cp_wait() {
 }
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Low word of the descriptor of a block of 128-byte rows with the 128-byte
-// swizzle: its address, and the distance 'lead' of the second 64-element half
-// where the rows are the contraction's (values), unused where they are the
-// result's.
-__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead) { return addr >> 4 | lead >> 4 << 16; }
+// Descriptor of a block of 128-byte rows with the 128-byte swizzle.  Eight rows
+// are 1024 bytes; 'lead' is the distance of the second 64-element half where the
+// rows are the contraction's (values), unused where they are the result's.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
+  return (uint64_t)(1024 >> 4 | 1u << 14 | 2u << 29) << 32 | (lead >> 4 << 16) | addr >> 4;
+}
 // Instruction descriptor: 32-bit sums of 16-bit products, 128 rows, n columns.
 template <typename T>
 __device__ __forceinline__ uint32_t instr_desc(int n, bool b_rows_contract) {
@@ -340,10 +343,8 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
 }
 
 // ---- the warps that issue the matrix instructions -------------------------------------
-// One warp for each group t, of which one thread issues: a product issued under
-// a predicate by a whole warp took nearly twice as long (113 cycles against 64,
-// 128 x 128 x 16), and every wait between products drains the issuing thread's
-// queue (some 200 cycles), which the other group's products fill.  The groups
+// One warp for each group t.  Every wait between products drains the warp's queue
+// of them (some 200 cycles), which the other group's products fill.  The groups
 // take turns: left to themselves they fell into step, both waiting for weights
 // or both for products (4500 cycles for a unit's 2048 of products).
 template <typename T, int DP>
@@ -352,7 +353,7 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
   // scores are negated where the scale is negative
   const uint32_t id_qk = instr_desc<T>(UNIT, false) | (a.scale2 < 0 ? 1u << 13 : 0), id_pv = instr_desc<T>(DP, true);
   // descriptors differ in their address field alone
-  const uint32_t q_desc = desc_low(qs, 16), k_desc = desc_low(ring, 16), v_desc = desc_low(ring, 128 * 128);
+  const uint64_t q_desc = smem_desc(qs, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, 128 * 128);
   constexpr uint32_t kBlk = S::kBlock >> 4;
   const uint32_t s_at = tmem + col_s(t), o_at = tmem + col_o(t);
   uint32_t p_phase = 0, turn = t ^ 1;  // group 0 has the first turn
@@ -362,8 +363,8 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
   for (; more; ++seg, more = ps.next()) {
     const bool pair = ps.pair();
     const int n = ps.count;
-    if (!bar_wait(&sh->q_full, seg & 1)) return false;
-    const uint32_t q = q_desc + (pair ? t : 0) * kBlk;
+    if (!warp_wait(&sh->q_full, seg & 1)) return false;
+    const uint64_t q = q_desc + (pair ? t : 0) * kBlk;
     // a block's two arrivals: one of each group, or both of the one that uses it
     auto release = [&](const Place<S::kBuffers>& b) {
       tc_commit(&sh->empty[b.slot]);
@@ -381,39 +382,43 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
       const Place<S::kBuffers> vb = kb.ahead(1);
       const bool product = i >= 0 && u < n, more_keys = u + step < n;
       if (product) {
-        if (!bar_wait(&sh->full[vb.slot], vb.par)) return false;
+        if (!warp_wait(&sh->full[vb.slot], vb.par)) return false;
         kb = kb.ahead(2 * step);
       }
-      if (more_keys && !bar_wait(&sh->full[kb.slot], kb.par)) return false;
+      if (more_keys && !warp_wait(&sh->full[kb.slot], kb.par)) return false;
       if (product) {
-        if (!bar_wait(&sh->p_full[t], p_phase)) return false;
+        if (!warp_wait(&sh->p_full[t], p_phase)) return false;
         p_phase ^= 1;
       }
-      if (!bar_wait(&sh->turn[t], turn)) return false;
+      if (!warp_wait(&sh->turn[t], turn)) return false;
       turn ^= 1;
       tc_after();
-      if (product) {
-        const uint32_t v = v_desc + vb.slot * kBlk;
+      if (elect()) {
+        if (product) {
+          const uint64_t v = v_desc + vb.slot * kBlk;
 #pragma unroll
-        for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
-      }
-      if (more_keys) {
-        const uint32_t k = k_desc + kb.slot * kBlk;
-#pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) {
-          const int x = (s >> 2) * (128 * 128 >> 4) + (s & 3) * 2;
-          mma_ss(s_at, q + x, k + x, id_qk, s > 0);
+          for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
         }
-        tc_commit(&sh->s_full[t]);
-      } else if (product) {
-        tc_commit(&sh->o_full[t]);
+        if (more_keys) {
+          const uint64_t k = k_desc + kb.slot * kBlk;
+#pragma unroll
+          for (int s = 0; s < S::kSteps; ++s) {
+            const int x = (s >> 2) * (128 * 128 >> 4) + (s & 3) * 2;
+            mma_ss(s_at, q + x, k + x, id_qk, s > 0);
+          }
+          tc_commit(&sh->s_full[t]);
+        } else if (product) {
+          tc_commit(&sh->o_full[t]);
+        }
+        bar_arrive(&sh->turn[t ^ 1]);
+        if (product) release(vb);
+        if (more_keys) release(kb);
+        if (more_keys && u + 2 * step >= n) tc_commit(&sh->q_empty);  // the last scores are on their way
       }
-      bar_arrive(&sh->turn[t ^ 1]);
-      if (product) release(vb);
-      if (more_keys) release(kb);
-      if (more_keys && u + 2 * step >= n) tc_commit(&sh->q_empty);  // the last scores are on their way
+      __syncwarp();
     }
-    if (first >= n) tc_commit(&sh->q_empty);  // no scores at all
+    if (first >= n && elect()) tc_commit(&sh->q_empty);  // no scores at all
+    __syncwarp();
     at = at.skip(2 * n);
   }
   return true;
@@ -644,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoaderWarps) {
     ok = load_role<DP>(a, maps, &sh, qs, ring, ps);
     cp_wait<0>();
-  } else if (warp >= kSoftmaxWarps + kLoaderWarps && warp < kSoftmaxWarps + kLoaderWarps + 2 && lane == 0) {
+  } else if (warp >= kSoftmaxWarps + kLoaderWarps && warp < kSoftmaxWarps + kLoaderWarps + 2) {
     ok = mma_role<T, DP>(a, &sh, warp & 1, tmem, qs, ring, ps);
   }
   if (!ok && lane == 0) set_error(a.status, PS_ERR_TIMEOUT);
