@@ -29,9 +29,11 @@ struct Pool {
 // The work of a batch is a list of tiles: some query rows against a range of
 // keys.  The rows of a tile are (token, query head of one kv head) pairs, token
 // major, so a tile is run once for each kv head.  A tile's keys are cut into
-// units; unit u of the whole list (tile major, then kv head, then unit) belongs
-// to CTA c with floor(U c / C) <= u < floor(U (c + 1) / C): every CTA gets the
-// same number of units whatever the lengths are.  A (tile, head) that several
+// units.  A (tile, head) costs its units and tile_cost() more, for its beginning
+// and end; of the whole list's cost U (tile major, then kv head) CTA c gets
+// [floor(U c / C), floor(U (c + 1) / C)): every CTA the same, whatever the
+// lengths are.  Within a (tile, head) the beginning's cost comes first, unit u is
+// place tile_cost() + u.  A (tile, head) that several
 // CTAs work on, or whose rows also have a shared prefix, leaves partial results
 // (a running maximum, a sum, an unnormalized output) that k_attend_join puts
 // together in a fixed order.
@@ -57,6 +59,8 @@ struct ReqRec {
 constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen05)
 __host__ __device__ constexpr int tile_rows(int list) { return list ? 256 : 16; }
 __host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 64; }
+// What a (tile, head) costs beside its units, in units.
+__host__ __device__ constexpr int tile_cost(int list) { return list ? 2 : 1; }
 // The list of an item of so many rows.
 __host__ __device__ constexpr int list_of(int rows) { return rows > tile_rows(0) ? 1 : 0; }
 constexpr int kNoMask = 1 << 30;
@@ -82,7 +86,7 @@ struct __align__(16) PlanHdr {
   int32_t pad0;
   int32_t ntiles[kLists];
   int32_t ctas[kLists];     // C, 0 without tiles
-  int64_t units[kLists];    // U
+  int64_t cost[kLists];     // U
 };
 
 // Requests of more rows than this fill tiles of their own; a prefix shared by
@@ -102,7 +106,7 @@ inline PlanBounds plan_bounds(int list, int64_t R, int64_t rows) {
   return {2 * own, own, 2 * (rows < R * kShareRows ? rows : R * kShareRows)};
 }
 
-// The CTA of unit u: the largest c with floor(U c / C) <= u.
+// The CTA of place u: the largest c with floor(U c / C) <= u.
 __host__ __device__ __forceinline__ int cta_of(int64_t u, int64_t U, int64_t C) {
   return (int)(((u + 1) * C - 1) / U);
 }
@@ -117,10 +121,10 @@ struct Plan {
   int32_t* common;    // [max_requests] leading pages in common with the group's first request
   int32_t* bad;       // [max_requests]
   Tile* tiles[kLists];
-  int64_t* ucum[kLists];      // [tiles + 1] units before a tile, all heads
-  int32_t* cta_tile[kLists];  // [C] tile of a CTA's first unit
+  int64_t* ucum[kLists];      // [tiles + 1] cost before a tile, all heads
+  int32_t* cta_tile[kLists];  // [C] tile of a CTA's first place
   JoinRec* joins[kLists];     // [tiles of requests x kv heads]
-  float* part_o[kLists];      // [rows][head_dim] unnormalized outputs, see part_row
+  float4* part_o[kLists];     // unnormalized outputs of the rows, see part_row and part_word
   float2* part_ml[kLists];    // [rows] (maximum, sum), base 2
   int32_t max_ctas[kLists];
 };
@@ -144,6 +148,53 @@ struct PoolMaps {
   int32_t box;
 };
 bool make_maps(const Pool& p, PoolMaps* m);
+
+// Place of the four elements from 4 c on of partial row r: eight rows' words lie
+// side by side, so that a warp of 32 rows (wide tiles) and one of eight rows by
+// four words (narrow tiles, the join) write and read whole lines.
+__device__ __forceinline__ int64_t part_word(int64_t r, int c, int head_dim) {
+  return ((r >> 3) * (head_dim >> 2) + c) * 8 + (r & 7);
+}
+
+// A CTA's part of a list, one (tile, head) at a time.
+template <int LIST>
+struct Parts {
+  static constexpr int K = tile_cost(LIST);
+  const Tile* tiles;
+  const int64_t* ucum;
+  int heads, left, tile, head, unit, nunits, count;  // units [unit, unit + count) of nunits; left: cost from the head's begin
+  Tile t;
+  // False if there is no unit in it.
+  __device__ __forceinline__ bool start(const Plan& plan, int kv_heads, int c, int64_t u0, int64_t u1) {
+    tiles = plan.tiles[LIST];
+    ucum = plan.ucum[LIST];
+    heads = kv_heads;
+    tile = plan.cta_tile[LIST][c];
+    t = tiles[tile];
+    const int64_t b = ucum[tile];
+    const int each = (int)((ucum[tile + 1] - b) / heads);
+    nunits = each - K;
+    head = (int)((u0 - b) / each);
+    const int at = (int)((u0 - b) % each);
+    left = (int)(u1 - u0) + at;
+    unit = at > K ? at - K : 0;
+    count = (left < each ? left : each) - K - unit;
+    return count > 0;
+  }
+  __device__ __forceinline__ bool next() {
+    left -= nunits + K;
+    if (left <= K) return false;
+    unit = 0;
+    if (++head == heads) {
+      head = 0;
+      ++tile;
+      t = tiles[tile];
+      nunits = (int)((ucum[tile + 1] - ucum[tile]) / heads) - K;
+    }
+    count = (left < nunits + K ? left : nunits + K) - K;
+    return true;
+  }
+};
 
 struct Batch {
   const int32_t *q_offsets, *kv_lens, *tables, *group_offsets;

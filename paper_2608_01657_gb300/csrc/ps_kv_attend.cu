@@ -90,42 +90,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
     after_wide();
     return;
   }
-  const int64_t U = hdr->units[0];
-  const int64_t u0 = U * c / C;
-  const int n = (int)(U * (c + 1) / C - u0);
+  const int64_t U = hdr->cost[0];
+  Parts<0> ps;
+  if (!ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) {
+    after_wide();
+    return;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t ring = smem_addr(smem) + warp * S::kWarpBytes;
-  const Tile* tiles = a.plan.tiles[0];
-  const int64_t* ucum = a.plan.ucum[0];
-
-  // where the first unit lies
-  int tile = a.plan.cta_tile[0][c], head, unit, nunits;
-  {
-    const int64_t b = ucum[tile];
-    nunits = (int)((ucum[tile + 1] - b) / a.pool.kv_heads);
-    head = (int)((u0 - b) / nunits);
-    unit = (int)((u0 - b) % nunits);
-  }
 
   // ---- the loader: runs STAGES - 1 units ahead ----
-  Tile lt = tiles[tile];
-  int ltile = tile, lhead = head, lunit = unit, lnunits = nunits, lleft = n;
+  Parts<0> lp = ps;
+  int lunit = lp.unit, lend = lp.unit + lp.count;
+  bool lmore = true;
   const char* kbase = a.k;
   const char* vbase = a.v;
   // page id of this lane's key in the loader's unit, -1 past the end
   auto key_page = [&]() -> int {
-    const int t = lt.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
-    return t < lt.kv1 ? __ldg(a.tables + lt.req * a.table_stride + (t >> a.pool.page_log2)) : -1;
+    const int t = lp.t.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
+    return t < lp.t.kv1 ? __ldg(a.tables + lp.t.req * a.table_stride + (t >> a.pool.page_log2)) : -1;
   };
-  int page = lleft > 0 ? key_page() : -1;
+  int page = key_page();
   int lstage = 0;
   auto load_unit = [&]() {
-    if (lleft > 0) {
-      const int t = lt.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
+    if (lmore) {
+      const int t = lp.t.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
       int64_t off = -1;
       if (page >= 0)
         off = page * a.pool.page_stride + (int64_t)(t & (a.pool.page_size - 1)) * a.pool.token_stride +
-              lhead * a.pool.head_stride;
+              lp.head * a.pool.head_stride;
       const uint32_t dst = ring + lstage * S::kStage;
 #pragma unroll
       for (int j = 0; j < 16 * CH / 32; ++j) {
@@ -137,19 +130,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
         cp16(d, kbase + at, ok);
         cp16(d + 16 * S::kRow, vbase + at, ok);
       }
-      --lleft;
-      if (lleft > 0) {
-        if (++lunit == lnunits) {
-          lunit = 0;
-          if (++lhead == a.pool.kv_heads) {
-            lhead = 0;
-            ++ltile;
-            lt = tiles[ltile];
-            lnunits = (int)((ucum[ltile + 1] - ucum[ltile]) / a.pool.kv_heads);
-          }
-        }
-        page = key_page();
+      if (++lunit == lend) {
+        lmore = lp.next();
+        lunit = lp.unit;
+        lend = lp.unit + lp.count;
       }
+      if (lmore) page = key_page();
     }
     cp_commit();
     lstage = lstage + 1 == S::kStages ? 0 : lstage + 1;
@@ -158,10 +144,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
   for (int s = 0; s < S::kStages - 1; ++s) load_unit();
 
   // ---- the consumer ----
-  int stage = 0, left = n;
+  int stage = 0;
   const int g = lane >> 2, q4 = lane & 3;
-  while (left > 0) {
-    const Tile t = tiles[tile];
+  for (bool more = true; more; more = ps.next()) {
+    const Tile t = ps.t;
+    const int head = ps.head;
     // queries of the 16 rows, as the A operand
     uint32_t qf[KS][4];
 #pragma unroll
@@ -189,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0;
 
-    const int first = unit, count = min(left, nunits - unit);
+    const int first = ps.unit, count = ps.count;
     for (int it = 0; it < count; ++it) {
       cp_wait<S::kStages - 2>();
       __syncwarp();  // the unit has landed, and the stage of the one before it is read
@@ -306,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
       }
     }
     if (warp == 0) {
-      const bool whole = first == 0 && count == nunits;
+      const bool whole = first == 0 && count == ps.nunits;
       if (whole && t.sidx < 0) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -327,7 +314,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
         }
       } else {
         const int64_t prow = part_row<H>(t.sidx, t.nrows, head, c, first > 0, C);
-        float* po = a.plan.part_o[0] + prow * a.pool.head_dim;
         float2* pml = a.plan.part_ml[0] + prow;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -336,19 +322,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i)
               if (i * 8 < a.pool.head_dim)
-                *reinterpret_cast<float2*>(po + r * a.pool.head_dim + i * 8 + q4 * 2) =
+                reinterpret_cast<float2*>(a.plan.part_o[0] + part_word(prow + r, 2 * i + (q4 >> 1), a.pool.head_dim))[q4 & 1] =
                     make_float2(o[i][2 * hf], o[i][2 * hf + 1]);
             if (q4 == 0) pml[r] = make_float2(m[hf], l[hf]);
           }
         }
       }
-    }
-    left -= count;
-    unit = 0;
-    if (++head == a.pool.kv_heads) {
-      head = 0;
-      ++tile;
-      if (left > 0) nunits = (int)((ucum[tile + 1] - ucum[tile]) / a.pool.kv_heads);
     }
   }
   cp_wait<0>();
@@ -356,86 +335,116 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
 }
 
 // ---- the join --------------------------------------------------------------------
-// W warps for each (tile, head) that has partial results, a row at a time: its
-// own tile's parts, then its group's prefix's, in CTA order, a lane for each.
-// Bound by the latency of its four dependent reads (the entry, the parts' maxima
-// and sums, their outputs, written just before and so in L2), which is why a
-// row's parts are all in flight at once.
-template <typename T, int W>
-__device__ __forceinline__ void join_rows(const AttendArgs& a, int list, int entries, int64_t item0, int64_t step, int lane) {
-  const int dim = a.pool.head_dim;
-  const bool on = lane * 4 < dim;
+// A warp for eight rows of a (tile, head) that has partial results, lane = row +
+// 8 (word mod 4): their own tile's parts, then their group's prefix's, in CTA
+// order.  Bound by the latency of its dependent reads (the entry; then each
+// part's maximum, sum and outputs, written just before and so in L2; the parts'
+// reads do not depend on one another).  SPLIT 4: the four warps of a CTA take a
+// quarter of the parts each, for when there are fewer rows than warps.
+constexpr int kJoinWords = PS_KV_MAX_HEAD_DIM / 16;  // of a lane
+struct JoinShared {
+  float4 o[3][kJoinWords][32];
+  float2 ml[3][32];
+};
+template <typename T, int H, int SPLIT>
+__device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, int list, int entries, int64_t item0,
+                                          int64_t step, int sub, int lane) {
+  const int dim = a.pool.head_dim, words = dim >> 2;
+  constexpr int W = H / 8, NW = kJoinWords;  // warps of an entry
   for (int64_t it = item0; it < (int64_t)entries * W; it += step) {
     static_assert(sizeof(JoinRec) == 80, "one word a lane");
     const int word = lane < 20 ? __ldg(reinterpret_cast<const int*>(a.plan.joins[list] + it / W) + lane) : 0;
     auto field = [&](int i) { return __shfl_sync(0xFFFFFFFFu, word, i); };
+    const int nrows = field(14);
+    const int r = (int)(it % W) * 8 + (lane & 7), c0 = lane >> 3;
+    if (r - (lane & 7) >= nrows) continue;  // the whole warp, and with SPLIT the whole CTA
     const Parts4 own = {field(0), field(1), field(2), field(3)};
     const Parts4 pa = {field(4), field(5), field(6), field(7)}, pb = {field(8), field(9), field(10), field(11)};
-    const int tok0 = field(12), row0 = field(13), nrows = field(14), head = field(15);
+    const int tok0 = field(12), row0 = field(13), head = field(15);
     const int plist = field(16), pofs = field(17), psplit = field(18);
-    for (int r = (int)(it % W); r < nrows; r += W) {
-      const bool second = r >= psplit;
-      const Parts4 pp = second ? pb : pa;
-      const int prow = second ? r - psplit : r + pofs, n = own.count + (plist >= 0 ? pp.count : 0);
-      float m = -INFINITY, l = 0;
-      float4 o = make_float4(0, 0, 0, 0);
-      for (int k0 = 0; k0 < n; k0 += 32) {
-        const int k = k0 + lane, kp = k - own.count;
-        const bool mine = kp < 0;
-        const int from = mine ? list : plist;
-        int64_t at = 0;
-        if (mine) at = (k ? own.second + (int64_t)(k - 1) * own.stride : own.first) + r;
-        else if (k < n) at = (kp ? pp.second + (int64_t)(kp - 1) * pp.stride : pp.first) + prow;
-        float2 ml = make_float2(-INFINITY, 0);
-        if (k < n) ml = from ? a.plan.part_ml[1][at] : a.plan.part_ml[0][at];
-        const uint64_t src = reinterpret_cast<uint64_t>((k < n && from ? a.plan.part_o[1] : a.plan.part_o[0]) + at * dim);
-        float top = ml.x;
+    const bool in = r < nrows;
+    float m = -INFINITY, l = 0;
+    float4 o[NW];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
-        const float f0 = ex2(m - ref), f = ex2(ml.x - ref);
-        float sum = ml.y * f;
+    for (int i = 0; i < NW; ++i) o[i] = make_float4(0, 0, 0, 0);
+    auto take = [&](float mx, float lx, const float4 (&v)[NW]) {
+      const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.0f : mn;
+      const float f0 = ex2(m - ref), f1 = ex2(mx - ref);
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-        l = l * f0 + sum;
-        m = mn;
-        o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
-        const int count = min(32, n - k0);
-        for (int i0 = 0; i0 < count; i0 += 4) {
-          float4 x[4];
-          float w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4* q = reinterpret_cast<const float4*>(__shfl_sync(0xFFFFFFFFu, src, i0 + i)) + lane;
-            w[i] = __shfl_sync(0xFFFFFFFFu, f, i0 + i);
-            x[i] = on && i0 + i < count ? __ldcg(q) : make_float4(0, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (i0 + i >= count) break;
-            o.x += x[i].x * w[i]; o.y += x[i].y * w[i]; o.z += x[i].z * w[i]; o.w += x[i].w * w[i];
-          }
-        }
+      for (int i = 0; i < NW; ++i) {
+        o[i].x = o[i].x * f0 + v[i].x * f1;
+        o[i].y = o[i].y * f0 + v[i].y * f1;
+        o[i].z = o[i].z * f0 + v[i].z * f1;
+        o[i].w = o[i].w * f0 + v[i].w * f1;
       }
-      const int rr = row0 + r;
-      const int64_t tok = tok0 + rr / a.pool.ratio;
-      const int hq = head * a.pool.ratio + rr % a.pool.ratio;
-      const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-      if (on)
-        *reinterpret_cast<uint2*>(a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + lane * 4)) =
-            make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
-      if (a.lse && lane == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
+      l = l * f0 + lx * f1;
+      m = mn;
+    };
+    // the parts sub, sub + SPLIT, ... of the row's own and its prefix's, as one list
+    const bool second = r >= psplit;
+    const Parts4 pp = {second ? pb.first : pa.first, second ? pb.second : pa.second,
+                       plist < 0 ? 0 : (second ? pb.count : pa.count), second ? pb.stride : pa.stride};
+    const int prow = second ? r - psplit : r + pofs, n = in ? own.count + pp.count : 0;
+#pragma unroll 2
+    for (int k = sub; k < n; k += SPLIT) {
+      const bool mine = k < own.count;
+      const int kp = k - own.count;
+      const int64_t at = mine ? (k ? own.second + (int64_t)(k - 1) * own.stride : own.first) + r
+                              : (kp ? pp.second + (int64_t)(kp - 1) * pp.stride : pp.first) + prow;
+      const bool from = mine ? list : plist;
+      const float4* po = from ? a.plan.part_o[1] : a.plan.part_o[0];
+      const float2 x = __ldcg((from ? a.plan.part_ml[1] : a.plan.part_ml[0]) + at);
+      float4 v[NW];
+#pragma unroll
+      for (int i = 0; i < NW; ++i)
+        v[i] = c0 + 4 * i < words ? __ldcg(po + part_word(at, c0 + 4 * i, dim)) : make_float4(0, 0, 0, 0);
+      take(x.x, x.y, v);
     }
+    if (SPLIT > 1) {
+      __syncthreads();
+      if (sub > 0) {
+        sh->ml[sub - 1][lane] = make_float2(m, l);
+#pragma unroll
+        for (int i = 0; i < NW; ++i) sh->o[sub - 1][i][lane] = o[i];
+      }
+      __syncthreads();
+      if (sub > 0) continue;
+      for (int x = 0; x < SPLIT - 1; ++x) {
+        float4 v[NW];
+#pragma unroll
+        for (int i = 0; i < NW; ++i) v[i] = sh->o[x][i][lane];
+        take(sh->ml[x][lane].x, sh->ml[x][lane].y, v);
+      }
+    }
+    if (!in) continue;
+    const int rr = row0 + r;
+    const int64_t tok = tok0 + rr / a.pool.ratio;
+    const int hq = head * a.pool.ratio + rr % a.pool.ratio;
+    const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+    char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+      if (c0 + 4 * i < words)
+        *reinterpret_cast<uint2*>(op + 8 * (c0 + 4 * i)) =
+            make_uint2(Num<T>::pack(o[i].x * inv, o[i].y * inv), Num<T>::pack(o[i].z * inv, o[i].w * inv));
+    if (a.lse && c0 == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
   }
 }
 template <typename T>
-__global__ void __launch_bounds__(128, 8) k_attend_join(AttendArgs a) {
+__global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
+  __shared__ JoinShared sh;
   chain();
   const int4 h = __ldg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries
   if (h.x != PS_OK) return;
-  const int64_t warp = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5, warps = (int64_t)gridDim.x * (blockDim.x >> 5);
-  join_rows<T, 4>(a, 0, h.y, warp, warps, threadIdx.x & 31);
-  join_rows<T, 128>(a, 1, h.z, warp, warps, threadIdx.x & 31);
+  const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+  if ((int64_t)h.y * (tile_rows(0) / 8) + (int64_t)h.z * (tile_rows(1) / 8) <= 2 * (int64_t)gridDim.x) {
+    join_rows<T, tile_rows(0), 4>(a, &sh, 0, h.y, blockIdx.x, gridDim.x, sub, lane);
+    join_rows<T, tile_rows(1), 4>(a, &sh, 1, h.z, blockIdx.x, gridDim.x, sub, lane);
+  } else {
+    const int64_t warp = (int64_t)blockIdx.x * 4 + sub, warps = (int64_t)gridDim.x * 4;
+    join_rows<T, tile_rows(0), 1>(a, &sh, 0, h.y, warp, warps, 0, lane);
+    join_rows<T, tile_rows(1), 1>(a, &sh, 1, h.z, warp, warps, 0, lane);
+  }
 }
 
 template <typename T, int DP>
@@ -498,8 +507,8 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   cudaError_t e = wide ? launch_wide(a, maps, st) : cudaSuccess;
   if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
   if (e != cudaSuccess) return status_of(e);
-  // warps for every narrow tile's rows at once, up to one full wave
-  const int64_t want = (int64_t)b.num_tokens * p.kv_heads, most = (int64_t)plan.max_ctas[1] * 16;
+  // a CTA for every eight rows of narrow tiles, up to one full wave
+  const int64_t want = (int64_t)b.num_tokens * p.kv_heads * 2, most = (int64_t)plan.max_ctas[1] * 4;
   const dim3 grid((unsigned)(want < most ? want : most));
   e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 128, 0, st, a)
                             : launch(k_attend_join<__half>, grid, 128, 0, st, a);

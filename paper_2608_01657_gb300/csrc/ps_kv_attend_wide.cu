@@ -50,7 +50,7 @@ struct Shape {
 };
 
 struct Shared {
-  uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full, q_empty, ml_full, ml_free, turn[2];
+  uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full[2], q_empty[2], ml_full, ml_free, turn[2];
   uint32_t tmem;
   float2 ml[128];  // split mode: group 1's (maximum, sum)
 };
@@ -67,6 +67,15 @@ __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+      : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Whether it has, without waiting (try_wait may suspend the thread for thousands
+// of cycles before it answers no).
+__device__ __forceinline__ bool bar_peek(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
       : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return ok != 0;
 }
@@ -170,39 +179,19 @@ __device__ __forceinline__ uint32_t instr_desc(int n, bool b_rows_contract) {
   return 1u << 4 | type << 7 | type << 10 | (b_rows_contract ? 1u << 16 : 0) | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
 }
 
-// The CTA's part of the list, one (tile, head) at a time; every role runs its own.
-struct Parts {
-  const Tile* tiles;
-  const int64_t* ucum;
-  int heads, left, tile, head, unit, nunits, count;
-  Tile t;
-  __device__ __forceinline__ void start(const AttendArgs& a, int64_t u0, int n, int first_tile) {
-    tiles = a.plan.tiles[1];
-    ucum = a.plan.ucum[1];
-    heads = a.pool.kv_heads;
-    left = n;
-    tile = first_tile;
-    t = tiles[tile];
-    const int64_t b = ucum[tile];
-    nunits = (int)((ucum[tile + 1] - b) / heads);
-    head = (int)((u0 - b) / nunits);
-    unit = (int)((u0 - b) % nunits);
-    count = min(left, nunits - unit);
+// Two row blocks?
+__device__ __forceinline__ bool is_pair(const Tile& t) { return t.nrows > 128; }
+
+// The two blocks of queries: both are a pair's, one is a single row block's, the
+// other one next time, so that a tile's queries arrive while the last one's are
+// in use.  'fills' bit b: parity of block b's fills so far.
+struct QueryBlocks {
+  uint32_t fills = 0, turn = 0;
+  __device__ __forceinline__ uint32_t first(bool pair) const { return pair ? 0 : turn; }
+  __device__ __forceinline__ void next(bool pair) {
+    fills ^= pair ? 3u : 1u << turn;
+    if (!pair) turn ^= 1;
   }
-  __device__ __forceinline__ bool next() {
-    left -= count;
-    if (left <= 0) return false;
-    unit = 0;
-    if (++head == heads) {
-      head = 0;
-      ++tile;
-      t = tiles[tile];
-      nunits = (int)((ucum[tile + 1] - ucum[tile]) / heads);
-    }
-    count = min(left, nunits);
-    return true;
-  }
-  __device__ __forceinline__ bool pair() const { return t.nrows > 128; }
 };
 
 // ---- loader warps ------------------------------------------------------------------
@@ -259,7 +248,7 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, const char* base, int64_
 }
 
 template <int DP>
-__device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& maps, Shared* sh, uint32_t qs, uint32_t ring, Parts ps) {
+__device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& maps, Shared* sh, uint32_t qs, uint32_t ring, Parts<1> ps) {
   using S = Shape<DP>;
   static_assert(kSoftmaxWarps % 4 == 0, "copy_rows takes the warp's place in its group");
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kSoftmaxWarps;
@@ -269,18 +258,19 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
   const bool issues = tma && lane < boxes * S::kHalves;
   const uint32_t box_at = myhalf * (128 * 128) + (warp * 32 + mybox * maps.box) * 128;
   Place<S::kBuffers> at;       // the next block
-  uint64_t* copied = nullptr;  // a block whose copies are under way
-  auto told = [&]() {          // wait for them and say so
-    if (!copied) return;
+  uint64_t* copied[2] = {nullptr, nullptr};  // blocks whose copies are under way
+  auto told = [&]() {                        // wait for them and say so
+    if (!copied[0]) return;
     cp_wait<0>();
     to_async_proxy();
     __syncwarp();
-    if (lane == 0) bar_arrive(copied);
-    copied = nullptr;
+    if (lane == 0) bar_arrive(copied[0]);
+    if (lane == 0 && copied[1]) bar_arrive(copied[1]);
+    copied[0] = copied[1] = nullptr;
   };
-  uint32_t seg = 0;
+  QueryBlocks qb;
   bool more = true;
-  for (; more; ++seg, more = ps.next()) {
+  for (; more; more = ps.next()) {
     const Tile t = ps.t;
     const int32_t* row = a.tables + t.req * a.table_stride;
     // ids are looked up one unit ahead
@@ -298,15 +288,16 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
       const int id = page;
       page = id_of(u + 1);
       const int key = base + warp * 32 + (whole ? mybox * maps.box : lane), token = key & (a.pool.page_size - 1);
-      // keys, values; with a tile's first unit under way its queries, once the last
-      // tile's are read (one loop, so that the copies' code is there once)
-      const int jobs = u > 0 ? 2 : (ps.pair() ? 4 : 3);
+      // keys, values; with a tile's first unit under way its queries (one loop, so
+      // that the copies' code is there once)
+      const int jobs = u > 0 ? 2 : (is_pair(ps.t) ? 4 : 3);
 #pragma unroll 1
       for (int job = 0; job < jobs; ++job) {
-        uint64_t* bar = job < 2 ? &sh->full[at.slot] : &sh->q_full;
-        uint64_t* free = job < 2 ? &sh->empty[at.slot] : &sh->q_empty;
-        const uint32_t parity = job < 2 ? at.par ^ 1 : (seg & 1) ^ 1;
-        if (job < 3 && !__all_sync(0xFFFFFFFFu, bar_test(free, parity))) {
+        const uint32_t qblk = qb.first(is_pair(ps.t)) ^ (job & 1);  // of jobs 2 and 3
+        uint64_t* bar = job < 2 ? &sh->full[at.slot] : &sh->q_full[qblk];
+        uint64_t* free = job < 2 ? &sh->empty[at.slot] : &sh->q_empty[qblk];
+        const uint32_t parity = (job < 2 ? at.par : qb.fills >> qblk & 1) ^ 1;
+        if (!__all_sync(0xFFFFFFFFu, bar_peek(free, parity))) {
           told();  // what was copied is not held back by the wait
           if (!warp_wait(free, parity)) return false;
         }
@@ -326,16 +317,16 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
           if (id < 0) off = -1;
         } else {
           const int r = (job - 2) * 128 + warp * 32 + lane, rr = t.row0 + r;
-          dst = qs + (job - 2) * S::kBlock;
+          dst = qs + qblk * S::kBlock;
           off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
                 (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
           if (r >= t.nrows) off = -1;
         }
         if (job != 3) told();
         copy_rows<DP>(dst, src, off, a.pool.head_dim);
-        copied = bar;
+        copied[copied[0] ? 1 : 0] = bar;
       }
-      if (u == 0) told();
+      if (u == 0) qb.next(is_pair(ps.t));
     }
   }
   told();
@@ -348,7 +339,7 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
 // take turns: left to themselves they fell into step, both waiting for weights
 // or both for products (4500 cycles for a unit's 2048 of products).
 template <typename T, int DP>
-__device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t, uint32_t tmem, uint32_t qs, uint32_t ring, Parts ps) {
+__device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t, uint32_t tmem, uint32_t qs, uint32_t ring, Parts<1> ps) {
   using S = Shape<DP>;
   // scores are negated where the scale is negative
   const uint32_t id_qk = instr_desc<T>(UNIT, false) | (a.scale2 < 0 ? 1u << 13 : 0), id_pv = instr_desc<T>(DP, true);
@@ -358,14 +349,21 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
   const uint32_t s_at = tmem + col_s(t), o_at = tmem + col_o(t);
   uint32_t p_phase = 0, turn = t ^ 1;  // group 0 has the first turn
   Place<S::kBuffers> at;  // the key block of the tile's unit in turn; its value block is the next
-  uint32_t seg = 0;
+  QueryBlocks qb;
   bool more = true;
-  for (; more; ++seg, more = ps.next()) {
-    const bool pair = ps.pair();
+  for (; more; more = ps.next()) {
+    const bool pair = is_pair(ps.t);
     const int n = ps.count;
-    if (!warp_wait(&sh->q_full, seg & 1)) return false;
-    const uint64_t q = q_desc + (pair ? t : 0) * kBlk;
-    // a block's two arrivals: one of each group, or both of the one that uses it
+    const uint32_t qblk = pair ? t : qb.first(false);
+    if (!warp_wait(&sh->q_full[qblk], qb.fills >> qblk & 1)) return false;
+    qb.next(pair);
+    const uint64_t q = q_desc + qblk * kBlk;
+    // a block's two arrivals: both of the one group of a pair, one of each otherwise
+    auto release_q = [&]() {
+      tc_commit(&sh->q_empty[qblk]);
+      if (pair) tc_commit(&sh->q_empty[qblk]);
+    };
+    // and of a key or value block: one of each group of a pair, both of the one that uses it otherwise
     auto release = [&](const Place<S::kBuffers>& b) {
       tc_commit(&sh->empty[b.slot]);
       if (!pair) tc_commit(&sh->empty[b.slot]);
@@ -413,11 +411,11 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
         bar_arrive(&sh->turn[t ^ 1]);
         if (product) release(vb);
         if (more_keys) release(kb);
-        if (more_keys && u + 2 * step >= n) tc_commit(&sh->q_empty);  // the last scores are on their way
+        if (more_keys && u + 2 * step >= n) release_q();  // the last scores are on their way
       }
       __syncwarp();
     }
-    if (first >= n && elect()) tc_commit(&sh->q_empty);  // no scores at all
+    if (first >= n && elect()) release_q();  // no scores at all
     __syncwarp();
     at = at.skip(2 * n);
   }
@@ -426,7 +424,7 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
 
 // ---- softmax warps ------------------------------------------------------------------
 template <typename T, int DP>
-__device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, uint32_t tmem, Parts ps, int c, int C) {
+__device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, uint32_t tmem, Parts<1> ps, int c, int C) {
   const int warp = threadIdx.x >> 5, t = warp >> 2, lane = threadIdx.x & 31;
   const int row = (warp & 3) * 32 + lane;  // of the row block, and the tensor memory lane
   const uint32_t at = tmem + ((uint32_t)(warp & 3) << 21);
@@ -446,7 +444,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
   bool more = true;
   for (; more; more = ps.next()) {
     const Tile tl = ps.t;
-    const bool pair = ps.pair();
+    const bool pair = is_pair(ps.t);
     const int n = ps.count;
     const int mine = pair ? n : (t == 0 ? (n + 1) / 2 : n / 2);
     const int trow = pair ? t * 128 + row : row;  // row of the tile
@@ -551,38 +549,58 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
     const int64_t tok = tl.tok0 + rr / a.pool.ratio;
     const int hq = ps.head * a.pool.ratio + rr % a.pool.ratio;
     const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-    char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
+    const int64_t out_at = in ? tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1] : -1;
     const int64_t prow = part_row<H>(tl.sidx, tl.nrows, ps.head, c, ps.unit > 0, C) + trow;
-    float* po = a.plan.part_o[1] + prow * a.pool.head_dim;
+    // where this lane writes: four lanes exchange words so that each has the
+    // same 16 bytes of four rows, and they write 64 bytes of a row together
+    int64_t rows_at[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) rows_at[x] = __shfl_sync(0xFFFFFFFFu, out_at, (lane & ~3) + x);
 #pragma unroll 1
-    for (int j = 0; j < DP; j += 16) {
-      uint32_t o[16];
-      tm_load16(o, o_at + j);
+    for (int j = 0; j < DP; j += 32) {
+      uint32_t o[32];
+      tm_load32(o, o_at + j);
       tm_wait_ld();
       float* x = reinterpret_cast<float*>(o);
       if (!pair) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] *= f[0];
+        for (int e = 0; e < 32; ++e) x[e] *= f[0];
         if (both) {
-          uint32_t o1[16];
-          tm_load16(o1, at + col_o(1) + j);
+          uint32_t o1[32];
+          tm_load32(o1, at + col_o(1) + j);
           tm_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] += __uint_as_float(o1[e]) * f[1];
+          for (int e = 0; e < 32; ++e) x[e] += __uint_as_float(o1[e]) * f[1];
         }
       }
-      if (!in) continue;
+      if (direct) {
+        uint32_t w[4][4];
 #pragma unroll
-      for (int e = 0; e < 16; e += 8) {
-        if (j + e >= a.pool.head_dim) continue;
-        if (direct) {
-          *reinterpret_cast<uint4*>(op + 2 * (j + e)) =
-              make_uint4(Num<T>::pack(x[e] * inv, x[e + 1] * inv), Num<T>::pack(x[e + 2] * inv, x[e + 3] * inv),
-                         Num<T>::pack(x[e + 4] * inv, x[e + 5] * inv), Num<T>::pack(x[e + 6] * inv, x[e + 7] * inv));
-        } else {
-          *reinterpret_cast<float4*>(po + j + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-          *reinterpret_cast<float4*>(po + j + e + 4) = make_float4(x[e + 4], x[e + 5], x[e + 6], x[e + 7]);
+        for (int e = 0; e < 32; e += 2) w[e >> 3][(e >> 1) & 3] = Num<T>::pack(x[e] * inv, x[e + 1] * inv);
+#pragma unroll
+        for (int b = 1; b <= 2; b <<= 1) {
+          const bool up = lane & b;
+#pragma unroll
+          for (int c4 = 0; c4 < 4; ++c4) {
+            if (c4 & b) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, up ? w[c4][e] : w[c4 | b][e], b);
+              if (up) w[c4][e] = got;
+              else w[c4 | b][e] = got;
+            }
+          }
         }
+        const int col = j + (lane & 3) * 8;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (rows_at[y] >= 0 && col < a.pool.head_dim)
+            *reinterpret_cast<uint4*>(a.out + 2 * (rows_at[y] + col)) = make_uint4(w[y][0], w[y][1], w[y][2], w[y][3]);
+      } else if (in) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          if (j + e < a.pool.head_dim)
+            a.plan.part_o[1][part_word(prow, (j + e) >> 2, a.pool.head_dim)] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
       }
     }
     if (in) {
@@ -608,8 +626,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   const PlanHdr* hdr = a.plan.hdr;
   const int C = hdr->ctas[1], c = blockIdx.x;
   if (c >= C) return;
-  const int64_t U = hdr->units[1], u0 = U * c / C;
-  const int n = (int)(U * (c + 1) / C - u0);
+  const int64_t U = hdr->cost[1];
+  Parts<1> ps;
+  if (!ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t qs = (smem_addr(dyn) + 1023) & ~1023u, ring = qs + 2 * S::kBlock;
   if (warp == kSoftmaxWarps + kLoaderWarps) {
@@ -626,9 +645,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
       bar_init(&sh.p_full[t], 4);
       bar_init(&sh.o_full[t], 1);
       bar_init(&sh.turn[t], 1);
+      bar_init(&sh.q_full[t], kLoaderWarps);
+      bar_init(&sh.q_empty[t], 2);
     }
-    bar_init(&sh.q_full, kLoaderWarps);
-    bar_init(&sh.q_empty, 2);
     bar_init(&sh.ml_full, 4);
     bar_init(&sh.ml_free, 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -637,8 +656,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   __syncthreads();
   tc_after();
   const uint32_t tmem = sh.tmem;
-  Parts ps;
-  ps.start(a, u0, n, a.plan.cta_tile[1][c]);
   bool ok = true;
   if (warp < kSoftmaxWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));

@@ -12,6 +12,11 @@ constexpr int kAnyPages = 0x7FFFFFFF;
 // Shared tokens below which the second part of a row costs more than it saves.
 constexpr int kShareTokens = 128;
 
+// Cycles of one unit, measured: a wide one on its SM (128 keys, with the other
+// SMs at the narrow tiles' memory traffic), a narrow one in its CTA when loads wait on latency alone, and when all CTAs
+// share the HBM bandwidth (64 keys of 128 elements).
+constexpr double kWideCycles = 3600, kNarrowCycles = 1250, kNarrowBandwidth = 3300;
+
 // Pages of a request that every one of its queries sees whole.
 __device__ __forceinline__ int whole_pages(const Pool& p, const Batch& b, int r) {
   const int n = b.q_offsets[r + 1] - b.q_offsets[r], len = b.kv_lens[r];
@@ -165,7 +170,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   // items: the groups' prefixes, then the requests
   const int ngroups = b.group_offsets ? b.num_groups : 0;
   const int nitems = ngroups + b.num_requests;
-  int64_t tiles[kLists] = {}, units[kLists] = {}, shared[kLists] = {};
+  int64_t tiles[kLists] = {}, units[kLists] = {}, shared[kLists] = {};  // units: their cost
   for (int i0 = 0; i0 < nitems; i0 += kPlanThreads) {
     const int i = i0 + tid;
     Item it{};
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
     int64_t nu = 0;
     for (int t = 0; t < nt; ++t) {
       const int last = min(it.rows, (t + 1) * H) - 1;
-      nu += unit_count(tile_end(it, p, last) - it.kv0, unit);
+      nu += unit_count(tile_end(it, p, last) - it.kv0, unit) + tile_cost(it.list);
     }
     int64_t tile_at = 0, unit_at = 0, shared_at = 0;
     for (int l = 0; l < kLists; ++l) {
@@ -224,7 +229,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
       x.sidx = it.shared ? (int)shared_at + t * H * p.kv_heads : -1;
       plan.tiles[it.list][tile_at + t] = x;
       plan.ucum[it.list][tile_at + t] = unit_at;
-      unit_at += (int64_t)unit_count(x.kv1 - x.kv0, unit) * p.kv_heads;
+      unit_at += (int64_t)(unit_count(x.kv1 - x.kv0, unit) + tile_cost(it.list)) * p.kv_heads;
     }
     if (i < ngroups) {
       plan.grp_tile[i] = it.rows > 0 ? (int)tile_at : -1;
@@ -246,9 +251,26 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
       plan.req[r].prow0 = (b.q_offsets[r] - b.q_offsets[b.group_offsets[g]]) * p.ratio;
     }
   }
+  // SMs for the wide tiles, the rest for the narrow ones, so that both lists end
+  // together: thread x weighs x SMs.
+  __shared__ unsigned long long s_best;
+  if (tid == 0) s_best = ~0ull;
+  __syncthreads();
+  const int sms = plan.max_ctas[1], per_sm = plan.max_ctas[0] / sms;
+  if (tid <= sms) {
+    const bool can = (tid > 0 || units[1] == 0) && (tid < sms || units[0] == 0);
+    const double wide = units[1] > 0 && tid > 0 ? (double)units[1] * kWideCycles / tid : 0;
+    const double fast = units[0] > 0 && tid < sms ? (double)units[0] * kNarrowCycles / (per_sm * (sms - tid)) : 0;
+    const double bytes = (double)units[0] * kNarrowBandwidth * p.head_dim / (128 * per_sm * sms);
+    const double t = fmax(wide, fmax(fast, bytes));
+    if (can) atomicMin(&s_best, (unsigned long long)t << 10 | tid);
+  }
+  __syncthreads();
+  const int wide_sms = (int)(s_best & 1023);
+  const int64_t room[kLists] = {(int64_t)per_sm * (sms - wide_sms), wide_sms};
   int ctas[kLists];
   for (int l = 0; l < kLists; ++l) {
-    ctas[l] = (int)(units[l] < plan.max_ctas[l] ? units[l] : plan.max_ctas[l]);
+    ctas[l] = (int)(units[l] < room[l] ? units[l] : room[l]);
     if (tid == 0) plan.ucum[l][tiles[l]] = units[l];
   }
   __syncthreads();
@@ -270,7 +292,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
     for (int l = 0; l < kLists; ++l) {
       h.ntiles[l] = (int)tiles[l];
       h.ctas[l] = ctas[l];
-      h.units[l] = units[l];
+      h.cost[l] = units[l];
     }
     *plan.hdr = h;
   }
@@ -279,10 +301,11 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
 // The partial results of a (tile, head).
 template <int H>
 __device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, const PlanHdr& h, int list, int tile, int head) {
-  const int64_t U = h.units[list], b = plan.ucum[list][tile];
+  const int64_t U = h.cost[list], b = plan.ucum[list][tile];
   const int C = h.ctas[list];
-  const int64_t nu = (plan.ucum[list][tile + 1] - b) / p.kv_heads, ua = b + head * nu;
-  const int ca = cta_of(ua, U, C), cb = cta_of(ua + nu - 1, U, C);
+  const int64_t each = (plan.ucum[list][tile + 1] - b) / p.kv_heads;
+  const int64_t ua = b + head * each + tile_cost(list);  // the place of unit 0
+  const int ca = cta_of(ua, U, C), cb = cta_of(b + (head + 1) * each - 1, U, C);
   const Tile& t = plan.tiles[list][tile];
   Parts4 r;
   r.count = t.sidx < 0 && ca == cb ? 0 : cb - ca + 1;  // a whole one is written where it is computed
