@@ -30,11 +30,11 @@ struct Pool {
 // keys.  The rows of a tile are (token, query head of one kv head) pairs, token
 // major, so a tile is run once for each kv head.  A tile's keys are cut into
 // units.  A (tile, head) costs its units and tile_cost() more, for its beginning
-// and end; of the whole list's cost U (tile major, then kv head) CTA c gets
-// [floor(U c / C), floor(U (c + 1) / C)): every CTA the same, whatever the
-// lengths are.  Within a (tile, head) the beginning's cost comes first, unit u is
-// place tile_cost() + u.  A (tile, head) that several
-// CTAs work on, or whose rows also have a shared prefix, leaves partial results
+// and end; of the whole list's cost U (tile major, then kv head) worker c of C
+// (a CTA of the wide tiles' kernel, a warp of the narrow ones') gets
+// [floor(U c / C), floor(U (c + 1) / C)): each the same, whatever the lengths
+// are.  Within a (tile, head) the beginning's cost comes first, unit u is place
+// tile_cost() + u.  A (tile, head) that several workers share, or whose rows also have a shared prefix, leaves partial results
 // (a running maximum, a sum, an unnormalized output) that k_attend_join puts
 // together in a fixed order.
 struct __align__(32) Tile {
@@ -58,7 +58,7 @@ struct ReqRec {
 
 constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen05)
 __host__ __device__ constexpr int tile_rows(int list) { return list ? 256 : 16; }
-__host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 64; }
+__host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 16; }
 // What a (tile, head) costs beside its units, in units.
 __host__ __device__ constexpr int tile_cost(int list) { return list ? 2 : 1; }
 // The list of an item of so many rows.
@@ -85,7 +85,8 @@ struct __align__(16) PlanHdr {
   int32_t joins[kLists];    // entries of joins[]
   int32_t pad0;
   int32_t ntiles[kLists];
-  int32_t ctas[kLists];     // C, 0 without tiles
+  int32_t workers[kLists];  // C, 0 without tiles
+  int32_t narrow_ctas;      // CTAs that the narrow tiles' workers are spread over
   int64_t cost[kLists];     // U
 };
 
@@ -106,8 +107,8 @@ inline PlanBounds plan_bounds(int list, int64_t R, int64_t rows) {
   return {2 * own, own, 2 * (rows < R * kShareRows ? rows : R * kShareRows)};
 }
 
-// The CTA of place u: the largest c with floor(U c / C) <= u.
-__host__ __device__ __forceinline__ int cta_of(int64_t u, int64_t U, int64_t C) {
+// The worker of place u: the largest c with floor(U c / C) <= u.
+__host__ __device__ __forceinline__ int worker_of(int64_t u, int64_t U, int64_t C) {
   return (int)(((u + 1) * C - 1) / U);
 }
 
@@ -122,15 +123,15 @@ struct Plan {
   int32_t* bad;       // [max_requests]
   Tile* tiles[kLists];
   int64_t* ucum[kLists];      // [tiles + 1] cost before a tile, all heads
-  int32_t* cta_tile[kLists];  // [C] tile of a CTA's first place
+  int32_t* first_tile[kLists];  // [C] tile of a worker's first place
   JoinRec* joins[kLists];     // [tiles of requests x kv heads]
   float4* part_o[kLists];     // unnormalized outputs of the rows, see part_row and part_word
   float2* part_ml[kLists];    // [rows] (maximum, sum), base 2
-  int32_t max_ctas[kLists];
+  int32_t max_workers[kLists];
 };
 
-// The first row of the partial results of a (tile, head)'s part that CTA c
-// computed.  A CTA leaves at most two partial results of (tile, head)s that are
+// The first row of the partial results of a (tile, head)'s part that worker c
+// computed.  A worker leaves at most two partial results of (tile, head)s that are
 // not shared, of the one it continues and of the one it leaves unfinished: two
 // places of H rows each.  Along the list of shared (tile, head)s neither the
 // rows before one nor c ever decreases, and one of them grows by as much as a
@@ -141,7 +142,7 @@ __host__ __device__ __forceinline__ int64_t part_row(int sidx, int nrows, int he
 }
 
 // Tensor maps of the pool's keys and values: (element, head, token, page, layer),
-// a box of 64 elements of min(page_size, 32) tokens.
+// a box of 64 elements of min(page_size, 16) tokens.
 struct PoolMaps {
   CUtensorMap k, v;
   int32_t ok;  // 0: pages of fewer than 8 tokens, or no maps
@@ -156,7 +157,7 @@ __device__ __forceinline__ int64_t part_word(int64_t r, int c, int head_dim) {
   return ((r >> 3) * (head_dim >> 2) + c) * 8 + (r & 7);
 }
 
-// A CTA's part of a list, one (tile, head) at a time.
+// A worker's part of a list, one (tile, head) at a time.
 template <int LIST>
 struct Parts {
   static constexpr int K = tile_cost(LIST);
@@ -169,7 +170,7 @@ struct Parts {
     tiles = plan.tiles[LIST];
     ucum = plan.ucum[LIST];
     heads = kv_heads;
-    tile = plan.cta_tile[LIST][c];
+    tile = plan.first_tile[LIST][c];
     t = tiles[tile];
     const int64_t b = ucum[tile];
     const int each = (int)((ucum[tile + 1] - b) / heads);
@@ -301,8 +302,9 @@ int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_k
 int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, int32_t row_pages,
                        const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                        int32_t* status, int nsm, cudaStream_t st);
-// Kernel attributes (shared-memory opt-ins) and the CTAs of each attention list
+// Kernel attributes (shared-memory opt-ins) and the workers of each attention list
 // that the current device holds at once.
-int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]);
+constexpr int kNarrowWarps = 4;  // of a CTA
+int32_t configure_attention(const Pool& p, int nsm, int32_t workers[kLists]);
 
 }  // namespace pskv

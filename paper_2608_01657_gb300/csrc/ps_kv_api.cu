@@ -71,7 +71,7 @@ struct Carver {
 
 // The workspace: sizes with base == nullptr, pointers otherwise.  Every region
 // starts on a 256-byte boundary.  The page header comes first (cleared once).
-size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Plan* plan, PageScratch* pages) {
+size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base, Plan* plan, PageScratch* pages) {
   Carver cv{base};
   const int64_t R = c.max_requests, T = c.max_tokens, ratio = c.num_q_heads / c.num_kv_heads;
   PageScratch w{};
@@ -104,11 +104,11 @@ size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Pl
   for (int l = 0; l < kLists; ++l) {
     const PlanBounds b = plan_bounds(l, R, T * ratio);
     const int64_t shared = b.shared * c.num_kv_heads;
-    p.max_ctas[l] = ctas[l];
-    const size_t part_rows = (size_t)(3 * (int64_t)ctas[l] * tile_rows(l) + shared);
+    p.max_workers[l] = workers[l];
+    const size_t part_rows = (size_t)(3 * (int64_t)workers[l] * tile_rows(l) + shared);
     p.tiles[l] = cv.take<Tile>((size_t)b.tiles);
     p.ucum[l] = cv.take<int64_t>((size_t)b.tiles + 1);
-    p.cta_tile[l] = cv.take<int32_t>((size_t)ctas[l]);
+    p.first_tile[l] = cv.take<int32_t>((size_t)workers[l]);
     p.joins[l] = cv.take<JoinRec>((size_t)b.own_tiles * c.num_kv_heads);
     p.part_o[l] = cv.take<float4>((part_rows + 7) / 8 * 8 * (c.head_dim / 4));
     p.part_ml[l] = cv.take<float2>(part_rows);
@@ -118,9 +118,9 @@ size_t carve(const ps_kv_config_t& c, const int32_t ctas[kLists], char* base, Pl
   return (cv.off + 255) / 256 * 256;
 }
 
-// The workspace has the same size wherever it is asked for: the CTA counts are
+// The workspace has the same size wherever it is asked for: the worker counts are
 // bounded by the device's at ps_kv_create().
-constexpr int32_t kSizedCtas[kLists] = {kMaxSms * 4, kMaxSms};
+constexpr int32_t kSizedWorkers[kLists] = {kMaxSms * 4 * kNarrowWarps, kMaxSms};
 
 bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
   return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
@@ -134,13 +134,13 @@ int32_t row_pages(const ps_kv* kv, int64_t stride) {
 extern "C" {
 
 size_t ps_kv_workspace_bytes(const ps_kv_config_t* cfg) {
-  return check_config(cfg) ? carve(*cfg, kSizedCtas, nullptr, nullptr, nullptr) : 0;
+  return check_config(cfg) ? carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr) : 0;
 }
 
 int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace, size_t workspace_bytes,
                      void* stream) {
   if (!out || !check_config(cfg) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0 ||
-      workspace_bytes < carve(*cfg, kSizedCtas, nullptr, nullptr, nullptr))
+      workspace_bytes < carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr))
     return PS_ERR_INVALID_ARG;
   int dev = 0, nsm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
@@ -154,13 +154,13 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   kv->max_requests = cfg->max_requests;
   kv->max_tokens = cfg->max_tokens;
   kv->max_row_pages = cfg->max_row_pages;
-  int32_t ctas[kLists];
-  int32_t rc = configure_attention(kv->pool, kv->nsm, ctas);
+  int32_t workers[kLists];
+  int32_t rc = configure_attention(kv->pool, kv->nsm, workers);
   for (int l = 0; l < kLists; ++l)
-    if (ctas[l] > kSizedCtas[l]) ctas[l] = kSizedCtas[l];
+    if (workers[l] > kSizedWorkers[l]) workers[l] = kSizedWorkers[l];
   if (rc == PS_OK) {
-    carve(*cfg, kSizedCtas, static_cast<char*>(d_workspace), &kv->plan, &kv->pages);
-    for (int l = 0; l < kLists; ++l) kv->plan.max_ctas[l] = ctas[l];
+    carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages);
+    for (int l = 0; l < kLists; ++l) kv->plan.max_workers[l] = workers[l];
     if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess) rc = PS_ERR_CUDA;
   }
   if (rc != PS_OK) {

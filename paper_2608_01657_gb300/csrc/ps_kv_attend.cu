@@ -15,18 +15,8 @@ namespace pskv {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kWarps = 4;
+constexpr int kWarps = kNarrowWarps;
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes into shared memory, or zeros where !ok (src is not read then).
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -52,32 +42,39 @@ __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4
 
 __device__ __forceinline__ void after_wide() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Shared memory of a warp: STAGES x (16 keys, 16 values) of ROW bytes each, a
-// 16-byte word c of row r at word c ^ (r & 7), so that the eight rows of an
-// ldmatrix lie in eight different banks groups.
+// Shared memory of a warp: STAGES x (16 keys, 16 values), each as halves of 64
+// elements, 16 rows of 128 bytes in which a 16-byte word c of row r lies at word
+// c ^ (r & 7) (the copies' 128-byte swizzle), so that the eight rows of an
+// ldmatrix lie in eight different bank groups.
 template <int DP>
 struct Shape {
-  static constexpr int kRow = DP <= 64 ? 128 : 256;  // bytes
+  static constexpr int kHalves = DP > 64 ? 2 : 1;
+  static constexpr int kBlock = kHalves * 16 * 128;  // bytes of 16 keys, or values
   static constexpr int kStages = DP <= 64 ? 6 : 3;
-  static constexpr int kStage = 2 * 16 * kRow;
-  static constexpr int kWarpBytes = kStages * kStage;
-  static constexpr int kMergeRow = DP + 2;  // floats: padded against bank conflicts
-  static constexpr int kMergeBytes = 2 * 16 * (kMergeRow + 2) * 4;
-  static constexpr int kSmem = kWarps * kWarpBytes + kMergeBytes;
+  static constexpr int kWarpBytes = kStages * 2 * kBlock;
+  // two CTAs an SM: 113 KB each at most
+  static constexpr int kSmem = kWarps * kWarpBytes + kWarps * kStages * 8;
+  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
 };
+// Place of word c of row r in a block.
+__device__ __forceinline__ uint32_t word_at(int r, int c) { return (c >> 3) * (16 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 
-// Narrow tiles: decode.  Bound by HBM (a key is used by at most 16 rows).  A
-// unit is 64 keys, 16 for each warp; a warp streams its own keys and values
-// through its own ring of stages with no barrier, runs its own (m, l, sum) over
-// them, and the four are joined where a (tile, head) ends.  The stream of units
-// runs on across tiles, so that short requests do not drain it.
+// Narrow tiles: decode.  Bound by HBM (a key is used by at most 16 rows).  Every
+// warp is a worker of its own: it streams its keys and values, 16 at a time,
+// through its own ring of stages, with no barrier (four warps to a (tile, head),
+// joined where it ends, waited 3400 to 5600 cycles for one another there, two
+// units' time).  The stream runs on across tiles, so that short requests do not
+// drain it.  Keys and values come by TMA, four boxes for 16 keys; pages of 2 or 4
+// tokens, whose boxes would not fill the 1024 bytes after which the swizzle
+// repeats, by 16-byte copies.
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_constant__ AttendArgs a,
+                                                               const __grid_constant__ PoolMaps maps) {
   using S = Shape<DP>;
   constexpr int CH = DP / 8;   // 16-byte words of a row
   constexpr int KS = DP / 16;  // k steps of q k^T
   constexpr int H = tile_rows(0), UNIT = unit_keys(0);
-  extern __shared__ __align__(128) char smem[];
+  extern __shared__ __align__(1024) char smem[];  // the swizzle repeats after 1024 bytes
   // If the wide tiles' kernel goes before this one, it is independent of it, so
   // this one's CTAs run as soon as there is room: every CTA of that kernel has
   // waited for the work before both by then.  Its end is waited for at this
@@ -85,19 +82,23 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
   if (!a.after_wide) chain();
   else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PlanHdr* hdr = a.plan.hdr;
-  const int C = hdr->ctas[0], c = blockIdx.x;
-  if (c >= C) {
-    after_wide();
-    return;
-  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // the first workers of all CTAs, then the second ones: few are spread over many SMs
+  const int C = hdr->workers[0], c = (int)blockIdx.x < hdr->narrow_ctas ? (int)blockIdx.x + warp * hdr->narrow_ctas : C;
   const int64_t U = hdr->cost[0];
   Parts<0> ps;
-  if (!ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) {
+  if (c >= C || !ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) {
     after_wide();
     return;
   }
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t ring = smem_addr(smem) + warp * S::kWarpBytes;
+  uint64_t* landed = reinterpret_cast<uint64_t*>(smem + kWarps * S::kWarpBytes) + warp * S::kStages;
+  const bool tma = maps.ok;
+  if (lane == 0) {
+    for (int i = 0; i < S::kStages; ++i) bar_init(&landed[i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
 
   // ---- the loader: runs STAGES - 1 units ahead ----
   Parts<0> lp = ps;
@@ -105,30 +106,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
   bool lmore = true;
   const char* kbase = a.k;
   const char* vbase = a.v;
+  // by TMA, lane i looks up box i's page; otherwise lane i key i's
+  const int boxes = 16 / maps.box;
+  const int mykey = tma ? (lane < boxes ? lane * maps.box : 0) : lane & 15;  // within a unit
   // page id of this lane's key in the loader's unit, -1 past the end
   auto key_page = [&]() -> int {
-    const int t = lp.t.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
+    const int t = lp.t.kv0 + lunit * UNIT + mykey;
     return t < lp.t.kv1 ? __ldg(a.tables + lp.t.req * a.table_stride + (t >> a.pool.page_log2)) : -1;
   };
   int page = key_page();
   int lstage = 0;
   auto load_unit = [&]() {
     if (lmore) {
-      const int t = lp.t.kv0 + lunit * UNIT + warp * 16 + (lane & 15);
-      int64_t off = -1;
-      if (page >= 0)
-        off = page * a.pool.page_stride + (int64_t)(t & (a.pool.page_size - 1)) * a.pool.token_stride +
-              lp.head * a.pool.head_stride;
-      const uint32_t dst = ring + lstage * S::kStage;
+      const int token = (lp.t.kv0 + lunit * UNIT + mykey) & (a.pool.page_size - 1);
+      const uint32_t dst = ring + lstage * 2 * S::kBlock;
+      if (tma) {
+        // boxes with a key in them: none of a tile without keys
+        const int there = min(boxes, (lp.t.kv1 - lp.t.kv0 - lunit * UNIT + maps.box - 1) / maps.box);
+#pragma unroll 1
+        for (int box = 0; box < there; ++box) {
+          const int id = __shfl_sync(0xFFFFFFFFu, page, box), tok = __shfl_sync(0xFFFFFFFFu, token, box);
+          if (elect()) {
+            uint64_t* bar = &landed[lstage];
+            if (box == 0) bar_expect(bar, there * 2 * S::kHalves * maps.box * 128);
+            const uint32_t d = dst + box * maps.box * 128;
 #pragma unroll
-      for (int j = 0; j < 16 * CH / 32; ++j) {
-        const int idx = j * 32 + lane, row = idx / CH, w = idx % CH;
-        const int64_t o = __shfl_sync(0xFFFFFFFFu, off, row);
-        const bool ok = o >= 0 && w * 8 < a.pool.head_dim;
-        const int64_t at = ok ? 2 * o + w * 16 : 0;
-        const uint32_t d = dst + row * S::kRow + ((w ^ (row & 7)) << 4);
-        cp16(d, kbase + at, ok);
-        cp16(d + 16 * S::kRow, vbase + at, ok);
+            for (int half = 0; half < S::kHalves; ++half) {
+              tma_load(d + half * (16 * 128), &maps.k, bar, half * 64, lp.head, tok, id, a.layer);
+              tma_load(d + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, tok, id, a.layer);
+            }
+          }
+          __syncwarp();
+        }
+      } else {
+        int64_t off = -1;
+        if (page >= 0)
+          off = page * a.pool.page_stride + (int64_t)token * a.pool.token_stride + lp.head * a.pool.head_stride;
+#pragma unroll
+        for (int j = 0; j < 16 * CH / 32; ++j) {
+          const int idx = j * 32 + lane, row = idx / CH, w = idx % CH;
+          const int64_t o = __shfl_sync(0xFFFFFFFFu, off, row);
+          const bool ok = o >= 0 && w * 8 < a.pool.head_dim;
+          const int64_t at = ok ? 2 * o + w * 16 : 0;
+          const uint32_t d = dst + word_at(row, w);
+          cp16(d, kbase + at, ok);
+          cp16(d + S::kBlock, vbase + at, ok);
+        }
       }
       if (++lunit == lend) {
         lmore = lp.next();
@@ -145,6 +168,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
 
   // ---- the consumer ----
   int stage = 0;
+  uint32_t phases = 0;  // bit i: parity of stage i's next landing
+  bool ok = true;
   const int g = lane >> 2, q4 = lane & 3;
   for (bool more = true; more; more = ps.next()) {
     const Tile t = ps.t;
@@ -178,21 +203,38 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
 
     const int first = ps.unit, count = ps.count;
     for (int it = 0; it < count; ++it) {
-      cp_wait<S::kStages - 2>();
+      const int base = t.kv0 + (first + it) * UNIT;
+      const int keys = t.kv1 - base;
+      if (!tma) {
+        cp_wait<S::kStages - 2>();
+      } else if (keys > 0) {
+        ok = ok && bar_wait(&landed[stage], phases >> stage & 1);
+        phases ^= 1u << stage;
+      }
       __syncwarp();  // the unit has landed, and the stage of the one before it is read
       load_unit();
-      const int base = t.kv0 + (first + it) * UNIT + warp * 16;
-      if (base < t.kv1) {
-        const uint32_t ks_at = ring + stage * S::kStage, vs_at = ks_at + 16 * S::kRow;
-        float s[2][4] = {};
+      if (keys > 0) {
+        const uint32_t ks_at = ring + stage * 2 * S::kBlock, vs_at = ks_at + S::kBlock;
+        if (tma && keys < 16) {  // what lies past the end must weigh nothing: zeros for the values
+          for (int i = lane; i < (16 - keys) * CH; i += 32)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vs_at + word_at(keys + i / CH, i % CH)), "r"(0) : "memory");
+          to_async_proxy();
+          __syncwarp();
+        }
+        // two sums a score, of even and odd steps: half the products' latency
+        float s[2][4] = {}, s1[2][4] = {};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           uint32_t b[4];
           const int row = (lane & 7) + ((lane >> 4) << 3), w = 2 * ks + ((lane >> 3) & 1);
-          ldsm4(b, ks_at + row * S::kRow + ((w ^ (row & 7)) << 4));
-          mma<T>(s[0], qf[ks], b[0], b[1]);
-          mma<T>(s[1], qf[ks], b[2], b[3]);
+          ldsm4(b, ks_at + word_at(row, w));
+          mma<T>(ks & 1 ? s1[0] : s[0], qf[ks], b[0], b[1]);
+          mma<T>(ks & 1 ? s1[1] : s[1], qf[ks], b[2], b[3]);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] += s1[i][j];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -241,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
         for (int np = 0; np < DP / 16; ++np) {
           uint32_t b[4];
           const int row = (lane & 7) + (((lane >> 3) & 1) << 3), w = 2 * np + (lane >> 4);
-          ldsm4t(b, vs_at + row * S::kRow + ((w ^ (row & 7)) << 4));
+          ldsm4t(b, vs_at + word_at(row, w));
           mma<T>(o[2 * np], pf, b[0], b[1]);
           mma<T>(o[2 * np + 1], pf, b[2], b[3]);
         }
@@ -249,50 +291,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
       stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
 
-    // ---- join the four warps' results: 2 into 0, 3 into 1, then 1 into 0 ----
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       l[hf] += __shfl_xor_sync(0xFFFFFFFFu, l[hf], 1);
       l[hf] += __shfl_xor_sync(0xFFFFFFFFu, l[hf], 2);
     }
-    float* mbuf = reinterpret_cast<float*>(smem + kWarps * S::kWarpBytes);
-    constexpr int BUF = 16 * (S::kMergeRow + 2);
-#pragma unroll
-    for (int round = 0; round < 2; ++round) {
-      const int from = round == 0 ? 2 : 1;  // warps [from, 2 from) give to [0, from)
-      __syncthreads();
-      if (warp >= from && warp < 2 * from) {
-        float* b = mbuf + (warp - from) * BUF;
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          float* row = b + (g + 8 * hf) * S::kMergeRow;
-#pragma unroll
-          for (int i = 0; i < DP / 8; ++i)
-            *reinterpret_cast<float2*>(row + i * 8 + q4 * 2) = make_float2(o[i][2 * hf], o[i][2 * hf + 1]);
-          if (q4 == 0) *reinterpret_cast<float2*>(b + 16 * S::kMergeRow + 2 * (g + 8 * hf)) = make_float2(m[hf], l[hf]);
-        }
-      }
-      __syncthreads();
-      if (warp < from) {
-        const float* b = mbuf + warp * BUF;
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const float2 ml = *reinterpret_cast<const float2*>(b + 16 * S::kMergeRow + 2 * (g + 8 * hf));
-          const float mn = fmaxf(m[hf], ml.x), ms = mn == -INFINITY ? 0.0f : mn;
-          const float f0 = ex2(m[hf] - ms), f1 = ex2(ml.x - ms);
-          const float* row = b + (g + 8 * hf) * S::kMergeRow;
-#pragma unroll
-          for (int i = 0; i < DP / 8; ++i) {
-            const float2 x = *reinterpret_cast<const float2*>(row + i * 8 + q4 * 2);
-            o[i][2 * hf] = o[i][2 * hf] * f0 + x.x * f1;
-            o[i][2 * hf + 1] = o[i][2 * hf + 1] * f0 + x.y * f1;
-          }
-          l[hf] = l[hf] * f0 + ml.y * f1;
-          m[hf] = mn;
-        }
-      }
-    }
-    if (warp == 0) {
+    {
       const bool whole = first == 0 && count == ps.nunits;
       if (whole && t.sidx < 0) {
 #pragma unroll
@@ -331,6 +335,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(AttendArgs a) {
     }
   }
   cp_wait<0>();
+  if (!ok && lane == 0) set_error(a.status, PS_ERR_TIMEOUT);
   after_wide();
 }
 
@@ -448,37 +453,37 @@ __global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
 }
 
 template <typename T, int DP>
-cudaError_t narrow(const AttendArgs& a, cudaStream_t st) {
-  return launch(k_attend_narrow<T, DP>, dim3((unsigned)a.plan.max_ctas[0]), kThreads, Shape<DP>::kSmem, st, a);
+cudaError_t narrow(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
+  return launch(k_attend_narrow<T, DP>, dim3((unsigned)(a.plan.max_workers[0] / kWarps)), kThreads, Shape<DP>::kSmem, st, a, m);
 }
 template <typename T>
-cudaError_t narrow_t(const AttendArgs& a, cudaStream_t st) {
+cudaError_t narrow_t(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
   const int d = a.pool.head_dim;
-  return d <= 64 ? narrow<T, 64>(a, st) : d <= 80 ? narrow<T, 80>(a, st) : d <= 96 ? narrow<T, 96>(a, st) : narrow<T, 128>(a, st);
+  return d <= 64 ? narrow<T, 64>(a, m, st) : d <= 80 ? narrow<T, 80>(a, m, st) : d <= 96 ? narrow<T, 96>(a, m, st) : narrow<T, 128>(a, m, st);
 }
 template <typename T, int DP>
-cudaError_t configure_narrow(int nsm, int32_t* ctas) {
+cudaError_t configure_narrow(int nsm, int32_t* workers) {
   cudaError_t e = cudaFuncSetAttribute(k_attend_narrow<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem);
   int occ = 0;
   if (e == cudaSuccess)
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_attend_narrow<T, DP>, kThreads, Shape<DP>::kSmem);
-  *ctas = nsm * (occ > 0 ? occ : 1);
+  *workers = nsm * (occ > 0 ? occ : 1) * kWarps;
   return e;
 }
 template <typename T>
-cudaError_t configure_t(int d, int nsm, int32_t* ctas) {
-  return d <= 64 ? configure_narrow<T, 64>(nsm, ctas) : d <= 80 ? configure_narrow<T, 80>(nsm, ctas)
-       : d <= 96 ? configure_narrow<T, 96>(nsm, ctas) : configure_narrow<T, 128>(nsm, ctas);
+cudaError_t configure_t(int d, int nsm, int32_t* workers) {
+  return d <= 64 ? configure_narrow<T, 64>(nsm, workers) : d <= 80 ? configure_narrow<T, 80>(nsm, workers)
+       : d <= 96 ? configure_narrow<T, 96>(nsm, workers) : configure_narrow<T, 128>(nsm, workers);
 }
 
 }  // namespace
 
-int32_t configure_attention(const Pool& p, int nsm, int32_t ctas[kLists]) {
-  ctas[1] = nsm;
+int32_t configure_attention(const Pool& p, int nsm, int32_t workers[kLists]) {
+  workers[1] = nsm;
   const cudaError_t e = configure_wide(p);
   if (e != cudaSuccess) return status_of(e);
-  return status_of(p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim, nsm, ctas)
-                                         : configure_t<__half>(p.head_dim, nsm, ctas));
+  return status_of(p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim, nsm, workers)
+                                         : configure_t<__half>(p.head_dim, nsm, workers));
 }
 
 int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer,
@@ -505,10 +510,10 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   const bool wide = list_of(b.num_tokens * p.ratio) == 1;
   a.after_wide = wide;
   cudaError_t e = wide ? launch_wide(a, maps, st) : cudaSuccess;
-  if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, st) : narrow_t<__half>(a, st);
+  if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, maps, st) : narrow_t<__half>(a, maps, st);
   if (e != cudaSuccess) return status_of(e);
   // a CTA for every eight rows of narrow tiles, up to one full wave
-  const int64_t want = (int64_t)b.num_tokens * p.kv_heads * 2, most = (int64_t)plan.max_ctas[1] * 4;
+  const int64_t want = (int64_t)b.num_tokens * p.kv_heads * 2, most = (int64_t)plan.max_workers[1] * 4;
   const dim3 grid((unsigned)(want < most ? want : most));
   e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 128, 0, st, a)
                             : launch(k_attend_join<__half>, grid, 128, 0, st, a);

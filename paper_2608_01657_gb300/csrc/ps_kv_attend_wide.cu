@@ -5,7 +5,7 @@
 // its part of the list of units; a unit is 128 keys.  Its warps:
 //   8 softmax warps, two groups t of four, a thread a query row;
 //   4 loader warps, each with a quarter of every unit's keys and values: whole
-//     units by TMA, a box for a page (or half a page of 64) and 64 elements.  A
+//     units by TMA, a box for 16 tokens of a page and 64 elements.  A
 //     request's last unit, whose values past its end must read as zero, queries,
 //     and pages of 2 or 4 tokens, whose boxes would not fill the 1024 bytes after
 //     which the swizzle repeats, go by 16-byte asynchronous copies instead, eight
@@ -35,9 +35,6 @@ constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;  // 2 x 128 x (192 + 64) = 51
 constexpr int UNIT = unit_keys(1), H = tile_rows(1);
 __device__ __forceinline__ constexpr uint32_t col_s(int t) { return 128u * t; }
 __device__ __forceinline__ constexpr uint32_t col_o(int t) { return 256u + 128u * t; }
-// Bound of every wait: far beyond any tile's time, so it only ends a wait that
-// would never end.
-constexpr int kWaitLimit = 1 << 20;
 constexpr float kRescale = 8.0f;
 
 template <int DP>
@@ -56,21 +53,7 @@ struct Shared {
 };
 
 // ---- barriers, tensor memory ---------------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void bar_init(uint64_t* b, int count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint64_t* b) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
-}
-__device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-      : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
-  return ok != 0;
-}
-// Whether it has, without waiting (try_wait may suspend the thread for thousands
+// Whether a wait would succeed, without waiting (try_wait may suspend the thread for thousands
 // of cycles before it answers no).
 __device__ __forceinline__ bool bar_peek(uint64_t* b, uint32_t parity) {
   uint32_t ok;
@@ -79,15 +62,6 @@ __device__ __forceinline__ bool bar_peek(uint64_t* b, uint32_t parity) {
       : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return ok != 0;
 }
-// False if the wait ran out.  (The other roles' waits then run out too.)
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity) {
-#pragma unroll 1
-  for (int i = 0; i < kWaitLimit; ++i)
-    if (bar_test(b, parity)) return true;
-  return false;
-}
-// The same by a whole warp, with one answer.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, bar_wait(b, parity)); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // The commits and products below are one thread's.
@@ -102,14 +76,6 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
                "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
-}
-// True in one lane of a converged warp.  The matrix instructions' operands are
-// uniform registers: issued by the elected lane they take 5 instructions each,
-// under a test of the lane's number up to 44.
-__device__ __forceinline__ bool elect() {
-  uint32_t e;
-  asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(e));
-  return e != 0;
 }
 #define R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -156,16 +122,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
 // Descriptor of a block of 128-byte rows with the 128-byte swizzle.  Eight rows
 // are 1024 bytes; 'lead' is the distance of the second 64-element half where the
 // rows are the contraction's (values), unused where they are the result's.
@@ -195,16 +151,6 @@ struct QueryBlocks {
 };
 
 // ---- loader warps ------------------------------------------------------------------
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int page,
-                                         int layer) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(smem_addr(bar)) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
-}
-
 // A place in the ring of blocks, and the parity of its use.
 template <int N>
 struct Place {
@@ -624,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   __shared__ Shared sh;
   chain();
   const PlanHdr* hdr = a.plan.hdr;
-  const int C = hdr->ctas[1], c = blockIdx.x;
+  const int C = hdr->workers[1], c = blockIdx.x;
   if (c >= C) return;
   const int64_t U = hdr->cost[1];
   Parts<1> ps;
@@ -680,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
 
 template <typename T, int DP>
 cudaError_t wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
-  return launch(k_attend_wide<T, DP>, dim3((unsigned)a.plan.max_ctas[1]), kThreads, Shape<DP>::kSmem, st, a, m);
+  return launch(k_attend_wide<T, DP>, dim3((unsigned)a.plan.max_workers[1]), kThreads, Shape<DP>::kSmem, st, a, m);
 }
 template <typename T>
 cudaError_t wide_t(const AttendArgs& a, const PoolMaps& m, cudaStream_t st) {
@@ -704,7 +650,7 @@ cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st)
 
 bool make_maps(const Pool& p, PoolMaps* m) {
   m->ok = 0;
-  m->box = p.page_size < 32 ? p.page_size : 32;
+  m->box = p.page_size < 16 ? p.page_size : 16;
   if (p.page_size < 8) return false;
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult found;

@@ -13,9 +13,13 @@ constexpr int kAnyPages = 0x7FFFFFFF;
 constexpr int kShareTokens = 128;
 
 // Cycles of one unit, measured: a wide one on its SM (128 keys, with the other
-// SMs at the narrow tiles' memory traffic), a narrow one in its CTA when loads wait on latency alone, and when all CTAs
-// share the HBM bandwidth (64 keys of 128 elements).
-constexpr double kWideCycles = 3600, kNarrowCycles = 1250, kNarrowBandwidth = 3300;
+// SMs at the narrow tiles' memory traffic), a narrow one in its warp (16 keys of
+// 128 elements) when loads wait on latency alone, and when all warps share the
+// HBM bandwidth.
+constexpr double kWideCycles = 4500, kNarrowCycles = 1500, kNarrowBandwidth = 3200;
+// A narrow worker has at least so many units: more workers would cost the join
+// more than they save.
+constexpr int kLeastUnits = 2;
 
 // Pages of a request that every one of its queries sees whole.
 __device__ __forceinline__ int whole_pages(const Pool& p, const Batch& b, int r) {
@@ -256,7 +260,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   __shared__ unsigned long long s_best;
   if (tid == 0) s_best = ~0ull;
   __syncthreads();
-  const int sms = plan.max_ctas[1], per_sm = plan.max_ctas[0] / sms;
+  const int sms = plan.max_workers[1], per_sm = plan.max_workers[0] / sms;
   if (tid <= sms) {
     const bool can = (tid > 0 || units[1] == 0) && (tid < sms || units[0] == 0);
     const double wide = units[1] > 0 && tid > 0 ? (double)units[1] * kWideCycles / tid : 0;
@@ -268,30 +272,32 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   __syncthreads();
   const int wide_sms = (int)(s_best & 1023);
   const int64_t room[kLists] = {(int64_t)per_sm * (sms - wide_sms), wide_sms};
-  int ctas[kLists];
+  int workers[kLists];
   for (int l = 0; l < kLists; ++l) {
-    ctas[l] = (int)(units[l] < room[l] ? units[l] : room[l]);
+    const int64_t want = l ? units[l] : (units[l] + kLeastUnits - 1) / kLeastUnits;
+    workers[l] = (int)(want < room[l] ? want : room[l]);
     if (tid == 0) plan.ucum[l][tiles[l]] = units[l];
   }
   __syncthreads();
   for (int l = 0; l < kLists; ++l) {
-    for (int c = tid; c < ctas[l]; c += kPlanThreads) {
-      const int64_t u = units[l] * c / ctas[l];
+    for (int c = tid; c < workers[l]; c += kPlanThreads) {
+      const int64_t u = units[l] * c / workers[l];
       int lo = 0, hi = (int)tiles[l] - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
         if (plan.ucum[l][mid] <= u) lo = mid;
         else hi = mid - 1;
       }
-      plan.cta_tile[l][c] = lo;
+      plan.first_tile[l][c] = lo;
     }
   }
   if (tid == 0) {
     PlanHdr h{};
     h.status = PS_OK;
+    h.narrow_ctas = (int)room[0] / kNarrowWarps;
     for (int l = 0; l < kLists; ++l) {
       h.ntiles[l] = (int)tiles[l];
-      h.ctas[l] = ctas[l];
+      h.workers[l] = workers[l];
       h.cost[l] = units[l];
     }
     *plan.hdr = h;
@@ -302,10 +308,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
 template <int H>
 __device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, const PlanHdr& h, int list, int tile, int head) {
   const int64_t U = h.cost[list], b = plan.ucum[list][tile];
-  const int C = h.ctas[list];
+  const int C = h.workers[list];
   const int64_t each = (plan.ucum[list][tile + 1] - b) / p.kv_heads;
   const int64_t ua = b + head * each + tile_cost(list);  // the place of unit 0
-  const int ca = cta_of(ua, U, C), cb = cta_of(b + (head + 1) * each - 1, U, C);
+  const int ca = worker_of(ua, U, C), cb = worker_of(b + (head + 1) * each - 1, U, C);
   const Tile& t = plan.tiles[list][tile];
   Parts4 r;
   r.count = t.sidx < 0 && ca == cb ? 0 : cb - ca + 1;  // a whole one is written where it is computed
