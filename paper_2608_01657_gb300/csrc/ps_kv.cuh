@@ -141,14 +141,18 @@ __host__ __device__ __forceinline__ int64_t part_row(int sidx, int nrows, int he
   return sidx >= 0 ? (int64_t)(2 * C + c) * H + sidx + (int64_t)head * nrows : (int64_t)(2 * c + (continued ? 0 : 1)) * H;
 }
 
-// Tensor maps of the pool's keys and values: (element, head, token, page, layer),
-// a box of 64 elements of min(page_size, 16) tokens.
+// Tensor maps of one layer's keys and values: (element, head, token, page) with a
+// box of 64 elements of min(page_size, 16) tokens, and, where a head is whole
+// times 64 elements, (element, token, 64-element part, head, page) with a box of
+// all of a head's elements.
 struct PoolMaps {
-  CUtensorMap k, v;
-  int32_t ok;  // 0: pages of fewer than 8 tokens, or no maps
-  int32_t box;
+  CUtensorMap k, v, whole_k, whole_v;
+  int32_t ok;     // 0: pages of fewer than 8 tokens, or no maps
+  int32_t whole;  // whole_k and whole_v are there
+  int32_t box;    // tokens of a box
+  int32_t pad0;
 };
-bool make_maps(const Pool& p, PoolMaps* m);
+bool make_maps(const Pool& p, int32_t layer, PoolMaps* m);
 
 // Place of the four elements from 4 c on of partial row r: eight rows' words lie
 // side by side, so that a warp of 32 rows (wide tiles) and one of eight rows by

@@ -9,7 +9,7 @@ using namespace pskv;
 
 struct ps_kv {
   Pool pool;
-  PoolMaps maps;
+  PoolMaps* maps = nullptr;  // [layers]
   Plan plan;
   PageScratch pages;
   Batch batch;
@@ -149,7 +149,12 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   ps_kv* kv = new (std::nothrow) ps_kv{};
   if (!kv) return PS_ERR_CUDA;
   kv->pool = make_pool(*cfg);
-  make_maps(kv->pool, &kv->maps);
+  kv->maps = new (std::nothrow) PoolMaps[(size_t)cfg->num_layers];
+  if (!kv->maps) {
+    delete kv;
+    return PS_ERR_CUDA;
+  }
+  for (int32_t l = 0; l < cfg->num_layers; ++l) make_maps(kv->pool, l, kv->maps + l);
   kv->nsm = nsm < kMaxSms ? nsm : kMaxSms;
   kv->max_requests = cfg->max_requests;
   kv->max_tokens = cfg->max_tokens;
@@ -164,14 +169,18 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
     if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess) rc = PS_ERR_CUDA;
   }
   if (rc != PS_OK) {
-    delete kv;
+    ps_kv_destroy(kv);
     return rc;
   }
   *out = kv;
   return PS_OK;
 }
 
-void ps_kv_destroy(ps_kv_t* kv) { delete kv; }
+void ps_kv_destroy(ps_kv_t* kv) {
+  if (!kv) return;
+  delete[] kv->maps;
+  delete kv;
+}
 
 int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_append_t* a, int32_t* d_status) {
   if (!kv || !a || layer < 0 || layer >= kv->pool.num_layers || a->num_tokens < 0) return PS_ERR_INVALID_ARG;
@@ -216,7 +225,7 @@ int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_at
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) || !good_strides(a->q_stride) ||
       !good_strides(a->out_stride) || !(a->scale - a->scale == 0))
     return PS_ERR_INVALID_ARG;
-  return launch_attention(kv->pool, kv->maps, kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
+  return launch_attention(kv->pool, kv->maps[layer], kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
 }
 
 int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,

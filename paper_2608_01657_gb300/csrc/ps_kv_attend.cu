@@ -130,10 +130,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
             uint64_t* bar = &landed[lstage];
             if (box == 0) bar_expect(bar, there * 2 * S::kHalves * maps.box * 128);
             const uint32_t d = dst + box * maps.box * 128;
+            // one box's 16 tokens by 64 elements lie side by side where there is one box
+            if (maps.whole && boxes == 1) {
+              tma_load_whole(d, &maps.whole_k, bar, lp.head, tok, id);
+              tma_load_whole(d + S::kBlock, &maps.whole_v, bar, lp.head, tok, id);
+            } else {
 #pragma unroll
-            for (int half = 0; half < S::kHalves; ++half) {
-              tma_load(d + half * (16 * 128), &maps.k, bar, half * 64, lp.head, tok, id, a.layer);
-              tma_load(d + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, tok, id, a.layer);
+              for (int half = 0; half < S::kHalves; ++half) {
+                tma_load(d + half * (16 * 128), &maps.k, bar, half * 64, lp.head, tok, id);
+                tma_load(d + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, tok, id);
+              }
             }
           }
           __syncwarp();
@@ -504,7 +510,6 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   a.table_stride = b.table_stride;
   a.q_offsets = b.q_offsets;
   a.status = status;
-  a.layer = layer;
   a.scale2 = in.scale * 1.4426950408889634f;
   // no tile has more rows than the whole batch
   const bool wide = list_of(b.num_tokens * p.ratio) == 1;

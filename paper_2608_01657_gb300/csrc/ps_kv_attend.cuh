@@ -19,7 +19,7 @@ struct AttendArgs {
   int64_t table_stride;
   const int32_t* q_offsets;
   int32_t* status;
-  int32_t layer, after_wide;  // after_wide: the wide tiles' kernel was launched
+  int32_t after_wide;  // the wide tiles' kernel was launched
   float scale2;  // scale log2(e)
 };
 
@@ -61,12 +61,16 @@ __device__ __forceinline__ bool elect() {
   asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(e));
   return e != 0;
 }
-// A box of one page: 64 elements from x on, of the map's number of tokens.
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int page,
-                                         int layer) {
+// A box of one page, see PoolMaps: 64 elements from x on, or a head's elements.
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int head, int token, int page) {
   asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(smem_addr(bar)) : "memory");
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(head), "r"(token), "r"(page), "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_load_whole(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int head, int token, int page) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(token), "r"(head), "r"(page), "r"(smem_addr(bar)) : "memory");
 }
 // 16 bytes into shared memory, or zeros where !ok (src is not read then).
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {

@@ -256,7 +256,7 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
           if (whole) {
             if (lane == 0) bar_expect(bar, 32 * 128 * S::kHalves);
             __syncwarp();
-            if (issues) tma_load(dst + box_at, job ? &maps.v : &maps.k, bar, myhalf * 64, ps.head, token, id, a.layer);
+            if (issues) tma_load(dst + box_at, job ? &maps.v : &maps.k, bar, myhalf * 64, ps.head, token, id);
             continue;
           }
           off = id * a.pool.page_stride + (int64_t)token * a.pool.token_stride + (int64_t)ps.head * a.pool.head_stride;
@@ -294,7 +294,7 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
   constexpr uint32_t kBlk = S::kBlock >> 4;
   const uint32_t s_at = tmem + col_s(t), o_at = tmem + col_o(t);
   uint32_t p_phase = 0, turn = t ^ 1;  // group 0 has the first turn
-  Place<S::kBuffers> at;  // the key block of the tile's unit in turn; its value block is the next
+  Place<S::kBuffers> at;  // the tile's first block: unit 0's keys, then its values, unit 1's keys ...
   QueryBlocks qb;
   bool more = true;
   for (; more; more = ps.next()) {
@@ -304,18 +304,21 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
     if (!warp_wait(&sh->q_full[qblk], qb.fills >> qblk & 1)) return false;
     qb.next(pair);
     const uint64_t q = q_desc + qblk * kBlk;
-    // a block's two arrivals: both of the one group of a pair, one of each otherwise
+    // a query block's two arrivals: both of the one group of a pair, one of each otherwise
     auto release_q = [&]() {
       tc_commit(&sh->q_empty[qblk]);
       if (pair) tc_commit(&sh->q_empty[qblk]);
     };
-    // and of a key or value block: one of each group of a pair, both of the one that uses it otherwise
-    auto release = [&](const Place<S::kBuffers>& b) {
-      tc_commit(&sh->empty[b.slot]);
-      if (!pair) tc_commit(&sh->empty[b.slot]);
+    // A key or value block's arrivals are one of each group: a group passes over
+    // the blocks that the other one alone uses, so that it has seen every use of
+    // a place in the ring (a wait tells a use from the one after next, no more).
+    auto pass = [&](const Place<S::kBuffers>& b) {
+      if (!warp_wait(&sh->full[b.slot], b.par)) return false;
+      if (elect()) bar_arrive(&sh->empty[b.slot]);
+      __syncwarp();
+      return true;
     };
-    Place<S::kBuffers> kb = at;
-    if (!pair && t == 1) kb = kb.ahead(2);
+    Place<S::kBuffers> next = at;  // the first block that this group has not seen
     const int step = pair ? 1 : 2, first = pair ? 0 : t, turns = pair ? n : (n + 1) / 2;
     // Turn i: unit u's values, then the scores of this group's next unit (turn -1
     // is the first scores alone).  The blocks' waits come before the wait for the
@@ -323,13 +326,21 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
 #pragma unroll 1
     for (int i = -1; i < turns; ++i) {
       const int u = first + i * step;
-      const Place<S::kBuffers> vb = kb.ahead(1);
       const bool product = i >= 0 && u < n, more_keys = u + step < n;
+      const Place<S::kBuffers> vb = next;
       if (product) {
         if (!warp_wait(&sh->full[vb.slot], vb.par)) return false;
-        kb = kb.ahead(2 * step);
+        next = next.ahead(1);
       }
-      if (more_keys && !warp_wait(&sh->full[kb.slot], kb.par)) return false;
+      if (!pair && u + 1 >= 0 && u + 1 < n) {  // the other group's unit
+        if (!pass(next) || !pass(next.ahead(1))) return false;
+        next = next.ahead(2);
+      }
+      const Place<S::kBuffers> kb = next;
+      if (more_keys) {
+        if (!warp_wait(&sh->full[kb.slot], kb.par)) return false;
+        next = next.ahead(1);
+      }
       if (product) {
         if (!warp_wait(&sh->p_full[t], p_phase)) return false;
         p_phase ^= 1;
@@ -355,8 +366,8 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
           tc_commit(&sh->o_full[t]);
         }
         bar_arrive(&sh->turn[t ^ 1]);
-        if (product) release(vb);
-        if (more_keys) release(kb);
+        if (product) tc_commit(&sh->empty[vb.slot]);
+        if (more_keys) tc_commit(&sh->empty[kb.slot]);
         if (more_keys && u + 2 * step >= n) release_q();  // the last scores are on their way
       }
       __syncwarp();
@@ -648,8 +659,8 @@ cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st)
   return a.pool.dtype == PS_KV_BF16 ? wide_t<__nv_bfloat16>(a, m, st) : wide_t<__half>(a, m, st);
 }
 
-bool make_maps(const Pool& p, PoolMaps* m) {
-  m->ok = 0;
+bool make_maps(const Pool& p, int32_t layer, PoolMaps* m) {
+  m->ok = m->whole = 0;
   m->box = p.page_size < 16 ? p.page_size : 16;
   if (p.page_size < 8) return false;
   void* fn = nullptr;
@@ -658,22 +669,37 @@ bool make_maps(const Pool& p, PoolMaps* m) {
       found != cudaDriverEntryPointSuccess || !fn)
     return false;
   const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
-  const cuuint64_t dims[5] = {(cuuint64_t)p.head_dim, (cuuint64_t)p.kv_heads, (cuuint64_t)p.page_size, (cuuint64_t)p.num_pages,
-                              (cuuint64_t)p.num_layers};
-  const int64_t stride[4] = {p.head_stride, p.token_stride, p.page_stride, p.layer_stride};
-  cuuint64_t bytes[4];
-  for (int i = 0; i < 4; ++i) {  // an axis of one place is never stepped over: any stride will do
-    bytes[i] = dims[i + 1] > 1 ? 2 * (cuuint64_t)stride[i] : 16;
-    if (bytes[i] == 0 || bytes[i] >= (1ull << 40)) return false;
-  }
-  const cuuint32_t box[5] = {64, 1, (cuuint32_t)m->box, 1, 1}, step[5] = {1, 1, 1, 1, 1};
   const CUtensorMapDataType type = p.dtype == PS_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  for (int i = 0; i < 2; ++i)
-    if (encode(i ? &m->v : &m->k, type, 5, i ? p.v : p.k, dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return false;
-  m->ok = 1;
-  return true;
+  const int parts = p.head_dim / 64;
+  struct Axis {
+    int64_t size, stride;  // stride in elements
+    uint32_t box;
+  };
+  auto make = [&](CUtensorMap* map, void* base, const Axis* axes, int n) {
+    cuuint64_t dims[5], bytes[5];
+    cuuint32_t box[5], step[5];
+    for (int i = 0; i < n; ++i) {
+      dims[i] = (cuuint64_t)axes[i].size;
+      box[i] = axes[i].box;
+      step[i] = 1;
+      if (i == 0) continue;
+      // an axis of one place is never stepped over: any stride will do
+      bytes[i - 1] = axes[i].size > 1 ? 2 * (cuuint64_t)axes[i].stride : 16;
+      if (bytes[i - 1] == 0 || bytes[i - 1] >= (1ull << 40)) return false;
+    }
+    return encode(map, type, (cuuint32_t)n, base, dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  const uint32_t tokens = (uint32_t)m->box;
+  const Axis head = {p.kv_heads, p.head_stride, 1}, page = {p.num_pages, p.page_stride, 1},
+             token = {p.page_size, p.token_stride, tokens};
+  const Axis plain[4] = {{p.head_dim, 1, 64}, head, token, page};
+  const Axis whole[5] = {{64, 1, 64}, token, {parts, 64, (uint32_t)parts}, head, page};
+  char *k = p.k + 2 * layer * p.layer_stride, *v = p.v + 2 * layer * p.layer_stride;
+  m->ok = make(&m->k, k, plain, 4) && make(&m->v, v, plain, 4);
+  m->whole = m->ok && p.head_dim == 64 * parts && make(&m->whole_k, k, whole, 5) && make(&m->whole_v, v, whole, 5);
+  return m->ok != 0;
 }
 cudaError_t configure_wide(const Pool& p) {
   return p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim) : configure_t<__half>(p.head_dim);

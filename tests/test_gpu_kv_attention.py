@@ -174,6 +174,28 @@ def test_same_bits_again_and_on_another_stream():
     assert torch.equal(a, b) and torch.equal(la, lb)
 
 
+@pytest.mark.parametrize("new", [1, 5])
+def test_same_bits_many_times_under_memory_traffic(new):
+    """Many short prefixes beside many long rows: loads land in any order, results do not change."""
+    from paper_2608_01657_gb300 import kv as KV
+    r = np.random.RandomState(3)
+    groups, per, ps = 24, 8, 16
+    prefix = [ps * int(r.randint(10, 70)) for _ in range(groups)]
+    n = [new] * (groups * per)
+    kv = [prefix[i // per] + int(r.randint(1, 3000)) + new for i in range(groups * per)]
+    tables, pages, bounds = batch(n, kv, prefix, [g * per for g in range(groups)], ps)
+    k, v = make_pool(1, pages, ps, 4, 128, BF)
+    q = torch.randn(sum(n), 16, 128, device="cuda").to(BF)
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    pool = KV.KVPool(k, v, num_q_heads=16, max_requests=len(n), max_tokens=sum(n), max_row_pages=tables.shape[1])
+    pool.plan(dev(np.concatenate([[0], np.cumsum(n)])), dev(kv), dev(tables), sum(n), group_offsets=dev(bounds))
+    first = pool.attention(0, q, 0.09).clone()
+    for _ in range(60):
+        outs = [pool.attention(0, q, 0.09) for _ in range(3)]
+        assert all(torch.equal(o, first) for o in outs)
+    pool.check()
+
+
 def test_non_finite_values_stay_with_their_rows():
     """A NaN key or value reaches the rows that see it and no others."""
     from paper_2608_01657_gb300 import kv as KV
