@@ -149,7 +149,7 @@ struct PoolMaps {
   CUtensorMap k, v, whole_k, whole_v;
   int32_t ok;     // 0: pages of fewer than 8 tokens, or no maps
   int32_t whole;  // whole_k and whole_v are there
-  int32_t box;    // tokens of a box
+  int32_t box;    // tokens of a box: 8 or 16
   int32_t pad0;
 };
 bool make_maps(const Pool& p, int32_t layer, PoolMaps* m);

@@ -102,34 +102,42 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
 
   // ---- the loader: runs STAGES - 1 units ahead ----
   Parts<0> lp = ps;
-  int lunit = lp.unit, lend = lp.unit + lp.count;
   bool lmore = true;
+  int lkey, lend, lkv1;      // the loader's first key, the end of its units, the end of the keys
+  const int32_t* lrow;       // page ids of the request
+  auto enter = [&]() {
+    lkey = lp.t.kv0 + lp.unit * UNIT;
+    lend = lkey + lp.count * UNIT;
+    lkv1 = lp.t.kv1;
+    lrow = a.tables + lp.t.req * a.table_stride;
+  };
+  enter();
   const char* kbase = a.k;
   const char* vbase = a.v;
   // by TMA, lane i looks up box i's page; otherwise lane i key i's
-  const int boxes = 16 / maps.box;
-  const int mykey = tma ? (lane < boxes ? lane * maps.box : 0) : lane & 15;  // within a unit
+  const int boxes = maps.box == 8 ? 2 : 1;
+  const int mykey = tma ? (lane == 1 && boxes == 2 ? 8 : 0) : lane & 15;  // within a unit
   // page id of this lane's key in the loader's unit, -1 past the end
   auto key_page = [&]() -> int {
-    const int t = lp.t.kv0 + lunit * UNIT + mykey;
-    return t < lp.t.kv1 ? __ldg(a.tables + lp.t.req * a.table_stride + (t >> a.pool.page_log2)) : -1;
+    const int t = lkey + mykey;
+    return t < lkv1 ? __ldg(lrow + (t >> a.pool.page_log2)) : -1;
   };
   int page = key_page();
   int lstage = 0;
   auto load_unit = [&]() {
     if (lmore) {
-      const int token = (lp.t.kv0 + lunit * UNIT + mykey) & (a.pool.page_size - 1);
+      const int token = (lkey + mykey) & (a.pool.page_size - 1);
       const uint32_t dst = ring + lstage * 2 * S::kBlock;
       if (tma) {
         // boxes with a key in them: none of a tile without keys
-        const int there = min(boxes, (lp.t.kv1 - lp.t.kv0 - lunit * UNIT + maps.box - 1) / maps.box);
+        const int there = lkey >= lkv1 ? 0 : (boxes == 2 && lkey + 8 < lkv1 ? 2 : 1);
 #pragma unroll 1
         for (int box = 0; box < there; ++box) {
           const int id = __shfl_sync(0xFFFFFFFFu, page, box), tok = __shfl_sync(0xFFFFFFFFu, token, box);
           if (elect()) {
             uint64_t* bar = &landed[lstage];
-            if (box == 0) bar_expect(bar, there * 2 * S::kHalves * maps.box * 128);
-            const uint32_t d = dst + box * maps.box * 128;
+            if (box == 0) bar_expect(bar, boxes == 1 ? 2 * S::kBlock : there * S::kBlock);
+            const uint32_t d = dst + box * (8 * 128);
             // one box's 16 tokens by 64 elements lie side by side where there is one box
             if (maps.whole && boxes == 1) {
               tma_load_whole(d, &maps.whole_k, bar, lp.head, tok, id);
@@ -159,14 +167,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
           cp16(d + S::kBlock, vbase + at, ok);
         }
       }
-      if (++lunit == lend) {
+      lkey += UNIT;
+      if (lkey == lend) {
         lmore = lp.next();
-        lunit = lp.unit;
-        lend = lp.unit + lp.count;
+        if (lmore) enter();
       }
       if (lmore) page = key_page();
     }
-    cp_commit();
+    if (!tma) cp_commit();
     lstage = lstage + 1 == S::kStages ? 0 : lstage + 1;
   };
 #pragma unroll
