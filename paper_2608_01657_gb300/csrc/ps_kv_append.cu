@@ -21,18 +21,31 @@ struct AppendArgs {
 // The mathematics, for one head x of D elements: y = x w / sqrt(sum x^2 / D +
 // eps), then for each rotated pair (a, b) -> (a cos - b sin, b cos + a sin).
 //
-// Bound by HBM: every element is read once and written once.  A head's
-// elements are held by G = 8 or 16 lanes, 8 elements (16 bytes) each, so the
-// sum of squares is a shuffle over G lanes, and a pair's partner is either in
-// the lane itself (interleaved) or rope_dim / 2 elements away.  A group of lanes
-// takes several heads of one token, so that the token's cosines and sines are
-// read once into registers; a CTA's blockIdx.y takes a slice of the heads
-// (queries, then keys, then values).
-template <typename T, int G, bool INTERLEAVED>
+// Every element is read once and written once, so HBM is the floor; what it
+// comes to lies with the instructions per element, so there are few of them.  A
+// head is held by G = 8 or 16 lanes of two quads (4 elements) each, chosen so
+// that a pair's partner is in the lane itself: of the rotated part quad i with
+// quad i + rope_dim / 8, of the rest (and of interleaved pairs) neighbours.  The
+// sum of squares is a shuffle over G lanes; products and sums go two at a time.
+// A group of lanes takes several heads of one token, whose cosines and sines
+// stay in registers, U heads' loads in flight together.  A CTA's blockIdx.y
+// takes a slice of the heads (queries, then keys, then values).
+template <typename T>
+__device__ __forceinline__ uint64_t wide2(uint32_t x) {
+  const float2 f = Num<T>::unpack(x);
+  return pack2(f.x, f.y);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t narrow2(uint64_t x) {
+  const float2 f = unpack2(x);
+  return Num<T>::pack(f.x, f.y);
+}
+
+template <typename T, int G, bool INTERLEAVED, int U>
 __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
   chain();
-  const int lane = threadIdx.x % G, grp = threadIdx.x / G;
   constexpr int kGroups = 128 / G;
+  const int lane = threadIdx.x % G, grp = threadIdx.x / G;
   const int t = blockIdx.x;
   const int nheads = a.hq + 2 * a.hk;
   const int64_t slot = a.slots[t];
@@ -42,125 +55,123 @@ __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
     return;
   }
   const bool on = lane * 8 < a.dim;
-  // Rotated elements in quarter words of four: quarter g is one of the lane's
-  // two, g = 2 lane + s; without interleaving its partner is 'half' quarters
-  // up or down (in the lane's other place where half is odd).
-  const int half = a.rope_dim / 8;
-  const bool odd = half & 1;
-  // this lane's cosines and sines: of its own 8 elements, or of its 4 pairs
-  constexpr int NC = INTERLEAVED ? 4 : 8;
-  float cs[NC], sn[NC];
-#pragma unroll
-  for (int s = 0; s < NC / 4; ++s) {
-    const int g = INTERLEAVED ? lane : 2 * lane + s;
-    const int at = INTERLEAVED || g < half ? g : g - half;
-    if (a.rope && at < half) {
-      const float* row = a.rope + (int64_t)pos * a.rope_dim + 4 * at;
-      const float4 c = __ldg(reinterpret_cast<const float4*>(row));
-      const float4 x = __ldg(reinterpret_cast<const float4*>(row + a.rope_dim / 2));
-      cs[4 * s] = c.x; cs[4 * s + 1] = c.y; cs[4 * s + 2] = c.z; cs[4 * s + 3] = c.w;
-      sn[4 * s] = x.x; sn[4 * s + 1] = x.y; sn[4 * s + 2] = x.z; sn[4 * s + 3] = x.w;
-    } else {  // not rotated
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        cs[4 * s + i] = 1.0f;
-        sn[4 * s + i] = 0.0f;
-      }
-    }
+  const int pairs = a.rope_dim / 8;  // quads of half the rotated part
+  const bool rotated = lane < pairs;
+  // byte offsets of the lane's two quads in a head
+  const int qa = INTERLEAVED || !rotated ? 2 * lane : lane;
+  const int at0 = 8 * qa, at1 = 8 * (INTERLEAVED || !rotated ? qa + 1 : qa + pairs);
+  // the pairs' cosines and sines; 1 and 0 where nothing turns
+  uint64_t cs[2], sn[2];
+  if (rotated) {
+    const float* row = a.rope + (int64_t)pos * a.rope_dim + 4 * lane;
+    const float4 c = __ldg(reinterpret_cast<const float4*>(row));
+    const float4 s = __ldg(reinterpret_cast<const float4*>(row + a.rope_dim / 2));
+    cs[0] = pack2(c.x, c.y); cs[1] = pack2(c.z, c.w);
+    sn[0] = pack2(s.x, s.y); sn[1] = pack2(s.z, s.w);
+  } else {
+    cs[0] = cs[1] = pack2(1.0f, 1.0f);
+    sn[0] = sn[1] = 0;
   }
-  const int64_t at = slot < 0 ? 0 : (slot >> a.page_log2) * a.page_stride +
-                                        (slot & ((1 << a.page_log2) - 1)) * a.token_stride;
-  for (int h0 = blockIdx.y * kGroups; h0 < nheads; h0 += gridDim.y * kGroups) {
-    const int h = h0 + grp;
-    const bool have = h < nheads;
-    const int kind = h < a.hq ? 0 : (h < a.hq + a.hk ? 1 : 2);
-    const int hh = kind == 0 ? h : (kind == 1 ? h - a.hq : h - a.hq - a.hk);
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (have && on) {
-      const char* src = kind == 0 ? a.q + 2 * (t * a.qs[0] + hh * a.qs[1])
-                                  : (kind == 1 ? a.k + 2 * (t * a.ks[0] + hh * a.ks[1])
-                                               : a.v + 2 * (t * a.vs[0] + hh * a.vs[1]));
-      raw = *reinterpret_cast<const uint4*>(src + lane * 16);
-    }
-    float x[8];
-    {
-      const float2 f0 = Num<T>::unpack(raw.x), f1 = Num<T>::unpack(raw.y), f2 = Num<T>::unpack(raw.z),
-                   f3 = Num<T>::unpack(raw.w);
-      x[0] = f0.x; x[1] = f0.y; x[2] = f1.x; x[3] = f1.y; x[4] = f2.x; x[5] = f2.y; x[6] = f3.x; x[7] = f3.y;
-    }
-    const char* wp = kind == 0 ? a.qw : a.kw;
-    if (a.qw || a.kw) {  // both shuffles and branches are uniform over the CTA
-      float ss = 0;
+  // the norms' weights, as they are
+  uint2 wq[2] = {}, wk[2] = {};
+  if (on && a.qw) {
+    wq[0] = __ldg(reinterpret_cast<const uint2*>(a.qw + at0));
+    wq[1] = __ldg(reinterpret_cast<const uint2*>(a.qw + at1));
+  }
+  if (on && a.kw) {
+    wk[0] = __ldg(reinterpret_cast<const uint2*>(a.kw + at0));
+    wk[1] = __ldg(reinterpret_cast<const uint2*>(a.kw + at1));
+  }
+  const char* q = a.q + 2 * t * a.qs[0];
+  const char* k = a.k + 2 * t * a.ks[0];
+  const char* v = a.v + 2 * t * a.vs[0];
+  char* qo = a.qo + 2 * t * a.os[0];
+  const int64_t at = slot < 0 ? 0 : 2 * ((slot >> a.page_log2) * a.page_stride +
+                                         (slot & ((1 << a.page_log2) - 1)) * a.token_stride);
+  char *pk = a.pk + at, *pv = a.pv + at;
+  const float inv_dim = 1.0f / a.dim;
+  for (int h0 = blockIdx.y * kGroups * U + grp; h0 < nheads + grp; h0 += gridDim.y * kGroups * U) {
+    uint2 raw[U][2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-#pragma unroll
-      for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-      if (kind < 2 && wp && on) {
-        const float r = 1.0f / sqrtf(ss / a.dim + a.eps);
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(wp + lane * 16));
-        const float2 f0 = Num<T>::unpack(w.x), f1 = Num<T>::unpack(w.y), f2 = Num<T>::unpack(w.z),
-                     f3 = Num<T>::unpack(w.w);
-        x[0] *= r * f0.x; x[1] *= r * f0.y; x[2] *= r * f1.x; x[3] *= r * f1.y;
-        x[4] *= r * f2.x; x[5] *= r * f2.y; x[6] *= r * f3.x; x[7] *= r * f3.y;
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * kGroups;
+      const char* src = h < a.hq ? q + 2 * h * a.qs[1]
+                                 : (h < a.hq + a.hk ? k + 2 * (h - a.hq) * a.ks[1] : v + 2 * (h - a.hq - a.hk) * a.vs[1]);
+      raw[u][0] = raw[u][1] = make_uint2(0, 0);
+      if (h < nheads && on) {
+        raw[u][0] = *reinterpret_cast<const uint2*>(src + at0);
+        raw[u][1] = *reinterpret_cast<const uint2*>(src + at1);
       }
     }
-    if (a.rope) {
-      if (INTERLEAVED) {
-        if (kind < 2 && lane < half) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float u = x[2 * i], w = x[2 * i + 1];
-            x[2 * i] = u * cs[i % NC] - w * sn[i % NC];
-            x[2 * i + 1] = w * cs[i % NC] + u * sn[i % NC];
-          }
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * kGroups;
+      const bool query = h < a.hq, key = !query && h < a.hq + a.hk;
+      // both quads, two elements at a time; x[0], x[1] pair with x[2], x[3]
+      uint64_t x[4] = {wide2<T>(raw[u][0].x), wide2<T>(raw[u][0].y), wide2<T>(raw[u][1].x), wide2<T>(raw[u][1].y)};
+      if (a.qw || a.kw) {  // uniform over the CTA: the shuffles are for whole warps
+        uint64_t s2 = mul2(x[0], x[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) s2 = fma2(x[i], x[i], s2);
+        const float2 f = unpack2(s2);
+        float ss = f.x + f.y;
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+        if (query ? a.qw != nullptr : a.kw != nullptr) {
+          const float r = rsqrtf(ss * inv_dim + a.eps);
+          const uint64_t r2 = pack2(r, r);
+          const uint2 w0 = query ? wq[0] : wk[0], w1 = query ? wq[1] : wk[1];
+          x[0] = mul2(mul2(x[0], r2), wide2<T>(w0.x));
+          x[1] = mul2(mul2(x[1], r2), wide2<T>(w0.y));
+          x[2] = mul2(mul2(x[2], r2), wide2<T>(w1.x));
+          x[3] = mul2(mul2(x[3], r2), wide2<T>(w1.y));
         }
-      } else {
-        float o[8];
+      }
+      if (rotated) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int g = 2 * lane + s;
-          const int peer = g < half ? g + half : (g < 2 * half ? g - half : g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            o[4 * s + i] = __shfl_sync(0xFFFFFFFFu, odd ? x[4 * (1 - s) + i] : x[4 * s + i], peer >> 1, G);
-        }
-        if (kind < 2) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int g = 2 * lane + i / 4;
-            if (g < half) x[i] = x[i] * cs[i % NC] - o[i] * sn[i % NC];
-            else if (g < 2 * half) x[i] = x[i] * cs[i % NC] + o[i] * sn[i % NC];
+        for (int i = 0; i < 2; ++i) {
+          if (INTERLEAVED) {  // pairs (x, y) of quad i: its elements 0, 1 and 2, 3
+            const float2 p = unpack2(x[2 * i]), r = unpack2(x[2 * i + 1]), c = unpack2(cs[i]), s = unpack2(sn[i]);
+            x[2 * i] = pack2(p.x * c.x - p.y * s.x, p.y * c.x + p.x * s.x);
+            x[2 * i + 1] = pack2(r.x * c.y - r.y * s.y, r.y * c.y + r.x * s.y);
+          } else {
+            const uint64_t p = x[i], r = x[i + 2];
+            const uint64_t minus = sn[i] ^ 0x8000000080000000ull;
+            x[i] = fma2(r, minus, mul2(p, cs[i]));
+            x[i + 2] = fma2(p, sn[i], mul2(r, cs[i]));
           }
         }
       }
+      if (h >= nheads || !on || (slot < 0 && !query)) continue;
+      // values are moved as they are (a conversion could change a NaN's bits)
+      uint2 y0 = raw[u][0], y1 = raw[u][1];
+      if (query || key) {
+        y0 = make_uint2(narrow2<T>(x[0]), narrow2<T>(x[1]));
+        y1 = make_uint2(narrow2<T>(x[2]), narrow2<T>(x[3]));
+      }
+      char* dst = query ? qo + 2 * h * a.os[1]
+                        : (key ? pk + 2 * (h - a.hq) * a.head_stride : pv + 2 * (h - a.hq - a.hk) * a.head_stride);
+      *reinterpret_cast<uint2*>(dst + at0) = y0;
+      *reinterpret_cast<uint2*>(dst + at1) = y1;
     }
-    if (!have || !on) continue;
-    // values are moved as they are (a conversion could change a NaN's bits)
-    if (kind < 2)
-      raw = make_uint4(Num<T>::pack(x[0], x[1]), Num<T>::pack(x[2], x[3]), Num<T>::pack(x[4], x[5]),
-                       Num<T>::pack(x[6], x[7]));
-    char* dst;
-    if (kind == 0) {
-      dst = a.qo + 2 * (t * a.os[0] + hh * a.os[1]);
-    } else {
-      if (slot < 0) continue;
-      dst = (kind == 1 ? a.pk : a.pv) + 2 * (at + hh * a.head_stride);
-    }
-    *reinterpret_cast<uint4*>(dst + lane * 16) = raw;
   }
 }
 
-template <typename T>
-cudaError_t launch_t(const AppendArgs& a, bool interleaved, int nsm, cudaStream_t st) {
-  const int groups = a.dim <= 64 ? 16 : 8;
-  // few tokens: spread a token's heads over CTAs until the GPU has one wave
-  const int slices = (a.hq + 2 * a.hk + groups - 1) / groups;
+template <typename T, int G, bool I>
+cudaError_t launch_g(const AppendArgs& a, int nsm, cudaStream_t st) {
+  // few tokens: spread a token's heads over CTAs until the GPU has some waves;
+  // otherwise three heads of a group at a time (8191 tokens of 48 heads of 128:
+  // 41 us, one at a time 53)
+  const int groups = 128 / G, slices = (a.hq + 2 * a.hk + groups - 1) / groups;
   int ny = (4 * nsm + a.T - 1) / a.T;
   ny = ny < 1 ? 1 : (ny > slices ? slices : ny);
   const dim3 grid((unsigned)a.T, (unsigned)ny);
-  if (a.dim <= 64)
-    return interleaved ? launch(k_append<T, 8, true>, grid, 128, 0, st, a) : launch(k_append<T, 8, false>, grid, 128, 0, st, a);
-  return interleaved ? launch(k_append<T, 16, true>, grid, 128, 0, st, a) : launch(k_append<T, 16, false>, grid, 128, 0, st, a);
+  return slices >= 3 * ny ? launch(k_append<T, G, I, 3>, grid, 128, 0, st, a) : launch(k_append<T, G, I, 1>, grid, 128, 0, st, a);
+}
+template <typename T>
+cudaError_t launch_t(const AppendArgs& a, bool interleaved, int nsm, cudaStream_t st) {
+  if (a.dim <= 64) return interleaved ? launch_g<T, 8, true>(a, nsm, st) : launch_g<T, 8, false>(a, nsm, st);
+  return interleaved ? launch_g<T, 16, true>(a, nsm, st) : launch_g<T, 16, false>(a, nsm, st);
 }
 
 }  // namespace
@@ -180,7 +191,7 @@ int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& in, in
   a.page_stride = p.page_stride; a.token_stride = p.token_stride; a.head_stride = p.head_stride;
   a.nslots = p.num_pages << p.page_log2;
   a.T = in.num_tokens; a.hq = p.q_heads; a.hk = p.kv_heads; a.dim = p.head_dim; a.page_log2 = p.page_log2;
-  a.rope_rows = in.rope_rows; a.rope_dim = in.rope_dim; a.eps = in.eps;
+  a.rope_rows = in.rope_rows; a.rope_dim = a.rope ? in.rope_dim : 0; a.eps = in.eps;
   return status_of(p.dtype == PS_KV_BF16 ? launch_t<__nv_bfloat16>(a, in.rope_interleaved != 0, nsm, st)
                                          : launch_t<__half>(a, in.rope_interleaved != 0, nsm, st));
 }
