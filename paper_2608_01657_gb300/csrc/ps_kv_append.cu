@@ -28,8 +28,7 @@ struct AppendArgs {
 // quad i + rope_dim / 8, of the rest (and of interleaved pairs) neighbours.  The
 // sum of squares is a shuffle over G lanes; products and sums go two at a time.
 // A group of lanes takes several heads of one token, whose cosines and sines
-// stay in registers, U heads' loads in flight together.  A CTA's blockIdx.y
-// takes a slice of the heads (queries, then keys, then values).
+// stay in registers, U query heads' loads in flight together.
 template <typename T>
 __device__ __forceinline__ uint64_t wide2(uint32_t x) {
   const float2 f = Num<T>::unpack(x);
@@ -41,25 +40,39 @@ __device__ __forceinline__ uint32_t narrow2(uint64_t x) {
   return Num<T>::pack(f.x, f.y);
 }
 
+// Enough warps to hide the loads' latency (8191 tokens: 53 us with 8, 44 with 12).
+constexpr int kCtasPerSm = 12;
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+
 template <typename T, int G, bool INTERLEAVED, int U>
-__global__ void __launch_bounds__(128) k_append(AppendArgs a) {
+__global__ void __launch_bounds__(128, kCtasPerSm) k_append(AppendArgs a) {
   chain();
   constexpr int kGroups = 128 / G;
   const int lane = threadIdx.x % G, grp = threadIdx.x / G;
-  const int t = blockIdx.x;
-  const int nheads = a.hq + 2 * a.hk;
-  const int64_t slot = a.slots[t];
-  const int pos = a.rope ? a.positions[t] : 0;
-  if (slot >= a.nslots || (a.rope && (pos < 0 || pos >= a.rope_rows))) {
-    if (threadIdx.x == 0) set_error(a.status, PS_ERR_INVALID_ARG);
-    return;
-  }
   const bool on = lane * 8 < a.dim;
   const int pairs = a.rope_dim / 8;  // quads of half the rotated part
   const bool rotated = lane < pairs;
   // byte offsets of the lane's two quads in a head
   const int qa = INTERLEAVED || !rotated ? 2 * lane : lane;
   const int at0 = 8 * qa, at1 = 8 * (INTERLEAVED || !rotated ? qa + 1 : qa + pairs);
+  const float inv_dim = 1.0f / a.dim;
+  // A token's slot and position are read while the one before it is worked on.
+  int64_t next_slot = blockIdx.x < a.T ? a.slots[blockIdx.x] : 0;
+  int next_pos = a.rope && blockIdx.x < a.T ? a.positions[blockIdx.x] : 0;
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+  const int64_t slot = next_slot;
+  const int pos = next_pos;
+  if (t + (int64_t)gridDim.x < a.T) {
+    next_slot = a.slots[t + gridDim.x];
+    if (a.rope) next_pos = a.positions[t + gridDim.x];
+  }
+  if (slot >= a.nslots || (a.rope && (pos < 0 || pos >= a.rope_rows))) {
+    if (threadIdx.x == 0) set_error(a.status, PS_ERR_INVALID_ARG);
+    continue;
+  }
   // the pairs' cosines and sines; 1 and 0 where nothing turns
   uint64_t cs[2], sn[2];
   if (rotated) {
@@ -72,101 +85,106 @@ __global__ void __launch_bounds__(128) k_append(AppendArgs a) {
     cs[0] = cs[1] = pack2(1.0f, 1.0f);
     sn[0] = sn[1] = 0;
   }
-  // the norms' weights, as they are
-  uint2 wq[2] = {}, wk[2] = {};
-  if (on && a.qw) {
-    wq[0] = __ldg(reinterpret_cast<const uint2*>(a.qw + at0));
-    wq[1] = __ldg(reinterpret_cast<const uint2*>(a.qw + at1));
-  }
-  if (on && a.kw) {
-    wk[0] = __ldg(reinterpret_cast<const uint2*>(a.kw + at0));
-    wk[1] = __ldg(reinterpret_cast<const uint2*>(a.kw + at1));
-  }
-  const char* q = a.q + 2 * t * a.qs[0];
-  const char* k = a.k + 2 * t * a.ks[0];
-  const char* v = a.v + 2 * t * a.vs[0];
-  char* qo = a.qo + 2 * t * a.os[0];
   const int64_t at = slot < 0 ? 0 : 2 * ((slot >> a.page_log2) * a.page_stride +
                                          (slot & ((1 << a.page_log2) - 1)) * a.token_stride);
-  char *pk = a.pk + at, *pv = a.pv + at;
-  const float inv_dim = 1.0f / a.dim;
-  for (int h0 = blockIdx.y * kGroups * U + grp; h0 < nheads + grp; h0 += gridDim.y * kGroups * U) {
-    uint2 raw[U][2];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * kGroups;
-      const char* src = h < a.hq ? q + 2 * h * a.qs[1]
-                                 : (h < a.hq + a.hk ? k + 2 * (h - a.hq) * a.ks[1] : v + 2 * (h - a.hq - a.hk) * a.vs[1]);
-      raw[u][0] = raw[u][1] = make_uint2(0, 0);
-      if (h < nheads && on) {
-        raw[u][0] = *reinterpret_cast<const uint2*>(src + at0);
-        raw[u][1] = *reinterpret_cast<const uint2*>(src + at1);
-      }
+  // Heads grp, grp + kGroups, ... of the queries (slices [0, nq)), the keys
+  // [nq, nq + nk) and the values, of which this CTA takes every gridDim.y-th.
+  const int nq = (a.hq + kGroups - 1) / kGroups, nk = (a.hk + kGroups - 1) / kGroups;
+  int slice = blockIdx.y;
+
+  // norm and rotation of a slice's heads, U slices' loads at a time
+  auto heads = [&](auto batch, int end, int base, int count, const char* src, int64_t src_stride, char* dst,
+                   int64_t dst_stride, const char* weight, bool write) {
+    constexpr int B = decltype(batch)::value;
+    uint64_t w[4] = {};
+    if (on && weight) {
+      const uint2 w0 = __ldg(reinterpret_cast<const uint2*>(weight + at0)), w1 = __ldg(reinterpret_cast<const uint2*>(weight + at1));
+      w[0] = wide2<T>(w0.x); w[1] = wide2<T>(w0.y); w[2] = wide2<T>(w1.x); w[3] = wide2<T>(w1.y);
     }
+    int h = (slice - base) * kGroups + grp;
+    const int step = (int)gridDim.y * kGroups;
+    src += 2 * h * src_stride;
+    dst += 2 * h * dst_stride;
+    for (; slice < end; slice += (int)gridDim.y * B) {
+      uint2 raw[B][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * kGroups;
-      const bool query = h < a.hq, key = !query && h < a.hq + a.hk;
-      // both quads, two elements at a time; x[0], x[1] pair with x[2], x[3]
-      uint64_t x[4] = {wide2<T>(raw[u][0].x), wide2<T>(raw[u][0].y), wide2<T>(raw[u][1].x), wide2<T>(raw[u][1].y)};
-      if (a.qw || a.kw) {  // uniform over the CTA: the shuffles are for whole warps
-        uint64_t s2 = mul2(x[0], x[0]);
+      for (int u = 0; u < B; ++u) {
+        raw[u][0] = raw[u][1] = make_uint2(0, 0);
+        if (h + u * step < count && on) {
+          const char* p = src + 2 * u * step * src_stride;
+          raw[u][0] = *reinterpret_cast<const uint2*>(p + at0);
+          raw[u][1] = *reinterpret_cast<const uint2*>(p + at1);
+        }
+      }
 #pragma unroll
-        for (int i = 1; i < 4; ++i) s2 = fma2(x[i], x[i], s2);
-        const float2 f = unpack2(s2);
-        float ss = f.x + f.y;
+      for (int u = 0; u < B; ++u) {
+        // both quads, two elements at a time; x[0], x[1] pair with x[2], x[3]
+        uint64_t x[4] = {wide2<T>(raw[u][0].x), wide2<T>(raw[u][0].y), wide2<T>(raw[u][1].x), wide2<T>(raw[u][1].y)};
+        if (weight) {
+          uint64_t s2 = mul2(x[0], x[0]);
 #pragma unroll
-        for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-        if (query ? a.qw != nullptr : a.kw != nullptr) {
+          for (int i = 1; i < 4; ++i) s2 = fma2(x[i], x[i], s2);
+          const float2 f = unpack2(s2);
+          float ss = f.x + f.y;
+#pragma unroll
+          for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
           const float r = rsqrtf(ss * inv_dim + a.eps);
           const uint64_t r2 = pack2(r, r);
-          const uint2 w0 = query ? wq[0] : wk[0], w1 = query ? wq[1] : wk[1];
-          x[0] = mul2(mul2(x[0], r2), wide2<T>(w0.x));
-          x[1] = mul2(mul2(x[1], r2), wide2<T>(w0.y));
-          x[2] = mul2(mul2(x[2], r2), wide2<T>(w1.x));
-          x[3] = mul2(mul2(x[3], r2), wide2<T>(w1.y));
-        }
-      }
-      if (rotated) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (INTERLEAVED) {  // pairs (x, y) of quad i: its elements 0, 1 and 2, 3
-            const float2 p = unpack2(x[2 * i]), r = unpack2(x[2 * i + 1]), c = unpack2(cs[i]), s = unpack2(sn[i]);
-            x[2 * i] = pack2(p.x * c.x - p.y * s.x, p.y * c.x + p.x * s.x);
-            x[2 * i + 1] = pack2(r.x * c.y - r.y * s.y, r.y * c.y + r.x * s.y);
-          } else {
-            const uint64_t p = x[i], r = x[i + 2];
-            const uint64_t minus = sn[i] ^ 0x8000000080000000ull;
-            x[i] = fma2(r, minus, mul2(p, cs[i]));
-            x[i + 2] = fma2(p, sn[i], mul2(r, cs[i]));
+          for (int i = 0; i < 4; ++i) x[i] = mul2(mul2(x[i], r2), w[i]);
+        }
+        if (rotated) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (INTERLEAVED) {  // pairs (x, y) of quad i: its elements 0, 1 and 2, 3
+              const float2 p = unpack2(x[2 * i]), r = unpack2(x[2 * i + 1]), c = unpack2(cs[i]), s = unpack2(sn[i]);
+              x[2 * i] = pack2(p.x * c.x - p.y * s.x, p.y * c.x + p.x * s.x);
+              x[2 * i + 1] = pack2(r.x * c.y - r.y * s.y, r.y * c.y + r.x * s.y);
+            } else {
+              const uint64_t p = x[i], r = x[i + 2];
+              x[i] = fma2(r, sn[i] ^ 0x8000000080000000ull, mul2(p, cs[i]));
+              x[i + 2] = fma2(p, sn[i], mul2(r, cs[i]));
+            }
           }
         }
+        if (h + u * step < count && on && write) {
+          char* p = dst + 2 * u * step * dst_stride;
+          *reinterpret_cast<uint2*>(p + at0) = make_uint2(narrow2<T>(x[0]), narrow2<T>(x[1]));
+          *reinterpret_cast<uint2*>(p + at1) = make_uint2(narrow2<T>(x[2]), narrow2<T>(x[3]));
+        }
       }
-      if (h >= nheads || !on || (slot < 0 && !query)) continue;
-      // values are moved as they are (a conversion could change a NaN's bits)
-      uint2 y0 = raw[u][0], y1 = raw[u][1];
-      if (query || key) {
-        y0 = make_uint2(narrow2<T>(x[0]), narrow2<T>(x[1]));
-        y1 = make_uint2(narrow2<T>(x[2]), narrow2<T>(x[3]));
-      }
-      char* dst = query ? qo + 2 * h * a.os[1]
-                        : (key ? pk + 2 * (h - a.hq) * a.head_stride : pv + 2 * (h - a.hq - a.hk) * a.head_stride);
-      *reinterpret_cast<uint2*>(dst + at0) = y0;
-      *reinterpret_cast<uint2*>(dst + at1) = y1;
+      h += B * step;
+      src += 2 * B * step * src_stride;
+      dst += 2 * B * step * dst_stride;
     }
+  };
+  if (slice < nq)
+    heads(Count<U>{}, nq, 0, a.hq, a.q + 2 * t * a.qs[0], a.qs[1], a.qo + 2 * t * a.os[0], a.os[1], a.qw, true);
+  // a batch may have stepped over slices that are not the queries'
+  slice = nq > (int)blockIdx.y ? (int)blockIdx.y + (nq - (int)blockIdx.y + (int)gridDim.y - 1) / (int)gridDim.y * (int)gridDim.y
+                               : (int)blockIdx.y;
+  if (slice < nq + nk)
+    heads(Count<1>{}, nq + nk, nq, a.hk, a.k + 2 * t * a.ks[0], a.ks[1], a.pk + at, a.head_stride, a.kw, slot >= 0);
+  if (slot < 0) continue;
+  // values are moved as they are (a conversion could change a NaN's bits)
+  for (; slice < nq + 2 * nk; slice += gridDim.y) {
+    const int h = (slice - nq - nk) * kGroups + grp;
+    if (h < a.hk && on)
+      *reinterpret_cast<uint4*>(a.pv + at + 2 * h * a.head_stride + 16 * lane) =
+          *reinterpret_cast<const uint4*>(a.v + 2 * (t * a.vs[0] + h * a.vs[1]) + 16 * lane);
+  }
   }
 }
 
 template <typename T, int G, bool I>
 cudaError_t launch_g(const AppendArgs& a, int nsm, cudaStream_t st) {
   // few tokens: spread a token's heads over CTAs until the GPU has some waves;
-  // otherwise three heads of a group at a time (8191 tokens of 48 heads of 128:
-  // 41 us, one at a time 53)
-  const int groups = 128 / G, slices = (a.hq + 2 * a.hk + groups - 1) / groups;
+  // otherwise the loads of two heads of a group at a time
+  const int groups = 128 / G, nq = (a.hq + groups - 1) / groups, slices = nq + 2 * ((a.hk + groups - 1) / groups);
   int ny = (4 * nsm + a.T - 1) / a.T;
   ny = ny < 1 ? 1 : (ny > slices ? slices : ny);
-  const dim3 grid((unsigned)a.T, (unsigned)ny);
-  return slices >= 3 * ny ? launch(k_append<T, G, I, 3>, grid, 128, 0, st, a) : launch(k_append<T, G, I, 1>, grid, 128, 0, st, a);
+  const dim3 grid((unsigned)(a.T < nsm * kCtasPerSm ? a.T : nsm * kCtasPerSm), (unsigned)ny);
+  return nq >= 2 * ny ? launch(k_append<T, G, I, 2>, grid, 128, 0, st, a) : launch(k_append<T, G, I, 1>, grid, 128, 0, st, a);
 }
 template <typename T>
 cudaError_t launch_t(const AppendArgs& a, bool interleaved, int nsm, cudaStream_t st) {
