@@ -113,7 +113,7 @@ typedef struct {
   const void* q_weight;      /* [head_dim], the pool's type; NULL: no norm of the queries */
   const void* k_weight;      /* [head_dim]; NULL: no norm of the keys */
   float eps;                 /* > 0 */
-  int32_t num_tokens;        /* T, any number >= 0 */
+  int32_t num_tokens;        /* T, 0..2^30 */
   int32_t rope_rows;
   int32_t rope_dim;          /* rotated leading elements of a head: a multiple of 8, at most head_dim */
   int32_t rope_interleaved;  /* pairs (2i, 2i + 1) instead of (i, i + rope_dim / 2) */

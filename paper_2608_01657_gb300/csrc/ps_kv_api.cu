@@ -183,7 +183,8 @@ void ps_kv_destroy(ps_kv_t* kv) {
 }
 
 int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_append_t* a, int32_t* d_status) {
-  if (!kv || !a || layer < 0 || layer >= kv->pool.num_layers || a->num_tokens < 0) return PS_ERR_INVALID_ARG;
+  if (!kv || !a || layer < 0 || layer >= kv->pool.num_layers || a->num_tokens < 0 || a->num_tokens > (1 << 30))
+    return PS_ERR_INVALID_ARG;
   if (a->num_tokens == 0) return PS_OK;
   if (!a->q || !a->k || !a->v || !a->q_out || !a->slots) return PS_ERR_INVALID_ARG;
   for (const void* p : {a->q, a->k, a->v, (const void*)a->q_out, a->q_weight, a->k_weight, (const void*)a->rope})

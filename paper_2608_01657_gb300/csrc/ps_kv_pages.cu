@@ -8,57 +8,70 @@ namespace {
 constexpr int kCopyThreads = 256;
 
 // ---- moving keys and values ---------------------------------------------------
-// Copy 'tok' tokens of one page of one layer (keys or values) by the CTA.  Bound
-// by HBM: one read and one write of the page.  A page that is one run of memory
-// is copied as such, four 16-byte words a thread in flight; otherwise a 16-byte
-// word's token, head and place are found by division.
-__device__ __forceinline__ void copy_page(const Pool& p, char* base, int64_t src, int64_t dst, int tok) {
+constexpr int kCopyWords = 512;  // 16-byte words of a page that a warp copies at a time
+constexpr int kCopyWarps = kCopyThreads / 32;
+
+__host__ __device__ __forceinline__ int copy_parts(const Pool& p, int tok) {
+  return (tok * p.kv_heads * (p.head_dim / 8) + kCopyWords - 1) / kCopyWords;
+}
+// Part 'part' of copying 'tok' tokens of one page of one layer (slice / 2; keys
+// or values by slice mod 2), by a warp.  Bound by HBM: one read and one write of
+// the page, eight words a lane in flight.  (A CTA of 256 threads for a page had
+// two words a thread in flight where a page is 8 KB: 5.1 TB/s of the 6.8 that
+// copies reach.)  A page that is one run of memory is copied as such; otherwise
+// a word's token, head and place are found by division.
+__device__ __forceinline__ void copy_part(const Pool& p, int64_t src, int64_t dst, int slice, int tok, int part, int lane) {
   const int words = p.head_dim / 8;  // 16-byte words of a head
-  const int n = tok * p.kv_heads * words;
+  const int n = min(tok * p.kv_heads * words, (part + 1) * kCopyWords);
+  char* base = ((slice & 1) ? p.v : p.k) + 2 * (slice >> 1) * p.layer_stride;
   const uint4* s = reinterpret_cast<const uint4*>(base + 2 * src * p.page_stride);
   uint4* d = reinterpret_cast<uint4*>(base + 2 * dst * p.page_stride);
   const bool token_major = p.head_stride == p.head_dim && p.token_stride == (int64_t)p.kv_heads * p.head_dim;
   const bool head_major = tok == p.page_size && p.token_stride == p.head_dim &&
                           p.head_stride == (int64_t)p.page_size * p.head_dim;
-  if (token_major || head_major) {
-    int i = threadIdx.x;
-    for (; i + 3 * kCopyThreads < n; i += 4 * kCopyThreads) {
-      uint4 w[4];
+  const bool run = token_major || head_major;
+  for (int i0 = part * kCopyWords + lane; i0 < n; i0 += 8 * 32) {
+    uint4 w[8];
+    int64_t at[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = __ldcs(s + i + u * kCopyThreads);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) __stcs(d + i + u * kCopyThreads, w[u]);
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + 32 * u;
+      at[u] = i;
+      if (!run) {
+        const int r = i / words, h = r % p.kv_heads, t = r / p.kv_heads;
+        at[u] = (t * p.token_stride + h * p.head_stride) / 8 + i % words;
+      }
+      if (i < n) w[u] = __ldcs(s + at[u]);
     }
-    for (; i < n; i += kCopyThreads) d[i] = s[i];
-    return;
-  }
-  for (int i = threadIdx.x; i < n; i += kCopyThreads) {
-    const int w = i % words, r = i / words, h = r % p.kv_heads, t = r / p.kv_heads;
-    const int64_t at = (t * p.token_stride + h * p.head_stride) / 8 + w;
-    d[at] = s[at];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + 32 * u < n) __stcs(d + at[u], w[u]);
   }
 }
 
-// Copy (pair, layer, keys or values) number u of a list of page pairs.
-__device__ __forceinline__ void copy_unit(const Pool& p, int64_t src, int64_t dst, int slice, int tok) {
-  const int layer = slice >> 1;
-  copy_page(p, ((slice & 1) ? p.v : p.k) + 2 * layer * p.layer_stride, src, dst, tok);
+// Whole pages src(i) -> dst(i), all layers, by all warps of the grid.
+template <typename Pair>
+__device__ __forceinline__ void copy_pages(const Pool& p, int64_t n, Pair pair) {
+  const int lane = threadIdx.x & 31, slices = 2 * p.num_layers, parts = copy_parts(p, p.page_size);
+  const int64_t total = n * slices * parts, step = (int64_t)gridDim.x * kCopyWarps;
+  for (int64_t u = (int64_t)blockIdx.x * kCopyWarps + (threadIdx.x >> 5); u < total; u += step) {
+    const int64_t i = u / (slices * parts);
+    const int rest = (int)(u % (slices * parts));
+    int64_t s, d;
+    if (pair(i, &s, &d)) copy_part(p, s, d, rest / parts, p.page_size, rest % parts, lane);
+  }
 }
 
 __global__ void __launch_bounds__(kCopyThreads) k_page_copy(Pool p, const int32_t* src, const int32_t* dst, int n,
                                                             int32_t* status) {
   chain();
-  const int slices = 2 * p.num_layers;
-  const int64_t total = (int64_t)n * slices;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    const int i = (int)(u / slices), slice = (int)(u % slices);
-    const int64_t s = src[i], d = dst[i];
-    if (s < 0 || s >= p.num_pages || d < 0 || d >= p.num_pages) {
-      if (threadIdx.x == 0) set_error(status, PS_ERR_INVALID_ARG);
-      continue;
-    }
-    copy_unit(p, s, d, slice, p.page_size);
-  }
+  copy_pages(p, n, [&](int64_t i, int64_t* s, int64_t* d) {
+    *s = src[i];
+    *d = dst[i];
+    const bool ok = *s >= 0 && *s < p.num_pages && *d >= 0 && *d < p.num_pages;
+    if (!ok && (threadIdx.x & 31) == 0) set_error(status, PS_ERR_INVALID_ARG);
+    return ok;
+  });
 }
 
 // ---- scans ----------------------------------------------------------------------
@@ -95,6 +108,41 @@ __device__ __forceinline__ int scan_array(const int32_t* in, int32_t* out, int n
     carry += tot;
   }
   return carry;
+}
+// Ranks of flagged elements in a tile of kTile: thread t holds the flags of
+// elements u kScanThreads + t, u = 0..kEach-1, and gets the flagged elements
+// before each; *total of the tile.  One pass over the tile's loads.
+constexpr int kEach = 8, kTile = kEach * kScanThreads;
+__device__ __forceinline__ void tile_ranks(const bool (&flag)[kEach], int (&rank)[kEach], int* total) {
+  constexpr int kWarps = kScanThreads / 32;
+  __shared__ int count[kEach * kWarps + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const unsigned m = __ballot_sync(0xFFFFFFFFu, flag[u]);
+    rank[u] = __popc(m & ((1u << lane) - 1));
+    if (lane == 0) count[u * kWarps + warp] = __popc(m);
+  }
+  __syncthreads();
+  if (warp == 0) {  // exclusive sums of the 64 counts, two a lane
+    static_assert(kEach * kWarps == 64, "two counts a lane");
+    const int a = count[2 * lane], b = count[2 * lane + 1];
+    int incl = a + b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    __syncwarp();
+    count[2 * lane] = incl - a - b;
+    count[2 * lane + 1] = incl - b;
+    if (lane == 31) count[64] = incl;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) rank[u] += count[u * kWarps + warp];
+  *total = count[64];
 }
 // True in every thread of the last CTA of the grid to come here; what the other
 // CTAs wrote before is then visible.  The count returns to 0 for the next call.
@@ -155,16 +203,22 @@ __global__ void __launch_bounds__(kScanThreads) k_fork_scan(Pool p, PageScratch 
     const int64_t c0 = (int64_t)blockIdx.x * w.chunk_size;
     const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
     int count = 0;
-    for (int64_t i0 = c0; i0 < c1; i0 += kScanThreads) {
-      const int64_t i = i0 + threadIdx.x;
-      int r = 1;
-      if (i < c1) {
-        r = a.refs_in[i];
-        if (a.refs_out != a.refs_in) a.refs_out[i] = r;
+    for (int64_t i0 = c0; i0 < c1; i0 += kTile) {
+      int r[kEach], rank[kEach], tot;
+      bool free[kEach];
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int64_t i = i0 + u * kScanThreads + threadIdx.x;
+        r[u] = i < c1 ? a.refs_in[i] : 1;
+        free[u] = r[u] == 0;
       }
-      int tot;
-      const int e = block_scan(r == 0, &tot);
-      if (r == 0) w.list[c0 + count + e] = (int32_t)i;
+      tile_ranks(free, rank, &tot);
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int64_t i = i0 + u * kScanThreads + threadIdx.x;
+        if (i < c1 && a.refs_out != a.refs_in) a.refs_out[i] = r[u];
+        if (free[u]) w.list[c0 + count + rank[u]] = (int32_t)i;
+      }
       count += tot;
     }
     if (threadIdx.x == 0) w.chunk_cnt[blockIdx.x] = count;
@@ -216,21 +270,24 @@ __global__ void __launch_bounds__(kScanThreads) k_fork_scan(Pool p, PageScratch 
   }
 }
 
-// The free page of rank r (ascending ids), as an index into the reference array.
-__device__ __forceinline__ int free_page(const PageScratch& w, int r) {
+// The free page of rank r (ascending ids), as an index into the reference array;
+// base: the free pages before each chunk.
+__device__ __forceinline__ int free_page(const PageScratch& w, const int* base, int r) {
   int lo = 0, hi = w.chunks - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
-    if (w.chunk_base[mid] <= r) lo = mid;
+    if (base[mid] <= r) lo = mid;
     else hi = mid - 1;
   }
-  return w.list[(int64_t)lo * w.chunk_size + (r - w.chunk_base[lo])];
+  return w.list[(int64_t)lo * w.chunk_size + (r - base[lo])];
 }
 
 // blockIdx.x: the item; blockIdx.y: a slice of the layers' keys and values.
 // Slice 0 also writes the child's row and the references.
 __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch w, ForkArgs a) {
+  __shared__ int base[kMaxChunks];
   chain();
+  for (int c = threadIdx.x; c < w.chunks; c += kCopyThreads) base[c] = w.chunk_base[c];
   if (w.hdr->status != PS_OK) return;
   const int i = blockIdx.x;
   const int pr = a.parents[i], ch = a.children[i];
@@ -238,8 +295,8 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch
   int len = 0, full = 0, total = 0;
   fork_item(p, a, i, &len, &full, &total);
   const int start = w.start[i];
+  __syncthreads();  // (the row's lengths are read by every thread before they change, too)
   if (blockIdx.y == 0) {
-    __syncthreads();  // the row's lengths are read by every thread before they change
     const int32_t* src = a.tables + pr * a.table_stride;
     int32_t* row = a.tables + ch * a.table_stride;
     for (int k = threadIdx.x; k < total; k += kCopyThreads) {
@@ -249,7 +306,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch
         row[k] = id;
         if (id >= p.first_page) atomicAdd(a.refs_out + (id - p.first_page), 1);
       } else {
-        const int f = free_page(w, start + (k - full));
+        const int f = free_page(w, base, start + (k - full));
         row[k] = (int32_t)(p.first_page + f);
         a.refs_out[f] = 1;
       }
@@ -261,8 +318,10 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch
   }
   const int part = len & (p.page_size - 1);
   if (pr < 0 || pr == ch || part == 0) return;
-  const int64_t from = a.tables[pr * a.table_stride + full], to = p.first_page + free_page(w, start);
-  for (int s = blockIdx.y; s < 2 * p.num_layers; s += gridDim.y) copy_unit(p, from, to, s, part);
+  const int64_t from = a.tables[pr * a.table_stride + full], to = p.first_page + free_page(w, base, start);
+  const int parts = copy_parts(p, part), n = 2 * p.num_layers * parts;
+  for (int u = blockIdx.y * kCopyWarps + (threadIdx.x >> 5); u < n; u += gridDim.y * kCopyWarps)
+    copy_part(p, from, to, u / parts, part, u % parts, threadIdx.x & 31);
 }
 
 // ---- release ----------------------------------------------------------------------
@@ -308,6 +367,7 @@ __global__ void __launch_bounds__(kScanThreads) k_compact_count(Pool p, PageScra
   const int64_t c0 = (int64_t)blockIdx.x * w.chunk_size;
   const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
   int count = 0;
+#pragma unroll 8
   for (int64_t i = c0 + threadIdx.x; i < c1; i += kScanThreads) count += refs[i] > 0;
   int tot;
   block_scan(count, &tot);
@@ -325,31 +385,41 @@ __global__ void __launch_bounds__(kScanThreads) k_compact_lists(Pool p, PageScra
   const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
   const int live = w.hdr->live;
   int before = w.chunk_base[blockIdx.x];
-  for (int64_t i0 = c0; i0 < c1; i0 += kScanThreads) {
-    const int64_t i = i0 + threadIdx.x;
-    const int r = i < c1 ? refs[i] : 0;
-    int tot;
-    const int b = before + block_scan(r > 0, &tot);
-    before += tot;
-    if (i >= c1) continue;
-    if (i < live) {
-      if (r > 0) {
-        if (refs_out != refs) refs_out[i] = r;
-      } else {
-        w.list[i - b] = (int32_t)i;  // its count comes with the mover's
-      }
-    } else {
-      if (r > 0) {
-        const int m = live - 1 - b;
-        w.movers[m] = (int32_t)i;
-        w.mover_refs[m] = r;
-        w.inv[i] = m;
-      } else {
-        w.inv[i] = -1;
-      }
-      refs_out[i] = 0;
-      if (i == live) w.hdr->free_pages = live - b;  // movers: the pages in use from here on
+  for (int64_t i0 = c0; i0 < c1; i0 += kTile) {
+    int ref[kEach], rank[kEach], tot;
+    bool used[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t i = i0 + u * kScanThreads + threadIdx.x;
+      ref[u] = i < c1 ? refs[i] : 0;
+      used[u] = ref[u] > 0;
     }
+    tile_ranks(used, rank, &tot);
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t i = i0 + u * kScanThreads + threadIdx.x;
+      const int r = ref[u], b = before + rank[u];
+      if (i >= c1) continue;
+      if (i < live) {
+        if (r > 0) {
+          if (refs_out != refs) refs_out[i] = r;
+        } else {
+          w.list[i - b] = (int32_t)i;  // its count comes with the mover's
+        }
+      } else {
+        if (r > 0) {
+          const int m = live - 1 - b;
+          w.movers[m] = (int32_t)i;
+          w.mover_refs[m] = r;
+          w.inv[i] = m;
+        } else {
+          w.inv[i] = -1;
+        }
+        refs_out[i] = 0;
+        if (i == live) w.hdr->free_pages = live - b;  // movers: the pages in use from here on
+      }
+    }
+    before += tot;
   }
   // every page in use lies below 'live' if the array ends there: no movers
   if (blockIdx.x == 0 && threadIdx.x == 0 && live == np) w.hdr->free_pages = 0;
@@ -383,19 +453,18 @@ __global__ void __launch_bounds__(kCopyThreads) k_compact_move(Pool p, PageScrat
       tables_out[r * rows.table_stride + k] = (int32_t)id;
     }
   }
-  const int slices = 2 * p.num_layers;
-  const int64_t total = (int64_t)moved * slices;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    const int m = (int)(u / slices);
-    copy_unit(p, p.first_page + w.movers[m], p.first_page + w.list[m], (int)(u % slices), p.page_size);
-  }
+  copy_pages(p, moved, [&](int64_t m, int64_t* s, int64_t* d) {
+    *s = p.first_page + w.movers[m];
+    *d = p.first_page + w.list[m];
+    return true;
+  });
 }
 
 }  // namespace
 
 int32_t launch_copy(const Pool& p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* status, int nsm,
                     cudaStream_t st) {
-  const int64_t total = (int64_t)n * 2 * p.num_layers;
+  const int64_t warps = (int64_t)n * 2 * p.num_layers * copy_parts(p, p.page_size), total = (warps + kCopyWarps - 1) / kCopyWarps;
   const int grid = (int)(total < (int64_t)nsm * 8 ? total : (int64_t)nsm * 8);
   return status_of(launch(k_page_copy, dim3((unsigned)grid), kCopyThreads, 0, st, p, src, dst, n, status));
 }
@@ -411,9 +480,10 @@ int32_t launch_fork(const Pool& p, const PageScratch& w, int32_t n, const int32_
   cudaError_t e = launch(k_fork_scan, dim3((unsigned)(w.chunks + n)), kScanThreads, 0, st, p, w, a);
   if (e != cudaSuccess) return status_of(e);
   if (n == 0) return PS_OK;
-  // enough CTAs for a few waves, at most one for each layer's keys or values
+  // enough CTAs for a few waves, at most a warp for each part of the copies
+  const int most = (2 * p.num_layers * copy_parts(p, p.page_size) + kCopyWarps - 1) / kCopyWarps;
   int ny = 8 * nsm / n;
-  ny = ny < 1 ? 1 : (ny > 2 * p.num_layers ? 2 * p.num_layers : ny);
+  ny = ny < 1 ? 1 : (ny > most ? most : ny);
   return status_of(launch(k_fork_apply, dim3((unsigned)n, (unsigned)ny), kCopyThreads, 0, st, p, w, a));
 }
 
