@@ -129,28 +129,40 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
       const int token = (lkey + mykey) & (a.pool.page_size - 1);
       const uint32_t dst = ring + lstage * 2 * S::kBlock;
       if (tma) {
-        // boxes with a key in them: none of a tile without keys
-        const int there = lkey >= lkv1 ? 0 : (boxes == 2 && lkey + 8 < lkv1 ? 2 : 1);
-#pragma unroll 1
-        for (int box = 0; box < there; ++box) {
-          const int id = __shfl_sync(0xFFFFFFFFu, page, box), tok = __shfl_sync(0xFFFFFFFFu, token, box);
+        uint64_t* bar = &landed[lstage];
+        if (lkey >= lkv1) {
+          // a tile without keys
+        } else if (boxes == 1) {  // every lane has the one page
           if (elect()) {
-            uint64_t* bar = &landed[lstage];
-            if (box == 0) bar_expect(bar, boxes == 1 ? 2 * S::kBlock : there * S::kBlock);
-            const uint32_t d = dst + box * (8 * 128);
-            // one box's 16 tokens by 64 elements lie side by side where there is one box
-            if (maps.whole && boxes == 1) {
-              tma_load_whole(d, &maps.whole_k, bar, lp.head, tok, id);
-              tma_load_whole(d + S::kBlock, &maps.whole_v, bar, lp.head, tok, id);
+            bar_expect(bar, 2 * S::kBlock);
+            if (maps.whole) {
+              tma_load_whole(dst, &maps.whole_k, bar, lp.head, token, page);
+              tma_load_whole(dst + S::kBlock, &maps.whole_v, bar, lp.head, token, page);
             } else {
 #pragma unroll
               for (int half = 0; half < S::kHalves; ++half) {
-                tma_load(d + half * (16 * 128), &maps.k, bar, half * 64, lp.head, tok, id);
-                tma_load(d + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, tok, id);
+                tma_load(dst + half * (16 * 128), &maps.k, bar, half * 64, lp.head, token, page);
+                tma_load(dst + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, token, page);
               }
             }
           }
           __syncwarp();
+        } else {  // two pages of 8 tokens, the second only if it has a key
+          const int there = lkey + 8 < lkv1 ? 2 : 1;
+#pragma unroll 1
+          for (int box = 0; box < there; ++box) {
+            const int id = __shfl_sync(0xFFFFFFFFu, page, box);
+            if (elect()) {
+              if (box == 0) bar_expect(bar, there * S::kBlock);
+              const uint32_t d = dst + box * (8 * 128);
+#pragma unroll
+              for (int half = 0; half < S::kHalves; ++half) {
+                tma_load(d + half * (16 * 128), &maps.k, bar, half * 64, lp.head, 0, id);
+                tma_load(d + S::kBlock + half * (16 * 128), &maps.v, bar, half * 64, lp.head, 0, id);
+              }
+            }
+            __syncwarp();
+          }
         }
       } else {
         int64_t off = -1;
