@@ -83,7 +83,7 @@ struct __align__(16) JoinRec {
 struct __align__(16) PlanHdr {
   int32_t status;           // PS_OK, or why the plan is empty
   int32_t joins[kLists];    // entries of joins[]
-  int32_t pad0;
+  int32_t mend;             // some byte of mend[] is set
   int32_t ntiles[kLists];
   int32_t workers[kLists];  // C, 0 without tiles
   int32_t narrow_ctas;      // CTAs that the narrow tiles' workers are spread over
@@ -125,6 +125,7 @@ struct Plan {
   int64_t* ucum[kLists];      // [tiles + 1] cost before a tile, all heads
   int32_t* first_tile[kLists];  // [C] tile of a worker's first place
   JoinRec* joins[kLists];     // [tiles of requests x kv heads]
+  uint8_t* mend[kLists];      // [tiles x kv heads] an output written by its tile is not finite, see mend_row
   float4* part_o[kLists];     // unnormalized outputs of the rows, see part_row and part_word
   float2* part_ml[kLists];    // [rows] (maximum, sum), base 2
   int32_t max_workers[kLists];

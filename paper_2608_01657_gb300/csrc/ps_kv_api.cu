@@ -110,6 +110,7 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
     p.ucum[l] = cv.take<int64_t>((size_t)b.tiles + 1);
     p.first_tile[l] = cv.take<int32_t>((size_t)workers[l]);
     p.joins[l] = cv.take<JoinRec>((size_t)b.own_tiles * c.num_kv_heads);
+    p.mend[l] = cv.take<uint8_t>((size_t)b.tiles * c.num_kv_heads);
     p.part_o[l] = cv.take<float4>((part_rows + 7) / 8 * 8 * (c.head_dim / 4));
     p.part_ml[l] = cv.take<float2>(part_rows);
   }

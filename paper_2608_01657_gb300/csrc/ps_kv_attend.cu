@@ -334,6 +334,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
             const int hq = head * a.pool.ratio + rr % a.pool.ratio;
             const float inv = l[hf] > 0 ? 1.0f / l[hf] : (l[hf] == 0 ? 0.0f : l[hf]);
             char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
+            float z = 0;
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) z = spoil(spoil(z, o[i][2 * hf]), o[i][2 * hf + 1]);
+            if (a.causal && z != 0) ask_mend(a, 0, ps.tile, head);
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i)
               if (i * 8 < a.pool.head_dim)
@@ -377,6 +381,100 @@ struct JoinShared {
   float4 o[3][kJoinWords][32];
   float2 ml[3][32];
 };
+
+// Numbers that are not finite among the values of tokens that a row does not
+// see.  The matrix products give those tokens the weight 0, and 0 times infinity
+// is NaN: only the last tokens of a tile are hidden from some of its rows, so
+// only a prompt's rows can be spoilt, and only elements that are not finite in
+// the result.  Those of a row whose hidden values have such a number there, and
+// whose own token's value is not NaN itself, are computed again by a warp over the keys that
+// the row sees alone: a lane a key for the scores, a lane four elements for the
+// sum.  None of it runs on finite data.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint2 x) {
+  const float2 a = Num<T>::unpack(x.x), b = Num<T>::unpack(x.y);
+  return (spoil(0, a.x) != 0 ? 1u : 0u) | (spoil(0, a.y) != 0 ? 2u : 0u) | (spoil(0, b.x) != 0 ? 4u : 0u) |
+         (spoil(0, b.y) != 0 ? 8u : 0u);
+}
+template <typename T>
+__device__ __noinline__ void mend_row(const AttendArgs& a, int tok0, int row, int head, int lane) {
+  const Pool& p = a.pool;
+  const int tok = tok0 + row / p.ratio, hq = head * p.ratio + row % p.ratio;
+  const int req = a.plan.tok_req[tok], q0 = a.q_offsets[req], len = a.kv_lens[req];
+  const int seen = max(len - (a.q_offsets[req + 1] - q0) + tok - q0 + 1, 0);
+  const bool mine = 4 * lane < p.head_dim;
+  uint2* op = reinterpret_cast<uint2*>(a.out + 2 * (tok * a.out_stride[0] + hq * a.out_stride[1])) + lane;
+  auto at = [&](int key) {  // element 0 of a key of this head
+    const int64_t page = a.tables[req * a.table_stride + (key >> p.page_log2)];
+    return 2 * (page * p.page_stride + (key & (p.page_size - 1)) * p.token_stride + head * p.head_stride);
+  };
+  auto value = [&](int key) { return mine ? *reinterpret_cast<const uint2*>(a.v + at(key) + 8 * lane) : make_uint2(0, 0); };
+  __syncwarp();
+  const uint2 was = mine ? __ldcg(op) : make_uint2(0, 0);
+  uint32_t redo = not_finite<T>(was), hidden = 0;
+  if (seen > 0) {
+    const uint2 own = value(seen - 1);
+    const float2 x = Num<T>::unpack(own.x), y = Num<T>::unpack(own.y);
+    redo &= (x.x == x.x ? 1u : 0u) | (x.y == x.y ? 2u : 0u) | (y.x == y.x ? 4u : 0u) | (y.y == y.y ? 8u : 0u);
+  }
+  if (!__any_sync(0xFFFFFFFFu, redo)) return;
+  for (int k = seen; k < min(len, seen + tile_rows(1)); ++k) hidden |= not_finite<T>(value(k));
+  redo &= hidden;
+  if (!__any_sync(0xFFFFFFFFu, redo)) return;
+  const char* qp = a.q + 2 * (tok * a.q_stride[0] + hq * a.q_stride[1]);
+  float m = -INFINITY, l = 0;
+  float4 o = make_float4(0, 0, 0, 0);
+  for (int k0 = 0; k0 < seen; k0 += 32) {
+    float t = -INFINITY;
+    if (k0 + lane < seen) {
+      const char* kp = a.k + at(k0 + lane);
+      float dot = 0;
+      for (int e = 0; e < p.head_dim; e += 2) {
+        const float2 x = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(qp + 2 * e));
+        const float2 y = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(kp + 2 * e));
+        dot = fmaf(x.y, y.y, fmaf(x.x, y.x, dot));
+      }
+      t = dot * a.scale2;
+    }
+    float mn = t;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, x));
+    mn = fmaxf(mn, m);
+    const float ref = mn == -INFINITY ? 0.0f : mn, f = ex2(m - ref), w = ex2(t - ref);
+    m = mn;
+    l = l * f + w;  // the lane's own keys
+    o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+    for (int j = 0; j < min(32, seen - k0); ++j) {
+      const float wj = __shfl_sync(0xFFFFFFFFu, w, j);
+      const uint2 v = value(k0 + j);
+      const float2 lo = Num<T>::unpack(v.x), hi = Num<T>::unpack(v.y);
+      o.x = fmaf(wj, lo.x, o.x);
+      o.y = fmaf(wj, lo.y, o.y);
+      o.z = fmaf(wj, hi.x, o.z);
+      o.w = fmaf(wj, hi.y, o.w);
+    }
+  }
+#pragma unroll
+  for (int x = 1; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+  const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+  const uint32_t lo = Num<T>::pack(o.x * inv, o.y * inv), hi = Num<T>::pack(o.z * inv, o.w * inv);
+  const uint32_t keep_lo = (redo & 1 ? 0u : 0xFFFFu) | (redo & 2 ? 0u : 0xFFFF0000u);
+  const uint32_t keep_hi = (redo & 4 ? 0u : 0xFFFFu) | (redo & 8 ? 0u : 0xFFFF0000u);
+  if (redo) *op = make_uint2((was.x & keep_lo) | (lo & ~keep_lo), (was.y & keep_hi) | (hi & ~keep_hi));
+}
+// The rows of the tiles that asked for it.
+template <typename T, int LIST>
+__device__ __forceinline__ void mend_tiles(const AttendArgs& a, int64_t warp, int64_t warps, int lane) {
+  constexpr int W = tile_rows(LIST) / 8;  // eight rows at a time
+  const int64_t n = (int64_t)a.plan.hdr->ntiles[LIST] * a.pool.kv_heads;
+  for (int64_t i = warp; i < n * W; i += warps) {
+    if (!__ldcg(a.plan.mend[LIST] + i / W)) continue;
+    const Tile& t = a.plan.tiles[LIST][i / W / a.pool.kv_heads];
+    const int r0 = (int)(i % W) * 8;
+    for (int r = r0; r < min(t.nrows, r0 + 8); ++r) mend_row<T>(a, t.tok0, t.row0 + r, (int)(i / W % a.pool.kv_heads), lane);
+  }
+}
+
 template <typename T, int H, int SPLIT>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, int list, int entries, int64_t item0,
                                           int64_t step, int sub, int lane) {
@@ -447,25 +545,32 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, i
         take(sh->ml[x][lane].x, sh->ml[x][lane].y, v);
       }
     }
-    if (!in) continue;
     const int rr = row0 + r;
     const int64_t tok = tok0 + rr / a.pool.ratio;
     const int hq = head * a.pool.ratio + rr % a.pool.ratio;
-    const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-    char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
+    float z = 0;
+    if (in) {
+      const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+      char* op = a.out + 2 * (tok * a.out_stride[0] + (int64_t)hq * a.out_stride[1]);
 #pragma unroll
-    for (int i = 0; i < NW; ++i)
-      if (c0 + 4 * i < words)
-        *reinterpret_cast<uint2*>(op + 8 * (c0 + 4 * i)) =
-            make_uint2(Num<T>::pack(o[i].x * inv, o[i].y * inv), Num<T>::pack(o[i].z * inv, o[i].w * inv));
-    if (a.lse && c0 == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
+      for (int i = 0; i < NW; ++i)
+        if (c0 + 4 * i < words) {
+          z = spoil(spoil(spoil(spoil(z, o[i].x), o[i].y), o[i].z), o[i].w);
+          *reinterpret_cast<uint2*>(op + 8 * (c0 + 4 * i)) =
+              make_uint2(Num<T>::pack(o[i].x * inv, o[i].y * inv), Num<T>::pack(o[i].z * inv, o[i].w * inv));
+        }
+      if (a.lse && c0 == 0) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
+    }
+    if (!a.causal) continue;
+    for (uint32_t spoilt = __reduce_or_sync(0xFFFFFFFFu, z != 0 ? 1u << (lane & 7) : 0u); spoilt; spoilt &= spoilt - 1)
+      mend_row<T>(a, tok0, row0 + (int)(it % W) * 8 + __ffs(spoilt) - 1, head, lane);
   }
 }
 template <typename T>
 __global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
   __shared__ JoinShared sh;
   chain();
-  const int4 h = __ldg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries
+  const int4 h = __ldcg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries, mend
   if (h.x != PS_OK) return;
   const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
   if ((int64_t)h.y * (tile_rows(0) / 8) + (int64_t)h.z * (tile_rows(1) / 8) <= 2 * (int64_t)gridDim.x) {
@@ -475,6 +580,10 @@ __global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
     const int64_t warp = (int64_t)blockIdx.x * 4 + sub, warps = (int64_t)gridDim.x * 4;
     join_rows<T, tile_rows(0), 1>(a, &sh, 0, h.y, warp, warps, 0, lane);
     join_rows<T, tile_rows(1), 1>(a, &sh, 1, h.z, warp, warps, 0, lane);
+  }
+  if (h.w) {
+    mend_tiles<T, 0>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
+    mend_tiles<T, 1>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
   }
 }
 
@@ -529,6 +638,8 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   a.tables = b.tables;
   a.table_stride = b.table_stride;
   a.q_offsets = b.q_offsets;
+  a.kv_lens = b.kv_lens;
+  a.causal = b.causal;
   a.status = status;
   a.scale2 = in.scale * 1.4426950408889634f;
   // no tile has more rows than the whole batch

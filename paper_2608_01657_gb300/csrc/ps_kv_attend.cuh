@@ -17,9 +17,10 @@ struct AttendArgs {
   int64_t q_stride[2], out_stride[2];
   const int32_t* tables;
   int64_t table_stride;
-  const int32_t* q_offsets;
+  const int32_t *q_offsets, *kv_lens;
   int32_t* status;
   int32_t after_wide;  // the wide tiles' kernel was launched
+  int32_t causal;
   float scale2;  // scale log2(e)
 };
 
@@ -86,6 +87,14 @@ __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.asy
 // The log of a row's sum of exponentials, from its base-2 maximum and sum.
 __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0 ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// x is added to z as 0, or as NaN if it is not finite.
+__device__ __forceinline__ float spoil(float z, float x) { return fmaf(x, 0.0f, z); }
+// An output of (tile, head) is not finite: the join looks at its rows (mend_row).
+__device__ __forceinline__ void ask_mend(const AttendArgs& a, int list, int tile, int head) {
+  a.plan.mend[list][(int64_t)tile * a.pool.kv_heads + head] = 1;
+  a.plan.hdr->mend = 1;
 }
 
 // The wide tiles' kernel (ps_kv_attend_wide.cu).

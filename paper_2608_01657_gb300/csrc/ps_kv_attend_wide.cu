@@ -492,6 +492,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
     int64_t rows_at[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) rows_at[x] = __shfl_sync(0xFFFFFFFFu, out_at, (lane & ~3) + x);
+    float z = 0;
 #pragma unroll 1
     for (int j = 0; j < DP; j += 32) {
       uint32_t o[32];
@@ -510,6 +511,9 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         }
       }
       if (direct) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (j + e < a.pool.head_dim) z = spoil(z, x[e]);
         uint32_t w[4][4];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) w[e >> 3][(e >> 1) & 3] = Num<T>::pack(x[e] * inv, x[e + 1] * inv);
@@ -540,6 +544,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       }
     }
     if (in) {
+      if (a.causal && z != 0) ask_mend(a, 1, ps.tile, ps.head);
       if (!direct) a.plan.part_ml[1][prow] = make_float2(m, l);
       else if (a.lse) a.lse[tok * a.pool.q_heads + hq] = log_sum(m, l);
     }

@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(kReqThreads) k_plan_joins(Pool p, Plan plan, B
   const int n = (rows + H - 1) / H * p.kv_heads;
   for (int i = threadIdx.x; i < n; i += kReqThreads) {
     const int tile = rec.tile0 + i / p.kv_heads, head = i % p.kv_heads;
+    plan.mend[rec.list][(int64_t)tile * p.kv_heads + head] = 0;
     JoinRec j{};
     j.own = parts_of(plan, p, h, rec.list, tile, head);
     if (j.own.count == 0) continue;

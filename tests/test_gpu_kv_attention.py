@@ -302,3 +302,45 @@ def test_refusals():
         KV.KVPool(*make_pool(1, 8, 16, 2, 136, BF), num_q_heads=4)       # head size
     with pytest.raises(ValueError):
         KV.KVPool(*make_pool(1, 8, 12, 2, 64, BF), num_q_heads=4)        # page size
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new,kv,ratio,shared", [
+    ([3], [40], 4, 0), ([3, 1], [3000, 17], 4, 0),      # narrow tiles, whole and split
+    ([20], [70], 4, 0), ([20, 2], [5000, 30], 4, 0),    # wide tiles of one row block
+    ([60], [60], 4, 0), ([60], [4000], 4, 0), ([200, 7], [333, 7], 2, 0),  # of two, several
+    ([10], [4], 4, 0), ([70], [20], 4, 0),              # rows that see nothing
+    ([5, 4, 1], [270, 300, 257], 4, 256),               # after a shared prefix
+])
+def test_non_finite_values_of_later_tokens(new, kv, ratio, shared, dtype):
+    """What a causal row does not see does not reach it: NaN and infinities in later tokens' keys and values."""
+    from paper_2608_01657_gb300 import kv as KV
+    heads, dim, ps = 2, 72, 16
+    tables, pages, bounds = batch(new, kv, [shared], [0], ps, seed=len(new))
+    k, v = make_pool(1, pages, ps, heads, dim, dtype, "token", sum(kv))
+    r = np.random.RandomState(sum(new))
+    for i, n in enumerate(new):  # some of the new tokens
+        for j, pos in enumerate(r.permutation(np.arange(max(kv[i] - n, shared), kv[i]))[:3]):
+            page, at = int(tables[i, pos // ps]), int(pos % ps)
+            v[0, page, at, j % heads, int(r.randint(dim))] = [float("nan"), float("inf"), -float("inf")][j]
+            v[0, page, at, j % heads, 71] = float("inf")
+            if j == 0:
+                k[0, page, at, 1, 5] = float("inf")
+    qo = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(qo[-1])
+    g = torch.Generator("cuda").manual_seed(3)
+    q = torch.randn(T, heads * ratio, dim, generator=g, device="cuda").to(dtype)
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    pool = KV.KVPool(k, v, num_q_heads=heads * ratio, max_requests=len(new), max_tokens=T, max_row_pages=tables.shape[1])
+    pool.plan(dev(qo), dev(kv), dev(tables), T, group_offsets=dev(bounds) if shared else None)
+    lse = torch.empty(T, heads * ratio, device="cuda")
+    outs = [pool.attention(0, q, 0.1, lse=lse) for _ in range(3)]
+    pool.check()
+    for o in outs[1:]:
+        assert torch.equal(o.view(torch.int16), outs[0].view(torch.int16))
+    want, _, spread, size = attention(q, k[0], v[0], qo.tolist(), kv, dev(tables), 0.1, True)
+    finite = torch.isfinite(want)
+    assert not finite.all() and finite.any()
+    assert torch.equal(torch.isfinite(outs[0]), finite)
+    bound = attention_bound(want, spread, size, dtype, dim, max(kv), 8.0)
+    assert ((outs[0].double() - want).abs() <= bound)[finite].all()
