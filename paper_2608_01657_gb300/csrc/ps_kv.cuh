@@ -237,7 +237,8 @@ __device__ __forceinline__ void set_error(int32_t* status, int32_t code) {
   if (status) atomicMin(status, code);
 }
 // Wait for the kernels before this one, then let the next one be scheduled (its
-// CTAs wait here in turn).  Every kernel of these operators starts with it.
+// CTAs wait here in turn).  Every kernel of these operators starts with it, but
+// for the attention's, which read the plan first.
 __device__ __forceinline__ void chain() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

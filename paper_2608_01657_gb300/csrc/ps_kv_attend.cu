@@ -79,8 +79,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
   // this one's CTAs run as soon as there is room: every CTA of that kernel has
   // waited for the work before both by then.  Its end is waited for at this
   // one's end instead, so that the join after this kernel follows both.
-  if (!a.after_wide) chain();
-  else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // The plan and the tables are there before either wait: the kernel before this
+  // one has at least waited for the plan's tiles (see k_plan_joins).
+  if (a.after_wide) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PlanHdr* hdr = a.plan.hdr;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the first workers of all CTAs, then the second ones: few are spread over many SMs
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
     if (!tma) cp_commit();
     lstage = lstage + 1 == S::kStages ? 0 : lstage + 1;
   };
+  if (!a.after_wide) chain();
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) load_unit();
 
@@ -476,8 +478,8 @@ __device__ __forceinline__ void mend_tiles(const AttendArgs& a, int64_t warp, in
 }
 
 template <typename T, int H, int SPLIT>
-__device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, int list, int entries, int64_t item0,
-                                          int64_t step, int sub, int lane) {
+__device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, bool* waited, int list, int entries,
+                                          int64_t item0, int64_t step, int sub, int lane) {
   const int dim = a.pool.head_dim, words = dim >> 2;
   constexpr int W = H / 8, NW = kJoinWords;  // warps of an entry
   for (int64_t it = item0; it < (int64_t)entries * W; it += step) {
@@ -492,6 +494,8 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, i
     const int tok0 = field(12), row0 = field(13), head = field(15);
     const int plist = field(16), pofs = field(17), psplit = field(18);
     const bool in = r < nrows;
+    if (!*waited) chain();
+    *waited = true;
     float m = -INFINITY, l = 0;
     float4 o[NW];
 #pragma unroll
@@ -569,19 +573,24 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, i
 template <typename T>
 __global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
   __shared__ JoinShared sh;
-  chain();
-  const int4 h = __ldcg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries, mend
-  if (h.x != PS_OK) return;
+  // the entries are the plan's: they are read before the wait for the tiles' kernels
+  const int4 h = __ldcg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries
+  bool waited = false;
+  if (h.x != PS_OK) {
+    chain();
+    return;
+  }
   const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
   if ((int64_t)h.y * (tile_rows(0) / 8) + (int64_t)h.z * (tile_rows(1) / 8) <= 2 * (int64_t)gridDim.x) {
-    join_rows<T, tile_rows(0), 4>(a, &sh, 0, h.y, blockIdx.x, gridDim.x, sub, lane);
-    join_rows<T, tile_rows(1), 4>(a, &sh, 1, h.z, blockIdx.x, gridDim.x, sub, lane);
+    join_rows<T, tile_rows(0), 4>(a, &sh, &waited, 0, h.y, blockIdx.x, gridDim.x, sub, lane);
+    join_rows<T, tile_rows(1), 4>(a, &sh, &waited, 1, h.z, blockIdx.x, gridDim.x, sub, lane);
   } else {
     const int64_t warp = (int64_t)blockIdx.x * 4 + sub, warps = (int64_t)gridDim.x * 4;
-    join_rows<T, tile_rows(0), 1>(a, &sh, 0, h.y, warp, warps, 0, lane);
-    join_rows<T, tile_rows(1), 1>(a, &sh, 1, h.z, warp, warps, 0, lane);
+    join_rows<T, tile_rows(0), 1>(a, &sh, &waited, 0, h.y, warp, warps, 0, lane);
+    join_rows<T, tile_rows(1), 1>(a, &sh, &waited, 1, h.z, warp, warps, 0, lane);
   }
-  if (h.w) {
+  if (!waited) chain();
+  if (__ldcg(&a.plan.hdr->mend)) {
     mend_tiles<T, 0>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
     mend_tiles<T, 1>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
   }

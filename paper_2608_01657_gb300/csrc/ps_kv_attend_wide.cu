@@ -563,13 +563,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   using S = Shape<DP>;
   extern __shared__ char dyn[];
   __shared__ Shared sh;
-  chain();
+  // the plan is read before the wait, as in k_attend_narrow; the CTAs that have no
+  // part wait too, since the narrow tiles' kernel counts on it
   const PlanHdr* hdr = a.plan.hdr;
   const int C = hdr->workers[1], c = blockIdx.x;
-  if (c >= C) return;
   const int64_t U = hdr->cost[1];
   Parts<1> ps;
-  if (!ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) return;
+  if (c >= C || !ps.start(a.plan, a.pool.kv_heads, c, U * c / C, U * (c + 1) / C)) {
+    chain();
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t qs = (smem_addr(dyn) + 1023) & ~1023u, ring = qs + 2 * S::kBlock;
   if (warp == kSoftmaxWarps + kLoaderWarps) {
@@ -597,6 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
   __syncthreads();
   tc_after();
   const uint32_t tmem = sh.tmem;
+  chain();
   bool ok = true;
   if (warp < kSoftmaxWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));

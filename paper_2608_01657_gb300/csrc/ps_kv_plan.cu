@@ -324,7 +324,10 @@ __device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, cons
   return list ? parts_of<tile_rows(1)>(plan, p, h, 1, tile, head) : parts_of<tile_rows(0)>(plan, p, h, 0, tile, head);
 }
 
-// One CTA a request: the (tile, head)s whose rows have partial results.  Their
+// One CTA a request: the (tile, head)s whose rows have partial results (and the
+// bytes of mend[] cleared).  It lets the next kernel start only when the tiles
+// above are written, so that an attention kernel may read them before it waits.
+// Their
 // order is left to the counter: each is joined by itself.
 __global__ void __launch_bounds__(kReqThreads) k_plan_joins(Pool p, Plan plan, Batch b) {
   chain();
