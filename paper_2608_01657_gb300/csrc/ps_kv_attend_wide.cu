@@ -36,6 +36,7 @@ constexpr int UNIT = unit_keys(1), H = tile_rows(1);
 __device__ __forceinline__ constexpr uint32_t col_s(int t) { return 128u * t; }
 __device__ __forceinline__ constexpr uint32_t col_o(int t) { return 256u + 128u * t; }
 constexpr float kRescale = 8.0f;
+constexpr int kEarly = 64;  // keys of a unit whose weights are announced by themselves
 
 template <int DP>
 struct Shape {
@@ -47,7 +48,7 @@ struct Shape {
 };
 
 struct Shared {
-  uint64_t full[10], empty[10], s_full[2], p_full[2], o_full[2], q_full[2], q_empty[2], ml_full, ml_free, turn[2];
+  uint64_t full[10], empty[10], s_full[2], p_part[2], p_full[2], o_full[2], q_full[2], q_empty[2], ml_full, ml_free, turn[2];
   uint32_t tmem;
   float2 ml[128];  // split mode: group 1's (maximum, sum)
 };
@@ -321,17 +322,26 @@ __device__ __forceinline__ bool mma_role(const AttendArgs& a, Shared* sh, int t,
         next = next.ahead(1);
       }
       if (product) {
-        if (!warp_wait(&sh->p_full[t], p_phase)) return false;
-        p_phase ^= 1;
+        if (!warp_wait(&sh->p_part[t], p_phase)) return false;
       }
       if (!warp_wait(&sh->turn[t], turn)) return false;
       turn ^= 1;
+      const uint64_t v = v_desc + vb.slot * kBlk;
+      if (product) {
+        tc_after();
+        if (elect()) {
+#pragma unroll
+          for (int s = 0; s < kEarly / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
+        }
+        __syncwarp();
+        if (!warp_wait(&sh->p_full[t], p_phase)) return false;
+        p_phase ^= 1;
+      }
       tc_after();
       if (elect()) {
         if (product) {
-          const uint64_t v = v_desc + vb.slot * kBlk;
 #pragma unroll
-          for (int s = 0; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, i > 0 || s > 0);
+          for (int s = kEarly / 16; s < UNIT / 16; ++s) mma_ts(o_at, s_at + s * 8, v + s * (2048 >> 4), id_pv, true);
         }
         if (more_keys) {
           const uint64_t k = k_desc + kb.slot * kBlk;
@@ -443,12 +453,14 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
           p[x] = Num<T>::pack(e0, e1);
         }
         tm_store16(s_at + j / 2, p);
+        if (j + 32 == kEarly || j + 32 == UNIT) {
+          tm_wait_st();
+          if (j + 32 == kEarly && i == 0 && !let_go()) return false;
+          tc_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(j + 32 == kEarly ? &sh->p_part[t] : &sh->p_full[t]);
+        }
       }
-      tm_wait_st();
-      if (i == 0 && !let_go()) return false;
-      tc_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(&sh->p_full[t]);
       const float2 total = unpack2(add2(sum[0], sum[1]));
       l += total.x + total.y;
     }
@@ -586,6 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(const __grid_consta
     }
     for (int t = 0; t < 2; ++t) {
       bar_init(&sh.s_full[t], 1);
+      bar_init(&sh.p_part[t], 4);
       bar_init(&sh.p_full[t], 4);
       bar_init(&sh.o_full[t], 1);
       bar_init(&sh.turn[t], 1);
