@@ -420,7 +420,7 @@ __device__ __noinline__ void mend_row(const AttendArgs& a, int tok0, int row, in
     redo &= (x.x == x.x ? 1u : 0u) | (x.y == x.y ? 2u : 0u) | (y.x == y.x ? 4u : 0u) | (y.y == y.y ? 8u : 0u);
   }
   if (!__any_sync(0xFFFFFFFFu, redo)) return;
-  for (int k = seen; k < min(len, seen + tile_rows(1)); ++k) hidden |= not_finite<T>(value(k));
+  for (int k = seen; k < min(len, seen + tile_rows(1) + unit_keys(1)); ++k) hidden |= not_finite<T>(value(k));
   redo &= hidden;
   if (!__any_sync(0xFFFFFFFFu, redo)) return;
   const char* qp = a.q + 2 * (tok * a.q_stride[0] + hq * a.q_stride[1]);

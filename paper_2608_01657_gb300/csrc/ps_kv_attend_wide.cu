@@ -199,18 +199,22 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
   for (; more; more = ps.next()) {
     const Tile t = ps.t;
     const int32_t* row = a.tables + t.req * a.table_stride;
+    // A unit is read whole up to here: the keys that follow a causal tile's last
+    // one are the request's own, and weigh nothing (see mend_row for what is not
+    // finite among them).
+    const int end = t.ctx == kNoMask ? t.kv1 : a.kv_lens[t.req];
     // ids are looked up one unit ahead
     auto id_of = [&](int u) -> int {
       const int base = t.kv0 + (ps.unit + u) * UNIT;
-      const bool whole = tma && base + UNIT <= t.kv1;
+      const bool whole = tma && base + UNIT <= end;
       const int key = base + warp * 32 + (whole ? mybox * maps.box : lane);
-      return u < ps.count && key < t.kv1 ? __ldg(row + (key >> a.pool.page_log2)) : -1;
+      return u < ps.count && key < (whole ? end : t.kv1) ? __ldg(row + (key >> a.pool.page_log2)) : -1;
     };
     int page = id_of(0);
 #pragma unroll 1
     for (int u = 0; u < ps.count; ++u) {
       const int base = t.kv0 + (ps.unit + u) * UNIT;
-      const bool whole = tma && base + UNIT <= t.kv1;
+      const bool whole = tma && base + UNIT <= end;
       const int id = page;
       page = id_of(u + 1);
       const int key = base + warp * 32 + (whole ? mybox * maps.box : lane), token = key & (a.pool.page_size - 1);
@@ -252,6 +256,7 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
         copy_rows<DP>(dst, src, off, a.pool.head_dim);
         copied[copied[0] ? 1 : 0] = bar;
       }
+      told();
       if (u == 0) qb.next(is_pair(ps.t));
     }
   }
