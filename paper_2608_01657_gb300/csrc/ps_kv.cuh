@@ -148,10 +148,11 @@ __host__ __device__ __forceinline__ int64_t part_row(int sidx, int nrows, int he
 // all of a head's elements.
 struct PoolMaps {
   CUtensorMap k, v, whole_k, whole_v;
+  CUtensorMap q;  // a call's queries: (element, head of a group, group, token), a box of 64 elements of 128 rows
   int32_t ok;     // 0: pages of fewer than 8 tokens, or no maps
   int32_t whole;  // whole_k and whole_v are there
   int32_t box;    // tokens of a box: 8 or 16
-  int32_t pad0;
+  int32_t q_ok;   // q is there
 };
 bool make_maps(const Pool& p, int32_t layer, PoolMaps* m);
 

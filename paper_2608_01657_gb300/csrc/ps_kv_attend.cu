@@ -654,7 +654,12 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   // no tile has more rows than the whole batch
   const bool wide = list_of(b.num_tokens * p.ratio) == 1;
   a.after_wide = wide;
-  cudaError_t e = wide ? launch_wide(a, maps, st) : cudaSuccess;
+  cudaError_t e = cudaSuccess;
+  if (wide) {
+    PoolMaps with_q = maps;
+    make_query_map(p, in.q, in.q_stride, b.num_tokens, &with_q);
+    e = launch_wide(a, with_q, st);
+  }
   if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, maps, st) : narrow_t<__half>(a, maps, st);
   if (e != cudaSuccess) return status_of(e);
   // a CTA for every eight rows of narrow tiles, up to one full wave

@@ -100,5 +100,6 @@ __device__ __forceinline__ void ask_mend(const AttendArgs& a, int list, int tile
 // The wide tiles' kernel (ps_kv_attend_wide.cu).
 cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& maps, cudaStream_t st);
 cudaError_t configure_wide(const Pool& p);
+void make_query_map(const Pool& p, const void* q, const int64_t* stride, int32_t tokens, PoolMaps* m);
 
 }  // namespace pskv

@@ -234,6 +234,7 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
         const char* src = job == 0 ? a.k : (job == 1 ? a.v : a.q);
         uint32_t dst;
         int64_t off;
+        int qtok = 0;
         if (job < 2) {
           dst = ring + at.slot * S::kBlock;
           at = at.ahead(1);
@@ -248,9 +249,24 @@ __device__ __forceinline__ bool load_role(const AttendArgs& a, const PoolMaps& m
         } else {
           const int r = (job - 2) * 128 + warp * 32 + lane, rr = t.row0 + r;
           dst = qs + qblk * S::kBlock;
+          qtok = t.tok0 + (t.row0 + (job - 2) * 128) / a.pool.ratio;
           off = (int64_t)(t.tok0 + rr / a.pool.ratio) * a.q_stride[0] +
                 (int64_t)(ps.head * a.pool.ratio + rr % a.pool.ratio) * a.q_stride[1];
           if (r >= t.nrows) off = -1;
+        }
+        if (job >= 2 && maps.q_ok) {
+          if (warp == 0) {
+            if (elect()) {
+              bar_expect(bar, S::kBlock);
+#pragma unroll
+              for (int half = 0; half < S::kHalves; ++half)
+                tma_load(dst + half * (128 * 128), &maps.q, bar, half * 64, 0, ps.head, qtok);
+            }
+          } else if (lane == 0) {
+            bar_arrive(bar);
+          }
+          __syncwarp();
+          continue;
         }
         if (job != 3) told();
         copy_rows<DP>(dst, src, off, a.pool.head_dim);
@@ -665,38 +681,44 @@ cudaError_t launch_wide(const AttendArgs& a, const PoolMaps& m, cudaStream_t st)
   return a.pool.dtype == PS_KV_BF16 ? wide_t<__nv_bfloat16>(a, m, st) : wide_t<__half>(a, m, st);
 }
 
+namespace {
+struct Axis {
+  int64_t size, stride;  // stride in elements
+  uint32_t box;
+};
+bool encode_map(CUtensorMap* map, int32_t dtype, const void* base, const Axis* axes, int n) {
+  static const auto encode = []() -> decltype(&cuTensorMapEncodeTiled) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      return nullptr;
+    return reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
+  }();
+  if (!encode) return false;
+  cuuint64_t dims[5], bytes[5];
+  cuuint32_t box[5], step[5];
+  for (int i = 0; i < n; ++i) {
+    dims[i] = (cuuint64_t)axes[i].size;
+    box[i] = axes[i].box;
+    step[i] = 1;
+    if (i == 0) continue;
+    // an axis of one place is never stepped over: any stride will do
+    bytes[i - 1] = axes[i].size > 1 ? 2 * (cuuint64_t)axes[i].stride : 16;
+    if (bytes[i - 1] == 0 || bytes[i - 1] >= (1ull << 40)) return false;
+  }
+  return encode(map, dtype == PS_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)n,
+                const_cast<void*>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace
+
 bool make_maps(const Pool& p, int32_t layer, PoolMaps* m) {
-  m->ok = m->whole = 0;
+  m->ok = m->whole = m->q_ok = 0;
   m->box = p.page_size < 16 ? p.page_size : 16;
   if (p.page_size < 8) return false;
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-      found != cudaDriverEntryPointSuccess || !fn)
-    return false;
-  const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
-  const CUtensorMapDataType type = p.dtype == PS_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   const int parts = p.head_dim / 64;
-  struct Axis {
-    int64_t size, stride;  // stride in elements
-    uint32_t box;
-  };
-  auto make = [&](CUtensorMap* map, void* base, const Axis* axes, int n) {
-    cuuint64_t dims[5], bytes[5];
-    cuuint32_t box[5], step[5];
-    for (int i = 0; i < n; ++i) {
-      dims[i] = (cuuint64_t)axes[i].size;
-      box[i] = axes[i].box;
-      step[i] = 1;
-      if (i == 0) continue;
-      // an axis of one place is never stepped over: any stride will do
-      bytes[i - 1] = axes[i].size > 1 ? 2 * (cuuint64_t)axes[i].stride : 16;
-      if (bytes[i - 1] == 0 || bytes[i - 1] >= (1ull << 40)) return false;
-    }
-    return encode(map, type, (cuuint32_t)n, base, dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-  };
+  auto make = [&](CUtensorMap* map, void* base, const Axis* axes, int n) { return encode_map(map, p.dtype, base, axes, n); };
   const uint32_t tokens = (uint32_t)m->box;
   const Axis head = {p.kv_heads, p.head_stride, 1}, page = {p.num_pages, p.page_stride, 1},
              token = {p.page_size, p.token_stride, tokens};
@@ -706,6 +728,14 @@ bool make_maps(const Pool& p, int32_t layer, PoolMaps* m) {
   m->ok = make(&m->k, k, plain, 4) && make(&m->v, v, plain, 4);
   m->whole = m->ok && p.head_dim == 64 * parts && make(&m->whole_k, k, whole, 5) && make(&m->whole_v, v, whole, 5);
   return m->ok != 0;
+}
+// The queries' map, where a block of 128 rows is whole tokens.
+void make_query_map(const Pool& p, const void* q, const int64_t* stride, int32_t tokens, PoolMaps* m) {
+  m->q_ok = 0;
+  if (p.ratio > 128 || 128 % p.ratio != 0) return;
+  const Axis axes[4] = {{p.head_dim, 1, 64}, {p.ratio, stride[1], (uint32_t)p.ratio}, {p.kv_heads, p.ratio * stride[1], 1},
+                        {tokens, stride[0], (uint32_t)(128 / p.ratio)}};
+  m->q_ok = encode_map(&m->q, p.dtype, q, axes, 4);
 }
 cudaError_t configure_wide(const Pool& p) {
   return p.dtype == PS_KV_BF16 ? configure_t<__nv_bfloat16>(p.head_dim) : configure_t<__half>(p.head_dim);
