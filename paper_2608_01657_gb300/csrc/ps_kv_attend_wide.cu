@@ -546,7 +546,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       if (direct) {
 #pragma unroll
         for (int e = 0; e < 32; ++e)
-          if (j + e < a.pool.head_dim) z = spoil(z, x[e]);
+          z = spoil(z, x[e]);
         uint32_t w[4][4];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) w[e >> 3][(e >> 1) & 3] = Num<T>::pack(x[e] * inv, x[e + 1] * inv);

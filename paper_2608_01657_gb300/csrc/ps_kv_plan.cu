@@ -16,7 +16,7 @@ constexpr int kShareTokens = 128;
 // SMs at the narrow tiles' memory traffic), a narrow one in its warp (16 keys of
 // 128 elements) when loads wait on latency alone, and when all warps share the
 // HBM bandwidth.
-constexpr double kWideCycles = 5700, kNarrowCycles = 2400, kNarrowBandwidth = 3000;
+constexpr double kWideCycles = 5250, kNarrowCycles = 2400, kNarrowBandwidth = 2400;
 // A narrow worker has at least so many units: more workers would cost the join
 // more than they save.
 constexpr int kLeastUnits = 2;
