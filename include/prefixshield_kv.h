@@ -131,7 +131,8 @@ int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_appen
  * kv_lens[i] tokens, whose keys and values lie in the pages tables[i *
  * table_stride ...].  Causal: token j of the n new ones sees the keys before
  * position kv_len - n + j + 1; else every query sees all kv_len keys.  A query
- * that sees no key gives 0 (and -infinity in lse).
+ * that sees no key gives 0 (and -infinity in lse).  What a query does not see
+ * does not reach it, infinities and NaN included.
  * group_offsets (NULL: no sharing) divides the requests into num_groups runs
  * [group_offsets[g], group_offsets[g+1]) of neighbours that may share a
  * prefix: how many leading pages all of them have in common is found from the

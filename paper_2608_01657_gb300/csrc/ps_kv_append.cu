@@ -78,6 +78,11 @@ __device__ __forceinline__ void write_part(char* p, const Part<E>& r) {
   else *reinterpret_cast<uint2*>(p) = make_uint2(r.x[0], r.x[1]);
 }
 
+// 8191 bf16 tokens, 32 + 2 x 8 heads of 128, both norms, all rotated: 36 us, 5.7
+// TB/s of the 6.8 that copies reach, with the issue slots at 69 % (283
+// instructions a slice of four heads).  Loads into registers, one slice ahead:
+// 50 us; 8-byte parts, two heads' loads together and 48 warps an SM: 44 us.
+// Six CTAs an SM spill registers (47 us), three or six stages change nothing.
 constexpr int kThreads = 128;
 constexpr int kCtasPerSm = 5;
 constexpr int kStages = 4;  // slices of a warp in flight or at work
@@ -289,7 +294,8 @@ cudaError_t launch_g(const AppendArgs& a, int nsm, cudaStream_t st) {
   const int64_t want = (units + W - 1) / W;
   return launch(k_append<T, E, G, I>, dim3((unsigned)(want < most ? want : most)), kThreads, 0, st, a);
 }
-// Parts of 8 elements (16 bytes) where the rotated half is whole times 8, else of 4.
+// Parts of 8 elements (16 bytes) where the rotated half is whole times 8, else of 4
+// (half the bytes an instruction: 8191 tokens took 44 us with parts of 4).
 template <typename T, bool I>
 cudaError_t launch_e(const AppendArgs& a, int nsm, cudaStream_t st) {
   if (a.rope_dim % 16 == 0) return a.dim <= 64 ? launch_g<T, 8, 4, I>(a, nsm, st) : launch_g<T, 8, 8, I>(a, nsm, st);

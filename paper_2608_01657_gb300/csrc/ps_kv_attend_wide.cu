@@ -5,12 +5,15 @@
 // its part of the list of units; a unit is 128 keys.  Its warps:
 //   8 softmax warps, two groups t of four, a thread a query row;
 //   4 loader warps, each with a quarter of every unit's keys and values: whole
-//     units by TMA, a box for 16 tokens of a page and 64 elements.  A
-//     request's last unit, whose values past its end must read as zero, queries,
-//     and pages of 2 or 4 tokens, whose boxes would not fill the 1024 bytes after
-//     which the swizzle repeats, go by 16-byte asynchronous copies instead, eight
-//     times the instructions and waited for by the copying threads: with them for
-//     all units the loader warps took 7400 cycles a unit, the products 2350;
+//     units by TMA, a box for 16 tokens of a page and 64 elements, and the
+//     queries, a box of 64 elements of 128 rows.  A
+//     request's last unit, whose values past its end must read as zero, queries
+//     of which 128 rows are not whole tokens, and pages of 2 or 4 tokens, whose
+//     boxes would not fill the 1024 bytes after which the swizzle repeats, go by
+//     16-byte asynchronous copies instead, eight times the instructions and
+//     waited for by the copying threads: with them for all units the loader
+//     warps took 7400 cycles a unit, and for queries alone 3400 a tile, in
+//     which the next tile's products waited;
 //   2 warps that issue the matrix instructions, one for each group (2 more idle).
 // A tile of more than 128 rows is two row blocks, one for each group, that use
 // every unit's keys and values (pair mode).  A tile of up to 128 rows is one
@@ -21,9 +24,20 @@
 // the first 64 with pairs of 16 bits) and outputs O_t (up to 128 columns).
 // S_t = Q K^T reads both operands from shared memory; O_t += P_t V takes P_t
 // from tensor memory.  While group t computes weights, the other group's
-// products run.  The maximum that the weights refer to moves only when a score
+// products run; the first half of its weights is multiplied while it computes
+// the second (prompts 324 -> 308 us).  The maximum that the weights refer to moves only when a score
 // passes it by 2^8: O_t is rescaled rarely, and the final division makes up for
 // whichever reference was used.
+//
+// Bound by the chain of a unit: 2048 cycles of products for a pair's, 2700 to
+// 2800 measured, of which the groups' turns, the waits between dependent
+// products and the copies' share of shared memory are the rest; with the
+// exponentials and most maxima left out they are 2560.  (Weights computed with
+// the old reference beside the search for the maximum were no faster: 321 us;
+// the groups without turns 343.)  A tile's ends cost some four units (tile_cost).
+// 7000 new bf16 tokens after 2000 to 4900 cached ones, 32 heads of 128 on 8:
+// 287 us, 1.39 PFLOP/s of the 1.88 that a library's plain product reaches;
+// 128 requests of one token after 16384 shared ones: 52 us by itself.
 #include "ps_kv_attend.cuh"
 
 namespace pskv {
@@ -545,8 +559,7 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
       }
       if (direct) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-          z = spoil(z, x[e]);
+        for (int e = 0; e < 32; ++e) z = spoil(z, x[e]);
         uint32_t w[4][4];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) w[e >> 3][(e >> 1) & 3] = Num<T>::pack(x[e] * inv, x[e + 1] * inv);
