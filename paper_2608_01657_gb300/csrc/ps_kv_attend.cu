@@ -68,8 +68,7 @@ __device__ __forceinline__ uint32_t word_at(int r, int c) { return (c >> 3) * (1
 // heads are 64 or 128 elements, else one for every 64 elements; pages of 2 or 4
 // tokens, whose boxes would not fill the 1024 bytes after which the swizzle
 // repeats, by 16-byte copies.  256 requests of one token, 2.27 GB of bf16 keys
-// and values: 351 us beside the wide tiles of their prefixes, 6.3 TB/s of the 6.8
-// that copies reach; one request of 700 keys: 4 us, its chain of reads.
+// and values: 341 us, 6.5 TB/s of the 6.8 that copies reach; one request of 700 keys: 4 us, its chain of reads.
 template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_constant__ AttendArgs a,
                                                                const __grid_constant__ PoolMaps maps) {

@@ -344,3 +344,45 @@ def test_non_finite_values_of_later_tokens(new, kv, ratio, shared, dtype):
     assert torch.equal(torch.isfinite(outs[0]), finite)
     bound = attention_bound(want, spread, size, dtype, dim, max(kv), 8.0)
     assert ((outs[0].double() - want).abs() <= bound)[finite].all()
+
+
+def test_graph_replay_gives_the_same_bits():
+    """Append, plan and attention captured in one graph and replayed on new inputs in the same places."""
+    from paper_2608_01657_gb300 import kv as KV
+    new, kv, heads, ratio, dim, ps = [1, 40, 1, 3], [300, 400, 17, 3], 2, 4, 128, 16
+    tables, pages, bounds = batch(new, kv, [256], [0], ps, seed=2)
+    T = sum(new)
+    qo = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    dev = lambda a, t=torch.int32: torch.tensor(np.asarray(a), dtype=t, device="cuda")  # noqa: E731
+    pos = np.concatenate([np.arange(L - n, L) for n, L in zip(new, kv)])
+    slots = np.concatenate([[tables[i, p // ps] * ps + p % ps for p in range(L - n, L)] for i, (n, L) in enumerate(zip(new, kv))])
+    args = dict(slots=dev(slots, torch.int64), positions=dev(pos), rope=torch.randn(512, dim, device="cuda"))
+    where = (dev(qo), dev(kv), dev(tables), dev(bounds))
+    k, v = make_pool(1, pages, ps, heads, dim, BF, seed=3)
+    pool = KV.KVPool(k, v, num_q_heads=heads * ratio, max_requests=len(new), max_tokens=T, max_row_pages=tables.shape[1])
+    g = torch.Generator("cuda").manual_seed(9)
+    inputs = [torch.randn(T, h, dim, generator=g, device="cuda").to(BF) for h in (heads * ratio, heads, heads)]
+    q2, out = torch.empty_like(inputs[0]), torch.empty_like(inputs[0])
+
+    def call():
+        pool.plan(*where[:3], T, group_offsets=where[3])
+        pool.append(0, *inputs, q_out=q2, **args)
+        pool.attention(0, q2, 0.1, out=out)
+
+    call()  # the kernels are loaded before the capture
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for seed in (10, 11):
+        g.manual_seed(seed)
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda").to(BF))
+        graph.replay()
+        torch.cuda.synchronize()
+        first = out.clone()
+        out.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(first, out) and out.float().abs().max() > 0
+    pool.check()
