@@ -286,18 +286,22 @@ __device__ __forceinline__ int free_page(const PageScratch& w, const int* base, 
 }
 
 // blockIdx.x: the item; blockIdx.y: a slice of the layers' keys and values.
-// Slice 0 also writes the child's row and the references.
+// Slice 0 also writes the child's row and the references.  The items and their
+// parents' rows are read before the wait for k_fork_scan, which only reads them
+// and lets this kernel start when all that came before it is done.
 __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch w, ForkArgs a) {
   __shared__ int base[kMaxChunks];
-  chain();
-  for (int c = threadIdx.x; c < w.chunks; c += kCopyThreads) base[c] = w.chunk_base[c];
-  if (w.hdr->status != PS_OK) return;
   const int i = blockIdx.x;
   const int pr = a.parents[i], ch = a.children[i];
-  if (pr == ch && blockIdx.y > 0) return;
   int len = 0, full = 0, total = 0;
-  fork_item(p, a, i, &len, &full, &total);
+  const bool ok = fork_item(p, a, i, &len, &full, &total);
+  const int part = len & (p.page_size - 1);
+  const bool copies = ok && pr >= 0 && pr != ch && part > 0;
+  const int64_t from = copies ? a.tables[pr * a.table_stride + full] : 0;
+  chain();
+  for (int c = threadIdx.x; c < w.chunks; c += kCopyThreads) base[c] = w.chunk_base[c];
   const int start = w.start[i];
+  if (w.hdr->status != PS_OK || (pr == ch && blockIdx.y > 0)) return;
   __syncthreads();  // (the row's lengths are read by every thread before they change, too)
   if (blockIdx.y == 0) {
     const int32_t* src = a.tables + pr * a.table_stride;
@@ -319,9 +323,8 @@ __global__ void __launch_bounds__(kCopyThreads) k_fork_apply(Pool p, PageScratch
       a.held[ch] = total;
     }
   }
-  const int part = len & (p.page_size - 1);
-  if (pr < 0 || pr == ch || part == 0) return;
-  const int64_t from = a.tables[pr * a.table_stride + full], to = p.first_page + free_page(w, base, start);
+  if (!copies) return;
+  const int64_t to = p.first_page + free_page(w, base, start);
   const int parts = copy_parts(p, part), n = 2 * p.num_layers * parts;
   for (int u = blockIdx.y * kCopyWarps + (threadIdx.x >> 5); u < n; u += gridDim.y * kCopyWarps)
     copy_part(p, from, to, u / parts, part, u % parts, threadIdx.x & 31);
