@@ -380,13 +380,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(const __grid_cons
 // part's maximum, sum and outputs, written just before and so in L2; the parts'
 // reads do not depend on one another).  The entries are read before the wait for
 // the tiles' kernels (one request's token: 11.9 us a call with them read after
-// it and the tiles' kernels reading their plan after theirs, 9.6 so).  SPLIT 4:
-// the four warps of a CTA take a quarter of the parts each, for when there are
-// fewer rows than warps.  256 requests' rows: 8 us.
+// it and the tiles' kernels reading their plan after theirs, 9.6 so).  SPLIT
+// kJoinWarps: the warps of a CTA take an equal share of the parts each, for when
+// there are fewer rows than warps.  256 requests' rows: 8 us.
 constexpr int kJoinWords = PS_KV_MAX_HEAD_DIM / 16;  // of a lane
+constexpr int kJoinWarps = 4;                         // of a CTA
 struct JoinShared {
-  float4 o[3][kJoinWords][32];
-  float2 ml[3][32];
+  float4 o[kJoinWarps - 1][kJoinWords][32];
+  float2 ml[kJoinWarps - 1][32];
 };
 
 // Numbers that are not finite among the values of tokens that a row does not
@@ -576,7 +577,7 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, JoinShared* sh, b
   }
 }
 template <typename T>
-__global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps, 16 / kJoinWarps) k_attend_join(AttendArgs a) {
   __shared__ JoinShared sh;
   // the entries are the plan's: they are read before the wait for the tiles' kernels
   const int4 h = __ldcg(reinterpret_cast<const int4*>(a.plan.hdr));  // status, entries
@@ -586,18 +587,18 @@ __global__ void __launch_bounds__(128, 4) k_attend_join(AttendArgs a) {
     return;
   }
   const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+  const int64_t warp = (int64_t)blockIdx.x * kJoinWarps + sub, warps = (int64_t)gridDim.x * kJoinWarps;
   if ((int64_t)h.y * (tile_rows(0) / 8) + (int64_t)h.z * (tile_rows(1) / 8) <= 2 * (int64_t)gridDim.x) {
-    join_rows<T, tile_rows(0), 4>(a, &sh, &waited, 0, h.y, blockIdx.x, gridDim.x, sub, lane);
-    join_rows<T, tile_rows(1), 4>(a, &sh, &waited, 1, h.z, blockIdx.x, gridDim.x, sub, lane);
+    join_rows<T, tile_rows(0), kJoinWarps>(a, &sh, &waited, 0, h.y, blockIdx.x, gridDim.x, sub, lane);
+    join_rows<T, tile_rows(1), kJoinWarps>(a, &sh, &waited, 1, h.z, blockIdx.x, gridDim.x, sub, lane);
   } else {
-    const int64_t warp = (int64_t)blockIdx.x * 4 + sub, warps = (int64_t)gridDim.x * 4;
     join_rows<T, tile_rows(0), 1>(a, &sh, &waited, 0, h.y, warp, warps, 0, lane);
     join_rows<T, tile_rows(1), 1>(a, &sh, &waited, 1, h.z, warp, warps, 0, lane);
   }
   if (!waited) chain();
   if (__ldcg(&a.plan.hdr->mend)) {
-    mend_tiles<T, 0>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
-    mend_tiles<T, 1>(a, (int64_t)blockIdx.x * 4 + sub, (int64_t)gridDim.x * 4, lane);
+    mend_tiles<T, 0>(a, warp, warps, lane);
+    mend_tiles<T, 1>(a, warp, warps, lane);
   }
 }
 
@@ -668,10 +669,10 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   if (e == cudaSuccess) e = p.dtype == PS_KV_BF16 ? narrow_t<__nv_bfloat16>(a, maps, st) : narrow_t<__half>(a, maps, st);
   if (e != cudaSuccess) return status_of(e);
   // a CTA for every eight rows of narrow tiles, up to one full wave
-  const int64_t want = (int64_t)b.num_tokens * p.kv_heads * 2, most = (int64_t)plan.max_workers[1] * 4;
+  const int64_t want = (int64_t)b.num_tokens * p.kv_heads * 2, most = (int64_t)plan.max_workers[1] * (16 / kJoinWarps);
   const dim3 grid((unsigned)(want < most ? want : most));
-  e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 128, 0, st, a)
-                            : launch(k_attend_join<__half>, grid, 128, 0, st, a);
+  e = p.dtype == PS_KV_BF16 ? launch(k_attend_join<__nv_bfloat16>, grid, 32 * kJoinWarps, 0, st, a)
+                            : launch(k_attend_join<__half>, grid, 32 * kJoinWarps, 0, st, a);
   return status_of(e);
 }
 

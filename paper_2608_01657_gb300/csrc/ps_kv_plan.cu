@@ -22,8 +22,9 @@ constexpr int kShareTokens = 128;
 // (371 as it stands), 128 requests on one prefix 75 to 88 (76).
 constexpr double kWideCycles = 5250, kNarrowCycles = 2400, kNarrowBandwidth = 2400;
 // A narrow worker has at least so many units: more workers would cost the join
-// more than they save.
-constexpr int kLeastUnits = 2;
+// more than they save (one request of 700 keys, 8 heads: 10.6 us a call with 2,
+// 9.9 with 4, 10.9 with 5, 12.0 with 8; 33 requests of up to 7 tokens 17.2 and 16.8).
+constexpr int kLeastUnits = 4;
 
 // Pages of a request that every one of its queries sees whole.
 __device__ __forceinline__ int whole_pages(const Pool& p, const Batch& b, int r) {
