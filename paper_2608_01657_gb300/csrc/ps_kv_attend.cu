@@ -470,7 +470,7 @@ __device__ __noinline__ void mend_row(const AttendArgs& a, int tok0, int row, in
   const uint32_t keep_hi = (redo & 4 ? 0u : 0xFFFFu) | (redo & 8 ? 0u : 0xFFFF0000u);
   if (redo) *op = make_uint2((was.x & keep_lo) | (lo & ~keep_lo), (was.y & keep_hi) | (hi & ~keep_hi));
 }
-// The rows of the tiles that asked for it.
+// The rows of the tiles that asked for it: those that wrote their outputs themselves.
 template <typename T, int LIST>
 __device__ __forceinline__ void mend_tiles(const AttendArgs& a, int64_t warp, int64_t warps, int lane) {
   constexpr int W = tile_rows(LIST) / 8;  // eight rows at a time
@@ -478,6 +478,7 @@ __device__ __forceinline__ void mend_tiles(const AttendArgs& a, int64_t warp, in
   for (int64_t i = warp; i < n * W; i += warps) {
     if (!__ldcg(a.plan.mend[LIST] + i / W)) continue;
     const Tile& t = a.plan.tiles[LIST][i / W / a.pool.kv_heads];
+    if (t.sidx >= 0) continue;  // its rows are the join's, and its byte is not kept
     const int r0 = (int)(i % W) * 8;
     for (int r = r0; r < min(t.nrows, r0 + 8); ++r) mend_row<T>(a, t.tok0, t.row0 + r, (int)(i / W % a.pool.kv_heads), lane);
   }
