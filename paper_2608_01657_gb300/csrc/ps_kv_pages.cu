@@ -197,7 +197,7 @@ __device__ __forceinline__ bool fork_item(const Pool& p, const ForkArgs& a, int 
 // each (and copy it to refs_out); the others check one item each.  The last CTA
 // to finish turns the counts into offsets and decides whether the call goes
 // ahead, so that the second kernel needs no further pass.  Both are bound by the
-// latency of a few dependent reads: 9.5 us for 7 forks, 20 us for 512 forks of
+// latency of a few dependent reads: 7.8 us for 7 forks, 19.5 us for 512 forks of
 // 2048-token rows and their release (8.8 us of it the partial pages' copies).
 __global__ void __launch_bounds__(kScanThreads) k_fork_scan(Pool p, PageScratch w, ForkArgs a) {
   chain();
