@@ -76,19 +76,20 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_copy(Pool p, const int32_
 }
 
 // ---- scans ----------------------------------------------------------------------
-// Exclusive scan over the CTA of one value a thread.
-__device__ __forceinline__ int block_scan(int v, int* total) {
-  __shared__ int wsum[kScanThreads / 32];
+// Exclusive scan over the CTA of one value a thread, in the type of its sums.
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, T* total) {
+  __shared__ T wsum[kScanThreads / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int incl = v;
+  T incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    const T x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
     if (lane >= o) incl += x;
   }
   if (lane == 31) wsum[warp] = incl;
   __syncthreads();
-  int base = 0, tot = 0;
+  T base = 0, tot = 0;
 #pragma unroll
   for (int w = 0; w < kScanThreads / 32; ++w) {
     if (w < warp) base += wsum[w];
@@ -249,14 +250,13 @@ __global__ void __launch_bounds__(kScanThreads) k_fork_scan(Pool p, PageScratch 
   }
   if (!last_cta(&w.hdr->done)) return;
   const int free_pages = scan_array(w.chunk_cnt, w.chunk_base, w.chunks);
-  // the items' needs in 64 bits: their sum may pass 2^31
+  // the items' needs in 64 bits: the sum of a few may pass 2^31
   int64_t need = 0;
   int any_bad = 0;
   for (int i0 = 0; i0 < a.n; i0 += kScanThreads) {
     const int i = i0 + threadIdx.x;
-    int tot;
-    const int v = i < a.n ? __ldcg(w.need + i) : 0;
-    const int e = block_scan(v, &tot);
+    int64_t tot;
+    const int64_t e = block_scan<int64_t>(i < a.n ? __ldcg(w.need + i) : 0, &tot);
     if (i < a.n) {
       const int64_t s = need + e;
       w.start[i] = s < 0x7FFFFFFF ? (int)s : 0x7FFFFFFF;

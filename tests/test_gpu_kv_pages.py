@@ -266,6 +266,21 @@ def test_fork_takes_all_free_pages_or_none():
     pool.check()
 
 
+def test_fork_needs_past_32_bits():
+    """256 new rows whose needs add up to 2^31 pages of a pool of 30: refused, nothing changes."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 30, 2, 1, 8, BF)
+    rows, width = 256, 1 << 23
+    pool = KV.KVPool(k, v, num_q_heads=1, max_requests=rows, max_row_pages=width)
+    t = torch.empty(rows, width, dtype=torch.int32, device="cuda")
+    t[:, :4] = -3
+    l, h, r = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda"), dev([0] * 30)
+    pool.fork(dev([-1] * rows), dev(range(rows)), dev([2 * width] * rows), t, l, h, r)
+    with pytest.raises(RuntimeError, match="capacity"):
+        pool.check()
+    assert not r.any() and not l.any() and not h.any() and (t[:, :4] == -3).all()
+
+
 @pytest.mark.parametrize("parents,children,room", [
     ([4], [1], [1]), ([-2], [1], [1]), ([0], [4], [1]), ([0], [-1], [1]), ([0], [1], [-1]), ([0], [1], [129]),
     ([0, 0], [1, 1], [40, 40]), ([0, 1], [1, 2], [40, 40]), ([0, 0], [0, 1], [60, 40]), ([3], [2], [1])])
