@@ -87,10 +87,13 @@ void ps_kv_destroy(ps_kv_t* kv);
  * leading blocks resident after the step (its cached prefix, its in-step hits
  * and its own admitted blocks, up to the first block the pool could not hold)
  * go to d_tables[i * table_stride ...] in position order, at most table_stride
- * of them, and their number to d_counts[i].  num_requests and d_group_ids: that step's.
+ * of them, and their number to d_counts[i].  d_group_ids: that step's;
+ * num_requests: its number of requests, or fewer (the leading ones).
  * Must follow the step, in stream order, before any other call on h (they
- * share scratch).  After a step that failed, every count is 0.  *d_status: an error
- * if the step failed or a row was cut at table_stride. */
+ * share scratch): refused before the first step, for more requests than the
+ * last one had, and after ps_cached_prefix() or ps_reset().  After a step that
+ * failed, every count is 0.  *d_status: an error if the step failed or a row was
+ * cut at table_stride. */
 int32_t ps_step_blocks(ps_handle_t* h, void* stream, int32_t num_requests, const int32_t* d_group_ids,
                        int32_t* d_tables, int64_t table_stride, int32_t* d_counts, int32_t* d_status);
 

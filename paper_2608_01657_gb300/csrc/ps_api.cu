@@ -43,6 +43,7 @@ struct ps_handle {
   cudaGraphExec_t exec = nullptr;
   bool exec_timing = false;
   bool use_graph = true;
+  int32_t scratch_requests = 0;  // requests of the step whose positions and keys the workspace still holds, 0: of none
 };
 
 namespace {
@@ -425,6 +426,7 @@ void capture_step(ps_handle* h) {
 namespace ps {
 // Device state of a handle, for entry points defined outside this file.
 const DevState* handle_state(const ps_handle_t* h) { return &h->base; }
+int32_t handle_scratch_requests(const ps_handle_t* h) { return h->scratch_requests; }
 }  // namespace ps
 
 extern "C" {
@@ -529,11 +531,16 @@ int32_t ps_step(ps_handle_t* h, void* stream, int64_t now_ticks, int32_t num_req
   s.args = h->step_args;
   cudaStream_t st = as_stream(stream);
   const StepArgs a = args_of(s);
+  h->scratch_requests = 0;
   if (cudaMemcpyAsync(h->step_args, &a, sizeof(a), cudaMemcpyHostToDevice, st) != cudaSuccess) return PS_ERR_CUDA;
   if (h->use_graph && (!h->exec || h->exec_timing != h->trace.timing)) capture_step(h);
+  int32_t rc;
   if (h->use_graph && h->exec)
-    return cudaGraphLaunch(h->exec, st) == cudaSuccess ? PS_OK : PS_ERR_CUDA;
-  return launch_step(s, st, &h->trace);
+    rc = cudaGraphLaunch(h->exec, st) == cudaSuccess ? PS_OK : PS_ERR_CUDA;
+  else
+    rc = launch_step(s, st, &h->trace);
+  if (rc == PS_OK) h->scratch_requests = num_requests;
+  return rc;
 }
 
 int32_t ps_step_host(ps_handle_t* h, void* stream, int64_t now_ticks, int32_t num_requests, const int32_t* h_group_ids,
@@ -656,6 +663,7 @@ int32_t ps_clear_status(ps_handle_t* h, void* stream) {
 int32_t ps_reset(ps_handle_t* h, void* stream) {
   if (!h) return PS_ERR_INVALID_ARG;
   cudaStream_t st = as_stream(stream);
+  h->scratch_requests = 0;
   const int32_t rc = init_state(h, st);
   return rc != PS_OK ? rc : upload_constants(h, st);
 }
@@ -674,6 +682,7 @@ int32_t ps_cached_prefix(ps_handle_t* h, void* stream, int32_t num_requests, con
   s.in_contract = nullptr;
   s.in_prefix = nullptr;
   s.tokens_aligned16 = (reinterpret_cast<uintptr_t>(d_tokens) & 15) == 0;
+  h->scratch_requests = 0;  // the probe works in the same place
   return launch_probe(s, as_stream(stream), d_cached_blocks, d_status);
 }
 

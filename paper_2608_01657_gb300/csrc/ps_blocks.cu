@@ -10,6 +10,7 @@
 struct ps_handle;
 namespace ps {
 const DevState* handle_state(const ps_handle_t* h);
+int32_t handle_scratch_requests(const ps_handle_t* h);
 
 namespace {
 
@@ -70,7 +71,8 @@ extern "C" int32_t ps_step_blocks(ps_handle_t* h, void* stream, int32_t num_requ
                                   int32_t* d_tables, int64_t table_stride, int32_t* d_counts, int32_t* d_status) {
   if (!h || num_requests < 0 || table_stride < 0) return PS_ERR_INVALID_ARG;
   const ps::DevState& s = *ps::handle_state(h);
-  if (num_requests > s.max_requests) return PS_ERR_INVALID_ARG;
+  // only what a step wrote may be read: the rest of the scratch was never set
+  if (num_requests > ps::handle_scratch_requests(h)) return PS_ERR_INVALID_ARG;
   if (num_requests == 0) return PS_OK;
   if (!d_group_ids || !d_counts || (!d_tables && table_stride > 0)) return PS_ERR_INVALID_ARG;
   const int64_t threads = (int64_t)num_requests * 32;

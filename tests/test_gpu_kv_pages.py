@@ -412,3 +412,29 @@ def test_step_blocks_after_a_failed_step():
     assert c.step_blocks(g, tables, status=status).tolist() == [0] and int(status) == B.PS_ERR_INVALID_ARG
     with pytest.raises(RuntimeError):
         c.step_blocks(dev([0] * 5), torch.zeros(5, 4, dtype=torch.int32, device="cuda"))
+
+
+def test_step_blocks_needs_a_step_of_so_many_requests():
+    """What no step wrote is not read: refused on the host."""
+    from paper_2608_01657_gb300 import binding as B
+    c = B.Cache(64, 16, 2, "lru", B.Params(), max_requests=8, max_tokens=1024)
+    toks = torch.arange(64, dtype=torch.int32, device="cuda")
+    offs = torch.tensor([0, 32, 64], device="cuda")
+    groups, tables = dev([0, 1, 0]), torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+
+    def refused(n):
+        with pytest.raises(RuntimeError):
+            c.step_blocks(groups[:n], tables[:n])
+
+    refused(1)  # no step yet
+    assert c.step_blocks(groups[:0], tables[:0]) is not None
+    assert c.step(1, groups[:2], offs, toks) == 0
+    refused(3)  # the step had two requests
+    assert c.step_blocks(groups[:2], tables[:2]).tolist() == [2, 2]
+    assert c.step_blocks(groups[:1], tables[:1]).tolist() == [2]
+    c.cached_prefix(groups[:2], offs, toks)
+    refused(1)  # the probe's scratch is the step's
+    assert c.step(2, groups[:2], offs, toks) == 0
+    assert c.step_blocks(groups[:2], tables[:2]).tolist() == [2, 2]
+    assert c.reset() == 0
+    refused(1)
