@@ -341,10 +341,14 @@ class Cache:
         right after the step.  Returns counts."""
         import torch
         R = int(groups.shape[0])
-        if counts is None:
-            counts = torch.empty(max(1, R), dtype=torch.int32, device=groups.device)
         if tables.dim() != 2 or tables.shape[0] < R or tables.dtype != torch.int32 or tables.stride(1) != 1:
             raise ValueError("tables must be int32 [requests, blocks] with contiguous rows")
+        for name, t, least in (("groups", groups, R), ("counts", counts, R), ("status", status, 1)):
+            if t is not None and (t.dim() != 1 or t.shape[0] < least or t.dtype != torch.int32 or not t.is_contiguous()
+                                  or t.device != tables.device):
+                raise ValueError(f"{name} must be a contiguous int32 array of {least} on {tables.device}")
+        if counts is None:
+            counts = torch.empty(max(1, R), dtype=torch.int32, device=groups.device)
         if tables.stride(0) != tables.shape[1]:
             raise ValueError("tables must have rows of exactly their width")
         rc = load().ps_step_blocks(self._h, _stream_ptr(stream), R, _ptr(groups), _ptr(tables), tables.shape[1],

@@ -438,3 +438,20 @@ def test_step_blocks_needs_a_step_of_so_many_requests():
     assert c.step_blocks(groups[:2], tables[:2]).tolist() == [2, 2]
     assert c.reset() == 0
     refused(1)
+
+
+def test_step_blocks_refuses_wrong_arrays():
+    """An array that is too short, or of another type or place, is not handed to the kernel."""
+    from paper_2608_01657_gb300 import binding as B
+    c = B.Cache(64, 16, 2, "lru", B.Params(), max_requests=8, max_tokens=1024)
+    toks = torch.arange(64, dtype=torch.int32, device="cuda")
+    offs = torch.tensor([0, 32, 64], device="cuda")
+    groups, tables = dev([0, 1]), torch.zeros(2, 4, dtype=torch.int32, device="cuda")
+    assert c.step(1, groups, offs, toks) == 0
+    for bad in (dict(counts=dev([0])), dict(counts=dev([0, 0], torch.int64)), dict(counts=dev([0] * 4)[::2]),
+                dict(groups=groups.long()), dict(groups=groups.cpu()), dict(groups=dev([[0], [1]])),
+                dict(status=dev([])), dict(status=dev([0], torch.int64)), dict(counts=torch.zeros(2, dtype=torch.int32)),
+                dict(tables=tables[:1]), dict(tables=tables.long())):
+        with pytest.raises(ValueError):
+            c.step_blocks(**(dict(groups=groups, tables=tables) | bad))
+    assert c.step_blocks(groups, tables, counts=dev([7, 7, 7])).tolist() == [2, 2, 7]
