@@ -156,7 +156,8 @@ typedef struct {
  * the work into equal parts.  One plan serves every layer of a step; the
  * batch's arrays must stay unchanged until the last ps_kv_attention() of the
  * plan has run.  Bad offsets, lengths or page ids make *d_status
- * PS_ERR_INVALID_ARG and the plan empty: attention on it writes nothing. */
+ * PS_ERR_INVALID_ARG and the plan empty: attention on it writes nothing.  Until
+ * the first plan has run (a captured one runs when its graph does) it is empty, too. */
 int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* batch, int32_t* d_status);
 
 /* softmax(scale q k^T) v of one layer for the planned batch, softmax and sums

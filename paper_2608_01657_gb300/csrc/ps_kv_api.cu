@@ -167,7 +167,13 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   if (rc == PS_OK) {
     carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages);
     for (int l = 0; l < kLists; ++l) kv->plan.max_workers[l] = workers[l];
-    if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess) rc = PS_ERR_CUDA;
+    // and a plan that is empty, for an attention that runs before its plan has (one that was only captured into a graph)
+    static_assert(PS_ERR_INVALID_ARG == -1, "the status word of all ones");
+    PlanHdr* hdr = kv->plan.hdr;
+    if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess ||
+        cudaMemsetAsync(hdr, 0, sizeof(PlanHdr), as_stream(stream)) != cudaSuccess ||
+        cudaMemsetAsync(&hdr->status, 0xFF, sizeof(hdr->status), as_stream(stream)) != cudaSuccess)
+      rc = PS_ERR_CUDA;
   }
   if (rc != PS_OK) {
     ps_kv_destroy(kv);

@@ -386,3 +386,27 @@ def test_graph_replay_gives_the_same_bits():
         torch.cuda.synchronize()
         assert torch.equal(first, out) and out.float().abs().max() > 0
     pool.check()
+
+
+def test_attention_before_its_captured_plan_has_run_writes_nothing():
+    """A plan that was only captured has divided nothing yet."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 12, 16, 2, 64, BF, seed=5)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    where = dev([0, 1, 21]), dev([40, 60]), torch.arange(8, device="cuda", dtype=torch.int32).view(2, 4)
+    q = torch.randn(21, 8, 64, device="cuda").to(BF)
+    make = lambda: KV.KVPool(k, v, num_q_heads=8, max_requests=2, max_tokens=21, max_row_pages=4)  # noqa: E731
+    first = make()  # the kernels are loaded before the capture
+    first.plan(*where, 21)
+    want = first.attention(0, q, 0.125)
+    pool, out = make(), torch.full_like(want, 7.0)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        pool.plan(*where, 21)
+    pool.attention(0, q, 0.125, out=out)
+    assert (out == 7.0).all()
+    graph.replay()
+    pool.attention(0, q, 0.125, out=out)
+    pool.check()
+    assert torch.equal(out, want)
