@@ -6,6 +6,7 @@ the library has not been built; nothing here falls back to a CPU path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -255,6 +256,32 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _on_stream(stream, device):
+    """Makes ``stream`` (an object or a raw handle; None: no change) the current one.
+
+    Memory that a call on another stream writes is allocated under that stream:
+    the current stream may still be at work on a block that a freed tensor of
+    its own had."""
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = _stream_ptr(stream)
+        stream = torch.cuda.ExternalStream(raw, device) if raw else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _made(shape, dtype, device, stream):
+    """A new tensor that a call on ``stream`` writes and the current stream may read."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on_stream(stream, device):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 class Cache:
     """One multi-tenant block pool on the current CUDA device."""
 
@@ -348,7 +375,7 @@ class Cache:
                                   or t.device != tables.device):
                 raise ValueError(f"{name} must be a contiguous int32 array of {least} on {tables.device}")
         if counts is None:
-            counts = torch.empty(max(1, R), dtype=torch.int32, device=groups.device)
+            counts = _made(max(1, R), torch.int32, groups.device, stream)
         if tables.stride(0) != tables.shape[1]:
             raise ValueError("tables must have rows of exactly their width")
         rc = load().ps_step_blocks(self._h, _stream_ptr(stream), R, _ptr(groups), _ptr(tables), tables.shape[1],

@@ -57,8 +57,9 @@ class KVPool:
                          max_requests=self.max_requests, max_tokens=self.max_tokens, max_row_pages=self.max_row_pages)
         nbytes = L.ps_kv_workspace_bytes(C.byref(c))
         _need(nbytes > 0, "invalid pool configuration")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        with B._on_stream(stream, self.device):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         h = C.c_void_p()
         self._raise("ps_kv_create", L.ps_kv_create(C.byref(h), C.byref(c), self.workspace.data_ptr(), nbytes,
                                                    B._stream_ptr(stream)))
@@ -99,13 +100,6 @@ class KVPool:
             self.status.zero_()
             self._raise("a call on the pool", rc)
 
-    def _made(self, tokens: int, stream):
-        """A new [tokens, q_heads, head_dim] tensor that a call on ``stream`` writes."""
-        t = torch.empty(tokens, self.q_heads, self.head_dim, dtype=self.dtype, device=self.device)
-        if stream is not None:
-            t.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
-        return t
-
     # -- argument checks ---------------------------------------------------
     def _stream(self, stream):
         return _raw_stream(self.device.index) if stream is None else B._stream_ptr(stream)
@@ -144,7 +138,7 @@ class KVPool:
         a, st = self._append_args, self._append_strides
         T = q.shape[0]
         if q_out is None:
-            q_out = self._made(T, stream)
+            q_out = B._made((T, self.q_heads, self.head_dim), self.dtype, self.device, stream)
         a.q = self._heads(q, T, self.q_heads, "q", st[0])
         a.k = self._heads(k, T, self.kv_heads, "k", st[1])
         a.v = self._heads(v, T, self.kv_heads, "v", st[2])
@@ -196,7 +190,7 @@ class KVPool:
             raise ValueError("attention needs a plan")
         T = self._batch[4]
         if out is None:
-            out = self._made(T, stream)
+            out = B._made((T, self.q_heads, self.head_dim), self.dtype, self.device, stream)
         a, st = self._attention_args, self._attention_strides
         a.q = self._heads(q, T, self.q_heads, "q", st[0])
         a.out = self._heads(out, T, self.q_heads, "out", st[1])
@@ -260,9 +254,7 @@ class KVPool:
         tensor (pages in use, pages moved)."""
         r, before = self._rows(tables, None, held), self._refs(refs)
         if counts is None:
-            counts = torch.empty(2, dtype=torch.int32, device=self.device)
-            if stream is not None:
-                counts.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+            counts = B._made(2, torch.int32, self.device, stream)
         tables_out = tables if tables_out is None else tables_out
         self._table(tables_out, "tables_out")
         _need(tables_out.shape == tables.shape, "tables_out must be shaped as tables")
