@@ -256,6 +256,15 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_object(stream, device):
+    """The torch stream of an object or a raw handle."""
+    import torch
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    raw = _stream_ptr(stream)
+    return torch.cuda.ExternalStream(raw, device) if raw else torch.cuda.default_stream(device)
+
+
 def _on_stream(stream, device):
     """Makes ``stream`` (an object or a raw handle; None: no change) the current one.
 
@@ -265,10 +274,7 @@ def _on_stream(stream, device):
     import torch
     if stream is None:
         return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        raw = _stream_ptr(stream)
-        stream = torch.cuda.ExternalStream(raw, device) if raw else torch.cuda.default_stream(device)
-    return torch.cuda.stream(stream)
+    return torch.cuda.stream(_stream_object(stream, device))
 
 
 def _made(shape, dtype, device, stream):
@@ -382,6 +388,10 @@ class Cache:
                                    _ptr(counts), _ptr(status))
         if rc != PS_OK:
             raise RuntimeError(f"ps_step_blocks failed ({rc})")
+        if stream is not None:
+            for t in (groups, tables, counts, status):
+                if t is not None:
+                    t.record_stream(_stream_object(stream, tables.device))
         return counts
 
     def step_host(self, now: int, groups, offsets, tokens, contracts=None, prefixes=None, stream=None,

@@ -6,7 +6,9 @@ rotation, page write), attention over the pages with shared prefixes read once,
 and copying, forking, freeing and compacting pages.  As in ``binding``,
 arguments are marshalled here and all work runs in the library's CUDA kernels;
 torch provides device memory and streams.  Calls are enqueued on ``stream``
-(default: the current one) and do not synchronize; errors that only the device
+(default: the current one) and do not synchronize; what a call that names its
+stream is given may be dropped once the call returns, and so may a plan's
+tensors once the next plan is made, and the pool; errors that only the device
 can see are reported in the int32 tensor ``pool.status``, which is sticky until
 ``check()``.
 """
@@ -65,6 +67,8 @@ class KVPool:
                                                    B._stream_ptr(stream)))
         self._h = h
         self._batch = None
+        self._used, self._batch_used = {}, set()  # streams that the pool's memory, and the plan's, is recorded on
+        self._stream(stream)
         # argument structures and entry points of the calls that a decode step
         # makes for every layer; their fields are filled in anew each time
         self._lib = L
@@ -102,7 +106,26 @@ class KVPool:
 
     # -- argument checks ---------------------------------------------------
     def _stream(self, stream):
-        return _raw_stream(self.device.index) if stream is None else B._stream_ptr(stream)
+        """The raw handle of a call's stream.  What the handle keeps (the pool, the
+        workspace, the status) is recorded on each stream that it is used on, so
+        that its memory outlives the work there."""
+        raw = _raw_stream(self.device.index) if stream is None else B._stream_ptr(stream)
+        if raw not in self._used:
+            self._used[raw] = B._stream_object(raw, self.device)
+            self._record(raw, self.k, self.v, self.workspace, self.status)
+        return raw
+
+    def _record(self, raw, *tensors):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self._used[raw])
+
+    def _done(self, name, rc, stream, raw, *tensors):
+        """The end of a call: its error, or its arguments recorded on the stream that it named."""
+        if rc:
+            self._raise(name, rc)
+        if stream is not None:
+            self._record(raw, *tensors)
 
     def _heads(self, t, tokens: int, heads: int, name: str, strides):
         """Checks [tokens, heads, head_dim]; its strides go to ``strides``."""
@@ -159,9 +182,9 @@ class KVPool:
         a.q_weight = None if q_weight is None else self._array(q_weight, self.dtype, "q_weight", self.head_dim)
         a.k_weight = None if k_weight is None else self._array(k_weight, self.dtype, "k_weight", self.head_dim)
         a.eps, a.num_tokens = eps, T
-        rc = self._lib.ps_kv_append(self._h, self._stream(stream), layer, self._append_ref, self._status)
-        if rc:
-            self._raise("ps_kv_append", rc)
+        raw = self._stream(stream)
+        rc = self._lib.ps_kv_append(self._h, raw, layer, self._append_ref, self._status)
+        self._done("ps_kv_append", rc, stream, raw, q, k, v, slots, positions, rope, q_weight, k_weight, q_out)
         return q_out
 
     # -- attention -------------------------------------------------------------
@@ -180,8 +203,12 @@ class KVPool:
         if group_offsets is not None:
             b.group_offsets, b.num_groups = self._array(group_offsets, torch.int32, "group_offsets"), int(group_offsets.shape[0]) - 1
         self._batch = None
-        self._raise("ps_kv_plan", self._lib.ps_kv_plan(self._h, self._stream(stream), C.byref(b), self._status))
-        self._batch = (q_offsets, kv_lens, tables, group_offsets, int(num_tokens))  # alive while the plan is
+        raw = self._stream(stream)
+        self._raise("ps_kv_plan", self._lib.ps_kv_plan(self._h, raw, C.byref(b), self._status))
+        # alive while the plan is, and after it until the work on the streams that use it is done
+        self._batch = (q_offsets, kv_lens, tables, group_offsets, int(num_tokens))
+        self._batch_used = {raw}
+        self._record(raw, *self._batch[:4])
 
     def attention(self, layer: int, q, scale: float, out=None, lse=None, stream=None):
         """softmax(scale q k^T) v of one layer for the planned batch.  ``lse``
@@ -201,19 +228,21 @@ class KVPool:
             a.lse = lse.data_ptr()
         else:
             a.lse = None
-        rc = self._lib.ps_kv_attention(self._h, self._stream(stream), layer, self._attention_ref, self._status)
-        if rc:
-            self._raise("ps_kv_attention", rc)
+        raw = self._stream(stream)
+        if raw not in self._batch_used:
+            self._batch_used.add(raw)
+            self._record(raw, *self._batch[:4])
+        rc = self._lib.ps_kv_attention(self._h, raw, layer, self._attention_ref, self._status)
+        self._done("ps_kv_attention", rc, stream, raw, q, out, lse)
         return out
 
     # -- pages -------------------------------------------------------------------
     def copy(self, src, dst, stream=None):
         """Copy whole pages src[i] -> dst[i], all layers."""
-        n = src.shape[0]
-        rc = self._lib.ps_kv_copy(self._h, self._stream(stream), n, self._array(src, torch.int32, "src"),
+        n, raw = src.shape[0], self._stream(stream)
+        rc = self._lib.ps_kv_copy(self._h, raw, n, self._array(src, torch.int32, "src"),
                                   self._array(dst, torch.int32, "dst", n), self._status)
-        if rc:
-            self._raise("ps_kv_copy", rc)
+        self._done("ps_kv_copy", rc, stream, raw, src, dst)
 
     def _rows(self, tables, lens, held):
         """Fills in the structure of the rows; returns the reference to pass."""
@@ -232,22 +261,20 @@ class KVPool:
         """Rows ``children`` become continuations of rows ``parents`` with
         pages for ``room`` tokens: in place (parent == child), new (parent -1)
         or a fork that shares the full pages and copies the partial one."""
-        n = parents.shape[0]
+        n, raw = parents.shape[0], self._stream(stream)
         rows, before = self._rows(tables, lens, held), self._refs(refs)
         rc = self._lib.ps_kv_fork(
-            self._h, self._stream(stream), n, self._array(parents, torch.int32, "parents"),
+            self._h, raw, n, self._array(parents, torch.int32, "parents"),
             self._array(children, torch.int32, "children", n), self._array(room, torch.int32, "room", n), rows,
             before, before if refs_out is None else self._refs(refs_out, "refs_out"), self._status)
-        if rc:
-            self._raise("ps_kv_fork", rc)
+        self._done("ps_kv_fork", rc, stream, raw, parents, children, room, tables, lens, held, refs, refs_out)
 
     def release(self, rows, tables, lens, held, refs, stream=None):
         """Free the pages that ``rows`` hold."""
-        r = self._rows(tables, lens, held)
-        rc = self._lib.ps_kv_release(self._h, self._stream(stream), rows.shape[0], self._array(rows, torch.int32, "rows"), r,
+        r, raw = self._rows(tables, lens, held), self._stream(stream)
+        rc = self._lib.ps_kv_release(self._h, raw, rows.shape[0], self._array(rows, torch.int32, "rows"), r,
                                      self._refs(refs), self._status)
-        if rc:
-            self._raise("ps_kv_release", rc)
+        self._done("ps_kv_release", rc, stream, raw, rows, tables, lens, held, refs)
 
     def compact(self, tables, held, refs, tables_out=None, refs_out=None, counts=None, stream=None):
         """Move the private pages in use to the lowest ids.  Returns the int32
@@ -258,10 +285,10 @@ class KVPool:
         tables_out = tables if tables_out is None else tables_out
         self._table(tables_out, "tables_out")
         _need(tables_out.shape == tables.shape, "tables_out must be shaped as tables")
+        raw = self._stream(stream)
         rc = self._lib.ps_kv_compact(
-            self._h, self._stream(stream), r, before, tables_out.data_ptr(),
+            self._h, raw, r, before, tables_out.data_ptr(),
             before if refs_out is None else self._refs(refs_out, "refs_out"), self._array(counts, torch.int32, "counts", 2),
             self._status)
-        if rc:
-            self._raise("ps_kv_compact", rc)
+        self._done("ps_kv_compact", rc, stream, raw, tables, held, refs, tables_out, refs_out, counts)
         return counts

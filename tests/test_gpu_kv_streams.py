@@ -1,4 +1,6 @@
 """The pool's calls on streams other than the current one."""
+import gc
+
 import pytest
 import torch
 
@@ -27,6 +29,18 @@ def small(first_page=0, **kw):
 
 
 WHERE = ([0, 1, 21], [40, 60], [[0, 1, 2, 3], [4, 5, 6, 7]])
+
+
+@pytest.fixture(scope="module", autouse=True)
+def kernels_are_loaded():
+    """So that no first launch holds a test up while a stream is kept busy."""
+    pool = small()
+    pool.plan(*(dev(a) for a in WHERE), 21)
+    x = torch.zeros(21, 8, 64, device="cuda", dtype=BF)
+    pool.append(0, x, x[:, :2], x[:, :2], dev([-1] * 21, torch.int64))
+    pool.attention(0, x, 1.0)
+    pool.copy(dev([0]), dev([1]))
+    pool.check()
 
 
 @pytest.mark.parametrize("raw", [False, True])
@@ -77,3 +91,78 @@ def test_step_blocks_counts_on_another_stream():
     assert counts.data_ptr() != block
     torch.cuda.synchronize()
     assert counts.tolist() == [2, 2]
+
+
+@pytest.mark.parametrize("named", [True, False])
+def test_a_plans_tensors_outlive_its_attention(named):
+    """Temporaries given to a plan stay until the work on its streams is done, the next plan made or not."""
+    pool = small(max_row_pages=600)
+    q = torch.randn(21, 8, 64, device="cuda").to(BF)
+    table = torch.zeros(2, 600, dtype=torch.int32, device="cuda")
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for planned_on, run_on in ((s, s), (other, s)):
+        torch.cuda.synchronize()
+        big = table.clone()
+        with torch.cuda.stream(torch.cuda.current_stream() if named else planned_on):
+            pool.plan(dev(WHERE[0]), dev(WHERE[1]), big, 21, stream=planned_on if named else None)
+        planned_on.synchronize()
+        with torch.cuda.stream(run_on):
+            torch.cuda._sleep(400_000_000)
+        with torch.cuda.stream(torch.cuda.current_stream() if named else run_on):
+            pool.attention(0, q, 0.125, stream=run_on if named else None)
+        where = big.data_ptr()
+        del big
+        pool.plan(dev(WHERE[0]), dev(WHERE[1]), table, 21, stream=run_on)
+        assert not run_on.query()
+        again = torch.empty(2, 600, dtype=torch.int32, device="cuda")
+        assert again.data_ptr() != where
+
+
+def test_a_pool_outlives_its_calls():
+    pool = small()
+    offsets, lens, tables = (dev(a) for a in WHERE)
+    q, s = torch.randn(21, 8, 64, device="cuda").to(BF), torch.cuda.Stream()
+    nbytes, where = pool.workspace.numel(), {t.data_ptr() for t in (pool.workspace, pool.status, pool.k, pool.v)}
+    shape = pool.k.shape
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(400_000_000)
+        pool.plan(offsets, lens, tables, 21)
+        pool.attention(0, q, 0.125)
+    del pool
+    gc.collect()
+    assert not s.query()
+    new = [torch.empty(nbytes, dtype=torch.uint8, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")]
+    new += [torch.empty(shape, dtype=BF, device="cuda") for _ in range(2)]
+    assert not where & {t.data_ptr() for t in new}
+
+
+def test_arguments_of_a_call_that_names_its_stream_outlive_it():
+    pool = small()
+    offsets, lens, tables = (dev(a) for a in WHERE)
+    kv, slots = torch.randn(21, 2, 64, device="cuda").to(BF), dev(range(150, 171), torch.int64)
+    s = torch.cuda.Stream()
+    pool.plan(offsets, lens, tables, 21)
+    calls = (lambda q: pool.append(0, q, kv, kv, slots, stream=s), lambda q: pool.attention(0, q, 0.125, stream=s),
+             lambda q: pool.attention(0, kv.repeat_interleave(4, 1), 0.125, out=q, stream=s.cuda_stream))
+    for call in calls:
+        torch.cuda.synchronize()
+        q = torch.zeros(21, 8, 64, device="cuda", dtype=BF)
+        where = q.data_ptr()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(400_000_000)
+        call(q)
+        del q
+        assert not s.query()
+        assert torch.empty(21, 8, 64, device="cuda", dtype=BF).data_ptr() != where
+    torch.cuda.synchronize()
+    src = dev(range(6))
+    where = src.data_ptr()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(400_000_000)
+    pool.copy(src, dev(range(6, 12)), stream=s)
+    del src
+    assert not s.query()
+    assert dev(range(6)).data_ptr() != where
+    torch.cuda.synchronize()
+    pool.check()
