@@ -98,10 +98,16 @@ class KVPool:
             raise RuntimeError(f"{name} failed: {B.load().ps_status_string(rc).decode()} ({rc})")
 
     def check(self):
-        """Raise if a call's device work reported an error; clears it (synchronizes)."""
+        """Raise if a call's device work reported an error; clears it (synchronizes:
+        the device, if calls were made on other streams than the current one)."""
+        elsewhere = any(raw != _raw_stream(self.device.index) for raw in self._used)
+        if elsewhere:
+            torch.cuda.synchronize(self.device)
         rc = int(self.status.item())
         if rc != B.PS_OK:
             self.status.zero_()
+            if elsewhere:  # before the next call on another stream
+                torch.cuda.synchronize(self.device)
             self._raise("a call on the pool", rc)
 
     # -- argument checks ---------------------------------------------------

@@ -166,3 +166,25 @@ def test_arguments_of_a_call_that_names_its_stream_outlive_it():
     assert dev(range(6)).data_ptr() != where
     torch.cuda.synchronize()
     pool.check()
+
+
+@pytest.mark.parametrize("named", [True, False])
+def test_check_sees_errors_of_calls_on_other_streams(named):
+    pool = small()
+    x = torch.zeros(1, 8, 64, device="cuda", dtype=BF)
+    good, bad = dev([0], torch.int64), dev([12 * 16], torch.int64)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    pool.append(0, x, x[:, :2], x[:, :2], good)
+    for _ in range(2):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(200_000_000)
+            if not named:
+                pool.append(0, x, x[:, :2], x[:, :2], bad)
+        if named:
+            pool.append(0, x, x[:, :2], x[:, :2], bad, stream=s)
+        with pytest.raises(RuntimeError, match="invalid argument"):
+            pool.check()
+        pool.check()
+        pool.append(0, x, x[:, :2], x[:, :2], good, stream=s)
+        pool.check()
