@@ -223,8 +223,9 @@ int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_row
  * tables (all num_rows rows' held pages) are written to d_tables_out with the
  * new ids (entries past held are copied as they are), and the references to
  * d_refs_out; both may be the inputs themselves.  d_counts [2]: L, and the
- * pages moved.  Held ids out of range are copied as they are and set
- * *d_status. */
+ * pages moved.  Rows may be wider than max_row_pages.  Held ids out of range
+ * are copied as they are and set *d_status; a row with fewer than 0 or more
+ * than table_stride pages sets it, too, and has none or all its ids rewritten. */
 int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
                       int32_t* d_tables_out, int32_t* d_refs_out, int32_t* d_counts, int32_t* d_status);
 

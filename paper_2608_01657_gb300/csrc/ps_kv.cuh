@@ -334,8 +334,7 @@ int32_t launch_fork(const Pool& p, const PageScratch& w, int32_t n, const int32_
                     int32_t* refs_out, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_kv_rows_t& rows, int32_t row_pages,
                        int32_t* refs, int32_t* status, cudaStream_t st);
-int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, int32_t row_pages,
-                       const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
+int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                        int32_t* status, int nsm, cudaStream_t st);
 // Kernel attributes (shared-memory opt-ins) and the workers of each attention list
 // that the current device holds at once.

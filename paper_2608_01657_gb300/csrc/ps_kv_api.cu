@@ -266,8 +266,8 @@ int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const
   if (!kv || !rows || !rows->tables || !rows->held || rows->num_rows < 1 || rows->table_stride < 1 || !d_refs_in ||
       !d_tables_out || !d_refs_out || !d_counts)
     return PS_ERR_INVALID_ARG;
-  return launch_compact(kv->pool, kv->pages, *rows, row_pages(kv, rows->table_stride), d_refs_in, d_tables_out,
-                        d_refs_out, d_counts, d_status, kv->nsm, as_stream(stream));
+  return launch_compact(kv->pool, kv->pages, *rows, d_refs_in, d_tables_out, d_refs_out, d_counts, d_status, kv->nsm,
+                        as_stream(stream));
 }
 
 }  // extern "C"

@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(kScanThreads) k_compact_lists(Pool p, PageScra
   if (blockIdx.x == 0 && threadIdx.x == 0 && live == np) w.hdr->free_pages = 0;
 }
 
-__global__ void __launch_bounds__(kCopyThreads) k_compact_move(Pool p, PageScratch w, ps_kv_rows_t rows, int row_pages,
+__global__ void __launch_bounds__(kCopyThreads) k_compact_move(Pool p, PageScratch w, ps_kv_rows_t rows,
                                                                int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                                                                int32_t* status) {
   chain();
@@ -444,8 +444,11 @@ __global__ void __launch_bounds__(kCopyThreads) k_compact_move(Pool p, PageScrat
   for (int64_t m = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; m < moved; m += (int64_t)gridDim.x * kCopyThreads)
     refs_out[w.list[m]] = w.mover_refs[m];
   for (int r = blockIdx.x; r < rows.num_rows; r += gridDim.x) {
-    const int held = rows.held[r];
-    for (int k = threadIdx.x; k < row_pages; k += kCopyThreads) {
+    const int64_t held = rows.held[r], width = rows.table_stride;
+    if ((held < 0 || held > width) && threadIdx.x == 0) set_error(status, PS_ERR_INVALID_ARG);
+    // in place, what is past the held pages stays as it is
+    const int64_t n = tables_out == rows.tables && held < width ? held : width;
+    for (int64_t k = threadIdx.x; k < n; k += kCopyThreads) {
       int64_t id = rows.tables[r * rows.table_stride + k];
       if (k < held) {
         if (id < 0 || id >= p.num_pages) {
@@ -498,14 +501,14 @@ int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_k
   return status_of(launch(k_release, dim3((unsigned)n), kScanThreads, 0, st, p, list, rows, row_pages, refs, status));
 }
 
-int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, int32_t row_pages,
-                       const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
+int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, const int32_t* refs_in,
+                       int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                        int32_t* status, int nsm, cudaStream_t st) {
   cudaError_t e = launch(k_compact_count, dim3((unsigned)w.chunks), kScanThreads, 0, st, p, w, refs_in);
   if (e == cudaSuccess)
     e = launch(k_compact_lists, dim3((unsigned)w.chunks), kScanThreads, 0, st, p, w, refs_in, refs_out);
   if (e == cudaSuccess)
-    e = launch(k_compact_move, dim3((unsigned)(nsm * 8)), kCopyThreads, 0, st, p, w, rows, row_pages, tables_out,
+    e = launch(k_compact_move, dim3((unsigned)(nsm * 8)), kCopyThreads, 0, st, p, w, rows, tables_out,
                refs_out, counts, status);
   return status_of(e);
 }

@@ -246,6 +246,44 @@ def test_a_life_of_pages(ps, layout, dtype, dim):
     b.compact()  # nothing in use
 
 
+@pytest.mark.parametrize("out_of_place", [False, True])
+def test_compaction_of_rows_wider_than_the_handles(out_of_place):
+    """Every held page is renamed and every other column copied, whatever max_row_pages is."""
+    from paper_2608_01657_gb300 import kv as KV
+    t, l, h, r = rows_in_use(6, 3, 150, 16, 20, 400, 4)
+    refs = Pages(t, l, h, r, 20, 16)
+    k, v = make_pool(2, 400, 16, 2, 64, BF, seed=4)
+    rk, rv = k.clone(), v.clone()
+    tables, held, before = dev(t), dev(h), dev(r)
+    assert (h > 2).any() and t.shape[1] > h.max()
+    pool = KV.KVPool(k, v, num_q_heads=2, first_page=20, max_row_pages=2)
+    to, ro = (torch.full_like(tables, 77), torch.full_like(before, 77)) if out_of_place else (None, None)
+    counts = pool.compact(tables, held, before, tables_out=to, refs_out=ro)
+    pool.check()
+    moves, live = refs.compact()
+    assert counts.tolist() == [live, len(moves)] and moves
+    for a, b in moves:
+        rk[:, b], rv[:, b] = rk[:, a], rv[:, a]
+    assert np.array_equal((to if out_of_place else tables).cpu().numpy(), refs.tables)
+    assert np.array_equal((ro if out_of_place else before).cpu().numpy(), refs.refs)
+    assert torch.equal(k, rk) and torch.equal(v, rv)
+
+
+@pytest.mark.parametrize("out_of_place", [False, True])
+def test_compaction_reports_rows_of_impossible_lengths(out_of_place):
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 10, 16, 1, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=1)
+    for held, renamed in ((4, True), (-1, False)):
+        t, r = dev([[9, 8, 2]]), dev([0] * 8 + [1, 1])  # the third id has no reference, and lies where nothing moves from
+        to = torch.full_like(t, 77) if out_of_place else None
+        counts = pool.compact(t, dev([held]), r, tables_out=to)
+        with pytest.raises(RuntimeError, match="invalid"):
+            pool.check()
+        assert counts.tolist() == [2, 2]
+        assert (to if out_of_place else t).tolist() == [[0, 1, 2] if renamed else [9, 8, 2]]
+
+
 def test_fork_takes_all_free_pages_or_none():
     from paper_2608_01657_gb300 import kv as KV
     k, v = make_pool(1, 12, 16, 1, 64, BF)
