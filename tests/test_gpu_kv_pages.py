@@ -275,13 +275,13 @@ def test_compaction_reports_rows_of_impossible_lengths(out_of_place):
     k, v = make_pool(1, 10, 16, 1, 64, BF)
     pool = KV.KVPool(k, v, num_q_heads=1)
     for held, renamed in ((4, True), (-1, False)):
-        t, r = dev([[9, 8, 2]]), dev([0] * 8 + [1, 1])  # the third id has no reference, and lies where nothing moves from
+        t, r = dev([[9, 8, 1]]), dev([0] * 8 + [1, 1])  # nothing moves from the third
         to = torch.full_like(t, 77) if out_of_place else None
         counts = pool.compact(t, dev([held]), r, tables_out=to)
         with pytest.raises(RuntimeError, match="invalid"):
             pool.check()
         assert counts.tolist() == [2, 2]
-        assert (to if out_of_place else t).tolist() == [[0, 1, 2] if renamed else [9, 8, 2]]
+        assert (to if out_of_place else t).tolist() == [[0, 1, 1] if renamed else [9, 8, 1]]
 
 
 def test_fork_takes_all_free_pages_or_none():
