@@ -6,7 +6,14 @@
  * num_layers layers.  Page ids below first_page belong to the prefix cache (the
  * block ids of ps_step()); the ids from first_page on are private pages of
  * running requests, counted by a reference array (ps_kv_fork() and the calls
- * after it).  The operators:
+ * after it).  Nothing holds the prefix cache's pages for a running request:
+ * ps_step() keeps the blocks of its own batch only, and a later step may evict
+ * one that a row's table still names (it lists them in evicted_ids and
+ * invalidated_ids) and give it to another prompt, whose ps_kv_append() then
+ * writes over it.  So either no step runs while rows name cached pages, or,
+ * after the step and before its appends, each listed page that a row names is
+ * copied to a private page (ps_kv_copy()) that takes its place in the table.
+ * The operators:
  *   ps_step_blocks   the block ids of every request of the last ps_step();
  *   ps_kv_append     norm of queries and keys for each head, position
  *                    rotation, write of keys and values into their pages;

@@ -36,7 +36,10 @@ class KVPool:
     ``k`` and ``v`` are tensors [layers, pages, page_size, kv_heads, head_dim]
     with the same strides, the innermost one 1 (a head-major pool is passed as
     its transposed view).  Page ids below ``first_page`` are the prefix
-    cache's block ids, the others private pages of running requests."""
+    cache's block ids, the others private pages of running requests.  The
+    references count private pages alone: a later step of the cache may evict a
+    block that a row still names, so no step runs while rows name cached pages,
+    or the pages that it evicts are copied to private ones before its appends."""
 
     def __init__(self, k, v, num_q_heads: int, first_page: int = 0, max_requests: int = 1, max_tokens: int = 1,
                  max_row_pages: int = 1, stream=None):

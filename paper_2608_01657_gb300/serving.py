@@ -70,6 +70,7 @@ class Server:
         self.tables = torch.zeros(s.max_requests, width, **i32)
         self.lens, self.held = torch.zeros(s.max_requests, **i32), torch.zeros(s.max_requests, **i32)
         self.refs = torch.zeros(s.private_pages, **i32)
+        self.running = set()  # rows that hold pages
         self.tick = 0
 
     # -- one pass over all layers ------------------------------------------------
@@ -107,8 +108,12 @@ class Server:
     def admit(self, groups: Sequence[int], prompts: List[np.ndarray], room: int) -> dict:
         """Rows 0.. for a batch of prompts, with room for ``room`` more tokens each.
 
-        Returns the hidden state of each prompt's last token and how many tokens were cached."""
+        Returns the hidden state of each prompt's last token and how many tokens were cached.
+        No row may be running: nothing holds the cached pages of a running row, so that a
+        step could evict them and give them to a prompt of the new batch."""
         s, R = self.s, len(prompts)
+        if self.running:
+            raise RuntimeError(f"rows {sorted(self.running)} are running: finish them before the next batch")
         lens = [len(p) for p in prompts]
         flat = torch.from_numpy(np.concatenate(prompts).astype(np.int32)).cuda()
         offs = np.concatenate([[0], np.cumsum(lens)])
@@ -121,6 +126,7 @@ class Server:
         blocks = self.cache.step_blocks(g, self.tables, status=status)[:R]
         if int(status):
             raise RuntimeError(f"the step failed ({int(status)})")
+        self.running = set(range(R))
         # the cache's blocks first, then private pages for the rest of the prompt and the answer
         self.held[:R], self.lens[:R] = blocks, blocks * s.page
         rows = torch.arange(R, dtype=torch.int32, device="cuda")
@@ -145,9 +151,13 @@ class Server:
 
         Returns the hidden states [t, request * samples, hidden]; the sampled rows stay."""
         n, T = requests * samples, steps.shape[0]
+        rows = range(requests, requests + n)
+        if self.running.intersection(rows):
+            raise RuntimeError("the samples' rows are running: finish them first")
         dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
         parents = dev(np.repeat(np.arange(requests), samples))
-        children = dev(requests + np.arange(n))
+        children = dev(np.asarray(rows))
+        self.running.update(rows)
         self.pool.fork(parents, children, self.lens[parents.long()] + T, self.tables, self.lens, self.held, self.refs)
         bounds = list(range(0, n + 1, samples))  # a request's samples share its pages
         out = []
@@ -160,6 +170,7 @@ class Server:
     def finish(self, rows: Sequence[int]):
         """Frees rows and moves the pages in use together; returns (in use, moved)."""
         self.pool.release(torch.tensor(rows, dtype=torch.int32, device="cuda"), self.tables, self.lens, self.held, self.refs)
+        self.running.difference_update(rows)
         counts = self.pool.compact(self.tables, self.held, self.refs)
         self.pool.check()
         return tuple(counts.tolist())

@@ -79,3 +79,28 @@ def test_the_example_runs(capsys):
     S.main()
     text = capsys.readouterr().out
     assert "first batch" in text and "sampled hidden states (4, 15, 256)" in text
+
+
+def test_no_batch_is_admitted_while_rows_name_cached_pages():
+    """Nothing holds a running row's cached pages: the next batch could be given them."""
+    from paper_2608_01657_gb300 import serving as S
+    s = S.Shape()
+    server = S.Server(s, groups=2, seed=1)
+    groups = [0, 0, 1]
+    prompts, others = S.prompts_of(groups, s, 1), S.prompts_of(groups, s, 2)
+    steps = np.zeros((2, 3, 2), np.int32)
+    server.admit(groups, prompts, room=0)
+    with pytest.raises(RuntimeError, match="running"):
+        server.admit(groups, others, room=0)
+    before = server.sample(3, 2, steps)
+    with pytest.raises(RuntimeError, match="running"):
+        server.sample(3, 2, steps)          # the rows hold the first samples
+    server.finish(range(3))                 # the samples go on
+    with pytest.raises(RuntimeError, match="running"):
+        server.admit(groups, others, room=0)
+    server.finish(range(3, 9))
+    assert not server.refs.any()
+    server.admit(groups, others, room=0)
+    server.finish(range(3))
+    server.admit(groups, prompts, room=0)   # the same again
+    assert near(server.sample(3, 2, steps), before)
