@@ -110,7 +110,8 @@ int32_t ps_step_blocks(ps_handle_t* h, void* stream, int32_t num_requests, const
  * in 32 bits, rounded once; queries go to q_out, keys and values to the pool.
  * Head h, element e of token t's queries is q[t * q_stride[0] + h *
  * q_stride[1] + e], and so on; inputs and q_out start on 16-byte boundaries
- * with strides that are multiples of 8 elements.  q_out may be q itself. */
+ * with strides that are multiples of 8 elements.  q_out may be q itself; else
+ * it lies on none of q, k and v (refused). */
 typedef struct {
   const void* q;
   const void* k;
@@ -170,7 +171,7 @@ int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* batch, int32_
 /* softmax(scale q k^T) v of one layer for the planned batch, softmax and sums
  * in 32 bits.  q and out: element (t, h, e) at t * stride[0] + h * stride[1] +
  * e, on 16-byte boundaries with strides that are multiples of 8 elements; out
- * does not overlap q.  lse (NULL: none): float [num_tokens][num_q_heads], log of the sum of the
+ * does not overlap q (refused).  lse (NULL: none): float [num_tokens][num_q_heads], log of the sum of the
  * exponentials of a query's scaled scores.  Results do not depend on timing:
  * the same call gives the same bits.  *d_status: PS_ERR_TIMEOUT if a wait inside
  * the kernel ran out (never expected). */

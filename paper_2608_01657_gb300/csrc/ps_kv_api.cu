@@ -4,6 +4,7 @@
 #include <new>
 
 #include "ps_kv.cuh"
+#include "ps_kv_overlap.cuh"
 
 using namespace pskv;
 
@@ -21,6 +22,7 @@ namespace {
 
 inline cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline HeadRuns runs(const void* p, const int64_t stride[2], int64_t heads) { return {p, stride[0], stride[1], heads}; }
 inline bool good_strides(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && s[0] % 8 == 0 && s[1] % 8 == 0; }
 
 bool check_config(const ps_kv_config_t* c) {
@@ -203,6 +205,14 @@ int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_appen
   if (a->rope && (!a->positions || a->rope_rows < 1 || a->rope_dim < 8 || a->rope_dim % 8 != 0 ||
                   a->rope_dim > kv->pool.head_dim))
     return PS_ERR_INVALID_ARG;
+  // q_out is q, or lies on none of the inputs: warps read ahead of what others write
+  const Pool& p = kv->pool;
+  const int64_t T = a->num_tokens, hq = p.q_heads, hk = p.kv_heads, dim = p.head_dim;
+  const HeadRuns q = runs(a->q, a->q_stride, hq), out = runs(a->q_out, a->q_out_stride, hq);
+  const bool in_place = q.p == out.p && (T == 1 || q.s0 == out.s0) && (hq == 1 || q.s1 == out.s1);
+  if (heads_overlap(out, out, T, dim, true) || (!in_place && heads_overlap(out, q, T, dim)) ||
+      heads_overlap(out, runs(a->k, a->k_stride, hk), T, dim) || heads_overlap(out, runs(a->v, a->v_stride, hk), T, dim))
+    return PS_ERR_INVALID_ARG;
   return launch_append(kv->pool, layer, *a, d_status, kv->nsm, as_stream(stream));
 }
 
@@ -232,6 +242,10 @@ int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_at
   if (kv->batch.num_tokens == 0 || kv->batch.num_requests == 0) return PS_OK;
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) || !good_strides(a->q_stride) ||
       !good_strides(a->out_stride) || !(a->scale - a->scale == 0))
+    return PS_ERR_INVALID_ARG;
+  const HeadRuns q = runs(a->q, a->q_stride, kv->pool.q_heads), out = runs(a->out, a->out_stride, kv->pool.q_heads);
+  if (heads_overlap(out, out, kv->batch.num_tokens, kv->pool.head_dim, true) ||
+      heads_overlap(out, q, kv->batch.num_tokens, kv->pool.head_dim))
     return PS_ERR_INVALID_ARG;
   return launch_attention(kv->pool, kv->maps[layer], kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
 }

@@ -410,3 +410,26 @@ def test_attention_before_its_captured_plan_has_run_writes_nothing():
     pool.attention(0, q, 0.125, out=out)
     pool.check()
     assert torch.equal(out, want)
+
+
+def test_outputs_on_their_queries_are_refused():
+    """An output shares no element with the queries, nor with itself; among them it may lie."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 12, 16, 2, 64, BF, seed=5)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    pool = KV.KVPool(k, v, num_q_heads=4, max_requests=2, max_tokens=21, max_row_pages=4)
+    pool.plan(dev([0, 1, 21]), dev([40, 60]), torch.arange(8, device="cuda", dtype=torch.int32).view(2, 4), 21)
+    both = torch.randn(23, 8, 64, device="cuda").to(BF)
+    q = both[:21, :4]
+    want = pool.attention(0, q.clone(), 0.125)
+    flat = both.view(-1)
+    shifted = torch.as_strided(both, (21, 4, 64), (512, 64, 1), 8)
+    steps = torch.as_strided(both, (21, 4, 64), (256, 64, 1), 0)
+    before = both.clone()
+    for bad in (q, shifted, both[1:22, :4], both[:21, 3:7], steps, flat[:64].expand(21, 4, 64), both[2:3, 4:].expand(21, 4, 64)):
+        with pytest.raises(RuntimeError, match="invalid"):
+            pool.attention(0, q, 0.125, out=bad)
+    assert torch.equal(both, before)
+    for good in (both[:21, 4:], both[2:, 4:]):
+        assert torch.equal(pool.attention(0, q, 0.125, out=good), want)
+    pool.check()

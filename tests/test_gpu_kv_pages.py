@@ -152,6 +152,25 @@ def test_append_refusals():
         pool.append(1, x, x, x, s)
 
 
+def test_append_refuses_queries_that_lie_on_its_inputs():
+    """q_out is q itself or shares no element with q, k or v."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 4, 16, 2, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=4)
+    qkv = torch.randn(22, 12, 64, device="cuda").to(BF)  # four spare heads
+    q, nk, nv, s = qkv[:21, :4], qkv[:21, 4:6], qkv[:21, 6:8], dev(range(21), torch.int64)
+    weight = dict(q_weight=torch.ones(64, device="cuda", dtype=BF))
+    before, want = qkv.clone(), pool.append(0, q.clone(), nk.clone(), nv.clone(), s, **weight)
+    for bad in (qkv[1:, :4], qkv[:21, 1:5], qkv[:21, 2:6], qkv[:21, 5:9], torch.as_strided(qkv, (21, 4, 64), (768, 64, 1), 16),
+                torch.as_strided(qkv, (21, 4, 64), (256, 64, 1), 0), qkv[:1, 8:].expand(21, 4, 64)):
+        with pytest.raises(RuntimeError, match="invalid"):
+            pool.append(0, q, nk, nv, s, q_out=bad, **weight)
+    assert torch.equal(qkv, before)
+    assert torch.equal(pool.append(0, q, nk, nv, s, q_out=qkv[1:, 8:], **weight), want)
+    assert torch.equal(pool.append(0, q, nk, nv, s, q_out=q, **weight), want)
+    pool.check()
+
+
 # ---- pages ------------------------------------------------------------------------
 def rows_in_use(rows, spare, most, ps, first, pages, seed):
     """Rows of up to ``most`` tokens with cached and private pages, some held by two rows."""
