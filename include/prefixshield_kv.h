@@ -128,12 +128,12 @@ typedef struct {
   int32_t rope_rows;
   int32_t rope_dim;          /* rotated leading elements of a head: a multiple of 8, at most head_dim */
   int32_t rope_interleaved;  /* pairs (2i, 2i + 1) instead of (i, i + rope_dim / 2) */
-  int32_t pad0;
+  int32_t fill;              /* nonzero: q_out of a token that is left out becomes NaN (for memory that nothing wrote before) */
 } ps_kv_append_t;
 
 /* Append to layer 'layer'.  A token whose slot is past the pool or whose
- * position is outside the table is left out (its q_out, K and V stay as they
- * were) and *d_status becomes PS_ERR_INVALID_ARG. */
+ * position is outside the table is left out (its q_out, but for 'fill', K and V
+ * stay as they were) and *d_status becomes PS_ERR_INVALID_ARG. */
 int32_t ps_kv_append(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_append_t* a, int32_t* d_status);
 
 /* A batch of requests.  Request i's queries are the rows [q_offsets[i],
@@ -164,7 +164,7 @@ typedef struct {
  * the work into equal parts.  One plan serves every layer of a step; the
  * batch's arrays must stay unchanged until the last ps_kv_attention() of the
  * plan has run.  Bad offsets, lengths or page ids make *d_status
- * PS_ERR_INVALID_ARG and the plan empty: attention on it writes nothing.  Until
+ * PS_ERR_INVALID_ARG and the plan empty: attention on it writes nothing (but for 'fill').  Until
  * the first plan has run (a captured one runs when its graph does) it is empty, too. */
 int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* batch, int32_t* d_status);
 
@@ -181,7 +181,7 @@ typedef struct {
   float* lse;
   int64_t q_stride[2], out_stride[2]; /* token, head; in elements */
   float scale;
-  int32_t pad0;
+  int32_t fill; /* nonzero: after an empty plan out becomes NaN (for memory that nothing wrote before) */
 } ps_kv_attention_t;
 int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_attention_t* a, int32_t* d_status);
 

@@ -106,7 +106,7 @@ class PsKvAppend(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out")] + [
         (n, C.c_int64 * 2) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")] + [
         (n, C.c_void_p) for n in ("slots", "positions", "rope", "q_weight", "k_weight")] + [("eps", C.c_float)] + [
-        (n, C.c_int32) for n in ("num_tokens", "rope_rows", "rope_dim", "rope_interleaved", "pad0")]
+        (n, C.c_int32) for n in ("num_tokens", "rope_rows", "rope_dim", "rope_interleaved", "fill")]
 
 
 class PsKvBatch(C.Structure):
@@ -116,7 +116,7 @@ class PsKvBatch(C.Structure):
 
 class PsKvAttention(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + [
-        (n, C.c_int64 * 2) for n in ("q_stride", "out_stride")] + [("scale", C.c_float), ("pad0", C.c_int32)]
+        (n, C.c_int64 * 2) for n in ("q_stride", "out_stride")] + [("scale", C.c_float), ("fill", C.c_int32)]
 
 
 class PsKvRows(C.Structure):

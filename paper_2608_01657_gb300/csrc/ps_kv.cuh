@@ -251,6 +251,7 @@ struct Num;
 template <>
 struct Num<__nv_bfloat16> {
   static constexpr bool kBf16 = true;
+  static constexpr uint32_t kNan2 = 0x7FC07FC0u;
   static __device__ __forceinline__ float2 unpack(uint32_t x) {
     return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
   }
@@ -263,6 +264,7 @@ struct Num<__nv_bfloat16> {
 template <>
 struct Num<__half> {
   static constexpr bool kBf16 = false;
+  static constexpr uint32_t kNan2 = 0x7E007E00u;
   static __device__ __forceinline__ float2 unpack(uint32_t x) {
     return __half22float2(*reinterpret_cast<const __half2*>(&x));
   }

@@ -14,7 +14,7 @@ struct AppendArgs {
   int32_t* status;
   int64_t qs[2], ks[2], vs[2], os[2];       // strides in elements
   int64_t page_stride, token_stride, head_stride, nslots;
-  int32_t T, hq, hk, dim, page_log2, rope_rows, rope_dim;
+  int32_t T, hq, hk, dim, page_log2, rope_rows, rope_dim, fill;
   float eps;
 };
 
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_append(AppendArgs a) {
     const int h = (query ? s : s - nq) * H + grp;
     const bool value = !query && h >= a.hk;
     char* dst = nullptr;
-    if (query && h < a.hq && valid) dst = a.qo + 2 * (t * a.os[0] + h * a.os[1]);
+    if (query && h < a.hq && (valid || a.fill)) dst = a.qo + 2 * (t * a.os[0] + h * a.os[1]);
     if (!query && h < 2 * a.hk && at >= 0) dst = (value ? a.pv - 2 * a.hk * a.head_stride : a.pk) + at + 2 * h * a.head_stride;
     if (!__all_sync(0xFFFFFFFFu, value)) {
       const bool weight = query ? a.qw != nullptr : a.kw != nullptr;
@@ -266,6 +266,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_append(AppendArgs a) {
         raw[0] = y[0];
         raw[1] = y[1];
       }
+    }
+    if (!valid && query) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) raw[0].x[j] = raw[1].x[j] = Num<T>::kNan2;
     }
     if (dst && on0) write_part<E>(dst + at0, raw[0]);
     if (dst && on1) write_part<E>(dst + at1, raw[1]);
@@ -324,6 +328,7 @@ int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& in, in
   a.nslots = p.num_pages << p.page_log2;
   a.T = in.num_tokens; a.hq = p.q_heads; a.hk = p.kv_heads; a.dim = p.head_dim; a.page_log2 = p.page_log2;
   a.rope_rows = in.rope_rows; a.rope_dim = a.rope ? in.rope_dim : 0; a.eps = in.eps;
+  a.fill = in.fill;
   return status_of(p.dtype == PS_KV_BF16 ? launch_t<__nv_bfloat16>(a, in.rope_interleaved != 0, nsm, st)
                                          : launch_t<__half>(a, in.rope_interleaved != 0, nsm, st));
 }

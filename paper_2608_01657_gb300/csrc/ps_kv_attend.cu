@@ -585,6 +585,16 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 16 / kJoinWarps) k_attend_joi
   bool waited = false;
   if (h.x != PS_OK) {
     chain();
+    if (a.fill) {
+      const int words = a.pool.head_dim / 8;
+      const int64_t n = (int64_t)a.num_tokens * a.pool.q_heads * words;
+      for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / words;
+        char* p = a.out + 2 * (row / a.pool.q_heads * a.out_stride[0] + row % a.pool.q_heads * a.out_stride[1]);
+        constexpr uint32_t x = Num<T>::kNan2;
+        reinterpret_cast<uint4*>(p)[i % words] = make_uint4(x, x, x, x);
+      }
+    }
     return;
   }
   const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
@@ -656,6 +666,8 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   a.q_offsets = b.q_offsets;
   a.kv_lens = b.kv_lens;
   a.causal = b.causal;
+  a.fill = in.fill;
+  a.num_tokens = b.num_tokens;
   a.status = status;
   a.scale2 = in.scale * 1.4426950408889634f;
   // no tile has more rows than the whole batch

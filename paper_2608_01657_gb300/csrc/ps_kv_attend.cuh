@@ -21,6 +21,7 @@ struct AttendArgs {
   int32_t* status;
   int32_t after_wide;  // the wide tiles' kernel was launched
   int32_t causal;
+  int32_t fill, num_tokens;  // the outputs' rows become NaN after an empty plan
   float scale2;  // scale log2(e)
 };
 

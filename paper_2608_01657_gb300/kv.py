@@ -166,9 +166,11 @@ class KVPool:
         """Norm (with ``q_weight`` / ``k_weight``) and rotation (with ``rope``
         [rows, rope_dim] float32: cosines, then sines) of the new tokens'
         queries and keys; keys and values go to ``slots`` (page * page_size +
-        offset, int64; negative: not written).  Returns the queries."""
+        offset, int64; negative: not written).  Returns the queries, NaN where a
+        token was left out and ``q_out`` not given."""
         a, st = self._append_args, self._append_strides
         T = q.shape[0]
+        a.fill = q_out is None
         if q_out is None:
             q_out = B._made((T, self.q_heads, self.head_dim), self.dtype, self.device, stream)
         a.q = self._heads(q, T, self.q_heads, "q", st[0])
@@ -221,13 +223,16 @@ class KVPool:
 
     def attention(self, layer: int, q, scale: float, out=None, lse=None, stream=None):
         """softmax(scale q k^T) v of one layer for the planned batch.  ``lse``
-        (optional, float32 [tokens, q_heads]) receives the scores' log-sum-exp."""
+        (optional, float32 [tokens, q_heads]) receives the scores' log-sum-exp.
+        If the plan was found bad, nothing is written; an output that was not
+        given is NaN then."""
         if self._batch is None:
             raise ValueError("attention needs a plan")
         T = self._batch[4]
+        a, st = self._attention_args, self._attention_strides
+        a.fill = out is None
         if out is None:
             out = B._made((T, self.q_heads, self.head_dim), self.dtype, self.device, stream)
-        a, st = self._attention_args, self._attention_strides
         a.q = self._heads(q, T, self.q_heads, "q", st[0])
         a.out = self._heads(out, T, self.q_heads, "out", st[1])
         a.scale = scale

@@ -433,3 +433,26 @@ def test_outputs_on_their_queries_are_refused():
     for good in (both[:21, 4:], both[2:, 4:]):
         assert torch.equal(pool.attention(0, q, 0.125, out=good), want)
     pool.check()
+
+
+def test_outputs_that_nothing_wrote_are_nan():
+    """After a bad plan an output that the call made holds NaN, not what the memory held before."""
+    from paper_2608_01657_gb300 import kv as KV
+    for dtype, dim, T in ((BF, 128, 300), (HF, 72, 3), (BF, 8, 1)):
+        k, v = make_pool(1, 20, 16, 2, dim, dtype)
+        dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+        pool = KV.KVPool(k, v, num_q_heads=6, max_requests=1, max_tokens=T, max_row_pages=20)
+        q = torch.randn(T, 6, dim, device="cuda").to(dtype)
+        tables = torch.arange(20, device="cuda", dtype=torch.int32).view(1, 20)
+        pool.plan(dev([0, T]), dev([321]), tables, T)
+        for stream in (None, torch.cuda.Stream()):
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream or torch.cuda.current_stream()):
+                del_me = torch.full_like(q, 7.0)
+                del del_me
+            assert torch.isnan(pool.attention(0, q, 0.1, stream=stream)).all()
+        with pytest.raises(RuntimeError):
+            pool.check()
+        pool.plan(dev([0, T]), dev([320]), tables, T)
+        assert torch.isfinite(pool.attention(0, q, 0.1)).all()
+        pool.check()

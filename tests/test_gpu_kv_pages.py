@@ -120,6 +120,24 @@ def test_append_leaves_out_bad_tokens_and_reports_them():
         assert torch.equal(k[0, 0, 5], before[0, 0, 5]) and not torch.equal(k[0, 0, :3], before[0, 0, :3])
 
 
+@pytest.mark.parametrize("dtype,dim,rope_dim", [(BF, 128, 128), (HF, 64, 0), (BF, 40, 24), (HF, 8, 8)])
+def test_queries_that_append_left_out_are_nan(dtype, dim, rope_dim):
+    """In an output that the call made; the other tokens' queries are what they are."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 4, 16, 3, dim, dtype)
+    pool = KV.KVPool(k, v, num_q_heads=9)
+    q, kv = torch.randn(6, 9, dim, device="cuda").to(dtype), torch.randn(6, 3, dim, device="cuda").to(dtype)
+    extra = dict(positions=dev(range(6)), rope=rope_table(10, rope_dim)) if rope_dim else {}
+    want = pool.append(0, q, kv, kv, dev([0, 5, 1, 2, 3, -1], torch.int64), **extra)
+    pool.check()
+    del_me = torch.full_like(q, 7.0)
+    del del_me
+    got = pool.append(0, q, kv, kv, dev([64, 5, 1, 1 << 40, 3, -1], torch.int64), **extra)
+    with pytest.raises(RuntimeError):
+        pool.check()
+    assert torch.isnan(got[[0, 3]]).all() and torch.equal(got[[1, 2, 4, 5]], want[[1, 2, 4, 5]])
+
+
 def test_append_zero_heads_of_zeros():
     """A head of zeros stays zero under the norm."""
     from paper_2608_01657_gb300 import kv as KV
