@@ -558,8 +558,13 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         }
       }
       if (direct) {
+        // (the last columns may be past the products' and hold anything)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) z = spoil(z, x[e]);
+        for (int e = 0; e < 32; e += 8)
+          if (j + e < a.pool.head_dim) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z = spoil(z, x[e + i]);
+          }
         uint32_t w[4][4];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) w[e >> 3][(e >> 1) & 3] = Num<T>::pack(x[e] * inv, x[e + 1] * inv);

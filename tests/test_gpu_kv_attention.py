@@ -456,3 +456,29 @@ def test_outputs_that_nothing_wrote_are_nan():
         pool.plan(dev([0, T]), dev([320]), tables, T)
         assert torch.isfinite(pool.attention(0, q, 0.1)).all()
         pool.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [72, 80])
+@pytest.mark.parametrize("new", [20, 70])
+def test_finite_rows_are_not_looked_at_again(new, dim, dtype):
+    """Tiles that write their own outputs leave no mark in the workspace: none of their numbers is
+    taken for one that is not finite, whatever earlier calls left on the SMs."""
+    from paper_2608_01657_gb300 import kv as KV
+    R, heads, ratio, ps = 40, 8, 3, 16
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    tables = torch.arange(R * 8, device="cuda", dtype=torch.int32).view(R, 8)
+    offsets, lens = dev(np.arange(R + 1) * new), dev([new + i for i in range(R)])
+    for d, fill in ((128, math.nan), (dim, None)):
+        k, v = make_pool(1, R * 8, ps, heads, d, dtype, seed=d)
+        if fill is not None:
+            v.fill_(fill)
+        q = torch.randn(R * new, heads * ratio, d, device="cuda").to(dtype)
+        pool = KV.KVPool(k, v, num_q_heads=heads * ratio, max_requests=R, max_tokens=R * new, max_row_pages=8)
+        pool.workspace.zero_()
+        pool.plan(offsets, lens, tables, R * new)
+        before = pool.workspace.clone()
+        out = pool.attention(0, q, 0.1)
+        pool.check()
+        assert torch.isnan(out).all() if fill is not None else torch.isfinite(out).all()
+    assert torch.equal(pool.workspace, before)
