@@ -16,11 +16,12 @@ constexpr int kShareTokens = 128;
 
 // Cycles of one unit as the division weighs them: a wide one on its SM (128
 // keys; 2800 measured for prompts, 3900 beside narrow tiles, up to 5900 where a
-// tile has one or two units), a narrow one in its warp (16 keys of 128 elements)
-// when loads wait on latency alone, and when all warps share the HBM bandwidth.
-// Measured over 4000 to 7800 and 1900 to 3400: 256 tenants' decode 366 to 420 us
-// (371 as it stands), 128 requests on one prefix 75 to 88 (76).
-constexpr double kWideCycles = 5250, kNarrowCycles = 2400, kNarrowBandwidth = 2400;
+// tile has one or two units), a narrow one in its warp (16 keys).  Both are those
+// of heads of 128 elements and are used for all, so the division of the SMs does
+// not follow the head's size.  Measured over 4000 to 7800 and 1900 to 3400: 256
+// tenants' decode 366 to 420 us (371 as it stands), 128 requests on one prefix 75
+// to 88 (76).
+constexpr double kWideCycles = 5250, kNarrowCycles = 2400;
 // A narrow worker has at least so many units: more workers would cost the join
 // more than they save (one request of 700 keys, 8 heads: 10.6 us a call with 2,
 // 9.9 with 4, 10.9 with 5, 12.0 with 8; 33 requests of up to 7 tokens 17.2 and 16.8).
@@ -269,10 +270,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   if (tid <= sms) {
     const bool can = (tid > 0 || units[1] == 0) && (tid < sms || units[0] == 0);
     const double wide = units[1] > 0 && tid > 0 ? (double)units[1] * kWideCycles / tid : 0;
-    const double fast = units[0] > 0 && tid < sms ? (double)units[0] * kNarrowCycles / (per_sm * (sms - tid)) : 0;
-    const double bytes = (double)units[0] * kNarrowBandwidth * p.head_dim / (128 * per_sm * sms);
-    const double t = fmax(wide, fmax(fast, bytes));
-    if (can) atomicMin(&s_best, (unsigned long long)t << 10 | tid);
+    const double narrow = units[0] > 0 && tid < sms ? (double)units[0] * kNarrowCycles / (per_sm * (sms - tid)) : 0;
+    if (can) atomicMin(&s_best, (unsigned long long)fmax(wide, narrow) << 10 | tid);
   }
   __syncthreads();
   const int wide_sms = (int)(s_best & 1023);
@@ -320,7 +319,7 @@ __device__ __forceinline__ Parts4 parts_of(const Plan& plan, const Pool& p, cons
   const Tile& t = plan.tiles[list][tile];
   Parts4 r;
   r.count = t.sidx < 0 && ca == cb ? 0 : cb - ca + 1;  // a whole one is written where it is computed
-  r.first = (int)part_row<H>(t.sidx, t.nrows, head, ca, U * ca / C > ua, C);
+  r.first = (int)part_row<H>(t.sidx, t.nrows, head, ca, false, C);  // worker ca begins the (tile, head): unit 0 is its
   r.second = (int)part_row<H>(t.sidx, t.nrows, head, ca + 1, true, C);
   r.stride = t.sidx < 0 ? 2 * H : H;
   return r;
