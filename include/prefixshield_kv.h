@@ -193,6 +193,7 @@ int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, c
 /* The sequences of the page calls: row r holds held[r] pages, ids
  * tables[r * table_stride ...], with lens[r] tokens written.  refs[id -
  * first_page] counts the rows that hold a private page; 0 means free.
+ * Where a pool has no private pages the references may be NULL.
  * num_rows may exceed max_requests. */
 typedef struct {
   int32_t* tables;

@@ -125,6 +125,10 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
 // bounded by the device's at ps_kv_create().
 constexpr int32_t kSizedWorkers[kLists] = {kMaxSms * 4 * kNarrowWarps, kMaxSms};
 
+// References to private pages: none are needed, and an empty array may have no address, where there are no such pages.
+bool refs_ok(const ps_kv* kv, const int32_t* in, const int32_t* out) {
+  return (in && out) || kv->pool.first_page == kv->pool.num_pages;
+}
 bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
   return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
 }
@@ -260,7 +264,7 @@ int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, c
 int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parents, const int32_t* d_children,
                    const int32_t* d_room, const ps_kv_rows_t* rows, const int32_t* d_refs_in, int32_t* d_refs_out,
                    int32_t* d_status) {
-  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !d_refs_in || !d_refs_out) return PS_ERR_INVALID_ARG;
+  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !refs_ok(kv, d_refs_in, d_refs_out)) return PS_ERR_INVALID_ARG;
   if (n > 0 && (!d_parents || !d_children || !d_room)) return PS_ERR_INVALID_ARG;
   return launch_fork(kv->pool, kv->pages, n, d_parents, d_children, d_room, *rows, row_pages(kv, rows->table_stride),
                      d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
@@ -268,7 +272,7 @@ int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parent
 
 int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_rows, const ps_kv_rows_t* rows,
                       int32_t* d_refs, int32_t* d_status) {
-  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !d_refs || (n > 0 && !d_rows))
+  if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !refs_ok(kv, d_refs, d_refs) || (n > 0 && !d_rows))
     return PS_ERR_INVALID_ARG;
   if (n == 0) return PS_OK;
   return launch_release(kv->pool, n, d_rows, *rows, row_pages(kv, rows->table_stride), d_refs, d_status,
@@ -277,8 +281,8 @@ int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_row
 
 int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
                       int32_t* d_tables_out, int32_t* d_refs_out, int32_t* d_counts, int32_t* d_status) {
-  if (!kv || !rows || !rows->tables || !rows->held || rows->num_rows < 1 || rows->table_stride < 1 || !d_refs_in ||
-      !d_tables_out || !d_refs_out || !d_counts)
+  if (!kv || !rows || !rows->tables || !rows->held || rows->num_rows < 1 || rows->table_stride < 1 ||
+      !refs_ok(kv, d_refs_in, d_refs_out) || !d_tables_out || !d_counts)
     return PS_ERR_INVALID_ARG;
   return launch_compact(kv->pool, kv->pages, *rows, d_refs_in, d_tables_out, d_refs_out, d_counts, d_status, kv->nsm,
                         as_stream(stream));

@@ -386,6 +386,27 @@ def test_bad_releases_are_reported():
         assert r[:3].tolist() == after
 
 
+def test_page_calls_on_a_pool_without_private_pages():
+    """The references are an empty array: cached pages are shared, released and left where they are."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 8, 16, 1, 64, BF)
+    before = k.clone()
+    pool = KV.KVPool(k, v, num_q_heads=1, first_page=8, max_requests=4, max_row_pages=4)
+    t, l, h, r = dev([[5, 2, 7, -1], [-1] * 4, [-1] * 4]), dev([48, 0, 0]), dev([3, 0, 0]), dev([])
+    pool.fork(dev([0, -1]), dev([1, 2]), dev([48, 0]), t, l, h, r)
+    pool.check()
+    assert t.tolist() == [[5, 2, 7, -1], [5, 2, 7, -1], [-1] * 4] and l.tolist() == [48, 48, 0] and h.tolist() == [3, 3, 0]
+    to = torch.full_like(t, 77)
+    assert pool.compact(t, h, r, tables_out=to).tolist() == [0, 0] and torch.equal(to, t)
+    pool.release(dev([0]), t, l, h, r)
+    pool.check()
+    assert h.tolist() == [0, 3, 0] and torch.equal(k, before)
+    pool.fork(dev([1]), dev([1]), dev([49]), t, l, h, r)  # there is no page to grow into
+    with pytest.raises(RuntimeError, match="capacity"):
+        pool.check()
+    assert h.tolist() == [0, 3, 0]
+
+
 def test_many_forks_of_one_row_and_a_large_pool():
     """More chunks of the reference array than one, more items than CTAs at once."""
     b = Both(3, 500, 400, pages=9000, first=1, layers=1, heads=1, dim=8, seed=8)
