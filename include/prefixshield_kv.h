@@ -155,7 +155,7 @@ typedef struct {
   const int32_t* group_offsets; /* [num_groups + 1] or NULL */
   int64_t table_stride;         /* elements between rows; a row holds min(table_stride, max_row_pages) ids */
   int32_t num_requests;
-  int32_t num_groups;
+  int32_t num_groups;           /* 1..num_requests; not looked at in a batch of no requests */
   int32_t num_tokens;
   int32_t causal;
 } ps_kv_batch_t;

@@ -227,9 +227,11 @@ int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* b, int32_t* d
     return PS_ERR_INVALID_ARG;
   if (b->num_requests > 0 && (!b->q_offsets || !b->kv_lens || (!b->tables && b->table_stride > 0)))
     return PS_ERR_INVALID_ARG;
-  if (b->group_offsets && (b->num_groups < 1 || b->num_groups > b->num_requests)) return PS_ERR_INVALID_ARG;
+  const bool grouped = b->group_offsets && b->num_requests > 0;  // an empty batch has nothing to group
+  if (grouped && (b->num_groups < 1 || b->num_groups > b->num_requests)) return PS_ERR_INVALID_ARG;
   Batch x{};
-  x.q_offsets = b->q_offsets; x.kv_lens = b->kv_lens; x.tables = b->tables; x.group_offsets = b->group_offsets;
+  x.q_offsets = b->q_offsets; x.kv_lens = b->kv_lens; x.tables = b->tables;
+  x.group_offsets = grouped ? b->group_offsets : nullptr;
   x.table_stride = b->table_stride;
   x.num_requests = b->num_requests; x.num_groups = b->num_groups; x.num_tokens = b->num_tokens;
   x.causal = b->causal != 0;

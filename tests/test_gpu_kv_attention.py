@@ -482,3 +482,20 @@ def test_finite_rows_are_not_looked_at_again(new, dim, dtype):
         pool.check()
         assert torch.isnan(out).all() if fill is not None else torch.isfinite(out).all()
     assert torch.equal(pool.workspace, before)
+
+
+@pytest.mark.parametrize("groups", [None, [0], [0, 0]])
+def test_a_batch_of_no_requests(groups):
+    """A step in which nobody has anything to say, grouped or not."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 8, 16, 2, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=4, max_requests=2, max_tokens=4, max_row_pages=4)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = torch.zeros(0, 4, dtype=torch.int32, device="cuda")
+    pool.plan(dev([0]), dev([]), none, 0, group_offsets=None if groups is None else dev(groups))
+    assert pool.attention(0, torch.zeros(0, 4, 64, device="cuda", dtype=BF), 0.125).shape == (0, 4, 64)
+    pool.check()
+    with pytest.raises(RuntimeError):
+        pool.plan(dev([0, 1]), dev([1]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 1, group_offsets=dev([0]))
+    with pytest.raises(RuntimeError):
+        pool.plan(dev([0, 1]), dev([1]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 1, group_offsets=dev([0, 0, 1]))
