@@ -225,6 +225,7 @@ int32_t ps_kv_plan(ps_kv_t* kv, void* stream, const ps_kv_batch_t* b, int32_t* d
   if (b->num_requests < 0 || b->num_requests > kv->max_requests || b->num_tokens < 0 ||
       b->num_tokens > kv->max_tokens || b->table_stride < 0)
     return PS_ERR_INVALID_ARG;
+  if (b->num_requests == 0 && b->num_tokens > 0) return PS_ERR_INVALID_ARG;
   if (b->num_requests > 0 && (!b->q_offsets || !b->kv_lens || (!b->tables && b->table_stride > 0)))
     return PS_ERR_INVALID_ARG;
   const bool grouped = b->group_offsets && b->num_requests > 0;  // an empty batch has nothing to group

@@ -140,7 +140,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan_tiles(Pool p, Plan plan, 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int bad = 0;
   for (int r = tid; r < b.num_requests; r += kPlanThreads) bad |= plan.bad[r];
-  if (b.num_requests == 0) bad |= b.num_tokens != 0;
   if (b.group_offsets) {
     for (int g = tid; g < b.num_groups; g += kPlanThreads) bad |= b.group_offsets[g] > b.group_offsets[g + 1];
     if (tid == 0) bad |= b.group_offsets[0] != 0 || b.group_offsets[b.num_groups] != b.num_requests;

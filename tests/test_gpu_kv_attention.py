@@ -499,3 +499,16 @@ def test_a_batch_of_no_requests(groups):
         pool.plan(dev([0, 1]), dev([1]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 1, group_offsets=dev([0]))
     with pytest.raises(RuntimeError):
         pool.plan(dev([0, 1]), dev([1]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), 1, group_offsets=dev([0, 0, 1]))
+
+
+def test_tokens_without_requests_are_refused():
+    """On the host: attention of such a batch would run nothing at all."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 8, 16, 2, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=4, max_requests=2, max_tokens=4, max_row_pages=4)
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    with pytest.raises(RuntimeError, match="ps_kv_plan"):
+        pool.plan(dev([0]), dev([]), torch.zeros(0, 4, dtype=torch.int32, device="cuda"), 3)
+    with pytest.raises(ValueError):
+        pool.attention(0, torch.zeros(3, 4, 64, device="cuda", dtype=BF), 0.125)
+    pool.check()
