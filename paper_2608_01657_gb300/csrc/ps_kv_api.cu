@@ -36,6 +36,11 @@ bool check_config(const ps_kv_config_t* c) {
       c->num_q_heads > PS_KV_MAX_HEADS || c->num_q_heads % c->num_kv_heads != 0)
     return false;
   if (c->head_dim < 8 || c->head_dim > PS_KV_MAX_HEAD_DIM || c->head_dim % 8 != 0) return false;
+  // an axis of several places steps over a head's elements at least, or elements share addresses
+  const struct { int64_t places, stride; } axes[] = {{c->num_layers, c->layer_stride}, {c->num_pages, c->page_stride},
+                                                     {ps, c->token_stride}, {c->num_kv_heads, c->head_stride}};
+  for (const auto& x : axes)
+    if (x.places > 1 && x.stride < c->head_dim) return false;
   if (c->dtype != PS_KV_BF16 && c->dtype != PS_KV_F16) return false;
   if (c->max_requests < 1 || c->max_requests > PS_MAX_REQUESTS_PER_STEP) return false;
   if (c->max_tokens < 1 || c->max_tokens > (1 << 22) || (int64_t)c->max_tokens * c->num_q_heads >= (1ll << 30))

@@ -98,3 +98,16 @@ def test_null_and_misaligned_arguments_are_refused(B):
     assert L.ps_kv_compact(None, None, C.byref(B.PsKvRows()), None, None, None, None, None) == bad
     assert L.ps_step_blocks(None, None, 0, None, None, 0, None, None) == bad
     L.ps_kv_destroy(None)
+
+
+@pytest.mark.parametrize("bad", [dict(head_stride=0), dict(token_stride=0), dict(page_stride=0), dict(head_stride=56),
+                                 dict(page_stride=32), dict(num_layers=2, layer_stride=0), dict(num_layers=3, layer_stride=8)])
+def test_pools_whose_elements_share_addresses_have_no_size(B, bad):
+    """An axis of several places steps over a head's elements at least (an expanded tensor does not)."""
+    assert size(B, **bad) == 0
+
+
+def test_axes_of_one_place_may_have_any_stride(B):
+    base = size(B)
+    assert size(B, layer_stride=0) == base and size(B, num_pages=1, first_page=1, page_stride=0) > 0
+    assert size(B, num_kv_heads=1, head_stride=0) > 0
