@@ -558,10 +558,10 @@ __device__ __forceinline__ bool softmax_role(const AttendArgs& a, Shared* sh, ui
         }
       }
       if (direct) {
-        // (the last columns may be past the products' and hold anything)
+        // (where DP is not whole times 32 the last columns are past the products' and hold anything)
 #pragma unroll
         for (int e = 0; e < 32; e += 8)
-          if (j + e < a.pool.head_dim) {
+          if (DP % 32 == 0 || j + e < DP) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) z = spoil(z, x[e + i]);
           }
