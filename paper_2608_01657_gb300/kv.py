@@ -51,6 +51,7 @@ class KVPool:
         _need(k.dtype in (torch.bfloat16, torch.float16), "a pool is bfloat16 or float16")
         _need(k.stride(4) == 1, "the innermost stride must be 1")
         self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self._index = self.device.index
         self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim = (int(x) for x in k.shape)
         self.q_heads, self.first_page = int(num_q_heads), int(first_page)
         self.max_requests, self.max_tokens, self.max_row_pages = int(max_requests), int(max_tokens), int(max_row_pages)
@@ -103,7 +104,7 @@ class KVPool:
     def check(self):
         """Raise if a call's device work reported an error; clears it (synchronizes:
         the device, if calls were made on other streams than the current one)."""
-        elsewhere = any(raw != _raw_stream(self.device.index) for raw in self._used)
+        elsewhere = any(raw != _raw_stream(self._index) for raw in self._used)
         if elsewhere:
             torch.cuda.synchronize(self.device)
         rc = int(self.status.item())
@@ -118,7 +119,7 @@ class KVPool:
         """The raw handle of a call's stream.  What the handle keeps (the pool, the
         workspace, the status) is recorded on each stream that it is used on, so
         that its memory outlives the work there."""
-        raw = _raw_stream(self.device.index) if stream is None else B._stream_ptr(stream)
+        raw = _raw_stream(self._index) if stream is None else B._stream_ptr(stream)
         if raw not in self._used:
             self._used[raw] = B._stream_object(raw, self.device)
             self._record(raw, self.k, self.v, self.workspace, self.status)
@@ -129,16 +130,9 @@ class KVPool:
             if t is not None:
                 t.record_stream(self._used[raw])
 
-    def _done(self, name, rc, stream, raw, *tensors):
-        """The end of a call: its error, or its arguments recorded on the stream that it named."""
-        if rc:
-            self._raise(name, rc)
-        if stream is not None:
-            self._record(raw, *tensors)
-
     def _heads(self, t, tokens: int, heads: int, name: str, strides):
         """Checks [tokens, heads, head_dim]; its strides go to ``strides``."""
-        if t.shape != (tokens, heads, self.head_dim) or t.dtype is not self.dtype or t.device != self.device:
+        if t.shape != (tokens, heads, self.head_dim) or t.dtype is not self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name} must be {self.dtype} [{tokens}, {heads}, {self.head_dim}] on {self.device}")
         s0, s1, s2 = t.stride()
         # an axis of one element is never stepped over: its stride may be any number
@@ -151,7 +145,7 @@ class KVPool:
 
     def _array(self, t, dtype, name: str, n: Optional[int] = None):
         sh = t.shape
-        if len(sh) != 1 or t.dtype is not dtype or t.device != self.device or not t.is_contiguous() or (
+        if len(sh) != 1 or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous() or (
                 n is not None and sh[0] != n):
             raise ValueError(f"{name} must be a contiguous {dtype} array" + ("" if n is None else f" of {n}"))
         return t.data_ptr()
@@ -195,7 +189,10 @@ class KVPool:
         a.eps, a.num_tokens = eps, T
         raw = self._stream(stream)
         rc = self._lib.ps_kv_append(self._h, raw, layer, self._append_ref, self._status)
-        self._done("ps_kv_append", rc, stream, raw, q, k, v, slots, positions, rope, q_weight, k_weight, q_out)
+        if rc:
+            self._raise("ps_kv_append", rc)
+        if stream is not None:
+            self._record(raw, q, k, v, slots, positions, rope, q_weight, k_weight, q_out)
         return q_out
 
     # -- attention -------------------------------------------------------------
@@ -247,7 +244,10 @@ class KVPool:
             self._batch_used.add(raw)
             self._record(raw, *self._batch[:4])
         rc = self._lib.ps_kv_attention(self._h, raw, layer, self._attention_ref, self._status)
-        self._done("ps_kv_attention", rc, stream, raw, q, out, lse)
+        if rc:
+            self._raise("ps_kv_attention", rc)
+        if stream is not None:
+            self._record(raw, q, out, lse)
         return out
 
     # -- pages -------------------------------------------------------------------
@@ -256,7 +256,10 @@ class KVPool:
         n, raw = src.shape[0], self._stream(stream)
         rc = self._lib.ps_kv_copy(self._h, raw, n, self._array(src, torch.int32, "src"),
                                   self._array(dst, torch.int32, "dst", n), self._status)
-        self._done("ps_kv_copy", rc, stream, raw, src, dst)
+        if rc:
+            self._raise("ps_kv_copy", rc)
+        if stream is not None:
+            self._record(raw, src, dst)
 
     def _rows(self, tables, lens, held):
         """Fills in the structure of the rows; returns the reference to pass."""
@@ -281,14 +284,20 @@ class KVPool:
             self._h, raw, n, self._array(parents, torch.int32, "parents"),
             self._array(children, torch.int32, "children", n), self._array(room, torch.int32, "room", n), rows,
             before, before if refs_out is None else self._refs(refs_out, "refs_out"), self._status)
-        self._done("ps_kv_fork", rc, stream, raw, parents, children, room, tables, lens, held, refs, refs_out)
+        if rc:
+            self._raise("ps_kv_fork", rc)
+        if stream is not None:
+            self._record(raw, parents, children, room, tables, lens, held, refs, refs_out)
 
     def release(self, rows, tables, lens, held, refs, stream=None):
         """Free the pages that ``rows`` hold."""
         r, raw = self._rows(tables, lens, held), self._stream(stream)
         rc = self._lib.ps_kv_release(self._h, raw, rows.shape[0], self._array(rows, torch.int32, "rows"), r,
                                      self._refs(refs), self._status)
-        self._done("ps_kv_release", rc, stream, raw, rows, tables, lens, held, refs)
+        if rc:
+            self._raise("ps_kv_release", rc)
+        if stream is not None:
+            self._record(raw, rows, tables, lens, held, refs)
 
     def compact(self, tables, held, refs, tables_out=None, refs_out=None, counts=None, stream=None):
         """Move the private pages in use to the lowest ids.  Returns the int32
@@ -304,5 +313,8 @@ class KVPool:
             self._h, raw, r, before, tables_out.data_ptr(),
             before if refs_out is None else self._refs(refs_out, "refs_out"), self._array(counts, torch.int32, "counts", 2),
             self._status)
-        self._done("ps_kv_compact", rc, stream, raw, tables, held, refs, tables_out, refs_out, counts)
+        if rc:
+            self._raise("ps_kv_compact", rc)
+        if stream is not None:
+            self._record(raw, tables, held, refs, tables_out, refs_out, counts)
         return counts
