@@ -215,7 +215,7 @@ typedef struct {
  * item's child or parent.  All or nothing: an item out of range sets *d_status
  * to PS_ERR_INVALID_ARG, too few free pages to PS_ERR_CAPACITY, and then
  * nothing changes but refs_out, which becomes refs_in.  refs_out may be
- * refs_in.  n is at most max_requests. */
+ * refs_in, but not overlap it otherwise (refused).  n is at most max_requests. */
 int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parents, const int32_t* d_children,
                    const int32_t* d_room, const ps_kv_rows_t* rows, const int32_t* d_refs_in, int32_t* d_refs_out,
                    int32_t* d_status);
@@ -231,10 +231,11 @@ int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_row
  * or above it, and so on.  Their keys and values are copied (all layers), the
  * tables (all num_rows rows' held pages) are written to d_tables_out with the
  * new ids (entries past held are copied as they are), and the references to
- * d_refs_out; both may be the inputs themselves.  d_counts [2]: L, and the
- * pages moved.  Rows may be wider than max_row_pages.  Held ids out of range
- * are copied as they are and set *d_status; a row with fewer than 0 or more
- * than table_stride pages sets it, too, and has none or all its ids rewritten. */
+ * d_refs_out; both may be the inputs themselves, but not overlap them otherwise
+ * (refused).  d_counts [2]: L, and the pages moved.  Rows may be wider than
+ * max_row_pages.  Held ids out of range are copied as they are and set
+ * *d_status; a row with fewer than 0 or more than table_stride pages sets it,
+ * too, and has none or all of its ids rewritten. */
 int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
                       int32_t* d_tables_out, int32_t* d_refs_out, int32_t* d_counts, int32_t* d_status);
 

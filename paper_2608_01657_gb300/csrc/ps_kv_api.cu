@@ -134,6 +134,11 @@ constexpr int32_t kSizedWorkers[kLists] = {kMaxSms * 4 * kNarrowWarps, kMaxSms};
 bool refs_ok(const ps_kv* kv, const int32_t* in, const int32_t* out) {
   return (in && out) || kv->pool.first_page == kv->pool.num_pages;
 }
+// Do two arrays of n int32 overlap without being the same one?
+bool partly_same(const int32_t* a, const int32_t* b, int64_t n) {
+  const int64_t d = ((intptr_t)a - (intptr_t)b) / 4;
+  return a != b && d < n && d > -n;
+}
 bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
   return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
 }
@@ -274,6 +279,7 @@ int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parent
                    int32_t* d_status) {
   if (!kv || !rows_ok(kv, rows) || n < 0 || n > kv->max_requests || !refs_ok(kv, d_refs_in, d_refs_out)) return PS_ERR_INVALID_ARG;
   if (n > 0 && (!d_parents || !d_children || !d_room)) return PS_ERR_INVALID_ARG;
+  if (partly_same(d_refs_in, d_refs_out, kv->pool.num_pages - kv->pool.first_page)) return PS_ERR_INVALID_ARG;
   return launch_fork(kv->pool, kv->pages, n, d_parents, d_children, d_room, *rows, row_pages(kv, rows->table_stride),
                      d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
 }
@@ -291,6 +297,9 @@ int32_t ps_kv_compact(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const
                       int32_t* d_tables_out, int32_t* d_refs_out, int32_t* d_counts, int32_t* d_status) {
   if (!kv || !rows || !rows->tables || !rows->held || rows->num_rows < 1 || rows->table_stride < 1 ||
       !refs_ok(kv, d_refs_in, d_refs_out) || !d_tables_out || !d_counts)
+    return PS_ERR_INVALID_ARG;
+  if (partly_same(d_refs_in, d_refs_out, kv->pool.num_pages - kv->pool.first_page) ||
+      partly_same(rows->tables, d_tables_out, rows->num_rows * rows->table_stride))
     return PS_ERR_INVALID_ARG;
   return launch_compact(kv->pool, kv->pages, *rows, d_refs_in, d_tables_out, d_refs_out, d_counts, d_status, kv->nsm,
                         as_stream(stream));

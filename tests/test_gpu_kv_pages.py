@@ -454,6 +454,29 @@ def test_page_refusals():
         pool.compact(t, h, r, tables_out=t[:1])
 
 
+def test_shifted_outputs_of_page_calls_are_refused():
+    """References and tables go to their own place or to another one, not to one that overlaps it."""
+    from paper_2608_01657_gb300 import kv as KV
+    k, v = make_pool(1, 10, 16, 1, 64, BF)
+    pool = KV.KVPool(k, v, num_q_heads=1, first_page=4, max_requests=2, max_row_pages=3)
+    t, h, l = torch.zeros(4, 3, dtype=torch.int32, device="cuda"), dev([0, 0]), dev([0, 0])
+    both, one = dev([0] * 13), dev([0])
+    refs = both[:6]
+    for shift in (1, 5):
+        with pytest.raises(RuntimeError, match="invalid"):
+            pool.fork(one, one, one, t[:2], l, h, refs, refs_out=both[shift:shift + 6])
+        with pytest.raises(RuntimeError, match="invalid"):
+            pool.compact(t[:2], h, refs, refs_out=both[shift:shift + 6])
+    with pytest.raises(RuntimeError, match="invalid"):
+        pool.compact(t[:2], h, refs, tables_out=t[1:3])
+    with pytest.raises(RuntimeError, match="invalid"):
+        pool.compact(t[1:3], h, refs, tables_out=t[:2])
+    pool.fork(one, one, dev([17]), t[:2], l, h, refs, refs_out=both[6:12])
+    pool.compact(t[:2], h, both[6:12], tables_out=t[2:])
+    pool.check()
+    assert t.tolist() == [[4, 5, 0], [0, 0, 0]] * 2
+
+
 # ---- the step's blocks ---------------------------------------------------------------
 @pytest.mark.parametrize("policy", ["lru", "s3fifo", "prefixshield", "staticquota"])
 def test_step_blocks_against_the_pool_state(policy):
