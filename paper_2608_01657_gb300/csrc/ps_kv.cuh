@@ -84,7 +84,7 @@ struct __align__(16) JoinRec {
 struct __align__(16) PlanHdr {
   int32_t status;           // PS_OK, or why the plan is empty
   int32_t joins[kLists];    // entries of joins[]
-  int32_t mend;             // some byte of mend[] is set
+  int32_t mend[2];          // some byte of mend[] was set by the last call with this place, see AttendArgs
   int32_t ntiles[kLists];
   int32_t workers[kLists];  // C, 0 without tiles
   int32_t narrow_ctas;      // CTAs that the narrow tiles' workers are spread over
@@ -327,7 +327,7 @@ inline int32_t status_of(cudaError_t e) { return e == cudaSuccess ? PS_OK : PS_E
 
 int32_t launch_append(const Pool& p, int32_t layer, const ps_kv_append_t& a, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_plan(const Pool& p, const Plan& plan, const Batch& b, int32_t* status, cudaStream_t st);
-int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer, const ps_kv_attention_t& a,
+int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer, int32_t turn, const ps_kv_attention_t& a,
                          int32_t* status, cudaStream_t st);
 int32_t launch_copy(const Pool& p, int32_t n, const int32_t* src, const int32_t* dst, int32_t* status, int nsm,
                     cudaStream_t st);

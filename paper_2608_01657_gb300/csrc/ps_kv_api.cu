@@ -15,6 +15,7 @@ struct ps_kv {
   PageScratch pages;
   Batch batch;
   bool planned;
+  int32_t turn;  // of the next attention, 0 or 1
   int32_t nsm, max_requests, max_tokens, max_row_pages;
 };
 
@@ -264,7 +265,8 @@ int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_at
   if (heads_overlap(out, out, kv->batch.num_tokens, kv->pool.head_dim, true) ||
       heads_overlap(out, q, kv->batch.num_tokens, kv->pool.head_dim))
     return PS_ERR_INVALID_ARG;
-  return launch_attention(kv->pool, kv->maps[layer], kv->plan, kv->batch, layer, *a, d_status, as_stream(stream));
+  kv->turn ^= 1;
+  return launch_attention(kv->pool, kv->maps[layer], kv->plan, kv->batch, layer, kv->turn, *a, d_status, as_stream(stream));
 }
 
 int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,

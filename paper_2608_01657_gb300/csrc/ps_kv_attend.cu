@@ -607,7 +607,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 16 / kJoinWarps) k_attend_joi
     join_rows<T, tile_rows(1), 1>(a, &sh, &waited, 1, h.z, warp, warps, 0, lane);
   }
   if (!waited) chain();
-  if (__ldcg(&a.plan.hdr->mend)) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.plan.hdr->mend[a.turn ^ 1] = 0;
+  if (__ldcg(&a.plan.hdr->mend[a.turn])) {
     mend_tiles<T, 0>(a, warp, warps, lane);
     mend_tiles<T, 1>(a, warp, warps, lane);
   }
@@ -648,7 +649,7 @@ int32_t configure_attention(const Pool& p, int nsm, int32_t workers[kLists]) {
 }
 
 int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, const Batch& b, int32_t layer,
-                         const ps_kv_attention_t& in, int32_t* status, cudaStream_t st) {
+                         int32_t turn, const ps_kv_attention_t& in, int32_t* status, cudaStream_t st) {
   AttendArgs a{};
   a.pool = p;
   a.plan = plan;
@@ -666,6 +667,7 @@ int32_t launch_attention(const Pool& p, const PoolMaps& maps, const Plan& plan, 
   a.q_offsets = b.q_offsets;
   a.kv_lens = b.kv_lens;
   a.causal = b.causal;
+  a.turn = turn;
   a.fill = in.fill;
   a.num_tokens = b.num_tokens;
   a.status = status;

@@ -21,6 +21,10 @@ struct AttendArgs {
   int32_t* status;
   int32_t after_wide;  // the wide tiles' kernel was launched
   int32_t causal;
+  // Which of the header's two marks this call sets where an output is not finite:
+  // the calls take turns, and each one's join clears the other mark for the next
+  // call, so that finite layers after one that was not do not look at rows again.
+  int32_t turn;
   int32_t fill, num_tokens;  // the outputs' rows become NaN after an empty plan
   float scale2;  // scale log2(e)
 };
@@ -95,7 +99,7 @@ __device__ __forceinline__ float spoil(float z, float x) { return fmaf(x, 0.0f, 
 // An output of (tile, head) is not finite: the join looks at its rows (mend_row).
 __device__ __forceinline__ void ask_mend(const AttendArgs& a, int list, int tile, int head) {
   a.plan.mend[list][(int64_t)tile * a.pool.kv_heads + head] = 1;
-  a.plan.hdr->mend = 1;
+  a.plan.hdr->mend[a.turn] = 1;
 }
 
 // The wide tiles' kernel (ps_kv_attend_wide.cu).

@@ -512,3 +512,27 @@ def test_tokens_without_requests_are_refused():
     with pytest.raises(ValueError):
         pool.attention(0, torch.zeros(3, 4, 64, device="cuda", dtype=BF), 0.125)
     pool.check()
+
+
+@pytest.mark.parametrize("new,dim", [(1, 64), (20, 128)])
+def test_a_layer_that_is_not_finite_leaves_the_later_ones_alone(new, dim):
+    """Its tiles' marks stay until the next plan, but the later calls do not follow them: the plan's
+    header is as the plan left it after one finite call."""
+    from paper_2608_01657_gb300 import kv as KV
+    R, heads, ps = 6, 2, 16
+    dev = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    tables = torch.arange(R * 2, device="cuda", dtype=torch.int32).view(R, 2)
+    k, v = make_pool(2, R * 2, ps, heads, dim, BF, seed=dim)
+    v[0].fill_(math.nan)
+    q = torch.randn(R * new, heads, dim, device="cuda").to(BF)
+    pool = KV.KVPool(k, v, num_q_heads=heads, max_requests=R, max_tokens=R * new, max_row_pages=2)
+    pool.workspace.zero_()
+    pool.plan(dev(np.arange(R + 1) * new), dev([new] * R), tables, R * new)
+    before = pool.workspace.clone()
+    for finite_calls in (1, 2, 1):
+        for layer in [0] + [1] * finite_calls:
+            out = pool.attention(layer, q, 0.1)
+            assert torch.isfinite(out).all() == (layer == 1) and torch.isnan(out).all() == (layer == 0)
+        # a byte for each tile and head
+        assert int((pool.workspace != before).sum()) == R * heads
+    pool.check()
