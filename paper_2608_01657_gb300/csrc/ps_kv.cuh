@@ -60,7 +60,8 @@ constexpr int kLists = 2;        // 0: narrow tiles (mma), 1: wide tiles (tcgen0
 __host__ __device__ constexpr int tile_rows(int list) { return list ? 256 : 16; }
 __host__ __device__ constexpr int unit_keys(int list) { return list ? 128 : 16; }
 // What a (tile, head) costs beside its units, in units (wide: 11000 cycles measured
-// for its beginning and end, of 2800 a unit; with 2 for it prompts took 293 us, with 4 281).
+// for its beginning and end, of 2800 a unit; with 2 for it prompts took 293 us, with
+// 4 281, on one input again).
 __host__ __device__ constexpr int tile_cost(int list) { return list ? 4 : 1; }
 // The list of an item of so many rows.
 __host__ __device__ constexpr int list_of(int rows) { return rows > tile_rows(0) ? 1 : 0; }

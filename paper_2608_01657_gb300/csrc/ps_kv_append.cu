@@ -79,7 +79,7 @@ __device__ __forceinline__ void write_part(char* p, const Part<E>& r) {
 }
 
 // 8191 bf16 tokens, 32 + 2 x 8 heads of 128, both norms, all rotated: 36 us, 5.7
-// TB/s of the 6.8 that copies reach, with the issue slots at 69 % (283
+// TB/s of the 6.8 that copies reach, with the issue slots at 70 % (293
 // instructions a slice of four heads).  Loads into registers, one slice ahead:
 // 50 us; 8-byte parts, two heads' loads together and 48 warps an SM: 44 us.
 // Six CTAs an SM spill registers (47 us), three or six stages change nothing.

@@ -35,9 +35,13 @@
 // exponentials and most maxima left out they are 2560.  (Weights computed with
 // the old reference beside the search for the maximum were no faster: 321 us;
 // the groups without turns 343.)  A tile's ends cost some four units (tile_cost).
-// 7000 new bf16 tokens after 2000 to 4900 cached ones, 32 heads of 128 on 8:
-// 287 us, 1.39 PFLOP/s of the 1.88 that a library's plain product reaches;
-// 128 requests of one token after 16384 shared ones: 52 us by itself.
+// 7000 new bf16 tokens after 2000 to 4900 cached ones, 32 heads of 128 on 8: a
+// call takes 310 us on inputs that change, 1.29 PFLOP/s of the 1.88 that a
+// library's plain product reaches, and 285 to 292 on one input again, whose
+// queries are in L2 (the other figures for prompts here are of that kind); 128
+// requests of one token after 16384 shared ones: 52 us by itself, on the 76 SMs
+// that it has there.  The compiler spills 168 bytes of stores and 292 of loads a
+// thread in every variant; in which warps' code was not looked into.
 #include "ps_kv_attend.cuh"
 
 namespace pskv {

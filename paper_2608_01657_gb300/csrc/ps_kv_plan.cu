@@ -1,7 +1,8 @@
 // ps_kv_plan: shared prefixes, tiles and the division of a batch's attention
 // into equal parts (see ps_kv.cuh for the plan's shape).  Three kernels bound by
-// the latency of their dependent reads and scans: 15 us for one request, 20 for
-// 256 in 32 groups, 23 for eight prompts; once a step, for all of its layers.
+// the latency of their dependent reads and scans: 16 us for one request, 20 for
+// 256 in 32 groups, 22 for eight prompts, about half of it k_plan_tiles, one CTA;
+// once a step, for all of its layers.
 #include "ps_kv.cuh"
 
 namespace pskv {
