@@ -20,6 +20,8 @@
  *   ps_kv_plan, ps_kv_attention
  *                    attention over the pages of a batch of requests, a prefix
  *                    shared by a group of requests read once for all of them;
+ *   ps_kv_layout     where a batch's new tokens go: the offsets, lengths, tables,
+ *                    positions and slots that the calls above take;
  *   ps_kv_copy, ps_kv_fork, ps_kv_release, ps_kv_compact
  *                    page copies, forks of sequences, freeing, compaction.
  *
@@ -205,6 +207,52 @@ typedef struct {
   int32_t num_rows;
   int32_t pad0;
 } ps_kv_rows_t;
+
+/* A batch's arrays, from its requests' rows: request i is row rows[i] (NULL: row
+ * i) and has counts[i] (NULL: one) new tokens after its first starts[i] (NULL:
+ * the row's lens).  Its pages are there already (held covers starts + counts).
+ * With o the exclusive sums of the counts, token t of request i, o[i] <= t <
+ * o[i + 1], has the position p = starts[i] + t - o[i] and the slot
+ * tables[row][p / page_size] * page_size + p % page_size, or -1 where p <
+ * written[i] (NULL: none; tokens whose keys and values are in their pages
+ * already).  The arrays are what ps_kv_append() and ps_kv_plan() take:
+ *   q_offsets  o, and the sum of all counts;
+ *   kv_lens    starts + counts;
+ *   tables     the row's ids of those tokens' pages, then -1, rows->table_stride
+ *              of them for each request;
+ *   group_offsets  runs of neighbours that attention may share a prefix of: before
+ *              their new tokens they have as many tokens in the same pages as
+ *              sharing needs, and few new ones.  The runs are followed by empty
+ *              ones, so that there are num_requests groups.
+ * num_tokens may be more than the sum.  A token past the sum has position 0 and
+ * slot -1; with 'pad' these tokens are those of one more request, the last, that
+ * has no keys and a group of its own (so that attention gives 0 for them): a batch
+ * whose counts change from replay to replay of one graph.  Outputs lie on no
+ * input and on no other output (refused). */
+typedef struct {
+  const int32_t* rows;      /* [num_requests] or NULL */
+  const int32_t* counts;    /* [num_requests] or NULL */
+  const int32_t* starts;    /* [num_requests] or NULL */
+  const int32_t* written;   /* [num_requests] or NULL */
+  int32_t* q_offsets;       /* [num_requests + pad + 1] */
+  int32_t* kv_lens;         /* [num_requests + pad] */
+  int32_t* tables;          /* [num_requests + pad][rows->table_stride] */
+  int32_t* positions;       /* [num_tokens] */
+  int64_t* slots;           /* [num_tokens] */
+  int32_t* group_offsets;   /* [num_requests + pad + 1], NULL: not wanted */
+  int32_t num_requests;     /* 0..max_requests, with the padding's */
+  int32_t num_tokens;       /* 0..max_tokens */
+  int32_t pad;              /* 0 or 1 */
+  int32_t pad0;
+} ps_kv_layout_t;
+
+/* A request out of range (its row, its numbers, more tokens than its pages hold)
+ * sets *d_status to PS_ERR_INVALID_ARG, more tokens than num_tokens to
+ * PS_ERR_CAPACITY, and then the whole batch is left out: offsets and lengths are
+ * 0, tables and slots -1, and ps_kv_plan() refuses it.  A page id out of range
+ * sets *d_status, and the slot is -1. */
+int32_t ps_kv_layout(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const ps_kv_layout_t* layout,
+                     int32_t* d_status);
 
 /* For each item i, row children[i] becomes a continuation of row parents[i]
  * (its lens[parent] tokens) with pages for room[i] tokens in all:

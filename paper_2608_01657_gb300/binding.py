@@ -37,7 +37,7 @@ EXPORTED = ("ps_workspace_bytes", "ps_create", "ps_step", "ps_step_host", "ps_st
             "ps_export_ghost", "ps_set_stage_timing", "ps_get_stage_times", "ps_cached_prefix",
             "ps_cached_prefix_noalloc", "ps_uses_graph", "ps_set_graph", "ps_step_blocks",
             "ps_kv_workspace_bytes", "ps_kv_create", "ps_kv_destroy", "ps_kv_append", "ps_kv_plan",
-            "ps_kv_attention", "ps_kv_copy", "ps_kv_fork", "ps_kv_release", "ps_kv_compact")
+            "ps_kv_attention", "ps_kv_layout", "ps_kv_copy", "ps_kv_fork", "ps_kv_release", "ps_kv_compact")
 PS_NUM_STAGES = 11
 STAGE_NAMES = ("validate", "hash_lookup", "claims", "grant_instep", "meter", "touch_gate", "select",
                "take_lists", "evict", "insert", "commit")
@@ -124,6 +124,12 @@ class PsKvRows(C.Structure):
         ("table_stride", C.c_int64), ("num_rows", C.c_int32), ("pad0", C.c_int32)]
 
 
+class PsKvLayout(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("rows", "counts", "starts", "written", "q_offsets", "kv_lens", "tables", "positions",
+                                          "slots", "group_offsets")] + [
+        (n, C.c_int32) for n in ("num_requests", "num_tokens", "pad", "pad0")]
+
+
 _lib = None
 
 
@@ -190,6 +196,8 @@ def load():
     L.ps_kv_plan.argtypes = [vp, vp, C.POINTER(PsKvBatch), vp]
     L.ps_kv_attention.restype = i32
     L.ps_kv_attention.argtypes = [vp, vp, i32, C.POINTER(PsKvAttention), vp]
+    L.ps_kv_layout.restype = i32
+    L.ps_kv_layout.argtypes = [vp, vp, C.POINTER(PsKvRows), C.POINTER(PsKvLayout), vp]
     L.ps_kv_copy.restype = i32
     L.ps_kv_copy.argtypes = [vp, vp, i32, vp, vp, vp]
     L.ps_kv_fork.restype = i32

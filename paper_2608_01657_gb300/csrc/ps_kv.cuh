@@ -95,6 +95,8 @@ struct __align__(16) PlanHdr {
 // Requests of more rows than this fill tiles of their own; a prefix shared by
 // smaller ones is read once for all of them.
 constexpr int kShareRows = 64;
+// Shared tokens below which the second part of a row costs more than it saves.
+constexpr int kShareTokens = 128;
 constexpr int kMaxSms = 160;
 
 // Tiles of one list, and rows of one kv head that have a shared prefix (in its
@@ -235,6 +237,18 @@ struct PageScratch {
   int32_t chunks, chunk_size;
 };
 
+// ---- layout --------------------------------------------------------------------
+// Of batches of more than kLayoutPart requests: offsets and groups from a part's
+// first on, the parts' totals, and where each part begins.
+constexpr int kLayoutPart = 1024;
+struct LayoutScratch {
+  int32_t *offset, *group;  // [max_requests], the page calls' start and need
+  int64_t* total;           // [parts]
+  int32_t* groups;          // [parts]
+  int32_t *base, *group_base;  // [parts + 1]
+  int32_t* done;
+};
+
 // ---- device helpers ----------------------------------------------------------------
 __device__ __forceinline__ void set_error(int32_t* status, int32_t code) {
   if (status) atomicMin(status, code);
@@ -339,6 +353,8 @@ int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_k
                        int32_t* refs, int32_t* status, cudaStream_t st);
 int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                        int32_t* status, int nsm, cudaStream_t st);
+int32_t launch_layout(const Pool& p, const LayoutScratch& w, const ps_kv_layout_t& l, const ps_kv_rows_t& rows, int32_t row_pages,
+                      int32_t* status, int nsm, cudaStream_t st);
 // Kernel attributes (shared-memory opt-ins) and the workers of each attention list
 // that the current device holds at once.
 constexpr int kNarrowWarps = 4;  // of a CTA

@@ -13,6 +13,7 @@ struct ps_kv {
   PoolMaps* maps = nullptr;  // [layers]
   Plan plan;
   PageScratch pages;
+  LayoutScratch layout;
   Batch batch;
   bool planned;
   int32_t turn;  // of the next attention, 0 or 1
@@ -79,7 +80,8 @@ struct Carver {
 
 // The workspace: sizes with base == nullptr, pointers otherwise.  Every region
 // starts on a 256-byte boundary.  The page header comes first (cleared once).
-size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base, Plan* plan, PageScratch* pages) {
+size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base, Plan* plan, PageScratch* pages,
+             LayoutScratch* layout) {
   Carver cv{base};
   const int64_t R = c.max_requests, T = c.max_tokens, ratio = c.num_q_heads / c.num_kv_heads;
   PageScratch w{};
@@ -122,6 +124,16 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
     p.part_o[l] = cv.take<float4>((part_rows + 7) / 8 * 8 * (c.head_dim / 4));
     p.part_ml[l] = cv.take<float2>(part_rows);
   }
+  LayoutScratch y{};
+  const size_t parts = ((size_t)R + kLayoutPart - 1) / kLayoutPart;
+  y.offset = w.start;
+  y.group = w.need;
+  y.done = &w.hdr->done;
+  y.total = cv.take<int64_t>(parts);
+  y.groups = cv.take<int32_t>(parts);
+  y.base = cv.take<int32_t>(parts + 1);
+  y.group_base = cv.take<int32_t>(parts + 1);
+  if (layout) *layout = y;
   if (plan) *plan = p;
   if (pages) *pages = w;
   return (cv.off + 255) / 256 * 256;
@@ -140,6 +152,22 @@ bool partly_same(const int32_t* a, const int32_t* b, int64_t n) {
   const int64_t d = ((intptr_t)a - (intptr_t)b) / 4;
   return a != b && d < n && d > -n;
 }
+// Arrays of a call, for finding outputs that lie on inputs or on one another.
+struct Span {
+  const void* p;
+  int64_t bytes;
+  bool out;
+};
+template <size_t N>
+bool outputs_apart(const Span (&s)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j) {
+      if (i == j || !s[i].out || !s[i].p || !s[j].p || s[i].bytes <= 0 || s[j].bytes <= 0) continue;
+      const int64_t d = (intptr_t)s[i].p - (intptr_t)s[j].p;
+      if (d < s[j].bytes && -d < s[i].bytes) return false;
+    }
+  return true;
+}
 bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
   return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
 }
@@ -152,13 +180,13 @@ int32_t row_pages(const ps_kv* kv, int64_t stride) {
 extern "C" {
 
 size_t ps_kv_workspace_bytes(const ps_kv_config_t* cfg) {
-  return check_config(cfg) ? carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr) : 0;
+  return check_config(cfg) ? carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr) : 0;
 }
 
 int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace, size_t workspace_bytes,
                      void* stream) {
   if (!out || !check_config(cfg) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0 ||
-      workspace_bytes < carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr))
+      workspace_bytes < carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr))
     return PS_ERR_INVALID_ARG;
   int dev = 0, nsm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
@@ -182,7 +210,7 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   for (int l = 0; l < kLists; ++l)
     if (workers[l] > kSizedWorkers[l]) workers[l] = kSizedWorkers[l];
   if (rc == PS_OK) {
-    carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages);
+    carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages, &kv->layout);
     for (int l = 0; l < kLists; ++l) kv->plan.max_workers[l] = workers[l];
     // and a plan that is empty, for an attention that runs before its plan has (one that was only captured into a graph)
     static_assert(PS_ERR_INVALID_ARG == -1, "the status word of all ones");
@@ -267,6 +295,21 @@ int32_t ps_kv_attention(ps_kv_t* kv, void* stream, int32_t layer, const ps_kv_at
     return PS_ERR_INVALID_ARG;
   kv->turn ^= 1;
   return launch_attention(kv->pool, kv->maps[layer], kv->plan, kv->batch, layer, kv->turn, *a, d_status, as_stream(stream));
+}
+
+int32_t ps_kv_layout(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const ps_kv_layout_t* l, int32_t* d_status) {
+  if (!kv || !l || !rows_ok(kv, rows) || (l->pad != 0 && l->pad != 1)) return PS_ERR_INVALID_ARG;
+  const int64_t n = l->num_requests, all = n + l->pad, T = l->num_tokens, stride = rows->table_stride;
+  if (n < 0 || all > kv->max_requests || T < 0 || T > kv->max_tokens || stride >= (1ll << 30)) return PS_ERR_INVALID_ARG;
+  if (!l->q_offsets || (all > 0 && (!l->kv_lens || !l->tables)) || (T > 0 && (!l->positions || !l->slots))) return PS_ERR_INVALID_ARG;
+  if (!l->rows && n > rows->num_rows) return PS_ERR_INVALID_ARG;
+  const Span spans[] = {{l->rows, 4 * n, false}, {l->counts, 4 * n, false}, {l->starts, 4 * n, false}, {l->written, 4 * n, false},
+                        {rows->tables, 4ll * rows->num_rows * stride, false}, {rows->lens, 4ll * rows->num_rows, false},
+                        {rows->held, 4ll * rows->num_rows, false}, {d_status, 4, false},
+                        {l->q_offsets, 4 * (all + 1), true}, {l->kv_lens, 4 * all, true}, {l->tables, 4 * all * stride, true},
+                        {l->positions, 4 * T, true}, {l->slots, 8 * T, true}, {l->group_offsets, 4 * (all + 1), true}};
+  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  return launch_layout(kv->pool, kv->layout, *l, *rows, row_pages(kv, stride), d_status, kv->nsm, as_stream(stream));
 }
 
 int32_t ps_kv_copy(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_src, const int32_t* d_dst,

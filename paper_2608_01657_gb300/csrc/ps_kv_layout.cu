@@ -1,0 +1,307 @@
+// ps_kv_layout: where a batch's new tokens go, from the requests' rows and counts.
+//
+// With o the exclusive sums of the requests' counts c, token t of request i (o_i
+// <= t < o_{i + 1}) has position p = s_i + t - o_i (s_i: the tokens before the new
+// ones) and slot table[row_i][p / page_size] page_size + p mod page_size.
+//
+// Integers only: bound by latency, a chain of three reads (a request's row, the
+// row's length, a page id) around a scan.  Up to kFused requests every CTA scans
+// all of them for itself, so that the call is one launch; of more, a first kernel
+// scans 1024 requests a CTA, its last CTA the totals.  The rest is a list of units
+// of equal size for the warps: 128 columns of a request's table, 128 tokens.  A
+// token finds its request by bisection of the offsets.
+#include "ps_kv_pages.cuh"
+
+namespace pskv {
+namespace {
+
+constexpr int kFused = kLayoutPart;
+constexpr int kItems = kFused / kScanThreads;
+constexpr int kUnit = 128;               // columns or tokens of a warp's unit
+constexpr int kUnitsPerCta = kScanThreads / 32;
+
+// The total of requests of which one is out of range: more than any real total (2^18
+// requests of 2^30 tokens), and 2^8 of them add up.
+constexpr int64_t kBad = 1ll << 50;
+
+struct Args {
+  ps_kv_layout_t l;
+  const int32_t *tables, *lens, *held;
+  int64_t stride, num_pages;
+  LayoutScratch w;
+  int32_t* status;
+  int32_t num_rows, row_pages, page_log2, lead, most;  // lead: pages that members of a group have in common; most: new tokens of a member
+};
+
+struct Item {
+  int row, start, count;
+};
+// Request i; false, and no tokens, if its row or its numbers are out of range.
+__device__ __forceinline__ bool item_of(const Args& a, int i, Item* it) {
+  const int row = a.l.rows ? a.l.rows[i] : i;
+  *it = Item{-1, 0, 0};
+  if (row < 0 || row >= a.num_rows) return false;
+  const int start = a.l.starts ? a.l.starts[i] : a.lens[row], count = a.l.counts ? a.l.counts[i] : 1;
+  const int held = a.held[row];
+  if (start < 0 || count < 0 || held < 0 || held > a.row_pages) return false;
+  if ((int64_t)start + count > (int64_t)held << a.page_log2) return false;
+  *it = Item{row, start, count};
+  return true;
+}
+// Do requests i and i - 1 share a prefix that is worth reading once?
+__device__ __forceinline__ bool joined(const Args& a, const Item& x, const Item& y) {
+  const int least = a.lead << a.page_log2;
+  if (x.row < 0 || y.row < 0 || x.start < least || y.start < least || x.count > a.most || y.count > a.most) return false;
+  const int32_t *p = a.tables + x.row * a.stride, *q = a.tables + y.row * a.stride;
+  bool same = true;
+#pragma unroll 8
+  for (int k = 0; k < a.lead; ++k) same = same && p[k] == q[k];
+  return same;
+}
+
+// The offsets of all requests, in shared memory.
+struct Near {
+  const int* off;
+  const Item* item;
+  int n;
+  __device__ __forceinline__ int offset(int i) const { return off[i]; }
+  __device__ __forceinline__ Item at(const Args&, int i) const { return item[i]; }
+};
+// In the workspace, each CTA's part from 0 on.
+struct Far {
+  const int32_t *local, *base;
+  int n;
+  __device__ __forceinline__ int offset(int i) const { return i < n ? local[i] + base[i / kFused] : base[(n + kFused - 1) / kFused]; }
+  __device__ __forceinline__ Item at(const Args& a, int i) const {
+    Item it;
+    item_of(a, i, &it);
+    return it;
+  }
+};
+
+// 'over': the batch is left out, for a request out of range or more tokens than there is room for.
+template <typename O>
+__device__ __forceinline__ void fill(const Args& a, const O& o, bool over, int cta, int ctas) {
+  const ps_kv_layout_t& l = a.l;
+  const int lane = threadIdx.x & 31, n = o.n, rows = n + (l.pad ? 1 : 0);
+  const int total = over ? 0 : o.offset(n);
+  const int64_t chunks = (a.stride + kUnit - 1) / kUnit;
+  const int64_t units = rows * chunks + (l.num_tokens + kUnit - 1) / kUnit;
+  for (int64_t u = (int64_t)cta * kUnitsPerCta + (threadIdx.x >> 5); u < units; u += (int64_t)ctas * kUnitsPerCta) {
+    if (u < rows * chunks) {  // a request's table
+      const int i = (int)(u / chunks);
+      const int64_t k0 = u % chunks * kUnit + lane;
+      Item it{-1, 0, 0};
+      if (i < n && !over) it = o.at(a, i);
+      const int64_t pages = it.row < 0 ? 0 : ((int64_t)it.start + it.count + (1 << a.page_log2) - 1) >> a.page_log2;
+      const int32_t* src = a.tables + it.row * a.stride;
+      int32_t* dst = l.tables + i * a.stride;
+#pragma unroll
+      for (int j = 0; j < kUnit / 32; ++j) {
+        const int64_t k = k0 + 32 * j;
+        if (k < a.stride) dst[k] = k < pages ? src[k] : -1;
+      }
+    } else {
+      const int64_t t0 = (u - rows * chunks) * kUnit + lane;
+#pragma unroll
+      for (int j = 0; j < kUnit / 32; ++j) {
+        const int64_t t = t0 + 32 * j;
+        if (t >= l.num_tokens) break;
+        int pos = 0;
+        int64_t slot = -1;
+        if (t < total) {
+          int lo = 0, hi = n - 1;  // the last request that begins at or before t; empty ones lie before it
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (o.offset(mid) <= t) lo = mid;
+            else hi = mid - 1;
+          }
+          const Item it = o.at(a, lo);
+          pos = it.start + (int)t - o.offset(lo);
+          const int id = a.tables[it.row * a.stride + (pos >> a.page_log2)];
+          if (id < 0 || id >= a.num_pages) set_error(a.status, PS_ERR_INVALID_ARG);
+          else if (pos >= (l.written ? l.written[lo] : it.start)) slot = ((int64_t)id << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
+        }
+        l.positions[t] = pos;
+        l.slots[t] = slot;
+      }
+    }
+  }
+}
+
+// The offsets' and groups' ends: written by one thread.  The offsets of a batch
+// that is left out do not end at its tokens, so that no plan is made of it.
+__device__ __forceinline__ void ends(const Args& a, bool over, int total, int groups) {
+  const ps_kv_layout_t& l = a.l;
+  const int n = l.num_requests;
+  l.q_offsets[n] = total;
+  if (l.pad) {  // a request without keys takes the tokens that are left, in a group of its own
+    l.q_offsets[n + 1] = over ? 0 : l.num_tokens;
+    l.kv_lens[n] = 0;
+  }
+  if (l.group_offsets && l.pad) l.group_offsets[groups] = n;
+}
+
+__global__ void __launch_bounds__(kScanThreads) k_layout(Args a) {
+  __shared__ int off[kFused + 1];
+  __shared__ Item item[kFused];
+  chain();
+  const ps_kv_layout_t& l = a.l;
+  const int n = l.num_requests, i0 = threadIdx.x * kItems;
+  Item it[kItems];
+  int64_t sum = 0, total;
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    it[j] = Item{-1, 0, 0};
+    if (i0 + j < n) bad |= !item_of(a, i0 + j, &it[j]);
+    sum += it[j].count;
+    item[i0 + j] = it[j];
+  }
+  int64_t o = block_scan(sum, &total);
+  bad = __syncthreads_or(bad);
+  const bool over = bad || total > l.num_tokens;
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    off[i0 + j] = over ? 0 : (int)o;
+    o += it[j].count;
+  }
+  if (threadIdx.x == kScanThreads - 1) off[kFused] = over ? 0 : (int)total;
+  __syncthreads();
+  if (blockIdx.x == 0) {  // the requests' own numbers, once
+    if (over && threadIdx.x == 0) set_error(a.status, bad ? PS_ERR_INVALID_ARG : PS_ERR_CAPACITY);
+    int begins = 0;
+#pragma unroll
+    for (int j = 0; j < kItems; ++j) {
+      const int i = i0 + j;
+      if (i >= n) break;
+      l.q_offsets[i] = off[i];
+      l.kv_lens[i] = over ? 0 : it[j].start + it[j].count;
+      if (l.group_offsets && (i == 0 || over || !joined(a, it[j], item[i - 1]))) begins |= 1 << j;
+    }
+    int groups = 0;
+    if (l.group_offsets) {
+      int g = block_scan(__popc(begins), &groups);
+#pragma unroll
+      for (int j = 0; j < kItems; ++j)
+        if (begins >> j & 1) l.group_offsets[g++] = i0 + j;
+      for (int g = groups + (l.pad ? 1 : 0) + threadIdx.x; g <= n + (l.pad ? 1 : 0); g += kScanThreads)
+        l.group_offsets[g] = n + (l.pad ? 1 : 0);
+    }
+    if (threadIdx.x == 0) ends(a, over, over ? 0 : (int)total, groups);
+  }
+  fill(a, Near{off, item, n}, over, blockIdx.x, gridDim.x);
+}
+
+// Many requests: kFused a CTA.  Their offsets and groups from the CTA's first on,
+// and the CTA's totals, which the last CTA turns into offsets.
+__global__ void __launch_bounds__(kScanThreads) k_layout_scan(Args a) {
+  chain();
+  const ps_kv_layout_t& l = a.l;
+  const int n = l.num_requests, i0 = blockIdx.x * kFused + threadIdx.x * kItems;
+  Item it[kItems], before{-1, 0, 0};
+  int64_t sum = 0;
+  int begins = 0;
+  bool bad = false;
+  if (i0 > 0 && i0 < n) item_of(a, i0 - 1, &before);
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    it[j] = Item{-1, 0, 0};
+    if (i0 + j < n) {
+      bad |= !item_of(a, i0 + j, &it[j]);
+      if (l.group_offsets && (i0 + j == 0 || !joined(a, it[j], j ? it[j ? j - 1 : 0] : before))) begins |= 1 << j;
+    }
+    sum += it[j].count;
+  }
+  int64_t total;
+  int groups;
+  int64_t o = block_scan(sum, &total);
+  bad = __syncthreads_or(bad);
+  int g = block_scan(__popc(begins), &groups);
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    const int i = i0 + j;
+    if (i < n) {
+      // a batch that is left out has offsets past 2^31 perhaps: none is looked at
+      a.w.offset[i] = (int32_t)(o < 0x7FFFFFFF ? o : 0x7FFFFFFF);
+      a.w.group[i] = begins >> j & 1 ? g : -1;
+    }
+    g += begins >> j & 1;
+    o += it[j].count;
+  }
+  if (threadIdx.x == 0) {
+    a.w.total[blockIdx.x] = bad ? kBad : total;
+    a.w.groups[blockIdx.x] = groups;
+  }
+  if (!last_cta(a.w.done)) return;
+  int64_t carry = 0;
+  int gcarry = 0;
+  for (int c0 = 0; c0 < (int)gridDim.x; c0 += kScanThreads) {
+    const int c = c0 + threadIdx.x;
+    const bool on = c < (int)gridDim.x;
+    int64_t tot;
+    int gtot;
+    const int64_t e = block_scan<int64_t>(on ? __ldcg(a.w.total + c) : 0, &tot);
+    const int ge = block_scan(on ? __ldcg(a.w.groups + c) : 0, &gtot);
+    if (on) {
+      a.w.base[c] = (int32_t)(carry + e < 0x7FFFFFFF ? carry + e : 0x7FFFFFFF);
+      a.w.group_base[c] = gcarry + ge;
+    }
+    carry += tot;
+    gcarry += gtot;
+  }
+  if (threadIdx.x == 0) {
+    a.w.base[gridDim.x] = (int32_t)(carry < 0x7FFFFFFF ? carry : 0x7FFFFFFF);
+    a.w.group_base[gridDim.x] = gcarry;
+    if (carry > l.num_tokens) set_error(a.status, carry >= kBad ? PS_ERR_INVALID_ARG : PS_ERR_CAPACITY);
+  }
+}
+
+__global__ void __launch_bounds__(kScanThreads) k_layout_fill(Args a) {
+  chain();
+  const ps_kv_layout_t& l = a.l;
+  const int n = l.num_requests, parts = (n + kFused - 1) / kFused;
+  const Far o{a.w.offset, a.w.base, n};
+  const int total = a.w.base[parts], groups = a.w.group_base[parts];
+  const bool over = total > l.num_tokens;
+  const int64_t id = (int64_t)blockIdx.x * kScanThreads + threadIdx.x, step = (int64_t)gridDim.x * kScanThreads;
+  for (int64_t i = id; i < n; i += step) {
+    const Item it = o.at(a, (int)i);
+    l.q_offsets[i] = over ? 0 : o.offset((int)i);
+    l.kv_lens[i] = over ? 0 : it.start + it.count;
+    if (l.group_offsets) {
+      const int g = a.w.group[i];
+      if (over) l.group_offsets[i] = (int)i;
+      else if (g >= 0) l.group_offsets[g + a.w.group_base[i / kFused]] = (int)i;
+    }
+  }
+  const int shown = over ? n : groups, all = n + (l.pad ? 1 : 0);
+  if (l.group_offsets)
+    for (int64_t g = shown + (l.pad ? 1 : 0) + id; g <= all; g += step) l.group_offsets[g] = all;
+  if (id == 0) ends(a, over, over ? 0 : total, shown);
+  fill(a, o, over, blockIdx.x, gridDim.x);
+}
+
+}  // namespace
+
+int32_t launch_layout(const Pool& p, const LayoutScratch& w, const ps_kv_layout_t& l, const ps_kv_rows_t& rows,
+                      int32_t row_pages, int32_t* status, int nsm, cudaStream_t st) {
+  Args a{};
+  a.l = l;
+  a.tables = rows.tables; a.lens = rows.lens; a.held = rows.held; a.stride = rows.table_stride;
+  a.num_pages = p.num_pages; a.w = w; a.status = status;
+  a.num_rows = rows.num_rows; a.row_pages = row_pages; a.page_log2 = p.page_log2;
+  a.lead = (kShareTokens + p.page_size - 1) >> p.page_log2;
+  a.most = kShareRows / p.ratio;
+  const int64_t n = l.num_requests;
+  const int64_t units = (n + (l.pad ? 1 : 0)) * ((a.stride + kUnit - 1) / kUnit) + ((int64_t)l.num_tokens + kUnit - 1) / kUnit;
+  const int64_t want = (units + kUnitsPerCta - 1) / kUnitsPerCta;
+  const int64_t most = (int64_t)nsm * 4;
+  const int grid = (int)(want < 1 ? 1 : (want > most ? most : want));
+  if (n <= kFused) return status_of(launch(k_layout, dim3((unsigned)grid), kScanThreads, 0, st, a));
+  cudaError_t e = launch(k_layout_scan, dim3((unsigned)((n + kFused - 1) / kFused)), kScanThreads, 0, st, a);
+  if (e == cudaSuccess) e = launch(k_layout_fill, dim3((unsigned)grid), kScanThreads, 0, st, a);
+  return status_of(e);
+}
+
+}  // namespace pskv

@@ -12,9 +12,6 @@ constexpr int kReqThreads = 128;
 constexpr int kPlanThreads = 1024;
 constexpr int kAnyPages = 0x7FFFFFFF;
 
-// Shared tokens below which the second part of a row costs more than it saves.
-constexpr int kShareTokens = 128;
-
 // Cycles of one unit as the division weighs them: a wide one on its SM (128
 // keys; 2800 measured for prompts, 3900 beside narrow tiles, up to 5900 where a
 // tile has one or two units), a narrow one in its warp (16 keys).  Both are those

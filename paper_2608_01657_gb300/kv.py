@@ -1,9 +1,10 @@
 """The operators on the KV pages whose block ids the prefix cache hands out.
 
 ``KVPool`` wraps one pool of keys and values and the C ABI of
-``include/prefixshield_kv.h``: appending tokens (norms of queries and keys,
-rotation, page write), attention over the pages with shared prefixes read once,
-and copying, forking, freeing and compacting pages.  As in ``binding``,
+``include/prefixshield_kv.h``: laying a batch out (offsets, lengths, tables,
+positions, slots), appending tokens (norms of queries and keys, rotation, page
+write), attention over the pages with shared prefixes read once, and copying,
+forking, freeing and compacting pages.  As in ``binding``,
 arguments are marshalled here and all work runs in the library's CUDA kernels;
 torch provides device memory and streams.  Calls are enqueued on ``stream``
 (default: the current one) and do not synchronize; what a call that names its
@@ -15,7 +16,7 @@ can see are reported in the int32 tensor ``pool.status``, which is sticky until
 from __future__ import annotations
 
 import ctypes as C
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -28,6 +29,16 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
+
+
+class Layout(NamedTuple):
+    """A batch's arrays, as ``append`` and ``plan`` take them."""
+    q_offsets: torch.Tensor                # int32 [requests + 1]
+    kv_lens: torch.Tensor                  # int32 [requests]
+    tables: torch.Tensor                   # int32 [requests, pages]
+    positions: torch.Tensor                # int32 [tokens]
+    slots: torch.Tensor                    # int64 [tokens]
+    group_offsets: Optional[torch.Tensor]  # int32 [requests + 1]
 
 
 class KVPool:
@@ -81,6 +92,8 @@ class KVPool:
         self._append_ref, self._attention_ref = C.byref(self._append_args), C.byref(self._attention_args)
         self._rows_args = B.PsKvRows()
         self._rows_ref = C.byref(self._rows_args)
+        self._layout_args = B.PsKvLayout()
+        self._layout_ref = C.byref(self._layout_args)
         self._private = max(0, self.pages - self.first_page)
         self._append_strides = [getattr(self._append_args, n) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
         self._attention_strides = [getattr(self._attention_args, n) for n in ("q_stride", "out_stride")]
@@ -194,6 +207,50 @@ class KVPool:
         if stream is not None:
             self._record(raw, q, k, v, slots, positions, rope, q_weight, k_weight, q_out)
         return q_out
+
+    # -- a batch's arrays ------------------------------------------------------
+    def layout(self, rows, tables, lens, held, num_tokens: int, counts=None, starts=None, written=None, pad: bool = False,
+               groups: bool = True, out: Optional[Layout] = None, stream=None) -> Layout:
+        """Where the new tokens of a batch go.  Request i is row ``rows[i]`` (None:
+        row i) of ``tables`` / ``lens`` / ``held`` and has ``counts[i]`` (None: one)
+        new tokens after its first ``starts[i]`` (None: the row's lens); tokens at
+        positions below ``written[i]`` get slot -1.  The rest of ``num_tokens`` has
+        slot -1, too, and with ``pad`` belongs to one more request without keys, so
+        that the layout of a captured graph can be planned whatever the counts are.
+        ``groups``: with the runs of requests that may share a prefix.  ``out``: an
+        earlier layout of the same shape to write to.  A batch with a request out
+        of range, or more tokens than ``num_tokens``, is left out whole: every slot
+        is -1, and a plan of it is refused."""
+        a = self._layout_args
+        r = self._rows(tables, lens, held)
+        n = tables.shape[0] if rows is None else rows.shape[0]
+        T, all_ = int(num_tokens), n + bool(pad)
+        i32 = torch.int32
+        if out is None:
+            made = lambda *shape, dtype=i32: B._made(shape, dtype, self.device, stream)  # noqa: E731
+            out = Layout(made(all_ + 1), made(all_), made(all_, tables.shape[1]), made(T), made(T, dtype=torch.int64),
+                         made(all_ + 1) if groups else None)
+        self._table(out.tables, "out.tables")
+        if out.tables.shape[0] != all_ or out.tables.shape[1] != tables.shape[1]:
+            raise ValueError(f"out.tables must be [{all_}, {tables.shape[1]}]")
+        a.rows = None if rows is None else self._array(rows, i32, "rows")
+        a.counts = None if counts is None else self._array(counts, i32, "counts", n)
+        a.starts = None if starts is None else self._array(starts, i32, "starts", n)
+        a.written = None if written is None else self._array(written, i32, "written", n)
+        a.q_offsets = self._array(out.q_offsets, i32, "out.q_offsets", all_ + 1)
+        a.kv_lens = self._array(out.kv_lens, i32, "out.kv_lens", all_)
+        a.tables = out.tables.data_ptr()
+        a.positions = self._array(out.positions, i32, "out.positions", T)
+        a.slots = self._array(out.slots, torch.int64, "out.slots", T)
+        a.group_offsets = None if out.group_offsets is None else self._array(out.group_offsets, i32, "out.group_offsets", all_ + 1)
+        a.num_requests, a.num_tokens, a.pad = n, T, 1 if pad else 0
+        raw = self._stream(stream)
+        rc = self._lib.ps_kv_layout(self._h, raw, r, self._layout_ref, self._status)
+        if rc:
+            self._raise("ps_kv_layout", rc)
+        if stream is not None:
+            self._record(raw, rows, tables, lens, held, counts, starts, written, *out)
+        return out
 
     # -- attention -------------------------------------------------------------
     def plan(self, q_offsets, kv_lens, tables, num_tokens: int, group_offsets=None, causal: bool = True, stream=None):
