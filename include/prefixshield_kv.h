@@ -23,7 +23,8 @@
  *   ps_kv_layout     where a batch's new tokens go: the offsets, lengths, tables,
  *                    positions and slots that the calls above take;
  *   ps_kv_copy, ps_kv_fork, ps_kv_release, ps_kv_compact
- *                    page copies, forks of sequences, freeing, compaction.
+ *                    page copies, forks of sequences, freeing, compaction;
+ *   ps_kv_reorder    the rows of a beam search follow the beams that they continue.
  *
  * Conventions are prefixshield.h's: d_* pointers (and every pointer inside the
  * argument structures) are device pointers, streams are void* holding a
@@ -51,6 +52,7 @@ typedef enum { PS_KV_BF16 = 0, PS_KV_F16 = 1 } ps_kv_dtype_t;
 
 #define PS_KV_MAX_HEAD_DIM 128
 #define PS_KV_MAX_HEADS 1024      /* query heads */
+#define PS_KV_MAX_BEAMS 32        /* beams of a request */
 
 /* The pool and the bounds of later calls.  Element (layer, page, t, head, e)
  * of K is k[layer * layer_stride + page * page_stride + t * token_stride +
@@ -269,6 +271,25 @@ int32_t ps_kv_layout(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const 
 int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parents, const int32_t* d_children,
                    const int32_t* d_room, const ps_kv_rows_t* rows, const int32_t* d_refs_in, int32_t* d_refs_out,
                    int32_t* d_status);
+
+/* A beam step on the rows of num_requests requests of 'beams' beams each (1..
+ * PS_KV_MAX_BEAMS): request r's beam j is row rows[r * beams + j] (distinct), and
+ * it becomes a continuation of its request's beam d_parents[r * beams + j], as that
+ * one was before the call, with pages for 'grow' more tokens than that one has.
+ * Full pages are shared.  The first of a beam's continuations takes over its partly
+ * filled page and those after it, the others copy that page's tokens (all layers) to
+ * a page of their own.  A parent of -1 leaves an empty row.  What a beam without
+ * continuations held loses a reference; pages without references are free for this
+ * call's own new pages: the free private pages of the lowest ids, in the order of
+ * the rows.  A row's entries past its pages stay as they were.  All or nothing:
+ * rows, parents or ids out of range, a row named twice, more pages than a row holds
+ * set *d_status to PS_ERR_INVALID_ARG, too few free pages to PS_ERR_CAPACITY, and
+ * then nothing changes but refs_out, which becomes refs_in.  refs_out may be
+ * refs_in; otherwise no output lies on another array (refused).  num_requests *
+ * beams is at most max_requests. */
+int32_t ps_kv_reorder(ps_kv_t* kv, void* stream, int32_t num_requests, int32_t beams, const int32_t* d_rows,
+                      const int32_t* d_parents, int32_t grow, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
+                      int32_t* d_refs_out, int32_t* d_status);
 
 /* Free the rows d_rows[i] (distinct): each private page they hold loses one
  * reference, their lens and held become 0.  A row out of range, a page id out

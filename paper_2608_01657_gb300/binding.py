@@ -37,7 +37,7 @@ EXPORTED = ("ps_workspace_bytes", "ps_create", "ps_step", "ps_step_host", "ps_st
             "ps_export_ghost", "ps_set_stage_timing", "ps_get_stage_times", "ps_cached_prefix",
             "ps_cached_prefix_noalloc", "ps_uses_graph", "ps_set_graph", "ps_step_blocks",
             "ps_kv_workspace_bytes", "ps_kv_create", "ps_kv_destroy", "ps_kv_append", "ps_kv_plan",
-            "ps_kv_attention", "ps_kv_layout", "ps_kv_copy", "ps_kv_fork", "ps_kv_release", "ps_kv_compact")
+            "ps_kv_attention", "ps_kv_layout", "ps_kv_copy", "ps_kv_fork", "ps_kv_reorder", "ps_kv_release", "ps_kv_compact")
 PS_NUM_STAGES = 11
 STAGE_NAMES = ("validate", "hash_lookup", "claims", "grant_instep", "meter", "touch_gate", "select",
                "take_lists", "evict", "insert", "commit")
@@ -92,7 +92,7 @@ class PsStateView(C.Structure):
 
 # -- the operators on KV pages (include/prefixshield_kv.h) --------------------
 PS_KV_BF16, PS_KV_F16 = 0, 1
-PS_KV_MAX_HEAD_DIM, PS_KV_MAX_HEADS = 128, 1024
+PS_KV_MAX_HEAD_DIM, PS_KV_MAX_HEADS, PS_KV_MAX_BEAMS = 128, 1024, 32
 
 
 class PsKvConfig(C.Structure):
@@ -202,6 +202,8 @@ def load():
     L.ps_kv_copy.argtypes = [vp, vp, i32, vp, vp, vp]
     L.ps_kv_fork.restype = i32
     L.ps_kv_fork.argtypes = [vp, vp, i32, vp, vp, vp, C.POINTER(PsKvRows), vp, vp, vp]
+    L.ps_kv_reorder.restype = i32
+    L.ps_kv_reorder.argtypes = [vp, vp, i32, i32, vp, vp, i32, C.POINTER(PsKvRows), vp, vp, vp]
     L.ps_kv_release.restype = i32
     L.ps_kv_release.argtypes = [vp, vp, i32, vp, C.POINTER(PsKvRows), vp, vp]
     L.ps_kv_compact.restype = i32

@@ -219,6 +219,7 @@ struct PageHdr {
   int32_t status;  // verdict of the call
   int32_t live;    // pages in use (compact)
   int32_t free_pages;
+  int32_t refused; // an error that a reorder's kernels found (back to 0 after each call)
 };
 constexpr int kScanThreads = 256;
 constexpr int kMaxChunks = 1024;  // chunks of the reference array: one CTA each
@@ -235,6 +236,19 @@ struct PageScratch {
   int32_t* start;       // [max_requests]
   int32_t* bad;         // [max_requests]
   int32_t chunks, chunk_size;
+};
+
+// What becomes of one row of a reorder.
+struct __align__(16) ReorderRec {
+  int32_t row, src;     // the row, and the beam of its request that it continues, -1: none
+  int32_t len, have, total;  // tokens, pages that it takes over or shares, pages in all
+  int32_t part, from;   // tokens to copy, and the page that they are in
+  int32_t pad0;
+};
+struct ReorderScratch {
+  ReorderRec* rec;  // [max_requests]
+  int32_t* delta;   // [private pages] changes of the references, 0 between calls
+  int32_t* refs;    // [private pages] the references to be, the page calls' inv
 };
 
 // ---- layout --------------------------------------------------------------------
@@ -353,6 +367,9 @@ int32_t launch_release(const Pool& p, int32_t n, const int32_t* list, const ps_k
                        int32_t* refs, int32_t* status, cudaStream_t st);
 int32_t launch_compact(const Pool& p, const PageScratch& w, const ps_kv_rows_t& rows, const int32_t* refs_in, int32_t* tables_out, int32_t* refs_out, int32_t* counts,
                        int32_t* status, int nsm, cudaStream_t st);
+int32_t launch_reorder(const Pool& p, const PageScratch& w, const ReorderScratch& o, int32_t requests, int32_t beams, const int32_t* list,
+                       const int32_t* parents, int32_t grow, const ps_kv_rows_t& rows, int32_t row_pages,
+                       const int32_t* refs_in, int32_t* refs_out, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_layout(const Pool& p, const LayoutScratch& w, const ps_kv_layout_t& l, const ps_kv_rows_t& rows, int32_t row_pages,
                       int32_t* status, int nsm, cudaStream_t st);
 // Kernel attributes (shared-memory opt-ins) and the workers of each attention list

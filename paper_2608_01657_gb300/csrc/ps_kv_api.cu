@@ -14,6 +14,7 @@ struct ps_kv {
   Plan plan;
   PageScratch pages;
   LayoutScratch layout;
+  ReorderScratch reorder;
   Batch batch;
   bool planned;
   int32_t turn;  // of the next attention, 0 or 1
@@ -81,7 +82,7 @@ struct Carver {
 // The workspace: sizes with base == nullptr, pointers otherwise.  Every region
 // starts on a 256-byte boundary.  The page header comes first (cleared once).
 size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base, Plan* plan, PageScratch* pages,
-             LayoutScratch* layout) {
+             LayoutScratch* layout, ReorderScratch* reorder) {
   Carver cv{base};
   const int64_t R = c.max_requests, T = c.max_tokens, ratio = c.num_q_heads / c.num_kv_heads;
   PageScratch w{};
@@ -134,6 +135,11 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
   y.base = cv.take<int32_t>(parts + 1);
   y.group_base = cv.take<int32_t>(parts + 1);
   if (layout) *layout = y;
+  ReorderScratch o{};
+  o.rec = cv.take<ReorderRec>((size_t)R);
+  o.delta = cv.take<int32_t>((size_t)np);
+  o.refs = w.inv;
+  if (reorder) *reorder = o;
   if (plan) *plan = p;
   if (pages) *pages = w;
   return (cv.off + 255) / 256 * 256;
@@ -180,13 +186,13 @@ int32_t row_pages(const ps_kv* kv, int64_t stride) {
 extern "C" {
 
 size_t ps_kv_workspace_bytes(const ps_kv_config_t* cfg) {
-  return check_config(cfg) ? carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr) : 0;
+  return check_config(cfg) ? carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr, nullptr) : 0;
 }
 
 int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace, size_t workspace_bytes,
                      void* stream) {
   if (!out || !check_config(cfg) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0 ||
-      workspace_bytes < carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr))
+      workspace_bytes < carve(*cfg, kSizedWorkers, nullptr, nullptr, nullptr, nullptr, nullptr))
     return PS_ERR_INVALID_ARG;
   int dev = 0, nsm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
@@ -210,12 +216,14 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
   for (int l = 0; l < kLists; ++l)
     if (workers[l] > kSizedWorkers[l]) workers[l] = kSizedWorkers[l];
   if (rc == PS_OK) {
-    carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages, &kv->layout);
+    carve(*cfg, kSizedWorkers, static_cast<char*>(d_workspace), &kv->plan, &kv->pages, &kv->layout, &kv->reorder);
     for (int l = 0; l < kLists; ++l) kv->plan.max_workers[l] = workers[l];
     // and a plan that is empty, for an attention that runs before its plan has (one that was only captured into a graph)
     static_assert(PS_ERR_INVALID_ARG == -1, "the status word of all ones");
     PlanHdr* hdr = kv->plan.hdr;
+    const size_t np = (size_t)(kv->pool.num_pages - kv->pool.first_page);
     if (cudaMemsetAsync(kv->pages.hdr, 0, sizeof(PageHdr), as_stream(stream)) != cudaSuccess ||
+        (np > 0 && cudaMemsetAsync(kv->reorder.delta, 0, 4 * np, as_stream(stream)) != cudaSuccess) ||
         cudaMemsetAsync(hdr, 0, sizeof(PlanHdr), as_stream(stream)) != cudaSuccess ||
         cudaMemsetAsync(&hdr->status, 0xFF, sizeof(hdr->status), as_stream(stream)) != cudaSuccess)
       rc = PS_ERR_CUDA;
@@ -327,6 +335,22 @@ int32_t ps_kv_fork(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_parent
   if (partly_same(d_refs_in, d_refs_out, kv->pool.num_pages - kv->pool.first_page)) return PS_ERR_INVALID_ARG;
   return launch_fork(kv->pool, kv->pages, n, d_parents, d_children, d_room, *rows, row_pages(kv, rows->table_stride),
                      d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
+}
+
+int32_t ps_kv_reorder(ps_kv_t* kv, void* stream, int32_t num_requests, int32_t beams, const int32_t* d_rows,
+                      const int32_t* d_parents, int32_t grow, const ps_kv_rows_t* rows, const int32_t* d_refs_in,
+                      int32_t* d_refs_out, int32_t* d_status) {
+  if (!kv || !rows_ok(kv, rows) || num_requests < 0 || beams < 1 || beams > PS_KV_MAX_BEAMS || grow < 0 ||
+      (int64_t)num_requests * beams > kv->max_requests || !refs_ok(kv, d_refs_in, d_refs_out) || rows->table_stride >= (1ll << 30))
+    return PS_ERR_INVALID_ARG;
+  if (num_requests > 0 && (!d_rows || !d_parents)) return PS_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)num_requests * beams, np = kv->pool.num_pages - kv->pool.first_page, m = rows->num_rows;
+  const Span spans[] = {{d_rows, 4 * n, false}, {d_parents, 4 * n, false}, {d_status, 4, false},
+                        {d_refs_in == d_refs_out ? nullptr : d_refs_in, 4 * np, false}, {d_refs_out, 4 * np, true},
+                        {rows->tables, 4 * m * rows->table_stride, true}, {rows->lens, 4 * m, true}, {rows->held, 4 * m, true}};
+  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  return launch_reorder(kv->pool, kv->pages, kv->reorder, num_requests, beams, d_rows, d_parents, grow, *rows,
+                        row_pages(kv, rows->table_stride), d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
 }
 
 int32_t ps_kv_release(ps_kv_t* kv, void* stream, int32_t n, const int32_t* d_rows, const ps_kv_rows_t* rows,

@@ -3,8 +3,8 @@
 ``KVPool`` wraps one pool of keys and values and the C ABI of
 ``include/prefixshield_kv.h``: laying a batch out (offsets, lengths, tables,
 positions, slots), appending tokens (norms of queries and keys, rotation, page
-write), attention over the pages with shared prefixes read once, and copying,
-forking, freeing and compacting pages.  As in ``binding``,
+write), attention over the pages with shared prefixes read once, copying,
+forking, freeing and compacting pages, and the beam step of a search's rows.  As in ``binding``,
 arguments are marshalled here and all work runs in the library's CUDA kernels;
 torch provides device memory and streams.  Calls are enqueued on ``stream``
 (default: the current one) and do not synchronize; what a call that names its
@@ -345,6 +345,26 @@ class KVPool:
             self._raise("ps_kv_fork", rc)
         if stream is not None:
             self._record(raw, parents, children, room, tables, lens, held, refs, refs_out)
+
+    def reorder(self, rows, parents, tables, lens, held, refs, grow: int = 1, refs_out=None, stream=None):
+        """A beam step: ``rows`` [requests, beams] become continuations of their
+        requests' beams ``parents`` [requests, beams] (-1: an empty row), with
+        pages for ``grow`` more tokens than those have.  Full pages are shared, a
+        beam's first continuation takes over its partly filled page, the others
+        copy it; what no beam continues is freed."""
+        if len(rows.shape) != 2 or rows.shape != parents.shape:
+            raise ValueError("rows and parents must be [requests, beams]")
+        (n, beams), raw = rows.shape, self._stream(stream)
+        for t, name in ((rows, "rows"), (parents, "parents")):
+            if t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 [requests, beams] tensor")
+        r, before = self._rows(tables, lens, held), self._refs(refs)
+        rc = self._lib.ps_kv_reorder(self._h, raw, n, beams, rows.data_ptr(), parents.data_ptr(), grow, r, before,
+                                     before if refs_out is None else self._refs(refs_out, "refs_out"), self._status)
+        if rc:
+            self._raise("ps_kv_reorder", rc)
+        if stream is not None:
+            self._record(raw, rows, parents, tables, lens, held, refs, refs_out)
 
     def release(self, rows, tables, lens, held, refs, stream=None):
         """Free the pages that ``rows`` hold."""
