@@ -3,8 +3,9 @@
 The compute path is the CUDA library ``libprefixshield.so`` (C ABI declared in
 ``include/prefixshield.h``); ``binding`` is its thin ctypes layer.  ``kv`` wraps
 the operators on the KV pages behind the block ids (``include/prefixshield_kv.h``),
-``serving`` is a small loop that uses both.  Importing
-this package does not load the library: ``binding.load()`` does, and it fails
-loudly when the library has not been built.
+``beam`` those of beam search (``include/prefixshield_beam.h``), ``serving`` is a
+small loop that uses all of them.  Importing this package does not load the
+library: ``binding.load()`` does, and it fails loudly when the library has not
+been built.
 """
-__all__ = ["binding", "workloads", "build", "kv", "serving"]
+__all__ = ["binding", "workloads", "build", "kv", "beam", "serving"]

@@ -37,7 +37,8 @@ EXPORTED = ("ps_workspace_bytes", "ps_create", "ps_step", "ps_step_host", "ps_st
             "ps_export_ghost", "ps_set_stage_timing", "ps_get_stage_times", "ps_cached_prefix",
             "ps_cached_prefix_noalloc", "ps_uses_graph", "ps_set_graph", "ps_step_blocks",
             "ps_kv_workspace_bytes", "ps_kv_create", "ps_kv_destroy", "ps_kv_append", "ps_kv_plan",
-            "ps_kv_attention", "ps_kv_layout", "ps_kv_copy", "ps_kv_fork", "ps_kv_reorder", "ps_kv_release", "ps_kv_compact")
+            "ps_kv_attention", "ps_kv_layout", "ps_kv_copy", "ps_kv_fork", "ps_kv_reorder", "ps_kv_release", "ps_kv_compact",
+            "ps_beam_workspace_bytes", "ps_beam_create", "ps_beam_destroy", "ps_beam_select", "ps_beam_trace")
 PS_NUM_STAGES = 11
 STAGE_NAMES = ("validate", "hash_lookup", "claims", "grant_instep", "meter", "touch_gate", "select",
                "take_lists", "evict", "insert", "commit")
@@ -130,6 +131,27 @@ class PsKvLayout(C.Structure):
         (n, C.c_int32) for n in ("num_requests", "num_tokens", "pad", "pad0")]
 
 
+# -- beam search (include/prefixshield_beam.h) --------------------------------
+PS_BEAM_BF16, PS_BEAM_F16, PS_BEAM_F32 = 0, 1, 2
+PS_BEAM_MAX_BEAMS, PS_BEAM_MAX_END = 32, 8
+
+
+class PsBeamConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("max_requests", "beams", "vocab", "dtype", "num_end")] + [
+        ("end_tokens", C.c_int32 * PS_BEAM_MAX_END), ("pad0", C.c_int32)]
+
+
+class PsBeamSelect(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "scores", "tokens", "parents", "scores_out", "ended_tokens",
+                                          "ended_parents", "ended_scores")] + [
+        (n, C.c_int64) for n in ("request_stride", "beam_stride")] + [(n, C.c_int32) for n in ("num_requests", "pad0")]
+
+
+class PsBeamTrace(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("tokens", "parents", "beams_of", "lengths", "out")] + [
+        (n, C.c_int32) for n in ("num_steps", "num_requests", "hyps", "pad0")]
+
+
 _lib = None
 
 
@@ -208,6 +230,16 @@ def load():
     L.ps_kv_release.argtypes = [vp, vp, i32, vp, C.POINTER(PsKvRows), vp, vp]
     L.ps_kv_compact.restype = i32
     L.ps_kv_compact.argtypes = [vp, vp, C.POINTER(PsKvRows), vp, vp, vp, vp, vp]
+    L.ps_beam_workspace_bytes.restype = sz
+    L.ps_beam_workspace_bytes.argtypes = [C.POINTER(PsBeamConfig)]
+    L.ps_beam_create.restype = i32
+    L.ps_beam_create.argtypes = [C.POINTER(vp), C.POINTER(PsBeamConfig), vp, sz, vp]
+    L.ps_beam_destroy.restype = None
+    L.ps_beam_destroy.argtypes = [vp]
+    L.ps_beam_select.restype = i32
+    L.ps_beam_select.argtypes = [vp, vp, C.POINTER(PsBeamSelect), vp]
+    L.ps_beam_trace.restype = i32
+    L.ps_beam_trace.argtypes = [vp, vp, C.POINTER(PsBeamTrace), vp]
     _lib = L
     return L
 

@@ -1,0 +1,528 @@
+// ps_beam_select: the best continuations of a request's beams.
+//
+// Of a beam with score c and logits x, token v continues it with the score c + x_v
+// - lse, lse = log sum_u exp x_u.  Within a beam the order is the logits', so one
+// pass over a row keeps two things: a sum of 2^((x - ref) log2 e), whose reference
+// rises with the greatest logit seen, and the 'beams' greatest logits whose tokens
+// end nothing (a request's best are among its beams' best).  Those are kept as whole
+// numbers, the logit's bits in order and then the token's complement, so that no two
+// are equal and equal logits go to the lowest token.
+//
+// Bound by HBM: a logit is read once.  A row is cut into parts, a CTA each, so that
+// a few rows fill the GPU, too; the last CTA of a request to finish puts the parts
+// together, in an order that does not depend on which one it is.
+//
+// A warp reads 4 KB at a time.  A list of 32 is sorted across its lanes; what is
+// greater than the list's beams-th enters a queue, 32 of which are sorted and merged
+// at a time.  The first threshold is the beams-th of the lanes' greatest, so that
+// about as many enter as are kept.
+//
+// Neighbours in the order of scores may be nearer than 32 bits tell: differences
+// from the reference are exact or rounded once, log2 e has two parts, the lanes' sums
+// are added in 64 bits, and so are the scores.
+#include "ps_beam.cuh"
+
+namespace psbeam {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kVecs = 8;           // 16-byte loads of a lane and chunk
+constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
+constexpr double kLn2 = 0.693147180559945309;
+constexpr unsigned kAll = 0xFFFFFFFFu;
+
+struct Args {
+  ps_beam_select_t a;
+  Search s;
+  int32_t* status;
+  int32_t parts;  // of a row
+};
+
+// ---- elements ---------------------------------------------------------------------
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int N = 4;  // of a 16-byte word
+  static __device__ __forceinline__ void wide(const uint4& v, float (&x)[N]) {
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&x)[N]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+  static __device__ __forceinline__ float one(const void* p) { return *static_cast<const float*>(p); }
+};
+template <typename H>
+struct Elem16 {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void wide(const uint4& v, float (&x)[N]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = pskv::Num<H>::unpack(w[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&x)[N]) {  // of values that H holds
+    return make_uint4(pskv::Num<H>::pack(x[0], x[1]), pskv::Num<H>::pack(x[2], x[3]), pskv::Num<H>::pack(x[4], x[5]),
+                      pskv::Num<H>::pack(x[6], x[7]));
+  }
+  static __device__ __forceinline__ uint4 none() {  // -infinity
+    constexpr uint32_t w = pskv::Num<H>::kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
+    return make_uint4(w, w, w, w);
+  }
+};
+template <>
+struct Elem<__nv_bfloat16> : Elem16<__nv_bfloat16> {
+  static __device__ __forceinline__ float one(const void* p) { return __bfloat162float(*static_cast<const __nv_bfloat16*>(p)); }
+};
+template <>
+struct Elem<__half> : Elem16<__half> {
+  static __device__ __forceinline__ float one(const void* p) { return __half2float(*static_cast<const __half*>(p)); }
+};
+// The greater, NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// ---- keys ---------------------------------------------------------------------------
+// The bits of x as a whole number in x's order; -0 is 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return (int32_t)u < 0 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((int32_t)o < 0 ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ uint64_t key_of(float x, int token) { return (uint64_t)ordered(x) << 32 | (uint32_t)~token; }
+__device__ __forceinline__ float logit_of(uint64_t key) { return unordered((uint32_t)(key >> 32)); }
+__device__ __forceinline__ int token_of(uint64_t key) { return (int)~(uint32_t)key; }
+// No token of -infinity has a greater one.
+constexpr uint64_t kNoKey = 0x007FFFFFFFFFFFFFull;
+
+__device__ __forceinline__ void exchange(uint64_t& x, int other, bool greater) {
+  const uint64_t y = __shfl_xor_sync(kAll, x, other);
+  x = (x > y) == greater ? x : y;
+}
+// 32 numbers, one a lane, from the greatest to the least.
+__device__ __forceinline__ uint64_t sort32(uint64_t x, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) exchange(x, j, ((lane & j) == 0) == ((lane & k) == 0));
+  return x;
+}
+// The 32 greatest of two such lists, as one.
+__device__ __forceinline__ uint64_t merge32(uint64_t x, uint64_t y, int lane) {
+  const uint64_t z = __shfl_sync(kAll, y, 31 - lane);
+  x = x > z ? x : z;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) exchange(x, j, (lane & j) == 0);
+  return x;
+}
+
+__device__ __forceinline__ bool ends(const Search& s, int token) {
+  bool e = false;
+  for (int i = 0; i < s.num_end; ++i) e = e || s.end[i] == token;
+  return e;
+}
+
+// A warp's best so far.
+constexpr int kQueue = 31 + 32 * 8;  // what may wait, and a word of every lane
+struct Best {
+  uint64_t list;    // of the lane
+  uint64_t floor;   // what enters is greater
+  int queued;
+  uint64_t* queue;  // [kQueue] of the warp
+  uint64_t* shared; // the greatest floor of the CTA's warps
+  int keep, lane;
+  __device__ __forceinline__ void raise(uint64_t to) { floor = floor > to ? floor : to; }
+  __device__ __forceinline__ void flush() {  // the last 32 of the queue, or all of it
+    const int from = queued > 32 ? queued - 32 : 0;
+    __syncwarp();
+    const uint64_t q = from + lane < queued ? queue[from + lane] : 0;
+    __syncwarp();
+    queued = from;
+    list = merge32(list, sort32(q, lane), lane);
+    raise(__shfl_sync(kAll, list, keep - 1));
+    if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(shared), (unsigned long long)floor);
+  }
+  // The lanes' words of neighbouring elements, from 'token' on.
+  template <int N>
+  __device__ __forceinline__ void add(const Search& s, const float (&x)[N], int token) {
+    const float least = logit_of(floor + 1);  // a smaller logit does not enter
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if (!__any_sync(kAll, x[e] >= least)) continue;
+      const uint64_t key = key_of(x[e], token + e);
+      const bool on = x[e] >= least && key > floor && !ends(s, token + e);
+      const unsigned m = __ballot_sync(kAll, on);
+      if (on) queue[queued + __popc(m & ((1u << lane) - 1))] = key;
+      queued += __popc(m);
+    }
+    while (queued >= 32) flush();
+  }
+};
+
+// A lane's sum of exp(x - ref).
+struct Sum {
+  float ref, sum;
+  __device__ __forceinline__ void raise(float to) {
+    if (to > ref) {
+      sum = ref == -INFINITY ? 0.0f : sum * pskv::ex2((ref - to) * kLog2e);
+      ref = to;
+    }
+  }
+  // What is subtracted: nothing while all are -infinity.
+  __device__ __forceinline__ float base() const { return ref == -INFINITY ? 0.0f : ref; }
+};
+
+// ---- a part of a row ------------------------------------------------------------------
+// Words of 16 bytes are counted from the row's first element on, wherever that lies in
+// memory, so that a row's sum does not depend on its address: equal beams are equal to
+// the last bit.  Where the row does not start on a 16-byte boundary a word is put
+// together from two aligned ones ('shift' elements of the first are not its own); what
+// would reach past the row is read by elements.
+template <typename T>
+__device__ __noinline__ uint4 edge_word(const T* row, int first, int V) {
+  constexpr int N = Elem<T>::N;
+  float x[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = first + e < V ? Elem<T>::one(row + first + e) : -INFINITY;
+  return Elem<T>::narrow(x);
+}
+template <typename T>
+__device__ __forceinline__ void read_chunk(const T* row, int shift, int w0, int words, int V, uint4 (&v)[kVecs]) {
+  constexpr int N = Elem<T>::N;
+  const int full = V / N;
+  if (shift == 0) {
+    const uint4* at = reinterpret_cast<const uint4*>(row);
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      const int w = w0 + 32 * j;
+      if (w < full) v[j] = __ldcs(at + w);
+    }
+  } else {
+    const uint4* at = reinterpret_cast<const uint4*>(row - shift);
+    const int last = (V + shift) / N - 1;  // the last aligned word that is wholly the row's
+    uint4 next[kVecs];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      const int w = w0 + 32 * j;
+      if (w > 0 && w < last) {
+        v[j] = __ldg(at + w);
+        next[j] = __ldg(at + w + 1);
+      }
+    }
+    const int words4 = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, next[j].x, next[j].y, next[j].z, next[j].w};
+      if (words4 & 2) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
+      }
+      if (words4 & 1) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) x[i] = x[i + 1];
+      }
+      v[j] = make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
+                        __funnelshift_r(x[3], x[4], bits));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int w = w0 + 32 * j;
+    if (shift == 0 ? w >= full : (w == 0 || w >= (V + shift) / N - 1)) v[j] = w < words ? edge_word(row, w * N, V) : Elem<T>::none();
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void scan_part(const Args& g, const T* row, int part, Best& best, Sum& sum, float& most) {
+  constexpr int N = Elem<T>::N, kChunk = 32 * kVecs;
+  const int lane = best.lane, warp = threadIdx.x >> 5, V = g.s.vocab;
+  const int shift = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(T);
+  const int words = (V + N - 1) / N;
+  const int chunks = (words + kChunk - 1) / kChunk;
+  const int c0 = (int)((int64_t)chunks * part / g.parts), c1 = (int)((int64_t)chunks * (part + 1) / g.parts);
+  bool seeded = false;
+  for (int c = c0 + warp; c < c1; c += kWarps) {
+    uint4 v[kVecs];
+    read_chunk(row, shift, c * kChunk + lane, words, V, v);
+    float top[kVecs], all = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      float x[N];
+      Elem<T>::wide(v[j], x);
+      float m = x[0];
+#pragma unroll
+      for (int e = 1; e < N; ++e) m = max_nan(m, x[e]);
+      top[j] = m;
+      all = max_nan(all, m);
+    }
+    most = max_nan(most, all);
+    sum.raise(all);
+    const float base = sum.base();
+    const uint64_t minus = pskv::pack2(-base, -base), hi = pskv::pack2(kLog2e, kLog2e), lo = pskv::pack2(kLog2eRest, kLog2eRest);
+    uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      float x[N];
+      Elem<T>::wide(v[j], x);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        const uint64_t d = pskv::add2(pskv::pack2(x[e], x[e + 1]), minus);
+        const float2 t = pskv::unpack2(pskv::fma2(d, lo, pskv::mul2(d, hi)));
+        const uint64_t p = pskv::pack2(pskv::ex2(t.x), pskv::ex2(t.y));
+        if (e & 2) s1 = pskv::add2(s1, p);
+        else s0 = pskv::add2(s0, p);
+      }
+    }
+    const float2 f = pskv::unpack2(pskv::add2(s0, s1));
+    sum.sum += f.x + f.y;
+    // candidates
+    const int t0 = (c * kChunk + lane) * N;  // token of the lane's first element
+    if (!seeded) {
+      seeded = true;
+      float m = all;
+      bool has = false;
+      for (int i = 0; i < g.s.num_end; ++i) {
+        const int at = g.s.end[i] - t0;
+        has = has || (at >= 0 && at < kVecs * 32 * N && at % (32 * N) < N);
+      }
+      if (__any_sync(kAll, has)) {  // end tokens do not count
+        m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+          float x[N];
+          Elem<T>::wide(v[j], x);
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (!ends(g.s, t0 + j * 32 * N + e)) m = fmaxf(m, x[e]);
+        }
+      }
+      const uint64_t s = __shfl_sync(kAll, sort32((uint64_t)ordered(m) << 32, lane), best.keep - 1);
+      if (s > 0) best.raise(s - 1);
+    }
+    best.raise(*reinterpret_cast<volatile uint64_t*>(best.shared));
+    const float least = logit_of(best.floor + 1);  // a smaller logit does not enter
+    if (!__any_sync(kAll, all >= least)) continue;
+    unsigned hits = 0;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) hits |= (__any_sync(kAll, top[j] >= least) ? 1u : 0u) << j;
+    while (hits) {  // one of the lane's words at a time
+      const int j = __ffs(hits) - 1;
+      hits &= hits - 1;
+      uint4 w = v[0];
+#pragma unroll
+      for (int i = 1; i < kVecs; ++i)
+        if (i == j) w = v[i];
+      float x[N];
+      Elem<T>::wide(w, x);
+      best.add(g.s, x, t0 + j * 32 * N);
+    }
+  }
+  while (best.queued > 0) best.flush();
+}
+
+// ---- the parts of a request -------------------------------------------------------------
+// A candidate: the greater score, then the lower beam, then the greater key is first.
+struct Cand {
+  double score;
+  int beam;
+  uint64_t key;
+  __device__ __forceinline__ bool before(const Cand& y) const {
+    return score != y.score ? score > y.score : (beam != y.beam ? beam < y.beam : key > y.key);
+  }
+  __device__ __forceinline__ Cand shfl(int from) const {
+    return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, beam, from), __shfl_sync(kAll, key, from)};
+  }
+};
+__device__ __forceinline__ Cand no_cand(int lane) { return {-INFINITY, PS_BEAM_MAX_BEAMS + lane, 0}; }
+__device__ __forceinline__ void exchange(Cand& x, int lane, int other, bool first) {
+  const Cand y = x.shfl(lane ^ other);
+  if (x.before(y) != first) x = y;
+}
+__device__ __forceinline__ Cand sort32(Cand x, int lane) {
+  for (int k = 2; k <= 32; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) exchange(x, lane, j, ((lane & j) == 0) == ((lane & k) == 0));
+  return x;
+}
+__device__ __forceinline__ Cand merge32(Cand x, const Cand& y, int lane) {
+  const Cand z = y.shfl(31 - lane);
+  if (z.before(x)) x = z;
+  for (int j = 16; j > 0; j >>= 1) exchange(x, lane, j, (lane & j) == 0);
+  return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish(const Args& g, int r) {
+  __shared__ Cand cand[PS_BEAM_MAX_BEAMS][32];
+  // of each beam: its score, the reference, the log of the sum over it (+infinity: no
+  // candidates).  The reference, which may be far from 0, is subtracted first.
+  __shared__ double s_sum[PS_BEAM_MAX_BEAMS];
+  __shared__ float s_score[PS_BEAM_MAX_BEAMS], s_ref[PS_BEAM_MAX_BEAMS];
+  auto score = [&](int b, float logit) { return (double)s_score[b] + (((double)logit - (double)s_ref[b]) - s_sum[b]); };
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams, S = g.parts;
+  for (int b = warp; b < B; b += kWarps) {
+    const int64_t row = (int64_t)r * B + b;
+    const float c = g.a.scores[row];
+    bool good = c - c == 0;  // finite
+    if (!good && c != -INFINITY && lane == 0) set_error(g.status, PS_ERR_INVALID_ARG);
+    double total = INFINITY;
+    float ref = -INFINITY;
+    uint64_t list = 0;
+    if (good) {
+      Part p{0.0, -INFINITY, 0};
+      if (lane < S) {
+        const Part* q = g.s.parts + row * S + lane;
+        p.sum = __ldcg(&q->sum);
+        p.ref = __ldcg(&q->ref);
+        p.bad = __ldcg(&q->bad);
+      }
+      if (__any_sync(kAll, p.bad)) {
+        if (lane == 0) set_error(g.status, PS_ERR_INVALID_ARG);
+        good = false;
+      }
+      ref = p.ref;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(kAll, ref, o));
+      if (ref == -INFINITY) good = false;  // no token may follow
+      double sum = p.ref == -INFINITY ? 0.0 : p.sum * exp2(((double)p.ref - (double)ref) / kLn2);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+      if (good) {
+        total = log(sum);
+        for (int i = 0; i < S; ++i) {
+          const uint64_t k = lane < B ? __ldcg(g.s.keys + (row * S + i) * B + lane) : 0;
+          list = i ? merge32(list, k, lane) : k;
+        }
+      }
+    }
+    const bool on = good && lane < B && list > kNoKey;
+    if (lane == 0) s_score[b] = c, s_ref[b] = ref, s_sum[b] = total;
+    __syncwarp();
+    cand[b][lane] = on ? Cand{score(b, logit_of(list)), b, list} : no_cand(lane);
+  }
+  __syncthreads();
+  if (warp != 0) return;
+  Cand best = cand[0][lane];
+  for (int b = 1; b < B; ++b) best = merge32(best, cand[b][lane], lane);
+  const int64_t to = (int64_t)r * B + lane;
+  if (lane < B) {
+    const bool on = best.score > -INFINITY;
+    g.a.tokens[to] = on ? token_of(best.key) : -1;
+    g.a.parents[to] = on ? best.beam : -1;
+    g.a.scores_out[to] = on ? (float)best.score : -INFINITY;
+  }
+  if (!g.a.ended_tokens) return;
+  // the end tokens' candidates, the 32 first
+  Cand last = no_cand(lane);
+  for (int i0 = 0; i0 < B * g.s.num_end; i0 += 32) {
+    const int i = i0 + lane;
+    Cand x = no_cand(lane);
+    if (i < B * g.s.num_end) {
+      const int b = i / g.s.num_end, token = g.s.end[i % g.s.num_end];
+      if (s_sum[b] < INFINITY) {
+        const T* row = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride;
+        const float l = Elem<T>::one(row + token);
+        if (l > -INFINITY) x = Cand{score(b, l), b, key_of(l, token)};
+      }
+    }
+    last = merge32(last, sort32(x, lane), lane);
+  }
+  // its place among all candidates: those of its kind before it are the lanes below
+  int place = lane;
+  for (int i = 0; i < B; ++i) place += best.shfl(i).before(last);
+  const bool on = last.score > -INFINITY && place < B;  // (places rise with the lanes)
+  if (lane < B) {
+    g.a.ended_tokens[to] = on ? token_of(last.key) : -1;
+    g.a.ended_parents[to] = on ? last.beam : -1;
+    g.a.ended_scores[to] = on ? (float)last.score : -INFINITY;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) k_select(Args g) {
+  __shared__ uint64_t queue[kWarps][kQueue], lists[kWarps][32], s_floor;
+  __shared__ double sums[kWarps];
+  __shared__ float refs[kWarps];
+  __shared__ int bads[kWarps];
+  __shared__ bool s_last;
+  chain();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams;
+  const int64_t row = blockIdx.x / g.parts;
+  const int part = (int)(blockIdx.x % g.parts), r = (int)(row / B), b = (int)(row % B);
+  const float c = g.a.scores[row];
+  if (c - c == 0) {  // (a score that is not finite: nothing is read of the row)
+    if (threadIdx.x == 0) s_floor = kNoKey;
+    __syncthreads();
+    Best best{0, kNoKey, 0, queue[warp], &s_floor, B, lane};
+    Sum sum{-INFINITY, 0.0f};
+    float most = -INFINITY;
+    scan_part(g, static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride, part, best, sum, most);
+    // the lanes', then the warps' sums and lists
+    float ref = sum.ref;
+    const bool bad = __any_sync(kAll, !(most < INFINITY));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(kAll, ref, o));
+    double s = sum.ref == -INFINITY ? 0.0 : (double)sum.sum * (double)pskv::ex2((sum.ref - ref) * kLog2e);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
+    lists[warp][lane] = best.list;
+    if (lane == 0) sums[warp] = s, refs[warp] = ref, bads[warp] = bad;
+    for (int half = kWarps / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      if (warp < half) {
+        best.list = merge32(best.list, lists[warp + half][lane], lane);
+        lists[warp][lane] = best.list;
+      }
+    }
+    if (warp == 0) {
+      const int64_t at = row * g.parts + part;
+      float top = lane < kWarps ? refs[lane] : -INFINITY;
+      const float mine = top;
+      const bool any = __any_sync(kAll, lane < kWarps && bads[lane < kWarps ? lane : 0]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+      double t = mine == -INFINITY ? 0.0 : sums[lane] * exp2(((double)mine - (double)top) / kLn2);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(kAll, t, o);
+      if (lane == 0) g.s.parts[at] = Part{t, top, any};
+      if (lane < B) g.s.keys[at * B + lane] = best.list;
+    }
+  }
+  // the last CTA of a request
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s_last = atomicAdd(g.s.done + r, 1) == B * g.parts - 1;
+    if (s_last) g.s.done[r] = 0;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  finish<T>(g, r);
+}
+
+}  // namespace
+
+int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, cudaStream_t st) {
+  Args g{a, s, status, 1};
+  const int64_t rows = (int64_t)a.num_requests * s.beams;
+  const int64_t chunk = 32 * kVecs * (s.dtype == PS_BEAM_F32 ? 4 : 8), chunks = (s.vocab + chunk - 1) / chunk;
+  int64_t parts = kSpreadCtas / rows;
+  const int64_t most = (chunks + kWarps - 1) / kWarps;
+  parts = parts < most ? parts : most;
+  g.parts = (int32_t)(parts < 1 ? 1 : (parts > kMaxParts ? kMaxParts : parts));
+  const dim3 grid((unsigned)(rows * g.parts));
+  switch (s.dtype) {
+    case PS_BEAM_BF16: return status_of(launch(k_select<__nv_bfloat16>, grid, kThreads, 0, st, g));
+    case PS_BEAM_F16: return status_of(launch(k_select<__half>, grid, kThreads, 0, st, g));
+    default: return status_of(launch(k_select<float>, grid, kThreads, 0, st, g));
+  }
+}
+
+}  // namespace psbeam

@@ -158,22 +158,6 @@ bool partly_same(const int32_t* a, const int32_t* b, int64_t n) {
   const int64_t d = ((intptr_t)a - (intptr_t)b) / 4;
   return a != b && d < n && d > -n;
 }
-// Arrays of a call, for finding outputs that lie on inputs or on one another.
-struct Span {
-  const void* p;
-  int64_t bytes;
-  bool out;
-};
-template <size_t N>
-bool outputs_apart(const Span (&s)[N]) {
-  for (size_t i = 0; i < N; ++i)
-    for (size_t j = 0; j < N; ++j) {
-      if (i == j || !s[i].out || !s[i].p || !s[j].p || s[i].bytes <= 0 || s[j].bytes <= 0) continue;
-      const int64_t d = (intptr_t)s[i].p - (intptr_t)s[j].p;
-      if (d < s[j].bytes && -d < s[i].bytes) return false;
-    }
-  return true;
-}
 bool rows_ok(const ps_kv* kv, const ps_kv_rows_t* r) {
   return r && r->tables && r->lens && r->held && r->num_rows >= 1 && r->table_stride >= 1;
 }

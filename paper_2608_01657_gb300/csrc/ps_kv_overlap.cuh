@@ -1,6 +1,7 @@
-// Whether strided arrays of heads lie on one another (host code).
+// Whether arrays of a call lie on one another (host code).
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 
 namespace pskv {
@@ -67,6 +68,23 @@ inline bool heads_overlap(HeadRuns x, HeadRuns y, int64_t tokens, int64_t dim, b
       }
     }
   return false;
+}
+
+// Arrays of a call, for finding outputs that lie on inputs or on one another.
+struct Span {
+  const void* p;
+  int64_t bytes;
+  bool out;
+};
+template <size_t N>
+inline bool outputs_apart(const Span (&s)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j) {
+      if (i == j || !s[i].out || !s[i].p || !s[j].p || s[i].bytes <= 0 || s[j].bytes <= 0) continue;
+      const int64_t d = (intptr_t)s[i].p - (intptr_t)s[j].p;
+      if (d < s[j].bytes && -d < s[i].bytes) return false;
+    }
+  return true;
 }
 
 }  // namespace pskv

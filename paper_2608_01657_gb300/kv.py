@@ -31,76 +31,26 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-class Layout(NamedTuple):
-    """A batch's arrays, as ``append`` and ``plan`` take them."""
-    q_offsets: torch.Tensor                # int32 [requests + 1]
-    kv_lens: torch.Tensor                  # int32 [requests]
-    tables: torch.Tensor                   # int32 [requests, pages]
-    positions: torch.Tensor                # int32 [tokens]
-    slots: torch.Tensor                    # int64 [tokens]
-    group_offsets: Optional[torch.Tensor]  # int32 [requests + 1]
+class Handle:
+    """What the wrappers of the library's handles share: ``status`` (a sticky int32
+    word of the device's errors), the streams that the handle's memory is used on,
+    and checks of arrays.  A subclass sets ``device``, ``workspace``, ``status``
+    and ``_kept``, the tensors that outlive its calls, and calls ``_begin``."""
 
+    _h = None
+    _destroy = ""               # entry point that frees the handle
+    _what = "a call on the pool"
 
-class KVPool:
-    """One paged pool of keys and values on the current CUDA device.
-
-    ``k`` and ``v`` are tensors [layers, pages, page_size, kv_heads, head_dim]
-    with the same strides, the innermost one 1 (a head-major pool is passed as
-    its transposed view).  Page ids below ``first_page`` are the prefix
-    cache's block ids, the others private pages of running requests.  The
-    references count private pages alone: a later step of the cache may evict a
-    block that a row still names, so no step runs while rows name cached pages,
-    or the pages that it evicts are copied to private ones before its appends."""
-
-    def __init__(self, k, v, num_q_heads: int, first_page: int = 0, max_requests: int = 1, max_tokens: int = 1,
-                 max_row_pages: int = 1, stream=None):
-        L = B.load()
-        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype,
-              "k and v must be alike: [layers, pages, page_size, kv_heads, head_dim]")
-        _need(k.is_cuda and v.device == k.device and k.device.index == torch.cuda.current_device(),
-              "k and v must be on the current CUDA device")
-        _need(k.dtype in (torch.bfloat16, torch.float16), "a pool is bfloat16 or float16")
-        _need(k.stride(4) == 1, "the innermost stride must be 1")
-        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+    def _begin(self, stream):
         self._index = self.device.index
-        self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim = (int(x) for x in k.shape)
-        self.q_heads, self.first_page = int(num_q_heads), int(first_page)
-        self.max_requests, self.max_tokens, self.max_row_pages = int(max_requests), int(max_tokens), int(max_row_pages)
-        c = B.PsKvConfig(k=k.data_ptr(), v=v.data_ptr(), num_pages=self.pages, first_page=self.first_page,
-                         layer_stride=k.stride(0), page_stride=k.stride(1), token_stride=k.stride(2),
-                         head_stride=k.stride(3), num_layers=self.layers, page_size=self.page_size,
-                         num_kv_heads=self.kv_heads, num_q_heads=self.q_heads, head_dim=self.head_dim,
-                         dtype=B.PS_KV_BF16 if k.dtype == torch.bfloat16 else B.PS_KV_F16,
-                         max_requests=self.max_requests, max_tokens=self.max_tokens, max_row_pages=self.max_row_pages)
-        nbytes = L.ps_kv_workspace_bytes(C.byref(c))
-        _need(nbytes > 0, "invalid pool configuration")
-        with B._on_stream(stream, self.device):
-            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        h = C.c_void_p()
-        self._raise("ps_kv_create", L.ps_kv_create(C.byref(h), C.byref(c), self.workspace.data_ptr(), nbytes,
-                                                   B._stream_ptr(stream)))
-        self._h = h
-        self._batch = None
-        self._used, self._batch_used = {}, set()  # streams that the pool's memory, and the plan's, is recorded on
-        self._stream(stream)
-        # argument structures and entry points of the calls that a decode step
-        # makes for every layer; their fields are filled in anew each time
-        self._lib = L
+        self._used = {}  # streams that the handle's memory is recorded on
+        self._lib = B.load()
         self._status = self.status.data_ptr()
-        self._append_args, self._attention_args = B.PsKvAppend(), B.PsKvAttention()
-        self._append_ref, self._attention_ref = C.byref(self._append_args), C.byref(self._attention_args)
-        self._rows_args = B.PsKvRows()
-        self._rows_ref = C.byref(self._rows_args)
-        self._layout_args = B.PsKvLayout()
-        self._layout_ref = C.byref(self._layout_args)
-        self._private = max(0, self.pages - self.first_page)
-        self._append_strides = [getattr(self._append_args, n) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
-        self._attention_strides = [getattr(self._attention_args, n) for n in ("q_stride", "out_stride")]
+        self._stream(stream)
 
     def close(self):
         if getattr(self, "_h", None):
-            B.load().ps_kv_destroy(self._h)
+            getattr(B.load(), self._destroy)(self._h)
             self._h = None
 
     def __del__(self):
@@ -125,7 +75,7 @@ class KVPool:
             self.status.zero_()
             if elsewhere:  # before the next call on another stream
                 torch.cuda.synchronize(self.device)
-            self._raise("a call on the pool", rc)
+            self._raise(self._what, rc)
 
     # -- argument checks ---------------------------------------------------
     def _stream(self, stream):
@@ -135,13 +85,88 @@ class KVPool:
         raw = _raw_stream(self._index) if stream is None else B._stream_ptr(stream)
         if raw not in self._used:
             self._used[raw] = B._stream_object(raw, self.device)
-            self._record(raw, self.k, self.v, self.workspace, self.status)
+            self._record(raw, *self._kept)
         return raw
 
     def _record(self, raw, *tensors):
         for t in tensors:
             if t is not None:
                 t.record_stream(self._used[raw])
+
+    def _array(self, t, dtype, name: str, n: Optional[int] = None):
+        sh = t.shape
+        if len(sh) != 1 or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous() or (
+                n is not None and sh[0] != n):
+            raise ValueError(f"{name} must be a contiguous {dtype} array" + ("" if n is None else f" of {n}"))
+        return t.data_ptr()
+
+
+class Layout(NamedTuple):
+    """A batch's arrays, as ``append`` and ``plan`` take them."""
+    q_offsets: torch.Tensor                # int32 [requests + 1]
+    kv_lens: torch.Tensor                  # int32 [requests]
+    tables: torch.Tensor                   # int32 [requests, pages]
+    positions: torch.Tensor                # int32 [tokens]
+    slots: torch.Tensor                    # int64 [tokens]
+    group_offsets: Optional[torch.Tensor]  # int32 [requests + 1]
+
+
+class KVPool(Handle):
+    """One paged pool of keys and values on the current CUDA device.
+
+    ``k`` and ``v`` are tensors [layers, pages, page_size, kv_heads, head_dim]
+    with the same strides, the innermost one 1 (a head-major pool is passed as
+    its transposed view).  Page ids below ``first_page`` are the prefix
+    cache's block ids, the others private pages of running requests.  The
+    references count private pages alone: a later step of the cache may evict a
+    block that a row still names, so no step runs while rows name cached pages,
+    or the pages that it evicts are copied to private ones before its appends."""
+
+    _destroy = "ps_kv_destroy"
+
+    def __init__(self, k, v, num_q_heads: int, first_page: int = 0, max_requests: int = 1, max_tokens: int = 1,
+                 max_row_pages: int = 1, stream=None):
+        L = B.load()
+        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype,
+              "k and v must be alike: [layers, pages, page_size, kv_heads, head_dim]")
+        _need(k.is_cuda and v.device == k.device and k.device.index == torch.cuda.current_device(),
+              "k and v must be on the current CUDA device")
+        _need(k.dtype in (torch.bfloat16, torch.float16), "a pool is bfloat16 or float16")
+        _need(k.stride(4) == 1, "the innermost stride must be 1")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim = (int(x) for x in k.shape)
+        self.q_heads, self.first_page = int(num_q_heads), int(first_page)
+        self.max_requests, self.max_tokens, self.max_row_pages = int(max_requests), int(max_tokens), int(max_row_pages)
+        c = B.PsKvConfig(k=k.data_ptr(), v=v.data_ptr(), num_pages=self.pages, first_page=self.first_page,
+                         layer_stride=k.stride(0), page_stride=k.stride(1), token_stride=k.stride(2),
+                         head_stride=k.stride(3), num_layers=self.layers, page_size=self.page_size,
+                         num_kv_heads=self.kv_heads, num_q_heads=self.q_heads, head_dim=self.head_dim,
+                         dtype=B.PS_KV_BF16 if k.dtype == torch.bfloat16 else B.PS_KV_F16,
+                         max_requests=self.max_requests, max_tokens=self.max_tokens, max_row_pages=self.max_row_pages)
+        nbytes = L.ps_kv_workspace_bytes(C.byref(c))
+        _need(nbytes > 0, "invalid pool configuration")
+        with B._on_stream(stream, self.device):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        h = C.c_void_p()
+        self._raise("ps_kv_create", L.ps_kv_create(C.byref(h), C.byref(c), self.workspace.data_ptr(), nbytes,
+                                                   B._stream_ptr(stream)))
+        self._h = h
+        self._batch = None
+        self._batch_used = set()  # streams that the plan's memory is recorded on
+        self._kept = (self.k, self.v, self.workspace, self.status)
+        self._begin(stream)
+        # argument structures and entry points of the calls that a decode step
+        # makes for every layer; their fields are filled in anew each time
+        self._append_args, self._attention_args = B.PsKvAppend(), B.PsKvAttention()
+        self._append_ref, self._attention_ref = C.byref(self._append_args), C.byref(self._attention_args)
+        self._rows_args = B.PsKvRows()
+        self._rows_ref = C.byref(self._rows_args)
+        self._layout_args = B.PsKvLayout()
+        self._layout_ref = C.byref(self._layout_args)
+        self._private = max(0, self.pages - self.first_page)
+        self._append_strides = [getattr(self._append_args, n) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+        self._attention_strides = [getattr(self._attention_args, n) for n in ("q_stride", "out_stride")]
 
     def _heads(self, t, tokens: int, heads: int, name: str, strides):
         """Checks [tokens, heads, head_dim]; its strides go to ``strides``."""
@@ -155,13 +180,6 @@ class KVPool:
         if s2 != 1 or (s0 | s1) & 7 or p & 15:
             raise ValueError(f"{name}: heads must be contiguous, on 16-byte boundaries")
         return p
-
-    def _array(self, t, dtype, name: str, n: Optional[int] = None):
-        sh = t.shape
-        if len(sh) != 1 or t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous() or (
-                n is not None and sh[0] != n):
-            raise ValueError(f"{name} must be a contiguous {dtype} array" + ("" if n is None else f" of {n}"))
-        return t.data_ptr()
 
     def _table(self, t, name: str):
         if len(t.shape) != 2 or t.dtype is not torch.int32 or t.device != self.device or not t.is_contiguous():
