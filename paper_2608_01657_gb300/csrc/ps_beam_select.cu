@@ -1,21 +1,22 @@
 // ps_beam_select: the best continuations of a request's beams.
 //
 // Of a beam with score c and logits x, token v continues it with the score c + x_v
-// - lse, lse = log sum_u exp x_u.  Within a beam the order is the logits', so one
-// pass over a row keeps two things: a sum of 2^((x - ref) log2 e), whose reference
-// rises with the greatest logit seen, and the 'beams' greatest logits whose tokens
-// end nothing (a request's best are among its beams' best).  Those are kept as whole
-// numbers, the logit's bits in order and then the token's complement, so that no two
-// are equal and equal logits go to the lowest token.
+// - lse, lse = log sum_u exp x_u.  Within a beam the order is the logits', and a
+// request's best are among its beams' best.  A row is read once, in words of 16
+// bytes, for two things: a sum of 2^((x - ref) log2 e), whose reference rises with the
+// greatest logit seen, and the 'beams' words of the greatest logits.  The row's best
+// tokens are in those words: every word that comes before one of theirs (by its
+// greatest logit, equal ones by place) holds a token that comes before it, too.  So
+// single elements are looked at in a few words only, at the end.  Words are kept as
+// whole numbers, the logit's bits in order and then the complement of the place, so
+// that no two are equal.
 //
-// Bound by HBM: a logit is read once.  A row is cut into parts, a CTA each, so that
-// a few rows fill the GPU, too; the last CTA of a request to finish puts the parts
-// together, in an order that does not depend on which one it is.
+// Bound by HBM.  A row is cut into parts, a CTA each, so that a few rows fill the GPU,
+// too; the last CTA of a request to finish puts the parts together, in an order that
+// does not depend on which one it is.
 //
-// A warp reads 4 KB at a time.  A list of 32 is sorted across its lanes; what is
-// greater than the list's beams-th enters a queue, 32 of which are sorted and merged
-// at a time.  The first threshold is the beams-th of the lanes' greatest, so that
-// about as many enter as are kept.
+// A warp keeps a list of 32 sorted across its lanes; what is greater than the list's
+// beams-th enters a queue, 32 of which are sorted and merged at a time.
 //
 // Neighbours in the order of scores may be nearer than 32 bits tell: differences
 // from the reference are exact or rounded once, log2 e has two parts, the lanes' sums
@@ -26,7 +27,7 @@ namespace psbeam {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kVecs = 8;           // 16-byte loads of a lane and chunk
+constexpr int kVecs = 4;           // words of a lane and chunk
 constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
 constexpr double kLn2 = 0.693147180559945309;
 constexpr unsigned kAll = 0xFFFFFFFFu;
@@ -39,6 +40,12 @@ struct Args {
 };
 
 // ---- elements ---------------------------------------------------------------------
+// The greater, NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 template <typename T>
 struct Elem;
 template <>
@@ -51,6 +58,9 @@ struct Elem<float> {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
   static __device__ __forceinline__ uint4 none() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
   static __device__ __forceinline__ float one(const void* p) { return *static_cast<const float*>(p); }
 };
 template <typename H>
@@ -69,6 +79,17 @@ struct Elem16 {
     return make_uint4(pskv::Num<H>::pack(x[0], x[1]), pskv::Num<H>::pack(x[2], x[3]), pskv::Num<H>::pack(x[4], x[5]),
                       pskv::Num<H>::pack(x[6], x[7]));
   }
+  // The greatest, NaN if one is.
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const float2 f = pskv::Num<H>::unpack(max2(max2(v.x, v.y), max2(v.z, v.w)));
+    return max_nan(f.x, f.y);
+  }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (pskv::Num<H>::kBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
   static __device__ __forceinline__ uint4 none() {  // -infinity
     constexpr uint32_t w = pskv::Num<H>::kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
     return make_uint4(w, w, w, w);
@@ -82,13 +103,6 @@ template <>
 struct Elem<__half> : Elem16<__half> {
   static __device__ __forceinline__ float one(const void* p) { return __half2float(*static_cast<const __half*>(p)); }
 };
-// The greater, NaN if one is.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 // ---- keys ---------------------------------------------------------------------------
 // The bits of x as a whole number in x's order; -0 is 0.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -96,10 +110,11 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return (int32_t)u < 0 ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((int32_t)o < 0 ? o & 0x7FFFFFFFu : ~o); }
-__device__ __forceinline__ uint64_t key_of(float x, int token) { return (uint64_t)ordered(x) << 32 | (uint32_t)~token; }
+// Of a logit and the place of its token (or of its word).
+__device__ __forceinline__ uint64_t key_of(float x, int place) { return (uint64_t)ordered(x) << 32 | (uint32_t)~place; }
 __device__ __forceinline__ float logit_of(uint64_t key) { return unordered((uint32_t)(key >> 32)); }
-__device__ __forceinline__ int token_of(uint64_t key) { return (int)~(uint32_t)key; }
-// No token of -infinity has a greater one.
+__device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
+// None of -infinity is greater.
 constexpr uint64_t kNoKey = 0x007FFFFFFFFFFFFFull;
 
 __device__ __forceinline__ void exchange(uint64_t& x, int other, bool greater) {
@@ -130,13 +145,12 @@ __device__ __forceinline__ bool ends(const Search& s, int token) {
 }
 
 // A warp's best so far.
-constexpr int kQueue = 31 + 32 * 8;  // what may wait, and a word of every lane
+constexpr int kQueue = 64;
 struct Best {
   uint64_t list;    // of the lane
   uint64_t floor;   // what enters is greater
   int queued;
   uint64_t* queue;  // [kQueue] of the warp
-  uint64_t* shared; // the greatest floor of the CTA's warps
   int keep, lane;
   __device__ __forceinline__ void raise(uint64_t to) { floor = floor > to ? floor : to; }
   __device__ __forceinline__ void flush() {  // the last 32 of the queue, or all of it
@@ -147,23 +161,15 @@ struct Best {
     queued = from;
     list = merge32(list, sort32(q, lane), lane);
     raise(__shfl_sync(kAll, list, keep - 1));
-    if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(shared), (unsigned long long)floor);
   }
-  // The lanes' words of neighbouring elements, from 'token' on.
-  template <int N>
-  __device__ __forceinline__ void add(const Search& s, const float (&x)[N], int token) {
-    const float least = logit_of(floor + 1);  // a smaller logit does not enter
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      if (!__any_sync(kAll, x[e] >= least)) continue;
-      const uint64_t key = key_of(x[e], token + e);
-      const bool on = x[e] >= least && key > floor && !ends(s, token + e);
-      const unsigned m = __ballot_sync(kAll, on);
-      if (on) queue[queued + __popc(m & ((1u << lane) - 1))] = key;
-      queued += __popc(m);
-    }
-    while (queued >= 32) flush();
+  __device__ __forceinline__ void add(uint64_t key, bool on) {
+    const unsigned m = __ballot_sync(kAll, on);
+    if (on) queue[queued + __popc(m & ((1u << lane) - 1))] = key;
+    queued += __popc(m);
+    if (queued >= 32) flush();
   }
+  // A smaller logit does not enter.
+  __device__ __forceinline__ float least() const { return logit_of(floor + 1); }
 };
 
 // A lane's sum of exp(x - ref).
@@ -247,20 +253,17 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
   const int words = (V + N - 1) / N;
   const int chunks = (words + kChunk - 1) / kChunk;
   const int c0 = (int)((int64_t)chunks * part / g.parts), c1 = (int)((int64_t)chunks * (part + 1) / g.parts);
-  bool seeded = false;
+  uint4 v[kVecs], next[kVecs];
+  if (c0 + warp < c1) read_chunk(row, shift, (c0 + warp) * kChunk + lane, words, V, next);
   for (int c = c0 + warp; c < c1; c += kWarps) {
-    uint4 v[kVecs];
-    read_chunk(row, shift, c * kChunk + lane, words, V, v);
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) v[j] = next[j];
+    if (c + kWarps < c1) read_chunk(row, shift, (c + kWarps) * kChunk + lane, words, V, next);
     float top[kVecs], all = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-      float x[N];
-      Elem<T>::wide(v[j], x);
-      float m = x[0];
-#pragma unroll
-      for (int e = 1; e < N; ++e) m = max_nan(m, x[e]);
-      top[j] = m;
-      all = max_nan(all, m);
+      top[j] = Elem<T>::top(v[j]);
+      all = max_nan(all, top[j]);
     }
     most = max_nan(most, all);
     sum.raise(all);
@@ -282,46 +285,23 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
     }
     const float2 f = pskv::unpack2(pskv::add2(s0, s1));
     sum.sum += f.x + f.y;
-    // candidates
-    const int t0 = (c * kChunk + lane) * N;  // token of the lane's first element
-    if (!seeded) {
-      seeded = true;
-      float m = all;
-      bool has = false;
-      for (int i = 0; i < g.s.num_end; ++i) {
-        const int at = g.s.end[i] - t0;
-        has = has || (at >= 0 && at < kVecs * 32 * N && at % (32 * N) < N);
+    if (!__any_sync(kAll, all >= best.least())) continue;
+    const int w0 = c * kChunk + lane;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      bool has = false;  // end tokens do not count
+      for (int i = 0; i < g.s.num_end; ++i) has = has || g.s.end[i] / N == w0 + 32 * j;
+      float t = top[j];
+      if (has) {
+        float x[N];
+        Elem<T>::wide(v[j], x);
+        t = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < N; ++e) t = ends(g.s, (w0 + 32 * j) * N + e) ? t : fmaxf(t, x[e]);
       }
-      if (__any_sync(kAll, has)) {  // end tokens do not count
-        m = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-          float x[N];
-          Elem<T>::wide(v[j], x);
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (!ends(g.s, t0 + j * 32 * N + e)) m = fmaxf(m, x[e]);
-        }
-      }
-      const uint64_t s = __shfl_sync(kAll, sort32((uint64_t)ordered(m) << 32, lane), best.keep - 1);
-      if (s > 0) best.raise(s - 1);
-    }
-    best.raise(*reinterpret_cast<volatile uint64_t*>(best.shared));
-    const float least = logit_of(best.floor + 1);  // a smaller logit does not enter
-    if (!__any_sync(kAll, all >= least)) continue;
-    unsigned hits = 0;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) hits |= (__any_sync(kAll, top[j] >= least) ? 1u : 0u) << j;
-    while (hits) {  // one of the lane's words at a time
-      const int j = __ffs(hits) - 1;
-      hits &= hits - 1;
-      uint4 w = v[0];
-#pragma unroll
-      for (int i = 1; i < kVecs; ++i)
-        if (i == j) w = v[i];
-      float x[N];
-      Elem<T>::wide(w, x);
-      best.add(g.s, x, t0 + j * 32 * N);
+      const uint64_t key = key_of(t, w0 + 32 * j);
+      const bool on = key > best.floor;
+      if (__any_sync(kAll, on)) best.add(key, on);
     }
   }
   while (best.queued > 0) best.flush();
@@ -357,8 +337,28 @@ __device__ __forceinline__ Cand merge32(Cand x, const Cand& y, int lane) {
   return x;
 }
 
+// The best tokens of a row, from the words that hold them.
 template <typename T>
-__device__ __forceinline__ void finish(const Args& g, int r) {
+__device__ __forceinline__ uint64_t best_tokens(const Args& g, const T* row, uint64_t words, uint64_t* queue, int lane) {
+  constexpr int N = Elem<T>::N, kEach = 32 / N;  // words that a warp looks at together
+  const int B = g.s.beams;
+  // each of the words has a token that is no smaller than the last one's
+  const uint64_t last = __shfl_sync(kAll, words, B - 1);
+  Best best{0, kNoKey, 0, queue, B, lane};
+  if (last > kNoKey) best.raise((last >> 32 << 32) - 1);
+  for (int i = 0; i < B; i += kEach) {
+    const uint64_t word = __shfl_sync(kAll, words, (i + lane / N) & 31);
+    const int token = place_of(word) * N + lane % N;
+    const bool on = i + lane / N < B && word > kNoKey && token < g.s.vocab;
+    const uint64_t key = key_of(on ? Elem<T>::one(row + token) : -INFINITY, token);
+    best.add(key, on && key > best.floor && !ends(g.s, token));
+  }
+  while (best.queued > 0) best.flush();
+  return best.list;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish(const Args& g, int r, uint64_t (*queue)[kQueue]) {
   __shared__ Cand cand[PS_BEAM_MAX_BEAMS][32];
   // of each beam: its score, the reference, the log of the sum over it (+infinity: no
   // candidates).  The reference, which may be far from 0, is subtracted first.
@@ -399,6 +399,7 @@ __device__ __forceinline__ void finish(const Args& g, int r) {
           const uint64_t k = lane < B ? __ldcg(g.s.keys + (row * S + i) * B + lane) : 0;
           list = i ? merge32(list, k, lane) : k;
         }
+        list = best_tokens(g, static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride, list, queue[warp], lane);
       }
     }
     const bool on = good && lane < B && list > kNoKey;
@@ -413,7 +414,7 @@ __device__ __forceinline__ void finish(const Args& g, int r) {
   const int64_t to = (int64_t)r * B + lane;
   if (lane < B) {
     const bool on = best.score > -INFINITY;
-    g.a.tokens[to] = on ? token_of(best.key) : -1;
+    g.a.tokens[to] = on ? place_of(best.key) : -1;
     g.a.parents[to] = on ? best.beam : -1;
     g.a.scores_out[to] = on ? (float)best.score : -INFINITY;
   }
@@ -438,15 +439,15 @@ __device__ __forceinline__ void finish(const Args& g, int r) {
   for (int i = 0; i < B; ++i) place += best.shfl(i).before(last);
   const bool on = last.score > -INFINITY && place < B;  // (places rise with the lanes)
   if (lane < B) {
-    g.a.ended_tokens[to] = on ? token_of(last.key) : -1;
+    g.a.ended_tokens[to] = on ? place_of(last.key) : -1;
     g.a.ended_parents[to] = on ? last.beam : -1;
     g.a.ended_scores[to] = on ? (float)last.score : -INFINITY;
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) k_select(Args g) {
-  __shared__ uint64_t queue[kWarps][kQueue], lists[kWarps][32], s_floor;
+__global__ void __launch_bounds__(kThreads, 3) k_select(Args g) {
+  __shared__ uint64_t queue[kWarps][kQueue], lists[kWarps][32];
   __shared__ double sums[kWarps];
   __shared__ float refs[kWarps];
   __shared__ int bads[kWarps];
@@ -457,9 +458,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_select(Args g) {
   const int part = (int)(blockIdx.x % g.parts), r = (int)(row / B), b = (int)(row % B);
   const float c = g.a.scores[row];
   if (c - c == 0) {  // (a score that is not finite: nothing is read of the row)
-    if (threadIdx.x == 0) s_floor = kNoKey;
-    __syncthreads();
-    Best best{0, kNoKey, 0, queue[warp], &s_floor, B, lane};
+    Best best{0, kNoKey, 0, queue[warp], B, lane};
     Sum sum{-INFINITY, 0.0f};
     float most = -INFINITY;
     scan_part(g, static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride, part, best, sum, most);
@@ -504,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_select(Args g) {
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  finish<T>(g, r);
+  finish<T>(g, r, queue);
 }
 
 }  // namespace
