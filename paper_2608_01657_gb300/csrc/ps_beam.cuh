@@ -24,7 +24,7 @@ struct __align__(16) Part {
 };
 
 struct Search {
-  int32_t beams, vocab, dtype, num_end, end[PS_BEAM_MAX_END];
+  int32_t beams, vocab, dtype, num_end, end[PS_BEAM_MAX_END];  // the end tokens rise
   Part* parts;      // [rows * parts of a row]
   uint64_t* keys;   // [rows * parts of a row][beams]
   int32_t* done;    // [max_requests] CTAs of a request that have finished (back to 0 after each call)

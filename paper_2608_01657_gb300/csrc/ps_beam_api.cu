@@ -1,6 +1,7 @@
 // C ABI of beam search (declared in include/prefixshield_beam.h).
 //
 // Host side only: argument checks, the workspace layout and the handle.
+#include <algorithm>
 #include <new>
 
 #include "ps_beam.cuh"
@@ -73,6 +74,7 @@ int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_wor
   b->s.dtype = cfg->dtype;
   b->s.num_end = cfg->num_end;
   for (int i = 0; i < cfg->num_end; ++i) b->s.end[i] = cfg->end_tokens[i];
+  std::sort(b->s.end, b->s.end + cfg->num_end);
   carve(*cfg, static_cast<char*>(d_workspace), &b->s);
   if (cudaMemsetAsync(b->s.done, 0, 4 * (size_t)cfg->max_requests, as_stream(stream)) != cudaSuccess) {
     delete b;

@@ -26,11 +26,14 @@
 namespace psbeam {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kCtasPerSm = 6;
 constexpr int kVecs = 4;           // words of a lane and chunk
 constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
-constexpr double kLn2 = 0.693147180559945309;
 constexpr unsigned kAll = 0xFFFFFFFFu;
+
+// A warp has so many chunks at least, where there are as many.
+constexpr int kLeastChunks = 2;
 
 struct Args {
   ps_beam_select_t a;
@@ -129,6 +132,16 @@ __device__ __forceinline__ uint64_t sort32(uint64_t x, int lane) {
     for (int j = k >> 1; j > 0; j >>= 1) exchange(x, j, ((lane & j) == 0) == ((lane & k) == 0));
   return x;
 }
+__device__ __forceinline__ uint32_t sort32(uint32_t x, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const uint32_t y = __shfl_xor_sync(kAll, x, j);
+      x = ((lane & j) == 0) == ((lane & k) == 0) ? max(x, y) : min(x, y);
+    }
+  return x;
+}
 // The 32 greatest of two such lists, as one.
 __device__ __forceinline__ uint64_t merge32(uint64_t x, uint64_t y, int lane) {
   const uint64_t z = __shfl_sync(kAll, y, 31 - lane);
@@ -171,6 +184,12 @@ struct Best {
   // A smaller logit does not enter.
   __device__ __forceinline__ float least() const { return logit_of(floor + 1); }
 };
+
+// exp(x) for x <= 0, the exponent in two parts; 0 below 2^-144 (where the parts are not finite at last).
+__device__ __forceinline__ float exp_of(float x) {
+  const float t = x * kLog2e;
+  return x < -100.0f ? 0.0f : pskv::ex2(t) * (1.0f + 0.693147181f * fmaf(x, kLog2eRest, fmaf(x, kLog2e, -t)));
+}
 
 // A lane's sum of exp(x - ref).
 struct Sum {
@@ -285,57 +304,64 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
     }
     const float2 f = pskv::unpack2(pskv::add2(s0, s1));
     sum.sum += f.x + f.y;
-    if (!__any_sync(kAll, all >= best.least())) continue;
     const int w0 = c * kChunk + lane;
+    bool ending = false;
+    for (int i = 0; i < g.s.num_end; ++i) ending = ending || g.s.end[i] / (kChunk * N) == c;
+    if (ending) {  // end tokens do not count
+      all = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      bool has = false;  // end tokens do not count
-      for (int i = 0; i < g.s.num_end; ++i) has = has || g.s.end[i] / N == w0 + 32 * j;
-      float t = top[j];
-      if (has) {
+      for (int j = 0; j < kVecs; ++j) {
         float x[N];
         Elem<T>::wide(v[j], x);
-        t = -INFINITY;
+        top[j] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) t = ends(g.s, (w0 + 32 * j) * N + e) ? t : fmaxf(t, x[e]);
+        for (int e = 0; e < N; ++e) top[j] = ends(g.s, (w0 + 32 * j) * N + e) ? top[j] : fmaxf(top[j], x[e]);
+        all = fmaxf(all, top[j]);
       }
-      const uint64_t key = key_of(t, w0 + 32 * j);
-      const bool on = key > best.floor;
-      if (__any_sync(kAll, on)) best.add(key, on);
+    }
+    if (c == c0 + warp) {  // the beams-th of the lanes' greatest: so many words are no smaller
+      const uint32_t s = __shfl_sync(kAll, sort32(ordered(all), lane), best.keep - 1);
+      best.raise(((uint64_t)s << 32) - 1);
+    }
+    const float least = best.least();
+    if (!__any_sync(kAll, all >= least)) continue;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      if (!__any_sync(kAll, top[j] >= least)) continue;
+      const uint64_t key = key_of(top[j], w0 + 32 * j);
+      best.add(key, key > best.floor);
     }
   }
   while (best.queued > 0) best.flush();
 }
 
 // ---- the parts of a request -------------------------------------------------------------
-// A candidate: the greater score, then the lower beam, then the greater key is first.
+// A candidate of a request: its score, and its beam and place in the beam's list.
 struct Cand {
   double score;
-  int beam;
-  uint64_t key;
-  __device__ __forceinline__ bool before(const Cand& y) const {
-    return score != y.score ? score > y.score : (beam != y.beam ? beam < y.beam : key > y.key);
-  }
-  __device__ __forceinline__ Cand shfl(int from) const {
-    return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, beam, from), __shfl_sync(kAll, key, from)};
-  }
+  int at;  // beam 32 + place
+  __device__ __forceinline__ bool before(const Cand& y) const { return score != y.score ? score > y.score : at < y.at; }
+  __device__ __forceinline__ Cand shfl(int from) const { return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, at, from)}; }
 };
-__device__ __forceinline__ Cand no_cand(int lane) { return {-INFINITY, PS_BEAM_MAX_BEAMS + lane, 0}; }
 __device__ __forceinline__ void exchange(Cand& x, int lane, int other, bool first) {
   const Cand y = x.shfl(lane ^ other);
   if (x.before(y) != first) x = y;
 }
 __device__ __forceinline__ Cand sort32(Cand x, int lane) {
+#pragma unroll
   for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
     for (int j = k >> 1; j > 0; j >>= 1) exchange(x, lane, j, ((lane & j) == 0) == ((lane & k) == 0));
   return x;
 }
 __device__ __forceinline__ Cand merge32(Cand x, const Cand& y, int lane) {
   const Cand z = y.shfl(31 - lane);
   if (z.before(x)) x = z;
+#pragma unroll
   for (int j = 16; j > 0; j >>= 1) exchange(x, lane, j, (lane & j) == 0);
   return x;
 }
+constexpr int kNobody = 1 << 20;  // a place after every candidate's
 
 // The best tokens of a row, from the words that hold them.
 template <typename T>
@@ -357,97 +383,124 @@ __device__ __forceinline__ uint64_t best_tokens(const Args& g, const T* row, uin
   return best.list;
 }
 
+// The request's own numbers, by the threads of its last CTA.
+struct Joined {
+  uint64_t keys[PS_BEAM_MAX_BEAMS][32];  // the beams' best tokens
+  double total[PS_BEAM_MAX_BEAMS];       // log of the sum over the reference, +infinity: no candidates
+  float score[PS_BEAM_MAX_BEAMS], ref[PS_BEAM_MAX_BEAMS];
+  Cand lists[kWarps][32];
+  Cand best[32];
+  // The reference, which may be far from 0, is subtracted first.
+  __device__ __forceinline__ double of(int b, float logit) const {
+    return (double)score[b] + (((double)logit - (double)ref[b]) - total[b]);
+  }
+};
+
 template <typename T>
-__device__ __forceinline__ void finish(const Args& g, int r, uint64_t (*queue)[kQueue]) {
-  __shared__ Cand cand[PS_BEAM_MAX_BEAMS][32];
-  // of each beam: its score, the reference, the log of the sum over it (+infinity: no
-  // candidates).  The reference, which may be far from 0, is subtracted first.
-  __shared__ double s_sum[PS_BEAM_MAX_BEAMS];
-  __shared__ float s_score[PS_BEAM_MAX_BEAMS], s_ref[PS_BEAM_MAX_BEAMS];
-  auto score = [&](int b, float logit) { return (double)s_score[b] + (((double)logit - (double)s_ref[b]) - s_sum[b]); };
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams, S = g.parts;
-  for (int b = warp; b < B; b += kWarps) {
+__device__ __forceinline__ void finish(const Args& g, int r, uint64_t (*queue)[kQueue], Joined& s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams, S = g.parts, E = g.s.num_end;
+  const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
+  if (threadIdx.x < B) {  // a beam a thread
+    const int b = threadIdx.x;
     const int64_t row = (int64_t)r * B + b;
     const float c = g.a.scores[row];
-    bool good = c - c == 0;  // finite
-    if (!good && c != -INFINITY && lane == 0) set_error(g.status, PS_ERR_INVALID_ARG);
-    double total = INFINITY;
     float ref = -INFINITY;
-    uint64_t list = 0;
-    if (good) {
-      Part p{0.0, -INFINITY, 0};
-      if (lane < S) {
-        const Part* q = g.s.parts + row * S + lane;
-        p.sum = __ldcg(&q->sum);
-        p.ref = __ldcg(&q->ref);
-        p.bad = __ldcg(&q->bad);
+    double sum = 0.0;
+    bool bad = c != -INFINITY && !(c - c == 0);
+    if (c - c == 0) {
+      for (int i = 0; i < S; ++i) {
+        const Part* p = g.s.parts + row * S + i;
+        bad = bad || __ldcg(&p->bad);
+        ref = fmaxf(ref, __ldcg(&p->ref));
       }
-      if (__any_sync(kAll, p.bad)) {
-        if (lane == 0) set_error(g.status, PS_ERR_INVALID_ARG);
-        good = false;
-      }
-      ref = p.ref;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(kAll, ref, o));
-      if (ref == -INFINITY) good = false;  // no token may follow
-      double sum = p.ref == -INFINITY ? 0.0 : p.sum * exp2(((double)p.ref - (double)ref) / kLn2);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
-      if (good) {
-        total = log(sum);
-        for (int i = 0; i < S; ++i) {
-          const uint64_t k = lane < B ? __ldcg(g.s.keys + (row * S + i) * B + lane) : 0;
-          list = i ? merge32(list, k, lane) : k;
-        }
-        list = best_tokens(g, static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride, list, queue[warp], lane);
+      for (int i = 0; i < S; ++i) {
+        const Part* p = g.s.parts + row * S + i;
+        const float x = __ldcg(&p->ref);
+        if (x > -INFINITY) sum += __ldcg(&p->sum) * (double)exp_of(x - ref);
       }
     }
-    const bool on = good && lane < B && list > kNoKey;
-    if (lane == 0) s_score[b] = c, s_ref[b] = ref, s_sum[b] = total;
-    __syncwarp();
-    cand[b][lane] = on ? Cand{score(b, logit_of(list)), b, list} : no_cand(lane);
+    if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
+    s.score[b] = c;
+    s.ref[b] = ref;
+    s.total[b] = bad || ref == -INFINITY ? (double)INFINITY : log(sum);  // (no token may follow)
   }
   __syncthreads();
-  if (warp != 0) return;
-  Cand best = cand[0][lane];
-  for (int b = 1; b < B; ++b) best = merge32(best, cand[b][lane], lane);
+  Cand mine{-INFINITY, kNobody + lane};
+  for (int b = warp; b < B; b += kWarps) {
+    if (!(s.total[b] < INFINITY)) continue;
+    const int64_t row = (int64_t)r * B + b;
+    uint64_t list = 0;
+    for (int i = 0; i < S; ++i) {
+      const uint64_t k = lane < B ? __ldcg(g.s.keys + (row * S + i) * B + lane) : 0;
+      list = i ? merge32(list, k, lane) : k;
+    }
+    list = best_tokens(g, logits + b * g.a.beam_stride, list, queue[warp], lane);
+    s.keys[b][lane] = list;
+    const bool on = lane < B && list > kNoKey;
+    mine = merge32(mine, on ? Cand{s.of(b, logit_of(list)), b * 32 + lane} : Cand{-INFINITY, kNobody + lane}, lane);
+  }
+  s.lists[warp][lane] = mine;
+  __syncthreads();
   const int64_t to = (int64_t)r * B + lane;
-  if (lane < B) {
-    const bool on = best.score > -INFINITY;
-    g.a.tokens[to] = on ? place_of(best.key) : -1;
-    g.a.parents[to] = on ? best.beam : -1;
-    g.a.scores_out[to] = on ? (float)best.score : -INFINITY;
+  if (warp == 0) {
+    for (int w = 1; w < kWarps && w < B; ++w) mine = merge32(mine, s.lists[w][lane], lane);
+    s.best[lane] = mine;
+    if (lane < B) {
+      const bool on = mine.score > -INFINITY;
+      g.a.tokens[to] = on ? place_of(s.keys[mine.at >> 5][mine.at & 31]) : -1;
+      g.a.parents[to] = on ? mine.at >> 5 : -1;
+      g.a.scores_out[to] = on ? (float)mine.score : -INFINITY;
+    }
   }
   if (!g.a.ended_tokens) return;
-  // the end tokens' candidates, the 32 first
-  Cand last = no_cand(lane);
-  for (int i0 = 0; i0 < B * g.s.num_end; i0 += 32) {
-    const int i = i0 + lane;
-    Cand x = no_cand(lane);
-    if (i < B * g.s.num_end) {
-      const int b = i / g.s.num_end, token = g.s.end[i % g.s.num_end];
-      if (s_sum[b] < INFINITY) {
-        const T* row = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride;
-        const float l = Elem<T>::one(row + token);
-        if (l > -INFINITY) x = Cand{score(b, l), b, key_of(l, token)};
-      }
+  if (E == 0) {
+    if (warp == 1 && lane < B) {
+      g.a.ended_tokens[to] = g.a.ended_parents[to] = -1;
+      g.a.ended_scores[to] = -INFINITY;
     }
-    last = merge32(last, sort32(x, lane), lane);
+    return;
   }
+  // the end tokens' candidates, the 32 first: 'at' is beam 32 + the end token's number,
+  // the numbers rising with the tokens
+  Cand last{-INFINITY, kNobody + lane};
+  if (warp == 1) {
+    for (int i0 = 0; i0 < B * E; i0 += 32) {
+      const int i = i0 + lane;
+      Cand x{-INFINITY, kNobody + lane};
+      if (i < B * E && s.total[i / E] < INFINITY) {
+        const int b = i / E;
+        const float l = Elem<T>::one(logits + b * g.a.beam_stride + g.s.end[i % E]);
+        if (l > -INFINITY) x = Cand{s.of(b, l), b * 32 + i % E};
+      }
+      x = sort32(x, lane);
+      last = i0 ? merge32(last, x, lane) : x;
+    }
+  }
+  __syncthreads();
+  if (warp != 1) return;
   // its place among all candidates: those of its kind before it are the lanes below
   int place = lane;
-  for (int i = 0; i < B; ++i) place += best.shfl(i).before(last);
-  const bool on = last.score > -INFINITY && place < B;  // (places rise with the lanes)
+  bool on = last.score > -INFINITY;
+  uint64_t key = 0;
+  if (on) key = key_of(Elem<T>::one(logits + (last.at >> 5) * g.a.beam_stride + g.s.end[last.at & 31]), g.s.end[last.at & 31]);
+  for (int i = 0; i < B; ++i) {
+    const Cand x = s.best[i];
+    const bool first = x.score != last.score ? x.score > last.score
+                                             : x.at >> 5 != last.at >> 5 ? x.at < last.at : x.at < kNobody && s.keys[x.at >> 5][x.at & 31] > key;
+    place += first;
+  }
+  on = on && place < B;  // (places rise with the lanes)
   if (lane < B) {
-    g.a.ended_tokens[to] = on ? place_of(last.key) : -1;
-    g.a.ended_parents[to] = on ? last.beam : -1;
+    g.a.ended_tokens[to] = on ? g.s.end[last.at & 31] : -1;
+    g.a.ended_parents[to] = on ? last.at >> 5 : -1;
     g.a.ended_scores[to] = on ? (float)last.score : -INFINITY;
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) k_select(Args g) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(Args g) {
   __shared__ uint64_t queue[kWarps][kQueue], lists[kWarps][32];
+  __shared__ Joined joined;
   __shared__ double sums[kWarps];
   __shared__ float refs[kWarps];
   __shared__ int bads[kWarps];
@@ -467,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_select(Args g) {
     const bool bad = __any_sync(kAll, !(most < INFINITY));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(kAll, ref, o));
-    double s = sum.ref == -INFINITY ? 0.0 : (double)sum.sum * (double)pskv::ex2((sum.ref - ref) * kLog2e);
+    double s = sum.ref == -INFINITY ? 0.0 : (double)(sum.sum * exp_of(sum.ref - ref));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
     lists[warp][lane] = best.list;
@@ -486,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_select(Args g) {
       const bool any = __any_sync(kAll, lane < kWarps && bads[lane < kWarps ? lane : 0]);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
-      double t = mine == -INFINITY ? 0.0 : sums[lane] * exp2(((double)mine - (double)top) / kLn2);
+      double t = mine == -INFINITY ? 0.0 : sums[lane] * (double)exp_of(mine - top);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(kAll, t, o);
       if (lane == 0) g.s.parts[at] = Part{t, top, any};
@@ -503,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_select(Args g) {
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  finish<T>(g, r, queue);
+  finish<T>(g, r, queue, joined);
 }
 
 }  // namespace
@@ -513,7 +566,7 @@ int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* statu
   const int64_t rows = (int64_t)a.num_requests * s.beams;
   const int64_t chunk = 32 * kVecs * (s.dtype == PS_BEAM_F32 ? 4 : 8), chunks = (s.vocab + chunk - 1) / chunk;
   int64_t parts = kSpreadCtas / rows;
-  const int64_t most = (chunks + kWarps - 1) / kWarps;
+  const int64_t most = (chunks + kWarps * kLeastChunks - 1) / (kWarps * kLeastChunks);
   parts = parts < most ? parts : most;
   g.parts = (int32_t)(parts < 1 ? 1 : (parts > kMaxParts ? kMaxParts : parts));
   const dim3 grid((unsigned)(rows * g.parts));
