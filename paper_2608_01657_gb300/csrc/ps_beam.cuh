@@ -15,10 +15,10 @@ using pskv::status_of;
 constexpr int kSpreadCtas = 152 * 16;
 constexpr int kMaxParts = 32;
 
-// What one CTA found of a row: the logits' greatest, the sum of exp(x - ref), and
-// whether a logit is NaN or +infinity.
+// What one CTA found of a row: the logits' greatest, the sum of exp(x - ref) in whole
+// numbers of 2^-32, and whether a logit is NaN or +infinity.
 struct __align__(16) Part {
-  double sum;
+  uint64_t sum;
   float ref;
   int32_t bad;
 };

@@ -15,25 +15,28 @@
 // too; the last CTA of a request to finish puts the parts together, in an order that
 // does not depend on which one it is.
 //
-// A warp keeps a list of 32 sorted across its lanes; what is greater than the list's
+// A warp reads 2 KB at a time through a ring in shared memory, three of them under way
+// while it works on one.  It keeps a list of 32 sorted across its lanes; what is greater than the list's
 // beams-th enters a queue, 32 of which are sorted and merged at a time.
 //
 // Neighbours in the order of scores may be nearer than 32 bits tell: differences
 // from the reference are exact or rounded once, log2 e has two parts, the lanes' sums
-// are added in 64 bits, and so are the scores.
+// are added as whole numbers of 2^-32, and scores in 64 bits.
 #include "ps_beam.cuh"
 
 namespace psbeam {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 6;
-constexpr int kVecs = 4;           // words of a lane and chunk
-constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
-constexpr unsigned kAll = 0xFFFFFFFFu;
-
+constexpr int kCtasPerSm = 5;
+constexpr int kVecs = 4;                 // words of a lane and chunk
+constexpr int kChunk = 32 * kVecs;       // words of a chunk
+constexpr int kStages = 4;               // chunks of a warp's ring
 // A warp has so many chunks at least, where there are as many.
 constexpr int kLeastChunks = 2;
+constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
+constexpr double kLn2 = 0.693147180559945309;
+constexpr unsigned kAll = 0xFFFFFFFFu;
 
 struct Args {
   ps_beam_select_t a;
@@ -153,7 +156,8 @@ __device__ __forceinline__ uint64_t merge32(uint64_t x, uint64_t y, int lane) {
 
 __device__ __forceinline__ bool ends(const Search& s, int token) {
   bool e = false;
-  for (int i = 0; i < s.num_end; ++i) e = e || s.end[i] == token;
+#pragma unroll
+  for (int i = 0; i < PS_BEAM_MAX_END; ++i) e = e || (i < s.num_end && s.end[i] == token);
   return e;
 }
 
@@ -185,10 +189,29 @@ struct Best {
   __device__ __forceinline__ float least() const { return logit_of(floor + 1); }
 };
 
+// ---- sums -----------------------------------------------------------------------------
 // exp(x) for x <= 0, the exponent in two parts; 0 below 2^-144 (where the parts are not finite at last).
 __device__ __forceinline__ float exp_of(float x) {
   const float t = x * kLog2e;
   return x < -100.0f ? 0.0f : pskv::ex2(t) * (1.0f + 0.693147181f * fmaf(x, kLog2eRest, fmaf(x, kLog2e, -t)));
+}
+// log(u 2^-32) for u > 0, to 4e-9.  With u = 2^e m, 0.7 < m < 1.42, and f = (m - 1) /
+// (m + 1): log m = 2 (f + f^3 / 3 + f^5 / 5 + ...), the first term in two parts.
+__device__ __forceinline__ double log_of(uint64_t u) {
+  const int lz = __clzll((long long)u);
+  const uint64_t n = u << lz;
+  float hi = (float)(uint32_t)(n >> 40) * 0x1p-23f, lo = (float)((uint32_t)(n >> 16) & 0xFFFFFFu) * 0x1p-47f;
+  int e = 31 - lz;
+  if (hi > 1.41421354f) hi *= 0.5f, lo *= 0.5f, ++e;
+  const float num = hi - 1.0f, den = hi + 1.0f, den_lo = hi - (den - 1.0f) + lo;
+  const float f = num / den, z = f * f;
+  const float f_lo = (fmaf(-f, den, num) + lo - f * den_lo) / den;
+  float p = fmaf(z, 1.0f / 13, 1.0f / 11);
+  p = fmaf(p, z, 1.0f / 9);
+  p = fmaf(p, z, 1.0f / 7);
+  p = fmaf(p, z, 1.0f / 5);
+  p = fmaf(p, z, 1.0f / 3) * z;
+  return (double)e * kLn2 + ((double)(2.0f * f) + (double)(2.0f * fmaf(f, p, f_lo)));
 }
 
 // A lane's sum of exp(x - ref).
@@ -203,53 +226,69 @@ struct Sum {
   // What is subtracted: nothing while all are -infinity.
   __device__ __forceinline__ float base() const { return ref == -INFINITY ? 0.0f : ref; }
 };
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kAll, x, o));
+  return x;
+}
+__device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kAll, x, o);
+  return x;
+}
 
 // ---- a part of a row ------------------------------------------------------------------
-// Words of 16 bytes are counted from the row's first element on, wherever that lies in
-// memory, so that a row's sum does not depend on its address: equal beams are equal to
-// the last bit.  Where the row does not start on a 16-byte boundary a word is put
-// together from two aligned ones ('shift' elements of the first are not its own); what
-// would reach past the row is read by elements.
+// Words are counted from the row's first element on, wherever that lies in memory, so
+// that a row's sum does not depend on its address: equal beams are equal to the last
+// bit.  A ring slot holds aligned words.  Where the row starts 'shift' elements into
+// one, a word is put together from two; elements of aligned words that are not the
+// row's are not read.
+constexpr int kSlot = kChunk + 1;  // with the word after the chunk's
+
 template <typename T>
-__device__ __noinline__ uint4 edge_word(const T* row, int first, int V) {
-  constexpr int N = Elem<T>::N;
-  float x[N];
+struct Row {
+  static constexpr int N = Elem<T>::N;
+  const T* row;
+  int V, shift;
+  uint4* ring;  // [kStages][kSlot] of the warp
+  int lane;
+  __device__ __forceinline__ void fetch_word(uint4* to, int w) const {
+    const int first = w * N - shift;
+    if (first >= 0 && first + N <= V) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(row + first) : "memory");
+    } else {
+      float x[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) x[e] = first + e < V ? Elem<T>::one(row + first + e) : -INFINITY;
-  return Elem<T>::narrow(x);
-}
-template <typename T>
-__device__ __forceinline__ void read_chunk(const T* row, int shift, int w0, int words, int V, uint4 (&v)[kVecs]) {
-  constexpr int N = Elem<T>::N;
-  const int full = V / N;
-  if (shift == 0) {
-    const uint4* at = reinterpret_cast<const uint4*>(row);
+      for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+      if (first < V) {
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const int w = w0 + 32 * j;
-      if (w < full) v[j] = __ldcs(at + w);
-    }
-  } else {
-    const uint4* at = reinterpret_cast<const uint4*>(row - shift);
-    const int last = (V + shift) / N - 1;  // the last aligned word that is wholly the row's
-    uint4 next[kVecs];
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const int w = w0 + 32 * j;
-      if (w > 0 && w < last) {
-        v[j] = __ldg(at + w);
-        next[j] = __ldg(at + w + 1);
+        for (int e = 0; e < N; ++e)
+          if (first + e >= 0 && first + e < V) x[e] = Elem<T>::one(row + first + e);
       }
+      *to = Elem<T>::narrow(x);
     }
-    const int words4 = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
+  }
+  __device__ __forceinline__ void fetch(int c, int stage) const {
+    uint4* slot = ring + stage * kSlot;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) fetch_word(slot + 32 * j + lane, c * kChunk + 32 * j + lane);
+    if (shift != 0 && lane == 0) fetch_word(slot + kChunk, c * kChunk + kChunk);
+  }
+  __device__ __forceinline__ void take(int stage, uint4 (&v)[kVecs]) const {
+    const uint4* slot = ring + stage * kSlot + lane;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) v[j] = slot[32 * j];
+    if (shift == 0) return;
+    const int words = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-      uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, next[j].x, next[j].y, next[j].z, next[j].w};
-      if (words4 & 2) {
+      const uint4 n = slot[32 * j + 1];
+      uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, n.x, n.y, n.z, n.w};
+      if (words & 2) {
 #pragma unroll
         for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
       }
-      if (words4 & 1) {
+      if (words & 1) {
 #pragma unroll
         for (int i = 0; i < 5; ++i) x[i] = x[i + 1];
       }
@@ -257,27 +296,29 @@ __device__ __forceinline__ void read_chunk(const T* row, int shift, int w0, int 
                         __funnelshift_r(x[3], x[4], bits));
     }
   }
-#pragma unroll
-  for (int j = 0; j < kVecs; ++j) {
-    const int w = w0 + 32 * j;
-    if (shift == 0 ? w >= full : (w == 0 || w >= (V + shift) / N - 1)) v[j] = w < words ? edge_word(row, w * N, V) : Elem<T>::none();
-  }
-}
+};
 
 template <typename T>
-__device__ __forceinline__ void scan_part(const Args& g, const T* row, int part, Best& best, Sum& sum, float& most) {
-  constexpr int N = Elem<T>::N, kChunk = 32 * kVecs;
-  const int lane = best.lane, warp = threadIdx.x >> 5, V = g.s.vocab;
-  const int shift = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(T);
-  const int words = (V + N - 1) / N;
+__device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int part, Best& best, Sum& sum, float& most) {
+  constexpr int N = Elem<T>::N;
+  const int lane = row.lane, warp = threadIdx.x >> 5;
+  const int words = (row.V - 1) / N + 1;
   const int chunks = (words + kChunk - 1) / kChunk;
-  const int c0 = (int)((int64_t)chunks * part / g.parts), c1 = (int)((int64_t)chunks * (part + 1) / g.parts);
-  uint4 v[kVecs], next[kVecs];
-  if (c0 + warp < c1) read_chunk(row, shift, (c0 + warp) * kChunk + lane, words, V, next);
-  for (int c = c0 + warp; c < c1; c += kWarps) {
+  const int c0 = (int)((int64_t)chunks * part / g.parts) + warp, c1 = (int)((int64_t)chunks * (part + 1) / g.parts);
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) v[j] = next[j];
-    if (c + kWarps < c1) read_chunk(row, shift, (c + kWarps) * kChunk + lane, words, V, next);
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (c0 + i * kWarps < c1) row.fetch(c0 + i * kWarps, i);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  int stage = 0;
+  for (int c = c0; c < c1; c += kWarps) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();  // the lanes' copies are there, and all have read the slot that is filled next
+    uint4 v[kVecs];
+    row.take(stage, v);
+    if (c + (kStages - 1) * kWarps < c1) row.fetch(c + (kStages - 1) * kWarps, stage == 0 ? kStages - 1 : stage - 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    stage = stage == kStages - 1 ? 0 : stage + 1;
     float top[kVecs], all = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
@@ -305,9 +346,13 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
     const float2 f = pskv::unpack2(pskv::add2(s0, s1));
     sum.sum += f.x + f.y;
     const int w0 = c * kChunk + lane;
-    bool ending = false;
-    for (int i = 0; i < g.s.num_end; ++i) ending = ending || g.s.end[i] / (kChunk * N) == c;
-    if (ending) {  // end tokens do not count
+    unsigned out = 0;  // the lane's end tokens: they do not count
+#pragma unroll
+    for (int i = 0; i < PS_BEAM_MAX_END; ++i) {
+      const int w = g.s.end[i] / N - w0;
+      if (i < g.s.num_end && w >= 0 && w < kChunk && (w & 31) == 0) out |= 1u << (w / 32 * N + g.s.end[i] % N);
+    }
+    if (out) {
       all = -INFINITY;
 #pragma unroll
       for (int j = 0; j < kVecs; ++j) {
@@ -315,11 +360,11 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
         Elem<T>::wide(v[j], x);
         top[j] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) top[j] = ends(g.s, (w0 + 32 * j) * N + e) ? top[j] : fmaxf(top[j], x[e]);
+        for (int e = 0; e < N; ++e) top[j] = out >> (j * N + e) & 1 ? top[j] : fmaxf(top[j], x[e]);
         all = fmaxf(all, top[j]);
       }
     }
-    if (c == c0 + warp) {  // the beams-th of the lanes' greatest: so many words are no smaller
+    if (c == c0) {  // the beams-th of the lanes' greatest: so many words are no smaller
       const uint32_t s = __shfl_sync(kAll, sort32(ordered(all), lane), best.keep - 1);
       best.raise(((uint64_t)s << 32) - 1);
     }
@@ -336,13 +381,21 @@ __device__ __forceinline__ void scan_part(const Args& g, const T* row, int part,
 }
 
 // ---- the parts of a request -------------------------------------------------------------
-// A candidate of a request: its score, and its beam and place in the beam's list.
+// A candidate of a request: its score as a whole number in the scores' order, and its
+// beam and place in the beam's list.
 struct Cand {
-  double score;
+  long long score;
   int at;  // beam 32 + place
   __device__ __forceinline__ bool before(const Cand& y) const { return score != y.score ? score > y.score : at < y.at; }
   __device__ __forceinline__ Cand shfl(int from) const { return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, at, from)}; }
+  __device__ __forceinline__ float value() const { return (float)__longlong_as_double(score < 0 ? score ^ 0x7FFFFFFFFFFFFFFFll : score); }
 };
+constexpr int kNobody = 1 << 20;  // a place after every candidate's
+__device__ __forceinline__ Cand cand(double score, int at) {
+  const long long b = __double_as_longlong(score + 0.0);
+  return {b < 0 ? b ^ 0x7FFFFFFFFFFFFFFFll : b, at};
+}
+__device__ __forceinline__ Cand nobody(int lane) { return {(long long)0x8000000000000000ull, kNobody + lane}; }
 __device__ __forceinline__ void exchange(Cand& x, int lane, int other, bool first) {
   const Cand y = x.shfl(lane ^ other);
   if (x.before(y) != first) x = y;
@@ -361,7 +414,6 @@ __device__ __forceinline__ Cand merge32(Cand x, const Cand& y, int lane) {
   for (int j = 16; j > 0; j >>= 1) exchange(x, lane, j, (lane & j) == 0);
   return x;
 }
-constexpr int kNobody = 1 << 20;  // a place after every candidate's
 
 // The best tokens of a row, from the words that hold them.
 template <typename T>
@@ -372,21 +424,29 @@ __device__ __forceinline__ uint64_t best_tokens(const Args& g, const T* row, uin
   const uint64_t last = __shfl_sync(kAll, words, B - 1);
   Best best{0, kNoKey, 0, queue, B, lane};
   if (last > kNoKey) best.raise((last >> 32 << 32) - 1);
-  for (int i = 0; i < B; i += kEach) {
-    const uint64_t word = __shfl_sync(kAll, words, (i + lane / N) & 31);
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t word = __shfl_sync(kAll, words, i * kEach + lane / N);
     const int token = place_of(word) * N + lane % N;
-    const bool on = i + lane / N < B && word > kNoKey && token < g.s.vocab;
-    const uint64_t key = key_of(on ? Elem<T>::one(row + token) : -INFINITY, token);
-    best.add(key, on && key > best.floor && !ends(g.s, token));
+    x[i] = -INFINITY;
+    if (i * kEach + lane / N < B && word > kNoKey && token < g.s.vocab) x[i] = Elem<T>::one(row + token);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i * kEach >= B) break;
+    const int token = place_of(__shfl_sync(kAll, words, i * kEach + lane / N)) * N + lane % N;
+    const uint64_t key = key_of(x[i], token);
+    best.add(key, key > best.floor && !ends(g.s, token));
   }
   while (best.queued > 0) best.flush();
   return best.list;
 }
 
-// The request's own numbers, by the threads of its last CTA.
 struct Joined {
   uint64_t keys[PS_BEAM_MAX_BEAMS][32];  // the beams' best tokens
-  double total[PS_BEAM_MAX_BEAMS];       // log of the sum over the reference, +infinity: no candidates
+  uint64_t sum[PS_BEAM_MAX_BEAMS];       // of 2^-32 exp(x - ref), 0: no candidates
+  double total[PS_BEAM_MAX_BEAMS];       // its logarithm
   float score[PS_BEAM_MAX_BEAMS], ref[PS_BEAM_MAX_BEAMS];
   Cand lists[kWarps][32];
   Cand best[32];
@@ -395,154 +455,152 @@ struct Joined {
     return (double)score[b] + (((double)logit - (double)ref[b]) - total[b]);
   }
 };
+struct Shared {
+  uint64_t queue[kWarps][kQueue];
+  union {
+    struct {
+      uint4 ring[kWarps][kStages * kSlot];
+      uint64_t lists[kWarps][32];
+    } scan;
+    Joined joined;
+  };
+  uint64_t sums[kWarps];
+  float refs[kWarps];
+  int bad[kWarps];
+  bool last;
+};
 
+// The request's outputs, by the threads of its last CTA.
 template <typename T>
 __device__ __forceinline__ void finish(const Args& g, int r, uint64_t (*queue)[kQueue], Joined& s) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams, S = g.parts, E = g.s.num_end;
   const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
-  if (threadIdx.x < B) {  // a beam a thread
-    const int b = threadIdx.x;
+  for (int b = warp; b < B; b += kWarps) {  // the beams' sums, a part a lane
     const int64_t row = (int64_t)r * B + b;
     const float c = g.a.scores[row];
-    float ref = -INFINITY;
-    double sum = 0.0;
-    bool bad = c != -INFINITY && !(c - c == 0);
-    if (c - c == 0) {
-      for (int i = 0; i < S; ++i) {
-        const Part* p = g.s.parts + row * S + i;
-        bad = bad || __ldcg(&p->bad);
-        ref = fmaxf(ref, __ldcg(&p->ref));
-      }
-      for (int i = 0; i < S; ++i) {
-        const Part* p = g.s.parts + row * S + i;
-        const float x = __ldcg(&p->ref);
-        if (x > -INFINITY) sum += __ldcg(&p->sum) * (double)exp_of(x - ref);
-      }
+    Part p{0, -INFINITY, 0};
+    if (lane < S && c - c == 0) {
+      const uint4 q = __ldcg(reinterpret_cast<const uint4*>(g.s.parts + row * S + lane));
+      p = Part{(uint64_t)q.y << 32 | q.x, __uint_as_float(q.z), (int32_t)q.w};
     }
-    if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
-    s.score[b] = c;
-    s.ref[b] = ref;
-    s.total[b] = bad || ref == -INFINITY ? (double)INFINITY : log(sum);  // (no token may follow)
+    const float ref = warp_max(p.ref);
+    const bool bad = __any_sync(kAll, p.bad) || (c != -INFINITY && !(c - c == 0));
+    if (p.ref < ref) p.sum = p.ref == -INFINITY ? 0 : __double2ull_rn((double)p.sum * (double)exp_of(p.ref - ref));
+    const uint64_t sum = warp_sum(p.sum);
+    if (lane == 0) {
+      if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
+      s.score[b] = c;
+      s.ref[b] = ref;
+      s.sum[b] = bad ? 0 : sum;  // 0: no token may follow
+    }
   }
   __syncthreads();
-  Cand mine{-INFINITY, kNobody + lane};
+  if (threadIdx.x < B && s.sum[threadIdx.x] != 0) s.total[threadIdx.x] = log_of(s.sum[threadIdx.x]);
+  __syncthreads();
+  Cand mine = nobody(lane);
   for (int b = warp; b < B; b += kWarps) {
-    if (!(s.total[b] < INFINITY)) continue;
-    const int64_t row = (int64_t)r * B + b;
-    uint64_t list = 0;
-    for (int i = 0; i < S; ++i) {
-      const uint64_t k = lane < B ? __ldcg(g.s.keys + (row * S + i) * B + lane) : 0;
-      list = i ? merge32(list, k, lane) : k;
+    if (s.sum[b] == 0) continue;
+    const uint64_t* keys = g.s.keys + ((int64_t)r * B + b) * S * B + lane;
+    uint64_t list = lane < B ? __ldcg(keys) : 0;
+    for (int i = 1; i < S; i += 4) {
+      uint64_t k[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) k[u] = lane < B && i + u < S ? __ldcg(keys + (i + u) * B) : 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i + u < S) list = merge32(list, k[u], lane);
     }
     list = best_tokens(g, logits + b * g.a.beam_stride, list, queue[warp], lane);
     s.keys[b][lane] = list;
-    const bool on = lane < B && list > kNoKey;
-    mine = merge32(mine, on ? Cand{s.of(b, logit_of(list)), b * 32 + lane} : Cand{-INFINITY, kNobody + lane}, lane);
+    const Cand x = lane < B && list > kNoKey ? cand(s.of(b, logit_of(list)), b * 32 + lane) : nobody(lane);
+    mine = b < kWarps ? x : merge32(mine, x, lane);
   }
   s.lists[warp][lane] = mine;
   __syncthreads();
   const int64_t to = (int64_t)r * B + lane;
+  Cand last = nobody(lane);
   if (warp == 0) {
     for (int w = 1; w < kWarps && w < B; ++w) mine = merge32(mine, s.lists[w][lane], lane);
     s.best[lane] = mine;
     if (lane < B) {
-      const bool on = mine.score > -INFINITY;
+      const bool on = mine.at < kNobody;
       g.a.tokens[to] = on ? place_of(s.keys[mine.at >> 5][mine.at & 31]) : -1;
       g.a.parents[to] = on ? mine.at >> 5 : -1;
-      g.a.scores_out[to] = on ? (float)mine.score : -INFINITY;
+      g.a.scores_out[to] = on ? mine.value() : -INFINITY;
     }
-  }
-  if (!g.a.ended_tokens) return;
-  if (E == 0) {
-    if (warp == 1 && lane < B) {
-      g.a.ended_tokens[to] = g.a.ended_parents[to] = -1;
-      g.a.ended_scores[to] = -INFINITY;
-    }
-    return;
-  }
-  // the end tokens' candidates, the 32 first: 'at' is beam 32 + the end token's number,
-  // the numbers rising with the tokens
-  Cand last{-INFINITY, kNobody + lane};
-  if (warp == 1) {
+  } else if (warp == 1 && g.a.ended_tokens) {
+    // the end tokens' candidates, the 32 first: 'at' is beam 32 + the end token's
+    // number, and the numbers rise with the tokens
     for (int i0 = 0; i0 < B * E; i0 += 32) {
-      const int i = i0 + lane;
-      Cand x{-INFINITY, kNobody + lane};
-      if (i < B * E && s.total[i / E] < INFINITY) {
-        const int b = i / E;
+      const int i = i0 + lane, b = i / E;
+      Cand x = nobody(lane);
+      if (i < B * E && s.sum[b] != 0) {
         const float l = Elem<T>::one(logits + b * g.a.beam_stride + g.s.end[i % E]);
-        if (l > -INFINITY) x = Cand{s.of(b, l), b * 32 + i % E};
+        if (l > -INFINITY) x = cand(s.of(b, l), b * 32 + i % E);
       }
       x = sort32(x, lane);
       last = i0 ? merge32(last, x, lane) : x;
     }
   }
+  if (!g.a.ended_tokens) return;
   __syncthreads();
   if (warp != 1) return;
   // its place among all candidates: those of its kind before it are the lanes below
   int place = lane;
-  bool on = last.score > -INFINITY;
+  bool on = last.at < kNobody;
+  const int beam = last.at >> 5, token = on ? g.s.end[last.at & 31] : -1;
   uint64_t key = 0;
-  if (on) key = key_of(Elem<T>::one(logits + (last.at >> 5) * g.a.beam_stride + g.s.end[last.at & 31]), g.s.end[last.at & 31]);
+  if (on) key = key_of(Elem<T>::one(logits + beam * g.a.beam_stride + token), token);
   for (int i = 0; i < B; ++i) {
     const Cand x = s.best[i];
-    const bool first = x.score != last.score ? x.score > last.score
-                                             : x.at >> 5 != last.at >> 5 ? x.at < last.at : x.at < kNobody && s.keys[x.at >> 5][x.at & 31] > key;
+    bool first = x.before(last);
+    if (x.score == last.score && x.at < kNobody && x.at >> 5 == beam) first = s.keys[beam][x.at & 31] > key;
     place += first;
   }
   on = on && place < B;  // (places rise with the lanes)
   if (lane < B) {
-    g.a.ended_tokens[to] = on ? g.s.end[last.at & 31] : -1;
-    g.a.ended_parents[to] = on ? last.at >> 5 : -1;
-    g.a.ended_scores[to] = on ? (float)last.score : -INFINITY;
+    g.a.ended_tokens[to] = on ? token : -1;
+    g.a.ended_parents[to] = on ? beam : -1;
+    g.a.ended_scores[to] = on ? last.value() : -INFINITY;
   }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(Args g) {
-  __shared__ uint64_t queue[kWarps][kQueue], lists[kWarps][32];
-  __shared__ Joined joined;
-  __shared__ double sums[kWarps];
-  __shared__ float refs[kWarps];
-  __shared__ int bads[kWarps];
-  __shared__ bool s_last;
+  __shared__ __align__(16) Shared sh;
   chain();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams;
   const int64_t row = blockIdx.x / g.parts;
   const int part = (int)(blockIdx.x % g.parts), r = (int)(row / B), b = (int)(row % B);
   const float c = g.a.scores[row];
   if (c - c == 0) {  // (a score that is not finite: nothing is read of the row)
-    Best best{0, kNoKey, 0, queue[warp], B, lane};
+    Best best{0, kNoKey, 0, sh.queue[warp], B, lane};
     Sum sum{-INFINITY, 0.0f};
     float most = -INFINITY;
-    scan_part(g, static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride, part, best, sum, most);
-    // the lanes', then the warps' sums and lists
-    float ref = sum.ref;
+    const T* from = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride;
+    const Row<T> x{from, g.s.vocab, (int)(reinterpret_cast<uintptr_t>(from) & 15) / (int)sizeof(T), sh.scan.ring[warp], lane};
+    scan_part(g, x, part, best, sum, most);
+    // the lanes' and the warps' sums and lists
+    const float own = warp_max(sum.ref);
     const bool bad = __any_sync(kAll, !(most < INFINITY));
+    sh.scan.lists[warp][lane] = best.list;
+    if (lane == 0) sh.refs[warp] = own, sh.bad[warp] = bad;
+    __syncthreads();
+    float ref = sh.refs[0];
+    int any = sh.bad[0];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(kAll, ref, o));
-    double s = sum.ref == -INFINITY ? 0.0 : (double)(sum.sum * exp_of(sum.ref - ref));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
-    lists[warp][lane] = best.list;
-    if (lane == 0) sums[warp] = s, refs[warp] = ref, bads[warp] = bad;
-    for (int half = kWarps / 2; half > 0; half >>= 1) {
-      __syncthreads();
-      if (warp < half) {
-        best.list = merge32(best.list, lists[warp + half][lane], lane);
-        lists[warp][lane] = best.list;
-      }
-    }
+    for (int w = 1; w < kWarps; ++w) ref = fmaxf(ref, sh.refs[w]), any |= sh.bad[w];
+    const float scaled = sum.ref == -INFINITY ? 0.0f : sum.sum * exp_of(sum.ref - ref);
+    const uint64_t total = warp_sum(__float2ull_rn(scaled * 0x1p32f));
+    if (lane == 0) sh.sums[warp] = total;
+    static_assert(kWarps == 4, "two rounds");
+    if (warp < 2) best.list = merge32(best.list, sh.scan.lists[warp + 2][lane], lane);
+    if (warp == 1) sh.scan.lists[1][lane] = best.list;
+    __syncthreads();
     if (warp == 0) {
       const int64_t at = row * g.parts + part;
-      float top = lane < kWarps ? refs[lane] : -INFINITY;
-      const float mine = top;
-      const bool any = __any_sync(kAll, lane < kWarps && bads[lane < kWarps ? lane : 0]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
-      double t = mine == -INFINITY ? 0.0 : sums[lane] * (double)exp_of(mine - top);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(kAll, t, o);
-      if (lane == 0) g.s.parts[at] = Part{t, top, any};
+      best.list = merge32(best.list, sh.scan.lists[1][lane], lane);
+      if (lane == 0) g.s.parts[at] = Part{sh.sums[0] + sh.sums[1] + sh.sums[2] + sh.sums[3], ref, any};
       if (lane < B) g.s.keys[at * B + lane] = best.list;
     }
   }
@@ -550,13 +608,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(Args g) {
   __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    s_last = atomicAdd(g.s.done + r, 1) == B * g.parts - 1;
-    if (s_last) g.s.done[r] = 0;
+    sh.last = atomicAdd(g.s.done + r, 1) == B * g.parts - 1;
+    if (sh.last) g.s.done[r] = 0;
   }
   __syncthreads();
-  if (!s_last) return;
+  if (!sh.last) return;
   __threadfence();
-  finish<T>(g, r, queue, joined);
+  finish<T>(g, r, sh.queue, sh.joined);
 }
 
 }  // namespace
@@ -564,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(Args g) {
 int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, cudaStream_t st) {
   Args g{a, s, status, 1};
   const int64_t rows = (int64_t)a.num_requests * s.beams;
-  const int64_t chunk = 32 * kVecs * (s.dtype == PS_BEAM_F32 ? 4 : 8), chunks = (s.vocab + chunk - 1) / chunk;
+  const int64_t chunk = kChunk * (s.dtype == PS_BEAM_F32 ? 4 : 8), chunks = (s.vocab + chunk - 1) / chunk;
   int64_t parts = kSpreadCtas / rows;
   const int64_t most = (chunks + kWarps * kLeastChunks - 1) / (kWarps * kLeastChunks);
   parts = parts < most ? parts : most;
