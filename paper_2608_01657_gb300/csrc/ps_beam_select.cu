@@ -28,7 +28,7 @@ namespace psbeam {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 5;
+constexpr int kCtasPerSm = 6;
 constexpr int kVecs = 4;                 // words of a lane and chunk
 constexpr int kChunk = 32 * kVecs;       // words of a chunk
 constexpr int kStages = 4;               // chunks of a warp's ring
@@ -67,6 +67,7 @@ struct Elem<float> {
   static __device__ __forceinline__ float top(const uint4& v) {
     return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
+  static __device__ __forceinline__ uint32_t max1(uint32_t a, uint32_t b) { return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b))); }
   static __device__ __forceinline__ float one(const void* p) { return *static_cast<const float*>(p); }
 };
 template <typename H>
@@ -87,10 +88,10 @@ struct Elem16 {
   }
   // The greatest, NaN if one is.
   static __device__ __forceinline__ float top(const uint4& v) {
-    const float2 f = pskv::Num<H>::unpack(max2(max2(v.x, v.y), max2(v.z, v.w)));
+    const float2 f = pskv::Num<H>::unpack(max1(max1(v.x, v.y), max1(v.z, v.w)));
     return max_nan(f.x, f.y);
   }
-  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  static __device__ __forceinline__ uint32_t max1(uint32_t a, uint32_t b) {
     uint32_t r;
     if (pskv::Num<H>::kBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -109,6 +110,16 @@ template <>
 struct Elem<__half> : Elem16<__half> {
   static __device__ __forceinline__ float one(const void* p) { return __half2float(*static_cast<const __half*>(p)); }
 };
+// The greatest of several words, place by place.
+template <typename T, int M>
+__device__ __forceinline__ uint4 greatest(const uint4 (&v)[M]) {
+  uint4 m = v[0];
+#pragma unroll
+  for (int j = 1; j < M; ++j)
+    m = make_uint4(Elem<T>::max1(m.x, v[j].x), Elem<T>::max1(m.y, v[j].y), Elem<T>::max1(m.z, v[j].z), Elem<T>::max1(m.w, v[j].w));
+  return m;
+}
+
 // ---- keys ---------------------------------------------------------------------------
 // The bits of x as a whole number in x's order; -0 is 0.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -270,7 +281,17 @@ struct Row {
   }
   __device__ __forceinline__ void fetch(int c, int stage) const {
     uint4* slot = ring + stage * kSlot;
+    if (c > 0 && (c + 1) * kChunk * N + N <= V) {  // all of it, and the word after it, is the row's
+      const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + lane * 16;
+      const char* from = reinterpret_cast<const char*>(row - shift) + ((int64_t)c * kChunk + lane) * 16;
 #pragma unroll
+      for (int j = 0; j < kVecs; ++j)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * j), "l"(from + 512 * j) : "memory");
+      if (shift != 0 && lane == 0)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * kVecs), "l"(from + 512 * kVecs) : "memory");
+      return;
+    }
+#pragma unroll 1
     for (int j = 0; j < kVecs; ++j) fetch_word(slot + 32 * j + lane, c * kChunk + 32 * j + lane);
     if (shift != 0 && lane == 0) fetch_word(slot + kChunk, c * kChunk + kChunk);
   }
@@ -310,7 +331,7 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
     if (c0 + i * kWarps < c1) row.fetch(c0 + i * kWarps, i);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  int stage = 0;
+  int stage = 0, end_chunk = g.s.num_end > 0 ? 0 : 1 << 30;
   for (int c = c0; c < c1; c += kWarps) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
     __syncwarp();  // the lanes' copies are there, and all have read the slot that is filled next
@@ -319,12 +340,7 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
     if (c + (kStages - 1) * kWarps < c1) row.fetch(c + (kStages - 1) * kWarps, stage == 0 ? kStages - 1 : stage - 1);
     asm volatile("cp.async.commit_group;" ::: "memory");
     stage = stage == kStages - 1 ? 0 : stage + 1;
-    float top[kVecs], all = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      top[j] = Elem<T>::top(v[j]);
-      all = max_nan(all, top[j]);
-    }
+    float all = Elem<T>::top(greatest<T>(v));
     most = max_nan(most, all);
     sum.raise(all);
     const float base = sum.base();
@@ -346,22 +362,24 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
     const float2 f = pskv::unpack2(pskv::add2(s0, s1));
     sum.sum += f.x + f.y;
     const int w0 = c * kChunk + lane;
-    unsigned out = 0;  // the lane's end tokens: they do not count
+    if (c >= end_chunk) {  // an end token is among these, or one lies behind: end tokens do not count
+      unsigned out = 0;
+      end_chunk = 1 << 30;
+      for (int i = 0; i < g.s.num_end; ++i) {
+        const int word = g.s.end[i] / N, w = word - w0;
+        if (w >= 0 && w < kChunk && (w & 31) == 0) out |= 1u << (w / 32 * N + g.s.end[i] % N);
+        if (word / kChunk > c) end_chunk = min(end_chunk, word / kChunk);
+      }
+      if (out) {
 #pragma unroll
-    for (int i = 0; i < PS_BEAM_MAX_END; ++i) {
-      const int w = g.s.end[i] / N - w0;
-      if (i < g.s.num_end && w >= 0 && w < kChunk && (w & 31) == 0) out |= 1u << (w / 32 * N + g.s.end[i] % N);
-    }
-    if (out) {
-      all = -INFINITY;
+        for (int j = 0; j < kVecs; ++j) {
+          float x[N];
+          Elem<T>::wide(v[j], x);
 #pragma unroll
-      for (int j = 0; j < kVecs; ++j) {
-        float x[N];
-        Elem<T>::wide(v[j], x);
-        top[j] = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < N; ++e) top[j] = out >> (j * N + e) & 1 ? top[j] : fmaxf(top[j], x[e]);
-        all = fmaxf(all, top[j]);
+          for (int e = 0; e < N; ++e) x[e] = out >> (j * N + e) & 1 ? -INFINITY : x[e];
+          v[j] = Elem<T>::narrow(x);
+        }
+        all = Elem<T>::top(greatest<T>(v));
       }
     }
     if (c == c0) {  // the beams-th of the lanes' greatest: so many words are no smaller
@@ -372,8 +390,9 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
     if (!__any_sync(kAll, all >= least)) continue;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-      if (!__any_sync(kAll, top[j] >= least)) continue;
-      const uint64_t key = key_of(top[j], w0 + 32 * j);
+      const float top = Elem<T>::top(v[j]);
+      if (!__any_sync(kAll, top >= least)) continue;
+      const uint64_t key = key_of(top, w0 + 32 * j);
       best.add(key, key > best.floor);
     }
   }
