@@ -41,15 +41,14 @@ typedef struct {
 typedef struct ps_beam ps_beam_t;
 
 /* Bytes of device workspace a handle needs (256-byte aligned base required), or 0
- * if the configuration is invalid: the partial results of rows that several CTAs
- * read, 16 + 8 beams bytes for each of max_requests * beams + 2432 of them. */
+ * if the configuration is invalid: partial results, 516 bytes for each of
+ * max_requests * beams rows, and 8 beams for each of 32 lists a row (up to 4096 rows;
+ * 2 a row of more, and 7680). */
 size_t ps_beam_workspace_bytes(const ps_beam_config_t* cfg);
 
-/* Create a handle on the current device; clearing its counters is enqueued on
- * 'stream'.  The workspace must stay allocated and untouched until
- * ps_beam_destroy(). */
-int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_workspace, size_t workspace_bytes,
-                       void* stream);
+/* Create a handle on the current device.  The workspace, which need not be cleared,
+ * must stay allocated and untouched until ps_beam_destroy(). */
+int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_workspace, size_t workspace_bytes);
 
 /* Free the host-side handle.  The workspace is the caller's to free. */
 void ps_beam_destroy(ps_beam_t* beam);
@@ -61,7 +60,7 @@ void ps_beam_destroy(ps_beam_t* beam);
  *   c + x[v] - log sum_u exp x[u],
  * the sum in 32 bits at least, the score in 64, rounded once.  A logit of
  * -infinity is a token that cannot follow.  Candidates are ordered by score, equal
- * ones by beam, then by logit, then by token, the lowest first.  Of each request
+ * ones by beam, then by token, the lowest first.  Of each request
  *   tokens, parents, scores_out  [beams] are the first candidates whose tokens end
  *     nothing, and the beams (0..beams - 1) that they continue;
  *   ended_tokens, ended_parents, ended_scores  [beams] (all three or none) are the

@@ -56,8 +56,7 @@ class BeamSearch(Handle):
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         h = C.c_void_p()
-        self._raise("ps_beam_create", L.ps_beam_create(C.byref(h), C.byref(c), self.workspace.data_ptr(), nbytes,
-                                                       B._stream_ptr(stream)))
+        self._raise("ps_beam_create", L.ps_beam_create(C.byref(h), C.byref(c), self.workspace.data_ptr(), nbytes))
         self._h = h
         self._kept = (self.workspace, self.status)
         self._begin(stream)

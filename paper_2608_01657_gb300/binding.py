@@ -233,7 +233,7 @@ def load():
     L.ps_beam_workspace_bytes.restype = sz
     L.ps_beam_workspace_bytes.argtypes = [C.POINTER(PsBeamConfig)]
     L.ps_beam_create.restype = i32
-    L.ps_beam_create.argtypes = [C.POINTER(vp), C.POINTER(PsBeamConfig), vp, sz, vp]
+    L.ps_beam_create.argtypes = [C.POINTER(vp), C.POINTER(PsBeamConfig), vp, sz]
     L.ps_beam_destroy.restype = None
     L.ps_beam_destroy.argtypes = [vp]
     L.ps_beam_select.restype = i32

@@ -13,7 +13,7 @@ using pskv::outputs_apart;
 
 struct ps_beam {
   Search s;
-  int32_t max_requests;
+  int32_t max_requests, nsm;
 };
 
 namespace {
@@ -43,14 +43,14 @@ size_t carve(const ps_beam_config_t& c, char* base, Search* s) {
     off += bytes;
     return p;
   };
-  const size_t parts = (size_t)c.max_requests * c.beams + kSpreadCtas;
-  char* done = take(4 * (size_t)c.max_requests);
-  char* part = take(sizeof(Part) * parts);
-  char* keys = take(8 * parts * c.beams);
+  const size_t rows = (size_t)c.max_requests * c.beams;
+  char* part = take(sizeof(Part) * rows * kRowParts);
+  char* keys = take(8 * (size_t)most_lists((int64_t)rows) * c.beams);
+  char* lists = take(4 * rows);
   if (s) {
-    s->done = reinterpret_cast<int32_t*>(done);
     s->parts = reinterpret_cast<Part*>(part);
     s->keys = reinterpret_cast<uint64_t*>(keys);
+    s->lists = reinterpret_cast<int32_t*>(lists);
   }
   return (off + 255) / 256 * 256;
 }
@@ -61,14 +61,18 @@ extern "C" {
 
 size_t ps_beam_workspace_bytes(const ps_beam_config_t* cfg) { return check_config(cfg) ? carve(*cfg, nullptr, nullptr) : 0; }
 
-int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_workspace, size_t workspace_bytes,
-                       void* stream) {
+int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_workspace, size_t workspace_bytes) {
   if (!out || !check_config(cfg) || !d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0 ||
       workspace_bytes < carve(*cfg, nullptr, nullptr))
     return PS_ERR_INVALID_ARG;
+  int dev = 0, nsm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return PS_ERR_CUDA;
   ps_beam* b = new (std::nothrow) ps_beam{};
   if (!b) return PS_ERR_CUDA;
   b->max_requests = cfg->max_requests;
+  b->nsm = nsm < pskv::kMaxSms ? nsm : pskv::kMaxSms;
   b->s.beams = cfg->beams;
   b->s.vocab = cfg->vocab;
   b->s.dtype = cfg->dtype;
@@ -76,10 +80,6 @@ int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_wor
   for (int i = 0; i < cfg->num_end; ++i) b->s.end[i] = cfg->end_tokens[i];
   std::sort(b->s.end, b->s.end + cfg->num_end);
   carve(*cfg, static_cast<char*>(d_workspace), &b->s);
-  if (cudaMemsetAsync(b->s.done, 0, 4 * (size_t)cfg->max_requests, as_stream(stream)) != cudaSuccess) {
-    delete b;
-    return PS_ERR_CUDA;
-  }
   *out = b;
   return PS_OK;
 }
@@ -101,7 +101,7 @@ int32_t ps_beam_select(ps_beam_t* beam, void* stream, const ps_beam_select_t* a,
                         {a->tokens, n, true}, {a->parents, n, true}, {a->scores_out, n, true},
                         {a->ended_tokens, n, true}, {a->ended_parents, n, true}, {a->ended_scores, n, true}};
   if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
-  return launch_select(beam->s, *a, d_status, as_stream(stream));
+  return launch_select(beam->s, *a, d_status, beam->nsm, as_stream(stream));
 }
 
 int32_t ps_beam_trace(ps_beam_t* beam, void* stream, const ps_beam_trace_t* a, int32_t* d_status) {

@@ -2,47 +2,57 @@
 //
 // Of a beam with score c and logits x, token v continues it with the score c + x_v
 // - lse, lse = log sum_u exp x_u.  Within a beam the order is the logits', and a
-// request's best are among its beams' best.  A row is read once, in words of 16
-// bytes, for two things: a sum of 2^((x - ref) log2 e), whose reference rises with the
-// greatest logit seen, and the 'beams' words of the greatest logits.  The row's best
-// tokens are in those words: every word that comes before one of theirs (by its
-// greatest logit, equal ones by place) holds a token that comes before it, too.  So
-// single elements are looked at in a few words only, at the end.  Words are kept as
-// whole numbers, the logit's bits in order and then the complement of the place, so
-// that no two are equal.
+// request's best are among its beams' best.  A row is read once, in runs of 64 bytes,
+// for two things: a sum of 2^((x - ref) log2 e), whose reference rises with the greatest
+// logit seen, and the 'beams' runs of the greatest logits.  The best tokens are in the
+// best runs: every run that comes before one of theirs (by its greatest logit, equal
+// ones by place) holds a token that comes before it, too, in a row as among a request's
+// beams.  So single elements are looked at in a request's best runs only, at the end.
+// Runs are kept as whole numbers, the logit's bits in order and then the complement of
+// the place, so that no two are equal.
 //
-// Bound by HBM.  A row is cut into parts, a CTA each, so that a few rows fill the GPU,
-// too; the last CTA of a request to finish puts the parts together, in an order that
-// does not depend on which one it is.
+// Bound by HBM.  k_select's resident warps divide the list of all rows' chunks of 2 KB
+// into equal shares.  Sums are kept for each of up to 32 parts of a row, always the
+// same, so that they do not depend on the shares: equal rows have equal sums.  Rows of
+// beams that are not there are left out of the list.  k_select_join puts the parts of
+// a request together, a CTA each.
 //
 // A warp reads 2 KB at a time through a ring in shared memory, three of them under way
-// while it works on one.  It keeps a list of 32 sorted across its lanes; what is greater than the list's
-// beams-th enters a queue, 32 of which are sorted and merged at a time.
+// while it works on one, a run a lane.  What is greater than the beams-th of its best
+// enters a queue, 32 of which are looked through at a time.  A lower bound of that
+// beams-th is the beams-th of the lanes' greatest logits, taken after 1, 2, 4, ... chunks.
 //
-// Neighbours in the order of scores may be nearer than 32 bits tell: differences
-// from the reference are exact or rounded once, log2 e has two parts, the lanes' sums
-// are added as whole numbers of 2^-32, and scores in 64 bits.
+// Neighbours in the order of scores may be nearer than 32 bits tell.  A term is 2^(x a -
+// R), a = log2 e rounded to 32 bits and R a whole number no less than any x a, so that a
+// product and a sum are rounded once and sums of other R are scaled exactly; sums are
+// added up as whole numbers of 2^-32.  They are those of exp((x - R / a) a ln 2): the
+// exponents are off by a ln 2 - 1 = 1.3e-8 of their size.  Scores are added in 64 bits.
 #include "ps_beam.cuh"
 
 namespace psbeam {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 6;
-constexpr int kVecs = 4;                 // words of a lane and chunk
-constexpr int kChunk = 32 * kVecs;       // words of a chunk
+constexpr int kCtasPerSm = 5;
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+constexpr int kVecs = 4;                 // 16-byte words of a run
+constexpr int kChunk = 32 * kVecs;       // words of a chunk, a run a lane
 constexpr int kStages = 4;               // chunks of a warp's ring
-// A warp has so many chunks at least, where there are as many.
-constexpr int kLeastChunks = 2;
-constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;  // their sum: log2 e to 2^-48
+constexpr float kLog2e = 1.44269502f;    // 'a'
 constexpr double kLn2 = 0.693147180559945309;
+constexpr float kFar = 1e38f;            // logits whose a-fold may not be finite
 constexpr unsigned kAll = 0xFFFFFFFFu;
 
 struct Args {
   ps_beam_select_t a;
   Search s;
   int32_t* status;
-  int32_t parts;  // of a row
+  int64_t rows;
+  int32_t chunks;   // of a row
+  int32_t size;     // chunks of a part
+  int32_t parts;    // of a row
+  int32_t slots;    // lists of a row at most
+  bool compact;     // rows of beams that are not there are left out
 };
 
 // ---- elements ---------------------------------------------------------------------
@@ -172,6 +182,36 @@ __device__ __forceinline__ bool ends(const Search& s, int token) {
   return e;
 }
 
+// Up to this many are taken out one by one, each by two reductions (2 x 8 of them take
+// 700 cycles, a sort of 32 and a merge 1150).
+constexpr int kOneByOne = 8;
+// The 'keep' greatest of two numbers a lane, none of them equal but zeros, from the
+// greatest on, one a lane; what is in the other lanes is less.
+__device__ __forceinline__ uint64_t greatest_of(uint64_t a, uint64_t b, int keep, int lane) {
+  if (keep > kOneByOne) return merge32(sort32(a, lane), sort32(b, lane), lane);
+  uint64_t out = 0;
+  for (int k = 0; k < keep; ++k) {
+    const uint64_t m = a > b ? a : b;
+    const uint32_t hi = __reduce_max_sync(kAll, (uint32_t)(m >> 32));
+    const uint32_t lo = __reduce_max_sync(kAll, (uint32_t)(m >> 32) == hi ? (uint32_t)m : 0);
+    const uint64_t top = (uint64_t)hi << 32 | lo;
+    if (lane == k) out = top;
+    if (a == top) a = 0;
+    if (b == top) b = 0;
+  }
+  return out;
+}
+// The keep-th of the lanes' numbers.
+__device__ __forceinline__ uint32_t kth_of(uint32_t x, int keep, int lane) {
+  if (keep > kOneByOne) return __shfl_sync(kAll, sort32(x, lane), keep - 1);
+  uint32_t top = 0;
+  for (int k = 0; k < keep; ++k) {
+    top = __reduce_max_sync(kAll, x);
+    if (lane == __ffs(__ballot_sync(kAll, x == top)) - 1) x = 0;
+  }
+  return top;
+}
+
 // A warp's best so far.
 constexpr int kQueue = 64;
 struct Best {
@@ -187,7 +227,7 @@ struct Best {
     const uint64_t q = from + lane < queued ? queue[from + lane] : 0;
     __syncwarp();
     queued = from;
-    list = merge32(list, sort32(q, lane), lane);
+    list = keep > kOneByOne ? merge32(list, sort32(q, lane), lane) : greatest_of(list, q, keep, lane);
     raise(__shfl_sync(kAll, list, keep - 1));
   }
   __device__ __forceinline__ void add(uint64_t key, bool on) {
@@ -196,16 +236,9 @@ struct Best {
     queued += __popc(m);
     if (queued >= 32) flush();
   }
-  // A smaller logit does not enter.
-  __device__ __forceinline__ float least() const { return logit_of(floor + 1); }
 };
 
 // ---- sums -----------------------------------------------------------------------------
-// exp(x) for x <= 0, the exponent in two parts; 0 below 2^-144 (where the parts are not finite at last).
-__device__ __forceinline__ float exp_of(float x) {
-  const float t = x * kLog2e;
-  return x < -100.0f ? 0.0f : pskv::ex2(t) * (1.0f + 0.693147181f * fmaf(x, kLog2eRest, fmaf(x, kLog2e, -t)));
-}
 // log(u 2^-32) for u > 0, to 4e-9.  With u = 2^e m, 0.7 < m < 1.42, and f = (m - 1) /
 // (m + 1): log m = 2 (f + f^3 / 3 + f^5 / 5 + ...), the first term in two parts.
 __device__ __forceinline__ double log_of(uint64_t u) {
@@ -225,17 +258,20 @@ __device__ __forceinline__ double log_of(uint64_t u) {
   return (double)e * kLn2 + ((double)(2.0f * f) + (double)(2.0f * fmaf(f, p, f_lo)));
 }
 
-// A lane's sum of exp(x - ref).
+// R of a greatest logit.
+__device__ __forceinline__ float exponent_of(float most) { return ceilf(most * kLog2e); }
+// A lane's sum of 2^(x a - R).
 struct Sum {
-  float ref, sum;
-  __device__ __forceinline__ void raise(float to) {
-    if (to > ref) {
-      sum = ref == -INFINITY ? 0.0f : sum * pskv::ex2((ref - to) * kLog2e);
-      ref = to;
+  float R, sum;
+  __device__ __forceinline__ void raise(float most) {
+    const float to = exponent_of(most);
+    if (to > R) {
+      sum = R == -INFINITY ? 0.0f : sum * pskv::ex2(R - to);
+      R = to;
     }
   }
   // What is subtracted: nothing while all are -infinity.
-  __device__ __forceinline__ float base() const { return ref == -INFINITY ? 0.0f : ref; }
+  __device__ __forceinline__ float base() const { return R == -INFINITY ? 0.0f : R; }
 };
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -255,96 +291,101 @@ __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
 // one, a word is put together from two; elements of aligned words that are not the
 // row's are not read.
 constexpr int kSlot = kChunk + 1;  // with the word after the chunk's
+// Where word w of a chunk lies in its slot: lanes that read their runs' words, four words
+// apart, and lanes that fill neighbouring ones meet no bank twice.
+__device__ __forceinline__ int place_in_slot(int w) { return w ^ (w >> 3 & 3); }
 
 template <typename T>
-struct Row {
-  static constexpr int N = Elem<T>::N;
-  const T* row;
-  int V, shift;
-  uint4* ring;  // [kStages][kSlot] of the warp
-  int lane;
-  __device__ __forceinline__ void fetch_word(uint4* to, int w) const {
-    const int first = w * N - shift;
-    if (first >= 0 && first + N <= V) {
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(row + first) : "memory");
-    } else {
-      float x[N];
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = -INFINITY;
-      if (first < V) {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (first + e >= 0 && first + e < V) x[e] = Elem<T>::one(row + first + e);
-      }
-      *to = Elem<T>::narrow(x);
-    }
-  }
-  __device__ __forceinline__ void fetch(int c, int stage) const {
-    uint4* slot = ring + stage * kSlot;
-    if (c > 0 && (c + 1) * kChunk * N + N <= V) {  // all of it, and the word after it, is the row's
-      const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + lane * 16;
-      const char* from = reinterpret_cast<const char*>(row - shift) + ((int64_t)c * kChunk + lane) * 16;
-#pragma unroll
-      for (int j = 0; j < kVecs; ++j)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * j), "l"(from + 512 * j) : "memory");
-      if (shift != 0 && lane == 0)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * kVecs), "l"(from + 512 * kVecs) : "memory");
-      return;
-    }
-#pragma unroll 1
-    for (int j = 0; j < kVecs; ++j) fetch_word(slot + 32 * j + lane, c * kChunk + 32 * j + lane);
-    if (shift != 0 && lane == 0) fetch_word(slot + kChunk, c * kChunk + kChunk);
-  }
-  __device__ __forceinline__ void take(int stage, uint4 (&v)[kVecs]) const {
-    const uint4* slot = ring + stage * kSlot + lane;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) v[j] = slot[32 * j];
-    if (shift == 0) return;
-    const int words = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const uint4 n = slot[32 * j + 1];
-      uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, n.x, n.y, n.z, n.w};
-      if (words & 2) {
-#pragma unroll
-        for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
-      }
-      if (words & 1) {
-#pragma unroll
-        for (int i = 0; i < 5; ++i) x[i] = x[i + 1];
-      }
-      v[j] = make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
-                        __funnelshift_r(x[3], x[4], bits));
-    }
-  }
-};
-
-template <typename T>
-__device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int part, Best& best, Sum& sum, float& most) {
+__device__ __forceinline__ void fetch_word(uint4* to, const T* row, int shift, int w, int V) {
   constexpr int N = Elem<T>::N;
-  const int lane = row.lane, warp = threadIdx.x >> 5;
-  const int words = (row.V - 1) / N + 1;
-  const int chunks = (words + kChunk - 1) / kChunk;
-  const int c0 = (int)((int64_t)chunks * part / g.parts) + warp, c1 = (int)((int64_t)chunks * (part + 1) / g.parts);
+  const int first = w * N - shift;
+  if (first >= 0 && first + N <= V) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(row + first) : "memory");
+  } else {
+    float x[N];
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    if (c0 + i * kWarps < c1) row.fetch(c0 + i * kWarps, i);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+    if (first < V) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (first + e >= 0 && first + e < V) x[e] = Elem<T>::one(row + first + e);
+    }
+    *to = Elem<T>::narrow(x);
   }
-  int stage = 0, end_chunk = g.s.num_end > 0 ? 0 : 1 << 30;
-  for (int c = c0; c < c1; c += kWarps) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncwarp();  // the lanes' copies are there, and all have read the slot that is filled next
-    uint4 v[kVecs];
-    row.take(stage, v);
-    if (c + (kStages - 1) * kWarps < c1) row.fetch(c + (kStages - 1) * kWarps, stage == 0 ? kStages - 1 : stage - 1);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    stage = stage == kStages - 1 ? 0 : stage + 1;
+}
+// Chunk c of a row into a slot of the ring, asynchronously.
+template <typename T>
+__device__ __forceinline__ void fetch_chunk(uint4* slot, const T* row, int shift, int c, int V, int lane) {
+  constexpr int N = Elem<T>::N;
+  if (c > 0 && (c + 1) * kChunk * N + N <= V) {  // all of it, and the word after it, is the row's
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + place_in_slot(lane) * 16;  // (32 words on the pattern is the same)
+    const char* from = reinterpret_cast<const char*>(row - shift) + ((int64_t)c * kChunk + lane) * 16;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * j), "l"(from + 512 * j) : "memory");
+    if (shift != 0 && lane == 0)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * kVecs), "l"(from + 512 * kVecs) : "memory");
+    return;
+  }
+#pragma unroll 1
+  for (int j = 0; j < kVecs; ++j) fetch_word(slot + place_in_slot(32 * j + lane), row, shift, c * kChunk + 32 * j + lane, V);
+  if (shift != 0 && lane == 0) fetch_word(slot + kChunk, row, shift, c * kChunk + kChunk, V);
+}
+// A lane's run of a chunk.
+template <typename T>
+__device__ __forceinline__ void take_run(const uint4* slot, int shift, int lane, uint4 (&v)[kVecs]) {
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) v[j] = slot[place_in_slot(kVecs * lane + j)];
+  if (shift == 0) return;
+  const int words = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
+  const uint4 behind = slot[lane == 31 ? kChunk : place_in_slot(kVecs * lane + kVecs)];
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const uint4 n = j + 1 < kVecs ? v[j + 1 < kVecs ? j + 1 : j] : behind;
+    uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, n.x, n.y, n.z, n.w};
+    if (words & 2) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
+    }
+    if (words & 1) {
+#pragma unroll
+      for (int i = 0; i < 5; ++i) x[i] = x[i + 1];
+    }
+    v[j] = make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
+                      __funnelshift_r(x[3], x[4], bits));
+  }
+}
+
+// One chunk of a row.
+template <typename T>
+struct Scan {
+  static constexpr int N = Elem<T>::N;
+  Best best;
+  Sum sum;
+  float most;
+  int end_chunk;   // no end token is in a chunk before this one
+  float top;       // the lane's greatest logit of a token that ends nothing
+  int seen, again; // chunks looked at, and when the lanes' greatest are looked at next
+  __device__ __forceinline__ void begin_part() {
+    sum = Sum{-INFINITY, 0.0f};
+    most = -INFINITY;
+  }
+  __device__ __forceinline__ void begin_row(const Args& g) {
+    best.list = 0;
+    best.floor = kNoKey;
+    best.queued = 0;
+    top = -INFINITY;
+    seen = 0;
+    again = 1;
+    end_chunk = g.s.num_end > 0 ? 0 : 1 << 30;
+  }
+  __device__ __forceinline__ void chunk(const Args& g, uint4 (&v)[kVecs], int c) {
+    const int lane = best.lane;
     float all = Elem<T>::top(greatest<T>(v));
     most = max_nan(most, all);
     sum.raise(all);
     const float base = sum.base();
-    const uint64_t minus = pskv::pack2(-base, -base), hi = pskv::pack2(kLog2e, kLog2e), lo = pskv::pack2(kLog2eRest, kLog2eRest);
+    const uint64_t minus = pskv::pack2(-base, -base), a = pskv::pack2(kLog2e, kLog2e);
     uint64_t s0 = 0, s1 = 0;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
@@ -352,8 +393,7 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
       Elem<T>::wide(v[j], x);
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
-        const uint64_t d = pskv::add2(pskv::pack2(x[e], x[e + 1]), minus);
-        const float2 t = pskv::unpack2(pskv::fma2(d, lo, pskv::mul2(d, hi)));
+        const float2 t = pskv::unpack2(pskv::fma2(pskv::pack2(x[e], x[e + 1]), a, minus));
         const uint64_t p = pskv::pack2(pskv::ex2(t.x), pskv::ex2(t.y));
         if (e & 2) s1 = pskv::add2(s1, p);
         else s0 = pskv::add2(s0, p);
@@ -361,13 +401,13 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
     }
     const float2 f = pskv::unpack2(pskv::add2(s0, s1));
     sum.sum += f.x + f.y;
-    const int w0 = c * kChunk + lane;
     if (c >= end_chunk) {  // an end token is among these, or one lies behind: end tokens do not count
+      const int w0 = c * kChunk + kVecs * lane;
       unsigned out = 0;
       end_chunk = 1 << 30;
       for (int i = 0; i < g.s.num_end; ++i) {
         const int word = g.s.end[i] / N, w = word - w0;
-        if (w >= 0 && w < kChunk && (w & 31) == 0) out |= 1u << (w / 32 * N + g.s.end[i] % N);
+        if (w >= 0 && w < kVecs) out |= 1u << (w * N + g.s.end[i] % N);
         if (word / kChunk > c) end_chunk = min(end_chunk, word / kChunk);
       }
       if (out) {
@@ -382,275 +422,412 @@ __device__ __forceinline__ void scan_part(const Args& g, const Row<T>& row, int 
         all = Elem<T>::top(greatest<T>(v));
       }
     }
-    if (c == c0) {  // the beams-th of the lanes' greatest: so many words are no smaller
-      const uint32_t s = __shfl_sync(kAll, sort32(ordered(all), lane), best.keep - 1);
-      best.raise(((uint64_t)s << 32) - 1);
+    top = fmaxf(top, all);
+    if (++seen == again) {  // so many runs are no smaller
+      again *= 2;
+      best.raise(((uint64_t)kth_of(ordered(top), best.keep, lane) << 32) - 1);
     }
-    const float least = best.least();
-    if (!__any_sync(kAll, all >= least)) continue;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const float top = Elem<T>::top(v[j]);
-      if (!__any_sync(kAll, top >= least)) continue;
-      const uint64_t key = key_of(top, w0 + 32 * j);
-      best.add(key, key > best.floor);
-    }
+    const uint64_t key = key_of(all, c * 32 + lane);
+    const bool on = key > best.floor;
+    if (__any_sync(kAll, on)) best.add(key, on);
   }
-  while (best.queued > 0) best.flush();
+};
+
+// The rows that are looked at: all, or those whose scores are finite.
+struct Live {
+  uint32_t bits[kRowWords];
+  int before[kRowWords + 1];  // live rows before a word's
+  // Row of the live row number a, the same in all lanes.
+  __device__ __forceinline__ int row(int a, int lane) const {
+    int lo = 0, hi = kRowWords - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (before[mid] <= a) lo = mid;
+      else hi = mid - 1;
+    }
+    const uint32_t m = bits[lo];
+    return lo * 32 + __ffs(__ballot_sync(kAll, (m >> lane & 1) && __popc(m & ((1u << lane) - 1)) == a - before[lo])) - 1;
+  }
+};
+
+// A row of the list: which one it is, where it begins, and whether it is looked at.
+template <typename T>
+struct Open {
+  const T* row;
+  int i, shift;
+  bool live;
+  __device__ __forceinline__ void open(const Args& g, const Live& live_rows, int number, int lane) {
+    i = g.compact ? live_rows.row(number, lane) : number;
+    const int r = i / g.s.beams;
+    live = true;
+    if (!g.compact) {
+      const float c = g.a.scores[i];
+      live = c - c == 0;
+    }
+    row = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + (i - r * g.s.beams) * g.a.beam_stride;
+    shift = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(T);
+  }
+};
+
+struct Shared {
+  uint4 ring[kWarps][kStages * kSlot];
+  uint64_t queue[kWarps][kQueue];
+  Live live;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(const __grid_constant__ Args g) {
+  __shared__ __align__(16) Shared sh;
+  chain();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams;
+  int count = (int)g.rows;
+  if (g.compact) {
+    constexpr int kAtOnce = 8;
+    const int words = (count + 31) / 32;
+    for (int i0 = warp; i0 < kRowWords; i0 += kWarps * kAtOnce) {
+      float c[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int row = (i0 + u * kWarps) * 32 + lane;
+        c[u] = row < g.rows ? g.a.scores[row] : -INFINITY;
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const unsigned m = __ballot_sync(kAll, c[u] - c[u] == 0);
+        if (lane == 0) sh.live.bits[i0 + u * kWarps] = m;
+      }
+      if (i0 + kWarps * kAtOnce - warp >= words) {  // no rows behind these
+        for (int i = i0 + kWarps * kAtOnce + lane * kWarps; i < kRowWords; i += 32 * kWarps) sh.live.bits[i] = 0;
+        break;
+      }
+    }
+    __syncthreads();
+    if (warp == 0) {  // four words a lane
+      int n[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        n[i] = sum;
+        sum += __popc(sh.live.bits[4 * lane + i]);
+      }
+      int incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(kAll, incl, o);
+        if (lane >= o) incl += x;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh.live.before[4 * lane + i] = incl - sum + n[i];
+      if (lane == 31) sh.live.before[kRowWords] = incl;
+    }
+    __syncthreads();
+    count = sh.live.before[kRowWords];
+    if (count == 0) return;
+  }
+  // the warp's share of the list of all parts
+  const int all = gridDim.x * kWarps, w = blockIdx.x * kWarps + warp;
+  const int64_t U = (int64_t)count * g.parts;
+  const int C = U < all ? (int)U : all;
+  if (w >= C) return;
+  int64_t u0, u1;
+  int slot;  // of the share's first row: workers before this one that have a share of it
+  if (U <= 1 << 19) {  // w < 2^12, so that products are below 2^31
+    const int n = (int)U;
+    u0 = n * w / C, u1 = n * (w + 1) / C;
+    slot = w - ((int)u0 / g.parts * g.parts * C + C - 1) / n;
+  } else {
+    u0 = U * w / C, u1 = U * (w + 1) / C;
+    slot = w - pskv::worker_of(u0 / g.parts * g.parts, U, C);
+  }
+  int number = (int)(u0 / g.parts), chunk = (int)(u0 - (int64_t)number * g.parts) * g.size;
+  const int last_number = (int)((u1 - 1) / g.parts);
+  const int last_end = min((int)(u1 - (int64_t)last_number * g.parts) * g.size, g.chunks);  // chunk after the last
+  uint4* const ring = sh.ring[warp];
+  // the chunk to fetch next, and the one at work
+  int ahead = number, ahead_chunk = chunk;
+  Open<T> from;
+  from.open(g, sh.live, ahead, lane);
+  int row = from.i, shift = from.shift;
+  bool live = from.live;
+  auto fetch = [&](int stage) {
+    if (ahead < last_number || (ahead == last_number && ahead_chunk < last_end)) {
+      if (from.live) fetch_chunk(ring + stage * kSlot, from.row, from.shift, ahead_chunk, g.s.vocab, lane);
+      if (++ahead_chunk == g.chunks) {
+        ahead_chunk = 0;
+        if (++ahead <= last_number) from.open(g, sh.live, ahead, lane);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = 0; i < kStages - 1; ++i) fetch(i);
+  Scan<T> scan;
+  scan.best.queue = sh.queue[warp];
+  scan.best.keep = B;
+  scan.best.lane = lane;
+  scan.begin_row(g);
+  scan.begin_part();
+  int stage = 0, stop = min(chunk + g.size, g.chunks);
+  while (true) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();  // the lanes' copies are there, and all have read the slot that is filled next
+    uint4 v[kVecs];
+    take_run<T>(ring + stage * kSlot, shift, lane, v);
+    fetch(stage == 0 ? kStages - 1 : stage - 1);
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+    if (live) scan.chunk(g, v, chunk);
+    if (++chunk < stop) continue;
+    // the end of a part
+    if (live) {
+      const float most = warp_max(scan.most);
+      const bool bad = __any_sync(kAll, !(scan.most < INFINITY));
+      const float scaled = scan.sum.R == -INFINITY ? 0.0f : scan.sum.sum * pskv::ex2(scan.sum.R - exponent_of(most));
+      const uint64_t sum = warp_sum(__float2ull_rn(scaled * 0x1p32f));
+      if (lane == 0) g.s.parts[(int64_t)row * g.parts + (chunk - 1) / g.size] = Part{sum, most, bad};
+      scan.begin_part();
+    }
+    stop = min(chunk + g.size, g.chunks);
+    if (chunk < g.chunks && !(number == last_number && chunk == last_end)) continue;
+    // the end of the warp's share of the row
+    if (live) {
+      while (scan.best.queued > 0) scan.best.flush();
+      if (lane < B) g.s.keys[((int64_t)row * g.slots + slot) * B + lane] = scan.best.list;
+      if (lane == 0 && chunk == g.chunks) g.s.lists[row] = slot + 1;
+    }
+    if (number == last_number) break;
+    ++number;
+    chunk = slot = 0;
+    stop = min(g.size, g.chunks);
+    Open<T> next;
+    next.open(g, sh.live, number, lane);
+    row = next.i, shift = next.shift, live = next.live;
+    scan.begin_row(g);
+  }
 }
 
 // ---- the parts of a request -------------------------------------------------------------
-// A candidate of a request: its score as a whole number in the scores' order, and its
-// beam and place in the beam's list.
+// A candidate of a request: its score as a whole number in the scores' order, and what
+// decides between equal ones.
 struct Cand {
-  long long score;
-  int at;  // beam 32 + place
-  __device__ __forceinline__ bool before(const Cand& y) const { return score != y.score ? score > y.score : at < y.at; }
-  __device__ __forceinline__ Cand shfl(int from) const { return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, at, from)}; }
+  long long score, tie;
+  __device__ __forceinline__ bool before(const Cand& y) const { return score != y.score ? score > y.score : tie < y.tie; }
+  __device__ __forceinline__ Cand shfl(int from) const { return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, tie, from)}; }
   __device__ __forceinline__ float value() const { return (float)__longlong_as_double(score < 0 ? score ^ 0x7FFFFFFFFFFFFFFFll : score); }
+  __device__ __forceinline__ bool somebody() const { return tie < 1ll << 60; }
 };
-constexpr int kNobody = 1 << 20;  // a place after every candidate's
-__device__ __forceinline__ Cand cand(double score, int at) {
+__device__ __forceinline__ Cand cand(double score, long long tie) {
   const long long b = __double_as_longlong(score + 0.0);
-  return {b < 0 ? b ^ 0x7FFFFFFFFFFFFFFFll : b, at};
+  return {b < 0 ? b ^ 0x7FFFFFFFFFFFFFFFll : b, tie};
 }
-__device__ __forceinline__ Cand nobody(int lane) { return {(long long)0x8000000000000000ull, kNobody + lane}; }
-__device__ __forceinline__ void exchange(Cand& x, int lane, int other, bool first) {
-  const Cand y = x.shfl(lane ^ other);
-  if (x.before(y) != first) x = y;
-}
-__device__ __forceinline__ Cand sort32(Cand x, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) exchange(x, lane, j, ((lane & j) == 0) == ((lane & k) == 0));
-  return x;
-}
+__device__ __forceinline__ Cand nobody(int lane) { return {(long long)0x8000000000000000ull, (1ll << 60) + lane}; }
 __device__ __forceinline__ Cand merge32(Cand x, const Cand& y, int lane) {
   const Cand z = y.shfl(31 - lane);
   if (z.before(x)) x = z;
 #pragma unroll
-  for (int j = 16; j > 0; j >>= 1) exchange(x, lane, j, (lane & j) == 0);
+  for (int j = 16; j > 0; j >>= 1) {
+    const Cand o = x.shfl(lane ^ j);
+    if (x.before(o) != ((lane & j) == 0)) x = o;
+  }
   return x;
 }
 
-// The best tokens of a row, from the words that hold them.
+// A beam's score, the reference R / a, and the log of the sum over it.
+struct Beam {
+  double total, ref;
+  float score;
+  // The reference, which may be far from 0, is subtracted first.
+  __device__ __forceinline__ double of(float logit) const { return (double)score + (((double)logit - ref) - total); }
+  __device__ __forceinline__ Beam shfl(int from) const {
+    return {__shfl_sync(kAll, total, from), __shfl_sync(kAll, ref, from), __shfl_sync(kAll, score, from)};
+  }
+};
+// The sum of exp(x - most) of a row, for logits that are too far from 0 for the others'
+// way.  Slow, and rare: such logits are masks of the type's lowest value without any
+// other, or mistakes.
 template <typename T>
-__device__ __forceinline__ uint64_t best_tokens(const Args& g, const T* row, uint64_t words, uint64_t* queue, int lane) {
-  constexpr int N = Elem<T>::N, kEach = 32 / N;  // words that a warp looks at together
-  const int B = g.s.beams;
-  // each of the words has a token that is no smaller than the last one's
-  const uint64_t last = __shfl_sync(kAll, words, B - 1);
-  Best best{0, kNoKey, 0, queue, B, lane};
-  if (last > kNoKey) best.raise((last >> 32 << 32) - 1);
-  float x[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint64_t word = __shfl_sync(kAll, words, i * kEach + lane / N);
-    const int token = place_of(word) * N + lane % N;
-    x[i] = -INFINITY;
-    if (i * kEach + lane / N < B && word > kNoKey && token < g.s.vocab) x[i] = Elem<T>::one(row + token);
+__device__ __noinline__ uint64_t far_sum(const T* row, int V, float most, int lane) {
+  uint64_t sum = 0;
+  for (int64_t i = lane; i < V; i += 32) {
+    const float d = Elem<T>::one(row + i) - most;
+    sum += __float2ull_rn((d < -100.0f ? 0.0f : pskv::ex2(d * kLog2e)) * 0x1p32f);
   }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (i * kEach >= B) break;
-    const int token = place_of(__shfl_sync(kAll, words, i * kEach + lane / N)) * N + lane % N;
-    const uint64_t key = key_of(x[i], token);
-    best.add(key, key > best.floor && !ends(g.s, token));
-  }
-  while (best.queued > 0) best.flush();
-  return best.list;
+  return warp_sum(sum);
 }
 
-struct Joined {
-  uint64_t keys[PS_BEAM_MAX_BEAMS][32];  // the beams' best tokens
-  uint64_t sum[PS_BEAM_MAX_BEAMS];       // of 2^-32 exp(x - ref), 0: no candidates
-  double total[PS_BEAM_MAX_BEAMS];       // its logarithm
-  float score[PS_BEAM_MAX_BEAMS], ref[PS_BEAM_MAX_BEAMS];
-  Cand lists[kWarps][32];
-  Cand best[32];
-  // The reference, which may be far from 0, is subtracted first.
-  __device__ __forceinline__ double of(int b, float logit) const {
-    return (double)score[b] + (((double)logit - (double)ref[b]) - total[b]);
-  }
-};
-struct Shared {
-  uint64_t queue[kWarps][kQueue];
-  union {
-    struct {
-      uint4 ring[kWarps][kStages * kSlot];
-      uint64_t lists[kWarps][32];
-    } scan;
-    Joined joined;
-  };
-  uint64_t sums[kWarps];
-  float refs[kWarps];
-  int bad[kWarps];
-  bool last;
-};
-
-// The request's outputs, by the threads of its last CTA.
-template <typename T>
-__device__ __forceinline__ void finish(const Args& g, int r, uint64_t (*queue)[kQueue], Joined& s) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams, S = g.parts, E = g.s.num_end;
-  const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
-  for (int b = warp; b < B; b += kWarps) {  // the beams' sums, a part a lane
-    const int64_t row = (int64_t)r * B + b;
-    const float c = g.a.scores[row];
-    Part p{0, -INFINITY, 0};
-    if (lane < S && c - c == 0) {
-      const uint4 q = __ldcg(reinterpret_cast<const uint4*>(g.s.parts + row * S + lane));
-      p = Part{(uint64_t)q.y << 32 | q.x, __uint_as_float(q.z), (int32_t)q.w};
+// The 'keep' greatest of n numbers: up to kOneByOne to keep, of any order, and else of
+// sorted lists of 'keep'.
+__device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int keep, int lane) {
+  uint64_t list = 0;
+  if (keep <= kOneByOne) {
+    for (int i = lane; i - lane < n; i += 64)
+      list = i == lane ? greatest_of(i < n ? keys[i] : 0, i + 32 < n ? keys[i + 32] : 0, keep, lane)
+                       : greatest_of(list, greatest_of(i < n ? keys[i] : 0, i + 32 < n ? keys[i + 32] : 0, keep, lane), keep, lane);
+  } else {
+    uint64_t key = lane < keep ? keys[lane] : 0;
+    for (int i = keep; i <= n; i += keep) {
+      const uint64_t next = lane < keep && i < n ? keys[i + lane] : 0;
+      list = i == keep ? key : merge32(list, key, lane);
+      key = next;
     }
-    const float ref = warp_max(p.ref);
-    const bool bad = __any_sync(kAll, p.bad) || (c != -INFINITY && !(c - c == 0));
-    if (p.ref < ref) p.sum = p.ref == -INFINITY ? 0 : __double2ull_rn((double)p.sum * (double)exp_of(p.ref - ref));
-    const uint64_t sum = warp_sum(p.sum);
+  }
+  return list;
+}
+
+// A CTA a request.  Its warps put a beam's parts together each; then the threads rank
+// the beams' best runs, and the tokens in the best of those, by counting what comes
+// before them.
+constexpr int kRanked = 16;  // up to so many beams: of more, the runs are merged
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_constant__ Args g) {
+  constexpr int N = Elem<T>::N, kTokens = kVecs * N;  // of a run
+  constexpr int kMost = PS_BEAM_MAX_BEAMS;
+  __shared__ Beam s_beam[kMost];
+  __shared__ Cand s_run[kRanked * kRanked], s_best[kMost], s_token[kMost * 32], s_chosen[kMost], s_end[kMost * PS_BEAM_MAX_END];
+  __shared__ int s_tokens, s_runs, s_ended;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, B = g.s.beams, r = blockIdx.x;
+  const int E = g.a.ended_tokens ? g.s.num_end : 0;
+  const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
+  if (t == 0) s_tokens = s_runs = s_ended = 0;
+  if (t < kMost) s_best[t] = s_chosen[t] = nobody(t);
+  for (int i = t; i < kRanked * kRanked; i += kJoinThreads) s_run[i] = nobody(i);
+  __syncthreads();
+  chain();
+  Cand mine = nobody(lane);
+  for (int b = warp; b < B; b += kJoinWarps) {
+    const int row = r * B + b;
+    const float c = g.a.scores[row];
+    Beam beam{INFINITY, 0.0, c};  // no candidates
+    uint64_t list = 0;
+    bool bad = c != -INFINITY && !(c - c == 0);
+    if (c - c == 0) {
+      Part p{0, -INFINITY, 0};
+      if (lane < g.parts) p = g.s.parts[(int64_t)row * g.parts + lane];
+      list = best_runs(g.s.keys + (int64_t)row * g.slots * B, g.s.lists[row] * B, B, lane);
+      const float most = warp_max(p.most), R = exponent_of(most), down = R - exponent_of(p.most);
+      uint64_t sum = warp_sum(down < 64.0f ? p.sum >> (int)down : 0);
+      bad = __any_sync(kAll, p.bad);
+      beam.ref = (double)R * (1.0 / (double)kLog2e);
+      if (fabsf(most) > kFar && most > -INFINITY && !bad) {
+        sum = far_sum(logits + b * g.a.beam_stride, g.s.vocab, most, lane);
+        beam.ref = most;
+      }
+      if (!bad && most > -INFINITY) beam.total = log_of(sum);
+    }
     if (lane == 0) {
       if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
-      s.score[b] = c;
-      s.ref[b] = ref;
-      s.sum[b] = bad ? 0 : sum;  // 0: no token may follow
+      s_beam[b] = beam;
+    }
+    const bool on = beam.total < INFINITY && lane < B && list > kNoKey;
+    const Cand x = on ? cand(beam.of(logit_of(list)), (long long)b << 32 | (uint32_t)place_of(list)) : nobody(lane);
+    if (B <= kRanked) {
+      if (on) s_run[b * B + lane] = x;
+    } else {
+      mine = b < kJoinWarps ? x : merge32(mine, x, lane);
     }
   }
+  if (B > kRanked) s_token[t] = mine;
   __syncthreads();
-  if (threadIdx.x < B && s.sum[threadIdx.x] != 0) s.total[threadIdx.x] = log_of(s.sum[threadIdx.x]);
-  __syncthreads();
-  Cand mine = nobody(lane);
-  for (int b = warp; b < B; b += kWarps) {
-    if (s.sum[b] == 0) continue;
-    const uint64_t* keys = g.s.keys + ((int64_t)r * B + b) * S * B + lane;
-    uint64_t list = lane < B ? __ldcg(keys) : 0;
-    for (int i = 1; i < S; i += 4) {
-      uint64_t k[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) k[u] = lane < B && i + u < S ? __ldcg(keys + (i + u) * B) : 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i + u < S) list = merge32(list, k[u], lane);
+  // the best runs, and the end tokens' candidates
+  if (B <= kRanked) {
+    if (t < B * B) {
+      const Cand x = s_run[t];
+      int place = 0;
+      for (int i = 0; i < B * B; ++i) place += s_run[i].before(x);
+      if (x.somebody() && place < B) s_best[place] = x;
     }
-    list = best_tokens(g, logits + b * g.a.beam_stride, list, queue[warp], lane);
-    s.keys[b][lane] = list;
-    const Cand x = lane < B && list > kNoKey ? cand(s.of(b, logit_of(list)), b * 32 + lane) : nobody(lane);
-    mine = b < kWarps ? x : merge32(mine, x, lane);
+  } else if (warp == 0) {
+    for (int w = 1; w < kJoinWarps; ++w) mine = merge32(mine, s_token[w * 32 + lane], lane);
+    if (lane < B) s_best[lane] = mine;
   }
-  s.lists[warp][lane] = mine;
+  for (int i = t; i < B * E; i += kJoinThreads) {
+    const int b = i / E, token = g.s.end[i % E];
+    Cand x = nobody(i);
+    if (s_beam[b].total < INFINITY) {
+      const float l = Elem<T>::one(logits + b * g.a.beam_stride + token);
+      if (l > -INFINITY) x = cand(s_beam[b].of(l), (long long)b << 32 | token);
+    }
+    s_end[i] = x;
+  }
   __syncthreads();
-  const int64_t to = (int64_t)r * B + lane;
-  Cand last = nobody(lane);
-  if (warp == 0) {
-    for (int w = 1; w < kWarps && w < B; ++w) mine = merge32(mine, s.lists[w][lane], lane);
-    s.best[lane] = mine;
-    if (lane < B) {
-      const bool on = mine.at < kNobody;
-      g.a.tokens[to] = on ? place_of(s.keys[mine.at >> 5][mine.at & 31]) : -1;
-      g.a.parents[to] = on ? mine.at >> 5 : -1;
-      g.a.scores_out[to] = on ? mine.value() : -INFINITY;
-    }
-  } else if (warp == 1 && g.a.ended_tokens) {
-    // the end tokens' candidates, the 32 first: 'at' is beam 32 + the end token's
-    // number, and the numbers rise with the tokens
-    for (int i0 = 0; i0 < B * E; i0 += 32) {
-      const int i = i0 + lane, b = i / E;
-      Cand x = nobody(lane);
-      if (i < B * E && s.sum[b] != 0) {
-        const float l = Elem<T>::one(logits + b * g.a.beam_stride + g.s.end[i % E]);
-        if (l > -INFINITY) x = cand(s.of(b, l), b * 32 + i % E);
-      }
-      x = sort32(x, lane);
-      last = i0 ? merge32(last, x, lane) : x;
-    }
+  // the tokens of the best runs; each run has one that is no later than the last run's best
+  const Cand last = s_best[B - 1];
+  for (int i = t; i < B * kTokens; i += kJoinThreads) {
+    const Cand x = s_best[i / kTokens];
+    if (!x.somebody()) break;
+    const int b = (int)(x.tie >> 32);
+    const int64_t token = (x.tie & 0xFFFFFFFF) * kTokens + i % kTokens;
+    if (token >= g.s.vocab || ends(g.s, (int)token)) continue;
+    const float l = Elem<T>::one(logits + b * g.a.beam_stride + token);
+    const Cand y = cand(s_beam[b].of(l), (long long)b << 32 | token);
+    if (l > -INFINITY && (!last.somebody() || y.score >= last.score)) s_token[atomicAdd(&s_tokens, 1)] = y;
+  }
+  __syncthreads();
+  const int64_t to = (int64_t)r * B;
+  for (int i = t; i < s_tokens; i += kJoinThreads) {
+    const Cand x = s_token[i];
+    int place = 0;
+    for (int j = 0; j < s_tokens; ++j) place += s_token[j].before(x);
+    if (place < B) s_chosen[place] = x;
+  }
+  __syncthreads();
+  if (t < B) {
+    const Cand x = s_chosen[t];
+    const bool on = x.somebody();
+    g.a.tokens[to + t] = on ? (int)(x.tie & 0xFFFFFFFF) : -1;
+    g.a.parents[to + t] = on ? (int)(x.tie >> 32) : -1;
+    g.a.scores_out[to + t] = on ? x.value() : -INFINITY;
   }
   if (!g.a.ended_tokens) return;
-  __syncthreads();
-  if (warp != 1) return;
-  // its place among all candidates: those of its kind before it are the lanes below
-  int place = lane;
-  bool on = last.at < kNobody;
-  const int beam = last.at >> 5, token = on ? g.s.end[last.at & 31] : -1;
-  uint64_t key = 0;
-  if (on) key = key_of(Elem<T>::one(logits + beam * g.a.beam_stride + token), token);
-  for (int i = 0; i < B; ++i) {
-    const Cand x = s.best[i];
-    bool first = x.before(last);
-    if (x.score == last.score && x.at < kNobody && x.at >> 5 == beam) first = s.keys[beam][x.at & 31] > key;
-    place += first;
-  }
-  on = on && place < B;  // (places rise with the lanes)
-  if (lane < B) {
-    g.a.ended_tokens[to] = on ? token : -1;
-    g.a.ended_parents[to] = on ? beam : -1;
-    g.a.ended_scores[to] = on ? last.value() : -INFINITY;
-  }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(Args g) {
-  __shared__ __align__(16) Shared sh;
-  chain();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams;
-  const int64_t row = blockIdx.x / g.parts;
-  const int part = (int)(blockIdx.x % g.parts), r = (int)(row / B), b = (int)(row % B);
-  const float c = g.a.scores[row];
-  if (c - c == 0) {  // (a score that is not finite: nothing is read of the row)
-    Best best{0, kNoKey, 0, sh.queue[warp], B, lane};
-    Sum sum{-INFINITY, 0.0f};
-    float most = -INFINITY;
-    const T* from = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + b * g.a.beam_stride;
-    const Row<T> x{from, g.s.vocab, (int)(reinterpret_cast<uintptr_t>(from) & 15) / (int)sizeof(T), sh.scan.ring[warp], lane};
-    scan_part(g, x, part, best, sum, most);
-    // the lanes' and the warps' sums and lists
-    const float own = warp_max(sum.ref);
-    const bool bad = __any_sync(kAll, !(most < INFINITY));
-    sh.scan.lists[warp][lane] = best.list;
-    if (lane == 0) sh.refs[warp] = own, sh.bad[warp] = bad;
-    __syncthreads();
-    float ref = sh.refs[0];
-    int any = sh.bad[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) ref = fmaxf(ref, sh.refs[w]), any |= sh.bad[w];
-    const float scaled = sum.ref == -INFINITY ? 0.0f : sum.sum * exp_of(sum.ref - ref);
-    const uint64_t total = warp_sum(__float2ull_rn(scaled * 0x1p32f));
-    if (lane == 0) sh.sums[warp] = total;
-    static_assert(kWarps == 4, "two rounds");
-    if (warp < 2) best.list = merge32(best.list, sh.scan.lists[warp + 2][lane], lane);
-    if (warp == 1) sh.scan.lists[1][lane] = best.list;
-    __syncthreads();
-    if (warp == 0) {
-      const int64_t at = row * g.parts + part;
-      best.list = merge32(best.list, sh.scan.lists[1][lane], lane);
-      if (lane == 0) g.s.parts[at] = Part{sh.sums[0] + sh.sums[1] + sh.sums[2] + sh.sums[3], ref, any};
-      if (lane < B) g.s.keys[at * B + lane] = best.list;
+  // an end token's place among all candidates, and among those of its kind
+  for (int i = t; i < B * E; i += kJoinThreads) {
+    const Cand x = s_end[i];
+    if (!x.somebody()) continue;
+    int place = 0, others = 0;
+    for (int j = 0; j < B * E; ++j) place += s_end[j].before(x);
+    for (int j = 0; j < B; ++j) others += s_chosen[j].before(x);
+    if (place + others < B) {
+      g.a.ended_tokens[to + place] = (int)(x.tie & 0xFFFFFFFF);
+      g.a.ended_parents[to + place] = (int)(x.tie >> 32);
+      g.a.ended_scores[to + place] = x.value();
+      atomicAdd(&s_ended, 1);
     }
   }
-  // the last CTA of a request
-  __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) {
-    sh.last = atomicAdd(g.s.done + r, 1) == B * g.parts - 1;
-    if (sh.last) g.s.done[r] = 0;
+  if (t < B && t >= s_ended) {
+    g.a.ended_tokens[to + t] = g.a.ended_parents[to + t] = -1;
+    g.a.ended_scores[to + t] = -INFINITY;
   }
-  __syncthreads();
-  if (!sh.last) return;
-  __threadfence();
-  finish<T>(g, r, sh.queue, sh.joined);
 }
 
 }  // namespace
 
-int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, cudaStream_t st) {
-  Args g{a, s, status, 1};
-  const int64_t rows = (int64_t)a.num_requests * s.beams;
-  const int64_t chunk = kChunk * (s.dtype == PS_BEAM_F32 ? 4 : 8), chunks = (s.vocab + chunk - 1) / chunk;
-  int64_t parts = kSpreadCtas / rows;
-  const int64_t most = (chunks + kWarps * kLeastChunks - 1) / (kWarps * kLeastChunks);
-  parts = parts < most ? parts : most;
-  g.parts = (int32_t)(parts < 1 ? 1 : (parts > kMaxParts ? kMaxParts : parts));
-  const dim3 grid((unsigned)(rows * g.parts));
+template <typename T>
+static int32_t launch_typed(const Args& g, int grid, cudaStream_t st) {
+  cudaError_t e = launch(k_select<T>, dim3((unsigned)grid), kThreads, 0, st, g);
+  if (e == cudaSuccess) e = launch(k_select_join<T>, dim3((unsigned)g.a.num_requests), kJoinThreads, 0, st, g);
+  return status_of(e);
+}
+
+int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, int nsm, cudaStream_t st) {
+  Args g{};
+  g.a = a;
+  g.s = s;
+  g.status = status;
+  g.rows = (int64_t)a.num_requests * s.beams;
+  const int64_t chunk = kChunk * (s.dtype == PS_BEAM_F32 ? 4 : 8);
+  g.chunks = (int32_t)((s.vocab + chunk - 1) / chunk);
+  g.size = (g.chunks + kRowParts - 1) / kRowParts;
+  g.parts = (g.chunks + g.size - 1) / g.size;
+  static_assert(kWarps * kCtasPerSm <= kWarpsPerSm, "the workspace's");
+  const int64_t U = g.rows * g.parts, most = (int64_t)nsm * kCtasPerSm, want = (U + kWarps - 1) / kWarps;
+  const int64_t grid = want < most ? want : most, C = U < grid * kWarps ? U : grid * kWarps;
+  // where every part has a warp there is nothing to gain
+  g.compact = U > C && g.rows <= 32 * kRowWords;
+  const int64_t slots = g.compact ? g.parts : g.parts / (U / C) + 2;
+  g.slots = (int32_t)(slots < g.parts ? slots : g.parts);
   switch (s.dtype) {
-    case PS_BEAM_BF16: return status_of(launch(k_select<__nv_bfloat16>, grid, kThreads, 0, st, g));
-    case PS_BEAM_F16: return status_of(launch(k_select<__half>, grid, kThreads, 0, st, g));
-    default: return status_of(launch(k_select<float>, grid, kThreads, 0, st, g));
+    case PS_BEAM_BF16: return launch_typed<__nv_bfloat16>(g, (int)grid, st);
+    case PS_BEAM_F16: return launch_typed<__half>(g, (int)grid, st);
+    default: return launch_typed<float>(g, (int)grid, st);
   }
 }
 

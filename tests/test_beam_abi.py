@@ -78,11 +78,11 @@ def test_invalid_configurations_have_no_size(B, bad):
 def test_arguments_are_refused(B):
     L, bad = B.load(), B.PS_ERR_INVALID_ARG
     c, h, n = config(B), C.c_void_p(), size(B)
-    assert L.ps_beam_create(None, C.byref(c), 1 << 20, n, None) == bad
-    assert L.ps_beam_create(C.byref(h), None, 1 << 20, n, None) == bad
-    assert L.ps_beam_create(C.byref(h), C.byref(c), None, n, None) == bad
-    assert L.ps_beam_create(C.byref(h), C.byref(c), (1 << 20) + 16, n, None) == bad
-    assert L.ps_beam_create(C.byref(h), C.byref(c), 1 << 20, n - 1, None) == bad
+    assert L.ps_beam_create(None, C.byref(c), 1 << 20, n) == bad
+    assert L.ps_beam_create(C.byref(h), None, 1 << 20, n) == bad
+    assert L.ps_beam_create(C.byref(h), C.byref(c), None, n) == bad
+    assert L.ps_beam_create(C.byref(h), C.byref(c), (1 << 20) + 16, n) == bad
+    assert L.ps_beam_create(C.byref(h), C.byref(c), 1 << 20, n - 1) == bad
     assert L.ps_beam_select(None, None, C.byref(B.PsBeamSelect()), None) == bad
     assert L.ps_beam_trace(None, None, C.byref(B.PsBeamTrace()), None) == bad
     assert L.ps_kv_layout(None, None, C.byref(B.PsKvRows()), C.byref(B.PsKvLayout()), None) == bad
