@@ -36,6 +36,7 @@ struct Search {
   int32_t* lists;  // [rows] lists of a row
 };
 
+int32_t configure_select();  // of the current device
 int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_trace(const Search& s, const ps_beam_trace_t& a, int32_t* status, cudaStream_t st);
 

@@ -2,7 +2,7 @@
 //
 // Of a beam with score c and logits x, token v continues it with the score c + x_v
 // - lse, lse = log sum_u exp x_u.  Within a beam the order is the logits', and a
-// request's best are among its beams' best.  A row is read once, in runs of 64 bytes,
+// request's best are among its beams' best.  A row is read once, in runs of 128 bytes,
 // for two things: a sum of 2^((x - ref) log2 e), whose reference rises with the greatest
 // logit seen, and the 'beams' runs of the greatest logits.  The best tokens are in the
 // best runs: every run that comes before one of theirs (by its greatest logit, equal
@@ -11,16 +11,16 @@
 // Runs are kept as whole numbers, the logit's bits in order and then the complement of
 // the place, so that no two are equal.
 //
-// Bound by HBM.  k_select's resident warps divide the list of all rows' chunks of 2 KB
+// Bound by HBM.  k_select's resident warps divide the list of all rows' chunks of 4 KB
 // into equal shares.  Sums are kept for each of up to 32 parts of a row, always the
 // same, so that they do not depend on the shares: equal rows have equal sums.  Rows of
 // beams that are not there are left out of the list.  k_select_join puts the parts of
 // a request together, a CTA each.
 //
-// A warp reads 2 KB at a time through a ring in shared memory, three of them under way
+// A warp reads 4 KB at a time through a ring in shared memory, two of them under way
 // while it works on one, a run a lane.  What is greater than the beams-th of its best
 // enters a queue, 32 of which are looked through at a time.  A lower bound of that
-// beams-th is the beams-th of the lanes' greatest logits, taken after 1, 2, 4, ... chunks.
+// beams-th is the beams-th of the lanes' greatest logits, taken after 1, 4, 16, ... chunks.
 //
 // Neighbours in the order of scores may be nearer than 32 bits tell.  A term is 2^(x a -
 // R), a = log2 e rounded to 32 bits and R a whole number no less than any x a, so that a
@@ -33,11 +33,11 @@ namespace psbeam {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 5;
+constexpr int kCtasPerSm = 3;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
-constexpr int kVecs = 4;                 // 16-byte words of a run
+constexpr int kVecs = 8;                 // 16-byte words of a run
 constexpr int kChunk = 32 * kVecs;       // words of a chunk, a run a lane
-constexpr int kStages = 4;               // chunks of a warp's ring
+constexpr int kStages = 3;               // chunks of a warp's ring
 constexpr float kLog2e = 1.44269502f;    // 'a'
 constexpr double kLn2 = 0.693147180559945309;
 constexpr float kFar = 1e38f;            // logits whose a-fold may not be finite
@@ -201,15 +201,15 @@ __device__ __forceinline__ uint64_t greatest_of(uint64_t a, uint64_t b, int keep
   }
   return out;
 }
-// The keep-th of the lanes' numbers.
+// The keep-th of the lanes' numbers, or a little less: the five lowest bits are cleared.
 __device__ __forceinline__ uint32_t kth_of(uint32_t x, int keep, int lane) {
-  if (keep > kOneByOne) return __shfl_sync(kAll, sort32(x, lane), keep - 1);
+  x = (x & ~31u) | lane;  // no two are equal
   uint32_t top = 0;
   for (int k = 0; k < keep; ++k) {
     top = __reduce_max_sync(kAll, x);
-    if (lane == __ffs(__ballot_sync(kAll, x == top)) - 1) x = 0;
+    if (x == top) x = 0;
   }
-  return top;
+  return top & ~31u;
 }
 
 // A warp's best so far.
@@ -265,23 +265,17 @@ struct Sum {
   float R, sum;
   __device__ __forceinline__ void raise(float most) {
     const float to = exponent_of(most);
-    if (to > R) {
-      sum = R == -INFINITY ? 0.0f : sum * pskv::ex2(R - to);
-      R = to;
-    }
+    sum = R == -INFINITY ? 0.0f : sum * pskv::ex2(R - to);
+    R = to;
   }
   // What is subtracted: nothing while all are -infinity.
   __device__ __forceinline__ float base() const { return R == -INFINITY ? 0.0f : R; }
 };
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kAll, x, o));
-  return x;
-}
+__device__ __forceinline__ float warp_max(float x) { return unordered(__reduce_max_sync(kAll, ordered(x))); }
+// Of numbers below 2^53.
 __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kAll, x, o);
-  return x;
+  const uint32_t lo = __reduce_add_sync(kAll, (uint32_t)x & 0x3FFFFFFu), hi = __reduce_add_sync(kAll, (uint32_t)(x >> 26));
+  return ((uint64_t)hi << 26) + lo;
 }
 
 // ---- a part of a row ------------------------------------------------------------------
@@ -291,9 +285,9 @@ __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
 // one, a word is put together from two; elements of aligned words that are not the
 // row's are not read.
 constexpr int kSlot = kChunk + 1;  // with the word after the chunk's
-// Where word w of a chunk lies in its slot: lanes that read their runs' words, four words
+// Where word w of a chunk lies in its slot: lanes that read their runs' words, eight words
 // apart, and lanes that fill neighbouring ones meet no bank twice.
-__device__ __forceinline__ int place_in_slot(int w) { return w ^ (w >> 3 & 3); }
+__device__ __forceinline__ int place_in_slot(int w) { return w ^ (w >> 3 & 7); }
 
 template <typename T>
 __device__ __forceinline__ void fetch_word(uint4* to, const T* row, int shift, int w, int V) {
@@ -318,11 +312,11 @@ template <typename T>
 __device__ __forceinline__ void fetch_chunk(uint4* slot, const T* row, int shift, int c, int V, int lane) {
   constexpr int N = Elem<T>::N;
   if (c > 0 && (c + 1) * kChunk * N + N <= V) {  // all of it, and the word after it, is the row's
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + place_in_slot(lane) * 16;  // (32 words on the pattern is the same)
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
     const char* from = reinterpret_cast<const char*>(row - shift) + ((int64_t)c * kChunk + lane) * 16;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * j), "l"(from + 512 * j) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + place_in_slot(32 * j + lane) * 16), "l"(from + 512 * j) : "memory");
     if (shift != 0 && lane == 0)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * kVecs), "l"(from + 512 * kVecs) : "memory");
     return;
@@ -382,8 +376,8 @@ struct Scan {
   __device__ __forceinline__ void chunk(const Args& g, uint4 (&v)[kVecs], int c) {
     const int lane = best.lane;
     float all = Elem<T>::top(greatest<T>(v));
+    if (all > most) sum.raise(all);
     most = max_nan(most, all);
-    sum.raise(all);
     const float base = sum.base();
     const uint64_t minus = pskv::pack2(-base, -base), a = pskv::pack2(kLog2e, kLog2e);
     uint64_t s0 = 0, s1 = 0;
@@ -403,11 +397,11 @@ struct Scan {
     sum.sum += f.x + f.y;
     if (c >= end_chunk) {  // an end token is among these, or one lies behind: end tokens do not count
       const int w0 = c * kChunk + kVecs * lane;
-      unsigned out = 0;
+      uint64_t out = 0;
       end_chunk = 1 << 30;
       for (int i = 0; i < g.s.num_end; ++i) {
         const int word = g.s.end[i] / N, w = word - w0;
-        if (w >= 0 && w < kVecs) out |= 1u << (w * N + g.s.end[i] % N);
+        if (w >= 0 && w < kVecs) out |= 1ull << (w * N + g.s.end[i] % N);
         if (word / kChunk > c) end_chunk = min(end_chunk, word / kChunk);
       }
       if (out) {
@@ -424,7 +418,7 @@ struct Scan {
     }
     top = fmaxf(top, all);
     if (++seen == again) {  // so many runs are no smaller
-      again *= 2;
+      again *= 4;
       best.raise(((uint64_t)kth_of(ordered(top), best.keep, lane) << 32) - 1);
     }
     const uint64_t key = key_of(all, c * 32 + lane);
@@ -477,7 +471,8 @@ struct Shared {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(const __grid_constant__ Args g) {
-  __shared__ __align__(16) Shared sh;
+  extern __shared__ __align__(16) unsigned char smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
   chain();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.s.beams;
   int count = (int)g.rows;
@@ -653,14 +648,18 @@ __device__ __noinline__ uint64_t far_sum(const T* row, int V, float most, int la
   return warp_sum(sum);
 }
 
-// The 'keep' greatest of n numbers: up to kOneByOne to keep, of any order, and else of
-// sorted lists of 'keep'.
-__device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int keep, int lane) {
+// The 'keep' greatest of n numbers (read before n is known, where there are 'most'): up
+// to kOneByOne to keep, of any order, and else of sorted lists of 'keep'.
+__device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int most, int keep, int lane) {
   uint64_t list = 0;
   if (keep <= kOneByOne) {
-    for (int i = lane; i - lane < n; i += 64)
-      list = i == lane ? greatest_of(i < n ? keys[i] : 0, i + 32 < n ? keys[i + 32] : 0, keep, lane)
-                       : greatest_of(list, greatest_of(i < n ? keys[i] : 0, i + 32 < n ? keys[i + 32] : 0, keep, lane), keep, lane);
+    uint64_t a = lane < most ? keys[lane] : 0, b = lane + 32 < most ? keys[lane + 32] : 0;
+    for (int i = lane; i - lane < n; i += 64) {
+      const uint64_t c = i + 64 < n ? keys[i + 64] : 0, d = i + 96 < n ? keys[i + 96] : 0;
+      a = greatest_of(i < n ? a : 0, i + 32 < n ? b : 0, keep, lane);
+      list = i == lane ? a : greatest_of(list, a, keep, lane);
+      a = c, b = d;
+    }
   } else {
     uint64_t key = lane < keep ? keys[lane] : 0;
     for (int i = keep; i <= n; i += keep) {
@@ -681,7 +680,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
   constexpr int N = Elem<T>::N, kTokens = kVecs * N;  // of a run
   constexpr int kMost = PS_BEAM_MAX_BEAMS;
   __shared__ Beam s_beam[kMost];
-  __shared__ Cand s_run[kRanked * kRanked], s_best[kMost], s_token[kMost * 32], s_chosen[kMost], s_end[kMost * PS_BEAM_MAX_END];
+  __shared__ Cand s_run[kRanked * kRanked], s_best[kMost], s_token[kMost * kTokens], s_chosen[kMost], s_end[kMost * PS_BEAM_MAX_END];
   __shared__ int s_tokens, s_runs, s_ended;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, B = g.s.beams, r = blockIdx.x;
   const int E = g.a.ended_tokens ? g.s.num_end : 0;
@@ -691,6 +690,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
   for (int i = t; i < kRanked * kRanked; i += kJoinThreads) s_run[i] = nobody(i);
   __syncthreads();
   chain();
+  // the end tokens' logits, on their way early
+  static_assert(kMost * PS_BEAM_MAX_END == kJoinThreads, "one a thread");
+  const int end_beam = E > 0 ? t / E : kMost, end_token = E > 0 ? g.s.end[t % E] : 0;
+  float end_logit = -INFINITY;
+  if (end_beam < B) end_logit = Elem<T>::one(logits + end_beam * g.a.beam_stride + end_token);
   Cand mine = nobody(lane);
   for (int b = warp; b < B; b += kJoinWarps) {
     const int row = r * B + b;
@@ -701,7 +705,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
     if (c - c == 0) {
       Part p{0, -INFINITY, 0};
       if (lane < g.parts) p = g.s.parts[(int64_t)row * g.parts + lane];
-      list = best_runs(g.s.keys + (int64_t)row * g.slots * B, g.s.lists[row] * B, B, lane);
+      list = best_runs(g.s.keys + (int64_t)row * g.slots * B, g.s.lists[row] * B, g.slots * B, B, lane);
       const float most = warp_max(p.most), R = exponent_of(most), down = R - exponent_of(p.most);
       uint64_t sum = warp_sum(down < 64.0f ? p.sum >> (int)down : 0);
       bad = __any_sync(kAll, p.bad);
@@ -731,6 +735,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
     if (t < B * B) {
       const Cand x = s_run[t];
       int place = 0;
+      #pragma unroll 8
       for (int i = 0; i < B * B; ++i) place += s_run[i].before(x);
       if (x.somebody() && place < B) s_best[place] = x;
     }
@@ -738,15 +743,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
     for (int w = 1; w < kJoinWarps; ++w) mine = merge32(mine, s_token[w * 32 + lane], lane);
     if (lane < B) s_best[lane] = mine;
   }
-  for (int i = t; i < B * E; i += kJoinThreads) {
-    const int b = i / E, token = g.s.end[i % E];
-    Cand x = nobody(i);
-    if (s_beam[b].total < INFINITY) {
-      const float l = Elem<T>::one(logits + b * g.a.beam_stride + token);
-      if (l > -INFINITY) x = cand(s_beam[b].of(l), (long long)b << 32 | token);
-    }
-    s_end[i] = x;
-  }
+  if (end_beam < B)
+    s_end[t] = s_beam[end_beam].total < INFINITY && end_logit > -INFINITY
+                   ? cand(s_beam[end_beam].of(end_logit), (long long)end_beam << 32 | end_token) : nobody(t);
   __syncthreads();
   // the tokens of the best runs; each run has one that is no later than the last run's best
   const Cand last = s_best[B - 1];
@@ -802,8 +801,26 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
 
 template <typename T>
 static int32_t launch_typed(const Args& g, int grid, cudaStream_t st) {
-  cudaError_t e = launch(k_select<T>, dim3((unsigned)grid), kThreads, 0, st, g);
+  cudaError_t e = launch(k_select<T>, dim3((unsigned)grid), kThreads, sizeof(Shared), st, g);
   if (e == cudaSuccess) e = launch(k_select_join<T>, dim3((unsigned)g.a.num_requests), kJoinThreads, 0, st, g);
+  return status_of(e);
+}
+
+// Both kernels prefer all of an SM's memory as shared memory: where two that run after
+// one another prefer different divisions, an SM has to run empty in between, and the
+// CTAs that find no room meanwhile begin when others end.
+template <typename T>
+static cudaError_t configure_typed() {
+  cudaError_t e = cudaFuncSetAttribute(k_select<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_select<T>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(k_select_join<T>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  return e;
+}
+int32_t configure_select() {
+  cudaError_t e = configure_typed<__nv_bfloat16>();
+  if (e == cudaSuccess) e = configure_typed<__half>();
+  if (e == cudaSuccess) e = configure_typed<float>();
   return status_of(e);
 }
 
