@@ -33,7 +33,10 @@ namespace psbeam {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 3;
+// Twelve warps an SM, of which none waits long for another (with 16 or 20 the last ones
+// ended 10 us behind the others), and registers for as many again, so that the next
+// kernel's CTAs have room beside them: 59 us as it stands, 61 and 65 with more warps.
+constexpr int kCtasPerSm = 3, kRoom = 4;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr int kVecs = 8;                 // 16-byte words of a run
 constexpr int kChunk = 32 * kVecs;       // words of a chunk, a run a lane
@@ -470,7 +473,7 @@ struct Shared {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_select(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kThreads, kRoom) k_select(const __grid_constant__ Args g) {
   extern __shared__ __align__(16) unsigned char smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   chain();
@@ -661,11 +664,11 @@ __device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int m
       a = c, b = d;
     }
   } else {
-    uint64_t key = lane < keep ? keys[lane] : 0;
+    uint64_t k = lane < keep ? keys[lane] : 0;
     for (int i = keep; i <= n; i += keep) {
       const uint64_t next = lane < keep && i < n ? keys[i + lane] : 0;
-      list = i == keep ? key : merge32(list, key, lane);
-      key = next;
+      list = i == keep ? k : merge32(list, k, lane);
+      k = next;
     }
   }
   return list;
@@ -676,23 +679,25 @@ __device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int m
 // before them.
 constexpr int kRanked = 16;  // up to so many beams: of more, the runs are merged
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_constant__ Args g) {
   constexpr int N = Elem<T>::N, kTokens = kVecs * N;  // of a run
   constexpr int kMost = PS_BEAM_MAX_BEAMS;
   __shared__ Beam s_beam[kMost];
   __shared__ Cand s_run[kRanked * kRanked], s_best[kMost], s_token[kMost * kTokens], s_chosen[kMost], s_end[kMost * PS_BEAM_MAX_END];
-  __shared__ int s_tokens, s_runs, s_ended;
+  __shared__ int s_tokens, s_ended;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, B = g.s.beams, r = blockIdx.x;
   const int E = g.a.ended_tokens ? g.s.num_end : 0;
   const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
-  if (t == 0) s_tokens = s_runs = s_ended = 0;
+  const int64_t to = (int64_t)r * B;
+  static_assert(kMost * PS_BEAM_MAX_END == kJoinThreads, "an end token's candidate a thread");
+  const int end_beam = E > 0 ? t / E : kMost, end_token = E > 0 ? g.s.end[t % E] : 0;
+  if (t == 0) s_tokens = s_ended = 0;
   if (t < kMost) s_best[t] = s_chosen[t] = nobody(t);
-  for (int i = t; i < kRanked * kRanked; i += kJoinThreads) s_run[i] = nobody(i);
+  s_run[t] = nobody(t);
+  static_assert(kRanked * kRanked == kJoinThreads, "one a thread");
   __syncthreads();
   chain();
   // the end tokens' logits, on their way early
-  static_assert(kMost * PS_BEAM_MAX_END == kJoinThreads, "one a thread");
-  const int end_beam = E > 0 ? t / E : kMost, end_token = E > 0 ? g.s.end[t % E] : 0;
   float end_logit = -INFINITY;
   if (end_beam < B) end_logit = Elem<T>::one(logits + end_beam * g.a.beam_stride + end_token);
   Cand mine = nobody(lane);
@@ -735,7 +740,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
     if (t < B * B) {
       const Cand x = s_run[t];
       int place = 0;
-      #pragma unroll 8
+#pragma unroll 8
       for (int i = 0; i < B * B; ++i) place += s_run[i].before(x);
       if (x.somebody() && place < B) s_best[place] = x;
     }
@@ -760,7 +765,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
     if (l > -INFINITY && (!last.somebody() || y.score >= last.score)) s_token[atomicAdd(&s_tokens, 1)] = y;
   }
   __syncthreads();
-  const int64_t to = (int64_t)r * B;
   for (int i = t; i < s_tokens; i += kJoinThreads) {
     const Cand x = s_token[i];
     int place = 0;
@@ -777,17 +781,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_select_join(const __grid_const
   }
   if (!g.a.ended_tokens) return;
   // an end token's place among all candidates, and among those of its kind
-  for (int i = t; i < B * E; i += kJoinThreads) {
-    const Cand x = s_end[i];
-    if (!x.somebody()) continue;
+  if (end_beam < B) {
+    const Cand x = s_end[t];
     int place = 0, others = 0;
     for (int j = 0; j < B * E; ++j) place += s_end[j].before(x);
     for (int j = 0; j < B; ++j) others += s_chosen[j].before(x);
-    if (place + others < B) {
+    if (x.somebody() && place + others < B) {
+      atomicAdd(&s_ended, 1);
       g.a.ended_tokens[to + place] = (int)(x.tie & 0xFFFFFFFF);
       g.a.ended_parents[to + place] = (int)(x.tie >> 32);
       g.a.ended_scores[to + place] = x.value();
-      atomicAdd(&s_ended, 1);
     }
   }
   __syncthreads();
