@@ -36,7 +36,9 @@ struct Search {
   int32_t* lists;  // [rows] lists of a row
 };
 
-int32_t configure_select();  // of the current device
+// Attributes of the kernels, for the current device.
+int32_t configure_select();
+int32_t configure_trace();
 int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* status, int nsm, cudaStream_t st);
 int32_t launch_trace(const Search& s, const ps_beam_trace_t& a, int32_t* status, cudaStream_t st);
 

@@ -69,7 +69,8 @@ int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_wor
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return PS_ERR_CUDA;
-  const int32_t rc = configure_select();
+  int32_t rc = configure_select();
+  if (rc == PS_OK) rc = configure_trace();
   if (rc != PS_OK) return rc;
   ps_beam* b = new (std::nothrow) ps_beam{};
   if (!b) return PS_ERR_CUDA;

@@ -1,125 +1,171 @@
 // ps_beam_trace: sequences of tokens, back through every step's parents.
 //
 // A hypothesis of L steps that ends in beam b: token L - 1 is tokens[L - 1][b], then
-// b <- parents[t][b] from t = L - 1 down to 1.  A chain of dependent lookups, cut into
-// segments of 32 steps, one a warp: the warp holds the segment's parents and tokens a
-// beam a lane, 32 registers of each, so that a lookup is a shuffle.  It first takes
-// every beam at the segment's end to its ancestor before the segment, and so does it
-// with the hypotheses that end inside; then a walk over the segments gives the beam in
-// which each hypothesis enters each segment, and the warps go through their segments
-// once more, for the tokens.  A CTA takes a request's last 16 segments at once, then
-// those before them.
+// b <- parents[t][b] from t = L - 1 down to 1.  A chain of dependent lookups, so the
+// steps are cut into segments and a CTA takes a request's segments at once, its parents
+// as bytes in shared memory.  First every beam at a segment's end is taken to its
+// ancestor before the segment, and every hypothesis to that of the segment in which it
+// ends; then a thread a hypothesis goes from segment to segment; then the segments are
+// gone through once more, from the beams that that gave, and the tokens are picked from
+// shared memory, where copies brought them meanwhile (gathered from global memory they
+// took as long as all the rest: a sector a lane).  With segments of 32 steps 2047 steps
+// are 128 lookups one after another.  What does not fit into shared memory is done in
+// rounds, from the last steps on.
 #include "ps_beam.cuh"
 
 namespace psbeam {
 namespace {
 
-constexpr int kSteps = 32, kSegs = 16, kThreads = 32 * kSegs;
-constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kHyps = 64;          // of a CTA at most
+constexpr int kBytes = 206 << 10;  // of tokens, parents and paths
+constexpr int kNone = 255;         // no beam
 
 struct Args {
   ps_beam_trace_t a;
   int32_t* status;
-  int32_t beams;
+  int32_t beams, hyps, steps, seg;  // hypotheses of a CTA, steps of a round and of a segment
+  int32_t stride;                   // tokens of a step in shared memory: lanes of neighbouring steps meet at most four times at a bank
+  bool words;                       // a step's beams are whole 16-byte words
 };
 
-// A beam that is not there: past an end, or a parent out of range.
-constexpr int kNone = -1;
-__device__ __forceinline__ int look(int mine, int beam) {
-  const int x = __shfl_sync(kAll, mine, beam & 31);
-  return beam < 0 ? kNone : x;
-}
-
-// blockIdx.x: the request; blockIdx.y: 32 of its hypotheses, one a lane.
-__global__ void __launch_bounds__(kThreads, 1) k_trace(Args g) {
-  __shared__ int ancestor[kSegs][32];  // of each beam at a segment's end
-  __shared__ int inside[kSegs][32];    // of the hypotheses that end in the segment
-  chain();
+// blockIdx.x: the request; blockIdx.y: 'hyps' of its hypotheses.
+__global__ void __launch_bounds__(kThreads) k_trace(const __grid_constant__ Args g) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int s_len[kHyps];
+  __shared__ unsigned char s_last[kHyps], s_enter[kHyps], s_first[kHyps];
   const ps_beam_trace_t& a = g.a;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = g.beams, T = a.num_steps;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = g.beams, T = a.num_steps, seg = g.seg;
   const int64_t r = blockIdx.x, R = a.num_requests;
-  const int h = blockIdx.y * 32 + lane;
-  const bool on = h < a.hyps;
-  const int64_t at = r * a.hyps + h;
-  int L = 0, last = kNone;
-  if (on) {
-    L = a.lengths ? a.lengths[at] : T;
-    last = a.beams_of[at];
-    if (L < 0 || L > T || last < -1 || last >= B) {
-      if (warp == 0) set_error(g.status, PS_ERR_INVALID_ARG);
-      last = kNone;
+  const int h0 = blockIdx.y * g.hyps, H = min(g.hyps, a.hyps - h0);
+  int32_t* const token = reinterpret_cast<int32_t*>(smem);       // [steps][stride]
+  unsigned char* const parent = smem + (size_t)g.steps * g.stride * 4;  // [steps][B]
+  unsigned char* const path = parent + g.steps * B;              // [H][steps]
+  unsigned char* const map = path + g.steps * g.hyps;            // [segments][B]
+  unsigned char* const entry = map + (g.steps / seg + 1) * B;    // [segments][H]
+  chain();
+  bool bad = false;
+  if (tid < H) {
+    const int64_t at = r * a.hyps + h0 + tid;
+    int len = a.lengths ? a.lengths[at] : T, last = a.beams_of[at];
+    if (len < 0 || len > T || last < -1 || last >= B) {
+      bad = true;
+      last = -1;
     }
-    if (last < 0) L = 0;
+    s_len[tid] = last < 0 ? 0 : len;
+    s_last[tid] = (unsigned char)(last < 0 ? kNone : last);
+    s_enter[tid] = kNone;
   }
-  int entry = kNone;  // the beam at the step before the segments that were done
-  const int segs = (T + kSteps - 1) / kSteps;
-  for (int s1 = segs; s1 > 0; s1 -= kSegs) {
-    const int seg = s1 - kSegs + warp;  // warp 0 the first of these
-    const int t0 = seg * kSteps;
-    int parent[kSteps], token[kSteps];
-    bool bad = false;
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int t = t0 + j;
-      parent[j] = kNone;
-      token[j] = -1;
-      if (t >= 0 && t < T && lane < B) {
-        const int64_t i = (t * R + r) * B + lane;
-        parent[j] = a.parents[i];
-        token[j] = a.tokens[i];
-      }
-    }
-    int beam = lane < B ? lane : kNone, own = kNone;
-    // parents that lead out of range: noticed where a hypothesis meets one, below
-#pragma unroll
-    for (int j = kSteps - 1; j >= 0; --j) {
-      const int t = t0 + j;
-      if (parent[j] < -1 || parent[j] >= B) parent[j] = -2;
-      if (t < T && t > 0) {
-        beam = look(parent[j], beam);
-        if (t == L - 1) own = last;
-        own = look(parent[j], own);
-      } else if (t == 0 && t == L - 1) {
-        own = last;
-      }
-    }
-    ancestor[warp][lane] = beam;
-    inside[warp][lane] = own;
+  for (int t1 = T; t1 > 0;) {
+    const int t0 = t1 > g.steps ? t1 - g.steps : 0, n = t1 - t0, segs = (n + seg - 1) / seg;
+    const int64_t from = ((int64_t)t0 * R + r) * B;
     __syncthreads();
-    // the beam at this warp's last step: from the segments after it
-    int cur = entry;
-    for (int w = kSegs - 1; w >= 0; --w) {
-      const int end = (s1 - kSegs + w + 1) * kSteps;  // of segment w
-      if (w == warp) {
-        int b = cur;
-#pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) {
-          const int t = t0 + j;
-          if (t == L - 1) b = last;
-          const int tok = look(token[j], b);
-          const int up = look(parent[j], b);
-          if (on && t >= 0 && t < T) {
-            a.out[at * T + t] = t < L && b >= 0 ? tok : -1;
-            if (t < L && t > 0 && b >= 0 && up < 0) bad = true;
-          }
-          if (t > 0 && t < T) b = up;
+    // the parents, and the tokens on their way
+    auto byte = [&](int p) { return (uint32_t)(p >= 0 && p < B ? p : kNone); };
+    if (g.words) {
+      const int each = B / 4;
+#pragma unroll 4
+      for (int i = tid; i < n * each; i += kThreads) {
+        const int t = i / each, w = i - t * each;
+        const int64_t at = from + (int64_t)t * R * B + 4 * w;
+        const int4 p = *reinterpret_cast<const int4*>(a.parents + at);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(token + t * g.stride + 4 * w)),
+                     "l"(a.tokens + at) : "memory");
+        reinterpret_cast<uint32_t*>(parent)[i] = byte(p.x) | byte(p.y) << 8 | byte(p.z) << 16 | byte(p.w) << 24;
+      }
+    } else {
+#pragma unroll 4
+      for (int i = tid; i < n * B; i += kThreads) {
+        const int t = i / B, b = i - t * B;
+        const int64_t at = from + (int64_t)t * R * B + b;
+        const int p = a.parents[at];
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(token + t * g.stride + b)),
+                     "l"(a.tokens + at) : "memory");
+        parent[i] = (unsigned char)byte(p);
+      }
+    }
+    __syncthreads();
+    // From beam 'b' at step t0 + t to the one before the steps from 'down' on.
+    auto back = [&](int b, int t, int down) {
+      for (; t >= down && b != kNone; --t) {
+        if (t0 + t == 0) return kNone;
+        b = parent[t * B + b];
+      }
+      return b;
+    };
+    for (int i = tid; i < segs * B; i += kThreads) {
+      const int s = i / B, b = i - s * B;
+      map[i] = (unsigned char)back(b, min(n, (s + 1) * seg) - 1, s * seg);
+    }
+    const int of = kThreads - 1 - tid;  // (the threads that have no part in the maps, where there are few)
+    if (of < H) {
+      const int end = s_len[of] - 1 - t0;
+      if (end >= 0 && end < n) s_first[of] = (unsigned char)back(s_last[of], end, end / seg * seg);
+    }
+    __syncthreads();
+    if (tid < H) {
+      const int end = s_len[tid] - 1 - t0;
+      int cur = s_enter[tid], s = segs - 1;
+      if (end < n) {  // it ends here, or before
+        cur = end >= 0 ? s_first[tid] : kNone;
+        s = end >= 0 ? end / seg - 1 : -1;
+      }
+      for (; s >= 0; --s) {
+        entry[s * H + tid] = (unsigned char)cur;
+        if (cur != kNone) cur = map[s * B + cur];
+      }
+      s_enter[tid] = (unsigned char)cur;
+    }
+    __syncthreads();
+    for (int i = tid; i < segs * H; i += kThreads) {
+      const int s = i / H, h = i - s * H, down = s * seg, end = s_len[h] - 1 - t0;
+      int t = min(n, down + seg) - 1, b = kNone;
+      if (end > t) b = entry[i];
+      for (; t >= down; --t) {
+        if (t == end) b = s_last[h];
+        path[h * n + t] = (unsigned char)b;
+        if (b != kNone && t0 + t > 0) {
+          b = parent[t * B + b];
+          bad = bad || b == kNone;
         }
       }
-      // and on to the segment before it
-      if (L >= end + 1) cur = cur < 0 ? cur : ancestor[w][cur];
-      else if (L > end - kSteps) cur = inside[w][lane];
     }
-    if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
-    entry = cur;
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
+    const int blocks = (n + 31) / 32;
+#pragma unroll 4
+    for (int i = warp; i < blocks * H; i += kWarps) {
+      const int h = i / blocks, t = (i - h * blocks) * 32 + lane;
+      if (t < n) {
+        const int b = path[h * n + t];
+        a.out[(r * a.hyps + h0 + h) * T + t0 + t] = b == kNone ? -1 : token[t * g.stride + b];
+      }
+    }
+    t1 = t0;
   }
+  if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
 }
 
 }  // namespace
 
+int32_t configure_trace() {
+  return status_of(cudaFuncSetAttribute(k_trace, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes + (8 << 10)));
+}
+
 int32_t launch_trace(const Search& s, const ps_beam_trace_t& a, int32_t* status, cudaStream_t st) {
-  const Args g{a, status, s.beams};
-  return status_of(launch(k_trace, dim3((unsigned)a.num_requests, (unsigned)((a.hyps + 31) / 32)), kThreads, 0, st, g));
+  Args g{};
+  g.a = a;
+  g.status = status;
+  g.beams = s.beams;
+  g.hyps = a.hyps < kHyps ? a.hyps : kHyps;
+  // segments of about the root of the steps: a third of the lookups each
+  g.seg = a.num_steps <= 128 ? 8 : (a.num_steps <= 512 ? 16 : 32);
+  g.words = s.beams % 4 == 0 && ((reinterpret_cast<uintptr_t>(a.parents) | reinterpret_cast<uintptr_t>(a.tokens)) & 15) == 0;
+  g.stride = !g.words ? s.beams | 1 : s.beams + (s.beams % 8 == 0 ? 4 : 0);
+  const int each = 4 * g.stride + s.beams + g.hyps, most = kBytes / each / g.seg * g.seg;
+  g.steps = a.num_steps < most ? (a.num_steps + g.seg - 1) / g.seg * g.seg : most;
+  const size_t smem = (size_t)g.steps * each + (size_t)(g.steps / g.seg + 1) * (s.beams + g.hyps);
+  return status_of(launch(k_trace, dim3((unsigned)a.num_requests, (unsigned)((a.hyps + g.hyps - 1) / g.hyps)), kThreads, smem, st, g));
 }
 
 }  // namespace psbeam
