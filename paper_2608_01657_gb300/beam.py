@@ -31,6 +31,11 @@ class Selection(NamedTuple):
     ended_scores: Optional[torch.Tensor]   # float32
 
 
+class _MadeSelection(Selection):
+    """A selection that ``BeamSearch.select`` made: ``made`` has the search, the requests
+    and the addresses, so that they are checked once.  (``_replace`` makes one without.)"""
+
+
 class BeamSearch(Handle):
     """Beam searches on the current CUDA device: at most ``max_requests`` requests
     of ``beams`` beams each, over logits of ``vocab`` tokens in ``dtype`` (bfloat16,
@@ -83,18 +88,23 @@ class BeamSearch(Handle):
             raise ValueError(f"logits must be {self.dtype} [requests, {self.beams}, {self.vocab}] on {self.device}, rows contiguous")
         R = logits.shape[0]
         shape, i32, f32 = (R, self.beams), torch.int32, torch.float32
+        a.logits = logits.data_ptr()
+        a.request_stride, a.beam_stride, _ = logits.stride()
+        a.scores = self._of(scores, f32, shape, "scores")
         if out is None:
             made = lambda dtype: B._made(shape, dtype, self.device, stream)  # noqa: E731
-            out = Selection(made(i32), made(i32), made(f32), *((made(i32), made(i32), made(f32)) if ended else (None, None, None)))
-        a.logits = logits.data_ptr()
-        a.request_stride, a.beam_stride = logits.stride(0), logits.stride(1)
-        a.scores = self._of(scores, f32, shape, "scores")
-        a.tokens = self._of(out.tokens, i32, shape, "out.tokens")
-        a.parents = self._of(out.parents, i32, shape, "out.parents")
-        a.scores_out = self._of(out.scores, f32, shape, "out.scores")
-        a.ended_tokens = None if out.ended_tokens is None else self._of(out.ended_tokens, i32, shape, "out.ended_tokens")
-        a.ended_parents = None if out.ended_parents is None else self._of(out.ended_parents, i32, shape, "out.ended_parents")
-        a.ended_scores = None if out.ended_scores is None else self._of(out.ended_scores, f32, shape, "out.ended_scores")
+            out = _MadeSelection(made(i32), made(i32), made(f32), *((made(i32), made(i32), made(f32)) if ended else (None, None, None)))
+            out.made = (self, R, *(0 if t is None else t.data_ptr() for t in out))
+        known = getattr(out, "made", None)
+        if known is not None and known[0] is self and known[1] == R:
+            a.tokens, a.parents, a.scores_out, a.ended_tokens, a.ended_parents, a.ended_scores = known[2:]
+        else:
+            a.tokens = self._of(out.tokens, i32, shape, "out.tokens")
+            a.parents = self._of(out.parents, i32, shape, "out.parents")
+            a.scores_out = self._of(out.scores, f32, shape, "out.scores")
+            a.ended_tokens = None if out.ended_tokens is None else self._of(out.ended_tokens, i32, shape, "out.ended_tokens")
+            a.ended_parents = None if out.ended_parents is None else self._of(out.ended_parents, i32, shape, "out.ended_parents")
+            a.ended_scores = None if out.ended_scores is None else self._of(out.ended_scores, f32, shape, "out.ended_scores")
         a.num_requests = R
         raw = self._stream(stream)
         rc = self._lib.ps_beam_select(self._h, raw, self._select_ref, self._status)

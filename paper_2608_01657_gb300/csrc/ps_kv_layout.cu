@@ -30,12 +30,42 @@ struct Args {
   int64_t stride, num_pages;
   LayoutScratch w;
   int32_t* status;
-  int32_t num_rows, row_pages, page_log2, lead, most;  // lead: pages that members of a group have in common; most: new tokens of a member
+  int32_t num_rows, row_pages, page_log2, lead, lead_log2, most;  // lead: pages that members of a group have in common; most: new tokens of a member
 };
 
 struct Item {
   int row, start, count;
 };
+// Requests i, i + step, ...: their reads go side by side.  False if one is out of
+// range; such a request has no tokens.
+template <int K>
+__device__ __forceinline__ bool items_of(const Args& a, int i, int step, int n, Item (&it)[K]) {
+  int row[K], start[K], count[K], held[K];
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const int k = i + j * step;
+    row[j] = k < n ? (a.l.rows ? a.l.rows[k] : k) : 0;
+    start[j] = k < n && a.l.starts ? a.l.starts[k] : 0;
+    count[j] = k < n && a.l.counts ? a.l.counts[k] : 1;
+  }
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const bool on = row[j] >= 0 && row[j] < a.num_rows;
+    held[j] = on ? a.held[row[j]] : -1;
+    if (on && !a.l.starts) start[j] = a.lens[row[j]];
+  }
+  bool ok = true;
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    it[j] = Item{row[j], start[j], count[j]};
+    const bool good = start[j] >= 0 && count[j] >= 0 && held[j] >= 0 && held[j] <= a.row_pages &&
+                      (int64_t)start[j] + count[j] <= (int64_t)held[j] << a.page_log2;
+    const bool on = i + j * step < n;
+    ok = ok && (good || !on);
+    if (!good || !on) it[j] = Item{-1, 0, 0};
+  }
+  return ok;
+}
 // Request i; false, and no tokens, if its row or its numbers are out of range.
 __device__ __forceinline__ bool item_of(const Args& a, int i, Item* it) {
   const int row = a.l.rows ? a.l.rows[i] : i;
@@ -142,55 +172,80 @@ __device__ __forceinline__ void ends(const Args& a, bool over, int total, int gr
   if (l.group_offsets && l.pad) l.group_offsets[groups] = n;
 }
 
+// CTA 0 writes the requests' own numbers, the others fill the tables and tokens.
 __global__ void __launch_bounds__(kScanThreads) k_layout(Args a) {
   __shared__ int off[kFused + 1];
   __shared__ Item item[kFused];
+  __shared__ unsigned char differs[kFused];
   chain();
   const ps_kv_layout_t& l = a.l;
-  const int n = l.num_requests, i0 = threadIdx.x * kItems;
+  const int n = l.num_requests, tid = threadIdx.x, i0 = tid * kItems;
   Item it[kItems];
-  int64_t sum = 0, total;
-  bool bad = false;
+  bool bad = !items_of(a, tid, kScanThreads, n, it);
 #pragma unroll
   for (int j = 0; j < kItems; ++j) {
-    it[j] = Item{-1, 0, 0};
-    if (i0 + j < n) bad |= !item_of(a, i0 + j, &it[j]);
+    item[j * kScanThreads + tid] = it[j];
+    differs[j * kScanThreads + tid] = 0;
+  }
+  bad = __syncthreads_or(bad);
+  int64_t sum = 0, total;
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    it[j] = item[i0 + j];
     sum += it[j].count;
-    item[i0 + j] = it[j];
   }
   int64_t o = block_scan(sum, &total);
-  bad = __syncthreads_or(bad);
   const bool over = bad || total > l.num_tokens;
 #pragma unroll
   for (int j = 0; j < kItems; ++j) {
     off[i0 + j] = over ? 0 : (int)o;
     o += it[j].count;
   }
-  if (threadIdx.x == kScanThreads - 1) off[kFused] = over ? 0 : (int)total;
+  if (tid == kScanThreads - 1) off[kFused] = over ? 0 : (int)total;
   __syncthreads();
-  if (blockIdx.x == 0) {  // the requests' own numbers, once
-    if (over && threadIdx.x == 0) set_error(a.status, bad ? PS_ERR_INVALID_ARG : PS_ERR_CAPACITY);
+  if (blockIdx.x > 0) {
+    fill(a, Near{off, item, n}, over, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  if (over && tid == 0) set_error(a.status, bad ? PS_ERR_INVALID_ARG : PS_ERR_CAPACITY);
+  for (int i = tid; i < n; i += kScanThreads) {
+    l.q_offsets[i] = off[i];
+    l.kv_lens[i] = over ? 0 : item[i].start + item[i].count;
+  }
+  int groups = 0;
+  if (l.group_offsets) {
+    // the leading ids of a request and of the one before it, side by side
+    const int pairs = over ? 0 : n * a.lead;
+    auto fits = [&](int i) { return item[i].start >= a.lead << a.page_log2 && item[i].count <= a.most; };
+    for (int p0 = tid; p0 < pairs; p0 += 8 * kScanThreads) {
+      int x[8], y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int p = p0 + u * kScanThreads, i = p >> a.lead_log2, k = p & (a.lead - 1);
+        x[u] = y[u] = 0;
+        if (p < pairs && i > 0 && fits(i) && fits(i - 1)) {
+          x[u] = a.tables[item[i].row * a.stride + k];
+          y[u] = a.tables[item[i - 1].row * a.stride + k];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (x[u] != y[u]) differs[(p0 + u * kScanThreads) >> a.lead_log2] = 1;
+    }
+    __syncthreads();
     int begins = 0;
 #pragma unroll
     for (int j = 0; j < kItems; ++j) {
       const int i = i0 + j;
-      if (i >= n) break;
-      l.q_offsets[i] = off[i];
-      l.kv_lens[i] = over ? 0 : it[j].start + it[j].count;
-      if (l.group_offsets && (i == 0 || over || !joined(a, it[j], item[i - 1]))) begins |= 1 << j;
+      if (i < n && (i == 0 || over || differs[i] || !fits(i) || !fits(i - 1))) begins |= 1 << j;
     }
-    int groups = 0;
-    if (l.group_offsets) {
-      int g = block_scan(__popc(begins), &groups);
+    int g = block_scan(__popc(begins), &groups);
 #pragma unroll
-      for (int j = 0; j < kItems; ++j)
-        if (begins >> j & 1) l.group_offsets[g++] = i0 + j;
-      for (int g = groups + (l.pad ? 1 : 0) + threadIdx.x; g <= n + (l.pad ? 1 : 0); g += kScanThreads)
-        l.group_offsets[g] = n + (l.pad ? 1 : 0);
-    }
-    if (threadIdx.x == 0) ends(a, over, over ? 0 : (int)total, groups);
+    for (int j = 0; j < kItems; ++j)
+      if (begins >> j & 1) l.group_offsets[g++] = i0 + j;
+    for (int g = groups + (l.pad ? 1 : 0) + tid; g <= n + (l.pad ? 1 : 0); g += kScanThreads) l.group_offsets[g] = n + (l.pad ? 1 : 0);
   }
-  fill(a, Near{off, item, n}, over, blockIdx.x, gridDim.x);
+  if (tid == 0) ends(a, over, over ? 0 : (int)total, groups);
 }
 
 // Many requests: kFused a CTA.  Their offsets and groups from the CTA's first on,
@@ -291,14 +346,16 @@ int32_t launch_layout(const Pool& p, const LayoutScratch& w, const ps_kv_layout_
   a.tables = rows.tables; a.lens = rows.lens; a.held = rows.held; a.stride = rows.table_stride;
   a.num_pages = p.num_pages; a.w = w; a.status = status;
   a.num_rows = rows.num_rows; a.row_pages = row_pages; a.page_log2 = p.page_log2;
-  a.lead = (kShareTokens + p.page_size - 1) >> p.page_log2;
+  static_assert(kShareTokens == 128, "whole pages of 2 to 64 tokens");
+  a.lead_log2 = 7 - p.page_log2;
+  a.lead = 1 << a.lead_log2;
   a.most = kShareRows / p.ratio;
   const int64_t n = l.num_requests;
   const int64_t units = (n + (l.pad ? 1 : 0)) * ((a.stride + kUnit - 1) / kUnit) + ((int64_t)l.num_tokens + kUnit - 1) / kUnit;
   const int64_t want = (units + kUnitsPerCta - 1) / kUnitsPerCta;
   const int64_t most = (int64_t)nsm * 4;
   const int grid = (int)(want < 1 ? 1 : (want > most ? most : want));
-  if (n <= kFused) return status_of(launch(k_layout, dim3((unsigned)grid), kScanThreads, 0, st, a));
+  if (n <= kFused) return status_of(launch(k_layout, dim3((unsigned)(grid + 1)), kScanThreads, 0, st, a));
   cudaError_t e = launch(k_layout_scan, dim3((unsigned)((n + kFused - 1) / kFused)), kScanThreads, 0, st, a);
   if (e == cudaSuccess) e = launch(k_layout_fill, dim3((unsigned)grid), kScanThreads, 0, st, a);
   return status_of(e);

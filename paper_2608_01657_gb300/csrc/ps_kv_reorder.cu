@@ -20,6 +20,8 @@ namespace {
 
 constexpr int kCols = kScanThreads;  // columns that a CTA takes at a time
 constexpr int kColCtas = 64;         // CTAs of a request at most
+constexpr int kAtOnce = 8;           // beams whose ids a thread reads together
+constexpr int kNoPage = -1;
 
 struct Args {
   const int32_t *rows, *parents;
@@ -65,31 +67,49 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
       // neighbouring beams mostly hold the same page: their changes go together
       int64_t at = -1;
       int change = 0;
-      for (int q = 0; q < B; ++q) {
-        if (k >= s_held[q]) continue;
-        const int64_t id = a.tables[s_row[q] * a.stride + k];
-        const int c = s_children[q], d = k < s_len[q] >> p.page_log2 ? c - 1 : (c > 0 ? 0 : -1);
-        if (id == at) {
-          change += d;
-          continue;
+      for (int q0 = 0; q0 < B; q0 += kAtOnce) {
+        int ids[kAtOnce], held[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int q = q0 + u;
+          ids[u] = q < B && k < s_held[q] ? a.tables[s_row[q] * a.stride + k] : kNoPage;
         }
-        if (change != 0 && at >= p.first_page) atomicAdd(o.delta + (at - p.first_page), change);
-        at = -1;
-        change = 0;
-        if (id < 0 || id >= p.num_pages || (id >= p.first_page && a.refs_in[id - p.first_page] <= 0)) {
-          ok = false;
-          continue;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {  // (a page that the beam before has, too, is looked at there)
+          const int64_t id = ids[u];
+          held[u] = 1;
+          if (id >= p.first_page && id < p.num_pages && (u == 0 || ids[u] != ids[u ? u - 1 : 0])) held[u] = a.refs_in[id - p.first_page];
         }
-        at = id;
-        change = d;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int64_t id = ids[u];
+          const int q = q0 + u;
+          if (ids[u] == kNoPage && (q >= B || k >= s_held[q])) continue;
+          const int c = s_children[q], d = k < s_len[q] >> p.page_log2 ? c - 1 : (c > 0 ? 0 : -1);
+          if (id == at) {
+            change += d;
+            continue;
+          }
+          if (change != 0 && at >= p.first_page) atomicAdd(o.delta + (at - p.first_page), change);
+          at = -1;
+          change = 0;
+          if (id < 0 || id >= p.num_pages || held[u] <= 0) {
+            ok = false;
+            continue;
+          }
+          at = id;
+          change = d;
+        }
       }
       if (change != 0 && at >= p.first_page) atomicAdd(o.delta + (at - p.first_page), change);
     }
     if (y == 0) {
       // a row is named once
-      for (int q = 0; q < B; ++q)
-        for (int64_t j = threadIdx.x; j < a.n; j += kScanThreads)
-          if (j != i0 + q && a.rows[j] == s_row[q]) ok = false;
+      for (int64_t j = threadIdx.x; j < a.n; j += kScanThreads) {
+        const int row = a.rows[j];
+        for (int q = 0; q < B; ++q)
+          if (j != i0 + q && row == s_row[q]) ok = false;
+      }
       if (b < B) {
         ReorderRec r{};
         const int q = s_parent[b];
@@ -118,21 +138,28 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
   if (!ok) atomicMin(&w.hdr->refused, (int32_t)PS_ERR_INVALID_ARG);
 }
 
-// CTA c: chunk c of the references.
+// CTA c: chunk c of the references.  These are read before the wait for
+// k_reorder_scan, which only reads them and lets this kernel start when all that came
+// before it is done.
 __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScratch w, ReorderScratch o, Args a) {
-  chain();
   const int64_t np = p.num_pages - p.first_page;
   const int64_t c0 = (int64_t)blockIdx.x * w.chunk_size;
   const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
   int count = 0;
   bool ok = true;
-  for (int64_t i0 = c0; i0 < c1; i0 += kTile) {
+  for (int64_t i0 = c0; i0 < c1 || i0 == c0; i0 += kTile) {
     int r[kEach], rank[kEach], tot;
     bool free[kEach];
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
       const int64_t i = i0 + u * kScanThreads + threadIdx.x;
-      r[u] = i < c1 ? a.refs_in[i] + o.delta[i] : 1;
+      r[u] = i < c1 ? __ldcg(a.refs_in + i) : 1;
+    }
+    if (i0 == c0) chain();
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t i = i0 + u * kScanThreads + threadIdx.x;
+      if (i < c1) r[u] += o.delta[i];
       free[u] = r[u] == 0;
       ok = ok && r[u] >= 0;
     }
@@ -171,17 +198,25 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScrat
   }
 }
 
+// A record, not from the SM's own cache: it is read before the wait.
+__device__ __forceinline__ ReorderRec record(const ReorderScratch& o, int64_t i) {
+  const int4 a = __ldcg(reinterpret_cast<const int4*>(o.rec + i)), b = __ldcg(reinterpret_cast<const int4*>(o.rec + i) + 1);
+  return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
 // CTAs, in order: a chunk of the references each; 256 columns of a request's rows;
-// the copies, warp by warp.
+// the copies, warp by warp.  What k_reorder_scan wrote, and the tables, are read before
+// the wait for k_reorder_free, which lets this kernel start when that one is done.
 __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScratch w, ReorderScratch o, Args a) {
   __shared__ int base[kMaxChunks];
   __shared__ ReorderRec s_rec[PS_KV_MAX_BEAMS];
   __shared__ int s_start[PS_KV_MAX_BEAMS];
   __shared__ int ids[PS_KV_MAX_BEAMS][kCols];
-  chain();
-  const int st = w.hdr->status, B = a.beams, requests = a.n / B;
+  const int B = a.beams, requests = a.n / B, tables = requests * a.col_ctas;
   int cta = blockIdx.x;
   if (cta < w.chunks) {
+    chain();
+    const int st = w.hdr->status;
     const int64_t np = p.num_pages - p.first_page, c0 = (int64_t)cta * w.chunk_size;
     const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
     if (st != PS_OK) {
@@ -189,26 +224,45 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScra
         for (int64_t i = c0 + threadIdx.x; i < c1; i += kScanThreads) a.refs_out[i] = a.refs_in[i];
       return;
     }
+#pragma unroll 8
     for (int64_t i = c0 + threadIdx.x; i < c1; i += kScanThreads) a.refs_out[i] = o.refs[i];
     __syncthreads();
     const int before = w.chunk_base[cta], taken = min(w.hdr->free_pages - before, w.chunk_cnt[cta]);
     for (int j = threadIdx.x; j < taken; j += kScanThreads) a.refs_out[w.list[c0 + j]] = 1;
     return;
   }
-  if (st != PS_OK) return;
-  for (int c = threadIdx.x; c < w.chunks; c += kScanThreads) base[c] = w.chunk_base[c];
   cta -= w.chunks;
-  if (cta < requests * a.col_ctas) {
+  if (cta < tables) {
     const int r = cta / a.col_ctas, y = cta % a.col_ctas, b = threadIdx.x;
-    if (b < B) {
-      s_rec[b] = o.rec[(int64_t)r * B + b];
-      s_start[b] = w.start[(int64_t)r * B + b];
-    }
+    if (b < B) s_rec[b] = record(o, (int64_t)r * B + b);
     __syncthreads();
     int most = 0;
-    for (int j = 0; j < B; ++j) most = max(most, s_rec[j].total);
-    for (int k = y * kCols + threadIdx.x; k < most; k += a.col_ctas * kCols) {
-      for (int j = 0; j < B; ++j) ids[j][threadIdx.x] = a.tables[s_rec[j].row * a.stride + k];
+    bool sane = true;  // (after a refusal the records may be anything)
+    for (int j = 0; j < B; ++j) {
+      most = max(most, s_rec[j].total);
+      sane = sane && s_rec[j].row >= 0 && s_rec[j].row < a.num_rows;
+    }
+    if (most > a.row_pages || !sane) most = 0;
+    int k = y * kCols + threadIdx.x;
+    auto read = [&]() {
+      for (int j0 = 0; j0 < B; j0 += kAtOnce) {
+        int id[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+          if (j0 + u < B) id[u] = __ldcg(a.tables + s_rec[j0 + u].row * a.stride + k);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+          if (j0 + u < B) ids[j0 + u][threadIdx.x] = id[u];
+      }
+    };
+    if (k < most) read();
+    chain();
+    if (w.hdr->status != PS_OK) return;
+    for (int c = threadIdx.x; c < w.chunks; c += kScanThreads) base[c] = w.chunk_base[c];
+    if (b < B) s_start[b] = w.start[(int64_t)r * B + b];
+    __syncthreads();
+    for (; k < most; k += a.col_ctas * kCols) {
+      if (k >= a.col_ctas * kCols) read();
       for (int j = 0; j < B; ++j) {
         const ReorderRec& x = s_rec[j];
         if (k >= x.total) continue;
@@ -223,17 +277,25 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScra
     }
     return;
   }
-  cta -= requests * a.col_ctas;
-  __syncthreads();
+  cta -= tables;
   const int parts = copy_parts(p, p.page_size), slices = 2 * p.num_layers;
-  const int64_t units = (int64_t)a.n * slices * parts, ctas = (int64_t)gridDim.x - w.chunks - requests * a.col_ctas;
-  for (int64_t u = (int64_t)cta * kCopyWarps + (threadIdx.x >> 5); u < units; u += ctas * kCopyWarps) {
+  const int64_t units = (int64_t)a.n * slices * parts, step = ((int64_t)gridDim.x - w.chunks - tables) * kCopyWarps;
+  int64_t u = (int64_t)cta * kCopyWarps + (threadIdx.x >> 5);
+  ReorderRec x{};
+  if (u < units) x = record(o, u / (slices * parts));
+  chain();
+  if (w.hdr->status != PS_OK) return;
+  for (int c = threadIdx.x; c < w.chunks; c += kScanThreads) base[c] = w.chunk_base[c];
+  __syncthreads();
+  while (u < units) {
     const int64_t i = u / (slices * parts);
     const int rest = (int)(u % (slices * parts));
-    const ReorderRec x = o.rec[i];
-    if (x.part == 0) continue;
-    const int64_t to = p.first_page + free_page(w, base, w.start[i]);
-    copy_part(p, x.from, to, rest / parts, x.part, rest % parts, threadIdx.x & 31);
+    if (x.part > 0) {
+      const int64_t to = p.first_page + free_page(w, base, w.start[i]);
+      copy_part(p, x.from, to, rest / parts, x.part, rest % parts, threadIdx.x & 31);
+    }
+    u += step;
+    if (u < units) x = record(o, u / (slices * parts));
   }
 }
 

@@ -111,6 +111,11 @@ class Layout(NamedTuple):
     group_offsets: Optional[torch.Tensor]  # int32 [requests + 1]
 
 
+class _MadeLayout(Layout):
+    """A layout that ``KVPool.layout`` made: ``made`` has the pool, the sizes and the
+    addresses, so that they are checked once.  (``_replace`` makes one without.)"""
+
+
 class KVPool(Handle):
     """One paged pool of keys and values on the current CUDA device.
 
@@ -241,26 +246,32 @@ class KVPool(Handle):
         is -1, and a plan of it is refused."""
         a = self._layout_args
         r = self._rows(tables, lens, held)
+        width = self._rows_args.table_stride
         n = tables.shape[0] if rows is None else rows.shape[0]
         T, all_ = int(num_tokens), n + bool(pad)
         i32 = torch.int32
-        if out is None:
-            made = lambda *shape, dtype=i32: B._made(shape, dtype, self.device, stream)  # noqa: E731
-            out = Layout(made(all_ + 1), made(all_), made(all_, tables.shape[1]), made(T), made(T, dtype=torch.int64),
-                         made(all_ + 1) if groups else None)
-        self._table(out.tables, "out.tables")
-        if out.tables.shape[0] != all_ or out.tables.shape[1] != tables.shape[1]:
-            raise ValueError(f"out.tables must be [{all_}, {tables.shape[1]}]")
         a.rows = None if rows is None else self._array(rows, i32, "rows")
         a.counts = None if counts is None else self._array(counts, i32, "counts", n)
         a.starts = None if starts is None else self._array(starts, i32, "starts", n)
         a.written = None if written is None else self._array(written, i32, "written", n)
-        a.q_offsets = self._array(out.q_offsets, i32, "out.q_offsets", all_ + 1)
-        a.kv_lens = self._array(out.kv_lens, i32, "out.kv_lens", all_)
-        a.tables = out.tables.data_ptr()
-        a.positions = self._array(out.positions, i32, "out.positions", T)
-        a.slots = self._array(out.slots, torch.int64, "out.slots", T)
-        a.group_offsets = None if out.group_offsets is None else self._array(out.group_offsets, i32, "out.group_offsets", all_ + 1)
+        if out is None:
+            made = lambda *shape, dtype=i32: B._made(shape, dtype, self.device, stream)  # noqa: E731
+            out = _MadeLayout(made(all_ + 1), made(all_), made(all_, width), made(T), made(T, dtype=torch.int64),
+                              made(all_ + 1) if groups else None)
+            out.made = (self, all_, width, T, *(0 if t is None else t.data_ptr() for t in out))
+        known = getattr(out, "made", None)
+        if known is not None and known[0] is self and known[1:4] == (all_, width, T):
+            a.q_offsets, a.kv_lens, a.tables, a.positions, a.slots, a.group_offsets = known[4:]
+        else:
+            self._table(out.tables, "out.tables")
+            if out.tables.shape[0] != all_ or out.tables.shape[1] != width:
+                raise ValueError(f"out.tables must be [{all_}, {width}]")
+            a.q_offsets = self._array(out.q_offsets, i32, "out.q_offsets", all_ + 1)
+            a.kv_lens = self._array(out.kv_lens, i32, "out.kv_lens", all_)
+            a.tables = out.tables.data_ptr()
+            a.positions = self._array(out.positions, i32, "out.positions", T)
+            a.slots = self._array(out.slots, torch.int64, "out.slots", T)
+            a.group_offsets = None if out.group_offsets is None else self._array(out.group_offsets, i32, "out.group_offsets", all_ + 1)
         a.num_requests, a.num_tokens, a.pad = n, T, 1 if pad else 0
         raw = self._stream(stream)
         rc = self._lib.ps_kv_layout(self._h, raw, r, self._layout_ref, self._status)
