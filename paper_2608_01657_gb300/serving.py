@@ -5,18 +5,20 @@ random weights: a prefix-cache step over a batch of prompts decides which blocks
 are cached, the uncached tokens' keys and values go to their pages, attention
 reads cached and new pages alike (a shared prefix once for all its requests),
 every request is forked into samples that share its pages, the samples decode
-some tokens, losers are freed and the pool is compacted.
+some tokens, losers are freed and the pool is compacted; or its beams search for
+likely answers, their pages following the beams that they continue.
 
     python -m paper_2608_01657_gb300.serving
 """
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 import numpy as np
 import torch
 
+from . import beam
 from . import binding as B
 from . import kv
 
@@ -75,29 +77,23 @@ class Server:
 
     # -- one pass over all layers ------------------------------------------------
     def forward(self, rows: torch.Tensor, start: torch.Tensor, tokens: torch.Tensor, counts: Sequence[int],
-                groups: Sequence[int], write=None) -> torch.Tensor:
+                groups: Optional[Sequence[int]] = None, written: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Hidden states of ``counts[i]`` new tokens of each row, from position ``start[i]`` on.
 
-        ``groups``: first rows of the runs that may share a prefix, and the number of rows."""
+        ``groups``: first rows of the runs that may share a prefix, and the number of rows (None: those
+        that their pages show).  ``written``: how many of a row's tokens have their keys and values."""
         s, w = self.s, self.layers
-        n = torch.tensor(counts, device="cuda")
-        offsets = torch.zeros(len(counts) + 1, dtype=torch.int64, device="cuda")
-        offsets[1:] = n.cumsum(0)
-        of = torch.repeat_interleave(torch.arange(len(counts), device="cuda"), n)
-        pos = (start.long()[of] + torch.arange(len(of), device="cuda") - offsets[of])
-        tables = self.tables[rows.long()].contiguous()
-        slots = tables.long()[of, pos // s.page] * s.page + pos % s.page
-        if write is not None:
-            slots = torch.where(write, slots, -1)
-        pos = pos.int()
-        self.pool.plan(offsets.int(), (start.long() + n).int(), tables, len(of),
-                       group_offsets=torch.tensor(groups, dtype=torch.int32, device="cuda"))
+        T = int(sum(counts))
+        at = self.pool.layout(rows, self.tables, self.lens, self.held, T,
+                              counts=torch.tensor(counts, dtype=torch.int32, device="cuda"), starts=start.int(), written=written)
+        bounds = at.group_offsets if groups is None else torch.tensor(groups, dtype=torch.int32, device="cuda")
+        self.pool.plan(at.q_offsets, at.kv_lens, at.tables, T, group_offsets=bounds)
         x = w.embed[tokens.long()]
         a, b = s.q_heads * s.head_dim, (s.q_heads + s.kv_heads) * s.head_dim
         for layer in range(s.layers):
             qkv = x @ w.qkv[layer].T
             q, k, v = (t.unflatten(1, (-1, s.head_dim)) for t in (qkv[:, :a], qkv[:, a:b], qkv[:, b:]))
-            q = self.pool.append(layer, q, k, v, slots, positions=pos, rope=w.rope, q_weight=w.q_norm[layer],
+            q = self.pool.append(layer, q, k, v, at.slots, positions=at.positions, rope=w.rope, q_weight=w.q_norm[layer],
                                  k_weight=w.k_norm[layer])
             o = self.pool.attention(layer, q, s.head_dim ** -0.5)
             x = x + o.flatten(1) @ w.out[layer].T
@@ -139,9 +135,7 @@ class Server:
         counts = [n - a for n, a in zip(lens, host)]
         new = torch.cat([flat[offs[i] + host[i]:offs[i + 1]] for i in range(R)])
         # a fully cached prompt's last token has its keys and values already
-        write = torch.cat([torch.full((c,), int(h) <= a, device="cuda") for c, h, a in zip(counts, hits.tolist(), host)])
-        bounds = [0] + [i for i in range(1, R) if groups[i] != groups[i - 1]] + [R]
-        x = self.forward(rows, start, new, counts, bounds, write)
+        x = self.forward(rows, start, new, counts, written=hits.int())
         last = torch.tensor(np.cumsum(counts) - 1, device="cuda")
         return {"hidden": x[last], "cached": int(hits.sum())}
 
@@ -159,13 +153,62 @@ class Server:
         children = dev(np.asarray(rows))
         self.running.update(rows)
         self.pool.fork(parents, children, self.lens[parents.long()] + T, self.tables, self.lens, self.held, self.refs)
-        bounds = list(range(0, n + 1, samples))  # a request's samples share its pages
         out = []
         for t in range(T):
             start = self.lens[children.long()]
-            out.append(self.forward(children, start, torch.from_numpy(steps[t].reshape(-1)).cuda(), [1] * n, bounds))
+            out.append(self.forward(children, start, torch.from_numpy(steps[t].reshape(-1)).cuda(), [1] * n))
             self.lens[children.long()] += 1
         return torch.stack(out)
+
+    # -- beams -----------------------------------------------------------------------
+    def beam_search(self, hidden: torch.Tensor, beams: int, steps: int, end: Sequence[int] = ()) -> dict:
+        """Likely answers of up to ``steps`` tokens to the admitted prompts.
+
+        ``hidden``: the states that ``admit`` gave.  Returns the ``beams`` answers of each request with the
+        highest mean log-probability a token: ``sequences`` [requests, beams, steps] (-1 past their ends),
+        their ``lengths`` and ``scores`` (sums of log-probabilities, an end token's among them; -infinity
+        where there are fewer).  The beams' rows, len(hidden) .. len(hidden) * (beams + 1), stay."""
+        s, R = self.s, hidden.shape[0]
+        n = R * beams
+        names = range(R, R + n)
+        if self.running.intersection(names):
+            raise RuntimeError("the beams' rows are running: finish them first")
+        i32 = dict(dtype=torch.int32, device="cuda")
+        children = torch.tensor(list(names), **i32)
+        rows = children.view(R, beams)
+        parents = torch.arange(R, **i32).repeat_interleave(beams)
+        self.running.update(names)
+        self.pool.fork(parents, children, self.lens[parents.long()] + 1, self.tables, self.lens, self.held, self.refs)
+        search = beam.BeamSearch(R, beams, s.vocab, torch.bfloat16, end)
+        whole = lambda dtype: torch.empty(steps, R, beams, dtype=dtype, device="cuda")  # noqa: E731
+        all_ = beam.Selection(*(whole(t) for t in (torch.int32, torch.int32, torch.float32) * 2))
+        # a prompt has one beam at first
+        scores = torch.full((R, beams), -torch.inf, device="cuda")
+        scores[:, 0] = 0
+        logits = (hidden @ self.layers.embed.T)[:, None].expand(R, beams, s.vocab)
+        for t in range(steps):
+            at = search.select(logits, scores, out=beam.Selection(*(x[t] for x in all_)))
+            scores = at.scores
+            if t + 1 == steps:
+                break
+            if t > 0:  # (after the first step all rows are alike)
+                self.pool.reorder(rows, at.parents, self.tables, self.lens, self.held, self.refs, grow=1)
+            x = self.forward(children, self.lens[children.long()], at.tokens.view(-1), [1] * n)
+            self.lens[children.long()] += 1
+            logits = (x @ self.layers.embed.T).view(R, beams, s.vocab)
+        search.check()
+        # the beams of the last step, and those that ended on the way: at step t with parent p, in p's row of step t - 1
+        step = torch.arange(steps, device="cuda")[:, None, None].expand(steps, R, beams)
+        score = torch.cat([all_.scores[-1:], all_.ended_scores]).movedim(0, 1).flatten(1)
+        last = torch.cat([torch.arange(beams, **i32).expand(1, R, beams), all_.ended_parents]).movedim(0, 1).flatten(1)
+        length = torch.cat([torch.full((1, R, beams), steps, device="cuda"), step]).movedim(0, 1).flatten(1)
+        tokens = torch.cat([length[:, :beams], length[:, beams:] + 1], 1)  # with the end token
+        best = (score / tokens).topk(beams, 1).indices
+        score, last, length = (x.gather(1, best) for x in (score, last, length))
+        last = torch.where(torch.isinf(score), -1, last).int().contiguous()
+        sequences = search.trace(all_.tokens, all_.parents, last, lengths=length.int().contiguous())
+        search.check()
+        return {"sequences": sequences, "lengths": length, "scores": score}
 
     def finish(self, rows: Sequence[int]):
         """Frees rows and moves the pages in use together; returns (in use, moved)."""
@@ -197,6 +240,11 @@ def main():
     out = server.sample(len(groups), 3, steps)
     print("sampled hidden states", tuple(out.shape))
     print("after freeing every second sample: pages in use, moved", server.finish(range(len(groups), len(groups) * 4, 2)))
+    server.finish(list(range(len(groups))) + list(range(len(groups) + 1, len(groups) * 4, 2)))
+    third = server.admit(groups, prompts_of(groups, s, 2), room=0)
+    found = server.beam_search(third["hidden"], beams=4, steps=6, end=[7])
+    print("likeliest answers", found["sequences"][:, 0].tolist())
+    print("their mean log-probabilities", [round(float(x), 3) for x in found["scores"][:, 0] / 6])
 
 
 if __name__ == "__main__":
