@@ -26,6 +26,7 @@ struct Args {
   int32_t* status;
   int32_t beams, hyps, steps, seg;  // hypotheses of a CTA, steps of a round and of a segment
   int32_t stride;                   // tokens of a step in shared memory: lanes of neighbouring steps meet at most four times at a bank
+  int32_t seg_log2, skew;           // of a segment; bytes between two segments' parents, so that they lie in other banks
   bool words;                       // a step's beams are whole 16-byte words
 };
 
@@ -39,15 +40,16 @@ __global__ void __launch_bounds__(kThreads) k_trace(const __grid_constant__ Args
   const int64_t r = blockIdx.x, R = a.num_requests;
   const int h0 = blockIdx.y * g.hyps, H = min(g.hyps, a.hyps - h0);
   int32_t* const token = reinterpret_cast<int32_t*>(smem);       // [steps][stride]
-  unsigned char* const parent = smem + (size_t)g.steps * g.stride * 4;  // [steps][B]
-  unsigned char* const path = parent + g.steps * B;              // [H][steps]
+  unsigned char* const parent = smem + (size_t)g.steps * g.stride * 4;      // [steps][B], see 'at'
+  unsigned char* const path = parent + g.steps * B + (g.steps / seg + 1) * g.skew;  // [steps][H]
   unsigned char* const map = path + g.steps * g.hyps;            // [segments][B]
   unsigned char* const entry = map + (g.steps / seg + 1) * B;    // [segments][H]
+  auto at = [&](int t) { return t * B + (t >> g.seg_log2) * g.skew; };  // where step t's parents are
   chain();
   bool bad = false;
   if (tid < H) {
-    const int64_t at = r * a.hyps + h0 + tid;
-    int len = a.lengths ? a.lengths[at] : T, last = a.beams_of[at];
+    const int64_t i = r * a.hyps + h0 + tid;
+    int len = a.lengths ? a.lengths[i] : T, last = a.beams_of[i];
     if (len < 0 || len > T || last < -1 || last >= B) {
       bad = true;
       last = -1;
@@ -67,30 +69,29 @@ __global__ void __launch_bounds__(kThreads) k_trace(const __grid_constant__ Args
 #pragma unroll 4
       for (int i = tid; i < n * each; i += kThreads) {
         const int t = i / each, w = i - t * each;
-        const int64_t at = from + (int64_t)t * R * B + 4 * w;
-        const int4 p = *reinterpret_cast<const int4*>(a.parents + at);
+        const int64_t k = from + (int64_t)t * R * B + 4 * w;
+        const int4 p = *reinterpret_cast<const int4*>(a.parents + k);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(token + t * g.stride + 4 * w)),
-                     "l"(a.tokens + at) : "memory");
-        reinterpret_cast<uint32_t*>(parent)[i] = byte(p.x) | byte(p.y) << 8 | byte(p.z) << 16 | byte(p.w) << 24;
+                     "l"(a.tokens + k) : "memory");
+        *reinterpret_cast<uint32_t*>(parent + at(t) + 4 * w) = byte(p.x) | byte(p.y) << 8 | byte(p.z) << 16 | byte(p.w) << 24;
       }
     } else {
 #pragma unroll 4
       for (int i = tid; i < n * B; i += kThreads) {
         const int t = i / B, b = i - t * B;
-        const int64_t at = from + (int64_t)t * R * B + b;
-        const int p = a.parents[at];
+        const int64_t k = from + (int64_t)t * R * B + b;
+        const int p = a.parents[k];
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(token + t * g.stride + b)),
-                     "l"(a.tokens + at) : "memory");
-        parent[i] = (unsigned char)byte(p);
+                     "l"(a.tokens + k) : "memory");
+        parent[at(t) + b] = (unsigned char)byte(p);
       }
     }
     __syncthreads();
     // From beam 'b' at step t0 + t to the one before the steps from 'down' on.
     auto back = [&](int b, int t, int down) {
-      for (; t >= down && b != kNone; --t) {
-        if (t0 + t == 0) return kNone;
-        b = parent[t * B + b];
-      }
+      if (t0 + down == 0) ++down;  // (what is before the first step is not looked at)
+      const unsigned char* p = parent + at(t);
+      for (; t >= down && b != kNone; --t, p -= B) b = p[b];
       return b;
     };
     for (int i = tid; i < segs * B; i += kThreads) {
@@ -120,25 +121,29 @@ __global__ void __launch_bounds__(kThreads) k_trace(const __grid_constant__ Args
     for (int i = tid; i < segs * H; i += kThreads) {
       const int s = i / H, h = i - s * H, down = s * seg, end = s_len[h] - 1 - t0;
       int t = min(n, down + seg) - 1, b = kNone;
+      unsigned char* to = path + t * H + h;
       if (end > t) b = entry[i];
-      for (; t >= down; --t) {
-        if (t == end) b = s_last[h];
-        path[h * n + t] = (unsigned char)b;
+      for (; t > end && t >= down && b == kNone; --t, to -= H) *to = kNone;
+      if (t == end) b = s_last[h];
+      const unsigned char* p = parent + at(t < 0 ? 0 : t);
+      for (; t >= down; --t, to -= H, p -= B) {
+        *to = (unsigned char)b;
         if (b != kNone && t0 + t > 0) {
-          b = parent[t * B + b];
+          b = p[b];
           bad = bad || b == kNone;
         }
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    const int blocks = (n + 31) / 32;
-#pragma unroll 4
-    for (int i = warp; i < blocks * H; i += kWarps) {
-      const int h = i / blocks, t = (i - h * blocks) * 32 + lane;
-      if (t < n) {
-        const int b = path[h * n + t];
-        a.out[(r * a.hyps + h0 + h) * T + t0 + t] = b == kNone ? -1 : token[t * g.stride + b];
+    for (int t = warp * 32 + lane; t < n; t += kThreads) {
+      const unsigned char* of = path + t * H;
+      const int32_t* pick = token + t * g.stride;
+      int32_t* to = a.out + (r * a.hyps + h0) * T + t0 + t;
+#pragma unroll 8
+      for (int h = 0; h < H; ++h, to += T) {
+        const int b = of[h];
+        *to = b == kNone ? -1 : pick[b];
       }
     }
     t1 = t0;
@@ -159,12 +164,14 @@ int32_t launch_trace(const Search& s, const ps_beam_trace_t& a, int32_t* status,
   g.beams = s.beams;
   g.hyps = a.hyps < kHyps ? a.hyps : kHyps;
   // segments of about the root of the steps: a third of the lookups each
-  g.seg = a.num_steps <= 128 ? 8 : (a.num_steps <= 512 ? 16 : 32);
+  g.seg_log2 = a.num_steps <= 128 ? 3 : (a.num_steps <= 512 ? 4 : 5);
+  g.seg = 1 << g.seg_log2;
   g.words = s.beams % 4 == 0 && ((reinterpret_cast<uintptr_t>(a.parents) | reinterpret_cast<uintptr_t>(a.tokens)) & 15) == 0;
   g.stride = !g.words ? s.beams | 1 : s.beams + (s.beams % 8 == 0 ? 4 : 0);
+  g.skew = (s.beams + 3) / 4 * 4;
   const int each = 4 * g.stride + s.beams + g.hyps, most = kBytes / each / g.seg * g.seg;
   g.steps = a.num_steps < most ? (a.num_steps + g.seg - 1) / g.seg * g.seg : most;
-  const size_t smem = (size_t)g.steps * each + (size_t)(g.steps / g.seg + 1) * (s.beams + g.hyps);
+  const size_t smem = (size_t)g.steps * each + (size_t)(g.steps / g.seg + 1) * (s.beams + g.hyps + g.skew);
   return status_of(launch(k_trace, dim3((unsigned)a.num_requests, (unsigned)((a.hyps + g.hyps - 1) / g.hyps)), kThreads, smem, st, g));
 }
 
