@@ -651,12 +651,11 @@ __device__ __noinline__ uint64_t far_sum(const T* row, int V, float most, int la
   return warp_sum(sum);
 }
 
-// The 'keep' greatest of n numbers (read before n is known, where there are 'most'): up
-// to kOneByOne to keep, of any order, and else of sorted lists of 'keep'.
-__device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int most, int keep, int lane) {
+// The 'keep' greatest of n numbers, of which the first 64 are in a and b: up to kOneByOne
+// to keep, of any order, and else of sorted lists of 'keep'.
+__device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, uint64_t a, uint64_t b, int n, int keep, int lane) {
   uint64_t list = 0;
   if (keep <= kOneByOne) {
-    uint64_t a = lane < most ? keys[lane] : 0, b = lane + 32 < most ? keys[lane + 32] : 0;
     for (int i = lane; i - lane < n; i += 64) {
       const uint64_t c = i + 64 < n ? keys[i + 64] : 0, d = i + 96 < n ? keys[i + 96] : 0;
       a = greatest_of(i < n ? a : 0, i + 32 < n ? b : 0, keep, lane);
@@ -664,7 +663,7 @@ __device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, int n, int m
       a = c, b = d;
     }
   } else {
-    uint64_t k = lane < keep ? keys[lane] : 0;
+    uint64_t k = lane < keep ? a : 0;
     for (int i = keep; i <= n; i += keep) {
       const uint64_t next = lane < keep && i < n ? keys[i + lane] : 0;
       list = i == keep ? k : merge32(list, k, lane);
@@ -703,14 +702,18 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_co
   Cand mine = nobody(lane);
   for (int b = warp; b < B; b += kJoinWarps) {
     const int row = r * B + b;
+    // all that may be needed is read at once, and looked at where it is some row's of this call
     const float c = g.a.scores[row];
+    const uint64_t* keys = g.s.keys + (int64_t)row * g.slots * B;
+    Part p{0, -INFINITY, 0};
+    if (lane < g.parts) p = g.s.parts[(int64_t)row * g.parts + lane];
+    const int lists = g.s.lists[row];
+    const uint64_t k0 = lane < g.slots * B ? keys[lane] : 0, k1 = lane + 32 < g.slots * B ? keys[lane + 32] : 0;
     Beam beam{INFINITY, 0.0, c};  // no candidates
     uint64_t list = 0;
     bool bad = c != -INFINITY && !(c - c == 0);
     if (c - c == 0) {
-      Part p{0, -INFINITY, 0};
-      if (lane < g.parts) p = g.s.parts[(int64_t)row * g.parts + lane];
-      list = best_runs(g.s.keys + (int64_t)row * g.slots * B, g.s.lists[row] * B, g.slots * B, B, lane);
+      list = best_runs(keys, k0, k1, lists * B, B, lane);
       const float most = warp_max(p.most), R = exponent_of(most), down = R - exponent_of(p.most);
       uint64_t sum = warp_sum(down < 64.0f ? p.sum >> (int)down : 0);
       bad = __any_sync(kAll, p.bad);
@@ -737,13 +740,15 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_co
   __syncthreads();
   // the best runs, and the end tokens' candidates
   if (B <= kRanked) {
-    if (t < B * B) {
-      const Cand x = s_run[t];
-      int place = 0;
-#pragma unroll 8
-      for (int i = 0; i < B * B; ++i) place += s_run[i].before(x);
-      if (x.somebody() && place < B) s_best[place] = x;
-    }
+    // a candidate for 'each' threads in a row, each of which counts a share
+    const int each = B * B <= 32 ? 8 : (B * B <= 64 ? 4 : (B * B <= 128 ? 2 : 1)), i = t / each, n = (B * B + each - 1) / each;
+    const Cand x = s_run[i];
+    int place = 0;
+    const int end = min(B * B, (t % each + 1) * n);
+#pragma unroll 4
+    for (int j = t % each * n; j < end; ++j) place += s_run[j].before(x);
+    for (int o = 1; o < each; o <<= 1) place += __shfl_xor_sync(kAll, place, o);
+    if (t % each == 0 && x.somebody() && place < B) s_best[place] = x;
   } else if (warp == 0) {
     for (int w = 1; w < kJoinWarps; ++w) mine = merge32(mine, s_token[w * 32 + lane], lane);
     if (lane < B) s_best[lane] = mine;
