@@ -32,11 +32,11 @@
 namespace psbeam {
 namespace {
 
-constexpr int kThreads = 128, kWarps = kThreads / 32;
-// Twelve warps an SM, of which none waits long for another (with 16 or 20 the last ones
-// ended 10 us behind the others), and registers for as many again, so that the next
-// kernel's CTAs have room beside them: 59 us as it stands, 61 and 65 with more warps.
-constexpr int kCtasPerSm = 3, kRoom = 4;
+constexpr int kThreads = 384, kWarps = kThreads / 32;
+// A CTA an SM, so that no SM has two while another has none, of twelve warps: with 16
+// the last ones ended 10 us behind the others, and a call of 128 requests took 66 us
+// instead of 57.  Registers as for 16 leave room for the next kernel's CTAs beside it.
+constexpr int kRoom = 512;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr int kVecs = 8;                 // 16-byte words of a run
 constexpr int kChunk = 32 * kVecs;       // words of a chunk, a run a lane
@@ -473,7 +473,7 @@ struct Shared {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, kRoom) k_select(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kRoom, 1) k_select(const __grid_constant__ Args g) {
   extern __shared__ __align__(16) unsigned char smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   chain();
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, kRoom) k_select(const __grid_constan
     if (count == 0) return;
   }
   // the warp's share of the list of all parts
-  const int all = gridDim.x * kWarps, w = blockIdx.x * kWarps + warp;
+  const int all = gridDim.x * kWarps, w = warp * gridDim.x + blockIdx.x;  // (few shares lie on different SMs)
   const int64_t U = (int64_t)count * g.parts;
   const int C = U < all ? (int)U : all;
   if (w >= C) return;
@@ -842,9 +842,8 @@ int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* statu
   g.chunks = (int32_t)((s.vocab + chunk - 1) / chunk);
   g.size = (g.chunks + kRowParts - 1) / kRowParts;
   g.parts = (g.chunks + g.size - 1) / g.size;
-  static_assert(kWarps * kCtasPerSm <= kWarpsPerSm, "the workspace's");
-  const int64_t U = g.rows * g.parts, most = (int64_t)nsm * kCtasPerSm, want = (U + kWarps - 1) / kWarps;
-  const int64_t grid = want < most ? want : most, C = U < grid * kWarps ? U : grid * kWarps;
+  static_assert(kWarps <= kWarpsPerSm, "the workspace's");
+  const int64_t U = g.rows * g.parts, grid = U < nsm ? U : nsm, C = U < grid * kWarps ? U : grid * kWarps;
   // where every part has a warp there is nothing to gain
   g.compact = U > C && g.rows <= 32 * kRowWords;
   const int64_t slots = g.compact ? g.parts : g.parts / (U / C) + 2;
