@@ -140,13 +140,15 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
 
 // CTA c: chunk c of the references.  These are read before the wait for
 // k_reorder_scan, which only reads them and lets this kernel start when all that came
-// before it is done.
+// before it is done.  (Without requests there is no such kernel, and what came before
+// may write them.)
 __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScratch w, ReorderScratch o, Args a) {
   const int64_t np = p.num_pages - p.first_page;
   const int64_t c0 = (int64_t)blockIdx.x * w.chunk_size;
   const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
   int count = 0;
   bool ok = true;
+  if (a.n == 0) chain();
   for (int64_t i0 = c0; i0 < c1 || i0 == c0; i0 += kTile) {
     int r[kEach], rank[kEach], tot;
     bool free[kEach];
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScrat
       const int64_t i = i0 + u * kScanThreads + threadIdx.x;
       r[u] = i < c1 ? __ldcg(a.refs_in + i) : 1;
     }
-    if (i0 == c0) chain();
+    if (i0 == c0 && a.n > 0) chain();
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
       const int64_t i = i0 + u * kScanThreads + threadIdx.x;

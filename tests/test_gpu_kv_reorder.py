@@ -216,6 +216,24 @@ def test_reorder_refusals():
     assert torch.equal(out, r)
 
 
+def test_calls_without_requests_lie_between_others():
+    """They pass the references on that the call right before them wrote."""
+    s = Search(8, 4, 300, pages=4000, seed=13)
+    rows, none = dev(s.rows), torch.zeros(0, 4, dtype=torch.int32, device="cuda")
+    steps = [s.random_parents() for _ in range(6)]
+    parents = [dev(p) for p in steps]
+    mid, last = torch.empty_like(s.f), s.f
+    for p in parents:
+        s.pool.reorder(rows, p, s.t, s.l, s.h, last, refs_out=mid)
+        last = torch.empty_like(mid)
+        s.pool.reorder(none, none, s.t, s.l, s.h, mid, refs_out=last)
+    s.pool.check()
+    for p in steps:
+        s.plain(p, 1)
+    s.f = last
+    s.same()
+
+
 def test_a_pool_without_private_pages():
     from paper_2608_01657_gb300 import kv as KV
     k, v = make_pool(1, 8, 16, 1, 64, BF)
