@@ -24,6 +24,7 @@ extern "C" {
 
 #define PS_BEAM_MAX_BEAMS 32
 #define PS_BEAM_MAX_END 8
+#define PS_BEAM_MAX_VOCAB (1 << 24)
 
 /* Element types of the logits. */
 typedef enum { PS_BEAM_BF16 = 0, PS_BEAM_F16 = 1, PS_BEAM_F32 = 2 } ps_beam_dtype_t;
@@ -31,7 +32,7 @@ typedef enum { PS_BEAM_BF16 = 0, PS_BEAM_F16 = 1, PS_BEAM_F32 = 2 } ps_beam_dtyp
 typedef struct {
   int32_t max_requests;                 /* of one call; max_requests * beams is at most 2^20 */
   int32_t beams;                        /* of a request: 1..PS_BEAM_MAX_BEAMS */
-  int32_t vocab;                        /* tokens: 1..2^30 */
+  int32_t vocab;                        /* tokens: 1..PS_BEAM_MAX_VOCAB */
   int32_t dtype;                        /* ps_beam_dtype_t */
   int32_t num_end;                      /* 0..PS_BEAM_MAX_END */
   int32_t end_tokens[PS_BEAM_MAX_END];  /* the tokens that end a sequence: distinct, 0..vocab - 1 */
@@ -41,9 +42,9 @@ typedef struct {
 typedef struct ps_beam ps_beam_t;
 
 /* Bytes of device workspace a handle needs (256-byte aligned base required), or 0
- * if the configuration is invalid: partial results, 516 bytes for each of
- * max_requests * beams rows, and 8 beams for each of 32 lists a row (up to 4096 rows;
- * 2 a row of more, and 7680). */
+ * if the configuration is invalid.  With n = max_requests * beams rows: partial
+ * results, 516 n bytes, and lists of 8 * beams bytes, the greater of 32 min(n, 4096)
+ * and 2 n + 3840 of them. */
 size_t ps_beam_workspace_bytes(const ps_beam_config_t* cfg);
 
 /* Create a handle on the current device.  The workspace, which need not be cleared,
@@ -60,7 +61,9 @@ void ps_beam_destroy(ps_beam_t* beam);
  *   c + x[v] - log sum_u exp x[u],
  * the sum in 32 bits at least, the score in 64, rounded once.  A logit of
  * -infinity is a token that cannot follow.  Candidates are ordered by score, equal
- * ones by beam, then by token, the lowest first.  Of each request
+ * ones by beam, then by token, the lowest first.  (Logits of one beam that differ by
+ * less than 64 bits hold beside the score, such as 1e-20 and 2e-20 where it is -5,
+ * are in either order.)  Of each request
  *   tokens, parents, scores_out  [beams] are the first candidates whose tokens end
  *     nothing, and the beams (0..beams - 1) that they continue;
  *   ended_tokens, ended_parents, ended_scores  [beams] (all three or none) are the

@@ -13,7 +13,7 @@ using pskv::status_of;
 
 // Parts of a row, and warps that a call's rows are divided between, at most, and rows
 // of which those that are not there are left out.
-constexpr int kRowParts = 32, kWarpsPerSm = 24, kRowWords = 128;
+constexpr int kRowParts = 32, kWarpsPerSm = 12, kRowWords = 128;
 constexpr int64_t kMostWarps = (int64_t)kWarpsPerSm * pskv::kMaxSms;
 // Lists of the best runs of a call's rows, one for each warp's share of a row: up to
 // kRowParts of a row in a call that leaves rows out, and else two for each warp and row.

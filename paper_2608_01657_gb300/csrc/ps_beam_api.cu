@@ -24,7 +24,7 @@ inline int64_t element_bytes(int32_t dtype) { return dtype == PS_BEAM_F32 ? 4 : 
 bool check_config(const ps_beam_config_t* c) {
   if (!c || c->max_requests < 1 || c->beams < 1 || c->beams > PS_BEAM_MAX_BEAMS) return false;
   if ((int64_t)c->max_requests * c->beams > (1 << 20)) return false;
-  if (c->vocab < 1 || c->vocab > (1 << 30)) return false;
+  if (c->vocab < 1 || c->vocab > PS_BEAM_MAX_VOCAB) return false;
   if (c->dtype != PS_BEAM_BF16 && c->dtype != PS_BEAM_F16 && c->dtype != PS_BEAM_F32) return false;
   if (c->num_end < 0 || c->num_end > PS_BEAM_MAX_END) return false;
   for (int i = 0; i < c->num_end; ++i) {

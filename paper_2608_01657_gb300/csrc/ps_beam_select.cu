@@ -32,7 +32,7 @@
 namespace psbeam {
 namespace {
 
-constexpr int kThreads = 384, kWarps = kThreads / 32;
+constexpr int kWarps = kWarpsPerSm, kThreads = 32 * kWarps;
 // A CTA an SM, so that no SM has two while another has none, of twelve warps: with 16
 // the last ones ended 10 us behind the others, and a call of 128 requests took 66 us
 // instead of 57.  Registers as for 16 leave room for the next kernel's CTAs beside it.
@@ -76,7 +76,6 @@ struct Elem<float> {
   static __device__ __forceinline__ uint4 narrow(const float (&x)[N]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
-  static __device__ __forceinline__ uint4 none() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
   static __device__ __forceinline__ float top(const uint4& v) {
     return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
@@ -109,10 +108,6 @@ struct Elem16 {
     if (pskv::Num<H>::kBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
-  }
-  static __device__ __forceinline__ uint4 none() {  // -infinity
-    constexpr uint32_t w = pskv::Num<H>::kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
-    return make_uint4(w, w, w, w);
   }
 };
 template <>
@@ -157,16 +152,6 @@ __device__ __forceinline__ uint64_t sort32(uint64_t x, int lane) {
   for (int k = 2; k <= 32; k <<= 1)
 #pragma unroll
     for (int j = k >> 1; j > 0; j >>= 1) exchange(x, j, ((lane & j) == 0) == ((lane & k) == 0));
-  return x;
-}
-__device__ __forceinline__ uint32_t sort32(uint32_t x, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const uint32_t y = __shfl_xor_sync(kAll, x, j);
-      x = ((lane & j) == 0) == ((lane & k) == 0) ? max(x, y) : min(x, y);
-    }
   return x;
 }
 // The 32 greatest of two such lists, as one.
@@ -275,7 +260,7 @@ struct Sum {
   __device__ __forceinline__ float base() const { return R == -INFINITY ? 0.0f : R; }
 };
 __device__ __forceinline__ float warp_max(float x) { return unordered(__reduce_max_sync(kAll, ordered(x))); }
-// Of numbers below 2^53.
+// Of numbers whose sum is below 2^58: a row has 2^24 terms of 2^32 at most.
 __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
   const uint32_t lo = __reduce_add_sync(kAll, (uint32_t)x & 0x3FFFFFFu), hi = __reduce_add_sync(kAll, (uint32_t)(x >> 26));
   return ((uint64_t)hi << 26) + lo;
@@ -842,7 +827,6 @@ int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* statu
   g.chunks = (int32_t)((s.vocab + chunk - 1) / chunk);
   g.size = (g.chunks + kRowParts - 1) / kRowParts;
   g.parts = (g.chunks + g.size - 1) / g.size;
-  static_assert(kWarps <= kWarpsPerSm, "the workspace's");
   const int64_t U = g.rows * g.parts, grid = U < nsm ? U : nsm, C = U < grid * kWarps ? U : grid * kWarps;
   // where every part has a warp there is nothing to gain
   g.compact = U > C && g.rows <= 32 * kRowWords;

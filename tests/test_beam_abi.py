@@ -64,12 +64,12 @@ def test_constants_match_the_headers():
 
 def test_workspace_sizes(B):
     assert size(B) > 0 and size(B) % 256 == 0 and size(B, max_requests=1000) > size(B)
-    assert size(B, vocab=1) > 0 and size(B, vocab=1 << 30) == size(B)  # partial results do not grow with the vocabulary
+    assert size(B, vocab=1) > 0 and size(B, vocab=1 << 24) == size(B)  # partial results do not grow with the vocabulary
     assert size(B, beams=32, max_requests=1 << 15) > 0
 
 
 @pytest.mark.parametrize("bad", [
-    dict(max_requests=0), dict(max_requests=1 << 18, beams=5), dict(beams=0), dict(beams=33), dict(vocab=0), dict(vocab=(1 << 30) + 1),
+    dict(max_requests=0), dict(max_requests=1 << 18, beams=5), dict(beams=0), dict(beams=33), dict(vocab=0), dict(vocab=(1 << 24) + 1),
     dict(dtype=3), dict(dtype=-1), dict(num_end=-1), dict(num_end=9), dict(end=(1000,)), dict(end=(-1,)), dict(end=(3, 4, 3))])
 def test_invalid_configurations_have_no_size(B, bad):
     assert size(B, **bad) == 0
