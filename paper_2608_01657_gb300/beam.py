@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from . import binding as B
-from .kv import Handle, _need
+from .kv import Handle, _addresses, _need
 
 _DTYPES = {torch.bfloat16: B.PS_BEAM_BF16, torch.float16: B.PS_BEAM_F16, torch.float32: B.PS_BEAM_F32}
 
@@ -33,7 +33,8 @@ class Selection(NamedTuple):
 
 class _MadeSelection(Selection):
     """A selection that ``BeamSearch.select`` made: ``made`` has the search, the requests
-    and the addresses, so that they are checked once.  (``_replace`` makes one without.)"""
+    and the addresses, so that its tensors are checked once, as long as their memory is
+    the same.  (``_replace`` makes one without.)"""
 
 
 class BeamSearch(Handle):
@@ -94,9 +95,9 @@ class BeamSearch(Handle):
         if out is None:
             made = lambda dtype: B._made(shape, dtype, self.device, stream)  # noqa: E731
             out = _MadeSelection(made(i32), made(i32), made(f32), *((made(i32), made(i32), made(f32)) if ended else (None, None, None)))
-            out.made = (self, R, *(0 if t is None else t.data_ptr() for t in out))
+            out.made = (self, R, *_addresses(out))
         known = getattr(out, "made", None)
-        if known is not None and known[0] is self and known[1] == R:
+        if known is not None and known[0] is self and known[1] == R and known[2:] == _addresses(out):
             a.tokens, a.parents, a.scores_out, a.ended_tokens, a.ended_parents, a.ended_scores = known[2:]
         else:
             a.tokens = self._of(out.tokens, i32, shape, "out.tokens")

@@ -101,6 +101,10 @@ class Handle:
         return t.data_ptr()
 
 
+def _addresses(tensors):
+    return tuple([0 if t is None else t.data_ptr() for t in tensors])
+
+
 class Layout(NamedTuple):
     """A batch's arrays, as ``append`` and ``plan`` take them."""
     q_offsets: torch.Tensor                # int32 [requests + 1]
@@ -113,7 +117,8 @@ class Layout(NamedTuple):
 
 class _MadeLayout(Layout):
     """A layout that ``KVPool.layout`` made: ``made`` has the pool, the sizes and the
-    addresses, so that they are checked once.  (``_replace`` makes one without.)"""
+    addresses, so that its tensors are checked once, as long as their memory is the
+    same.  (``_replace`` makes one without.)"""
 
 
 class KVPool(Handle):
@@ -258,9 +263,9 @@ class KVPool(Handle):
             made = lambda *shape, dtype=i32: B._made(shape, dtype, self.device, stream)  # noqa: E731
             out = _MadeLayout(made(all_ + 1), made(all_), made(all_, width), made(T), made(T, dtype=torch.int64),
                               made(all_ + 1) if groups else None)
-            out.made = (self, all_, width, T, *(0 if t is None else t.data_ptr() for t in out))
+            out.made = (self, all_, width, T, *_addresses(out))
         known = getattr(out, "made", None)
-        if known is not None and known[0] is self and known[1:4] == (all_, width, T):
+        if known is not None and known[0] is self and known[1:4] == (all_, width, T) and known[4:] == _addresses(out):
             a.q_offsets, a.kv_lens, a.tables, a.positions, a.slots, a.group_offsets = known[4:]
         else:
             self._table(out.tables, "out.tables")

@@ -30,11 +30,15 @@ def all_scores(logits, scores):
 def bound(scores, vocab):
     """How far a score may be off.
 
-    Its rounding to 32 bits, 2^-24 of it.  The sum: 2^-22 a term for the exponential
-    and, the terms' exponents t rounded twice at 2^-24 |t|, ln 2 * 2^-23 E|t| of the
-    whole, where the mean E|t| over the terms' shares is at most log2 of their number;
-    32-bit additions of at most 32 terms of a chunk and of a lane's chunks (a warp has
-    vocab / 2^13 at most, of 1024 elements and 8 warps), each also rescaled at 2^-22."""
+    Its rounding to 32 bits, 2^-24 of it.  The sum: 2^-22 a term for the exponential;
+    the terms' exponents t, rounded once at 2^-24 |t| and off by 1.3e-8 |t| for the
+    factor, are ln 2 (2^-24 + 2^-26) E|t| < 2^-24 E|t| of the whole, where the mean E|t|
+    over the terms' shares is at most 1 + log2 of their number; the whole numbers, 2^-33
+    for each of 1024 lanes' sums and 2^-32 for each of 32 parts', twice, of a sum of 1/2
+    at least, 2^-22 + 2^-25; 32-bit additions, 18 of a chunk's terms and one for each of
+    a lane's chunks of a part (vocab / 2^15 + 1 at most), also rescaled at 2^-22.  So
+    2^-22 (2.2 + (1 + log2 vocab) / 4) + 2^-24 (18 + 5 (vocab / 2^15 + 1)), which is less
+    than what is given here."""
     chunks = vocab / 2 ** 13 + 1
     return 2.0 ** -24 * scores.abs() + 2.0 ** -22 * (2 + math.log2(vocab + 1)) + 2.0 ** -24 * (36 + 6 * chunks)
 
@@ -244,6 +248,35 @@ def test_scores_in_place_and_outputs_reused():
     assert out.scores.data_ptr() == s.data_ptr()
 
 
+def test_outputs_whose_memory_has_changed():
+    """An output of an earlier call is written where its memory is now, and refused if that no longer fits."""
+    x, s = make(3, 4, 500, BF, seed=9)
+    h = search(3, 4, 500, BF, [2])
+    want, out = h.select(x, s), h.select(x, s)
+    old = out.tokens.data_ptr()
+    out.tokens.set_(torch.full((3, 4), -7, dtype=torch.int32, device="cuda"))
+    assert out.tokens.data_ptr() != old
+    got = h.select(x, s, out=out)
+    h.check()
+    assert got is out and all(torch.equal(a, b) for a, b in zip(out, want))
+    out.scores.set_(torch.zeros(2, 4, device="cuda"))
+    with pytest.raises(ValueError):
+        h.select(x, s, out=out)
+
+
+def test_rows_far_apart():
+    """A request's and a beam's logits past the 32-bit offsets of a buffer of 8.6 GB."""
+    V, far = 3001, (1 << 31) + 8 * 5
+    flat = torch.empty(2 * far + V, dtype=BF, device="cuda")
+    x = flat.as_strided((2, 2, V), (far, far, 1))  # (request 0's second beam is request 1's first)
+    y, s = make(2, 2, V, BF, seed=4)
+    x[0, 0], x[1, 0], x[1, 1] = y[0, 0], y[1, 0], y[1, 1]
+    h = search(2, 2, V, BF, [9])
+    got = h.select(x, s)
+    h.check()
+    check(x.contiguous(), s, [9], got)
+
+
 def test_select_refusals():
     x, s = make(2, 3, 100, BF, seed=1)
     h = search(2, 3, 100, BF, [1])
@@ -365,6 +398,36 @@ def test_bad_traces_are_reported():
             with pytest.raises(RuntimeError, match="invalid"):
                 h.check()
         assert (got.cpu().numpy() == want).all(), what
+
+
+def test_traces_captured_and_on_another_stream():
+    T, R, B, N = 700, 3, 5, 4
+    h = search(R, B, 100)
+    r = np.random.RandomState(17)
+    new = lambda: [dev(r.randint(*a)) for a in ((0, 100, (T, R, B)), (0, B, (T, R, B)), (-1, B, (R, N)), (0, T + 1, (R, N)))]  # noqa: E731
+    arrays = new()
+    out = h.trace(*arrays)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        h.trace(*arrays, out=out)
+    for _ in range(3):
+        for a, b in zip(arrays, new()):
+            a.copy_(b)
+        g.replay()
+        h.check()
+        assert np.array_equal(out.cpu().numpy(), trace_plain(*(a.cpu().numpy() for a in arrays)))
+    st = torch.cuda.Stream()
+    copies = [a.clone() for a in arrays]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(100_000_000)
+    got = h.trace(*copies, stream=st)
+    where = copies[0].data_ptr()
+    del copies
+    assert not st.query() and torch.empty_like(arrays[0]).data_ptr() != where
+    torch.cuda.synchronize()
+    assert torch.equal(got, out)
 
 
 def test_trace_refusals():

@@ -240,6 +240,22 @@ def test_a_padded_layout_is_replayed_planned_and_attended():
                     assert torch.equal(k[0, tables[i, p // ps], p % ps], nk[bounds[i] + j])
 
 
+def test_layouts_whose_memory_has_changed():
+    """An earlier layout is written where its memory is now, and refused if that no longer fits."""
+    pool = pool_of(16, 4, 4, 10)
+    args = dev([2, 0]), dev(np.arange(16).reshape(4, 4)), dev([5, 20, 40, 0]), dev([4] * 4), 2
+    want, out = pool.layout(*args), pool.layout(*args)
+    old = out.slots.data_ptr()
+    out.slots.set_(torch.full((2,), -7, dtype=torch.int64, device="cuda"))
+    assert out.slots.data_ptr() != old
+    assert pool.layout(*args, out=out) is out
+    pool.check()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    out.tables.set_(torch.zeros(1, 4, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        pool.layout(*args, out=out)
+
+
 def test_layout_on_another_stream():
     pool = pool_of(16, 4, 4, 10)
     t, ln, h = dev(np.arange(16).reshape(4, 4)), dev([5, 20, 40, 0]), dev([4] * 4)
