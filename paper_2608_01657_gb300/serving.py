@@ -171,15 +171,19 @@ class Server:
         s, R = self.s, hidden.shape[0]
         n = R * beams
         names = range(R, R + n)
+        if R + n > s.max_requests:
+            raise ValueError(f"prompts and beams need {R + n} rows of {s.max_requests}")
+        if beams > s.vocab - len(end):
+            raise ValueError("there must be as many tokens that end nothing as beams")
         if self.running.intersection(names):
             raise RuntimeError("the beams' rows are running: finish them first")
+        search = beam.BeamSearch(R, beams, s.vocab, torch.bfloat16, end)
         i32 = dict(dtype=torch.int32, device="cuda")
         children = torch.tensor(list(names), **i32)
         rows = children.view(R, beams)
         parents = torch.arange(R, **i32).repeat_interleave(beams)
         self.running.update(names)
         self.pool.fork(parents, children, self.lens[parents.long()] + 1, self.tables, self.lens, self.held, self.refs)
-        search = beam.BeamSearch(R, beams, s.vocab, torch.bfloat16, end)
         whole = lambda dtype: torch.empty(steps, R, beams, dtype=dtype, device="cuda")  # noqa: E731
         all_ = beam.Selection(*(whole(t) for t in (torch.int32, torch.int32, torch.float32) * 2))
         # a prompt has one beam at first
@@ -244,7 +248,8 @@ def main():
     third = server.admit(groups, prompts_of(groups, s, 2), room=0)
     found = server.beam_search(third["hidden"], beams=4, steps=6, end=[7])
     print("likeliest answers", found["sequences"][:, 0].tolist())
-    print("their mean log-probabilities", [round(float(x), 3) for x in found["scores"][:, 0] / 6])
+    tokens = found["lengths"][:, 0] + (found["lengths"][:, 0] < 6)  # with the end's
+    print("their mean log-probabilities", [round(float(x), 3) for x in found["scores"][:, 0] / tokens])
 
 
 if __name__ == "__main__":

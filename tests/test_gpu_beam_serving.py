@@ -91,6 +91,78 @@ def test_one_beam_is_greedy():
         server.beam_search(hidden, 1, 3)
 
 
+def test_searches_that_are_refused():
+    """Before anything is forked: too many rows, fewer tokens that go on than beams, what BeamSearch refuses."""
+    from paper_2608_01657_gb300 import serving as S
+    s = S.Shape(vocab=6)
+    server = S.Server(s, groups=2, seed=5)
+    hidden = server.admit([0, 1], S.prompts_of([0, 1], s, 5), room=0)["hidden"]
+    held, running = server.held.clone(), set(server.running)
+    for bad in (dict(beams=16), dict(beams=5, end=[1, 3]), dict(beams=0), dict(beams=2, end=[6]), dict(beams=2, end=[1, 1])):
+        with pytest.raises(ValueError):
+            server.beam_search(hidden, **(dict(steps=3) | bad))
+    assert torch.equal(held, server.held) and running == server.running
+    found = server.beam_search(hidden, 4, 3, [1, 3])
+    server.pool.check()
+    assert found["sequences"].shape == (2, 4, 3)
+
+
+def test_a_captured_step_is_the_eager_one():
+    """Selection, the beam step and the layout of what follows, in one graph, step after step."""
+    from paper_2608_01657_gb300 import beam
+    from paper_2608_01657_gb300 import kv as KV
+    R, B, V, ps, pages, width = 3, 4, 3000, 16, 200, 8
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    class Side:
+        def __init__(self):
+            self.k, self.v = (torch.zeros(1, pages, ps, 1, 64, device="cuda").bfloat16() for _ in range(2))
+            self.pool = KV.KVPool(self.k, self.v, num_q_heads=1, max_requests=R * B + 1, max_tokens=64, max_row_pages=width)
+            self.search = beam.BeamSearch(R, B, V, end_tokens=[5])
+            # every beam with 20 tokens: a page that all beams of a request share and one of its own
+            t = np.zeros((R * B, width), np.int64)
+            refs = np.zeros(pages, np.int64)
+            for i in range(R * B):
+                t[i, 0], t[i, 1] = i // B, R + i
+                refs[i // B] += 1
+                refs[R + i] += 1
+            self.t, self.refs = dev(t), dev(refs)
+            self.l, self.h = dev([20] * (R * B)), dev([2] * (R * B))
+            self.rows = dev(np.arange(R * B).reshape(R, B))
+            self.x = torch.zeros(R, B, V, device="cuda").bfloat16()
+            self.scores = torch.zeros(R, B, device="cuda")
+            self.out, self.at = None, None
+
+        def step(self):
+            self.out = self.search.select(self.x, self.scores, out=self.out)
+            self.pool.reorder(self.rows, self.out.parents, self.t, self.l, self.h, self.refs)
+            self.at = self.pool.layout(self.rows.view(-1), self.t, self.l, self.h, R * B + 3, pad=True, out=self.at)
+            self.l += 1
+            self.scores.copy_(self.out.scores)
+
+        def all(self):
+            return [*self.out, *self.at, self.t, self.l, self.h, self.refs, self.scores]
+
+    eager, graph = Side(), Side()
+    g = torch.Generator("cuda").manual_seed(2)
+    replay = None
+    for i in range(40):
+        eager.x.copy_(torch.randn(R, B, V, device="cuda", generator=g))
+        graph.x.copy_(eager.x)
+        eager.step()
+        if i == 1:  # (captured, not run)
+            torch.cuda.synchronize()
+            replay = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(replay):
+                graph.step()
+        replay.replay() if replay else graph.step()
+        for side in (eager, graph):
+            side.pool.check()
+            side.search.check()
+        assert all(torch.equal(a, b) for a, b in zip(eager.all(), graph.all()))
+        assert (eager.l == 21 + i).all() and int(eager.refs.sum()) == int(eager.h.sum())
+
+
 def test_the_example_searches(capsys):
     from paper_2608_01657_gb300 import serving as S
     S.main()
