@@ -373,6 +373,19 @@ def test_trace(T, R, B, N):
         assert (got.cpu().numpy() == trace_plain(tokens, parents, beams, ln)).all()
 
 
+@pytest.mark.parametrize("T,B,N", [(1537, 32, 64), (1537, 31, 1), (900, 4, 64), (129, 5, 7)])
+def test_traces_of_every_length(T, B, N):
+    """Hypotheses that end at every step, those at the borders of what fits into shared memory among them."""
+    r = np.random.RandomState(T + B)
+    R = T // N + 1
+    tokens, parents = r.randint(0, 1 << 24, (T, R, B)), r.randint(0, B, (T, R, B))
+    beams, lengths = r.randint(0, B, (R, N)), np.minimum(np.arange(R * N), T).reshape(R, N)
+    h = search(R, B, 100)
+    got = h.trace(dev(tokens), dev(parents), dev(beams), lengths=dev(lengths))
+    h.check()
+    assert (got.cpu().numpy() == trace_plain(tokens, parents, beams, lengths)).all()
+
+
 def test_bad_traces_are_reported():
     T, R, B, N = 100, 2, 3, 4
     r = np.random.RandomState(1)
