@@ -220,6 +220,9 @@ struct PageHdr {
   int32_t live;    // pages in use (compact)
   int32_t free_pages;
   int32_t refused; // an error that a reorder's kernels found (back to 0 after each call)
+  int32_t need;    // pages that a reorder takes
+  int32_t parts;   // rows of a reorder that copy a page, as they are found (back to 0 after each call)
+  int32_t copies;  // and all of them
 };
 constexpr int kScanThreads = 256;
 constexpr int kMaxChunks = 1024;  // chunks of the reference array: one CTA each
@@ -247,6 +250,7 @@ struct __align__(16) ReorderRec {
 };
 struct ReorderScratch {
   ReorderRec* rec;  // [max_requests]
+  int32_t* copy;    // [max_requests] the rows that copy a page, in any order
   int32_t* delta;   // [private pages] changes of the references, 0 between calls
   int32_t* refs;    // [private pages] the references to be, the page calls' inv
 };

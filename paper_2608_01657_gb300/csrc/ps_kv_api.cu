@@ -137,6 +137,7 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
   if (layout) *layout = y;
   ReorderScratch o{};
   o.rec = cv.take<ReorderRec>((size_t)R);
+  o.copy = cv.take<int32_t>((size_t)R);
   o.delta = cv.take<int32_t>((size_t)np);
   o.refs = w.inv;
   if (reorder) *reorder = o;

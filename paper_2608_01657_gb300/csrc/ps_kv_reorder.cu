@@ -7,12 +7,18 @@
 // the last pages by 0, or by -1 where c = 0: no sum depends on an order, and a page
 // that reaches 0 is free for this very call (nothing reads it any more).
 //
-// Three kernels: the first checks the rows and adds up the changes, one CTA for 256
-// columns of a request's rows; the second applies them to a copy of the references,
-// lists the free pages, and its last CTA decides whether the call goes ahead; the
-// third writes tables, lengths and references and copies the partial pages.  A
-// column of the tables is read and rewritten by one thread, so the rows are
-// permuted in place.
+// Three kernels: the first checks the rows, adds up the changes, one CTA for 256
+// columns of a request's rows, and lists the copies; the second applies the changes to
+// a copy of the references and lists the free pages, and its last CTA decides whether
+// the call goes ahead; the third writes tables, lengths and references and copies the
+// partial pages.  A column of the tables is read and rewritten by one thread, so the
+// rows are permuted in place.
+//
+// Bound by latency: chains of dependent reads (parent, length, page, reference, change;
+// free pages, their sums; new page, its tokens) in kernels that follow one another.
+// Each reads what it can before it waits for the one before it.  One request of four
+// beams takes 7.5 us; 64 of eight beams of 2048 tokens, whose copies are 21 MB (3.2 us),
+// 15.5: 4.5 for the changes, 4.7 to the verdict, 3 to 5 for the copies.
 #include "ps_kv_pages.cuh"
 
 namespace pskv {
@@ -22,6 +28,7 @@ constexpr int kCols = kScanThreads;  // columns that a CTA takes at a time
 constexpr int kColCtas = 64;         // CTAs of a request at most
 constexpr int kAtOnce = 8;           // beams whose ids a thread reads together
 constexpr int kNoPage = -1;
+constexpr int kRoom = 3;             // CTAs of the last kernel on an SM
 
 struct Args {
   const int32_t *rows, *parents;
@@ -33,13 +40,13 @@ struct Args {
   int32_t n, beams, grow, num_rows, row_pages, col_ctas;
 };
 
-// col_ctas CTAs a request.
+// Of a request: col_ctas CTAs for the changes, and one for the rows.
 __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScratch w, ReorderScratch o, Args a) {
   __shared__ int s_row[PS_KV_MAX_BEAMS], s_parent[PS_KV_MAX_BEAMS], s_len[PS_KV_MAX_BEAMS], s_held[PS_KV_MAX_BEAMS];
   __shared__ int s_children[PS_KV_MAX_BEAMS];
   chain();
-  const int B = a.beams, b = threadIdx.x, y = blockIdx.x % a.col_ctas;
-  const int64_t i0 = (int64_t)(blockIdx.x / a.col_ctas) * B;
+  const int B = a.beams, b = threadIdx.x, y = blockIdx.x % (a.col_ctas + 1);
+  const int64_t i0 = (int64_t)(blockIdx.x / (a.col_ctas + 1)) * B;
   bool ok = true;
   if (b < B) {
     const int row = a.rows[i0 + b], parent = a.parents[i0 + b];
@@ -58,7 +65,7 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
     s_children[b] = 0;
   }
   ok = __syncthreads_and(ok);
-  if (ok) {
+  if (ok && y < a.col_ctas) {
     if (b < B && s_parent[b] >= 0) atomicAdd(&s_children[s_parent[b]], 1);
     __syncthreads();
     int most = 0;
@@ -103,42 +110,48 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
       }
       if (change != 0 && at >= p.first_page) atomicAdd(o.delta + (at - p.first_page), change);
     }
-    if (y == 0) {
-      // a row is named once
-      for (int64_t j = threadIdx.x; j < a.n; j += kScanThreads) {
-        const int row = a.rows[j];
-        for (int q = 0; q < B; ++q)
-          if (j != i0 + q && row == s_row[q]) ok = false;
+  } else if (y == a.col_ctas) {
+    ReorderRec r{};
+    int need = 0;
+    if (ok && b < B) {
+      const int q = s_parent[b];
+      r.row = s_row[b];
+      r.src = q;
+      if (q >= 0) {
+        bool heir = true;
+        for (int j = 0; j < b; ++j) heir = heir && s_parent[j] != q;
+        r.len = s_len[q];
+        const int64_t total = ((int64_t)r.len + a.grow + p.page_size - 1) >> p.page_log2;
+        r.have = heir ? s_held[q] : r.len >> p.page_log2;
+        if (total > a.row_pages) ok = false;
+        r.total = total > r.have ? (int)total : r.have;
+        need = ok ? r.total - r.have : 0;
+        r.part = heir ? 0 : r.len & (p.page_size - 1);
+        r.from = r.part ? a.tables[s_row[q] * a.stride + r.have] : 0;
       }
-      if (b < B) {
-        ReorderRec r{};
-        const int q = s_parent[b];
-        r.row = s_row[b];
-        r.src = q;
-        int need = 0;
-        if (q >= 0) {
-          bool heir = true;
-          for (int j = 0; j < b; ++j) heir = heir && s_parent[j] != q;
-          r.len = s_len[q];
-          const int64_t total = ((int64_t)r.len + a.grow + p.page_size - 1) >> p.page_log2;
-          r.have = heir ? s_held[q] : r.len >> p.page_log2;
-          if (total > a.row_pages) ok = false;
-          r.total = total > r.have ? (int)total : r.have;
-          need = ok ? r.total - r.have : 0;
-          r.part = heir ? 0 : r.len & (p.page_size - 1);
-          r.from = r.part ? a.tables[s_row[q] * a.stride + r.have] : 0;
-        }
-        o.rec[i0 + b] = r;
-        w.need[i0 + b] = need;
-      }
+      o.rec[i0 + b] = r;
     }
-  } else if (y == 0 && b < B) {
-    w.need[i0 + b] = 0;
+    if (b < B) w.need[i0 + b] = need;
+    static_assert(PS_KV_MAX_BEAMS == 32, "a warp's");
+    if (b < 32) {
+      const unsigned m = __ballot_sync(0xFFFFFFFFu, r.part > 0);
+      int to = 0;
+      if (b == 0 && m) to = atomicAdd(&w.hdr->parts, __popc(m));
+      to = __shfl_sync(0xFFFFFFFFu, to, 0) + __popc(m & ((1u << b) - 1));
+      if (r.part > 0) o.copy[to] = (int)i0 + b;
+    }
+    // a row is named once
+    for (int64_t j = threadIdx.x; j < a.n; j += kScanThreads) {
+      const int row = a.rows[j];
+      for (int q = 0; q < B; ++q)
+        if (j != i0 + q && row == s_row[q]) ok = false;
+    }
   }
   if (!ok) atomicMin(&w.hdr->refused, (int32_t)PS_ERR_INVALID_ARG);
 }
 
-// CTA c: chunk c of the references.  These are read before the wait for
+// CTA c: chunk c of the references; the last one: the pages that the rows need.  The
+// references are read before the wait for
 // k_reorder_scan, which only reads them and lets this kernel start when all that came
 // before it is done.  (Without requests there is no such kernel, and what came before
 // may write them.)
@@ -146,10 +159,23 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScrat
   const int64_t np = p.num_pages - p.first_page;
   const int64_t c0 = (int64_t)blockIdx.x * w.chunk_size;
   const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
+  const bool chunk = (int)blockIdx.x < w.chunks;
   int count = 0;
   bool ok = true;
-  if (a.n == 0) chain();
-  for (int64_t i0 = c0; i0 < c1 || i0 == c0; i0 += kTile) {
+  if (a.n == 0 || !chunk) chain();
+  if (!chunk) {
+    int64_t need = 0;
+    for (int i0 = 0; i0 < a.n; i0 += kScanThreads) {
+      const int i = i0 + threadIdx.x;
+      int64_t tot;
+      const int64_t e = block_scan<int64_t>(i < a.n ? __ldcg(w.need + i) : 0, &tot);
+      const int64_t s = need + e;
+      if (i < a.n) w.start[i] = s < 0x7FFFFFFF ? (int)s : 0x7FFFFFFF;
+      need += tot;
+    }
+    if (threadIdx.x == 0) w.hdr->need = need < 0x7FFFFFFF ? (int)need : 0x7FFFFFFF;
+  }
+  for (int64_t i0 = c0; chunk && (i0 < c1 || i0 == c0); i0 += kTile) {
     int r[kEach], rank[kEach], tot;
     bool free[kEach];
 #pragma unroll
@@ -177,25 +203,17 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_free(Pool p, PageScrat
     }
     count += tot;
   }
-  if (threadIdx.x == 0) w.chunk_cnt[blockIdx.x] = count;
+  if (threadIdx.x == 0 && chunk) w.chunk_cnt[blockIdx.x] = count;
   if (!ok) atomicMin(&w.hdr->refused, (int32_t)PS_ERR_INVALID_ARG);
   if (!last_cta(&w.hdr->done)) return;
+  const int refused = __ldcg(&w.hdr->refused), need = __ldcg(&w.hdr->need), copies = __ldcg(&w.hdr->parts);
   const int free_pages = scan_array(w.chunk_cnt, w.chunk_base, w.chunks);
-  int64_t need = 0;
-  for (int i0 = 0; i0 < a.n; i0 += kScanThreads) {
-    const int i = i0 + threadIdx.x;
-    int64_t tot;
-    const int64_t e = block_scan<int64_t>(i < a.n ? __ldcg(w.need + i) : 0, &tot);
-    const int64_t s = need + e;
-    if (i < a.n) w.start[i] = s < 0x7FFFFFFF ? (int)s : 0x7FFFFFFF;
-    need += tot;
-  }
   if (threadIdx.x == 0) {
-    const int refused = __ldcg(&w.hdr->refused);
     const int st = refused ? refused : (need > free_pages ? PS_ERR_CAPACITY : PS_OK);
-    w.hdr->refused = 0;
+    w.hdr->refused = w.hdr->parts = 0;
     w.hdr->status = st;
-    w.hdr->free_pages = st == PS_OK ? (int)need : 0;  // taken
+    w.hdr->copies = copies;
+    w.hdr->free_pages = st == PS_OK ? need : 0;  // taken
     if (st != PS_OK) set_error(a.status, st);
   }
 }
@@ -213,12 +231,12 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScra
   __shared__ int base[kMaxChunks];
   __shared__ ReorderRec s_rec[PS_KV_MAX_BEAMS];
   __shared__ int s_start[PS_KV_MAX_BEAMS];
-  __shared__ int ids[PS_KV_MAX_BEAMS][kCols];
+  extern __shared__ int ids[][kCols];  // [beams]; no more, so that an SM has room for 8 CTAs of few beams
   const int B = a.beams, requests = a.n / B, tables = requests * a.col_ctas;
   int cta = blockIdx.x;
   if (cta < w.chunks) {
     chain();
-    const int st = w.hdr->status;
+    const int st = __ldcg(&w.hdr->status);
     const int64_t np = p.num_pages - p.first_page, c0 = (int64_t)cta * w.chunk_size;
     const int64_t c1 = c0 + w.chunk_size < np ? c0 + w.chunk_size : np;
     if (st != PS_OK) {
@@ -259,9 +277,10 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScra
     };
     if (k < most) read();
     chain();
-    if (w.hdr->status != PS_OK) return;
+    const int status = __ldcg(&w.hdr->status);
     for (int c = threadIdx.x; c < w.chunks; c += kScanThreads) base[c] = w.chunk_base[c];
-    if (b < B) s_start[b] = w.start[(int64_t)r * B + b];
+    if (b < B) s_start[b] = __ldcg(w.start + (int64_t)r * B + b);
+    if (status != PS_OK) return;
     __syncthreads();
     for (; k < most; k += a.col_ctas * kCols) {
       if (k >= a.col_ctas * kCols) read();
@@ -281,23 +300,33 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_apply(Pool p, PageScra
   }
   cta -= tables;
   const int parts = copy_parts(p, p.page_size), slices = 2 * p.num_layers;
-  const int64_t units = (int64_t)a.n * slices * parts, step = ((int64_t)gridDim.x - w.chunks - tables) * kCopyWarps;
+  const int64_t step = ((int64_t)gridDim.x - w.chunks - tables) * kCopyWarps;
   int64_t u = (int64_t)cta * kCopyWarps + (threadIdx.x >> 5);
-  ReorderRec x{};
-  if (u < units) x = record(o, u / (slices * parts));
+  auto row = [&]() {  // of unit u; where there are fewer, any row's
+    const int64_t c = u / (slices * parts);
+    const int i = c < a.n ? __ldcg(o.copy + c) : 0;
+    return i >= 0 && i < a.n ? i : 0;
+  };
+  int i = row();
+  ReorderRec x = record(o, i);
   chain();
-  if (w.hdr->status != PS_OK) return;
+  // all that the first copy needs side by side
+  const int status = __ldcg(&w.hdr->status), copies = __ldcg(&w.hdr->copies);
+  int start = __ldcg(w.start + i);
   for (int c = threadIdx.x; c < w.chunks; c += kScanThreads) base[c] = w.chunk_base[c];
+  if (status != PS_OK) return;
+  const int64_t units = (int64_t)copies * slices * parts;
+  if ((int64_t)cta * kCopyWarps >= units) return;
   __syncthreads();
   while (u < units) {
-    const int64_t i = u / (slices * parts);
     const int rest = (int)(u % (slices * parts));
-    if (x.part > 0) {
-      const int64_t to = p.first_page + free_page(w, base, w.start[i]);
-      copy_part(p, x.from, to, rest / parts, x.part, rest % parts, threadIdx.x & 31);
-    }
+    const int64_t to = p.first_page + free_page(w, base, start);
+    copy_part(p, x.from, to, rest / parts, x.part, rest % parts, threadIdx.x & 31);
     u += step;
-    if (u < units) x = record(o, u / (slices * parts));
+    if (u >= units) break;
+    i = row();
+    x = record(o, i);
+    start = __ldcg(w.start + i);
   }
 }
 
@@ -314,13 +343,15 @@ int32_t launch_reorder(const Pool& p, const PageScratch& w, const ReorderScratch
   a.col_ctas = (row_pages + kCols - 1) / kCols;
   if (a.col_ctas > kColCtas) a.col_ctas = kColCtas;
   cudaError_t e = cudaSuccess;
-  if (requests > 0) e = launch(k_reorder_scan, dim3((unsigned)(requests * a.col_ctas)), kScanThreads, 0, st, p, w, o, a);
-  if (e == cudaSuccess) e = launch(k_reorder_free, dim3((unsigned)w.chunks), kScanThreads, 0, st, p, w, o, a);
+  if (requests > 0) e = launch(k_reorder_scan, dim3((unsigned)(requests * (a.col_ctas + 1))), kScanThreads, 0, st, p, w, o, a);
+  if (e == cudaSuccess) e = launch(k_reorder_free, dim3((unsigned)w.chunks + 1), kScanThreads, 0, st, p, w, o, a);
   if (e != cudaSuccess) return status_of(e);
   const int64_t units = (int64_t)a.n * 2 * p.num_layers * copy_parts(p, p.page_size);
-  const int64_t want = (units + kCopyWarps - 1) / kCopyWarps, most = (int64_t)nsm * 8;
-  const int64_t grid = w.chunks + (int64_t)requests * a.col_ctas + (want < most ? want : most);
-  return status_of(launch(k_reorder_apply, dim3((unsigned)grid), kScanThreads, 0, st, p, w, o, a));
+  // of the copies as many as an SM has room for with the others, three CTAs in all
+  const int64_t others = w.chunks + (int64_t)requests * a.col_ctas, room = (int64_t)nsm * kRoom - others;
+  const int64_t want = (units + kCopyWarps - 1) / kCopyWarps, most = room > nsm ? room : nsm;
+  const int64_t grid = others + (want < most ? want : most);
+  return status_of(launch(k_reorder_apply, dim3((unsigned)grid), kScanThreads, (size_t)beams * kCols * 4, st, p, w, o, a));
 }
 
 }  // namespace pskv
