@@ -761,21 +761,12 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_co
     for (int j = 0; j < s_tokens; ++j) place += s_token[j].before(x);
     if (place < B) s_chosen[place] = x;
   }
-  __syncthreads();
-  if (t < B) {
-    const Cand x = s_chosen[t];
-    const bool on = x.somebody();
-    g.a.tokens[to + t] = on ? (int)(x.tie & 0xFFFFFFFF) : -1;
-    g.a.parents[to + t] = on ? (int)(x.tie >> 32) : -1;
-    g.a.scores_out[to + t] = on ? x.value() : -INFINITY;
-  }
-  if (!g.a.ended_tokens) return;
   // an end token's place among all candidates, and among those of its kind
   if (end_beam < B) {
     const Cand x = s_end[t];
     int place = 0, others = 0;
     for (int j = 0; j < B * E; ++j) place += s_end[j].before(x);
-    for (int j = 0; j < B; ++j) others += s_chosen[j].before(x);
+    for (int j = 0; j < s_tokens; ++j) others += s_token[j].before(x);
     if (x.somebody() && place + others < B) {
       atomicAdd(&s_ended, 1);
       g.a.ended_tokens[to + place] = (int)(x.tie & 0xFFFFFFFF);
@@ -784,7 +775,14 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_co
     }
   }
   __syncthreads();
-  if (t < B && t >= s_ended) {
+  if (t < B) {
+    const Cand x = s_chosen[t];
+    const bool on = x.somebody();
+    g.a.tokens[to + t] = on ? (int)(x.tie & 0xFFFFFFFF) : -1;
+    g.a.parents[to + t] = on ? (int)(x.tie >> 32) : -1;
+    g.a.scores_out[to + t] = on ? x.value() : -INFINITY;
+  }
+  if (g.a.ended_tokens && t < B && t >= s_ended) {
     g.a.ended_tokens[to + t] = g.a.ended_parents[to + t] = -1;
     g.a.ended_scores[to + t] = -INFINITY;
   }
