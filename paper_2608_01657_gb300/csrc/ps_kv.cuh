@@ -256,10 +256,11 @@ struct ReorderScratch {
 };
 
 // ---- layout --------------------------------------------------------------------
-// Of batches of more than kLayoutPart requests: offsets and groups from a part's
-// first on, the parts' totals, and where each part begins.
-constexpr int kLayoutPart = 1024;
+// Of batches that a CTA does not scan for itself: the requests, offsets and groups from
+// a part's first on, the parts' totals, and where each part begins.
+constexpr int kLayoutPart = 256;
 struct LayoutScratch {
+  int4* item;               // [max_requests] row, start, count, offset
   int32_t *offset, *group;  // [max_requests], the page calls' start and need
   int64_t* total;           // [parts]
   int32_t* groups;          // [parts]

@@ -130,6 +130,7 @@ size_t carve(const ps_kv_config_t& c, const int32_t workers[kLists], char* base,
   y.offset = w.start;
   y.group = w.need;
   y.done = &w.hdr->done;
+  y.item = cv.take<int4>((size_t)R);
   y.total = cv.take<int64_t>(parts);
   y.groups = cv.take<int32_t>(parts);
   y.base = cv.take<int32_t>(parts + 1);

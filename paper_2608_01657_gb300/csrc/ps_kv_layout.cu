@@ -7,29 +7,32 @@
 // Integers only: bound by latency, a chain of three reads (a request's row, the
 // row's length, a page id) around a scan.  Up to kFused requests every CTA scans
 // all of them for itself, so that the call is one launch; of more, a first kernel
-// scans 1024 requests a CTA, its last CTA the totals.  The rest is a list of units
+// scans 256 requests a CTA, its last CTA the totals.  The rest is a list of units
 // of equal size for the warps: 128 columns of a request's table, 128 tokens.  A
 // token finds its request by bisection of the offsets.
 //
 // Each read of the chain is 0.6 to 0.8 us from L2, a launch 2 to 3: decoding 256
-// requests of up to 4096 tokens takes 4.9 us, the prompts of 64 requests (31,000
-// tokens) 4.2, drafted tokens of 333 requests, padded, 5.0.  The runs of requests
-// that share a prefix cost nothing beside the tables, as CTA 0 compares the ids while
-// the others fill: a thread one of the leading ids of neighbouring requests, 8 or 24
-// of them side by side (a pair of ids a thread, 8 at a time, took 2.4 us longer for
-// the drafted tokens).
+// requests of up to 4096 tokens takes 4.3 us, the prompts of 64 requests (49,000
+// tokens) 3.8, drafted tokens of 333 requests, padded, 4.7, and two kernels for 3000
+// decoding requests 14.  The runs of requests that share a prefix cost nothing beside
+// the tables, as CTA 0 compares the ids while the others fill: a thread one of the
+// leading ids of neighbouring requests, 8 or 24 of them side by side (a pair of ids a
+// thread, 8 at a time, took 2.4 us longer for the drafted tokens).  A lane's four
+// tokens go through each read together.  8 CTAs an SM in place of 4 took 1 us longer
+// for 3000 requests: each reads all offsets.
 #include "ps_kv_pages.cuh"
 
 namespace pskv {
 namespace {
 
-constexpr int kFused = kLayoutPart;
+constexpr int kFused = 1024;             // requests that every CTA scans for itself
+constexpr int kNear = 8192;              // and whose offsets every CTA takes to shared memory
 constexpr int kItems = kFused / kScanThreads;
 constexpr int kUnit = 128;               // columns or tokens of a warp's unit
 constexpr int kUnitsPerCta = kScanThreads / 32;
 
 // The total of requests of which one is out of range: more than any real total (2^18
-// requests of 2^30 tokens), and 2^8 of them add up.
+// requests of 2^30 tokens), and 2^10 of them, one a part, add up.
 constexpr int64_t kBad = 1ll << 50;
 
 struct Args {
@@ -78,27 +81,37 @@ __device__ __forceinline__ bool items_of(const Args& a, int i, int step, int n, 
   }
   return ok;
 }
-// Request i; false, and no tokens, if its row or its numbers are out of range.
-__device__ __forceinline__ bool item_of(const Args& a, int i, Item* it) {
-  const int row = a.l.rows ? a.l.rows[i] : i;
-  *it = Item{-1, 0, 0};
-  if (row < 0 || row >= a.num_rows) return false;
-  const int start = a.l.starts ? a.l.starts[i] : a.lens[row], count = a.l.counts ? a.l.counts[i] : 1;
-  const int held = a.held[row];
-  if (start < 0 || count < 0 || held < 0 || held > a.row_pages) return false;
-  if ((int64_t)start + count > (int64_t)held << a.page_log2) return false;
-  *it = Item{row, start, count};
-  return true;
+// May a request share a prefix with its neighbours?
+__device__ __forceinline__ bool fits(const Args& a, const Item& x) {
+  return x.row >= 0 && x.start >= a.lead << a.page_log2 && x.count <= a.most;
 }
-// Do requests i and i - 1 share a prefix that is worth reading once?
-__device__ __forceinline__ bool joined(const Args& a, const Item& x, const Item& y) {
-  const int least = a.lead << a.page_log2;
-  if (x.row < 0 || y.row < 0 || x.start < least || y.start < least || x.count > a.most || y.count > a.most) return false;
-  const int32_t *p = a.tables + x.row * a.stride, *q = a.tables + y.row * a.stride;
-  bool same = true;
-#pragma unroll 8
-  for (int k = 0; k < a.lead; ++k) same = same && p[k] == q[k];
-  return same;
+// Marks the requests of first..n - 1 whose leading ids differ from those of the one before
+// them.  rows: -1 where a request does not share.  A thread takes one of the ids, of
+// neighbouring requests, whose ids it reads side by side.
+__device__ __forceinline__ void compare_leads(const Args& a, const int* rows, unsigned char* differs, int first, int n) {
+  const int threads = kScanThreads >> a.lead_log2, each = (n - first + threads - 1) / threads, k = threadIdx.x & (a.lead - 1);
+  const int begin = first + (threadIdx.x >> a.lead_log2) * each, end = min(n, begin + each);
+  auto id = [&](int row) { return row >= 0 ? a.tables[row * a.stride + k] : 0; };
+  int before = begin > 0 && begin < end ? rows[begin - 1] : -1, last = id(before);
+  auto compare = [&](int i0, auto count) {
+    constexpr int kIds = decltype(count)::value;
+    int row[kIds], x[kIds];
+#pragma unroll
+    for (int u = 0; u < kIds; ++u) {
+      row[u] = i0 + u < end ? rows[i0 + u] : -1;
+      x[u] = id(row[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kIds; ++u) {
+      if (before >= 0 && row[u] >= 0 && x[u] != last) differs[i0 + u] = 1;
+      before = row[u];
+      last = x[u];
+    }
+  };
+  for (int i = begin; i < end;) {  // (256 requests have 8 a thread where pages are of 16)
+    if (end - i > 8) compare(i, Count<24>()), i += 24;
+    else compare(i, Count<8>()), i += 8;
+  }
 }
 
 // The offsets of all requests, in shared memory.
@@ -109,16 +122,21 @@ struct Near {
   __device__ __forceinline__ int offset(int i) const { return off[i]; }
   __device__ __forceinline__ Item at(const Args&, int i) const { return item[i]; }
 };
-// In the workspace, each CTA's part from 0 on.
+// The offsets in shared memory, the requests in the workspace.
 struct Far {
-  const int32_t *local, *base;
+  const int* off;
+  const int4* item;
   int n;
-  __device__ __forceinline__ int offset(int i) const { return i < n ? local[i] + base[i / kFused] : base[(n + kFused - 1) / kFused]; }
-  __device__ __forceinline__ Item at(const Args& a, int i) const {
-    Item it;
-    item_of(a, i, &it);
-    return it;
+  __device__ __forceinline__ int offset(int i) const { return off[i]; }
+  __device__ __forceinline__ Item at(const Args&, int i) const {
+    const int4 x = item[i];
+    return {x.x, x.y, x.z};
   }
+};
+// Both in the workspace, each part's offsets from 0 on.
+struct Farther : Far {
+  const int32_t *local, *base;
+  __device__ __forceinline__ int offset(int i) const { return i < n ? local[i] + base[i / kLayoutPart] : base[(n + kLayoutPart - 1) / kLayoutPart]; }
 };
 
 // 'over': the batch is left out, for a request out of range or more tokens than there is room for.
@@ -145,26 +163,41 @@ __device__ __forceinline__ void fill(const Args& a, const O& o, bool over, int c
       }
     } else {
       const int64_t t0 = (u - rows * chunks) * kUnit + lane;
+      constexpr int kEachLane = kUnit / 32;
+      int of[kEachLane], pos[kEachLane], id[kEachLane], from[kEachLane];
 #pragma unroll
-      for (int j = 0; j < kUnit / 32; ++j) {
+      for (int j = 0; j < kEachLane; ++j) {  // the last request that begins at or before t; empty ones lie before it
+        const int64_t t = t0 + 32 * j;
+        int lo = 0, hi = t < total ? n - 1 : 0;
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) / 2;
+          if (o.offset(mid) <= t) lo = mid;
+          else hi = mid - 1;
+        }
+        of[j] = lo;
+      }
+#pragma unroll
+      for (int j = 0; j < kEachLane; ++j) {
+        const int64_t t = t0 + 32 * j;
+        pos[j] = from[j] = 0;
+        id[j] = -1;
+        if (t < total) {
+          const Item it = o.at(a, of[j]);
+          pos[j] = it.start + (int)t - o.offset(of[j]);
+          id[j] = a.tables[it.row * a.stride + (pos[j] >> a.page_log2)];
+          from[j] = l.written ? l.written[of[j]] : it.start;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kEachLane; ++j) {
         const int64_t t = t0 + 32 * j;
         if (t >= l.num_tokens) break;
-        int pos = 0;
         int64_t slot = -1;
         if (t < total) {
-          int lo = 0, hi = n - 1;  // the last request that begins at or before t; empty ones lie before it
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (o.offset(mid) <= t) lo = mid;
-            else hi = mid - 1;
-          }
-          const Item it = o.at(a, lo);
-          pos = it.start + (int)t - o.offset(lo);
-          const int id = a.tables[it.row * a.stride + (pos >> a.page_log2)];
-          if (id < 0 || id >= a.num_pages) set_error(a.status, PS_ERR_INVALID_ARG);
-          else if (pos >= (l.written ? l.written[lo] : it.start)) slot = ((int64_t)id << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
+          if (id[j] < 0 || id[j] >= a.num_pages) set_error(a.status, PS_ERR_INVALID_ARG);
+          else if (pos[j] >= from[j]) slot = ((int64_t)id[j] << a.page_log2) + (pos[j] & ((1 << a.page_log2) - 1));
         }
-        l.positions[t] = pos;
+        l.positions[t] = pos[j];
         l.slots[t] = slot;
       }
     }
@@ -227,34 +260,9 @@ __global__ void __launch_bounds__(kScanThreads) k_layout(Args a) {
   }
   int groups = 0;
   if (l.group_offsets) {
-    // the leading ids of a request and of the one before it: a thread takes one of the
-    // ids, of neighbouring requests
-    auto fits = [&](int i) { return item[i].start >= a.lead << a.page_log2 && item[i].count <= a.most; };
-    for (int i = tid; i < n; i += kScanThreads) lead_row[i] = fits(i) ? item[i].row : -1;
+    for (int i = tid; i < n; i += kScanThreads) lead_row[i] = fits(a, item[i]) ? item[i].row : -1;
     __syncthreads();
-    const int threads = kScanThreads >> a.lead_log2, each = (n + threads - 1) / threads, k = tid & (a.lead - 1);
-    const int first = (tid >> a.lead_log2) * each, end = over ? 0 : min(n, first + each);
-    auto id = [&](int row) { return row >= 0 ? a.tables[row * a.stride + k] : 0; };
-    int before = first > 0 && first < end ? lead_row[first - 1] : -1, last = id(before);
-    auto compare = [&](int i0, auto count) {
-      constexpr int kIds = decltype(count)::value;
-      int row[kIds], x[kIds];
-#pragma unroll
-      for (int u = 0; u < kIds; ++u) {
-        row[u] = i0 + u < end ? lead_row[i0 + u] : -1;
-        x[u] = id(row[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < kIds; ++u) {
-        if (before >= 0 && row[u] >= 0 && x[u] != last) differs[i0 + u] = 1;
-        before = row[u];
-        last = x[u];
-      }
-    };
-    for (int i = first; i < end;) {  // (256 requests have 8 a thread where pages are of 16)
-      if (end - i > 8) compare(i, Count<24>()), i += 24;
-      else compare(i, Count<8>()), i += 8;
-    }
+    compare_leads(a, lead_row, differs, 0, over ? 0 : n);
     __syncthreads();
     int begins = 0;
 #pragma unroll
@@ -271,41 +279,40 @@ __global__ void __launch_bounds__(kScanThreads) k_layout(Args a) {
   if (tid == 0) ends(a, over, over ? 0 : (int)total, groups);
 }
 
-// Many requests: kFused a CTA.  Their offsets and groups from the CTA's first on,
-// and the CTA's totals, which the last CTA turns into offsets.
+// Many requests: a part of them a CTA, one a thread.  Their offsets and groups from the
+// CTA's first on, and the CTA's totals, which the last CTA turns into offsets.
 __global__ void __launch_bounds__(kScanThreads) k_layout_scan(Args a) {
+  static_assert(kLayoutPart == kScanThreads, "one a thread");
+  __shared__ int lead_row[kLayoutPart + 1];  // of the request before the part, and the part's
+  __shared__ unsigned char differs[kLayoutPart + 1];
   chain();
   const ps_kv_layout_t& l = a.l;
-  const int n = l.num_requests, i0 = blockIdx.x * kFused + threadIdx.x * kItems;
-  Item it[kItems], before{-1, 0, 0};
-  int64_t sum = 0;
-  int begins = 0;
-  bool bad = false;
-  if (i0 > 0 && i0 < n) item_of(a, i0 - 1, &before);
-#pragma unroll
-  for (int j = 0; j < kItems; ++j) {
-    it[j] = Item{-1, 0, 0};
-    if (i0 + j < n) {
-      bad |= !item_of(a, i0 + j, &it[j]);
-      if (l.group_offsets && (i0 + j == 0 || !joined(a, it[j], j ? it[j ? j - 1 : 0] : before))) begins |= 1 << j;
-    }
-    sum += it[j].count;
+  const int n = l.num_requests, tid = threadIdx.x, i0 = blockIdx.x * kLayoutPart, i = i0 + tid;
+  Item both[2];  // the thread's, after the one before the part in thread 0
+  const int step = tid == 0 && i0 > 0 ? 1 : 0;
+  bool bad = !items_of(a, i - step, step, n, both);
+  const Item it = both[1];
+  bool begins = i < n;
+  if (l.group_offsets) {
+    lead_row[tid + 1] = fits(a, it) ? it.row : -1;
+    differs[tid + 1] = 0;
+    if (tid == 0) lead_row[0] = step && fits(a, both[0]) ? both[0].row : -1;
+    __syncthreads();
+    compare_leads(a, lead_row, differs, 1, min(kLayoutPart, n - i0) + 1);
+    __syncthreads();
+    begins = i < n && (differs[tid + 1] || lead_row[tid + 1] < 0 || lead_row[tid] < 0);
   }
   int64_t total;
   int groups;
-  int64_t o = block_scan(sum, &total);
+  const int64_t o = block_scan((int64_t)it.count, &total);
   bad = __syncthreads_or(bad);
-  int g = block_scan(__popc(begins), &groups);
-#pragma unroll
-  for (int j = 0; j < kItems; ++j) {
-    const int i = i0 + j;
-    if (i < n) {
-      // a batch that is left out has offsets past 2^31 perhaps: none is looked at
-      a.w.offset[i] = (int32_t)(o < 0x7FFFFFFF ? o : 0x7FFFFFFF);
-      a.w.group[i] = begins >> j & 1 ? g : -1;
-    }
-    g += begins >> j & 1;
-    o += it[j].count;
+  const int g = block_scan((int)begins, &groups);
+  if (i < n) {
+    // a batch that is left out has offsets past 2^31 perhaps: none is looked at
+    const int32_t off = (int32_t)(o < 0x7FFFFFFF ? o : 0x7FFFFFFF);
+    a.w.item[i] = make_int4(it.row, it.start, it.count, 0);
+    a.w.offset[i] = off;
+    a.w.group[i] = begins ? g : -1;
   }
   if (threadIdx.x == 0) {
     a.w.total[blockIdx.x] = bad ? kBad : total;
@@ -338,26 +345,35 @@ __global__ void __launch_bounds__(kScanThreads) k_layout_scan(Args a) {
 __global__ void __launch_bounds__(kScanThreads) k_layout_fill(Args a) {
   chain();
   const ps_kv_layout_t& l = a.l;
-  const int n = l.num_requests, parts = (n + kFused - 1) / kFused;
-  const Far o{a.w.offset, a.w.base, n};
+  const int n = l.num_requests, parts = (n + kLayoutPart - 1) / kLayoutPart;
   const int total = a.w.base[parts], groups = a.w.group_base[parts];
-  const bool over = total > l.num_tokens;
+  const bool over = total > l.num_tokens, near = n <= kNear;
   const int64_t id = (int64_t)blockIdx.x * kScanThreads + threadIdx.x, step = (int64_t)gridDim.x * kScanThreads;
+  extern __shared__ int off[];
+  if (near) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kScanThreads) off[i] = a.w.offset[i] + a.w.base[i / kLayoutPart];
+    if (threadIdx.x == 0) off[n] = total;
+    __syncthreads();
+  }
+  const Far o{off, a.w.item, n};
+  const Farther far{o, a.w.offset, a.w.base};
   for (int64_t i = id; i < n; i += step) {
     const Item it = o.at(a, (int)i);
-    l.q_offsets[i] = over ? 0 : o.offset((int)i);
+    l.q_offsets[i] = over ? 0 : far.offset((int)i);
     l.kv_lens[i] = over ? 0 : it.start + it.count;
     if (l.group_offsets) {
       const int g = a.w.group[i];
       if (over) l.group_offsets[i] = (int)i;
-      else if (g >= 0) l.group_offsets[g + a.w.group_base[i / kFused]] = (int)i;
+      else if (g >= 0) l.group_offsets[g + a.w.group_base[i / kLayoutPart]] = (int)i;
     }
   }
   const int shown = over ? n : groups, all = n + (l.pad ? 1 : 0);
   if (l.group_offsets)
     for (int64_t g = shown + (l.pad ? 1 : 0) + id; g <= all; g += step) l.group_offsets[g] = all;
   if (id == 0) ends(a, over, over ? 0 : total, shown);
-  fill(a, o, over, blockIdx.x, gridDim.x);
+  if (near) fill(a, o, over, blockIdx.x, gridDim.x);
+  else fill(a, far, over, blockIdx.x, gridDim.x);
 }
 
 }  // namespace
@@ -379,8 +395,8 @@ int32_t launch_layout(const Pool& p, const LayoutScratch& w, const ps_kv_layout_
   const int64_t most = (int64_t)nsm * 4;
   const int grid = (int)(want < 1 ? 1 : (want > most ? most : want));
   if (n <= kFused) return status_of(launch(k_layout, dim3((unsigned)(grid + 1)), kScanThreads, 0, st, a));
-  cudaError_t e = launch(k_layout_scan, dim3((unsigned)((n + kFused - 1) / kFused)), kScanThreads, 0, st, a);
-  if (e == cudaSuccess) e = launch(k_layout_fill, dim3((unsigned)grid), kScanThreads, 0, st, a);
+  cudaError_t e = launch(k_layout_scan, dim3((unsigned)((n + kLayoutPart - 1) / kLayoutPart)), kScanThreads, 0, st, a);
+  if (e == cudaSuccess) e = launch(k_layout_fill, dim3((unsigned)grid), kScanThreads, n <= kNear ? 4 * (n + 1) : 0, st, a);
   return status_of(e);
 }
 

@@ -91,7 +91,7 @@ def test_layout(n, before, new, ps, ratio, pad, spare):
     equal(got, plain(rows, tables, lens, held, T, count, start, written, int(pad), ps, ratio))
 
 
-@pytest.mark.parametrize("n", [1025, 2048, 5000])
+@pytest.mark.parametrize("n", [1025, 2048, 5000, 9001])
 @pytest.mark.parametrize("pad", [False, True])
 def test_layout_of_many_requests(n, pad):
     """More than one CTA scans at once."""
