@@ -37,7 +37,9 @@ constexpr int kWarps = kWarpsPerSm, kThreads = 32 * kWarps;
 // the last ones ended 10 us behind the others, and a call of 128 requests took 66 us
 // instead of 57.  Registers as for 16 leave room for the next kernel's CTAs beside it.
 constexpr int kRoom = 512;
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+// Threads of the joining kernel's CTAs: few fit beside the first kernel's CTA, many are a
+// warp a beam.
+constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kVecs = 8;                 // 16-byte words of a run
 constexpr int kChunk = 32 * kVecs;       // words of a chunk, a run a lane
 constexpr int kStages = 3;               // chunks of a warp's ring
@@ -192,12 +194,19 @@ __device__ __forceinline__ uint64_t greatest_of(uint64_t a, uint64_t b, int keep
 // The keep-th of the lanes' numbers, or a little less: the five lowest bits are cleared.
 __device__ __forceinline__ uint32_t kth_of(uint32_t x, int keep, int lane) {
   x = (x & ~31u) | lane;  // no two are equal
-  uint32_t top = 0;
-  for (int k = 0; k < keep; ++k) {
-    top = __reduce_max_sync(kAll, x);
-    if (x == top) x = 0;
+  uint32_t end = 0;
+  if (keep <= 16) {
+    for (int k = 0; k < keep; ++k) {
+      end = __reduce_max_sync(kAll, x);
+      if (x == end) x = 0;
+    }
+  } else {  // from the other side
+    for (int k = 32; k >= keep; --k) {
+      end = __reduce_min_sync(kAll, x);
+      if (x == end) x = ~0u;
+    }
   }
-  return top & ~31u;
+  return end & ~31u;
 }
 
 // A warp's best so far.
@@ -594,7 +603,8 @@ struct Cand {
   long long score, tie;
   __device__ __forceinline__ bool before(const Cand& y) const { return score != y.score ? score > y.score : tie < y.tie; }
   __device__ __forceinline__ Cand shfl(int from) const { return {__shfl_sync(kAll, score, from), __shfl_sync(kAll, tie, from)}; }
-  __device__ __forceinline__ float value() const { return (float)__longlong_as_double(score < 0 ? score ^ 0x7FFFFFFFFFFFFFFFll : score); }
+  __device__ __forceinline__ double exact() const { return __longlong_as_double(score < 0 ? score ^ 0x7FFFFFFFFFFFFFFFll : score); }
+  __device__ __forceinline__ float value() const { return (float)exact(); }
   __device__ __forceinline__ bool somebody() const { return tie < 1ll << 60; }
 };
 __device__ __forceinline__ Cand cand(double score, long long tie) {
@@ -619,9 +629,6 @@ struct Beam {
   float score;
   // The reference, which may be far from 0, is subtracted first.
   __device__ __forceinline__ double of(float logit) const { return (double)score + (((double)logit - ref) - total); }
-  __device__ __forceinline__ Beam shfl(int from) const {
-    return {__shfl_sync(kAll, total, from), __shfl_sync(kAll, ref, from), __shfl_sync(kAll, score, from)};
-  }
 };
 // The sum of exp(x - most) of a row, for logits that are too far from 0 for the others'
 // way.  Slow, and rare: such logits are masks of the type's lowest value without any
@@ -636,142 +643,220 @@ __device__ __noinline__ uint64_t far_sum(const T* row, int V, float most, int la
   return warp_sum(sum);
 }
 
-// The 'keep' greatest of n numbers, of which the first 64 are in a and b: up to kOneByOne
-// to keep, of any order, and else of sorted lists of 'keep'.
+// The 'keep' greatest of n numbers in any order, of which the first 64 are in a and b.
 __device__ __forceinline__ uint64_t best_runs(const uint64_t* keys, uint64_t a, uint64_t b, int n, int keep, int lane) {
   uint64_t list = 0;
-  if (keep <= kOneByOne) {
-    for (int i = lane; i - lane < n; i += 64) {
-      const uint64_t c = i + 64 < n ? keys[i + 64] : 0, d = i + 96 < n ? keys[i + 96] : 0;
-      a = greatest_of(i < n ? a : 0, i + 32 < n ? b : 0, keep, lane);
-      list = i == lane ? a : greatest_of(list, a, keep, lane);
-      a = c, b = d;
-    }
-  } else {
-    uint64_t k = lane < keep ? a : 0;
-    for (int i = keep; i <= n; i += keep) {
-      const uint64_t next = lane < keep && i < n ? keys[i + lane] : 0;
-      list = i == keep ? k : merge32(list, k, lane);
-      k = next;
-    }
+  for (int i = lane; i - lane < n; i += 64) {
+    const uint64_t c = i + 64 < n ? keys[i + 64] : 0, d = i + 96 < n ? keys[i + 96] : 0;
+    a = greatest_of(i < n ? a : 0, i + 32 < n ? b : 0, keep, lane);
+    list = i == lane ? a : greatest_of(list, a, keep, lane);
+    a = c, b = d;
   }
   return list;
 }
+// Of sorted lists of 'keep', of which the first ones (up to 'slots' may be read) are in k.
+constexpr int kLists = 8;
+__device__ __forceinline__ void read_lists(uint64_t (&k)[kLists], const uint64_t* keys, int from, int to, int keep, int lane) {
+#pragma unroll
+  for (int u = 0; u < kLists; ++u) k[u] = lane < keep && from + u < to ? keys[(from + u) * keep + lane] : 0;
+}
+__device__ __forceinline__ uint64_t best_lists(const uint64_t* keys, uint64_t (&k)[kLists], int lists, int keep, int lane) {
+  uint64_t x = 0, y = 0;  // two chains of merges side by side
+  for (int l = 0; l < lists; l += kLists) {
+    if (l > 0) read_lists(k, keys, l, lists, keep, lane);
+#pragma unroll
+    for (int u = 0; u < kLists; u += 2) {
+      if (l + u >= lists) break;
+      x = merge32(x, k[u], lane);
+      y = merge32(y, l + u + 1 < lists ? k[u + 1] : 0, lane);
+    }
+  }
+  return merge32(x, y, lane);
+}
 
-// A CTA a request.  Its warps put a beam's parts together each; then the threads rank
-// the beams' best runs, and the tokens in the best of those, by counting what comes
-// before them.
-constexpr int kRanked = 16;  // up to so many beams: of more, the runs are merged
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_constant__ Args g) {
+// A beam's sum of 2^(x a - R), or of exp(x - most) where that is 'far', and what else is
+// known of its row.
+struct RowSum {
+  uint64_t sum;
+  float most, score;
+  bool good, far;
+};
+
+// A CTA a request, of J threads, a warp a beam.  The warps put the beams' parts and lists
+// together, then the best runs of all beams are found, and the tokens in those: up to
+// kOneByOne beams' by counting what comes before each, more by merges of the beams' sorted
+// lists, two by two.  64-bit additions are slow (an SM does two at a time): of more beams
+// one warp makes the logarithms, and only those tokens are scored whose logits pass a
+// bound in 32 bits.
+template <typename T, int J>
+__global__ void __launch_bounds__(J, J == kFewThreads ? 4 : 1) k_select_join(const __grid_constant__ Args g) {
   constexpr int N = Elem<T>::N, kTokens = kVecs * N;  // of a run
-  constexpr int kMost = PS_BEAM_MAX_BEAMS;
+  constexpr bool kFew = J == kFewThreads;
+  constexpr int kMost = kFew ? kOneByOne : PS_BEAM_MAX_BEAMS, kEnds = kMost * PS_BEAM_MAX_END;
+  constexpr int kTurns = (kMost * kTokens + J - 1) / J;  // tokens of a thread
+  static_assert(32 * kMost <= J && kEnds <= J && kMost <= kTokens, "a warp a beam, an end token a thread, the runs' room");
+  __shared__ RowSum s_row[kMost];
   __shared__ Beam s_beam[kMost];
-  __shared__ Cand s_run[kRanked * kRanked], s_best[kMost], s_token[kMost * kTokens], s_chosen[kMost], s_end[kMost * PS_BEAM_MAX_END];
+  __shared__ float s_least[kMost];
+  __shared__ Cand s_best[kMost], s_token[kMost * kTokens], s_chosen[kMost], s_end[kEnds];
   __shared__ int s_tokens, s_ended;
+  Cand* const s_run = s_token;  // the tokens come after the runs
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, B = g.s.beams, r = blockIdx.x;
   const int E = g.a.ended_tokens ? g.s.num_end : 0;
   const T* logits = static_cast<const T*>(g.a.logits) + r * g.a.request_stride;
   const int64_t to = (int64_t)r * B;
-  static_assert(kMost * PS_BEAM_MAX_END == kJoinThreads, "an end token's candidate a thread");
   const int end_beam = E > 0 ? t / E : kMost, end_token = E > 0 ? g.s.end[t % E] : 0;
   if (t == 0) s_tokens = s_ended = 0;
   if (t < kMost) s_best[t] = s_chosen[t] = nobody(t);
-  s_run[t] = nobody(t);
-  static_assert(kRanked * kRanked == kJoinThreads, "one a thread");
-  __syncthreads();
+  if (kFew && t < kMost * kMost) s_run[t] = nobody(t);
+  if (kFew) __syncthreads();
   chain();
   // the end tokens' logits, on their way early
   float end_logit = -INFINITY;
   if (end_beam < B) end_logit = Elem<T>::one(logits + end_beam * g.a.beam_stride + end_token);
-  Cand mine = nobody(lane);
-  for (int b = warp; b < B; b += kJoinWarps) {
-    const int row = r * B + b;
+  uint64_t list = 0;
+  auto beam_of = [](const RowSum& x) {
+    Beam beam{INFINITY, 0.0, x.score};  // no candidates
+    if (x.good) {
+      beam.ref = x.far ? (double)x.most : (double)exponent_of(x.most) * (1.0 / (double)kLog2e);
+      beam.total = log_of(x.sum);
+    }
+    return beam;
+  };
+  if (warp < B) {
+    const int row = r * B + warp;
     // all that may be needed is read at once, and looked at where it is some row's of this call
     const float c = g.a.scores[row];
     const uint64_t* keys = g.s.keys + (int64_t)row * g.slots * B;
     Part p{0, -INFINITY, 0};
     if (lane < g.parts) p = g.s.parts[(int64_t)row * g.parts + lane];
     const int lists = g.s.lists[row];
-    const uint64_t k0 = lane < g.slots * B ? keys[lane] : 0, k1 = lane + 32 < g.slots * B ? keys[lane + 32] : 0;
-    Beam beam{INFINITY, 0.0, c};  // no candidates
-    uint64_t list = 0;
+    uint64_t k0 = 0, k1 = 0, k[kLists];
+    if (kFew) {
+      k0 = lane < g.slots * B ? keys[lane] : 0;
+      k1 = lane + 32 < g.slots * B ? keys[lane + 32] : 0;
+    } else {
+      read_lists(k, keys, 0, g.slots, B, lane);
+    }
+    RowSum x{0, -INFINITY, c, false, false};
     bool bad = c != -INFINITY && !(c - c == 0);
     if (c - c == 0) {
-      list = best_runs(keys, k0, k1, lists * B, B, lane);
-      const float most = warp_max(p.most), R = exponent_of(most), down = R - exponent_of(p.most);
-      uint64_t sum = warp_sum(down < 64.0f ? p.sum >> (int)down : 0);
+      list = kFew ? best_runs(keys, k0, k1, lists * B, B, lane) : best_lists(keys, k, lists, B, lane);
+      x.most = warp_max(p.most);
+      const float R = exponent_of(x.most), down = R - exponent_of(p.most);
+      x.sum = warp_sum(down < 64.0f ? p.sum >> (int)down : 0);
       bad = __any_sync(kAll, p.bad);
-      beam.ref = (double)R * (1.0 / (double)kLog2e);
-      if (fabsf(most) > kFar && most > -INFINITY && !bad) {
-        sum = far_sum(logits + b * g.a.beam_stride, g.s.vocab, most, lane);
-        beam.ref = most;
-      }
-      if (!bad && most > -INFINITY) beam.total = log_of(sum);
+      x.good = !bad && x.most > -INFINITY;
+      x.far = fabsf(x.most) > kFar && x.good;
+      if (x.far) x.sum = far_sum(logits + warp * g.a.beam_stride, g.s.vocab, x.most, lane);
     }
-    if (lane == 0) {
-      if (bad) set_error(g.status, PS_ERR_INVALID_ARG);
-      s_beam[b] = beam;
-    }
-    const bool on = beam.total < INFINITY && lane < B && list > kNoKey;
-    const Cand x = on ? cand(beam.of(logit_of(list)), (long long)b << 32 | (uint32_t)place_of(list)) : nobody(lane);
-    if (B <= kRanked) {
-      if (on) s_run[b * B + lane] = x;
-    } else {
-      mine = b < kJoinWarps ? x : merge32(mine, x, lane);
+    if (lane == 0 && bad) set_error(g.status, PS_ERR_INVALID_ARG);
+    if (kFew) {  // eight warps' additions take no longer than another step
+      const Beam beam = beam_of(x);
+      if (lane == 0) s_beam[warp] = beam;
+      if (lane < B && beam.total < INFINITY && list > kNoKey)
+        s_run[warp * B + lane] = cand(beam.of(logit_of(list)), (long long)warp << 32 | (uint32_t)place_of(list));
+    } else if (lane == 0) {
+      s_row[warp] = x;
     }
   }
-  if (B > kRanked) s_token[t] = mine;
   __syncthreads();
-  // the best runs, and the end tokens' candidates
-  if (B <= kRanked) {
-    // a candidate for 'each' threads in a row, each of which counts a share
-    const int each = B * B <= 32 ? 8 : (B * B <= 64 ? 4 : (B * B <= 128 ? 2 : 1)), i = t / each, n = (B * B + each - 1) / each;
-    const Cand x = s_run[i];
-    int place = 0;
-    const int end = min(B * B, (t % each + 1) * n);
-#pragma unroll 4
-    for (int j = t % each * n; j < end; ++j) place += s_run[j].before(x);
-    for (int o = 1; o < each; o <<= 1) place += __shfl_xor_sync(kAll, place, o);
-    if (t % each == 0 && x.somebody() && place < B) s_best[place] = x;
-  } else if (warp == 0) {
-    for (int w = 1; w < kJoinWarps; ++w) mine = merge32(mine, s_token[w * 32 + lane], lane);
-    if (lane < B) s_best[lane] = mine;
+  if (!kFew) {
+    if (t < B) s_beam[t] = beam_of(s_row[t]);
+    __syncthreads();
   }
-  if (end_beam < B)
-    s_end[t] = s_beam[end_beam].total < INFINITY && end_logit > -INFINITY
-                   ? cand(s_beam[end_beam].of(end_logit), (long long)end_beam << 32 | end_token) : nobody(t);
+  auto candidate = [&](int beam, bool on, float logit, uint32_t place) {
+    return on && s_beam[beam].total < INFINITY ? cand(s_beam[beam].of(logit), (long long)beam << 32 | place) : nobody(t);
+  };
+  if (end_beam < B) s_end[t] = candidate(end_beam, end_logit > -INFINITY, end_logit, end_token);
+  // x's place among n candidates, 'each' threads in a row counting a share each: in turns,
+  // so that a warp reads neighbours (64 in a row each took 15 us for 256)
+  auto place_among = [&](const Cand& x, const Cand* of, int n, int each) {
+    int place = 0;
+#pragma unroll 4
+    for (int j = t % each; j < n; j += each) place += of[j].before(x);
+    for (int o = 1; o < each; o <<= 1) place += __shfl_xor_sync(kAll, place, o);
+    return place;
+  };
+  auto threads_for = [&](int n) {
+    int each = 1;
+    while (2 * each * n <= J && each < 16) each *= 2;
+    return each;
+  };
+  // the best runs
+  if (kFew) {
+    const int each = threads_for(B * B), i = t / each;
+    const Cand x = i < B * B ? s_run[i] : nobody(J);
+    const int place = place_among(x, s_run, B * B, each);
+    if (t % each == 0 && x.somebody() && place < B) s_best[place] = x;
+  } else {
+    Cand x = nobody(t);
+    if (warp < B) x = candidate(warp, lane < B && list > kNoKey, logit_of(list), place_of(list));
+    for (int s = 1; s < B; s <<= 1) {
+      if ((warp & (2 * s - 1)) == s && warp < B) s_run[t] = x;
+      __syncthreads();
+      if ((warp & (2 * s - 1)) == 0 && warp + s < B) x = merge32(x, s_run[t + 32 * s], lane);
+    }
+    if (warp == 0 && lane < B) s_best[lane] = x;
+  }
   __syncthreads();
   // the tokens of the best runs; each run has one that is no later than the last run's best
   const Cand last = s_best[B - 1];
-  for (int i = t; i < B * kTokens; i += kJoinThreads) {
-    const Cand x = s_best[i / kTokens];
-    if (!x.somebody()) break;
-    const int b = (int)(x.tie >> 32);
-    const int64_t token = (x.tie & 0xFFFFFFFF) * kTokens + i % kTokens;
-    if (token >= g.s.vocab || ends(g.s, (int)token)) continue;
-    const float l = Elem<T>::one(logits + b * g.a.beam_stride + token);
-    const Cand y = cand(s_beam[b].of(l), (long long)b << 32 | token);
-    if (l > -INFINITY && (!last.somebody() || y.score >= last.score)) s_token[atomicAdd(&s_tokens, 1)] = y;
+  float logit[kTurns];
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    const int i = t + u * J;
+    logit[u] = -INFINITY;
+    if (i < B * kTokens && s_best[i / kTokens].somebody()) {
+      const long long run = s_best[i / kTokens].tie;
+      const int64_t token = (run & 0xFFFFFFFF) * kTokens + i % kTokens;
+      if (token < g.s.vocab) logit[u] = Elem<T>::one(logits + (run >> 32) * g.a.beam_stride + token);
+    }
+  }
+  if (!kFew && t < B) {  // a logit that its beam's tokens need, or a little less
+    const Beam x = s_beam[t];
+    float least = -INFINITY;
+    if (last.somebody() && x.total < INFINITY) {
+      const double want = (last.exact() - (double)x.score) + x.total;
+      least = __double2float_rd(want + x.ref - 1e-9 * (fabs(want) + fabs((double)x.score) + fabs(x.total) + fabs(x.ref)));
+    }
+    s_least[t] = least;
+  }
+  if (!kFew) __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    if (logit[u] == -INFINITY) continue;
+    const int i = t + u * J;
+    const long long run = s_best[i / kTokens].tie;
+    const int beam = (int)(run >> 32), token = (int)(run & 0xFFFFFFFF) * kTokens + i % kTokens;
+    if ((!kFew && logit[u] < s_least[beam]) || ends(g.s, token)) continue;
+    const Cand y = candidate(beam, true, logit[u], token);
+    if (!last.somebody() || y.score >= last.score) s_token[atomicAdd(&s_tokens, 1)] = y;
   }
   __syncthreads();
-  for (int i = t; i < s_tokens; i += kJoinThreads) {
-    const Cand x = s_token[i];
-    int place = 0;
-    for (int j = 0; j < s_tokens; ++j) place += s_token[j].before(x);
-    if (place < B) s_chosen[place] = x;
+  const int n = s_tokens, each = threads_for(n);
+  for (int i0 = 0; i0 < n; i0 += J / each) {
+    const int i = i0 + t / each;
+    const Cand x = i < n ? s_token[i] : nobody(J);
+    const int place = place_among(x, s_token, n, each);
+    if (t % each == 0 && x.somebody() && place < B) s_chosen[place] = x;
   }
-  // an end token's place among all candidates, and among those of its kind
+  // an end token's place among all candidates, and among those of its kind; after the last
+  // run's best it has none
   if (end_beam < B) {
     const Cand x = s_end[t];
-    int place = 0, others = 0;
-    for (int j = 0; j < B * E; ++j) place += s_end[j].before(x);
-    for (int j = 0; j < s_tokens; ++j) others += s_token[j].before(x);
-    if (x.somebody() && place + others < B) {
-      atomicAdd(&s_ended, 1);
-      g.a.ended_tokens[to + place] = (int)(x.tie & 0xFFFFFFFF);
-      g.a.ended_parents[to + place] = (int)(x.tie >> 32);
-      g.a.ended_scores[to + place] = x.value();
+    if (x.somebody() && (!last.somebody() || x.score >= last.score)) {
+      int place = 0, others = 0;
+#pragma unroll 4
+      for (int j = 0; j < B * E; ++j) place += s_end[j].before(x);
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) others += s_token[j].before(x);
+      if (place + others < B) {
+        atomicAdd(&s_ended, 1);
+        g.a.ended_tokens[to + place] = (int)(x.tie & 0xFFFFFFFF);
+        g.a.ended_parents[to + place] = (int)(x.tie >> 32);
+        g.a.ended_scores[to + place] = x.value();
+      }
     }
   }
   __syncthreads();
@@ -793,8 +878,10 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_select_join(const __grid_co
 template <typename T>
 static int32_t launch_typed(const Args& g, int grid, cudaStream_t st) {
   cudaError_t e = launch(k_select<T>, dim3((unsigned)grid), kThreads, sizeof(Shared), st, g);
-  if (e == cudaSuccess) e = launch(k_select_join<T>, dim3((unsigned)g.a.num_requests), kJoinThreads, 0, st, g);
-  return status_of(e);
+  if (e != cudaSuccess) return status_of(e);
+  const dim3 requests((unsigned)g.a.num_requests);
+  if (g.s.beams <= kOneByOne) return status_of(launch(k_select_join<T, kFewThreads>, requests, kFewThreads, 0, st, g));
+  return status_of(launch(k_select_join<T, kManyThreads>, requests, kManyThreads, 0, st, g));
 }
 
 // Both kernels prefer all of an SM's memory as shared memory: where two that run after
@@ -805,7 +892,9 @@ static cudaError_t configure_typed() {
   cudaError_t e = cudaFuncSetAttribute(k_select<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_select<T>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(k_select_join<T>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    e = cudaFuncSetAttribute(k_select_join<T, kFewThreads>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(k_select_join<T, kManyThreads>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   return e;
 }
 int32_t configure_select() {

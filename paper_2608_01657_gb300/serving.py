@@ -173,6 +173,8 @@ class Server:
         names = range(R, R + n)
         if R + n > s.max_requests:
             raise ValueError(f"prompts and beams need {R + n} rows of {s.max_requests}")
+        if steps < 1:
+            raise ValueError("there must be a step")
         if beams > s.vocab - len(end):
             raise ValueError("there must be as many tokens that end nothing as beams")
         if self.running.intersection(names):
@@ -200,6 +202,7 @@ class Server:
             x = self.forward(children, self.lens[children.long()], at.tokens.view(-1), [1] * n)
             self.lens[children.long()] += 1
             logits = (x @ self.layers.embed.T).view(R, beams, s.vocab)
+        self.pool.check()
         search.check()
         # the beams of the last step, and those that ended on the way: at step t with parent p, in p's row of step t - 1
         step = torch.arange(steps, device="cuda")[:, None, None].expand(steps, R, beams)

@@ -98,13 +98,24 @@ def test_searches_that_are_refused():
     server = S.Server(s, groups=2, seed=5)
     hidden = server.admit([0, 1], S.prompts_of([0, 1], s, 5), room=0)["hidden"]
     held, running = server.held.clone(), set(server.running)
-    for bad in (dict(beams=16), dict(beams=5, end=[1, 3]), dict(beams=0), dict(beams=2, end=[6]), dict(beams=2, end=[1, 1])):
+    for bad in (dict(beams=16), dict(beams=5, end=[1, 3]), dict(beams=0), dict(beams=2, end=[6]), dict(beams=2, end=[1, 1]), dict(beams=2, steps=0)):
         with pytest.raises(ValueError):
             server.beam_search(hidden, **(dict(steps=3) | bad))
     assert torch.equal(held, server.held) and running == server.running
     found = server.beam_search(hidden, 4, 3, [1, 3])
     server.pool.check()
     assert found["sequences"].shape == (2, 4, 3)
+
+
+def test_a_search_without_pages_says_so():
+    from paper_2608_01657_gb300 import serving as S
+    s = S.Shape()
+    server = S.Server(s, groups=2, seed=5)
+    hidden = server.admit([0, 1], S.prompts_of([0, 1], s, 5), room=0)["hidden"]
+    free = (server.refs == 0).nonzero().flatten()
+    server.refs[free[3:]] = 1
+    with pytest.raises(RuntimeError, match="capacity"):
+        server.beam_search(hidden, 8, 2)
 
 
 def test_a_captured_step_is_the_eager_one():
