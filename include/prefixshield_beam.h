@@ -11,7 +11,8 @@
  * are device pointers, every buffer is the caller's, calls are enqueued on a
  * stream and return a status, what only the device can see wrong is reported in
  * *d_status (NULL: not reported).  A handle is not thread-safe; its calls must be
- * issued in order on one stream (or with equivalent ordering).
+ * issued in order on one stream (or with equivalent ordering), with the device
+ * current that it was made on (refused otherwise).
  */
 #ifndef PREFIXSHIELD_BEAM_H
 #define PREFIXSHIELD_BEAM_H

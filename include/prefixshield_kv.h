@@ -252,7 +252,8 @@ typedef struct {
  * sets *d_status to PS_ERR_INVALID_ARG, more tokens than num_tokens to
  * PS_ERR_CAPACITY, and then the whole batch is left out: offsets and lengths are
  * 0, tables and slots -1, and ps_kv_plan() refuses it.  A page id out of range
- * sets *d_status, and the slot is -1. */
+ * sets *d_status, and the slot is -1.  Refused unless the handle's device is the
+ * current one, as ps_kv_reorder() is. */
 int32_t ps_kv_layout(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const ps_kv_layout_t* layout,
                      int32_t* d_status);
 

@@ -9,11 +9,12 @@
 
 using namespace psbeam;
 using pskv::Span;
+using pskv::on_device;
 using pskv::outputs_apart;
 
 struct ps_beam {
   Search s;
-  int32_t max_requests, nsm;
+  int32_t max_requests, dev, nsm;
 };
 
 namespace {
@@ -75,6 +76,7 @@ int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_wor
   ps_beam* b = new (std::nothrow) ps_beam{};
   if (!b) return PS_ERR_CUDA;
   b->max_requests = cfg->max_requests;
+  b->dev = dev;
   b->nsm = nsm < pskv::kMaxSms ? nsm : pskv::kMaxSms;
   b->s.beams = cfg->beams;
   b->s.vocab = cfg->vocab;
@@ -103,7 +105,7 @@ int32_t ps_beam_select(ps_beam_t* beam, void* stream, const ps_beam_select_t* a,
                         {a->scores == a->scores_out ? nullptr : a->scores, n, false}, {d_status, 4, false},
                         {a->tokens, n, true}, {a->parents, n, true}, {a->scores_out, n, true},
                         {a->ended_tokens, n, true}, {a->ended_parents, n, true}, {a->ended_scores, n, true}};
-  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  if (!outputs_apart(spans) || !on_device(beam->dev)) return PS_ERR_INVALID_ARG;
   return launch_select(beam->s, *a, d_status, beam->nsm, as_stream(stream));
 }
 
@@ -116,7 +118,7 @@ int32_t ps_beam_trace(ps_beam_t* beam, void* stream, const ps_beam_trace_t* a, i
   if (!a->tokens || !a->parents || !a->beams_of || !a->out) return PS_ERR_INVALID_ARG;
   const Span spans[] = {{a->tokens, 4 * T * R * B, false}, {a->parents, 4 * T * R * B, false}, {a->beams_of, 4 * R * N, false},
                         {a->lengths, 4 * R * N, false}, {d_status, 4, false}, {a->out, 4 * R * N * T, true}};
-  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  if (!outputs_apart(spans) || !on_device(beam->dev)) return PS_ERR_INVALID_ARG;
   return launch_trace(beam->s, *a, d_status, as_stream(stream));
 }
 

@@ -268,6 +268,13 @@ struct LayoutScratch {
   int32_t* done;
 };
 
+// Is the current device the one that a handle was made on (host code)?  A launch on another
+// one would follow addresses that are not its own.
+inline bool on_device(int32_t dev) {
+  int d;
+  return cudaGetDevice(&d) == cudaSuccess && d == dev;
+}
+
 // ---- device helpers ----------------------------------------------------------------
 __device__ __forceinline__ void set_error(int32_t* status, int32_t code) {
   if (status) atomicMin(status, code);

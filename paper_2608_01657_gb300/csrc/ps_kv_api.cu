@@ -18,7 +18,7 @@ struct ps_kv {
   Batch batch;
   bool planned;
   int32_t turn;  // of the next attention, 0 or 1
-  int32_t nsm, max_requests, max_tokens, max_row_pages;
+  int32_t dev, nsm, max_requests, max_tokens, max_row_pages;
 };
 
 namespace {
@@ -193,6 +193,7 @@ int32_t ps_kv_create(ps_kv_t** out, const ps_kv_config_t* cfg, void* d_workspace
     return PS_ERR_CUDA;
   }
   for (int32_t l = 0; l < cfg->num_layers; ++l) make_maps(kv->pool, l, kv->maps + l);
+  kv->dev = dev;
   kv->nsm = nsm < kMaxSms ? nsm : kMaxSms;
   kv->max_requests = cfg->max_requests;
   kv->max_tokens = cfg->max_tokens;
@@ -302,7 +303,7 @@ int32_t ps_kv_layout(ps_kv_t* kv, void* stream, const ps_kv_rows_t* rows, const 
                         {rows->held, 4ll * rows->num_rows, false}, {d_status, 4, false},
                         {l->q_offsets, 4 * (all + 1), true}, {l->kv_lens, 4 * all, true}, {l->tables, 4 * all * stride, true},
                         {l->positions, 4 * T, true}, {l->slots, 8 * T, true}, {l->group_offsets, 4 * (all + 1), true}};
-  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  if (!outputs_apart(spans) || !on_device(kv->dev)) return PS_ERR_INVALID_ARG;
   return launch_layout(kv->pool, kv->layout, *l, *rows, row_pages(kv, stride), d_status, kv->nsm, as_stream(stream));
 }
 
@@ -334,7 +335,7 @@ int32_t ps_kv_reorder(ps_kv_t* kv, void* stream, int32_t num_requests, int32_t b
   const Span spans[] = {{d_rows, 4 * n, false}, {d_parents, 4 * n, false}, {d_status, 4, false},
                         {d_refs_in == d_refs_out ? nullptr : d_refs_in, 4 * np, false}, {d_refs_out, 4 * np, true},
                         {rows->tables, 4 * m * rows->table_stride, true}, {rows->lens, 4 * m, true}, {rows->held, 4 * m, true}};
-  if (!outputs_apart(spans)) return PS_ERR_INVALID_ARG;
+  if (!outputs_apart(spans) || !on_device(kv->dev)) return PS_ERR_INVALID_ARG;
   return launch_reorder(kv->pool, kv->pages, kv->reorder, num_requests, beams, d_rows, d_parents, grow, *rows,
                         row_pages(kv, rows->table_stride), d_refs_in, d_refs_out, d_status, kv->nsm, as_stream(stream));
 }

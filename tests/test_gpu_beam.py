@@ -23,7 +23,9 @@ def all_scores(logits, scores):
     x, c = logits.double(), scores.double()[..., None]
     good = torch.isfinite(c) & ~(torch.isnan(x) | (x == math.inf)).any(-1, keepdim=True) & (x > -math.inf).any(-1, keepdim=True)
     far = x - torch.where(good, x, 0.0).amax(-1, keepdim=True)   # first, so that logits far from 0 lose nothing
-    p = c + (far - torch.where(good, far, 0.0).exp().sum(-1, keepdim=True).log())
+    # (sums of columns, so that equal rows' sums are equal to the last bit: those of rows depend on where they lie)
+    total = torch.where(good, far, 0.0).exp().movedim(-1, 0).contiguous().sum(0)[..., None]
+    p = c + (far - total.log())
     return torch.where(good & (x > -math.inf), p, -math.inf)
 
 
@@ -89,7 +91,8 @@ def make(R, B, V, dtype, seed, spread=3.0, masked=0.0):
 
 @pytest.mark.parametrize("dtype", [BF, HF, F32])
 @pytest.mark.parametrize("R,B,V", [(1, 1, 1), (2, 1, 7), (1, 3, 2), (3, 4, 31), (2, 32, 33), (5, 5, 1000), (1, 8, 2048), (3, 2, 2049),
-                                   (2, 16, 4097), (1, 32, 16384), (2, 7, 16411), (1, 4, 50001), (3, 8, 131072), (1, 1, 300001)])
+                                   (2, 16, 4097), (1, 32, 16384), (2, 7, 16411), (1, 4, 50001), (3, 8, 131072), (1, 1, 300001), (2, 9, 5000), (3, 12, 40001), (1, 17, 3001), (1, 31, 131072),
+                                   (2, 32, 70867), (40, 24, 700)])
 def test_select(R, B, V, dtype):
     end = sorted({0, V // 2, V - 1} if V > 3 else set())
     x, s = make(R, B, V, dtype, seed=V + B)
@@ -148,6 +151,39 @@ def test_equal_logits_go_to_the_lowest_token(V):
         got = h.select(x.to(dtype), s)
         assert (got.tokens[1] == torch.arange(B, device="cuda")).all() and (got.parents[1] == 0).all()
         check(x, s, (), got, exact_order=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("B", [9, 12, 16, 17, 31, 32])
+def test_many_beams(B, dtype):
+    """Ties, eight end tokens, few candidates, beams that are absent or not finite, where a beam has a warp."""
+    R = 8
+    for V in (B, 50, 3001, 40001):
+        g = torch.Generator("cuda").manual_seed(V + B)
+        x = torch.randint(0, 3, (R, 1, V), generator=g, device="cuda").to(dtype).expand(R, B, V).contiguous()
+        # (no two different scores are near one another: logits are whole numbers)
+        s = -0.37 * torch.randint(0, 2, (R, B), generator=g, device="cuda").float()
+        s[1] = -3.0
+        end = sorted({0, 1, 5, B - 1, V - 1, V // 2, V // 3, V - 2})
+        s[2, 1:] = -math.inf                # a first step
+        s[3] = -math.inf
+        x[4] = -math.inf
+        x[4, B - 1, 3] = 2                  # one candidate in all
+        x[5, :, 2:] = -math.inf             # two tokens of every beam
+        s[6, B - 1] = 40.0                  # one beam before all others
+        h = search(R, B, V, dtype, end)
+        got = h.select(x, s)
+        h.check()
+        check(x, s, end, got, exact_order=True)
+        got = search(R, B, V, dtype).select(x, s)
+        check(x, s, (), got, exact_order=True)
+        x[7, B // 2, V - 1] = math.nan
+        s[0, 0] = math.inf
+        got = h.select(x, s)
+        with pytest.raises(RuntimeError, match="invalid"):
+            h.check()
+        check(x, s, end, got, exact_order=True)
+        assert (got.parents[7] != B // 2).all() and (got.parents[0] != 0).all()
 
 
 @pytest.mark.parametrize("rising", [True, False])
