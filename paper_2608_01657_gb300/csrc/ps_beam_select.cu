@@ -29,7 +29,7 @@
 // exponents are off by a ln 2 - 1 = 1.3e-8 of their size.  Scores are added in 64 bits.
 //
 // 128 requests of 8 beams and 131072 tokens in bf16, 268 MB, take 57 us: 51 for k_select,
-// which reads 5.2 TB/s at 57 % of the issue slots (41 us with the loads alone), and 6 for
+// which reads 5.2 TB/s at 58 % of the issue slots (41 us with the loads alone), and 6 for
 // k_select_join.  64 x 8 in 32 bits take 56; 131071 tokens, whose rows begin anywhere in a
 // word, 67; 256 single rows 23; 32 x 32 beams 67.  Few rows are a chain of dependent
 // steps: 7.5 for one row of 1000 tokens, 9.6 for 8 x 4 of 65536.
