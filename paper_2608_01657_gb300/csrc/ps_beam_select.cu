@@ -31,7 +31,7 @@
 // 128 requests of 8 beams and 131072 tokens in bf16, 268 MB, take 57 us: 51 for k_select,
 // which reads 5.2 TB/s at 58 % of the issue slots (41 us with the loads alone), and 6 for
 // k_select_join.  64 x 8 in 32 bits take 56; 131071 tokens, whose rows begin anywhere in a
-// word, 67; 256 single rows 23; 32 x 32 beams 67.  Few rows are a chain of dependent
+// word, 64; 256 single rows 23; 32 x 32 beams 67.  Few rows are a chain of dependent
 // steps: 7.5 for one row of 1000 tokens, 9.6 for 8 x 4 of 65536.
 #include "ps_beam.cuh"
 
@@ -328,6 +328,20 @@ __device__ __forceinline__ void fetch_chunk(uint4* slot, const T* row, int shift
   for (int j = 0; j < kVecs; ++j) fetch_word(slot + place_in_slot(32 * j + lane), row, shift, c * kChunk + 32 * j + lane, V);
   if (shift != 0 && lane == 0) fetch_word(slot + kChunk, row, shift, c * kChunk + kChunk, V);
 }
+// A run that begins W 32-bit words and 'bits' further on.
+template <int W>
+__device__ __forceinline__ void shift_run(uint4 (&v)[kVecs], const uint4& behind, int bits) {
+  uint32_t x[4 * kVecs + 4];
+#pragma unroll
+  for (int j = 0; j <= kVecs; ++j) {
+    const uint4 n = j < kVecs ? v[j < kVecs ? j : 0] : behind;
+    x[4 * j] = n.x, x[4 * j + 1] = n.y, x[4 * j + 2] = n.z, x[4 * j + 3] = n.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * kVecs; ++i) x[i] = __funnelshift_r(x[i + W], x[i + W + 1], bits);
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) v[j] = make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+}
 // A lane's run of a chunk.
 template <typename T>
 __device__ __forceinline__ void take_run(const uint4* slot, int shift, int lane, uint4 (&v)[kVecs]) {
@@ -336,20 +350,11 @@ __device__ __forceinline__ void take_run(const uint4* slot, int shift, int lane,
   if (shift == 0) return;
   const int words = shift * (int)sizeof(T) / 4, bits = shift * (int)sizeof(T) % 4 * 8;
   const uint4 behind = slot[lane == 31 ? kChunk : place_in_slot(kVecs * lane + kVecs)];
-#pragma unroll
-  for (int j = 0; j < kVecs; ++j) {
-    const uint4 n = j + 1 < kVecs ? v[j + 1 < kVecs ? j + 1 : j] : behind;
-    uint32_t x[8] = {v[j].x, v[j].y, v[j].z, v[j].w, n.x, n.y, n.z, n.w};
-    if (words & 2) {
-#pragma unroll
-      for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
-    }
-    if (words & 1) {
-#pragma unroll
-      for (int i = 0; i < 5; ++i) x[i] = x[i + 1];
-    }
-    v[j] = make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
-                      __funnelshift_r(x[3], x[4], bits));
+  switch (words) {  // the same for all lanes
+    case 0: shift_run<0>(v, behind, bits); break;
+    case 1: shift_run<1>(v, behind, bits); break;
+    case 2: shift_run<2>(v, behind, bits); break;
+    default: shift_run<3>(v, behind, bits); break;
   }
 }
 

@@ -192,7 +192,7 @@ class KVPool(Handle):
         return p
 
     def _table(self, t, name: str):
-        if len(t.shape) != 2 or t.dtype is not torch.int32 or t.device != self.device or not t.is_contiguous():
+        if len(t.shape) != 2 or t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 [rows, pages] tensor")
 
     # -- one layer's new tokens ----------------------------------------------
