@@ -15,17 +15,17 @@
 // rest: a sector a lane).  What does not fit into shared memory is done in rounds, from
 // the last steps on.
 //
-// 2047 steps of 128 requests, 8 beams and 13 hypotheses take 13.6 us; their 30 MB need
+// 2047 steps of 128 requests, 8 beams and 13 hypotheses take 13.9 us; their 30 MB need
 // 4.6.  The parents take 3.4 (32 bytes of a step are a request's; next to one another
 // they took 2.3), the maps beside the tokens' copies 2.2, groups and hypotheses 1.2,
-// paths 1.9 and the output 3.0.  64 steps of 4 requests take 3.5, a launch and a chain
+// paths 1.9 and the output 3.0.  64 steps of 4 requests take 3.6, a launch and a chain
 // of reads.
 #include "ps_beam.cuh"
 
 namespace psbeam {
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kThreads = 1024;
 constexpr int kCopiers = kThreads / 2;  // threads that fetch tokens while the others are at the maps
 constexpr int kHyps = 64;          // of a CTA at most
 constexpr int kBytes = 206 << 10;  // of tokens, parents and paths

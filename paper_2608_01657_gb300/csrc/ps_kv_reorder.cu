@@ -17,8 +17,8 @@
 // Bound by latency: chains of dependent reads (parent, length, page, reference, change;
 // free pages, their sums; new page, its tokens) in kernels that follow one another.
 // Each reads what it can before it waits for the one before it.  One request of four
-// beams takes 7.5 us; 64 of eight beams of 2048 tokens, whose copies are 21 MB (3.2 us),
-// 15.5: 4.5 for the changes, 4.7 to the verdict, 3 to 5 for the copies.
+// beams takes 8 us; 64 of eight beams of 2048 tokens, whose copies are 21 MB (3.2 us),
+// 15.8: 4.5 for the changes, 4.7 to the decision, 3 to 5 for the copies.
 #include "ps_kv_pages.cuh"
 
 namespace pskv {
