@@ -56,8 +56,8 @@ int32_t ps_beam_create(ps_beam_t** out, const ps_beam_config_t* cfg, void* d_wor
 void ps_beam_destroy(ps_beam_t* beam);
 
 /* One step.  Beam b of request r has the score c = scores[r * beams + b] (the sum
- * of its tokens' log-probabilities; -infinity: there is no such beam, and its
- * logits are not read) and the logits x[v] = logits[r * request_stride + b *
+ * of its tokens' log-probabilities; -infinity: there is no such beam, whatever its
+ * logits are) and the logits x[v] = logits[r * request_stride + b *
  * beam_stride + v].  Continuing it with token v has the score
  *   c + x[v] - log sum_u exp x[u],
  * the sum in 32 bits at least, the score in 64, rounded once.  A logit of

@@ -84,13 +84,14 @@ class BeamSearch(Handle):
         earlier selection to write to; its scores may be ``scores``.  A beam whose
         score or logits are NaN or +infinity is reported and has no candidates."""
         a = self._select_args
-        if len(logits.shape) != 3 or logits.shape[1] != self.beams or logits.shape[2] != self.vocab or (
-                logits.dtype is not self.dtype) or logits.get_device() != self._index or (logits.stride(2) != 1 and self.vocab > 1):
+        sh, st = logits.shape, logits.stride()
+        if len(sh) != 3 or sh[1] != self.beams or sh[2] != self.vocab or logits.dtype is not self.dtype or (
+                logits.get_device() != self._index) or (st[2] != 1 and self.vocab > 1):
             raise ValueError(f"logits must be {self.dtype} [requests, {self.beams}, {self.vocab}] on {self.device}, rows contiguous")
-        R = logits.shape[0]
+        R = sh[0]
         shape, i32, f32 = (R, self.beams), torch.int32, torch.float32
         a.logits = logits.data_ptr()
-        a.request_stride, a.beam_stride, _ = logits.stride()
+        a.request_stride, a.beam_stride = st[0], st[1]
         a.scores = self._of(scores, f32, shape, "scores")
         if out is None:
             made = lambda dtype: B._made(shape, dtype, self.device, stream)  # noqa: E731
@@ -122,14 +123,15 @@ class BeamSearch(Handle):
         after ``lengths[r, h]`` steps (None: all), and is -1 from there on."""
         a = self._trace_args
         i32 = torch.int32
-        if len(tokens.shape) != 3 or tokens.shape[2] != self.beams or len(beams.shape) != 2 or beams.shape[0] != tokens.shape[1]:
+        sh, of = tokens.shape, beams.shape
+        if len(sh) != 3 or sh[2] != self.beams or len(of) != 2 or of[0] != sh[1]:
             raise ValueError(f"tokens must be [steps, requests, {self.beams}], beams [requests, hypotheses]")
-        T, R, _ = tokens.shape
-        N = beams.shape[1]
-        a.tokens = self._of(tokens, i32, tokens.shape, "tokens")
-        a.parents = self._of(parents, i32, tokens.shape, "parents")
-        a.beams_of = self._of(beams, i32, (R, N), "beams")
-        a.lengths = None if lengths is None else self._of(lengths, i32, (R, N), "lengths")
+        T, R, _ = sh
+        N = of[1]
+        a.tokens = self._of(tokens, i32, sh, "tokens")
+        a.parents = self._of(parents, i32, sh, "parents")
+        a.beams_of = self._of(beams, i32, of, "beams")
+        a.lengths = None if lengths is None else self._of(lengths, i32, of, "lengths")
         if out is None:
             out = B._made((R, N, T), i32, self.device, stream)
         a.out = self._of(out, i32, (R, N, T), "out")

@@ -64,6 +64,7 @@ struct Args {
   int32_t parts;    // of a row
   int32_t slots;    // lists of a row at most
   bool compact;     // rows of beams that are not there are left out
+  bool at_once;     // every part has a warp, which fetches before it knows whether the beam is there
 };
 
 // ---- elements ---------------------------------------------------------------------
@@ -452,20 +453,18 @@ struct Live {
   }
 };
 
-// A row of the list: which one it is, where it begins, and whether it is looked at.
+// A row of the list: which one it is, where it begins, and its score, which says whether
+// it is looked at.
 template <typename T>
 struct Open {
   const T* row;
   int i, shift;
-  bool live;
+  float score;  // looked at when it is needed: it may be on its way still
+  __device__ __forceinline__ bool live() const { return score - score == 0; }
   __device__ __forceinline__ void open(const Args& g, const Live& live_rows, int number, int lane) {
     i = g.compact ? live_rows.row(number, lane) : number;
     const int r = i / g.s.beams;
-    live = true;
-    if (!g.compact) {
-      const float c = g.a.scores[i];
-      live = c - c == 0;
-    }
+    score = g.compact ? 0.0f : g.a.scores[i];
     row = static_cast<const T*>(g.a.logits) + r * g.a.request_stride + (i - r * g.s.beams) * g.a.beam_stride;
     shift = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(T);
   }
@@ -549,11 +548,10 @@ __global__ void __launch_bounds__(kRoom, 1) k_select(const __grid_constant__ Arg
   int ahead = number, ahead_chunk = chunk;
   Open<T> from;
   from.open(g, sh.live, ahead, lane);
-  int row = from.i, shift = from.shift;
-  bool live = from.live;
+  Open<T> at = from;
   auto fetch = [&](int stage) {
     if (ahead < last_number || (ahead == last_number && ahead_chunk < last_end)) {
-      if (from.live) fetch_chunk(ring + stage * kSlot, from.row, from.shift, ahead_chunk, g.s.vocab, lane);
+      if (g.at_once || from.live()) fetch_chunk(ring + stage * kSlot, from.row, from.shift, ahead_chunk, g.s.vocab, lane);
       if (++ahead_chunk == g.chunks) {
         ahead_chunk = 0;
         if (++ahead <= last_number) from.open(g, sh.live, ahead, lane);
@@ -574,35 +572,33 @@ __global__ void __launch_bounds__(kRoom, 1) k_select(const __grid_constant__ Arg
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
     __syncwarp();  // the lanes' copies are there, and all have read the slot that is filled next
     uint4 v[kVecs];
-    take_run<T>(ring + stage * kSlot, shift, lane, v);
+    take_run<T>(ring + stage * kSlot, at.shift, lane, v);
     fetch(stage == 0 ? kStages - 1 : stage - 1);
     stage = stage == kStages - 1 ? 0 : stage + 1;
-    if (live) scan.chunk(g, v, chunk);
+    if (at.live()) scan.chunk(g, v, chunk);
     if (++chunk < stop) continue;
     // the end of a part
-    if (live) {
+    if (at.live()) {
       const float most = warp_max(scan.most);
       const bool bad = __any_sync(kAll, !(scan.most < INFINITY));
       const float scaled = scan.sum.R == -INFINITY ? 0.0f : scan.sum.sum * pskv::ex2(scan.sum.R - exponent_of(most));
       const uint64_t sum = warp_sum(__float2ull_rn(scaled * 0x1p32f));
-      if (lane == 0) g.s.parts[(int64_t)row * g.parts + (chunk - 1) / g.size] = Part{sum, most, bad};
+      if (lane == 0) g.s.parts[(int64_t)at.i * g.parts + (chunk - 1) / g.size] = Part{sum, most, bad};
       scan.begin_part();
     }
     stop = min(chunk + g.size, g.chunks);
     if (chunk < g.chunks && !(number == last_number && chunk == last_end)) continue;
     // the end of the warp's share of the row
-    if (live) {
+    if (at.live()) {
       while (scan.best.queued > 0) scan.best.flush();
-      if (lane < B) g.s.keys[((int64_t)row * g.slots + slot) * B + lane] = scan.best.list;
-      if (lane == 0 && chunk == g.chunks) g.s.lists[row] = slot + 1;
+      if (lane < B) g.s.keys[((int64_t)at.i * g.slots + slot) * B + lane] = scan.best.list;
+      if (lane == 0 && chunk == g.chunks) g.s.lists[at.i] = slot + 1;
     }
     if (number == last_number) break;
     ++number;
     chunk = slot = 0;
     stop = min(g.size, g.chunks);
-    Open<T> next;
-    next.open(g, sh.live, number, lane);
-    row = next.i, shift = next.shift, live = next.live;
+    at.open(g, sh.live, number, lane);
     scan.begin_row(g);
   }
 }
@@ -926,6 +922,7 @@ int32_t launch_select(const Search& s, const ps_beam_select_t& a, int32_t* statu
   g.size = (g.chunks + kRowParts - 1) / kRowParts;
   g.parts = (g.chunks + g.size - 1) / g.size;
   const int64_t U = g.rows * g.parts, grid = U < nsm ? U : nsm, C = U < grid * kWarps ? U : grid * kWarps;
+  g.at_once = U == C;
   // where every part has a warp there is nothing to gain
   g.compact = U > C && g.rows <= 32 * kRowWords;
   const int64_t slots = g.compact ? g.parts : g.parts / (U / C) + 2;

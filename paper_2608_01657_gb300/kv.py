@@ -192,8 +192,10 @@ class KVPool(Handle):
         return p
 
     def _table(self, t, name: str):
-        if len(t.shape) != 2 or t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
+        sh = t.shape
+        if len(sh) != 2 or t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 [rows, pages] tensor")
+        return sh
 
     # -- one layer's new tokens ----------------------------------------------
     def append(self, layer: int, q, k, v, slots, positions=None, rope=None, interleaved: bool = False, q_weight=None,
@@ -354,9 +356,9 @@ class KVPool(Handle):
 
     def _rows(self, tables, lens, held):
         """Fills in the structure of the rows; returns the reference to pass."""
-        self._table(tables, "tables")
+        n, width = self._table(tables, "tables")
         r = self._rows_args
-        r.num_rows, r.table_stride = n, _ = tables.shape
+        r.num_rows, r.table_stride = n, width
         r.tables = tables.data_ptr()
         r.lens = None if lens is None else self._array(lens, torch.int32, "lens", n)
         r.held = self._array(held, torch.int32, "held", n)
@@ -386,9 +388,10 @@ class KVPool(Handle):
         pages for ``grow`` more tokens than those have.  Full pages are shared, a
         beam's first continuation takes over its partly filled page, the others
         copy it; what no beam continues is freed."""
-        if len(rows.shape) != 2 or rows.shape != parents.shape:
+        sh = rows.shape
+        if len(sh) != 2 or sh != parents.shape:
             raise ValueError("rows and parents must be [requests, beams]")
-        (n, beams), raw = rows.shape, self._stream(stream)
+        (n, beams), raw = sh, self._stream(stream)
         for t, name in ((rows, "rows"), (parents, "parents")):
             if t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 [requests, beams] tensor")
