@@ -187,6 +187,7 @@ constexpr int kOneByOne = 8;
 __device__ __forceinline__ uint64_t greatest_of(uint64_t a, uint64_t b, int keep, int lane) {
   if (keep > kOneByOne) return merge32(sort32(a, lane), sort32(b, lane), lane);
   uint64_t out = 0;
+#pragma unroll 1
   for (int k = 0; k < keep; ++k) {
     const uint64_t m = a > b ? a : b;
     const uint32_t hi = __reduce_max_sync(kAll, (uint32_t)(m >> 32));
@@ -203,11 +204,13 @@ __device__ __forceinline__ uint32_t kth_of(uint32_t x, int keep, int lane) {
   x = (x & ~31u) | lane;  // no two are equal
   uint32_t end = 0;
   if (keep <= 16) {
+#pragma unroll 1
     for (int k = 0; k < keep; ++k) {
       end = __reduce_max_sync(kAll, x);
       if (x == end) x = 0;
     }
   } else {  // from the other side
+#pragma unroll 1
     for (int k = 32; k >= keep; --k) {
       end = __reduce_min_sync(kAll, x);
       if (x == end) x = ~0u;
