@@ -28,10 +28,10 @@
 // added up as whole numbers of 2^-32.  They are those of exp((x - R / a) a ln 2): the
 // exponents are off by a ln 2 - 1 = 1.3e-8 of their size.  Scores are added in 64 bits.
 //
-// 128 requests of 8 beams and 131072 tokens in bf16, 268 MB, take 57 us: 51 for k_select,
-// which reads 5.2 TB/s at 58 % of the issue slots (41 us with the loads alone), and 6 for
-// k_select_join.  64 x 8 in 32 bits take 56; 131071 tokens, whose rows begin anywhere in a
-// word, 64; 256 single rows 23; 32 x 32 beams 67.  Few rows are a chain of dependent
+// 128 requests of 8 beams and 131072 tokens in bf16, 268 MB, take 56 us: 50 for k_select,
+// which reads 5.3 TB/s at 58 % of the issue slots (45 us with the loads alone, 2 less without
+// the queues, no less without the exponentials), and 6 for k_select_join.  64 x 8 in 32 bits take 56; 131071 tokens, whose rows begin anywhere in a
+// word, 64; 256 single rows 23; 32 x 32 beams 66.  Few rows are a chain of dependent
 // steps: 7.5 for one row of 1000 tokens, 9.6 for 8 x 4 of 65536.
 #include "ps_beam.cuh"
 
