@@ -107,9 +107,11 @@ class Search:
 @pytest.mark.parametrize("requests,beams,most,ps,layout,dtype,dim", [
     (1, 1, 40, 16, "token", BF, 64), (1, 4, 100, 16, "token", BF, 64), (3, 5, 60, 8, "head", HF, 80), (7, 2, 90, 2, "both", BF, 8),
     (2, 32, 70, 16, "token", HF, 128), (5, 8, 300, 64, "head", BF, 40)])
-def test_beam_steps(requests, beams, most, ps, layout, dtype, dim):
-    """Steps in a row: identity, permutations, one winner, random, ends, and none left."""
-    s = Search(requests, beams, most, ps, pages=7000 if ps == 2 else 2500, layout=layout, dtype=dtype, dim=dim, seed=beams)
+@pytest.mark.parametrize("large", [True, False])
+def test_beam_steps(requests, beams, most, ps, layout, dtype, dim, large):
+    """Steps in a row: identity, permutations, one winner, random, ends, and none left; references of one chunk and of more."""
+    s = Search(requests, beams, most, ps, pages=(7000 if ps == 2 else 2500) if large else 2000, layout=layout, dtype=dtype, dim=dim,
+               seed=beams)
     every = np.tile(np.arange(beams), (requests, 1))
     s.step(every, grow=0)
     s.step(every[:, ::-1], out_of_place=True)
