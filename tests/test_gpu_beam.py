@@ -272,6 +272,29 @@ def test_a_large_batch_and_small_rows():
         check(x[rows], s[rows], [3], type(got)(*(t[rows] for t in got)))
 
 
+@pytest.mark.parametrize("R", [1024, 1100])
+def test_absent_beams_of_large_batches(R):
+    """Up to 4096 rows, of which those that are not there are left out, and more, of which they are passed over."""
+    B, V = 4, 5000
+    x, s = make(R, B, V, BF, seed=R)
+    g = torch.Generator("cuda").manual_seed(R)
+    gone = torch.rand(R, B, generator=g, device="cuda") < 0.6
+    gone[:3] = True
+    gone[-2:, 1:] = True
+    s[gone] = -math.inf
+    x[gone] = math.nan
+    h = search(R, B, V, BF, [7])
+    got = h.select(x, s)
+    h.check()
+    assert (got.tokens[:3] == -1).all()
+    rows = [0, 1, 2, R - 2, R - 1] + list(range(3, R, R // 30))
+    check(x[rows], s[rows], [7], type(got)(*(t[rows] for t in got)))
+    s[:] = -math.inf
+    got = h.select(x, s)
+    h.check()
+    assert (got.tokens == -1).all() and (got.ended_parents == -1).all() and (got.scores == -math.inf).all()
+
+
 def test_scores_in_place_and_outputs_reused():
     x, s = make(5, 4, 9000, BF, seed=8)
     h = search(5, 4, 9000, BF, [2])
