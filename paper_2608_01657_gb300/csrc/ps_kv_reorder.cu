@@ -93,17 +93,15 @@ __global__ void __launch_bounds__(kScanThreads) k_reorder_scan(Pool p, PageScrat
           const int q = q0 + u;
           if (ids[u] == kNoPage && (q >= B || k >= s_held[q])) continue;
           const int c = s_children[q], d = k < s_len[q] >> p.page_log2 ? c - 1 : (c > 0 ? 0 : -1);
+          if (id < 0 || id >= p.num_pages || held[u] <= 0) {  // (looked at first: -1 may be a row's id, too)
+            ok = false;
+            continue;
+          }
           if (id == at) {
             change += d;
             continue;
           }
           if (change != 0 && at >= p.first_page) atomicAdd(o.delta + (at - p.first_page), change);
-          at = -1;
-          change = 0;
-          if (id < 0 || id >= p.num_pages || held[u] <= 0) {
-            ok = false;
-            continue;
-          }
           at = id;
           change = d;
         }

@@ -284,3 +284,37 @@ def test_reorder_on_another_stream():
     s.pool.check()
     s.plain(p, 1)
     s.same()
+
+
+@pytest.mark.parametrize("name", [-1, -2, 12])
+@pytest.mark.parametrize("where", ["first beam", "second beam", "all beams", "after another", "one beam"])
+def test_impossible_ids_change_nothing(where, name):
+    """In whole pages' columns, whose ids no copy uses; -1, the usual filler of tables, among them."""
+    pool, k, (t, l, h, r) = small()
+    rows, parents = ([[0], [1], [2], [3]], [[0]] * 4) if where == "one beam" else ([[0, 1], [2, 3]], [[0, 0], [1, 0]])
+    at = {"first beam": (0, 0), "second beam": (1, 0), "all beams": (slice(0, 2), 1), "after another": (slice(2, 4), 0), "one beam": (3, 1)}[where]
+    t[at] = name
+    if where == "after another":   # the beams' ids differ, so that each is looked at
+        t[2, 0] = -1 if name != -1 else 13
+    state = [x.clone() for x in (t, l, h, r, k)]
+    out = torch.full_like(r, 9)
+    pool.reorder(dev(rows), dev(parents), t, l, h, r, refs_out=out)
+    with pytest.raises(RuntimeError, match="invalid"):
+        pool.check()
+    assert all(torch.equal(a, b) for a, b in zip(state, (t, l, h, r, k))) and torch.equal(out, r)
+    # and the changes that were found by then are forgotten
+    t, l, h, r = small()[2]
+    pool.reorder(dev([[0, 1], [2, 3]]), dev([[0, 0], [1, 0]]), t, l, h, r)
+    pool.check()
+    assert r.tolist() == [2, 2, 1, 1, 1, 1, 1, 0, 0, 0]
+
+
+def test_an_impossible_id_of_a_partly_filled_page_is_not_copied():
+    """A row that claims a page more than it has: the id past its own is the filler."""
+    pool, k, (t, l, h, r) = small()
+    t[:, 3], l[0], h[0] = -1, 50, 4
+    state = [x.clone() for x in (t, l, h, r, k)]
+    pool.reorder(dev([[0, 1], [2, 3]]), dev([[0, 0], [1, 0]]), t, l, h, r)
+    with pytest.raises(RuntimeError, match="invalid"):
+        pool.check()
+    assert all(torch.equal(a, b) for a, b in zip(state, (t, l, h, r, k)))
