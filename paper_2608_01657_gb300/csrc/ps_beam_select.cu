@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kRoom, 1) k_select(const __grid_constant__ Arg
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         const unsigned m = __ballot_sync(kAll, c[u] - c[u] == 0);
-        if (lane == 0) sh.live.bits[i0 + u * kWarps] = m;
+        if (lane == 0 && i0 + u * kWarps < kRowWords) sh.live.bits[i0 + u * kWarps] = m;
       }
       if (i0 + kWarps * kAtOnce - warp >= words) {  // no rows behind these
         for (int i = i0 + kWarps * kAtOnce + lane * kWarps; i < kRowWords; i += 32 * kWarps) sh.live.bits[i] = 0;

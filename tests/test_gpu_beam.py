@@ -295,6 +295,30 @@ def test_absent_beams_of_large_batches(R):
     assert (got.tokens == -1).all() and (got.ended_parents == -1).all() and (got.scores == -math.inf).all()
 
 
+@pytest.mark.parametrize("R", [31, 65, 3001, 3103, 3777, 4095])
+def test_absent_rows_at_every_word_of_the_list(R):
+    """Every row has a continuation of its own, so that a row that is taken for another one shows; single rows, up to
+    the most of which absent ones are left out, and few of long rows."""
+    V = 5000 if R > 100 else 300001
+    g = torch.Generator("cuda").manual_seed(R)
+    x = torch.zeros(R, 1, V, device="cuda", dtype=BF)
+    at = torch.randint(0, V, (R,), generator=g, device="cuda")
+    x[torch.arange(R, device="cuda"), 0, at] = 20.0
+    s = -torch.rand(R, 1, generator=g, device="cuda")
+    for share in (0.0, 0.3, 0.97):
+        gone = torch.rand(R, generator=g, device="cuda") < share
+        gone[-1] = False
+        c = torch.where(gone[:, None], -math.inf, s)
+        h = search(R, 1, V, BF)
+        got = h.select(x, c)
+        h.check()
+        assert torch.equal(got.tokens[:, 0], torch.where(gone, -1, at).int()) and torch.equal(got.parents[:, 0], -gone.int())
+        check(x[-3:], c[-3:], (), type(got)(*(t[-3:] for t in got)))
+        assert (got.scores[gone] == -math.inf).all() and (got.ended_tokens == -1).all()
+        want = s[:, 0].double() - math.log1p((V - 1) * math.exp(-20))
+        assert (got.scores[:, 0].double() - want)[~gone].abs().max() <= float(bound(want, V).max())
+
+
 def test_scores_in_place_and_outputs_reused():
     x, s = make(5, 4, 9000, BF, seed=8)
     h = search(5, 4, 9000, BF, [2])
