@@ -77,15 +77,18 @@ class Server:
 
     # -- one pass over all layers ------------------------------------------------
     def forward(self, rows: torch.Tensor, start: torch.Tensor, tokens: torch.Tensor, counts: Sequence[int],
-                groups: Optional[Sequence[int]] = None, written: Optional[torch.Tensor] = None) -> torch.Tensor:
+                groups: Optional[Sequence[int]] = None, write: Optional[torch.Tensor] = None,
+                written: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Hidden states of ``counts[i]`` new tokens of each row, from position ``start[i]`` on.
 
         ``groups``: first rows of the runs that may share a prefix, and the number of rows (None: those
-        that their pages show).  ``written``: how many of a row's tokens have their keys and values."""
+        that their pages show).  Keys and values are written but for tokens where ``write`` [tokens] is False,
+        and for those below ``written`` [rows], how many of a row's tokens have theirs."""
         s, w = self.s, self.layers
         T = int(sum(counts))
-        at = self.pool.layout(rows, self.tables, self.lens, self.held, T,
-                              counts=torch.tensor(counts, dtype=torch.int32, device="cuda"), starts=start.int(), written=written)
+        at = self.pool.layout(rows.int().contiguous(), self.tables, self.lens, self.held, T,
+                              counts=torch.tensor(counts, dtype=torch.int32, device="cuda"), starts=start.int().contiguous(), written=written)
+        slots = at.slots if write is None else torch.where(write, at.slots, -1)
         bounds = at.group_offsets if groups is None else torch.tensor(groups, dtype=torch.int32, device="cuda")
         self.pool.plan(at.q_offsets, at.kv_lens, at.tables, T, group_offsets=bounds)
         x = w.embed[tokens.long()]
@@ -93,7 +96,7 @@ class Server:
         for layer in range(s.layers):
             qkv = x @ w.qkv[layer].T
             q, k, v = (t.unflatten(1, (-1, s.head_dim)) for t in (qkv[:, :a], qkv[:, a:b], qkv[:, b:]))
-            q = self.pool.append(layer, q, k, v, at.slots, positions=at.positions, rope=w.rope, q_weight=w.q_norm[layer],
+            q = self.pool.append(layer, q, k, v, slots, positions=at.positions, rope=w.rope, q_weight=w.q_norm[layer],
                                  k_weight=w.k_norm[layer])
             o = self.pool.attention(layer, q, s.head_dim ** -0.5)
             x = x + o.flatten(1) @ w.out[layer].T

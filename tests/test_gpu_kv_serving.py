@@ -104,3 +104,40 @@ def test_no_batch_is_admitted_while_rows_name_cached_pages():
     server.finish(range(3))
     server.admit(groups, prompts, room=0)   # the same again
     assert near(server.sample(3, 2, steps), before)
+
+
+def test_tokens_that_are_not_written():
+    """A mask of tokens, after the groups, as a keyword, or as a number for each row; rows and starts of any kind."""
+    from paper_2608_01657_gb300 import serving as S
+    s = S.Shape()
+    server = S.Server(s, groups=2, seed=4)
+    groups, n = [0, 0, 1], 3
+    prompts = S.prompts_of(groups, s, 4)
+    server.admit(groups, prompts, room=8)
+    rows = torch.arange(n, device="cuda")
+    start = server.lens[:n].long().repeat_interleave(2)[::2]          # 64 bits, with strides
+    counts = [2, 1, 3]
+    tokens = torch.arange(sum(counts), device="cuda")
+    k, v = server.k.clone(), server.v.clone()
+    want = server.forward(rows, start, tokens, counts, [0, n])         # all are written
+    full = server.k.clone()
+    places = [(int(server.tables[i, (int(start[i]) + j) // s.page]), (int(start[i]) + j) % s.page) for i in range(n) for j in range(counts[i])]
+    for at, off in places:
+        assert not torch.equal(full[:, at, off], k[:, at, off])
+    write = torch.tensor([True, False, True, False, False, True], device="cuda")
+    for kind in ("place", "keyword", "rows", "both"):
+        server.k.copy_(k), server.v.copy_(v)
+        keep = write.tolist()
+        if kind == "place":
+            server.forward(rows, start, tokens, counts, [0, n], write)
+        elif kind == "keyword":
+            server.forward(rows.int(), start.int(), tokens, counts, write=write)
+        else:
+            written = (start + torch.tensor([1, 0, 2], device="cuda")).int()
+            server.forward(rows, start, tokens, counts, [0, n], write if kind == "both" else None, written)
+            keep = [False, True, True, False, False, True]
+            keep = [a and b for a, b in zip(keep, write.tolist())] if kind == "both" else keep
+        for (at, off), kept in zip(places, keep):
+            assert torch.equal(server.k[:1, at, off], (full if kept else k)[:1, at, off]), kind
+    server.k.copy_(k), server.v.copy_(v)
+    assert torch.equal(server.forward(rows, start, tokens, counts, [0, n], torch.ones_like(write)), want)
