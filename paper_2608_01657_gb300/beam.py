@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from . import binding as B
-from .kv import Handle, _addresses, _need
+from .kv import Handle, _addresses, _fit, _need
 
 _DTYPES = {torch.bfloat16: B.PS_BEAM_BF16, torch.float16: B.PS_BEAM_F16, torch.float32: B.PS_BEAM_F32}
 
@@ -51,6 +51,7 @@ class BeamSearch(Handle):
         _need(len(end_tokens) <= B.PS_BEAM_MAX_END, f"at most {B.PS_BEAM_MAX_END} end tokens")
         self.max_requests, self.beams, self.vocab, self.dtype = int(max_requests), int(beams), int(vocab), dtype
         self.end_tokens = tuple(end_tokens)
+        _fit("beam search", self.max_requests, self.beams, self.vocab, *end_tokens)
         self.device = torch.device("cuda", torch.cuda.current_device())
         c = B.PsBeamConfig(max_requests=self.max_requests, beams=self.beams, vocab=self.vocab, dtype=_DTYPES[dtype],
                            num_end=len(end_tokens))
@@ -89,6 +90,8 @@ class BeamSearch(Handle):
                 logits.get_device() != self._index) or (st[2] != 1 and self.vocab > 1):
             raise ValueError(f"logits must be {self.dtype} [requests, {self.beams}, {self.vocab}] on {self.device}, rows contiguous")
         R = sh[0]
+        if R >> 31:
+            _fit("select", R)
         shape, i32, f32 = (R, self.beams), torch.int32, torch.float32
         a.logits = logits.data_ptr()
         a.request_stride, a.beam_stride = st[0], st[1]
@@ -128,6 +131,8 @@ class BeamSearch(Handle):
             raise ValueError(f"tokens must be [steps, requests, {self.beams}], beams [requests, hypotheses]")
         T, R, _ = sh
         N = of[1]
+        if T >> 31 or R >> 31 or N >> 31:
+            _fit("trace", T, R, N)
         a.tokens = self._of(tokens, i32, sh, "tokens")
         a.parents = self._of(parents, i32, sh, "parents")
         a.beams_of = self._of(beams, i32, of, "beams")

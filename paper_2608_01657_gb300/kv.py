@@ -31,6 +31,13 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _fit(name: str, *sizes: int):
+    """The library's sizes have 32 bits, and what is greater would come to it as another number."""
+    for n in sizes:
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"{name}: {n} is out of range")
+
+
 class Handle:
     """What the wrappers of the library's handles share: ``status`` (a sticky int32
     word of the device's errors), the streams that the handle's memory is used on,
@@ -256,6 +263,8 @@ class KVPool(Handle):
         width = self._rows_args.table_stride
         n = tables.shape[0] if rows is None else rows.shape[0]
         T, all_ = int(num_tokens), n + bool(pad)
+        if T >> 31 or n >> 31:
+            _fit("layout", n, T)
         i32 = torch.int32
         a.rows = None if rows is None else self._array(rows, i32, "rows")
         a.counts = None if counts is None else self._array(counts, i32, "counts", n)
@@ -392,6 +401,7 @@ class KVPool(Handle):
         if len(sh) != 2 or sh != parents.shape:
             raise ValueError("rows and parents must be [requests, beams]")
         (n, beams), raw = sh, self._stream(stream)
+        _fit("reorder", n, beams, grow)
         for t, name in ((rows, "rows"), (parents, "parents")):
             if t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 [requests, beams] tensor")

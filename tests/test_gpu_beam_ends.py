@@ -1,4 +1,4 @@
-"""What lies past a selection's candidates: every entry of every output, written over what was there before."""
+"""What lies past a selection's candidates: every entry of every output, written over what was there before; and sizes past 32 bits."""
 import math
 
 import numpy as np
@@ -82,3 +82,27 @@ def test_beams_that_are_not_finite(B):
     strict(x, s, end, got)
     none = np.array([0, 2])
     assert (got.tokens[none] == -1).all() and (got.ended_tokens[none] == -1).all()
+
+
+def test_sizes_of_more_than_32_bits_are_refused():
+    """The library's numbers have 32 bits: 2^32 + 7 is not token 7."""
+    from paper_2608_01657_gb300 import kv
+    far = 1 << 32
+    for bad in (dict(end_tokens=[far + 7]), dict(end_tokens=[1, far + 1]), dict(vocab=far + 100), dict(beams=far + 3), dict(max_requests=far + 2),
+                dict(end_tokens=[7 - far])):
+        with pytest.raises(ValueError, match="out of range"):
+            search(**(dict(max_requests=2, beams=3, vocab=100) | bad))
+    h = search(2, 3, 100)
+    z = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    for steps, requests, hyps in ((far + 1, 0, 1), (1, 0, far + 1)):
+        with pytest.raises(ValueError, match="out of range"):
+            h.trace(z(steps, requests, 3), z(steps, requests, 3), z(requests, hyps))
+    k = torch.zeros(1, 8, 16, 1, 8, device="cuda", dtype=BF)
+    pool = kv.KVPool(k, k.clone(), num_q_heads=1, max_requests=2, max_tokens=8, max_row_pages=2)
+    tables, lens, held, refs = z(2, 2), z(2), z(2), z(8)
+    with pytest.raises(ValueError, match="out of range"):
+        pool.layout(z(1), tables, lens, held, far + 1)
+    with pytest.raises(ValueError, match="out of range"):
+        pool.reorder(z(1, 1), z(1, 1), tables, lens, held, refs, grow=far)
+    assert not held.any()
+    pool.check()
