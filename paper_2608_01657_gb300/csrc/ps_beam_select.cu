@@ -34,9 +34,11 @@
 //
 // 128 requests of 8 beams and 131072 tokens in bf16, 268 MB, take 56 us: 50 for k_select,
 // which reads 5.3 TB/s at 58 % of the issue slots (45 us with the loads alone, 2 less without
-// the queues, no less without the exponentials), and 6 for k_select_join.  64 x 8 in 32 bits take 56; 131071 tokens, whose rows begin anywhere in a
-// word, 64; 256 single rows 23; 32 x 32 beams 66.  Few rows are a chain of dependent
-// steps: 7.5 for one row of 1000 tokens, 9.6 for 8 x 4 of 65536.
+// the queues, no less without the exponentials), and 6 for k_select_join.  So they do in
+// f16; 64 x 8 in 32 bits take 55; 131071 tokens, whose rows begin anywhere in a word, 65;
+// 64000 tokens 39 (parts of two chunks in place of one: 37, but odd ones longer); 256 single
+// rows 22, of which the list of the rows that are there is 1.3; 32 x 32 beams 66.  Few rows
+// are a chain of dependent steps: 8 for one row of 1000 tokens, 9.5 for 8 x 4 of 65536.
 #include "ps_beam.cuh"
 
 namespace psbeam {

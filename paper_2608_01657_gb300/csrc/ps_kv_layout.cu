@@ -14,10 +14,12 @@
 // Each read of the chain is 0.6 to 0.8 us from L2, a launch 2 to 3: decoding 256
 // requests of up to 4096 tokens takes 4.3 us, the prompts of 64 requests (49,000
 // tokens) 3.8, drafted tokens of 333 requests, padded, 4.7, and two kernels for 3000
-// decoding requests 14.  The runs of requests that share a prefix cost nothing beside
+// decoding requests 14, whose 4.8 MB need 0.7.  The runs of requests that share a prefix cost nothing beside
 // the tables, as CTA 0 compares the ids while the others fill: a thread one of the
 // leading ids of neighbouring requests, 8 or 24 of them side by side (a pair of ids a
-// thread, 8 at a time, took 2.4 us longer for the drafted tokens).  A lane's four
+// thread, 8 at a time, took 2.4 us longer for the drafted tokens; 8 ids alone, whatever
+// their number, take 0.2 longer there and 1.5 for 1000 prompts, 24 alone 0.2 for decoding
+// and 0.8 for 1000 requests of drafted tokens).  A lane's four
 // tokens go through each read together.  8 CTAs an SM in place of 4 took 1 us longer
 // for 3000 requests: each reads all offsets.
 #include "ps_kv_pages.cuh"
